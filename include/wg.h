@@ -349,6 +349,32 @@ int wg_decode_step(wg_handle_t h, wg_state_t *d_states, const int32_t *d_tokens,
  * wg_vocab_create) are not part of the cache. */
 int wg_cache_clear(wg_handle_t h, void *stream);
 
+/* ---- beam search under the mask ------------------------------------------------------------
+ * wg_beam_select: one step of beam search over rows / beams requests, a request's `beams` beams in adjacent rows.  With x the
+ * allowed logits of a row (d_bitmask as in wg_apply_mask; NULL: every token is allowed), a continuation by token v scores
+ *     d_scores[row] + x_v - log(sum over the row's allowed tokens of exp(x)),
+ * the log-probability under the mask added to the beam's own: what masking the logits and a softmax give.  (A state that allows
+ * one token, as FINAL allows the end of sequence, adds 0: a finished hypothesis keeps its score.)  A request's rows receive its
+ * `beams` best continuations, best first: d_scores_out, the row that it continues (d_parents), its token (d_tokens) and that row's
+ * state (d_states_out <- d_states[parent]; both NULL for none).  Equal scores go to the lower beam; within a beam the larger logit is
+ * the better one, equal logits (-0.0 equals +0.0) the lower token.  A NaN or -inf logit is no continuation and not in the sum, +inf counts as
+ * the largest number; a row whose score is NaN or -inf has no continuations (before the first step, all beams of a request but
+ * one).  Rows that nothing is left for get a score of -inf, parent and token -1 and the state {WG_SID_ERROR, 0}.  Sums and scores are
+ * fp32.  1 <= beams <= 64, rows a multiple of it and at most 65535.  d_workspace: wg_beam_select_workspace(rows, V, beams) bytes of device
+ * memory, 8-byte aligned, overwritten; calls that share it must not overlap.  No output is one of the inputs.  Two kernels,
+ * nothing is allocated; arguments outside these limits give WG_ERR_INVALID and launch nothing. */
+uint64_t wg_beam_select_workspace(uint32_t rows, uint32_t V, uint32_t beams);
+int wg_beam_select(const void *d_logits, wg_dtype_t dtype, uint32_t rows, uint32_t V, int64_t row_stride_elems,
+                   const uint32_t *d_bitmask, uint32_t beams, const float *d_scores, const wg_state_t *d_states,
+                   float *d_scores_out, int32_t *d_parents, int32_t *d_tokens, wg_state_t *d_states_out,
+                   void *d_workspace, uint64_t workspace_bytes, void *stream);
+
+/* wg_reorder_rows: what else follows the parents (token histories, recurrent states): row r of each of `outer` arrays of `rows` rows
+ * <- row d_parents[r] of d_src, or zeros where that is not a row.  Strides are in bytes, those of rows at least row_bytes; d_src
+ * and d_dst must not overlap.  One kernel. */
+int wg_reorder_rows(const void *d_src, void *d_dst, const int32_t *d_parents, uint32_t outer, uint32_t rows, uint64_t row_bytes,
+                    int64_t src_outer_bytes, int64_t src_row_bytes, int64_t dst_outer_bytes, int64_t dst_row_bytes, void *stream);
+
 /* ---- introspection (these synchronise the device) ---------------------------------------- */
 /* (Counters are read in two small copies, whatever the number of keys; rows_in_use is counted by a launch while
  * the cache has a row for every key.) */

@@ -64,6 +64,7 @@ EXPORTS = [
     "wg_table_num_instances", "wg_advance_fill_masks", "wg_regex_to_template",
     "wg_decode_step", "wg_masked_topk", "wg_masked_topk_workspace", "wg_reserve_batch", "wg_max_batch", "wg_set_scan_batch",
     "wg_masked_topk_static", "wg_masked_topk_static_capacity", "wg_profile_apply_mask", "wg_forced_bytes",
+    "wg_beam_select", "wg_beam_select_workspace", "wg_reorder_rows",
 ]
 
 
@@ -127,6 +128,10 @@ def load_library():
     L.wg_masked_topk_static_capacity.restype = u64
     L.wg_masked_topk_static.argtypes = [vp, C.c_int, u32, u32, i64, vp, u32, vp, vp, vp]
     L.wg_forced_bytes.argtypes = [vp, vp, u32, u32, vp, vp, vp, vp]
+    L.wg_beam_select_workspace.argtypes = [u32, u32, u32]
+    L.wg_beam_select_workspace.restype = u64
+    L.wg_beam_select.argtypes = [vp, C.c_int, u32, u32, i64, vp, u32, vp, vp, vp, vp, vp, vp, vp, u64, vp]
+    L.wg_reorder_rows.argtypes = [vp, vp, vp, u32, u32, u64, i64, i64, i64, i64, vp]
     L.wg_cache_clear.argtypes = [vp, vp]
     L.wg_cache_stats.argtypes = [vp, C.POINTER(_Stats)]
     L.wg_error_count.argtypes = [vp, C.POINTER(u64)]
@@ -432,3 +437,20 @@ def masked_topk_static(logits, bitmask, ids, values, stream=None):
 def select_tokens(bitmask, V, draws, tokens, stream=None):
     """wg_select_tokens: harness sampler stand-in."""
     (_native or _load_native()).select_tokens(bitmask, V, draws, tokens, stream)
+
+
+def beam_select_workspace(rows, V, beams):
+    """wg_beam_select_workspace: bytes of device workspace a beam_select call of this shape needs."""
+    return int(load_library().wg_beam_select_workspace(rows, V, beams))
+
+
+def beam_select(logits, bitmask, scores, states, beams, out_scores, parents, tokens, out_states, workspace, stream=None):
+    """wg_beam_select: logits [R, V] float32 or bfloat16, bitmask int32 [R, ceil(V/32)] or None, scores and out_scores
+    float32 [R], states and out_states int32 [R, 2] or both None, parents and tokens int32 [R]; R is a multiple of `beams`."""
+    (_native or _load_native()).beam_select(logits, bitmask, scores, states, beams, out_scores, parents, tokens, out_states, workspace, stream)
+
+
+def reorder_rows(src, parents, dst, axis=0, stream=None):
+    """wg_reorder_rows: dst <- the rows of src that parents (int32) names along `axis` (0, or 1 behind one leading dimension),
+    zeros where it names none.  src and dst agree in shape and type; each row lies in one piece."""
+    (_native or _load_native()).reorder_rows(src, parents, dst, axis, stream)

@@ -87,6 +87,17 @@ uint32_t *words(const at::Tensor &t) { return static_cast<uint32_t *>(t.data_ptr
 int32_t *ints(const at::Tensor &t) { return static_cast<int32_t *>(t.data_ptr()); }
 uint32_t rows(const at::Tensor &t) { return (uint32_t)t.size(0); }
 
+uint64_t bytes_of(const at::Tensor &t) { return (uint64_t)t.numel() * t.element_size(); }
+// A count that the C call takes in 32 bits.
+bool number(PyObject *o, uint32_t *out, const char *name) {
+    const unsigned long long x = PyLong_AsUnsignedLongLong(o);
+    if (PyErr_Occurred()) return false;
+    if (x > 0xFFFFFFFFull) return bad(PyExc_ValueError, std::string(name) + " is out of range");
+    *out = (uint32_t)x;
+    return true;
+}
+bool fits32(const at::Tensor &t, int64_t dim) { return t.size(dim) <= 0x7FFFFFFF || bad(PyExc_ValueError, "a dimension is out of range"); }
+
 // A [B, V] float32 or bfloat16 device tensor with unit inner stride.
 bool logits_ok(const at::Tensor &t, wg_dtype_t *dt, const char *what) {
     if (t.dim() != 2 || !t.is_cuda() || t.stride(1) != 1) return bad(PyExc_ValueError, what);
@@ -227,6 +238,59 @@ PyObject *select_tokens(PyObject *, PyObject *const *a, Py_ssize_t n) {
     }));
 }
 
+// beam_select(logits, bitmask or None, scores, states or None, beams, out_scores, parents, tokens, out_states or None, workspace, stream)
+PyObject *beam_select(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    const at::Tensor *lg, *bm = nullptr, *sc, *st = nullptr, *os, *pa, *tk, *so = nullptr, *ws; void *s; wg_dtype_t dt;
+    if (!count(n, 11) || !tensor(a[0], &lg, "logits") || (a[1] != Py_None && !tensor(a[1], &bm, "bitmask")) || !tensor(a[2], &sc, "scores") ||
+        (a[3] != Py_None && !tensor(a[3], &st, "states")) || !tensor(a[5], &os, "out_scores") || !tensor(a[6], &pa, "parents") ||
+        !tensor(a[7], &tk, "tokens") || (a[8] != Py_None && !tensor(a[8], &so, "out_states")) || !tensor(a[9], &ws, "workspace")) return nullptr;
+    uint32_t beams;
+    if (!number(a[4], &beams, "beams") || !logits_ok(*lg, &dt, "logits must be a 2-d device tensor with unit inner stride")) return nullptr;
+    const int64_t R = lg->size(0);
+    if (bm && !mask_fits(*lg, *bm)) { bad(PyExc_ValueError, "bitmask must be [R, ceil(V/32)]"); return nullptr; }
+    if (!shape1(*sc, R) || !shape1(*os, R) || !shape1(*pa, R) || !shape1(*tk, R) || (st && !shape2(*st, R, 2)) || (so && !shape2(*so, R, 2))) {
+        bad(PyExc_ValueError, "scores, out_scores, parents and tokens must be [R], states and out_states [R, 2]");
+        return nullptr;
+    }
+    if ((bm && !device(*bm, at::kInt, "bitmask")) || !device(*sc, at::kFloat, "scores") || (st && !device(*st, at::kInt, "states")) ||
+        !device(*os, at::kFloat, "out_scores") || !device(*pa, at::kInt, "parents") || !device(*tk, at::kInt, "tokens") ||
+        (so && !device(*so, at::kInt, "out_states")) || !device(*ws, ws->scalar_type(), "workspace") || !fits32(*lg, 1) || !stream_of(a[10], &s)) return nullptr;
+    return result(unlocked([=, logits = lg->data_ptr(), B = rows(*lg), V = (uint32_t)lg->size(1), stride = lg->stride(0), mask = bm ? words(*bm) : nullptr,
+                            scores = static_cast<const float *>(sc->data_ptr()), states = st ? states_ptr(*st) : nullptr, out = static_cast<float *>(os->data_ptr()),
+                            parents = ints(*pa), tokens = ints(*tk), ends = so ? states_ptr(*so) : nullptr, work = ws->data_ptr(), bytes = bytes_of(*ws)] {
+        return wg_beam_select(logits, dt, B, V, stride, mask, beams, scores, states, out, parents, tokens, ends, work, bytes, s);
+    }));
+}
+
+// reorder_rows(src, parents, dst, axis, stream)
+PyObject *reorder_rows(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    const at::Tensor *src, *pa, *dst; void *s; uint32_t axis;
+    if (!count(n, 5) || !tensor(a[0], &src, "src") || !tensor(a[1], &pa, "parents") || !tensor(a[2], &dst, "dst") || !number(a[3], &axis, "axis")) return nullptr;
+    if (axis > 1 || src->dim() <= (int64_t)axis || src->sizes() != dst->sizes() || src->scalar_type() != dst->scalar_type()) {
+        bad(PyExc_ValueError, "src and dst must agree in shape and dtype, axis must be 0 or 1 and one of their dimensions");
+        return nullptr;
+    }
+    if (!src->is_cuda() || !dst->is_cuda()) { bad(PyExc_ValueError, "src and dst must be device tensors"); return nullptr; }
+    if (!shape1(*pa, src->size(axis)) || !device(*pa, at::kInt, "parents")) {
+        if (!PyErr_Occurred()) bad(PyExc_ValueError, "parents must be [R]");
+        return nullptr;
+    }
+    const int64_t e = (int64_t)src->element_size();
+    int64_t inside = 1;
+    for (int64_t d = src->dim() - 1; d > (int64_t)axis; d--) {                     // each row lies in one piece
+        if (src->size(d) != 1 && (src->stride(d) != inside || dst->stride(d) != inside)) { bad(PyExc_ValueError, "each row must lie in one piece"); return nullptr; }
+        inside *= src->size(d);
+    }
+    if (!fits32(*src, axis) || (axis && !fits32(*src, 0)) || !stream_of(a[4], &s)) return nullptr;
+    const int64_t R = src->size(axis), outer = axis ? src->size(0) : 1;
+    // (the stride of a dimension of one is of no account)
+    auto row = [&](const at::Tensor &t) { return R > 1 ? t.stride(axis) * e : inside * e; };
+    auto whole = [&](const at::Tensor &t) { return axis && outer > 1 ? t.stride(0) * e : 0; };
+    return result(unlocked([=, from = src->data_ptr(), to = dst->data_ptr(), parents = ints(*pa), so = whole(*src), sr = row(*src), d_o = whole(*dst), dr = row(*dst)] {
+        return wg_reorder_rows(from, to, parents, (uint32_t)outer, (uint32_t)R, (uint64_t)(inside * e), so, sr, d_o, dr, s);
+    }));
+}
+
 // add_instances(handle, texts, args or None, starts address, its rows, stream): sequences of template texts and of
 // argument mappings.  The C call reads the strings in place and without the lock, when other threads may
 // change the caller's lists and dictionaries, and a conversion to bytes may run Python code that does:
@@ -309,7 +373,7 @@ PyObject *set_error(PyObject *, PyObject *cls) {
 
 #define FAST(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(guarded<name>)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {FAST(fill_masks), FAST(advance), FAST(advance_fill_masks), FAST(decode_step), FAST(forced_bytes), FAST(cache_clear),
-                         FAST(apply_mask), FAST(masked_argmax), FAST(masked_topk), FAST(select_tokens), FAST(add_instances),
+                         FAST(apply_mask), FAST(masked_argmax), FAST(masked_topk), FAST(select_tokens), FAST(add_instances), FAST(beam_select), FAST(reorder_rows),
                          {"set_error", set_error, METH_O, nullptr}, {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_native", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
