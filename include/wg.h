@@ -375,6 +375,63 @@ int wg_beam_select(const void *d_logits, wg_dtype_t dtype, uint32_t rows, uint32
 int wg_reorder_rows(const void *d_src, void *d_dst, const int32_t *d_parents, uint32_t outer, uint32_t rows, uint64_t row_bytes,
                     int64_t src_outer_bytes, int64_t src_row_bytes, int64_t dst_outer_bytes, int64_t dst_row_bytes, void *stream);
 
+/* ---- pages of a model's cache ---------------------------------------------------------------
+ * The keys and values of a row's tokens lie in pages of page_tokens (16, 32 or 64) tokens: position p of row r at slot
+ * table[r][p / page_tokens] * page_tokens + p % page_tokens.  Pages that are free lie in a ring of `pages` page numbers, between two counters that only
+ * grow: counters[0] pages have been taken out of it and counters[1] have been put in, the next one to take is
+ * ring[counters[0] % pages].  (To begin with: every page's number in the ring, counters {0, pages}.)
+ *
+ * wg_page_step: the tables of the next step from the rows' lengths.  Row r, with d_lens[r] tokens in the cache, takes d_counts[r]
+ * (0 or more) further ones.  It gets the pages that these need, in order of its table, and d_lens_out[r] <- d_lens[r] + d_counts[r];
+ * the tokens of the call are numbered row by row, those of row r from d_starts[r] on (d_starts: rows + 1 numbers, the last one is how many there are), and for
+ * token t, as far as t < tokens: d_slots[t] is where its key and value go, d_positions[t] its position in the row, d_origins[t] below.
+ * With d_parents (rows / beams requests, a request's beams in adjacent rows) row r first becomes a copy of row d_parents[r] of its request:
+ * its length and its pages, which both share.  A row whose parent is not a row of its request starts empty.  Where a row takes tokens, its last page has begun and
+ * another row of the request has it too, the row gets a page of its own for it, and the origin of the row's first token is the page that the
+ * tokens before it are to be copied from (wg_cache_append does that); all other origins are -1.  Pages that no row of the request refers to any more go into the
+ * ring behind those that are there (in order of request, place in the table and row); they are not handed out in the same call.  (Pages are shared among the rows of a
+ * request only, and only at the same place of their tables, as parents make them.)
+ * Pages are handed out in order of the rows, a row's copied page first.  When they do not suffice, or a row's table is too short (columns), no row of that
+ * request takes tokens: their lengths stay, the slots of their tokens are -1; the requests behind it are served if they need no pages (or, where a table was too short,
+ * as if it had not been there).  d_table_out [rows][columns] receives the rows' pages; its other entries stay.  Without parents
+ * (d_parents NULL, beams 1) d_table_out may be d_table, which then is added to; else it must not.  d_lens_out and d_counters_out
+ * are not their inputs: the same call again gives the same result.  The sum of d_counts must be below 2^31.  rows <= 65535, beams <= 64;
+ * with d_parents, d_workspace is wg_page_step_workspace(rows, beams) bytes, 16-byte aligned.  One kernel, or with parents two. */
+uint64_t wg_page_step_workspace(uint32_t rows, uint32_t beams);
+int wg_page_step(const int32_t *d_table, uint32_t rows, uint32_t columns, const int32_t *d_lens, const int32_t *d_counts,
+                 const int32_t *d_parents, uint32_t beams, uint32_t page_tokens, int32_t *d_ring, uint32_t pages, const uint64_t *d_counters,
+                 int32_t *d_table_out, int32_t *d_lens_out, int32_t *d_starts, int32_t *d_slots, int32_t *d_positions, int32_t *d_origins,
+                 uint32_t tokens, uint64_t *d_counters_out, void *d_workspace, uint64_t workspace_bytes, void *stream);
+
+/* ---- a cache in 8 bits ----------------------------------------------------------------------
+ * Keys [pages][heads][page_tokens][dim] and values [pages][heads][dim][page_tokens] (each dim's tokens lie together) in 8-bit floating point
+ * (e4m3: 4 bits of exponent, 3 of mantissa, up to 448, no infinities), with a scale for every page and head, [pages][heads] fp32 each: a
+ * number is its 8 bits times the scale.  dim is 64, 128 or 256.
+ *
+ * wg_cache_append: token t's key and value (bfloat16, strides in elements, rows of `dim` at multiples of 16 bytes) go to
+ * slot d_slots[t]; a slot outside [0, pages * page_tokens) takes none.  Tokens of one page are adjacent and in ascending order (as wg_page_step numbers them), and
+ * the tokens in front of them in their page are there already.  The page's scale becomes the least power of two, 2^-64 at least, times which 448 reaches the
+ * largest finite magnitude among the new tokens, or stays where it is larger (not where the first token is the page's first); numbers are rounded
+ * to nearest, ties to even, larger ones (infinities) become 448 times the scale, NaN stays.  Where the scale grows, the page's earlier tokens are rounded anew
+ * to it.  d_origins (may be NULL): where d_origins[t] of a page's first new token is a page, the tokens in front of it come from that one (scale and all);
+ * no token of the call goes to that page.  One kernel. */
+int wg_cache_append(const void *d_k, const void *d_v, uint32_t tokens, uint32_t heads, uint32_t dim, int64_t k_token_stride,
+                    int64_t k_head_stride, int64_t v_token_stride, int64_t v_head_stride, const int32_t *d_slots, const int32_t *d_origins,
+                    uint8_t *d_k_cache, uint8_t *d_v_cache, float *d_k_scale, float *d_v_scale, uint32_t pages, uint32_t page_tokens, void *stream);
+
+/* wg_cache_attend: attention of the tokens of a step over the cache.  d_q, d_out: bfloat16 [tokens][q_heads][dim], d_out without gaps, d_q with
+ * strides in elements at multiples of 16 bytes.  Query head j reads cached head j / (q_heads / heads).  Row r has d_lens[r] tokens in the
+ * cache, the tokens d_starts[r] .. d_starts[r + 1] of the call being its last ones: token i of n sees the first d_lens[r] - n + i + 1 keys (none: its output is
+ * zeros).  d_out = sum of values weighted by softmax(scale * q . k).  Products in bfloat16 (the cache's values are exact in it, the
+ * weights are rounded to it), sums and the softmax in fp32.  d_table, d_lens, d_starts: what wg_page_step leaves.  Entries of a table
+ * behind a row's pages may be anything.  d_workspace: wg_cache_attend_workspace(...) bytes (0: may be NULL), 16-byte aligned, overwritten; calls that
+ * share it must not overlap.  One or two kernels. */
+uint64_t wg_cache_attend_workspace(uint32_t tokens, uint32_t rows, uint32_t q_heads, uint32_t heads, uint32_t dim, uint32_t columns, uint32_t page_tokens);
+int wg_cache_attend(const void *d_q, uint32_t tokens, uint32_t q_heads, uint32_t heads, uint32_t dim, int64_t q_token_stride, int64_t q_head_stride,
+                    const uint8_t *d_k_cache, const uint8_t *d_v_cache, const float *d_k_scale, const float *d_v_scale, uint32_t pages,
+                    uint32_t page_tokens, const int32_t *d_table, uint32_t rows, uint32_t columns, const int32_t *d_lens, const int32_t *d_starts,
+                    float scale, void *d_out, void *d_workspace, uint64_t workspace_bytes, void *stream);
+
 /* ---- introspection (these synchronise the device) ---------------------------------------- */
 /* (Counters are read in two small copies, whatever the number of keys; rows_in_use is counted by a launch while
  * the cache has a row for every key.) */

@@ -65,6 +65,7 @@ EXPORTS = [
     "wg_decode_step", "wg_masked_topk", "wg_masked_topk_workspace", "wg_reserve_batch", "wg_max_batch", "wg_set_scan_batch",
     "wg_masked_topk_static", "wg_masked_topk_static_capacity", "wg_profile_apply_mask", "wg_forced_bytes",
     "wg_beam_select", "wg_beam_select_workspace", "wg_reorder_rows",
+    "wg_page_step", "wg_page_step_workspace", "wg_cache_append", "wg_cache_attend", "wg_cache_attend_workspace",
 ]
 
 
@@ -132,6 +133,13 @@ def load_library():
     L.wg_beam_select_workspace.restype = u64
     L.wg_beam_select.argtypes = [vp, C.c_int, u32, u32, i64, vp, u32, vp, vp, vp, vp, vp, vp, vp, u64, vp]
     L.wg_reorder_rows.argtypes = [vp, vp, vp, u32, u32, u64, i64, i64, i64, i64, vp]
+    L.wg_page_step_workspace.argtypes = [u32, u32]
+    L.wg_page_step_workspace.restype = u64
+    L.wg_page_step.argtypes = [vp, u32, u32, vp, vp, vp, u32, u32, vp, u32, vp, vp, vp, vp, vp, vp, vp, u32, vp, vp, u64, vp]
+    L.wg_cache_append.argtypes = [vp, vp, u32, u32, u32, i64, i64, i64, i64, vp, vp, vp, vp, vp, vp, u32, u32, vp]
+    L.wg_cache_attend_workspace.argtypes = [u32] * 7
+    L.wg_cache_attend_workspace.restype = u64
+    L.wg_cache_attend.argtypes = [vp, u32, u32, u32, u32, i64, i64, vp, vp, vp, vp, u32, u32, vp, u32, u32, vp, vp, C.c_float, vp, vp, u64, vp]
     L.wg_cache_clear.argtypes = [vp, vp]
     L.wg_cache_stats.argtypes = [vp, C.POINTER(_Stats)]
     L.wg_error_count.argtypes = [vp, C.POINTER(u64)]
@@ -454,3 +462,33 @@ def reorder_rows(src, parents, dst, axis=0, stream=None):
     """wg_reorder_rows: dst <- the rows of src that parents (int32) names along `axis` (0, or 1 behind one leading dimension),
     zeros where it names none.  src and dst agree in shape and type; each row lies in one piece."""
     (_native or _load_native()).reorder_rows(src, parents, dst, axis, stream)
+
+
+def page_step_workspace(rows, beams):
+    """wg_page_step_workspace: bytes of device workspace a page_step call with parents needs."""
+    return int(load_library().wg_page_step_workspace(rows, beams))
+
+
+def page_step(table, lens, counts, parents, beams, page_tokens, ring, counters, out_table, out_lens, starts, slots, positions, origins, out_counters,
+              workspace=None, stream=None):
+    """wg_page_step: int32 tables [R, columns], lens, counts, parents (or None) and out_lens [R], starts [R + 1], slots, positions and
+    origins [T], ring [pages]; int64 counters and out_counters [2].  Without parents out_table may be table, and no workspace is needed."""
+    (_native or _load_native()).page_step(table, lens, counts, parents, beams, page_tokens, ring, counters, out_table, out_lens, starts, slots, positions, origins,
+                                          out_counters, workspace, stream)
+
+
+def cache_append(k, v, slots, origins, k_cache, v_cache, k_scale, v_scale, stream=None):
+    """wg_cache_append: k and v bfloat16 [T, heads, dim], slots and origins (or None) int32 [T], k_cache float8_e4m3fn
+    [pages, heads, page_tokens, dim], v_cache [pages, heads, dim, page_tokens], scales float32 [pages, heads]."""
+    (_native or _load_native()).cache_append(k, v, slots, origins, k_cache, v_cache, k_scale, v_scale, stream)
+
+
+def cache_attend_workspace(tokens, rows, q_heads, heads, dim, columns, page_tokens):
+    """wg_cache_attend_workspace: bytes of device workspace a cache_attend call of this shape needs."""
+    return int(load_library().wg_cache_attend_workspace(tokens, rows, q_heads, heads, dim, columns, page_tokens))
+
+
+def cache_attend(q, k_cache, v_cache, k_scale, v_scale, table, lens, starts, scale, out, workspace=None, stream=None):
+    """wg_cache_attend: q and out bfloat16 [T, q_heads, dim], the cache as for cache_append, table int32 [R, columns], lens [R] and
+    starts [R + 1] as page_step leaves them."""
+    (_native or _load_native()).cache_attend(q, k_cache, v_cache, k_scale, v_scale, table, lens, starts, scale, out, workspace, stream)

@@ -1,0 +1,516 @@
+// A model's cache of keys and values in 8 bits for gfx950: pages of P tokens, a scale for every page and head, keys as [page][head][token][dim], values as
+// [page][head][dim][token].
+//
+// Values lie transposed so that both products of attention find what a lane multiplies in one piece: with scores as S^T = K Q^T (rows: keys), the lane that
+// holds the scores of some keys after the first product is the one that needs their weights in the second, O^T = V^T P^T.  Nothing is exchanged between lanes
+// in between, and no LDS is used but to join wavefronts.
+#include <hip/hip_runtime.h>
+
+#include <cfloat>
+
+#include "wg_launch.h"
+#include "wg_serve.h"
+
+namespace wg {
+
+typedef __bf16 Half2 __attribute__((ext_vector_type(2)));
+typedef __bf16 Half8 __attribute__((ext_vector_type(8)));
+typedef float Float2 __attribute__((ext_vector_type(2)));
+typedef float Float4 __attribute__((ext_vector_type(4)));
+typedef uint32_t Word2 __attribute__((ext_vector_type(2)));
+typedef uint32_t Word4 __attribute__((ext_vector_type(4)));
+
+constexpr float kMost8 = 448.f;                      // the largest number of the format (e4m3: 4 exponent bits, 3 of mantissa)
+constexpr int kLeastExp = -64, kMostExp = 120;       // exponents that a scale may have
+
+// Numbers to 8 bits: nearest, ties to even; what is too large is the largest (NaN stays NaN).
+__device__ __forceinline__ float within(float x) { return __builtin_fabsf(x) > kMost8 ? __builtin_copysignf(kMost8, x) : x; }
+__device__ __forceinline__ uint32_t to_bytes(float a, float b, float c, float d)
+{
+    int r = __builtin_amdgcn_cvt_pk_fp8_f32(within(a), within(b), 0, false);
+    return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(within(c), within(d), r, true);
+}
+__device__ __forceinline__ float low(uint32_t two) { return __uint_as_float(two << 16); }
+__device__ __forceinline__ float high(uint32_t two) { return __uint_as_float(two & 0xFFFF0000u); }
+__device__ __forceinline__ uint32_t rescaled(uint32_t bytes, float ratio)
+{
+    const auto a = __builtin_amdgcn_cvt_pk_f32_fp8((int)bytes, false), b = __builtin_amdgcn_cvt_pk_f32_fp8((int)bytes, true);
+    return to_bytes(a[0] * ratio, a[1] * ratio, b[0] * ratio, b[1] * ratio);
+}
+// The larger of a and the magnitude of a number (bfloat16, in the upper half of a word), unless that is none or infinite.
+__device__ __forceinline__ float top_of(float a, float x) { const float y = __builtin_fabsf(x); return __builtin_fmaxf(a, y < __builtin_inff() ? y : 0.f); }
+
+// The least power of two times which 448 reaches `top`: 448 = 1.75 * 2^8.  A power of two costs no precision, the format keeps 3 bits of mantissa at any
+// scale, and where a page's scale grows its earlier tokens are rounded again only at the format's low end.
+__device__ __forceinline__ float scale_for(float top)
+{
+    const uint32_t bits = __float_as_uint(top);
+    int e = (int)(bits >> 23) - 127 - 8 + ((bits & 0x7FFFFFu) > 0x600000u);
+    e = e < kLeastExp ? kLeastExp : e > kMostExp ? kMostExp : e;
+    return __uint_as_float((uint32_t)(e + 127) << 23);
+}
+
+// ---------------------------------------------------------------------------------------------
+// append.  Tokens that lie one behind the other in a page are one run, which a wavefront takes for a head: their largest magnitude, the page's scale, then
+// the tokens; the earlier tokens of the page are rewritten where the scale grows or where they come from another page.
+struct AppendArgs {
+    const uint16_t *x[2];                            // keys, values: [token][head][dim]
+    int64_t token_stride[2], head_stride[2];         // elements
+    uint8_t *cache[2];
+    float *scale[2];
+    const int32_t *slots, *origins;
+    uint32_t tokens, heads, pages, shift;
+};
+
+template <uint32_t kD>
+__device__ __forceinline__ void append_run(const AppendArgs &a, uint32_t which, uint32_t t, uint32_t h)
+{
+    const uint32_t lane = threadIdx.x & 63u, P = 1u << a.shift;
+    const uint32_t slot = (uint32_t)a.slots[t], o = slot & (P - 1u), page = slot >> a.shift;
+    if (page >= a.pages) return;                     // (also a slot of -1)
+    if (o && t && (uint32_t)a.slots[t - 1u] == slot - 1u) return;          // in a run that began before
+    const bool mine = lane < P - o && lane < a.tokens - t && (uint32_t)a.slots[t + (lane < a.tokens - t ? lane : 0u)] == slot + lane;
+    const unsigned long long others = ~__ballot(mine);
+    const uint32_t n = others ? (uint32_t)__builtin_ctzll(others) : 64u, end = o + n;
+    const uint32_t origin = a.origins ? (uint32_t)a.origins[t] : 0xFFFFFFFFu, source = origin < a.pages ? origin : page;
+    const uint16_t *x = a.x[which] + (int64_t)t * a.token_stride[which] + (int64_t)h * a.head_stride[which];
+    const int64_t step = a.token_stride[which];
+    uint8_t *to = a.cache[which] + ((size_t)page * a.heads + h) * (P * kD);
+    const uint8_t *from = a.cache[which] + ((size_t)source * a.heads + h) * (P * kD);
+    const float was = o ? a.scale[which][(size_t)source * a.heads + h] : 0.f;
+    float top = 0.f;
+    constexpr uint32_t kLanes = kD / 8u, kTokens = 64u / kLanes;           // keys: eight dims to a lane
+    constexpr uint32_t kOwn = kD / 64u;                                    // values: dims of a lane
+    const uint32_t key_token = lane / kLanes, key_dim = lane % kLanes * 8u, value_dim = lane * kOwn;
+    auto values_of = [&](uint32_t token, float (&v)[kOwn]) {
+        const uint16_t *p = x + (int64_t)token * step + value_dim;
+        if (kOwn == 1u) v[0] = __uint_as_float((uint32_t)*p << 16);
+        else
+#pragma unroll
+            for (uint32_t i = 0; i < kOwn / 2u; i++) {
+                const uint32_t two = reinterpret_cast<const uint32_t *>(p)[i];
+                v[2u * i] = low(two); v[2u * i + 1u] = high(two);
+            }
+    };
+    if (which == 0u) {
+#pragma unroll 4
+        for (uint32_t i = key_token; i < n; i += kTokens) {
+            const Word4 w = *reinterpret_cast<const Word4 *>(x + (int64_t)i * step + key_dim);
+#pragma unroll
+            for (uint32_t j = 0; j < 4u; j++) { top = top_of(top, low(w[j])); top = top_of(top, high(w[j])); }
+        }
+    } else {
+#pragma unroll 8
+        for (uint32_t i = 0; i < n; i++) {
+            float v[kOwn];
+            values_of(i, v);
+#pragma unroll
+            for (uint32_t j = 0; j < kOwn; j++) top = top_of(top, v[j]);
+        }
+    }
+#pragma unroll
+    for (int s = 32; s > 0; s >>= 1) top = __builtin_fmaxf(top, __shfl_xor(top, s));
+    const float now = __builtin_fmaxf(scale_for(top), was), inverse = 1.f / now, ratio = was / now;
+    const bool again = o && (source != page || now != was);                // the earlier tokens are written too
+    if (lane == 0u) a.scale[which][(size_t)page * a.heads + h] = now;
+    if (which == 0u) {
+        if (again)
+            for (uint32_t u = lane; u < o * kD / 16u; u += 64u) {
+                Word4 w = reinterpret_cast<const Word4 *>(from)[u];
+#pragma unroll
+                for (uint32_t j = 0; j < 4u; j++) w[j] = rescaled(w[j], ratio);
+                reinterpret_cast<Word4 *>(to)[u] = w;
+            }
+#pragma unroll 4
+        for (uint32_t i = key_token; i < n; i += kTokens) {
+            const Word4 w = *reinterpret_cast<const Word4 *>(x + (int64_t)i * step + key_dim);
+            Word2 r;
+#pragma unroll
+            for (uint32_t j = 0; j < 2u; j++)
+                r[j] = to_bytes(low(w[2u * j]) * inverse, high(w[2u * j]) * inverse, low(w[2u * j + 1u]) * inverse, high(w[2u * j + 1u]) * inverse);
+            *reinterpret_cast<Word2 *>(to + (o + i) * kD + key_dim) = r;
+        }
+        return;
+    }
+    // values: sixteen tokens of a dim at a time
+    const uint32_t begin = again ? 0u : o;
+    for (uint32_t c = begin & ~15u; c < end; c += 16u) {
+        float v[16][kOwn];
+#pragma unroll
+        for (uint32_t j = 0; j < 16u; j++) {
+#pragma unroll
+            for (uint32_t d = 0; d < kOwn; d++) v[j][d] = 0.f;
+            if (c + j >= o && c + j < end) values_of(c + j - o, v[j]);
+        }
+#pragma unroll
+        for (uint32_t d = 0; d < kOwn; d++) {
+            uint8_t *at = to + (size_t)(value_dim + d) * P + c;
+            Word4 r;
+#pragma unroll
+            for (uint32_t w = 0; w < 4u; w++) r[w] = to_bytes(v[4u * w][d] * inverse, v[4u * w + 1u][d] * inverse, v[4u * w + 2u][d] * inverse, v[4u * w + 3u][d] * inverse);
+            if (again && c < o) {
+                const Word4 old = *reinterpret_cast<const Word4 *>(from + (size_t)(value_dim + d) * P + c);
+#pragma unroll
+                for (uint32_t w = 0; w < 4u; w++) {
+                    const uint32_t early = o <= c + 4u * w ? 0u : o - c - 4u * w;          // bytes of the word from before
+                    const uint32_t keep = early >= 4u ? 0xFFFFFFFFu : (1u << (8u * early)) - 1u;
+                    r[w] = (rescaled(old[w], ratio) & keep) | (r[w] & ~keep);
+                }
+            }
+            if (begin <= c && end >= c + 16u) { *reinterpret_cast<Word4 *>(at) = r; continue; }
+#pragma unroll
+            for (uint32_t w = 0; w < 4u; w++) {
+                const uint32_t b0 = c + 4u * w;
+                if (begin <= b0 && end >= b0 + 4u) { reinterpret_cast<uint32_t *>(at)[w] = r[w]; continue; }
+#pragma unroll
+                for (uint32_t i = 0; i < 4u; i++)
+                    if (b0 + i >= begin && b0 + i < end) at[4u * w + i] = (uint8_t)(r[w] >> (8u * i));
+            }
+        }
+    }
+}
+
+constexpr uint32_t kAppendWaves = 4;
+template <uint32_t kD>
+__global__ void __launch_bounds__(kAppendWaves * 64u)
+append_kernel(const AppendArgs a)
+{
+    const uint32_t h = blockIdx.y * kAppendWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    if (h < a.heads) append_run<kD>(a, blockIdx.z, blockIdx.x, h);
+}
+
+hipError_t launch_cache_append(const void *k, const void *v, uint32_t tokens, uint32_t heads, uint32_t dim, int64_t k_token, int64_t k_head, int64_t v_token,
+                               int64_t v_head, const int32_t *slots, const int32_t *origins, uint8_t *k_cache, uint8_t *v_cache, float *k_scale,
+                               float *v_scale, uint32_t pages, uint32_t shift, hipStream_t s)
+{
+    const AppendArgs a{{static_cast<const uint16_t *>(k), static_cast<const uint16_t *>(v)}, {k_token, v_token}, {k_head, v_head}, {k_cache, v_cache},
+                       {k_scale, v_scale}, slots, origins, tokens, heads, pages, shift};
+    const dim3 grid(tokens, (heads + kAppendWaves - 1u) / kAppendWaves, 2u), block(kAppendWaves * 64u);
+    return launch(dim == 64u ? append_kernel<64> : dim == 128u ? append_kernel<128> : append_kernel<256>, grid, block, 0, s, nullptr, a);
+}
+
+// ---------------------------------------------------------------------------------------------
+// attention.  A tile is 16 query rows of a request and a cached head: its tokens times the query heads that share the head.  A workgroup takes a share of a
+// tile's keys, its wavefronts 64 keys at a time in turn: 16 bytes to a lane and load straight into registers, turned into bfloat16 there (exactly), scores,
+// a running maximum and sum, weights, weighted values.  A page's scales multiply scores and weights, not its values: that of its values as a
+// summand of the scores, log2(vs), so that the running maximum is that of what the weights are with it; the sum takes them without, times 1 / vs.  Weights are then at most 1,
+// whatever the scales, and go into the second product as float16, up to 2^14: 11 bits of precision down to 2^-28 of the largest.  (In bfloat16 they had 8,
+// which was as large an error as the output's own rounding.)
+//
+// Lane l of a wavefront holds, of 64 keys: of K, for m = l % 16, key (m / 4) * 16 + u * 8 + t * 4 + m % 4 in tile (u, t), the dims of its quarter l / 16;
+// after S^T of tile (u, t), the scores of query l % 16 and the keys (l / 16) * 16 + u * 8 + t * 4 + 0 .. 3; of V, for dim l % 16 of 16, the keys
+// (l / 16) * 16 + 0 .. 15.  Sixteen neighbouring keys lie in one page.
+struct AttendArgs {
+    const uint16_t *q;
+    int64_t q_token, q_head;                         // strides, elements
+    const uint8_t *k_cache, *v_cache;
+    const float *k_scale, *v_scale;
+    const int32_t *table, *lens, *starts;
+    uint16_t *out;                                   // [token][head][dim]
+    float *partial;                                  // [token][head][split][dim + 2]
+    float scale;                                     // of the scores, times log2(e)
+    uint32_t tokens, rows, heads, group, columns, pages, shift, splits, tiles;
+};
+constexpr uint32_t kAttendWaves = 4, kBlock = 64, kTile = 16;
+constexpr float kHeadroom = 14.f;                    // weights go up to 2^14
+constexpr uint32_t kLeastBlocks = 4;                 // blocks of a share: one for each wavefront
+
+typedef _Float16 Short2 __attribute__((ext_vector_type(2)));
+typedef _Float16 Short8 __attribute__((ext_vector_type(8)));
+__device__ __forceinline__ uint32_t pk_f16(float a, float b) { return __builtin_bit_cast(uint32_t, __builtin_convertvector(Float2{a, b}, Short2)); }
+__device__ __forceinline__ Short8 widened16(uint32_t a, uint32_t b)
+{
+    const Short2 x = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(a, 1.f, false), y = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(a, 1.f, true);
+    const Short2 z = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(b, 1.f, false), w = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(b, 1.f, true);
+    return Short8{x[0], x[1], y[0], y[1], z[0], z[1], w[0], w[1]};
+}
+__device__ __forceinline__ uint32_t pk_bf16(float a, float b) { return __builtin_bit_cast(uint32_t, __builtin_convertvector(Float2{a, b}, Half2)); }
+__device__ __forceinline__ Half8 widened(uint32_t a, uint32_t b)
+{
+    const Half2 x = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, 1.f, false), y = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, 1.f, true);
+    const Half2 z = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, 1.f, false), w = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, 1.f, true);
+    return Half8{x[0], x[1], y[0], y[1], z[0], z[1], w[0], w[1]};
+}
+
+// Sixteen bytes, zero from the n-th on.
+__device__ __forceinline__ Word4 first_bytes(Word4 v, uint32_t n)
+{
+#pragma unroll
+    for (uint32_t w = 0; w < 4u; w++) {
+        const uint32_t k = n <= 4u * w ? 0u : n - 4u * w;
+        v[w] &= k >= 4u ? 0xFFFFFFFFu : (1u << (8u * k)) - 1u;
+    }
+    return v;
+}
+template <uint32_t kParts>
+__device__ __forceinline__ bool has_nan(const Word4 (&v)[kParts])
+{
+    uint32_t any = 0;                                // a byte is NaN where its low seven bits are ones: one more carries into the eighth
+#pragma unroll
+    for (uint32_t p = 0; p < kParts; p++)
+#pragma unroll
+        for (uint32_t w = 0; w < 4u; w++) any |= (v[p][w] & 0x7F7F7F7Fu) + 0x01010101u;
+    return any & 0x80808080u;
+}
+
+// Where a tile lies: the request whose tiles it is among, from the places at which the requests' tokens begin.  Request r's tiles begin at
+// starts[r] * group / 16 + r, which leaves room for each one's last, begun tile.  A wavefront asks 64 requests at a time.
+__device__ __forceinline__ uint32_t request_of(const AttendArgs &a, uint32_t tile)
+{
+    const uint32_t lane = threadIdx.x & 63u;
+    auto begins = [&](uint32_t r) { const uint32_t t = (uint32_t)a.starts[r] < a.tokens ? (uint32_t)a.starts[r] : a.tokens; return (uint32_t)((uint64_t)t * a.group / kTile) + r; };
+    uint32_t lo = 0, n = a.rows;                     // the request is in [lo, lo + n)
+    while (n > 1u) {
+        const uint32_t step = (n + 63u) / 64u, r = lo + lane * step;
+        const bool at = lane * step < n && begins(r) <= tile;
+        const uint32_t k = 63u - (uint32_t)__builtin_clzll(__ballot(at) | 1ull);
+        n = n - k * step < step ? n - k * step : step;
+        lo += k * step;
+    }
+    return __builtin_amdgcn_readfirstlane(lo);
+}
+
+struct TileOf { uint32_t row, first, last, begin, count; int32_t before; };      // query rows [first, last) of a request with `count` tokens from `begin` on, behind `before` others
+
+__device__ __forceinline__ bool tile_of(const AttendArgs &a, uint32_t tile, uint32_t *len, TileOf *out)
+{
+    const uint32_t r = request_of(a, tile);
+    const uint32_t b = (uint32_t)a.starts[r] < a.tokens ? (uint32_t)a.starts[r] : a.tokens, e0 = (uint32_t)a.starts[r + 1u], e = e0 < b ? b : e0 < a.tokens ? e0 : a.tokens;
+    const uint32_t at = tile - ((uint32_t)((uint64_t)b * a.group / kTile) + r), all = (e - b) * a.group;
+    const uint32_t most = a.columns << a.shift, l = (uint32_t)(a.lens[r] < 0 ? 0 : a.lens[r]);
+    *len = l < most ? l : most;
+    if (tile < (uint32_t)((uint64_t)b * a.group / kTile) + r || (uint64_t)at * kTile >= all) return false;
+    out->row = r; out->begin = b; out->count = e - b;
+    out->first = at * kTile;
+    out->last = all - out->first < kTile ? all : out->first + kTile;
+    out->before = (int32_t)*len - (int32_t)(e - b);
+    return true;
+}
+// Shares that a tile's keys are cut into, and the blocks of each.
+__device__ __forceinline__ uint32_t shares_of(uint32_t blocks, uint32_t splits, uint32_t *per)
+{
+    const uint32_t most = (blocks + kLeastBlocks - 1u) / kLeastBlocks, n = most < splits ? (most ? most : 1u) : splits;
+    *per = (blocks + n - 1u) / n;
+    return *per ? (blocks + *per - 1u) / *per : 1u;
+}
+// Keys that query row i of the tile sees.
+__device__ __forceinline__ uint32_t seen_by(const TileOf &t, uint32_t i, uint32_t group) { const int32_t n = t.before + (int32_t)(i / group) + 1; return n < 0 ? 0u : (uint32_t)n; }
+
+template <uint32_t kD>
+__global__ void __launch_bounds__(kAttendWaves * 64u)
+attend_kernel(const AttendArgs a)
+{
+    constexpr uint32_t kSteps = kD / 32u, kParts = kD / 16u;
+    __shared__ float join_o[kAttendWaves][kTile][kD + 4u];
+    __shared__ float join_m[kAttendWaves][kTile], join_l[kAttendWaves][kTile];
+    const uint32_t tid = threadIdx.x, lane = tid & 63u, wave = __builtin_amdgcn_readfirstlane(tid >> 6), m = lane & 15u, g = lane >> 4;
+    const uint32_t split = blockIdx.z, h = blockIdx.y, P = 1u << a.shift;
+    uint32_t len;
+    TileOf t;
+    if (!tile_of(a, blockIdx.x, &len, &t)) return;
+    const uint32_t sees_most = seen_by(t, t.last - 1u, a.group), blocks = (sees_most + kBlock - 1u) / kBlock;
+    uint32_t per;
+    const uint32_t shares = shares_of(blocks, a.splits, &per);
+    if (split >= shares) return;
+    const uint32_t b0 = split * per, b1 = blocks - b0 < per ? blocks : b0 + per;
+    // the lane's query row (a row behind the last is the last again, and is not stored)
+    const uint32_t i = t.first + m < t.last ? t.first + m : t.last - 1u;
+    const uint32_t sees = seen_by(t, i, a.group), sees_least = seen_by(t, t.first, a.group);
+    const uint16_t *q = a.q + (int64_t)(t.begin + i / a.group) * a.q_token + (int64_t)(h * a.group + i % a.group) * a.q_head;
+    Half8 qf[kSteps];
+#pragma unroll
+    for (uint32_t s = 0; s < kSteps; s++) qf[s] = __builtin_bit_cast(Half8, *reinterpret_cast<const Word4 *>(q + g * (kD / 4u) + s * 8u));
+    const int32_t *table = a.table + (size_t)t.row * a.columns;
+    const uint32_t last_column = a.columns - 1u;
+    auto page_at = [&](uint32_t key) {
+        const uint32_t c = key >> a.shift, id = (uint32_t)table[c < last_column ? c : last_column];
+        return id < a.pages ? id : 0u;               // (what lies behind a row's pages is masked, and must be somewhere)
+    };
+    Float4 o[kParts];
+#pragma unroll
+    for (uint32_t p = 0; p < kParts; p++) o[p] = Float4{0.f, 0.f, 0.f, 0.f};
+    float top = -__builtin_inff(), sum = 0.f;        // of the lane's query; the sum of the lane's own keys
+    for (uint32_t b = b0 + wave; b < b1; b += kAttendWaves) {
+        const uint32_t key0 = b * kBlock, mine = key0 + g * 16u, theirs = key0 + (m >> 2) * 16u;
+        const uint32_t k_page = page_at(theirs), v_page = page_at(mine);
+        const uint8_t *kp = a.k_cache + (((size_t)k_page * a.heads + h) * P + (theirs & (P - 1u)) + (m & 3u)) * kD + g * (kD / 4u);
+        const uint8_t *vp = a.v_cache + (((size_t)v_page * a.heads + h) * kD + m) * P + (mine & (P - 1u));
+        const float ks = a.k_scale[(size_t)v_page * a.heads + h] * a.scale;
+        // (a page of zeros may have a scale of zero; what lies behind a row's pages may have any)
+        const float vs = __builtin_fmaxf(a.v_scale[(size_t)v_page * a.heads + h], 0x1p-64f), v_log = __builtin_amdgcn_logf(vs), v_inverse = __builtin_amdgcn_rcpf(vs);
+        Word4 kw[4][kD / 64u];
+#pragma unroll
+        for (uint32_t n = 0; n < 4u; n++)
+#pragma unroll
+            for (uint32_t j = 0; j < kD / 64u; j++) kw[n][j] = *reinterpret_cast<const Word4 *>(kp + n * 4u * kD + j * 16u);
+        Word4 vw[kParts];
+#pragma unroll
+        for (uint32_t p = 0; p < kParts; p++) vw[p] = *reinterpret_cast<const Word4 *>(vp + (size_t)p * 16u * P);
+        Float4 s[4];
+#pragma unroll
+        for (uint32_t n = 0; n < 4u; n++) {
+            s[n] = Float4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (uint32_t k = 0; k < kSteps; k++)
+                s[n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widened(kw[n][k / 2u][k % 2u * 2u], kw[n][k / 2u][k % 2u * 2u + 1u]), qf[k], s[n], 0, 0, 0);
+        }
+        const bool edge = key0 + kBlock > sees_least;            // a query of the tile does not see all of the block
+        float high = -__builtin_inff();
+#pragma unroll
+        for (uint32_t n = 0; n < 4u; n++)
+#pragma unroll
+            for (uint32_t e = 0; e < 4u; e++) {
+                s[n][e] = s[n][e] * ks + v_log;
+                if (edge && mine + n * 4u + e >= sees) s[n][e] = -__builtin_inff();
+                high = __builtin_fmaxf(high, s[n][e]);
+            }
+        high = __builtin_fmaxf(high, __shfl_xor(high, 16));
+        high = __builtin_fmaxf(high, __shfl_xor(high, 32));
+        const float next = __builtin_fmaxf(top, high), base = next > -__builtin_inff() ? next - kHeadroom : 0.f;
+        if (edge) {
+            // values behind the row's end are whatever the pages held: they must not be NaN times a weight of zero
+            const uint32_t there = mine >= len ? 0u : len - mine < 16u ? len - mine : 16u;
+#pragma unroll
+            for (uint32_t p = 0; p < kParts; p++) vw[p] = first_bytes(vw[p], there);
+        }
+        if (__ballot(next != top)) {
+            const float shrink = __builtin_amdgcn_exp2f(top - (next > -__builtin_inff() ? next : 0.f));
+            sum *= shrink;
+#pragma unroll
+            for (uint32_t p = 0; p < kParts; p++) o[p] *= shrink;
+        }
+        top = next;
+        Short8 weights[2];
+#pragma unroll
+        for (uint32_t u = 0; u < 2u; u++) {
+            float w[8];
+#pragma unroll
+            for (uint32_t e = 0; e < 8u; e++) {
+                w[e] = __builtin_amdgcn_exp2f(s[u * 2u + e / 4u][e % 4u] - base);
+                sum += w[e] * v_inverse;
+            }
+            weights[u] = __builtin_bit_cast(Short8, Word4{pk_f16(w[0], w[1]), pk_f16(w[2], w[3]), pk_f16(w[4], w[5]), pk_f16(w[6], w[7])});
+        }
+        if (edge && __ballot(has_nan(vw))) {
+            // A NaN among the values, and queries that do not see all of them: each query has a product of its own, of what it sees.
+            for (uint32_t n = 0; n < kTile; n++) {
+                const uint32_t limit = __shfl(sees, n), mine_seen = mine >= limit ? 0u : limit - mine < 16u ? limit - mine : 16u;
+#pragma unroll
+                for (uint32_t p = 0; p < kParts; p++) {
+                    const Word4 v = first_bytes(vw[p], mine_seen);
+                    Float4 one{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                    for (uint32_t u = 0; u < 2u; u++) one = __builtin_amdgcn_mfma_f32_16x16x32_f16(widened16(v[u * 2u], v[u * 2u + 1u]), weights[u], one, 0, 0, 0);
+                    if (m == n) o[p] += one;
+                }
+            }
+            continue;
+        }
+#pragma unroll
+        for (uint32_t u = 0; u < 2u; u++)
+#pragma unroll
+            for (uint32_t p = 0; p < kParts; p++)
+                o[p] = __builtin_amdgcn_mfma_f32_16x16x32_f16(widened16(vw[p][u * 2u], vw[p][u * 2u + 1u]), weights[u], o[p], 0, 0, 0);
+    }
+    sum += __shfl_xor(sum, 16);
+    sum += __shfl_xor(sum, 32);
+    // the wavefronts' shares joined
+    if (g == 0u) { join_m[wave][m] = top; join_l[wave][m] = sum; }
+#pragma unroll
+    for (uint32_t p = 0; p < kParts; p++) *reinterpret_cast<Float4 *>(&join_o[wave][m][p * 16u + g * 4u]) = o[p];
+    __syncthreads();
+    constexpr uint32_t kPer = kTile * kD / (kAttendWaves * 64u);          // neighbouring dims of a thread
+    const uint32_t row = tid * kPer / kD, d0 = tid * kPer % kD, r = t.first + row;
+    if (r >= t.last) return;
+    float all = -__builtin_inff(), total = 0.f, acc[kPer];
+#pragma unroll
+    for (uint32_t w = 0; w < kAttendWaves; w++) all = __builtin_fmaxf(all, join_m[w][row]);
+    const float base = all > -__builtin_inff() ? all : 0.f;
+#pragma unroll
+    for (uint32_t d = 0; d < kPer; d++) acc[d] = 0.f;
+#pragma unroll
+    for (uint32_t w = 0; w < kAttendWaves; w++) {
+        const float by = __builtin_amdgcn_exp2f(join_m[w][row] - base);
+        total += by * join_l[w][row];
+#pragma unroll
+        for (uint32_t d = 0; d < kPer; d++) acc[d] += by * join_o[w][row][d0 + d];
+    }
+    const size_t at = (size_t)(t.begin + r / a.group) * (a.heads * a.group) + h * a.group + r % a.group;
+    if (shares > 1u) {
+        float *to = a.partial + (at * a.splits + split) * (kD + 2u);
+#pragma unroll
+        for (uint32_t d = 0; d < kPer; d++) to[d0 + d] = acc[d];
+        if (d0 == 0u) { to[kD] = all; to[kD + 1u] = total; }
+        return;
+    }
+    const float by = total > 0.f ? 1.f / total : 0.f;            // (a row that sees nothing: zeros)
+#pragma unroll
+    for (uint32_t d = 0; d < kPer; d += 2u) reinterpret_cast<uint32_t *>(a.out + at * kD + d0)[d / 2u] = pk_bf16(acc[d] * by, acc[d + 1u] * by);
+}
+
+// The shares of a tile's keys joined: a wavefront for a token and query head.
+template <uint32_t kD>
+__global__ void __launch_bounds__(256)
+attend_join_kernel(const AttendArgs a)
+{
+    const uint32_t lane = threadIdx.x & 63u, head = blockIdx.y * 4u + (threadIdx.x >> 6), Q = a.heads * a.group;
+    // by tile, to know how many shares it has
+    uint32_t len, per;
+    TileOf t;
+    if (!tile_of(a, blockIdx.x, &len, &t)) return;
+    const uint32_t sees_most = seen_by(t, t.last - 1u, a.group), shares = shares_of((sees_most + kBlock - 1u) / kBlock, a.splits, &per);
+    if (shares < 2u || head >= a.heads * kTile) return;
+    const uint32_t h = head / kTile, r = t.first + head % kTile;
+    if (r >= t.last) return;
+    const size_t at = (size_t)(t.begin + r / a.group) * Q + h * a.group + r % a.group;
+    const float *from = a.partial + at * a.splits * (kD + 2u);
+    constexpr uint32_t kOwn = kD / 64u;
+    float m = -__builtin_inff(), l = 0.f, acc[kOwn];
+    if (lane < shares) m = from[(size_t)lane * (kD + 2u) + kD];
+#pragma unroll
+    for (int s = 32; s > 0; s >>= 1) m = __builtin_fmaxf(m, __shfl_xor(m, s));
+    const float base = m > -__builtin_inff() ? m : 0.f;
+#pragma unroll
+    for (uint32_t d = 0; d < kOwn; d++) acc[d] = 0.f;
+#pragma unroll 4
+    for (uint32_t k = 0; k < shares; k++) {
+        const float *p = from + (size_t)k * (kD + 2u);
+        const float by = __builtin_amdgcn_exp2f(p[kD] - base);
+        l += by * p[kD + 1u];
+#pragma unroll
+        for (uint32_t d = 0; d < kOwn; d++) acc[d] += by * p[lane * kOwn + d];
+    }
+    const float by = l > 0.f ? 1.f / l : 0.f;
+    uint16_t *out = a.out + at * kD + lane * kOwn;
+    if (kOwn == 1u) out[0] = (uint16_t)pk_bf16(acc[0] * by, 0.f);
+    else
+#pragma unroll
+        for (uint32_t d = 0; d < kOwn; d += 2u) reinterpret_cast<uint32_t *>(out)[d / 2u] = pk_bf16(acc[d] * by, acc[(d + 1u) % kOwn] * by);
+}
+
+static uint32_t tiles_of(uint32_t tokens, uint32_t rows, uint32_t group) { return (uint32_t)((uint64_t)tokens * group / kTile) + rows; }
+
+// Shares of a tile's keys: workgroups for four of them on every compute unit, 64 shares at most.
+uint32_t attend_splits(uint32_t tokens, uint32_t rows, uint32_t heads, uint32_t group, uint32_t columns, uint32_t shift)
+{
+    const uint64_t tiles = (uint64_t)(tokens < rows ? tokens : rows) * ((group + kTile - 1u) / kTile) * heads;
+    const uint64_t all = tokens > rows ? (uint64_t)tokens * group / kTile * heads : tiles, n = all > tiles ? all : tiles;
+    const uint64_t want = (1024u + n - 1u) / n, blocks = (((uint64_t)columns << shift) + kBlock - 1u) / kBlock, most = (blocks + kLeastBlocks - 1u) / kLeastBlocks;
+    const uint64_t splits = want < most ? want : most;
+    return splits < 1u ? 1u : splits > 64u ? 64u : (uint32_t)splits;
+}
+
+hipError_t launch_cache_attend(const void *q, uint32_t tokens, uint32_t heads, uint32_t group, uint32_t dim, int64_t q_token, int64_t q_head, const uint8_t *k_cache,
+                               const uint8_t *v_cache, const float *k_scale, const float *v_scale, uint32_t pages, uint32_t shift, const int32_t *table,
+                               uint32_t rows, uint32_t columns, const int32_t *lens, const int32_t *starts, float scale, void *out, void *workspace, hipStream_t s)
+{
+    const uint32_t splits = attend_splits(tokens, rows, heads, group, columns, shift), tiles = tiles_of(tokens, rows, group);
+    const AttendArgs a{static_cast<const uint16_t *>(q), q_token, q_head, k_cache, v_cache, k_scale, v_scale, table, lens, starts, static_cast<uint16_t *>(out),
+                       static_cast<float *>(workspace), scale * 1.44269504088896340736f, tokens, rows, heads, group, columns, pages, shift, splits, tiles};
+    const dim3 grid(tiles, heads, splits), block(kAttendWaves * 64u);
+    const hipError_t e = launch(dim == 64u ? attend_kernel<64> : dim == 128u ? attend_kernel<128> : attend_kernel<256>, grid, block, 0, s, nullptr, a);
+    if (e != hipSuccess || splits == 1u) return e;
+    return launch(dim == 64u ? attend_join_kernel<64> : dim == 128u ? attend_join_kernel<128> : attend_join_kernel<256>, dim3(tiles, heads * kTile / 4u), dim3(256), 0, s, nullptr, a);
+}
+
+}  // namespace wg

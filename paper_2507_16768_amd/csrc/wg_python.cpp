@@ -291,6 +291,99 @@ PyObject *reorder_rows(PyObject *, PyObject *const *a, Py_ssize_t n) {
     }));
 }
 
+// An optional workspace: its address and bytes.
+bool work_of(PyObject *o, void **p, uint64_t *bytes) {
+    *p = nullptr; *bytes = 0;
+    if (o == Py_None) return true;
+    const at::Tensor *t;
+    if (!tensor(o, &t, "workspace") || !device(*t, t->scalar_type(), "workspace")) return false;
+    *p = t->data_ptr(); *bytes = bytes_of(*t);
+    return true;
+}
+
+// page_step(table, lens, counts, parents or None, beams, page_tokens, ring, counters, out_table, out_lens, starts, slots, positions, origins,
+//           out_counters, workspace or None, stream)
+PyObject *page_step(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    const at::Tensor *tb, *le, *co, *pa = nullptr, *ri, *ct, *to, *lo, *st, *sl, *po, *og, *cx; void *s, *work; uint64_t bytes; uint32_t beams, P;
+    if (!count(n, 17) || !tensor(a[0], &tb, "table") || !tensor(a[1], &le, "lens") || !tensor(a[2], &co, "counts") || (a[3] != Py_None && !tensor(a[3], &pa, "parents")) ||
+        !number(a[4], &beams, "beams") || !number(a[5], &P, "page_tokens") || !tensor(a[6], &ri, "ring") || !tensor(a[7], &ct, "counters") || !tensor(a[8], &to, "out_table") ||
+        !tensor(a[9], &lo, "out_lens") || !tensor(a[10], &st, "starts") || !tensor(a[11], &sl, "slots") || !tensor(a[12], &po, "positions") || !tensor(a[13], &og, "origins") ||
+        !tensor(a[14], &cx, "out_counters") || !work_of(a[15], &work, &bytes)) return nullptr;
+    if (tb->dim() != 2 || ri->dim() != 1 || sl->dim() != 1) { bad(PyExc_ValueError, "table must be [R, columns], ring [pages] and slots [T]"); return nullptr; }
+    const int64_t R = tb->size(0), M = tb->size(1), T = sl->size(0);
+    if (!shape2(*to, R, M) || !shape1(*le, R) || !shape1(*co, R) || (pa && !shape1(*pa, R)) || !shape1(*lo, R) || !shape1(*st, R + 1) || !shape1(*po, T) || !shape1(*og, T) ||
+        !shape1(*ct, 2) || !shape1(*cx, 2)) {
+        bad(PyExc_ValueError, "out_table must be [R, columns], lens, counts, parents and out_lens [R], starts [R + 1], positions and origins [T], counters [2]");
+        return nullptr;
+    }
+    if (!device(*tb, at::kInt, "table") || !device(*le, at::kInt, "lens") || !device(*co, at::kInt, "counts") || (pa && !device(*pa, at::kInt, "parents")) ||
+        !device(*ri, at::kInt, "ring") || !device(*ct, at::kLong, "counters") || !device(*to, at::kInt, "out_table") || !device(*lo, at::kInt, "out_lens") ||
+        !device(*st, at::kInt, "starts") || !device(*sl, at::kInt, "slots") || !device(*po, at::kInt, "positions") || !device(*og, at::kInt, "origins") ||
+        !device(*cx, at::kLong, "out_counters") || !fits32(*tb, 0) || !fits32(*tb, 1) || !fits32(*ri, 0) || !fits32(*sl, 0) || !stream_of(a[16], &s)) return nullptr;
+    return result(unlocked([=, table = ints(*tb), lens = ints(*le), counts = ints(*co), parents = pa ? ints(*pa) : nullptr, ring = ints(*ri), pages = rows(*ri),
+                            counters = static_cast<const uint64_t *>(ct->data_ptr()), table_out = ints(*to), lens_out = ints(*lo), starts = ints(*st), slots = ints(*sl),
+                            positions = ints(*po), origins = ints(*og), counters_out = static_cast<uint64_t *>(cx->data_ptr())] {
+        return wg_page_step(table, (uint32_t)R, (uint32_t)M, lens, counts, parents, beams, P, ring, pages, counters, table_out, lens_out, starts, slots, positions, origins,
+                            (uint32_t)T, counters_out, work, bytes, s);
+    }));
+}
+
+// The cache of keys [pages, heads, page_tokens, dim] and values [pages, heads, dim, page_tokens] with its scales.
+struct Cache { uint8_t *k, *v; float *ks, *vs; uint32_t pages, heads, page_tokens, dim; };
+bool cache_of(PyObject *const *a, Cache *out) {
+    const at::Tensor *k, *v, *ks, *vs;
+    if (!tensor(a[0], &k, "k_cache") || !tensor(a[1], &v, "v_cache") || !tensor(a[2], &ks, "k_scale") || !tensor(a[3], &vs, "v_scale")) return false;
+    if (k->dim() != 4 || v->dim() != 4 || v->size(0) != k->size(0) || v->size(1) != k->size(1) || v->size(2) != k->size(3) || v->size(3) != k->size(2) ||
+        !shape2(*ks, k->size(0), k->size(1)) || !shape2(*vs, k->size(0), k->size(1)))
+        return bad(PyExc_ValueError, "k_cache must be [pages, heads, page_tokens, dim], v_cache [pages, heads, dim, page_tokens] and the scales [pages, heads]");
+    if (k->scalar_type() != at::kFloat8_e4m3fn || v->scalar_type() != at::kFloat8_e4m3fn) return bad(PyExc_ValueError, "k_cache and v_cache must have dtype torch.float8_e4m3fn");
+    if (!device(*k, k->scalar_type(), "k_cache") || !device(*v, v->scalar_type(), "v_cache") || !device(*ks, at::kFloat, "k_scale") || !device(*vs, at::kFloat, "v_scale")) return false;
+    for (int64_t d = 0; d < 4; d++) if (!fits32(*k, d)) return false;
+    *out = Cache{static_cast<uint8_t *>(k->data_ptr()), static_cast<uint8_t *>(v->data_ptr()), static_cast<float *>(ks->data_ptr()), static_cast<float *>(vs->data_ptr()),
+                 (uint32_t)k->size(0), (uint32_t)k->size(1), (uint32_t)k->size(2), (uint32_t)k->size(3)};
+    return true;
+}
+// A [T, heads, dim] bfloat16 device tensor with unit inner stride.
+bool heads_ok(const at::Tensor &t, const char *name) {
+    if (t.dim() != 3 || !t.is_cuda() || t.scalar_type() != at::kBFloat16 || (t.size(2) != 1 && t.stride(2) != 1))
+        return bad(PyExc_ValueError, std::string(name) + " must be a [T, heads, dim] bfloat16 device tensor with unit inner stride");
+    return fits32(t, 0) && fits32(t, 1);
+}
+// (the stride of a dimension of one is of no account)
+int64_t step_of(const at::Tensor &t, int64_t d) { return t.size(d) > 1 ? t.stride(d) : 0; }
+
+// cache_append(k, v, slots, origins or None, k_cache, v_cache, k_scale, v_scale, stream)
+PyObject *cache_append(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    const at::Tensor *k, *v, *sl, *og = nullptr; void *s; Cache c;
+    if (!count(n, 9) || !tensor(a[0], &k, "k") || !tensor(a[1], &v, "v") || !tensor(a[2], &sl, "slots") || (a[3] != Py_None && !tensor(a[3], &og, "origins")) || !cache_of(a + 4, &c) ||
+        !heads_ok(*k, "k") || !heads_ok(*v, "v")) return nullptr;
+    const int64_t T = k->size(0);
+    if (k->sizes() != v->sizes() || k->size(1) != c.heads || k->size(2) != c.dim) { bad(PyExc_ValueError, "k and v must have the cache's heads and dim"); return nullptr; }
+    if (!shape1(*sl, T) || (og && !shape1(*og, T))) { bad(PyExc_ValueError, "slots and origins must be [T]"); return nullptr; }
+    if (!device(*sl, at::kInt, "slots") || (og && !device(*og, at::kInt, "origins")) || !stream_of(a[8], &s)) return nullptr;
+    return result(unlocked([=, kp = k->data_ptr(), vp = v->data_ptr(), k0 = step_of(*k, 0), k1 = step_of(*k, 1), v0 = step_of(*v, 0), v1 = step_of(*v, 1), slots = ints(*sl),
+                            origins = og ? ints(*og) : nullptr] {
+        return wg_cache_append(kp, vp, (uint32_t)T, c.heads, c.dim, k0, k1, v0, v1, slots, origins, c.k, c.v, c.ks, c.vs, c.pages, c.page_tokens, s);
+    }));
+}
+
+// cache_attend(q, k_cache, v_cache, k_scale, v_scale, table, lens, starts, scale, out, workspace or None, stream)
+PyObject *cache_attend(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    const at::Tensor *q, *tb, *le, *st, *ou; void *s, *work; uint64_t bytes; Cache c;
+    if (!count(n, 12) || !tensor(a[0], &q, "q") || !cache_of(a + 1, &c) || !tensor(a[5], &tb, "table") || !tensor(a[6], &le, "lens") || !tensor(a[7], &st, "starts") ||
+        !tensor(a[9], &ou, "out") || !work_of(a[10], &work, &bytes) || !heads_ok(*q, "q")) return nullptr;
+    const double scale = PyFloat_AsDouble(a[8]);
+    if (PyErr_Occurred()) return nullptr;
+    if (q->size(2) != c.dim || ou->sizes() != q->sizes()) { bad(PyExc_ValueError, "q and out must be [T, q_heads, dim] with the cache's dim"); return nullptr; }
+    if (tb->dim() != 2 || !shape1(*le, tb->size(0)) || !shape1(*st, tb->size(0) + 1)) { bad(PyExc_ValueError, "table must be [R, columns], lens [R] and starts [R + 1]"); return nullptr; }
+    if (!device(*tb, at::kInt, "table") || !device(*le, at::kInt, "lens") || !device(*st, at::kInt, "starts") || !device(*ou, at::kBFloat16, "out") || !fits32(*tb, 0) || !fits32(*tb, 1) ||
+        !stream_of(a[11], &s)) return nullptr;
+    return result(unlocked([=, qp = q->data_ptr(), T = rows(*q), Q = (uint32_t)q->size(1), q0 = step_of(*q, 0), q1 = step_of(*q, 1), table = ints(*tb), R = rows(*tb),
+                            M = (uint32_t)tb->size(1), lens = ints(*le), starts = ints(*st), out = ou->data_ptr()] {
+        return wg_cache_attend(qp, T, Q, c.heads, c.dim, q0, q1, c.k, c.v, c.ks, c.vs, c.pages, c.page_tokens, table, R, M, lens, starts, (float)scale, out, work, bytes, s);
+    }));
+}
+
 // add_instances(handle, texts, args or None, starts address, its rows, stream): sequences of template texts and of
 // argument mappings.  The C call reads the strings in place and without the lock, when other threads may
 // change the caller's lists and dictionaries, and a conversion to bytes may run Python code that does:
@@ -374,6 +467,7 @@ PyObject *set_error(PyObject *, PyObject *cls) {
 #define FAST(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(guarded<name>)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {FAST(fill_masks), FAST(advance), FAST(advance_fill_masks), FAST(decode_step), FAST(forced_bytes), FAST(cache_clear),
                          FAST(apply_mask), FAST(masked_argmax), FAST(masked_topk), FAST(select_tokens), FAST(add_instances), FAST(beam_select), FAST(reorder_rows),
+                         FAST(page_step), FAST(cache_append), FAST(cache_attend),
                          {"set_error", set_error, METH_O, nullptr}, {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_native", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

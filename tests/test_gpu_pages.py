@@ -1,0 +1,214 @@
+"""Page tables, slots and positions against the rules, followed row by row on the host."""
+import numpy as np
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+
+def _wg():
+    import torch
+    import paper_2507_16768_amd as wg
+    assert torch.cuda.is_available(), "this test needs the GPU"
+    return torch, wg
+
+
+def definition(table, lens, counts, parents, K, P, ring, counters, tokens, out_table):
+    """The step by its rules: returns a dict of what the call writes."""
+    R, M = table.shape
+    N = len(ring)
+    taken, given = int(counters[0]), int(counters[1])
+    free = max(0, min(given - taken, N))
+    ring, out = ring.copy(), out_table.copy()
+    lens_out, starts = np.zeros(R, np.int32), np.zeros(R + 1, np.int32)
+    slots, positions, origins = (np.full(tokens, -99, np.int32) for _ in range(3))
+    pages = lambda n: -(-n // P)
+    at, asked, used, t = taken, 0, 0, 0
+    back = []
+    for g in range(0, R, K):
+        rows = range(g, g + K)
+        source = {r: (r if parents is None else int(parents[r]) if g <= parents[r] < g + K else None) for r in rows}
+        length = {r: int(lens[source[r]]) if source[r] is not None else 0 for r in rows}
+        kept = {r: [int(p) for p in table[source[r]][:pages(length[r])]] if source[r] is not None else [] for r in rows}
+        count = {r: max(0, int(counts[r])) for r in rows}
+        fork = {}
+        for r in rows:
+            c = length[r] // P
+            begun = length[r] % P != 0 and count[r] > 0
+            fork[r] = parents is not None and begun and any(o != r and len(kept[o]) > c and kept[o][c] == kept[r][c] for o in rows)
+        need = {r: pages(length[r] + count[r]) - len(kept[r]) + int(fork[r]) for r in rows}
+        fits = all(pages(length[r] + count[r]) <= M for r in rows)
+        total = sum(need.values())
+        if fits:
+            asked += total
+        served = fits and (total == 0 or asked <= free)
+        final = {}
+        for r in rows:
+            mine, c, origin = list(kept[r]), length[r] // P, -1
+            if served:
+                if fork[r]:
+                    origin, mine[c] = mine[c], int(ring[at % N])
+                    at += 1
+                while len(mine) < pages(length[r] + count[r]):
+                    mine.append(int(ring[at % N]))
+                    at += 1
+            final[r] = mine
+            out[r, :len(mine)] = mine
+            lens_out[r] = length[r] + (count[r] if served else 0)
+            starts[r] = t
+            for i in range(count[r]):
+                if t < tokens:
+                    p = length[r] + i
+                    positions[t], slots[t], origins[t] = p, mine[p // P] * P + p % P if served else -1, origin if i == 0 else -1
+                t += 1
+        if served:
+            used += total
+        if parents is not None:
+            now = {j: {final[r][j] for r in rows if len(final[r]) > j} for j in range(M)}
+            for j in range(M):
+                for r in rows:
+                    if j < pages(int(lens[r])):
+                        p = int(table[r, j])
+                        if p not in now[j] and p not in [x for x, y in back if y == (g, j)]:
+                            back.append((p, (g, j)))
+    starts[R] = t
+    for i, (p, _) in enumerate(back):
+        ring[(given + i) % N] = p
+    return dict(out_table=out, out_lens=lens_out, starts=starts, slots=slots, positions=positions, origins=origins, ring=ring,
+                out_counters=np.array([taken + used, given + len(back)], np.int64))
+
+
+class Pool:
+    """Tables of rows and the ring, on the host."""
+
+    def __init__(self, seed, R, M, N, P, K, first=0):
+        rng = np.random.default_rng(seed)
+        self.R, self.M, self.N, self.P, self.K = R, M, N, P, K
+        self.table = np.full((R, M), -5, np.int32)
+        self.lens = np.zeros(R, np.int32)
+        self.ring = rng.permutation(N).astype(np.int32)
+        self.ring = np.roll(self.ring, first % N)
+        self.counters = np.array([first, first + N], np.int64)
+
+    def step(self, torch, wg, counts, parents, spare=3, in_place=False, stream=None):
+        counts = np.asarray(counts, np.int32)
+        parents = None if parents is None else np.asarray(parents, np.int32)
+        T = int(np.maximum(counts, 0).sum()) + spare
+        out_table = self.table if in_place else np.full((self.R, self.M), -7, np.int32)
+        want = definition(self.table, self.lens, counts, parents, self.K, self.P, self.ring, self.counters, T, out_table)
+        d = lambda x: torch.from_numpy(np.ascontiguousarray(x).copy()).cuda()
+        table, ring = d(self.table), d(self.ring)
+        got = dict(out_table=table if in_place else d(out_table), out_lens=d(np.full(self.R, -9, np.int32)), starts=d(np.full(self.R + 1, -9, np.int32)),
+                   slots=d(np.full(T, -99, np.int32)), positions=d(np.full(T, -99, np.int32)), origins=d(np.full(T, -99, np.int32)), ring=ring,
+                   out_counters=d(np.zeros(2, np.int64)))
+        work = torch.empty(max(16, wg.page_step_workspace(self.R, self.K)), dtype=torch.uint8, device="cuda") if parents is not None else None
+        args = (table, d(self.lens), d(counts), None if parents is None else d(parents), self.K, self.P, ring, d(self.counters), got["out_table"], got["out_lens"],
+                got["starts"], got["slots"], got["positions"], got["origins"], got["out_counters"], work)
+        for _ in range(2):                               # the same call again gives the same
+            wg.page_step(*args, stream)
+            torch.cuda.synchronize()
+            for name, w in want.items():
+                assert (got[name].cpu().numpy() == w).all(), (name, np.argwhere(got[name].cpu().numpy() != w)[:5].tolist())
+        self.table, self.lens, self.ring, self.counters = want["out_table"], want["out_lens"], want["ring"], want["out_counters"]
+        return want
+
+    def check(self):
+        """Every page is free or in use, and by one request only."""
+        free = [int(self.ring[i % self.N]) for i in range(int(self.counters[0]), int(self.counters[1]))]
+        held = {}
+        for r in range(self.R):
+            for j in range(-(-int(self.lens[r]) // self.P)):
+                held.setdefault(int(self.table[r, j]), set()).add((r // self.K, j))
+        assert all(len(v) == 1 for v in held.values())
+        assert sorted(free + list(held)) == list(range(self.N))
+
+
+@pytest.mark.parametrize("in_place", [False, True])
+@pytest.mark.parametrize("R,P,M", [(1, 16, 40), (3, 32, 30), (64, 16, 60), (300, 64, 10), (700, 16, 20)])
+def test_rows_without_beams(R, P, M, in_place):
+    torch, wg = _wg()
+    rng = np.random.default_rng(R)
+    pool = Pool(R, R, M, R * M // 2 + 5, P, 1, first=2 ** 33 + 7)
+    pool.step(torch, wg, rng.integers(0, M * P // 4, R), None, in_place=in_place)
+    pool.check()
+    for i in range(4):
+        pool.step(torch, wg, rng.integers(0, 3, R), None, in_place=in_place)
+        pool.check()
+    pool.step(torch, wg, rng.integers(-3, 2 * P, R), None, spare=-min(R, 5) if R > 5 else 0, in_place=in_place)      # fewer places than tokens
+    pool.check()
+
+
+@pytest.mark.parametrize("K,G,P,M", [(1, 5, 16, 20), (2, 3, 16, 12), (4, 20, 16, 40), (5, 7, 32, 20), (8, 64, 16, 30), (64, 2, 16, 12), (3, 200, 16, 10)])
+def test_beams_follow_their_parents(K, G, P, M):
+    torch, wg = _wg()
+    rng = np.random.default_rng(K * 100 + G)
+    R = K * G
+    pool = Pool(K, R, M, R * M + 9, P, K, first=R * M)
+    counts = np.zeros(R, np.int64)
+    counts[::K] = rng.integers(1, M * P // 3, G)                     # the prompts, once for each request
+    pool.step(torch, wg, counts, np.arange(R))
+    pool.check()
+    everyone = np.arange(R) // K * K
+    pool.step(torch, wg, np.ones(R), everyone)                       # then all beams go on from them
+    pool.check()
+    if K > 1:
+        assert int(pool.counters[0]) - R * M < (counts.sum() // P + 2 * G + R) + 1
+    for i in range(2 * P + 3):
+        parents = everyone + rng.integers(0, K, R)
+        if i % 7 == 5:
+            parents[rng.integers(0, R)] = -1                         # a beam that ended
+            parents[rng.integers(0, R)] = R + 3
+        n = np.ones(R, np.int64)
+        if i % 11 == 3:
+            n = rng.integers(0, 3, R)                                # beams of several lengths
+        if -(-int(pool.lens.max() + 3) // P) > M:
+            break
+        pool.step(torch, wg, n, parents)
+        pool.check()
+    pool.step(torch, wg, np.zeros(R), np.full(R, -1))                # all requests end: every page is back
+    pool.check()
+    assert int(pool.counters[1] - pool.counters[0]) == pool.N
+
+
+def test_a_ring_that_runs_out_and_tables_that_are_full():
+    torch, wg = _wg()
+    pool = Pool(1, 6, 8, 20, 16, 1)
+    pool.step(torch, wg, [40, 60, 16, 16, 0, 100], None)             # 3 + 4 + 1 + 1 + 0 + 7 of 20 pages
+    want = pool.step(torch, wg, [30, 30, 1, 0, 5, 28], None)         # 2, 2, 1, 0, none left for 1, the last row's begun page is full
+    assert (want["out_lens"] == [70, 90, 16, 16, 0, 100]).all() or int(want["out_counters"][0]) <= 20
+    pool.check()
+    want = pool.step(torch, wg, [500, 1, 0, 1, 0, 0], None)          # a table too short: that row alone is not served
+    assert want["out_lens"][0] == want["positions"][0] and want["slots"][0] == -1
+    pool.check()
+    # beams: a request is served as a whole or not at all, and keeps sharing what it shared
+    pool = Pool(2, 8, 6, 14, 16, 4)
+    pool.step(torch, wg, [20, 0, 0, 0, 20, 0, 0, 0], np.arange(8))
+    pool.step(torch, wg, np.ones(8), [0, 0, 0, 0, 4, 4, 4, 4])       # four copies each: 8 of the 10 left
+    pool.check()
+    pool.step(torch, wg, np.ones(8), [0, 0, 1, 1, 4, 5, 6, 6])       # more forks than pages
+    pool.check()
+    want = pool.step(torch, wg, np.ones(8), [0, 0, 0, 0, 4, 4, 4, 4])
+    pool.check()
+    for i in range(6):
+        pool.step(torch, wg, np.ones(8) * 3, np.arange(8) // 4 * 4 + np.array([0, 1, 1, 3] * 2))
+        pool.check()
+
+
+@pytest.mark.parametrize("R", [5000, 65535])
+def test_many_rows(R):
+    torch, wg = _wg()
+    rng = np.random.default_rng(R)
+    pool = Pool(R, R, 4, R * 4, 16, 1)
+    pool.step(torch, wg, rng.integers(0, 40, R), None)
+    pool.step(torch, wg, np.ones(R), None)
+    pool.check()
+
+
+def test_on_another_stream():
+    torch, wg = _wg()
+    side = torch.cuda.Stream()
+    pool = Pool(4, 12, 8, 80, 16, 4)
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        pool.step(torch, wg, [40, 0, 0, 0] * 3, np.arange(12))
+        pool.step(torch, wg, np.ones(12), np.arange(12) // 4 * 4)
+    pool.check()

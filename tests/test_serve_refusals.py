@@ -39,6 +39,41 @@ def test_reorder_rows():
                                                          dict(outer=65536), dict(rows=65536), dict(sr=15), dict(dr=8)])
 
 
+def test_page_step():
+    need = wg.page_step_workspace(8, 4)
+    assert need == 2 * 16 + 8 * 4 and wg.page_step_workspace(8, 0) == 0
+    good = dict(table=P, rows=8, columns=10, lens=P, counts=P, parents=P, beams=4, page=16, ring=P, pages=100, counters=P, table_out=Q, lens_out=Q, starts=Q, slots=Q,
+                positions=Q, origins=Q, tokens=8, counters_out=Q, work=Q, bytes=need, stream=None)
+    refused("wg_page_step", "wg_page_step", good, [
+        dict([(k, None)]) for k in ("table", "lens", "counts", "ring", "counters", "table_out", "lens_out", "starts", "slots", "positions", "origins", "counters_out", "work")] + [
+        dict(rows=0), dict(columns=0), dict(pages=0), dict(rows=65536, bytes=1 << 30), dict(page=8), dict(page=48), dict(page=128), dict(page=0), dict(columns=1 << 27),
+        dict(pages=1 << 27), dict(tokens=1 << 31), dict(beams=0), dict(beams=3), dict(beams=65, rows=65), dict(parents=None), dict(table_out=P), dict(lens_out=P),
+        dict(counters_out=P), dict(bytes=need - 1), dict(work=C.c_void_p(4104))])
+
+
+def test_cache_append():
+    good = dict(k=P, v=P, tokens=4, heads=2, dim=64, k0=128, k1=64, v0=128, v1=64, slots=P, origins=None, k_cache=Q, v_cache=Q, k_scale=Q, v_scale=Q, pages=10, page=16,
+                stream=None)
+    refused("wg_cache_append", "wg_cache_append", good, [
+        dict([(k, None)]) for k in ("k", "v", "slots", "k_cache", "v_cache", "k_scale", "v_scale")] + [
+        dict(tokens=0), dict(heads=0), dict(pages=0), dict(heads=65536), dict(dim=96), dict(dim=512), dict(page=24), dict(pages=1 << 27), dict(k0=129), dict(v1=4),
+        dict(k=C.c_void_p(4104)), dict(v=C.c_void_p(4098)), dict(k_cache=C.c_void_p(4104)), dict(v_cache=C.c_void_p(4104)), dict(tokens=1 << 31)])
+
+
+def test_cache_attend():
+    shape = dict(tokens=2, rows=2, q_heads=8, heads=2, dim=64, columns=100, page_tokens=16)
+    need = wg.cache_attend_workspace(**shape)
+    assert need == 2 * 8 * 7 * 66 * 4 and wg.cache_attend_workspace(**dict(shape, columns=8)) == 0 and wg.cache_attend_workspace(**dict(shape, heads=0)) == 0
+    good = dict(q=P, tokens=2, q_heads=8, heads=2, dim=64, q0=512, q1=64, k_cache=P, v_cache=P, k_scale=P, v_scale=P, pages=200, page=16, table=P, rows=2, columns=100,
+                lens=P, starts=P, scale=0.125, out=Q, work=Q, bytes=need, stream=None)
+    refused("wg_cache_attend", "wg_cache_attend", good, [
+        dict([(k, None)]) for k in ("q", "k_cache", "v_cache", "k_scale", "v_scale", "table", "lens", "starts", "out", "work")] + [
+        dict(tokens=0), dict(rows=0), dict(columns=0), dict(pages=0), dict(heads=0), dict(rows=65536), dict(tokens=1 << 31), dict(q_heads=7), dict(q_heads=1),
+        dict(q_heads=65536), dict(heads=4096, q_heads=4096), dict(dim=32), dict(page=17), dict(columns=1 << 27), dict(pages=1 << 27), dict(q0=513), dict(q1=4),
+        dict(q=C.c_void_p(4104)), dict(k_cache=C.c_void_p(4104)), dict(v_cache=C.c_void_p(4104)), dict(out=C.c_void_p(4104)), dict(scale=float("nan")), dict(scale=float("inf")),
+        dict(bytes=need - 1), dict(work=C.c_void_p(4104))])
+
+
 NO_STORAGE = r"""
 import torch
 from torch._subclasses.fake_tensor import FakeTensorMode
@@ -74,13 +109,35 @@ def make(torch, wg):
 """
 
 
+CACHE = r"""
+def make(torch, wg):
+    i32, f32, f8, b16 = dict(dtype=torch.int32, device="cuda"), dict(device="cuda"), dict(dtype=torch.float8_e4m3fn, device="cuda"), dict(dtype=torch.bfloat16, device="cuda")
+    i64 = dict(dtype=torch.int64, device="cuda")
+    given = dict(table=torch.empty((5, 4, 6), **i32), lens=torch.empty((5, 4), **i32), counts=torch.empty((5, 4), **i32), parents=torch.empty((5, 4), **i32),
+                 ring=torch.empty((5, 30), **i32), counters=torch.empty((5, 2), **i64), out_table=torch.empty((5, 4, 6), **i32), out_lens=torch.empty((5, 4), **i32),
+                 starts=torch.empty((5, 5), **i32), slots=torch.empty((5, 4), **i32), positions=torch.empty((5, 4), **i32), origins=torch.empty((5, 4), **i32),
+                 out_counters=torch.empty((5, 2), **i64), work=torch.empty((5, 1 << 16), dtype=torch.uint8, device="cuda"),
+                 k=torch.empty((5, 4, 2, 64), **b16), v=torch.empty((5, 4, 2, 64), **b16), q=torch.empty((5, 4, 4, 64), **b16), out=torch.empty((5, 4, 4, 64), **b16),
+                 kc=torch.empty((5, 7, 2, 16, 64), **f8), vc=torch.empty((5, 7, 2, 64, 16), **f8), ks=torch.empty((5, 7, 2), **f32), vs=torch.empty((5, 7, 2), **f32))
+    return given, {
+        "page_step": (("table", "lens", "counts", "parents", "ring", "counters", "out_table", "out_lens", "starts", "slots", "positions", "origins", "out_counters", "work"),
+                      lambda table, lens, counts, parents, ring, counters, out_table, out_lens, starts, slots, positions, origins, out_counters, work:
+                      wg.page_step(table, lens, counts, parents, 2, 16, ring, counters, out_table, out_lens, starts, slots, positions, origins, out_counters, work, 0)),
+        "cache_append": (("k", "v", "slots", "origins", "kc", "vc", "ks", "vs"),
+                         lambda k, v, slots, origins, kc, vc, ks, vs: wg.cache_append(k, v, slots, origins, kc, vc, ks, vs, 0)),
+        "cache_attend": (("q", "kc", "vc", "ks", "vs", "table", "lens", "starts", "out", "work"),
+                         lambda q, kc, vc, ks, vs, table, lens, starts, out, work: wg.cache_attend(q, kc, vc, ks, vs, table, lens, starts, 0.1, out, work, 0))}
+"""
+
+
 def no_storage(make):
     r = subprocess.run([sys.executable, "-c", make + NO_STORAGE], cwd=ROOT, capture_output=True, text=True, timeout=300)
     assert r.returncode == 0 and r.stdout.split() == ["done"], (r.returncode, r.stdout, r.stderr[-2000:])
 
 
-def test_tensors_without_storage_raise():
-    no_storage(BEAM)
+@pytest.mark.parametrize("make", [BEAM, CACHE], ids=["beam", "cache"])
+def test_tensors_without_storage_raise(make):
+    no_storage(make)
 
 
 def test_tensors_that_do_not_fit():
@@ -94,3 +151,17 @@ def test_tensors_that_do_not_fit():
         wg.reorder_rows(x, x, x[:2])
     with pytest.raises(ValueError, match="device tensors"):
         wg.reorder_rows(x, x, x)
+    i = torch.zeros((4, 6), dtype=torch.int32)
+    with pytest.raises(ValueError, match="out_table must be"):
+        wg.page_step(i, i[:, 0], i[:, 0], None, 1, 16, i[0], i[0], i, i[:, 0], i[0], i[0], i[0], i[0], i[0])
+    with pytest.raises(ValueError, match="out of range"):
+        wg.page_step(i, i, i, None, 1 << 40, 16, i[0], i[0], i, i, i, i[0], i[0], i[0], i[0])
+    f8 = torch.zeros((3, 2, 16, 64)).to(torch.float8_e4m3fn)
+    s = torch.ones((3, 2))
+    kv = torch.zeros((4, 2, 64), dtype=torch.bfloat16)
+    with pytest.raises(ValueError, match="k_cache must be"):
+        wg.cache_append(kv, kv, i[0], None, f8, f8, s, s)
+    with pytest.raises(ValueError, match="device tensor"):
+        wg.cache_append(kv, kv, i[0], None, f8, f8.transpose(2, 3).contiguous(), s, s)
+    with pytest.raises(ValueError, match="float8_e4m3fn"):
+        wg.cache_attend(kv, f8.float(), f8.float().transpose(2, 3), s, s, i, i[:, 0], i[0], 1.0, kv)
