@@ -396,8 +396,8 @@ int wg_reorder_rows(const void *d_src, void *d_dst, const int32_t *d_parents, ui
  * as if it had not been there).  d_table_out [rows][columns] receives the rows' pages; its other entries stay.  Without parents
  * (d_parents NULL, beams 1) d_table_out may be d_table, which then is added to; else it must not.  d_lens_out and d_counters_out
  * are not their inputs: the same call again gives the same result.  The sum of d_counts must be below 2^31.  rows <= 65535, beams <= 64;
- * with d_parents, d_workspace is wg_page_step_workspace(rows, beams) bytes, 16-byte aligned.  One kernel, or with parents two. */
-uint64_t wg_page_step_workspace(uint32_t rows, uint32_t beams);
+ * with d_parents, d_workspace is wg_page_step_workspace(rows, beams, columns) bytes, 16-byte aligned.  One kernel, or with parents two. */
+uint64_t wg_page_step_workspace(uint32_t rows, uint32_t beams, uint32_t columns);
 int wg_page_step(const int32_t *d_table, uint32_t rows, uint32_t columns, const int32_t *d_lens, const int32_t *d_counts,
                  const int32_t *d_parents, uint32_t beams, uint32_t page_tokens, int32_t *d_ring, uint32_t pages, const uint64_t *d_counters,
                  int32_t *d_table_out, int32_t *d_lens_out, int32_t *d_starts, int32_t *d_slots, int32_t *d_positions, int32_t *d_origins,

@@ -133,7 +133,7 @@ def load_library():
     L.wg_beam_select_workspace.restype = u64
     L.wg_beam_select.argtypes = [vp, C.c_int, u32, u32, i64, vp, u32, vp, vp, vp, vp, vp, vp, vp, u64, vp]
     L.wg_reorder_rows.argtypes = [vp, vp, vp, u32, u32, u64, i64, i64, i64, i64, vp]
-    L.wg_page_step_workspace.argtypes = [u32, u32]
+    L.wg_page_step_workspace.argtypes = [u32, u32, u32]
     L.wg_page_step_workspace.restype = u64
     L.wg_page_step.argtypes = [vp, u32, u32, vp, vp, vp, u32, u32, vp, u32, vp, vp, vp, vp, vp, vp, vp, u32, vp, vp, u64, vp]
     L.wg_cache_append.argtypes = [vp, vp, u32, u32, u32, i64, i64, i64, i64, vp, vp, vp, vp, vp, vp, u32, u32, vp]
@@ -464,9 +464,9 @@ def reorder_rows(src, parents, dst, axis=0, stream=None):
     (_native or _load_native()).reorder_rows(src, parents, dst, axis, stream)
 
 
-def page_step_workspace(rows, beams):
+def page_step_workspace(rows, beams, columns):
     """wg_page_step_workspace: bytes of device workspace a page_step call with parents needs."""
-    return int(load_library().wg_page_step_workspace(rows, beams))
+    return int(load_library().wg_page_step_workspace(rows, beams, columns))
 
 
 def page_step(table, lens, counts, parents, beams, page_tokens, ring, counters, out_table, out_lens, starts, slots, positions, origins, out_counters,

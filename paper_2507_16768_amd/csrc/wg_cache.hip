@@ -51,8 +51,13 @@ __device__ __forceinline__ float scale_for(float top)
 }
 
 // ---------------------------------------------------------------------------------------------
-// append.  Tokens that lie one behind the other in a page are one run, which a wavefront takes for a head: their largest magnitude, the page's scale, then
-// the tokens; the earlier tokens of the page are rewritten where the scale grows or where they come from another page.
+// append.  Tokens that lie one behind the other in a page are one run, which a wavefront takes for a head, and for keys or values: their largest
+// magnitude, the page's scale, then the tokens; the earlier tokens of the page are rewritten where the scale grows or where they come from another page.
+//
+// A wavefront looks at 64 tokens' slots and at the 64 behind them, a lane each, and finds the runs that begin among the first by ballots: prompts have few of them, rows
+// that take a token each have 64.  (A wavefront for every token, head and kind, of which all but those of first tokens left at once, took 99 us for 11,000 tokens
+// of prompts, 8 heads of 128.)  Runs are dealt out to as many wavefronts as the chip holds.  Numbers stay in registers between the
+// two looks at them, and what comes from another page is asked for together with them.
 struct AppendArgs {
     const uint16_t *x[2];                            // keys, values: [token][head][dim]
     int64_t token_stride[2], head_stride[2];         // elements
@@ -62,111 +67,177 @@ struct AppendArgs {
     uint32_t tokens, heads, pages, shift;
 };
 
-template <uint32_t kD>
-__device__ __forceinline__ void append_run(const AppendArgs &a, uint32_t which, uint32_t t, uint32_t h)
+// Where a run's tokens go: tokens o .. o + n of a page, behind `o` earlier ones that lie in page `source`.
+struct Run { uint32_t token, page, source, o, n; };
+
+template <uint32_t kD, bool kValues>
+__device__ __forceinline__ void append_run(const AppendArgs &a, const Run &run, uint32_t h)
 {
-    const uint32_t lane = threadIdx.x & 63u, P = 1u << a.shift;
-    const uint32_t slot = (uint32_t)a.slots[t], o = slot & (P - 1u), page = slot >> a.shift;
-    if (page >= a.pages) return;                     // (also a slot of -1)
-    if (o && t && (uint32_t)a.slots[t - 1u] == slot - 1u) return;          // in a run that began before
-    const bool mine = lane < P - o && lane < a.tokens - t && (uint32_t)a.slots[t + (lane < a.tokens - t ? lane : 0u)] == slot + lane;
-    const unsigned long long others = ~__ballot(mine);
-    const uint32_t n = others ? (uint32_t)__builtin_ctzll(others) : 64u, end = o + n;
-    const uint32_t origin = a.origins ? (uint32_t)a.origins[t] : 0xFFFFFFFFu, source = origin < a.pages ? origin : page;
-    const uint16_t *x = a.x[which] + (int64_t)t * a.token_stride[which] + (int64_t)h * a.head_stride[which];
-    const int64_t step = a.token_stride[which];
-    uint8_t *to = a.cache[which] + ((size_t)page * a.heads + h) * (P * kD);
-    const uint8_t *from = a.cache[which] + ((size_t)source * a.heads + h) * (P * kD);
-    const float was = o ? a.scale[which][(size_t)source * a.heads + h] : 0.f;
-    float top = 0.f;
-    constexpr uint32_t kLanes = kD / 8u, kTokens = 64u / kLanes;           // keys: eight dims to a lane
-    constexpr uint32_t kOwn = kD / 64u;                                    // values: dims of a lane
-    const uint32_t key_token = lane / kLanes, key_dim = lane % kLanes * 8u, value_dim = lane * kOwn;
-    auto values_of = [&](uint32_t token, float (&v)[kOwn]) {
-        const uint16_t *p = x + (int64_t)token * step + value_dim;
-        if (kOwn == 1u) v[0] = __uint_as_float((uint32_t)*p << 16);
+    constexpr uint32_t kWhich = kValues ? 1u : 0u;
+    constexpr uint32_t kLanes = kD / 8u, kTokens = 64u / kLanes;           // keys: eight dims to a lane, so many tokens to a load
+    constexpr uint32_t kOwn = kD / 64u, kWords = (kOwn + 1u) / 2u;         // values: dims of a lane, and the words that they are
+    constexpr uint32_t kHeld = kD == 256u ? 16u : 32u;                     // tokens that stay in registers
+    constexpr uint32_t kLoads = kValues ? kHeld : kHeld / kTokens, kLoadWords = kValues ? kWords : 4u, kLoadTokens = kValues ? 1u : kTokens;
+    constexpr uint32_t kGroup = kValues ? 8u : kLoads < 4u ? kLoads : 4u;  // loads that one question is asked for
+    constexpr uint32_t kEarly = 4;                                         // sixteen bytes each of the earlier tokens
+    const uint32_t lane = threadIdx.x & 63u, P = 1u << a.shift, o = run.o, n = run.n, end = o + n;
+    const uint16_t *x = a.x[kWhich] + (int64_t)run.token * a.token_stride[kWhich] + (int64_t)h * a.head_stride[kWhich];
+    const int64_t step = a.token_stride[kWhich];
+    uint8_t *to = a.cache[kWhich] + ((size_t)run.page * a.heads + h) * (P * kD);
+    const uint8_t *from = a.cache[kWhich] + ((size_t)run.source * a.heads + h) * (P * kD);
+    const uint32_t own_token = kValues ? 0u : lane / kLanes, own_dim = kValues ? lane * kOwn : lane % kLanes * 8u;
+    auto load = [&](uint32_t token, uint32_t (&w)[kLoadWords]) {
+        const uint16_t *p = x + (int64_t)token * step + own_dim;
+        if (!kValues) { const Word4 v = *reinterpret_cast<const Word4 *>(p); for (uint32_t i = 0; i < 4u; i++) w[i % kLoadWords] = v[i]; }
+        else if (kOwn == 1u) w[0] = (uint32_t)*p << 16;                    // (the lower half is a zero)
         else
-#pragma unroll
-            for (uint32_t i = 0; i < kOwn / 2u; i++) {
-                const uint32_t two = reinterpret_cast<const uint32_t *>(p)[i];
-                v[2u * i] = low(two); v[2u * i + 1u] = high(two);
-            }
+            for (uint32_t i = 0; i < kWords; i++) w[i] = reinterpret_cast<const uint32_t *>(p)[i];
     };
-    if (which == 0u) {
-#pragma unroll 4
-        for (uint32_t i = key_token; i < n; i += kTokens) {
-            const Word4 w = *reinterpret_cast<const Word4 *>(x + (int64_t)i * step + key_dim);
+    const bool held = n <= kHeld;
+    uint32_t w[kLoads][kLoadWords];
+    float top = 0.f;
+    if (held)
 #pragma unroll
-            for (uint32_t j = 0; j < 4u; j++) { top = top_of(top, low(w[j])); top = top_of(top, high(w[j])); }
+        for (uint32_t j = 0; j < kLoads; j += kGroup) {
+            if (j * kLoadTokens >= n) break;
+#pragma unroll
+            for (uint32_t i = j; i < j + kGroup; i++) {                    // (behind the last token the last again)
+                const uint32_t token = i * kLoadTokens + own_token;
+                load(token < n ? token : n - 1u, w[i]);
+            }
+        }
+    const float was = o ? a.scale[kWhich][(size_t)run.source * a.heads + h] : 0.f;
+    // the earlier tokens: of keys the page's first bytes, of values the first bytes of every dim
+    const bool moved = o && run.source != run.page, ahead = moved && P * kD <= kEarly * 1024u;
+    Word4 early[kEarly] = {};
+    const uint32_t early_units = kValues ? 0u : o * kD / 16u;
+    if (ahead)
+#pragma unroll
+        for (uint32_t i = 0; i < kEarly; i++) {
+            if (!kValues) { if (i * 64u + lane < early_units) early[i] = reinterpret_cast<const Word4 *>(from)[i * 64u + lane]; }
+            else if (i / kOwn * 16u < o) early[i] = *reinterpret_cast<const Word4 *>(from + (size_t)(own_dim + i % kOwn) * P + i / kOwn * 16u);
+        }
+    if (held) {
+#pragma unroll
+        for (uint32_t j = 0; j < kLoads; j += kGroup) {
+            if (j * kLoadTokens >= n) break;
+#pragma unroll
+            for (uint32_t i = j; i < j + kGroup; i++)
+#pragma unroll
+                for (uint32_t k = 0; k < kLoadWords; k++) { top = top_of(top, low(w[i][k])); top = top_of(top, high(w[i][k])); }
         }
     } else {
-#pragma unroll 8
-        for (uint32_t i = 0; i < n; i++) {
-            float v[kOwn];
-            values_of(i, v);
+#pragma unroll 4
+        for (uint32_t i = own_token; i < n; i += kLoadTokens) {
+            uint32_t v[kLoadWords];
+            load(i, v);
 #pragma unroll
-            for (uint32_t j = 0; j < kOwn; j++) top = top_of(top, v[j]);
+            for (uint32_t k = 0; k < kLoadWords; k++) { top = top_of(top, low(v[k])); top = top_of(top, high(v[k])); }
         }
     }
 #pragma unroll
     for (int s = 32; s > 0; s >>= 1) top = __builtin_fmaxf(top, __shfl_xor(top, s));
     const float now = __builtin_fmaxf(scale_for(top), was), inverse = 1.f / now, ratio = was / now;
-    const bool again = o && (source != page || now != was);                // the earlier tokens are written too
-    if (lane == 0u) a.scale[which][(size_t)page * a.heads + h] = now;
-    if (which == 0u) {
-        if (again)
-            for (uint32_t u = lane; u < o * kD / 16u; u += 64u) {
-                Word4 w = reinterpret_cast<const Word4 *>(from)[u];
+    const bool again = o && (moved || now != was);                         // the earlier tokens are written too
+    if (lane == 0u) a.scale[kWhich][(size_t)run.page * a.heads + h] = now;
+    if (!kValues) {
+        if (again) {
+            auto put = [&](uint32_t u, Word4 v) {
 #pragma unroll
-                for (uint32_t j = 0; j < 4u; j++) w[j] = rescaled(w[j], ratio);
-                reinterpret_cast<Word4 *>(to)[u] = w;
-            }
-#pragma unroll 4
-        for (uint32_t i = key_token; i < n; i += kTokens) {
-            const Word4 w = *reinterpret_cast<const Word4 *>(x + (int64_t)i * step + key_dim);
+                for (uint32_t k = 0; k < 4u; k++) v[k] = rescaled(v[k], ratio);
+                reinterpret_cast<Word4 *>(to)[u] = v;
+            };
+            if (ahead) {
+#pragma unroll
+                for (uint32_t i = 0; i < kEarly; i++) if (i * 64u + lane < early_units) put(i * 64u + lane, early[i]);
+            } else
+                for (uint32_t u = lane; u < early_units; u += 64u) put(u, reinterpret_cast<const Word4 *>(from)[u]);
+        }
+        auto put = [&](uint32_t token, const uint32_t (&v)[kLoadWords]) {
             Word2 r;
 #pragma unroll
-            for (uint32_t j = 0; j < 2u; j++)
-                r[j] = to_bytes(low(w[2u * j]) * inverse, high(w[2u * j]) * inverse, low(w[2u * j + 1u]) * inverse, high(w[2u * j + 1u]) * inverse);
-            *reinterpret_cast<Word2 *>(to + (o + i) * kD + key_dim) = r;
+            for (uint32_t k = 0; k < 2u; k++)
+                r[k] = to_bytes(low(v[2u * k % kLoadWords]) * inverse, high(v[2u * k % kLoadWords]) * inverse, low(v[(2u * k + 1u) % kLoadWords]) * inverse,
+                                high(v[(2u * k + 1u) % kLoadWords]) * inverse);
+            *reinterpret_cast<Word2 *>(to + (o + token) * kD + own_dim) = r;
+        };
+        if (held) {
+#pragma unroll
+            for (uint32_t j = 0; j < kLoads; j += kGroup) {
+                if (j * kLoadTokens >= n) break;
+#pragma unroll
+                for (uint32_t i = j; i < j + kGroup; i++)
+                    if (i * kLoadTokens + own_token < n) put(i * kLoadTokens + own_token, w[i]);
+            }
+        } else {
+#pragma unroll 4
+            for (uint32_t i = own_token; i < n; i += kLoadTokens) {
+                uint32_t v[kLoadWords];
+                load(i, v);
+                put(i, v);
+            }
         }
         return;
     }
-    // values: sixteen tokens of a dim at a time
-    const uint32_t begin = again ? 0u : o;
-    for (uint32_t c = begin & ~15u; c < end; c += 16u) {
-        float v[16][kOwn];
-#pragma unroll
-        for (uint32_t j = 0; j < 16u; j++) {
-#pragma unroll
-            for (uint32_t d = 0; d < kOwn; d++) v[j][d] = 0.f;
-            if (c + j >= o && c + j < end) values_of(c + j - o, v[j]);
-        }
+    // Values: sixteen tokens of a dim at a time.  at(token, d): the token's number in the lane's dim d.
+    auto column = [&](uint32_t c, auto at) {
+        const uint32_t begin = again ? 0u : o;
 #pragma unroll
         for (uint32_t d = 0; d < kOwn; d++) {
-            uint8_t *at = to + (size_t)(value_dim + d) * P + c;
+            uint8_t *out = to + (size_t)(own_dim + d) * P + c;
             Word4 r;
 #pragma unroll
-            for (uint32_t w = 0; w < 4u; w++) r[w] = to_bytes(v[4u * w][d] * inverse, v[4u * w + 1u][d] * inverse, v[4u * w + 2u][d] * inverse, v[4u * w + 3u][d] * inverse);
+            for (uint32_t k = 0; k < 4u; k++)
+                r[k] = to_bytes(at(4u * k, d) * inverse, at(4u * k + 1u, d) * inverse, at(4u * k + 2u, d) * inverse, at(4u * k + 3u, d) * inverse);
             if (again && c < o) {
-                const Word4 old = *reinterpret_cast<const Word4 *>(from + (size_t)(value_dim + d) * P + c);
+                Word4 old;
+                if (ahead) {
+                    // (by masks: a choice between registers by a number is one between addresses, which puts them into memory)
+                    old = Word4{0u, 0u, 0u, 0u};
 #pragma unroll
-                for (uint32_t w = 0; w < 4u; w++) {
-                    const uint32_t early = o <= c + 4u * w ? 0u : o - c - 4u * w;          // bytes of the word from before
-                    const uint32_t keep = early >= 4u ? 0xFFFFFFFFu : (1u << (8u * early)) - 1u;
-                    r[w] = (rescaled(old[w], ratio) & keep) | (r[w] & ~keep);
+                    for (uint32_t i = 0; i < kEarly / kOwn; i++) old |= early[i * kOwn + d] & (c == 16u * i ? 0xFFFFFFFFu : 0u);
+                } else old = *reinterpret_cast<const Word4 *>(from + (size_t)(own_dim + d) * P + c);
+#pragma unroll
+                for (uint32_t k = 0; k < 4u; k++) {
+                    const uint32_t before = o <= c + 4u * k ? 0u : o - c - 4u * k;         // bytes of the word that are earlier tokens'
+                    const uint32_t keep = before >= 4u ? 0xFFFFFFFFu : (1u << (8u * before)) - 1u;
+                    r[k] = (rescaled(old[k], ratio) & keep) | (r[k] & ~keep);
                 }
             }
-            if (begin <= c && end >= c + 16u) { *reinterpret_cast<Word4 *>(at) = r; continue; }
+            if (begin <= c && end >= c + 16u) { *reinterpret_cast<Word4 *>(out) = r; continue; }
 #pragma unroll
-            for (uint32_t w = 0; w < 4u; w++) {
-                const uint32_t b0 = c + 4u * w;
-                if (begin <= b0 && end >= b0 + 4u) { reinterpret_cast<uint32_t *>(at)[w] = r[w]; continue; }
+            for (uint32_t k = 0; k < 4u; k++) {
+                const uint32_t b0 = c + 4u * k;
+                if (begin <= b0 && end >= b0 + 4u) { reinterpret_cast<uint32_t *>(out)[k] = r[k]; continue; }
 #pragma unroll
                 for (uint32_t i = 0; i < 4u; i++)
-                    if (b0 + i >= begin && b0 + i < end) at[4u * w + i] = (uint8_t)(r[w] >> (8u * i));
+                    if (b0 + i >= begin && b0 + i < end) out[4u * k + i] = (uint8_t)(r[k] >> (8u * i));
             }
         }
+    };
+    auto number = [&](uint32_t word, uint32_t d) { return kOwn > 1u && d % 2u == 0u ? low(word) : high(word); };
+    if (held && (o & 15u) == 0u) {
+        // from the registers: token i of the run is number i % 16 of its column
+        if (again) for (uint32_t c = 0; c < o; c += 16u) column(c, [](uint32_t, uint32_t) { return 0.f; });
+#pragma unroll
+        for (uint32_t c = 0; c < kHeld; c += 16u)
+            if (c < n) column(o + c, [&](uint32_t i, uint32_t d) { return number(w[(c + i) % kLoads][d / 2u % kLoadWords], d); });
+        return;
+    }
+    for (uint32_t c = (again ? 0u : o) & ~15u; c < end; c += 16u) {
+        uint32_t v[16][kLoadWords];
+#pragma unroll
+        for (uint32_t i = 0; i < 16u; i++) {
+#pragma unroll
+            for (uint32_t k = 0; k < kLoadWords; k++) v[i][k] = 0u;
+            if (c + i >= o && c + i < end) {
+                if (n == 1u)
+#pragma unroll
+                    for (uint32_t k = 0; k < kLoadWords; k++) v[i][k] = w[0][k];
+                else load(c + i - o, v[i]);
+            }
+        }
+        column(c, [&](uint32_t i, uint32_t d) { return number(v[i][d / 2u % kLoadWords], d); });
     }
 }
 
@@ -175,8 +246,30 @@ template <uint32_t kD>
 __global__ void __launch_bounds__(kAppendWaves * 64u)
 append_kernel(const AppendArgs a)
 {
-    const uint32_t h = blockIdx.y * kAppendWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    if (h < a.heads) append_run<kD>(a, blockIdx.z, blockIdx.x, h);
+    const uint32_t lane = threadIdx.x & 63u, P = 1u << a.shift, first = blockIdx.x * 64u, t = first + lane;
+    const uint32_t none = 0xFFFFFFFFu;
+    const uint32_t slot = t < a.tokens ? (uint32_t)a.slots[t] : none, later = t + 64u < a.tokens ? (uint32_t)a.slots[t + 64u] : none;
+    const uint32_t ahead = first ? (uint32_t)a.slots[first - 1u] : none;
+    const uint32_t origin = a.origins && t < a.tokens ? (uint32_t)a.origins[t] : none;
+    const uint32_t up = __shfl_up(slot, 1), last = __shfl(slot, 63), up_later = __shfl_up(later, 1);
+    const uint32_t before = lane ? up : ahead, before_later = lane ? up_later : last;
+    // tokens that go on with the run of the one before them (a slot of none does not, and begins none)
+    const bool goes = (slot & (P - 1u)) && slot == before + 1u && slot >> a.shift < a.pages && before != none;
+    const bool goes_later = (later & (P - 1u)) && later == before_later + 1u && later >> a.shift < a.pages && before_later != none;
+    const unsigned long long begins = __ballot(slot >> a.shift < a.pages && !goes), on = __ballot(goes), on_later = __ballot(goes_later);
+    const uint32_t items = (uint32_t)__popcll(begins) * a.heads * 2u;
+    const uint32_t rank = (uint32_t)__popcll(begins & ((1ull << lane) - 1ull));
+    for (uint32_t i = blockIdx.y * kAppendWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); i < items; i += gridDim.y * kAppendWaves) {
+        const uint32_t which = i & 1u, h = (i >> 1) % a.heads, nth = (i >> 1) / a.heads;
+        const uint32_t at = (uint32_t)__builtin_ctzll(__ballot((begins >> lane & 1ull) && rank == nth));
+        // its length: how many of the next tokens go on
+        const unsigned long long rest = at == 63u ? on_later : on >> (at + 1u) | on_later << (63u - at);
+        const uint32_t follow = ~rest ? (uint32_t)__builtin_ctzll(~rest) : 64u;
+        const uint32_t s = __builtin_amdgcn_readlane(slot, at), from = __builtin_amdgcn_readlane(origin, at), page = s >> a.shift;
+        const Run run{first + at, page, from < a.pages ? from : page, s & (P - 1u), follow + 1u};
+        if (which) append_run<kD, true>(a, run, h);
+        else append_run<kD, false>(a, run, h);
+    }
 }
 
 hipError_t launch_cache_append(const void *k, const void *v, uint32_t tokens, uint32_t heads, uint32_t dim, int64_t k_token, int64_t k_head, int64_t v_token,
@@ -185,7 +278,9 @@ hipError_t launch_cache_append(const void *k, const void *v, uint32_t tokens, ui
 {
     const AppendArgs a{{static_cast<const uint16_t *>(k), static_cast<const uint16_t *>(v)}, {k_token, v_token}, {k_head, v_head}, {k_cache, v_cache},
                        {k_scale, v_scale}, slots, origins, tokens, heads, pages, shift};
-    const dim3 grid(tokens, (heads + kAppendWaves - 1u) / kAppendWaves, 2u), block(kAppendWaves * 64u);
+    // some 8,192 wavefronts, no more than there can be runs
+    const uint32_t blocks = (tokens + 63u) / 64u, want = (2048u + blocks - 1u) / blocks, most = (64u * heads * 2u + kAppendWaves - 1u) / kAppendWaves;
+    const dim3 grid(blocks, want < most ? want : most), block(kAppendWaves * 64u);
     return launch(dim == 64u ? append_kernel<64> : dim == 128u ? append_kernel<128> : append_kernel<256>, grid, block, 0, s, nullptr, a);
 }
 

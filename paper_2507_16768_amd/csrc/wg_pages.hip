@@ -3,8 +3,9 @@
 //
 // All of it is whole numbers: prefix sums over rows of pages needed, pages released and tokens.  Bound by launches and trips to memory, not by
 // bytes: rows wait for the sums of the rows before them, which every workgroup works out by itself from the lengths (a few KB in the L2) in place of
-// waiting for another.  Where rows follow parents, a first kernel counts for each request what it needs and releases (page_count_kernel), a workgroup for
-// each; the second (page_kernel) sums that up and writes.
+// waiting for another.  Where rows follow parents, a first kernel counts what each request needs and releases (page_count_kernel); the second
+// (page_beam_kernel) sums that up and writes.  A workgroup of either takes 256 columns of a request's tables, which it holds in LDS: a thread's loads of all rows are
+// in flight together, and what it looks for among the rows of a column it finds there.
 //
 // A row's new table is its parent's whole one, so that within a request a page is referred to at one place of the tables only, and an old row with a
 // child keeps all of its pages but for a begun one that all of its children copy.  Only what lies in the tables of rows without children is compared.
@@ -17,64 +18,94 @@ namespace wg {
 
 constexpr uint32_t kPageThreads = 256, kPageWaves = kPageThreads / 64u;
 
-// What a request needs: pages (kTooLong: a table that would not hold them), pages given back whatever becomes of it and those given back
-// where it is served, tokens.
-struct GroupNeed { uint32_t pages, released, released_served, tokens; };
+// What a request needs: pages (kTooLong: a table that would not hold them), and its tokens.
+struct GroupNeed { uint32_t pages, tokens; };
+// Pages that a request gives back from some columns of its tables: whatever becomes of it, and where it is served besides.
+struct Back { uint32_t always, served; };
 constexpr uint32_t kTooLong = 0xFFFFFFFFu;
+
+// Columns that a workgroup takes of a request's tables: as many as it has threads, half as many where the rows would fill more than 32 KB of LDS.
+static __host__ __device__ inline uint32_t columns_of(uint32_t K) { return K <= 32u ? kPageThreads : kPageThreads / 2u; }
 
 // The rows of a request before the step, after they took over their parents' tables.
 struct Rows {
-    int32_t source[kBeamMax];                        // the row whose table it takes; -1: none
+    int32_t source[kBeamMax];                        // the row of the request whose table it takes; -1: none
     uint32_t length[kBeamMax], have[kBeamMax], count[kBeamMax];    // of the new row: tokens, pages, tokens to come
     uint32_t old_have[kBeamMax], col[kBeamMax];      // of the old row: pages; the place of the page that its children begin in
     uint32_t child[kBeamMax], all_fork[kBeamMax];    // of the old row: has children; all of them copy their begun page
     uint32_t fork[kBeamMax];                         // the new row copies its begun page
-    uint32_t need[kBeamMax];
+    uint32_t need[kBeamMax], want[kBeamMax];         // of the new row: pages to be handed out, pages in all
 };
 
 __device__ __forceinline__ uint32_t tokens_of(int32_t n, uint32_t most) { return n < 0 ? 0u : (uint32_t)n < most ? (uint32_t)n : most; }
 
-__device__ __forceinline__ void read_rows(Rows &g, const int32_t *lens, const int32_t *counts, const int32_t *parents, uint32_t row0, uint32_t K, uint32_t M, uint32_t shift)
+// The request's columns [j0, j0 + width) to LDS, row by row, a column to a thread; nobody else reads it.
+__device__ __forceinline__ void read_columns(int32_t *ids, const int32_t *table, uint32_t row0, uint32_t K, uint32_t M, uint32_t j0, uint32_t width)
+{
+    const uint32_t tid = threadIdx.x, j = j0 + tid;
+    if (tid >= width || j >= M) return;
+    uint32_t k = 0;
+    for (; k + 8u <= K; k += 8u) {
+        int32_t x[8];
+#pragma unroll
+        for (uint32_t i = 0; i < 8u; i++) x[i] = table[(size_t)(row0 + k + i) * M + j];
+#pragma unroll
+        for (uint32_t i = 0; i < 8u; i++) ids[(k + i) * width + tid] = x[i];
+    }
+    for (; k < K; k++) ids[k * width + tid] = table[(size_t)(row0 + k) * M + j];
+}
+
+// Fills in g (kFind: and finds the forks; else they are read).  The whole workgroup calls it; it ends behind a barrier.
+template <bool kFind>
+__device__ __forceinline__ void read_rows(Rows &g, const int32_t *table, const int32_t *lens, const int32_t *counts, const int32_t *parents, const uint32_t *forks,
+                                          uint32_t row0, uint32_t K, uint32_t M, uint32_t shift)
 {
     const uint32_t k = threadIdx.x, page = 1u << shift;
     if (k < K) {
-        const int32_t p = parents[row0 + k];
-        const bool there = (uint32_t)p - row0 < K;
-        g.source[k] = there ? p : -1;
-        g.length[k] = there ? tokens_of(lens[p], M << shift) : 0u;
-        g.count[k] = tokens_of(counts[row0 + k], 0x7FFFFFFFu);
-        g.have[k] = (g.length[k] + page - 1u) >> shift;
+        const int32_t p = parents[row0 + k] - (int32_t)row0;
+        const bool there = (uint32_t)p < K;
         const uint32_t old = tokens_of(lens[row0 + k], M << shift);
+        g.source[k] = there ? p : -1;
+        g.count[k] = tokens_of(counts[row0 + k], 0x7FFFFFFFu);
         g.old_have[k] = (old + page - 1u) >> shift;
         g.col[k] = old >> shift;
+        g.length[k] = there ? tokens_of(lens[row0 + (there ? p : 0)], M << shift) : 0u;
+        g.have[k] = (g.length[k] + page - 1u) >> shift;
         g.child[k] = 0u;
         g.all_fork[k] = 1u;
+        g.fork[k] = kFind ? 0u : forks[row0 + k];
     }
+    __syncthreads();
+    if (kFind) {
+        // a begun page that another row has too
+        for (uint32_t i = threadIdx.x; i < K * K; i += kPageThreads) {
+            const uint32_t mine = i / K, other = i % K, c = g.length[mine] >> shift;
+            if (mine == other || !g.count[mine] || !(g.length[mine] & (page - 1u)) || g.have[other] <= c) continue;
+            if (table[(size_t)(row0 + g.source[mine]) * M + c] == table[(size_t)(row0 + g.source[other]) * M + c]) g.fork[mine] = 1u;
+        }
+        __syncthreads();
+    }
+    if (k < K) {
+        for (uint32_t c = 0; c < K; c++)
+            if (g.source[c] == (int32_t)k) { g.child[k] = 1u; g.all_fork[k] &= g.fork[c]; }
+        g.want[k] = (uint32_t)(((uint64_t)g.length[k] + g.count[k] + page - 1u) >> shift);
+        g.need[k] = g.fork[k] + g.want[k] - g.have[k];
+    }
+    __syncthreads();
 }
 
-// (after the forks are known; between two barriers)
-__device__ __forceinline__ void follow_rows(Rows &g, uint32_t row0, uint32_t K, uint32_t shift)
-{
-    const uint32_t k = threadIdx.x, page = 1u << shift;
-    if (k >= K) return;
-    for (uint32_t c = 0; c < K; c++)
-        if (g.source[c] == (int32_t)(row0 + k)) { g.child[k] = 1u; g.all_fork[k] &= g.fork[c]; }
-    const uint64_t all = (uint64_t)g.length[k] + g.count[k];
-    g.need[k] = g.fork[k] + (uint32_t)((all + page - 1u) >> shift) - g.have[k];
-}
-
-// Calls gone(b, id, whatever) for the pages of column j that no new row refers to, in the order of the old rows; whatever: they go whether or not the request
-// is served.
+// Calls gone(id, whatever) for the pages of column j that no new row refers to, in the order of the old rows; whatever: they go whether or not the request
+// is served.  ids: the thread's column.
 template <typename F>
-__device__ __forceinline__ void released_at(const Rows &g, const int32_t *table, uint32_t row0, uint32_t K, uint32_t M, uint32_t j, F gone)
+__device__ __forceinline__ void released_at(const Rows &g, const int32_t *ids, uint32_t width, uint32_t K, uint32_t j, F gone)
 {
     for (uint32_t b = 0; b < K; b++) {
         if (j >= g.old_have[b]) continue;
         if (g.child[b] && !(g.all_fork[b] && j == g.col[b])) continue;          // a child goes on with it
-        const int32_t id = table[(size_t)(row0 + b) * M + j];
+        const int32_t id = ids[b * width];
         bool first = true, referred = false, kept = false;
         for (uint32_t o = 0; o < K; o++) {
-            if (j >= g.old_have[o] || table[(size_t)(row0 + o) * M + j] != id) continue;
+            if (ids[o * width] != id || j >= g.old_have[o]) continue;
             if (o < b) first = false;
             if (g.child[o]) { referred = true; kept |= !(g.all_fork[o] && j == g.col[o]); }
         }
@@ -106,44 +137,31 @@ __device__ __forceinline__ uint32_t block_scan(uint32_t x, uint32_t *part, uint3
 
 __global__ void __launch_bounds__(kPageThreads)
 page_count_kernel(const int32_t *__restrict__ table, const int32_t *__restrict__ lens, const int32_t *__restrict__ counts, const int32_t *__restrict__ parents,
-                  uint32_t K, uint32_t M, uint32_t shift, GroupNeed *__restrict__ needs, uint32_t *__restrict__ forks)
+                  uint32_t K, uint32_t M, uint32_t shift, GroupNeed *__restrict__ needs, uint32_t *__restrict__ forks, Back *__restrict__ back)
 {
+    extern __shared__ int32_t ids[];
     __shared__ Rows g;
     __shared__ uint32_t part[2][kPageWaves];
-    const uint32_t tid = threadIdx.x, row0 = blockIdx.x * K, page = 1u << shift;
-    read_rows(g, lens, counts, parents, row0, K, M, shift);
+    const uint32_t tid = threadIdx.x, row0 = blockIdx.x * K, width = columns_of(K), j = blockIdx.y * width + tid;
+    read_columns(ids, table, row0, K, M, blockIdx.y * width, width);
+    read_rows<true>(g, table, lens, counts, parents, nullptr, row0, K, M, shift);
+    uint32_t always = 0, served = 0;
+    if (tid < width && j < M) released_at(g, ids + tid, width, K, j, [&](int32_t, bool whatever) { (whatever ? always : served)++; });
+    always = wave_sum(always); served = wave_sum(served);
+    if ((tid & 63u) == 0u) { part[0][tid >> 6] = always; part[1][tid >> 6] = served; }
     __syncthreads();
-    if (tid < K) {
-        // a begun page that another row has too
-        uint32_t fork = 0;
-        if (g.count[tid] && (g.length[tid] & (page - 1u))) {
-            const uint32_t c = g.length[tid] >> shift;
-            const int32_t mine = table[(size_t)g.source[tid] * M + c];
-            for (uint32_t o = 0; o < K; o++)
-                if (o != tid && g.have[o] > c) fork |= table[(size_t)g.source[o] * M + c] == mine;
-        }
-        g.fork[tid] = fork;
-        forks[row0 + tid] = fork;
-    }
-    __syncthreads();
-    follow_rows(g, row0, K, shift);
-    __syncthreads();
-    uint32_t most = 0;
-    for (uint32_t b = 0; b < K; b++) most = g.old_have[b] > most ? g.old_have[b] : most;
-    uint32_t released = 0, served = 0;
-    for (uint32_t j = tid; j < most; j += kPageThreads)
-        released_at(g, table, row0, K, M, j, [&](int32_t, bool whatever) { (whatever ? released : served)++; });
-    released = wave_sum(released); served = wave_sum(served);
-    if ((tid & 63u) == 0u) { part[0][tid >> 6] = released; part[1][tid >> 6] = served; }
-    __syncthreads();
+    if (blockIdx.y == 0u && tid < K) forks[row0 + tid] = g.fork[tid];
     if (tid) return;
-    GroupNeed n{0u, 0u, 0u, 0u};
-    for (uint32_t w = 0; w < kPageWaves; w++) { n.released += part[0][w]; n.released_served += part[1][w]; }
+    Back b{0u, 0u};
+    for (uint32_t w = 0; w < kPageWaves; w++) { b.always += part[0][w]; b.served += part[1][w]; }
+    back[(size_t)blockIdx.x * gridDim.y + blockIdx.y] = b;
+    if (blockIdx.y) return;
+    GroupNeed n{0u, 0u};
     bool fits = true;
     for (uint32_t k = 0; k < K; k++) {
         n.tokens += g.count[k];
         n.pages += g.need[k];
-        fits &= g.have[k] + g.need[k] - g.fork[k] <= M;
+        fits &= g.want[k] <= M;
     }
     if (!fits) n.pages = kTooLong;
     needs[blockIdx.x] = n;
@@ -157,6 +175,7 @@ struct PageArgs {
     uint64_t *counters_out;
     const GroupNeed *needs;
     const uint32_t *forks;
+    const Back *back;
     uint32_t rows, K, M, shift, N, tokens, per;      // per: requests of a workgroup
 };
 
@@ -166,99 +185,168 @@ __device__ __forceinline__ uint32_t ring_at(uint32_t base, uint32_t off, uint32_
     return (uint32_t)(i < N ? i : i - N < N ? i - N : i % N);
 }
 
-template <bool kParents>
+// Pages asked for: they end above what is free once a request is not served, and then no later one that needs any is either.  (Saturating: the sum may pass 32 bits.)
+__device__ __forceinline__ uint32_t add(uint32_t x, uint32_t y) { return x + y < x ? 0xFFFFFFFEu : x + y; }
+
+// Sums over the requests before one: pages asked for, handed out and given back, tokens.
+struct Sums { uint32_t pages, used, released, tokens; };
+struct Served { uint32_t asks, end; bool yes; };
+__device__ __forceinline__ Served served_of(const GroupNeed &n, uint32_t before, uint32_t free, uint32_t N)
+{
+    const uint32_t asks = n.pages == kTooLong ? 0u : n.pages < N + 1u ? n.pages : N + 1u, end = add(before, asks);
+    return Served{asks, end, n.pages != kTooLong && (asks == 0u || end <= free)};
+}
+
+// The whole workgroup works out the sums over the requests [0, g0); need(i) and back(i, served) are a request's own.
+template <typename Need, typename Given>
+__device__ __forceinline__ Sums sums_before(uint32_t g0, uint32_t free, uint32_t N, uint32_t *part, bool releases, Need need, Given back)
+{
+    Sums s{0u, 0u, 0u, 0u};
+    for (uint32_t i0 = 0; i0 < g0; i0 += kPageThreads) {
+        const uint32_t i = i0 + threadIdx.x;
+        const GroupNeed n = i < g0 ? need(i) : GroupNeed{0u, 0u};
+        const uint32_t asks = served_of(n, 0u, 0u, N).asks;
+        uint32_t all;
+        const uint32_t end = block_scan(asks, part, &all);
+        const Served v = served_of(n, add(s.pages, end - asks), free, N);
+        s.pages = add(s.pages, all);
+        (void)block_scan(v.yes ? asks : 0u, part, &all);
+        s.used += all;
+        if (releases) { (void)block_scan(i < g0 ? back(i, v.yes) : 0u, part, &all); s.released += all; }
+        (void)block_scan(n.tokens, part, &all);
+        s.tokens += all;
+    }
+    return s;
+}
+
+// Without parents: requests of one row.
 __global__ void __launch_bounds__(kPageThreads)
 page_kernel(const PageArgs a)
 {
-    __shared__ Rows g;
     __shared__ uint32_t part[kPageWaves];
-    const uint32_t tid = threadIdx.x, page = 1u << a.shift, K = kParents ? a.K : 1u, G = a.rows / K;
+    const uint32_t tid = threadIdx.x, page = 1u << a.shift;
+    const uint32_t r0 = blockIdx.x * a.per, r1 = a.rows - r0 < a.per ? a.rows : r0 + a.per;
+    const uint64_t taken = a.counters[0], given = a.counters[1];
+    const uint32_t free = given <= taken ? 0u : given - taken < a.N ? (uint32_t)(given - taken) : a.N, head = (uint32_t)(taken % a.N);
+    auto need_of = [&](uint32_t r) {
+        const uint32_t length = tokens_of(a.lens[r], a.M << a.shift), count = tokens_of(a.counts[r], 0x7FFFFFFFu);
+        const uint32_t have = (length + page - 1u) >> a.shift, want = (uint32_t)(((uint64_t)length + count + page - 1u) >> a.shift);
+        return GroupNeed{want > a.M ? kTooLong : want - have, count};
+    };
+    Sums s = sums_before(r0, free, a.N, part, false, need_of, [](uint32_t, bool) { return 0u; });
+    for (uint32_t r = r0; r < r1; r++) {
+        const GroupNeed n = need_of(r);
+        const Served v = served_of(n, s.pages, free, a.N);
+        const uint32_t length = tokens_of(a.lens[r], a.M << a.shift), have = (length + page - 1u) >> a.shift;
+        const uint32_t want = v.yes ? (length + n.tokens + page - 1u) >> a.shift : have, first = s.pages;
+        const int32_t *from = a.table + (size_t)r * a.M;
+        int32_t *to = a.table_out + (size_t)r * a.M;
+        auto page_at = [&](uint32_t j) { return j >= have ? a.ring[ring_at(head, first + j - have, a.N)] : from[j]; };
+        for (uint32_t j = (from == to ? have : 0u) + tid; j < want; j += kPageThreads) to[j] = page_at(j);
+        for (uint32_t t = tid; t < n.tokens; t += kPageThreads) {
+            const uint32_t at = s.tokens + t, pos = length + t;
+            if (at >= a.tokens || at < s.tokens) break;
+            a.positions[at] = (int32_t)pos;
+            a.slots[at] = v.yes ? page_at(pos >> a.shift) << a.shift | (int32_t)(pos & (page - 1u)) : -1;
+            a.origins[at] = -1;
+        }
+        if (tid == 0u) { a.lens_out[r] = (int32_t)(v.yes ? length + n.tokens : length); a.starts[r] = (int32_t)s.tokens; }
+        s.pages = v.end;
+        if (v.yes) s.used += v.asks;
+        s.tokens += n.tokens;
+    }
+    if (r1 == a.rows && tid == 0u) {
+        a.starts[a.rows] = (int32_t)s.tokens;
+        a.counters_out[0] = taken + s.used;
+        a.counters_out[1] = given;
+    }
+}
+
+// With parents: a workgroup takes some columns of a request's tables; the one of the first columns also the tokens.
+__global__ void __launch_bounds__(kPageThreads)
+page_beam_kernel(const PageArgs a)
+{
+    extern __shared__ int32_t ids[];
+    __shared__ Rows g;
+    __shared__ uint32_t part[kPageWaves], begins[2][kBeamMax];
+    const uint32_t tid = threadIdx.x, page = 1u << a.shift, K = a.K, G = a.rows / K, width = columns_of(K), j0 = blockIdx.y * width, j = j0 + tid, chunks = gridDim.y;
     const uint32_t g0 = blockIdx.x * a.per, g1 = G - g0 < a.per ? G : g0 + a.per;
     const uint64_t taken = a.counters[0], given = a.counters[1];
     const uint32_t free = given <= taken ? 0u : given - taken < a.N ? (uint32_t)(given - taken) : a.N;
     const uint32_t head = (uint32_t)(taken % a.N), tail = (uint32_t)(given % a.N);
-    auto need_of = [&](uint32_t i) {
-        if (kParents) return a.needs[i];
-        const uint32_t length = tokens_of(a.lens[i], a.M << a.shift), count = tokens_of(a.counts[i], 0x7FFFFFFFu);
-        const uint32_t have = (length + page - 1u) >> a.shift, want = (uint32_t)(((uint64_t)length + count + page - 1u) >> a.shift);
-        return GroupNeed{want > a.M ? kTooLong : want - have, 0u, 0u, count};
+    auto back_of = [&](uint32_t i, uint32_t n, bool served) {       // of the request's first n chunks
+        uint32_t x = 0;
+        for (uint32_t c = 0; c < n; c++) { const Back b = a.back[(size_t)i * chunks + c]; x += b.always + (served ? b.served : 0u); }
+        return x;
     };
-    // The sums over the requests before this workgroup's, then request by request.  The last workgroup also goes over its own for the totals.
-    uint32_t pages = 0, used = 0, released = 0, tokens = 0;       // pages asked for, pages handed out, pages given back, tokens
-    // (pages asked for end above `free` once a request is not served, and every later one that needs any is not either; saturating: the sum of
-    // what is asked for may pass 32 bits)
-    auto add = [](uint32_t x, uint32_t y) { return x + y < x ? 0xFFFFFFFEu : x + y; };
-    for (uint32_t i0 = 0; i0 < g0; i0 += kPageThreads) {
-        const uint32_t i = i0 + tid;
-        const GroupNeed n = i < g0 ? need_of(i) : GroupNeed{0u, 0u, 0u, 0u};
-        const uint32_t asks = n.pages == kTooLong ? 0u : n.pages < a.N + 1u ? n.pages : a.N + 1u;
-        uint32_t all;
-        const uint32_t end = add(pages, block_scan(asks, part, &all));
-        const bool served = n.pages != kTooLong && (asks == 0u || end <= free);
-        pages = add(pages, all);
-        (void)block_scan(served ? asks : 0u, part, &all);
-        used += all;
-        if (kParents) { (void)block_scan(n.released + (served ? n.released_served : 0u), part, &all); released += all; }
-        (void)block_scan(n.tokens, part, &all);
-        tokens += all;
-    }
+    read_columns(ids, a.table, g0 * K, K, a.M, j0, width);
+    Sums s = sums_before(g0, free, a.N, part, true, [&](uint32_t i) { return a.needs[i]; }, [&](uint32_t i, bool served) { return back_of(i, chunks, served); });
     for (uint32_t i = g0; i < g1; i++) {
-        const GroupNeed n = need_of(i);
-        const uint32_t asks = n.pages == kTooLong ? 0u : n.pages < a.N + 1u ? n.pages : a.N + 1u, end = add(pages, asks), row0 = i * K;
-        const bool served = n.pages != kTooLong && (asks == 0u || end <= free);
-        if (kParents) {
-            __syncthreads();
-            read_rows(g, a.lens, a.counts, a.parents, row0, K, a.M, a.shift);
-            if (tid < K) g.fork[tid] = a.forks[row0 + tid];
-            __syncthreads();
-            follow_rows(g, row0, K, a.shift);
-            __syncthreads();
+        const GroupNeed n = a.needs[i];
+        const Served v = served_of(n, s.pages, free, a.N);
+        const uint32_t row0 = i * K;
+        if (i != g0) { __syncthreads(); read_columns(ids, a.table, row0, K, a.M, j0, width); }
+        const Back mine = a.back[(size_t)i * chunks + blockIdx.y];
+        const uint32_t back = back_of(i, chunks, v.yes), before = back_of(i, blockIdx.y, v.yes);
+        read_rows<false>(g, a.table, a.lens, a.counts, a.parents, a.forks, row0, K, a.M, a.shift);
+        if (tid < K) {                                // where each row's pages and tokens begin
+            uint32_t p = s.pages, t = s.tokens;
+            for (uint32_t k = 0; k < tid; k++) { p += g.need[k]; t += g.count[k]; }
+            begins[0][tid] = p; begins[1][tid] = t;
         }
-        uint32_t first_page = pages, first_token = tokens;
-        for (uint32_t k = 0; k < K; k++) {
-            const uint32_t r = row0 + k;
-            const uint32_t length = kParents ? g.length[k] : tokens_of(a.lens[r], a.M << a.shift), have = (length + page - 1u) >> a.shift;
-            const uint32_t count = kParents ? g.count[k] : n.tokens, fork = kParents && served ? g.fork[k] : 0u;
-            const uint32_t want = served ? (length + count + page - 1u) >> a.shift : have, col = length >> a.shift;
-            const int32_t *from = a.table + (size_t)(kParents ? (g.source[k] < 0 ? 0 : g.source[k]) : (int32_t)r) * a.M;
-            int32_t *to = a.table_out + (size_t)r * a.M;
-            auto fresh = [&](uint32_t at) { return a.ring[ring_at(head, first_page + at, a.N)]; };
-            auto page_at = [&](uint32_t j) { return j >= have ? fresh(fork + j - have) : fork && j == col ? fresh(0u) : from[j]; };
-            for (uint32_t j = (from == to ? have : 0u) + tid; j < want; j += kPageThreads) to[j] = page_at(j);
-            for (uint32_t t = tid; t < count; t += kPageThreads) {
-                const uint32_t at = first_token + t, pos = length + t;
-                if (at >= a.tokens || at < first_token) break;
-                a.positions[at] = (int32_t)pos;
-                a.slots[at] = served ? page_at(pos >> a.shift) << a.shift | (int32_t)(pos & (page - 1u)) : -1;
-                a.origins[at] = t == 0u && fork ? from[col] : -1;
+        __syncthreads();
+        auto page_of = [&](uint32_t k, uint32_t at) { return a.ring[ring_at(head, begins[0][k] + at, a.N)]; };
+        if (tid < width)
+            for (uint32_t k = 0; k < K; k++) {
+                const uint32_t have = g.have[k], fork = v.yes ? g.fork[k] : 0u;
+                if (j >= (v.yes ? g.want[k] : have)) continue;
+                int32_t id;
+                if (j >= have) id = page_of(k, fork + j - have);
+                else if (fork && j == (g.length[k] >> a.shift)) id = page_of(k, 0u);
+                else id = ids[(uint32_t)g.source[k] * width + tid];
+                a.table_out[(size_t)(row0 + k) * a.M + j] = id;
             }
-            if (tid == 0u) { a.lens_out[r] = (int32_t)(served ? length + count : length); a.starts[r] = (int32_t)first_token; }
-            if (served) first_page += kParents ? g.need[k] : asks;
-            first_token += count;
+        if (blockIdx.y == 0u) {
+            for (uint32_t k = tid >> 6; k < K; k += kPageWaves) {
+                const uint32_t length = g.length[k], have = g.have[k], fork = v.yes ? g.fork[k] : 0u, col = length >> a.shift, first = begins[1][k], r = row0 + k;
+                const int32_t *from = a.table + (size_t)(row0 + (g.source[k] < 0 ? 0u : (uint32_t)g.source[k])) * a.M;
+                auto page_at = [&](uint32_t c) { return c >= have ? page_of(k, fork + c - have) : fork && c == col ? page_of(k, 0u) : from[c]; };
+                for (uint32_t t = tid & 63u; t < g.count[k]; t += 64u) {
+                    const uint32_t at = first + t, pos = length + t;
+                    if (at >= a.tokens || at < first) break;
+                    a.positions[at] = (int32_t)pos;
+                    a.slots[at] = v.yes ? page_at(pos >> a.shift) << a.shift | (int32_t)(pos & (page - 1u)) : -1;
+                    a.origins[at] = t == 0u && fork ? from[col] : -1;
+                }
+                if ((tid & 63u) == 0u) { a.lens_out[r] = (int32_t)(v.yes ? length + g.count[k] : length); a.starts[r] = (int32_t)first; }
+            }
         }
-        if (kParents && (n.released || (served && n.released_served))) {
+        if (mine.always || (v.yes && mine.served)) {
             // pages go back by place in the tables, then by row
-            uint32_t most = 0, base = released;
-            for (uint32_t b = 0; b < K; b++) most = g.old_have[b] > most ? g.old_have[b] : most;
-            for (uint32_t j0 = 0; j0 < most; j0 += kPageThreads) {
-                uint32_t mine = 0, all;
-                if (j0 + tid < most) released_at(g, a.table, row0, K, a.M, j0 + tid, [&](int32_t, bool whatever) { mine += whatever || served; });
-                uint32_t at = base + block_scan(mine, part, &all) - mine;
-                if (mine)
-                    released_at(g, a.table, row0, K, a.M, j0 + tid, [&](int32_t id, bool whatever) { if (whatever || served) a.ring[ring_at(tail, at++, a.N)] = id; });
-                base += all;
-            }
+            uint32_t count = 0, all;
+            if (tid < width && j < a.M) released_at(g, ids + tid, width, K, j, [&](int32_t, bool whatever) { count += whatever || v.yes; });
+            uint32_t at = s.released + before + block_scan(count, part, &all) - count;
+            if (count)
+                released_at(g, ids + tid, width, K, j, [&](int32_t id, bool whatever) { if (whatever || v.yes) a.ring[ring_at(tail, at++, a.N)] = id; });
         }
-        pages = end;
-        if (served) used += asks;
-        released += n.released + (served ? n.released_served : 0u);
-        tokens += n.tokens;
+        s.pages = v.end;
+        if (v.yes) s.used += v.asks;
+        s.released += back;
+        s.tokens += n.tokens;
     }
-    if (g1 == G && tid == 0u) {
-        a.starts[a.rows] = (int32_t)tokens;
-        a.counters_out[0] = taken + used;
-        a.counters_out[1] = given + released;
+    if (g1 == G && blockIdx.y == 0u && tid == 0u) {
+        a.starts[a.rows] = (int32_t)s.tokens;
+        a.counters_out[0] = taken + s.used;
+        a.counters_out[1] = given + s.released;
     }
+}
+
+static uint32_t chunks_of(uint32_t K, uint32_t columns) { return (columns + columns_of(K) - 1u) / columns_of(K); }
+
+uint64_t page_step_bytes(uint32_t rows, uint32_t K, uint32_t columns)
+{
+    const uint64_t G = rows / K;
+    return G * (sizeof(GroupNeed) + chunks_of(K, columns) * sizeof(Back)) + rows * 4ull;
 }
 
 hipError_t launch_page_step(const int32_t *table, uint32_t rows, uint32_t columns, const int32_t *lens, const int32_t *counts, const int32_t *parents,
@@ -266,18 +354,20 @@ hipError_t launch_page_step(const int32_t *table, uint32_t rows, uint32_t column
                             int32_t *starts, int32_t *slots, int32_t *positions, int32_t *origins, uint32_t tokens, uint64_t *counters_out,
                             void *workspace, hipStream_t s)
 {
+    const uint32_t G = rows / K, chunks = chunks_of(K, columns);
     GroupNeed *needs = static_cast<GroupNeed *>(workspace);
-    const uint32_t G = rows / K;
-    uint32_t *forks = reinterpret_cast<uint32_t *>(needs + G);
-    // every workgroup goes over all requests before its own: at most 512 of them
+    Back *back = reinterpret_cast<Back *>(needs + G);
+    uint32_t *forks = reinterpret_cast<uint32_t *>(back + (size_t)G * chunks);
+    // every workgroup goes over all requests before its own: at most 512 of them for the same columns
     const uint32_t per = (G + 511u) / 512u;
     const PageArgs a{table, lens, counts, parents, ring, counters, table_out, lens_out, starts, slots, positions, origins, counters_out,
-                     needs, forks, rows, K, columns, shift, pages, tokens, per};
-    const dim3 grid((G + per - 1u) / per), block(kPageThreads);
-    if (!parents) return launch(page_kernel<false>, grid, block, 0, s, nullptr, a);
-    const hipError_t e = launch(page_count_kernel, dim3(G), block, 0, s, nullptr, table, lens, counts, parents, K, columns, shift, needs, forks);
+                     needs, forks, back, rows, K, columns, shift, pages, tokens, per};
+    const dim3 block(kPageThreads);
+    if (!parents) return launch(page_kernel, dim3((G + per - 1u) / per), block, 0, s, nullptr, a);
+    const uint32_t lds = K * columns_of(K) * 4u;
+    const hipError_t e = launch(page_count_kernel, dim3(G, chunks), block, lds, s, nullptr, table, lens, counts, parents, K, columns, shift, needs, forks, back);
     if (e != hipSuccess) return e;
-    return launch(page_kernel<true>, grid, block, 0, s, nullptr, a);
+    return launch(page_beam_kernel, dim3((G + per - 1u) / per, chunks), block, lds, s, nullptr, a);
 }
 
 }  // namespace wg

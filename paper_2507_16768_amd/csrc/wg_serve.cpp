@@ -78,8 +78,8 @@ int wg_reorder_rows(const void *d_src, void *d_dst, const int32_t *d_parents, ui
     });
 }
 
-uint64_t wg_page_step_workspace(uint32_t rows, uint32_t beams) {
-    return beams ? (uint64_t)rows / beams * 16u + (uint64_t)rows * 4u : 0u;
+uint64_t wg_page_step_workspace(uint32_t rows, uint32_t beams, uint32_t columns) {
+    return beams && columns ? page_step_bytes(rows, beams, columns) : 0u;
 }
 
 int wg_page_step(const int32_t *d_table, uint32_t rows, uint32_t columns, const int32_t *d_lens, const int32_t *d_counts, const int32_t *d_parents,
@@ -94,10 +94,11 @@ int wg_page_step(const int32_t *d_table, uint32_t rows, uint32_t columns, const 
         WG_WANT(shift_of(page_tokens), "page_tokens must be 16, 32 or 64");
         WG_WANT((uint64_t)columns * page_tokens <= 0x7FFFFFFFull && (uint64_t)pages * page_tokens <= 0x7FFFFFFFull && tokens <= 0x7FFFFFFFu, "tokens above 2^31 - 1");
         WG_WANT(beams && beams <= kBeamMax && rows % beams == 0, "beams must be 1 .. 64 and divide rows");
+        WG_WANT(!d_parents || columns <= 65535u * 128u, "columns above 8388480 with parents");
         WG_WANT(d_parents || beams == 1u, "beams without parents");
         WG_WANT(!d_parents || d_table != d_table_out, "rows that follow parents must not be written in place");
         WG_WANT(d_lens != d_lens_out && d_counters != d_counters_out, "lengths and counters must not be written in place");
-        const uint64_t need = d_parents ? wg_page_step_workspace(rows, beams) : 0u;
+        const uint64_t need = d_parents ? wg_page_step_workspace(rows, beams, columns) : 0u;
         WG_WANT(!need || (d_workspace && workspace_bytes >= need), "the workspace is too small (wg_page_step_workspace)");
         WG_WANT(aligned(d_workspace, 16), "the workspace must be 16-byte aligned");
         return launch_page_step(d_table, rows, columns, d_lens, d_counts, d_parents, beams, shift_of(page_tokens), d_ring, pages, d_counters, d_table_out,

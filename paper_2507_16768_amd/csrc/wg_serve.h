@@ -16,6 +16,7 @@ hipError_t launch_beam_select(const void *logits, int dtype, uint32_t rows, uint
                               wg_state_t *states_out, void *workspace, hipStream_t s);
 hipError_t launch_reorder_rows(const void *src, void *dst, const int32_t *parents, uint32_t outer, uint32_t rows, uint64_t row_bytes,
                                int64_t src_outer, int64_t src_row, int64_t dst_outer, int64_t dst_row, hipStream_t s);
+uint64_t page_step_bytes(uint32_t rows, uint32_t K, uint32_t columns);
 hipError_t launch_page_step(const int32_t *table, uint32_t rows, uint32_t columns, const int32_t *lens, const int32_t *counts, const int32_t *parents,
                             uint32_t K, uint32_t shift, int32_t *ring, uint32_t pages, const uint64_t *counters, int32_t *table_out, int32_t *lens_out,
                             int32_t *starts, int32_t *slots, int32_t *positions, int32_t *origins, uint32_t tokens, uint64_t *counters_out,

@@ -100,7 +100,7 @@ class Pool:
         got = dict(out_table=table if in_place else d(out_table), out_lens=d(np.full(self.R, -9, np.int32)), starts=d(np.full(self.R + 1, -9, np.int32)),
                    slots=d(np.full(T, -99, np.int32)), positions=d(np.full(T, -99, np.int32)), origins=d(np.full(T, -99, np.int32)), ring=ring,
                    out_counters=d(np.zeros(2, np.int64)))
-        work = torch.empty(max(16, wg.page_step_workspace(self.R, self.K)), dtype=torch.uint8, device="cuda") if parents is not None else None
+        work = torch.empty(max(16, wg.page_step_workspace(self.R, self.K, self.M)), dtype=torch.uint8, device="cuda") if parents is not None else None
         args = (table, d(self.lens), d(counts), None if parents is None else d(parents), self.K, self.P, ring, d(self.counters), got["out_table"], got["out_lens"],
                 got["starts"], got["slots"], got["positions"], got["origins"], got["out_counters"], work)
         for _ in range(2):                               # the same call again gives the same
@@ -137,7 +137,8 @@ def test_rows_without_beams(R, P, M, in_place):
     pool.check()
 
 
-@pytest.mark.parametrize("K,G,P,M", [(1, 5, 16, 20), (2, 3, 16, 12), (4, 20, 16, 40), (5, 7, 32, 20), (8, 64, 16, 30), (64, 2, 16, 12), (3, 200, 16, 10)])
+@pytest.mark.parametrize("K,G,P,M", [(1, 5, 16, 20), (2, 3, 16, 12), (4, 20, 16, 40), (5, 7, 32, 20), (8, 64, 16, 30), (64, 2, 16, 12), (3, 200, 16, 10), (8, 3, 16, 700),
+                                     (40, 3, 16, 300), (2, 700, 16, 6)])
 def test_beams_follow_their_parents(K, G, P, M):
     torch, wg = _wg()
     rng = np.random.default_rng(K * 100 + G)
