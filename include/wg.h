@@ -408,7 +408,7 @@ int wg_page_step(const int32_t *d_table, uint32_t rows, uint32_t columns, const 
  * (e4m3: 4 bits of exponent, 3 of mantissa, up to 448, no infinities), with a scale for every page and head, [pages][heads] fp32 each: a
  * number is its 8 bits times the scale.  dim is 64, 128 or 256.
  *
- * wg_cache_append: token t's key and value (bfloat16, strides in elements, rows of `dim` at multiples of 16 bytes) go to
+ * wg_cache_append: token t's key and value (bfloat16, strides in elements, rows of `dim` at multiples of 16 bytes, tokens less than 2^24 elements apart) go to
  * slot d_slots[t]; a slot outside [0, pages * page_tokens) takes none.  Tokens of one page are adjacent and in ascending order (as wg_page_step numbers them), and
  * the tokens in front of them in their page are there already.  The page's scale becomes the least power of two, 2^-64 at least, times which 448 reaches the
  * largest finite magnitude among the new tokens, or stays where it is larger (not where the first token is the page's first); numbers are rounded

@@ -8,6 +8,7 @@
 
 #include <cfloat>
 
+#include "wg_buffer.h"
 #include "wg_launch.h"
 #include "wg_serve.h"
 
@@ -56,8 +57,8 @@ __device__ __forceinline__ float scale_for(float top)
 //
 // A wavefront looks at 64 tokens' slots and at the 64 behind them, a lane each, and finds the runs that begin among the first by ballots: prompts have few of them, rows
 // that take a token each have 64.  (A wavefront for every token, head and kind, of which all but those of first tokens left at once, took 99 us for 11,000 tokens
-// of prompts, 8 heads of 128.)  Runs are dealt out to as many wavefronts as the chip holds.  Numbers stay in registers between the
-// two looks at them, and what comes from another page is asked for together with them.
+// of prompts, 8 heads of 128.)  Runs are dealt out to as many wavefronts as the chip holds.  A run's numbers are read twice, the second time out of the
+// caches: held in registers they cost half of the wavefronts, and time.
 struct AppendArgs {
     const uint16_t *x[2];                            // keys, values: [token][head][dim]
     int64_t token_stride[2], head_stride[2];         // elements
@@ -66,6 +67,12 @@ struct AppendArgs {
     const int32_t *slots, *origins;
     uint32_t tokens, heads, pages, shift;
 };
+
+// The bytes of a word at `at` that lie below `end`, as ones.
+__device__ __forceinline__ uint32_t bytes_below(uint32_t end, uint32_t at) { return end <= at ? 0u : end - at >= 4u ? 0xFFFFFFFFu : (1u << (8u * (end - at))) - 1u; }
+
+// Behind every run's rows, which are 64 of less than 2^25 bytes from one to the next; with a lane's place in a row added too.
+constexpr uint32_t kFar = 0xF0000000u;
 
 // Where a run's tokens go: tokens o .. o + n of a page, behind `o` earlier ones that lie in page `source`.
 struct Run { uint32_t token, page, source, o, n; };
@@ -76,174 +83,179 @@ __device__ __forceinline__ void append_run(const AppendArgs &a, const Run &run, 
     constexpr uint32_t kWhich = kValues ? 1u : 0u;
     constexpr uint32_t kLanes = kD / 8u, kTokens = 64u / kLanes;           // keys: eight dims to a lane, so many tokens to a load
     constexpr uint32_t kOwn = kD / 64u, kWords = (kOwn + 1u) / 2u;         // values: dims of a lane, and the words that they are
-    constexpr uint32_t kHeld = kD == 256u ? 16u : 32u;                     // tokens that stay in registers
-    constexpr uint32_t kLoads = kValues ? kHeld : kHeld / kTokens, kLoadWords = kValues ? kWords : 4u, kLoadTokens = kValues ? 1u : kTokens;
-    constexpr uint32_t kGroup = kValues ? 8u : kLoads < 4u ? kLoads : 4u;  // loads that one question is asked for
-    constexpr uint32_t kEarly = 4;                                         // sixteen bytes each of the earlier tokens
+    constexpr uint32_t kLoadWords = kValues ? kWords : 4u, kLoadTokens = kValues ? 1u : kTokens;
     const uint32_t lane = threadIdx.x & 63u, P = 1u << a.shift, o = run.o, n = run.n, end = o + n;
     const uint16_t *x = a.x[kWhich] + (int64_t)run.token * a.token_stride[kWhich] + (int64_t)h * a.head_stride[kWhich];
-    const int64_t step = a.token_stride[kWhich];
+    // the run's rows as a buffer: a token behind its last lies behind the end, and reads as zeros
+    const uint32_t step = (uint32_t)a.token_stride[kWhich] * 2u;
+    const Window win = window_of(x, (n - 1u) * step + kD * 2u);
     uint8_t *to = a.cache[kWhich] + ((size_t)run.page * a.heads + h) * (P * kD);
     const uint8_t *from = a.cache[kWhich] + ((size_t)run.source * a.heads + h) * (P * kD);
     const uint32_t own_token = kValues ? 0u : lane / kLanes, own_dim = kValues ? lane * kOwn : lane % kLanes * 8u;
+    const uint32_t own_at = own_token * step + own_dim * 2u;
+    // (token: of the wavefront's first lane)
     auto load = [&](uint32_t token, uint32_t (&w)[kLoadWords]) {
-        const uint16_t *p = x + (int64_t)token * step + own_dim;
-        if (!kValues) { const Word4 v = *reinterpret_cast<const Word4 *>(p); for (uint32_t i = 0; i < 4u; i++) w[i % kLoadWords] = v[i]; }
-        else if (kOwn == 1u) w[0] = (uint32_t)*p << 16;                    // (the lower half is a zero)
+        if (!kValues) {
+            const FourWords v = __builtin_amdgcn_raw_buffer_load_b128(win, token + own_token < n ? token * step + own_at : kNowhere, 0, 0);
+            w[0] = v.x; w[1 % kLoadWords] = v.y; w[2 % kLoadWords] = v.z; w[3 % kLoadWords] = v.w;
+            return;
+        }
+        const uint32_t at = (token < n ? token * step : kFar) + own_at;
+        if (kOwn == 1u) w[0] = (uint32_t)__builtin_amdgcn_raw_buffer_load_b16(win, at, 0, 0) << 16;         // (the lower half is a zero)
         else
-            for (uint32_t i = 0; i < kWords; i++) w[i] = reinterpret_cast<const uint32_t *>(p)[i];
+            for (uint32_t i = 0; i < kWords; i++) w[i] = __builtin_amdgcn_raw_buffer_load_b32(win, at + 4u * i, 0, 0);
     };
-    const bool held = n <= kHeld;
-    uint32_t w[kLoads][kLoadWords];
-    float top = 0.f;
-    if (held)
-#pragma unroll
-        for (uint32_t j = 0; j < kLoads; j += kGroup) {
-            if (j * kLoadTokens >= n) break;
-#pragma unroll
-            for (uint32_t i = j; i < j + kGroup; i++) {                    // (behind the last token the last again)
-                const uint32_t token = i * kLoadTokens + own_token;
-                load(token < n ? token : n - 1u, w[i]);
-            }
-        }
     const float was = o ? a.scale[kWhich][(size_t)run.source * a.heads + h] : 0.f;
-    // the earlier tokens: of keys the page's first bytes, of values the first bytes of every dim
-    const bool moved = o && run.source != run.page, ahead = moved && P * kD <= kEarly * 1024u;
-    Word4 early[kEarly] = {};
-    const uint32_t early_units = kValues ? 0u : o * kD / 16u;
-    if (ahead)
+    constexpr uint32_t kRound = kValues ? 16u : 4u;                        // loads in flight together
+    float top = 0.f;
+#pragma nounroll
+    for (uint32_t i = 0; i < n; i += kRound * kLoadTokens) {
+        uint32_t w[kRound][kLoadWords];
 #pragma unroll
-        for (uint32_t i = 0; i < kEarly; i++) {
-            if (!kValues) { if (i * 64u + lane < early_units) early[i] = reinterpret_cast<const Word4 *>(from)[i * 64u + lane]; }
-            else if (i / kOwn * 16u < o) early[i] = *reinterpret_cast<const Word4 *>(from + (size_t)(own_dim + i % kOwn) * P + i / kOwn * 16u);
-        }
-    if (held) {
+        for (uint32_t j = 0; j < kRound; j++) load(i + j * kLoadTokens, w[j]);
 #pragma unroll
-        for (uint32_t j = 0; j < kLoads; j += kGroup) {
-            if (j * kLoadTokens >= n) break;
+        for (uint32_t j = 0; j < kRound; j++)
 #pragma unroll
-            for (uint32_t i = j; i < j + kGroup; i++)
-#pragma unroll
-                for (uint32_t k = 0; k < kLoadWords; k++) { top = top_of(top, low(w[i][k])); top = top_of(top, high(w[i][k])); }
-        }
-    } else {
-#pragma unroll 4
-        for (uint32_t i = own_token; i < n; i += kLoadTokens) {
-            uint32_t v[kLoadWords];
-            load(i, v);
-#pragma unroll
-            for (uint32_t k = 0; k < kLoadWords; k++) { top = top_of(top, low(v[k])); top = top_of(top, high(v[k])); }
-        }
+            for (uint32_t k = 0; k < kLoadWords; k++) { top = top_of(top, low(w[j][k])); top = top_of(top, high(w[j][k])); }
     }
 #pragma unroll
     for (int s = 32; s > 0; s >>= 1) top = __builtin_fmaxf(top, __shfl_xor(top, s));
     const float now = __builtin_fmaxf(scale_for(top), was), inverse = 1.f / now, ratio = was / now;
-    const bool again = o && (moved || now != was);                         // the earlier tokens are written too
+    const bool again = o && (run.source != run.page || now != was);        // the earlier tokens are written too
     if (lane == 0u) a.scale[kWhich][(size_t)run.page * a.heads + h] = now;
     if (!kValues) {
-        if (again) {
-            auto put = [&](uint32_t u, Word4 v) {
+        if (again)
+#pragma nounroll
+            for (uint32_t u = lane; u < o * kD / 16u; u += 64u) {
+                Word4 v = reinterpret_cast<const Word4 *>(from)[u];
 #pragma unroll
                 for (uint32_t k = 0; k < 4u; k++) v[k] = rescaled(v[k], ratio);
                 reinterpret_cast<Word4 *>(to)[u] = v;
-            };
-            if (ahead) {
-#pragma unroll
-                for (uint32_t i = 0; i < kEarly; i++) if (i * 64u + lane < early_units) put(i * 64u + lane, early[i]);
-            } else
-                for (uint32_t u = lane; u < early_units; u += 64u) put(u, reinterpret_cast<const Word4 *>(from)[u]);
-        }
-        auto put = [&](uint32_t token, const uint32_t (&v)[kLoadWords]) {
-            Word2 r;
-#pragma unroll
-            for (uint32_t k = 0; k < 2u; k++)
-                r[k] = to_bytes(low(v[2u * k % kLoadWords]) * inverse, high(v[2u * k % kLoadWords]) * inverse, low(v[(2u * k + 1u) % kLoadWords]) * inverse,
-                                high(v[(2u * k + 1u) % kLoadWords]) * inverse);
-            *reinterpret_cast<Word2 *>(to + (o + token) * kD + own_dim) = r;
-        };
-        if (held) {
-#pragma unroll
-            for (uint32_t j = 0; j < kLoads; j += kGroup) {
-                if (j * kLoadTokens >= n) break;
-#pragma unroll
-                for (uint32_t i = j; i < j + kGroup; i++)
-                    if (i * kLoadTokens + own_token < n) put(i * kLoadTokens + own_token, w[i]);
             }
-        } else {
-#pragma unroll 4
-            for (uint32_t i = own_token; i < n; i += kLoadTokens) {
-                uint32_t v[kLoadWords];
-                load(i, v);
-                put(i, v);
+#pragma nounroll
+        for (uint32_t i = 0; i < n; i += kRound * kLoadTokens) {
+            uint32_t w[kRound][kLoadWords];
+#pragma unroll
+            for (uint32_t j = 0; j < kRound; j++) load(i + j * kLoadTokens, w[j]);
+#pragma unroll
+            for (uint32_t j = 0; j < kRound; j++) {
+                const uint32_t token = i + j * kLoadTokens + own_token;
+                Word2 r;
+#pragma unroll
+                for (uint32_t k = 0; k < 2u; k++)
+                    r[k] = to_bytes(low(w[j][2u * k % kLoadWords]) * inverse, high(w[j][2u * k % kLoadWords]) * inverse, low(w[j][(2u * k + 1u) % kLoadWords]) * inverse,
+                                    high(w[j][(2u * k + 1u) % kLoadWords]) * inverse);
+                if (token < n) *reinterpret_cast<Word2 *>(to + (o + token) * kD + own_dim) = r;
             }
         }
         return;
     }
-    // Values: sixteen tokens of a dim at a time.  at(token, d): the token's number in the lane's dim d.
-    auto column = [&](uint32_t c, auto at) {
-        const uint32_t begin = again ? 0u : o;
+    // Values: sixteen tokens of a dim at a time.
+    const uint32_t begin = again ? 0u : o;
+#pragma nounroll
+    for (uint32_t c = begin & ~15u; c < end; c += 16u) {
+        uint32_t w[16][kLoadWords];
+#pragma unroll
+        for (uint32_t i = 0; i < 16u; i++) load(c + i - o, w[i]);          // (in front of the run's tokens a number of none, as behind them)
 #pragma unroll
         for (uint32_t d = 0; d < kOwn; d++) {
             uint8_t *out = to + (size_t)(own_dim + d) * P + c;
+            auto at = [&](uint32_t i) { const uint32_t x = w[i][d / 2u % kLoadWords]; return (kOwn > 1u && d % 2u == 0u ? low(x) : high(x)) * inverse; };
             Word4 r;
 #pragma unroll
-            for (uint32_t k = 0; k < 4u; k++)
-                r[k] = to_bytes(at(4u * k, d) * inverse, at(4u * k + 1u, d) * inverse, at(4u * k + 2u, d) * inverse, at(4u * k + 3u, d) * inverse);
-            if (again && c < o) {
-                Word4 old;
-                if (ahead) {
-                    // (by masks: a choice between registers by a number is one between addresses, which puts them into memory)
-                    old = Word4{0u, 0u, 0u, 0u};
+            for (uint32_t k = 0; k < 4u; k++) r[k] = to_bytes(at(4u * k), at(4u * k + 1u), at(4u * k + 2u), at(4u * k + 3u));
+            if (begin < o && c < o) {
+                const Word4 old = *reinterpret_cast<const Word4 *>(from + (size_t)(own_dim + d) * P + c);
 #pragma unroll
-                    for (uint32_t i = 0; i < kEarly / kOwn; i++) old |= early[i * kOwn + d] & (c == 16u * i ? 0xFFFFFFFFu : 0u);
-                } else old = *reinterpret_cast<const Word4 *>(from + (size_t)(own_dim + d) * P + c);
+                for (uint32_t k = 0; k < 4u; k++) { const uint32_t m = bytes_below(o, c + 4u * k); r[k] = (rescaled(old[k], ratio) & m) | (r[k] & ~m); }
+            }
+            if (begin > c || end < c + 16u) {                              // what is not written stays
+                const Word4 there = *reinterpret_cast<const Word4 *>(out);
 #pragma unroll
                 for (uint32_t k = 0; k < 4u; k++) {
-                    const uint32_t before = o <= c + 4u * k ? 0u : o - c - 4u * k;         // bytes of the word that are earlier tokens'
-                    const uint32_t keep = before >= 4u ? 0xFFFFFFFFu : (1u << (8u * before)) - 1u;
-                    r[k] = (rescaled(old[k], ratio) & keep) | (r[k] & ~keep);
+                    const uint32_t m = bytes_below(end, c + 4u * k) & ~bytes_below(begin, c + 4u * k);
+                    r[k] = (r[k] & m) | (there[k] & ~m);
                 }
             }
-            if (begin <= c && end >= c + 16u) { *reinterpret_cast<Word4 *>(out) = r; continue; }
+            *reinterpret_cast<Word4 *>(out) = r;
+        }
+    }
+}
+
+// A run of one token, as a step of decoding has them: a byte to every dim.  Where the scale grows or the earlier tokens come from another page they are
+// written with it, sixteen bytes of the page to a lane; what comes from another page is asked for together with the token.
+template <uint32_t kD, bool kValues>
+__device__ __forceinline__ void append_one(const AppendArgs &a, const Run &run, uint32_t h)
+{
+    constexpr uint32_t kWhich = kValues ? 1u : 0u, kOwn = kD / 64u;        // dims of a lane
+    constexpr uint32_t kEarly = 4;                                         // sixteen bytes each of the earlier tokens
+    const uint32_t lane = threadIdx.x & 63u, P = 1u << a.shift, o = run.o, dim = lane * kOwn;
+    const uint16_t *x = a.x[kWhich] + (int64_t)run.token * a.token_stride[kWhich] + (int64_t)h * a.head_stride[kWhich] + dim;
+    uint8_t *to = a.cache[kWhich] + ((size_t)run.page * a.heads + h) * (P * kD);
+    const uint8_t *from = a.cache[kWhich] + ((size_t)run.source * a.heads + h) * (P * kD);
+    float v[4] = {0.f, 0.f, 0.f, 0.f};
+    if (kOwn == 1u) v[0] = __uint_as_float((uint32_t)*x << 16);
+    else
+#pragma unroll
+        for (uint32_t i = 0; i < kOwn / 2u; i++) { const uint32_t w = reinterpret_cast<const uint32_t *>(x)[i]; v[2u * i] = low(w); v[2u * i + 1u] = high(w); }
+    const float was = o ? a.scale[kWhich][(size_t)run.source * a.heads + h] : 0.f;
+    // Sixteen bytes of the page, by their number.  Of keys the earlier tokens are the first o * kD bytes; of values the first o of every P bytes, with the new one behind them.
+    const bool moved = o && run.source != run.page, ahead = moved && P * kD <= kEarly * 1024u;
+    const uint32_t units = kValues ? P * kD / 16u : o * kD / 16u;
+    auto wanted = [&](uint32_t u) { return u < units && (!kValues || (u * 16u & (P - 1u)) <= o); };
+    Word4 early[kEarly] = {}, there[kEarly] = {};
+    if (ahead)
+#pragma unroll
+        for (uint32_t i = 0; i < kEarly; i++)
+            if (wanted(i * 64u + lane)) {
+                early[i] = reinterpret_cast<const Word4 *>(from)[i * 64u + lane];
+                if (kValues) there[i] = reinterpret_cast<const Word4 *>(to)[i * 64u + lane];
+            }
+    float top = 0.f;
+#pragma unroll
+    for (uint32_t i = 0; i < kOwn; i++) top = top_of(top, v[i]);
+#pragma unroll
+    for (int s = 32; s > 0; s >>= 1) top = __builtin_fmaxf(top, __shfl_xor(top, s));
+    const float now = __builtin_fmaxf(scale_for(top), was), inverse = 1.f / now, ratio = was / now;
+    if (lane == 0u) a.scale[kWhich][(size_t)run.page * a.heads + h] = now;
+    const uint32_t bytes = to_bytes(v[0] * inverse, v[1] * inverse, v[2] * inverse, v[3] * inverse);
+    const bool again = o && (moved || now != was);
+    if (again) {
+        auto put = [&](uint32_t u, Word4 w, const Word4 &was_there) {
+            const uint32_t of = u * 16u / P, at = u * 16u & (P - 1u);      // of values: the dim, and the first of these tokens
+            const uint32_t byte = kValues ? __shfl(bytes, of / kOwn) >> (8u * (of % kOwn)) & 0xFFu : 0u;
 #pragma unroll
             for (uint32_t k = 0; k < 4u; k++) {
-                const uint32_t b0 = c + 4u * k;
-                if (begin <= b0 && end >= b0 + 4u) { reinterpret_cast<uint32_t *>(out)[k] = r[k]; continue; }
-#pragma unroll
-                for (uint32_t i = 0; i < 4u; i++)
-                    if (b0 + i >= begin && b0 + i < end) out[4u * k + i] = (uint8_t)(r[k] >> (8u * i));
+                w[k] = rescaled(w[k], ratio);
+                if (!kValues) continue;
+                const uint32_t b0 = at + 4u * k, m = bytes_below(o, b0), mine = o - b0 < 4u ? 0xFFu << (8u * (o - b0)) : 0u;
+                w[k] = (w[k] & m) | (byte * 0x01010101u & mine) | (was_there[k] & ~(m | mine));
             }
-        }
-    };
-    auto number = [&](uint32_t word, uint32_t d) { return kOwn > 1u && d % 2u == 0u ? low(word) : high(word); };
-    if (held && (o & 15u) == 0u) {
-        // from the registers: token i of the run is number i % 16 of its column
-        if (again) for (uint32_t c = 0; c < o; c += 16u) column(c, [](uint32_t, uint32_t) { return 0.f; });
+            if (wanted(u)) reinterpret_cast<Word4 *>(to)[u] = w;
+        };
+        if (ahead) {
 #pragma unroll
-        for (uint32_t c = 0; c < kHeld; c += 16u)
-            if (c < n) column(o + c, [&](uint32_t i, uint32_t d) { return number(w[(c + i) % kLoads][d / 2u % kLoadWords], d); });
-        return;
-    }
-    for (uint32_t c = (again ? 0u : o) & ~15u; c < end; c += 16u) {
-        uint32_t v[16][kLoadWords];
-#pragma unroll
-        for (uint32_t i = 0; i < 16u; i++) {
-#pragma unroll
-            for (uint32_t k = 0; k < kLoadWords; k++) v[i][k] = 0u;
-            if (c + i >= o && c + i < end) {
-                if (n == 1u)
-#pragma unroll
-                    for (uint32_t k = 0; k < kLoadWords; k++) v[i][k] = w[0][k];
-                else load(c + i - o, v[i]);
+            for (uint32_t i = 0; i < kEarly; i++) if (i * 64u < units) put(i * 64u + lane, early[i], there[i]);
+        } else
+#pragma nounroll
+            for (uint32_t u0 = 0; u0 < units; u0 += 64u) {
+                const uint32_t u = u0 + lane < units ? u0 + lane : units - 1u;
+                const Word4 w = reinterpret_cast<const Word4 *>(from)[u];
+                put(u0 + lane, w, moved && kValues ? reinterpret_cast<const Word4 *>(to)[u] : w);
             }
-        }
-        column(c, [&](uint32_t i, uint32_t d) { return number(v[i][d / 2u % kLoadWords], d); });
     }
+    if (kValues) {
+        if (!again)
+#pragma unroll
+            for (uint32_t i = 0; i < kOwn; i++) to[(dim + i) * P + o] = (uint8_t)(bytes >> (8u * i));
+    } else if (kOwn == 1u) to[o * kD + dim] = (uint8_t)bytes;
+    else if (kOwn == 2u) *reinterpret_cast<uint16_t *>(to + o * kD + dim) = (uint16_t)bytes;
+    else *reinterpret_cast<uint32_t *>(to + o * kD + dim) = bytes;
 }
 
 constexpr uint32_t kAppendWaves = 4;
 template <uint32_t kD>
-__global__ void __launch_bounds__(kAppendWaves * 64u)
+__global__ void __launch_bounds__(kAppendWaves * 64u) __attribute__((amdgpu_waves_per_eu(4)))
 append_kernel(const AppendArgs a)
 {
     const uint32_t lane = threadIdx.x & 63u, P = 1u << a.shift, first = blockIdx.x * 64u, t = first + lane;
@@ -267,7 +279,10 @@ append_kernel(const AppendArgs a)
         const uint32_t follow = ~rest ? (uint32_t)__builtin_ctzll(~rest) : 64u;
         const uint32_t s = __builtin_amdgcn_readlane(slot, at), from = __builtin_amdgcn_readlane(origin, at), page = s >> a.shift;
         const Run run{first + at, page, from < a.pages ? from : page, s & (P - 1u), follow + 1u};
-        if (which) append_run<kD, true>(a, run, h);
+        if (run.n == 1u) {
+            if (which) append_one<kD, true>(a, run, h);
+            else append_one<kD, false>(a, run, h);
+        } else if (which) append_run<kD, true>(a, run, h);
         else append_run<kD, false>(a, run, h);
     }
 }

@@ -30,11 +30,12 @@ static __host__ __device__ inline uint32_t columns_of(uint32_t K) { return K <= 
 // The rows of a request before the step, after they took over their parents' tables.
 struct Rows {
     int32_t source[kBeamMax];                        // the row of the request whose table it takes; -1: none
+    uint32_t old[kBeamMax];                          // tokens of the old row
     uint32_t length[kBeamMax], have[kBeamMax], count[kBeamMax];    // of the new row: tokens, pages, tokens to come
-    uint32_t old_have[kBeamMax], col[kBeamMax];      // of the old row: pages; the place of the page that its children begin in
-    uint32_t child[kBeamMax], all_fork[kBeamMax];    // of the old row: has children; all of them copy their begun page
     uint32_t fork[kBeamMax];                         // the new row copies its begun page
     uint32_t need[kBeamMax], want[kBeamMax];         // of the new row: pages to be handed out, pages in all
+    // of the old row: its pages; those of them that some child has (all or none); those that a child goes on with (all but a begun one that all children copy)
+    uint4 ends[kBeamMax];
 };
 
 __device__ __forceinline__ uint32_t tokens_of(int32_t n, uint32_t most) { return n < 0 ? 0u : (uint32_t)n < most ? (uint32_t)n : most; }
@@ -55,62 +56,83 @@ __device__ __forceinline__ void read_columns(int32_t *ids, const int32_t *table,
     for (; k < K; k++) ids[k * width + tid] = table[(size_t)(row0 + k) * M + j];
 }
 
-// Fills in g (kFind: and finds the forks; else they are read).  The whole workgroup calls it; it ends behind a barrier.
+// What a thread k < K asks for of its row, early.
+struct RowLoads { int32_t parent, len, count; uint32_t fork; };
+__device__ __forceinline__ RowLoads load_row(const int32_t *lens, const int32_t *counts, const int32_t *parents, const uint32_t *forks, uint32_t row0, uint32_t K)
+{
+    const uint32_t k = threadIdx.x, r = row0 + k;
+    return k < K ? RowLoads{parents[r], lens[r], counts[r], forks ? forks[r] : 0u} : RowLoads{0, 0, 0, 0u};
+}
+
+// Fills in g.  kFind: and finds the forks (else they came with x): those that begin in the columns [j0, j0 + width), which lie in ids, and with `all` the others too.
+// The whole workgroup calls it; it ends behind a barrier.
 template <bool kFind>
-__device__ __forceinline__ void read_rows(Rows &g, const int32_t *table, const int32_t *lens, const int32_t *counts, const int32_t *parents, const uint32_t *forks,
-                                          uint32_t row0, uint32_t K, uint32_t M, uint32_t shift)
+__device__ __forceinline__ void read_rows(Rows &g, const RowLoads &x, const int32_t *table, const int32_t *ids, uint32_t j0, uint32_t width, bool all, uint32_t row0, uint32_t K,
+                                          uint32_t M, uint32_t shift)
 {
     const uint32_t k = threadIdx.x, page = 1u << shift;
     if (k < K) {
-        const int32_t p = parents[row0 + k] - (int32_t)row0;
-        const bool there = (uint32_t)p < K;
-        const uint32_t old = tokens_of(lens[row0 + k], M << shift);
-        g.source[k] = there ? p : -1;
-        g.count[k] = tokens_of(counts[row0 + k], 0x7FFFFFFFu);
-        g.old_have[k] = (old + page - 1u) >> shift;
-        g.col[k] = old >> shift;
-        g.length[k] = there ? tokens_of(lens[row0 + (there ? p : 0)], M << shift) : 0u;
-        g.have[k] = (g.length[k] + page - 1u) >> shift;
-        g.child[k] = 0u;
-        g.all_fork[k] = 1u;
-        g.fork[k] = kFind ? 0u : forks[row0 + k];
+        const int32_t p = x.parent - (int32_t)row0;
+        g.source[k] = (uint32_t)p < K ? p : -1;
+        g.old[k] = tokens_of(x.len, M << shift);
+        g.count[k] = tokens_of(x.count, 0x7FFFFFFFu);
+        g.fork[k] = x.fork;
     }
     __syncthreads();
+    if (k < K) {
+        g.length[k] = g.source[k] < 0 ? 0u : g.old[g.source[k]];
+        g.have[k] = (g.length[k] + page - 1u) >> shift;
+    }
     if (kFind) {
+        __syncthreads();
         // a begun page that another row has too
         for (uint32_t i = threadIdx.x; i < K * K; i += kPageThreads) {
             const uint32_t mine = i / K, other = i % K, c = g.length[mine] >> shift;
             if (mine == other || !g.count[mine] || !(g.length[mine] & (page - 1u)) || g.have[other] <= c) continue;
-            if (table[(size_t)(row0 + g.source[mine]) * M + c] == table[(size_t)(row0 + g.source[other]) * M + c]) g.fork[mine] = 1u;
+            const uint32_t a = (uint32_t)g.source[mine], b = (uint32_t)g.source[other];
+            if (c - j0 < width) { if (ids[a * width + c - j0] == ids[b * width + c - j0]) g.fork[mine] = 1u; }
+            else if (all && table[(size_t)(row0 + a) * M + c] == table[(size_t)(row0 + b) * M + c]) g.fork[mine] = 1u;
         }
         __syncthreads();
     }
     if (k < K) {
+        bool child = false, copied = true;
+#pragma unroll 8
         for (uint32_t c = 0; c < K; c++)
-            if (g.source[c] == (int32_t)k) { g.child[k] = 1u; g.all_fork[k] &= g.fork[c]; }
+            if (g.source[c] == (int32_t)k) { child = true; copied &= g.fork[c] != 0u; }
+        const uint32_t pages = (g.old[k] + page - 1u) >> shift;
+        g.ends[k] = uint4{pages, child ? pages : 0u, child ? (copied ? g.old[k] >> shift : pages) : 0u, 0u};
         g.want[k] = (uint32_t)(((uint64_t)g.length[k] + g.count[k] + page - 1u) >> shift);
         g.need[k] = g.fork[k] + g.want[k] - g.have[k];
     }
     __syncthreads();
 }
 
-// Calls gone(id, whatever) for the pages of column j that no new row refers to, in the order of the old rows; whatever: they go whether or not the request
-// is served.  ids: the thread's column.
-template <typename F>
-__device__ __forceinline__ void released_at(const Rows &g, const int32_t *ids, uint32_t width, uint32_t K, uint32_t j, F gone)
+// The old rows whose page at column j goes back, as bits: whatever becomes of the request, and where it is served besides.  ids: the thread's column.
+struct Gone { unsigned long long always, served; };
+__device__ __forceinline__ Gone gone_at(const Rows &g, const int32_t *ids, uint32_t width, uint32_t K, uint32_t j)
 {
-    for (uint32_t b = 0; b < K; b++) {
-        if (j >= g.old_have[b]) continue;
-        if (g.child[b] && !(g.all_fork[b] && j == g.col[b])) continue;          // a child goes on with it
+    Gone r{0ull, 0ull};
+    // (a child goes on with the others)
+    unsigned long long look = 0;
+#pragma unroll 8
+    for (uint32_t b = 0; b < K; b++) { const uint4 e = g.ends[b]; if (j < e.x && j >= e.z) look |= 1ull << b; }
+    while (look) {
+        const uint32_t b = (uint32_t)__builtin_ctzll(look);
+        look &= look - 1ull;
         const int32_t id = ids[b * width];
         bool first = true, referred = false, kept = false;
+#pragma unroll 4
         for (uint32_t o = 0; o < K; o++) {
-            if (ids[o * width] != id || j >= g.old_have[o]) continue;
-            if (o < b) first = false;
-            if (g.child[o]) { referred = true; kept |= !(g.all_fork[o] && j == g.col[o]); }
+            const uint4 e = g.ends[o];
+            const bool same = ids[o * width] == id && j < e.x;
+            first &= !(same && o < b);
+            referred |= same && j < e.y;
+            kept |= same && j < e.z;
         }
-        if (first && !kept) gone(id, !referred);
+        if (first && !kept) { if (referred) r.served |= 1ull << b; else r.always |= 1ull << b; }
     }
+    return r;
 }
 
 __device__ __forceinline__ uint32_t wave_sum(uint32_t x)
@@ -143,11 +165,12 @@ page_count_kernel(const int32_t *__restrict__ table, const int32_t *__restrict__
     __shared__ Rows g;
     __shared__ uint32_t part[2][kPageWaves];
     const uint32_t tid = threadIdx.x, row0 = blockIdx.x * K, width = columns_of(K), j = blockIdx.y * width + tid;
+    const RowLoads row = load_row(lens, counts, parents, nullptr, row0, K);
     read_columns(ids, table, row0, K, M, blockIdx.y * width, width);
-    read_rows<true>(g, table, lens, counts, parents, nullptr, row0, K, M, shift);
-    uint32_t always = 0, served = 0;
-    if (tid < width && j < M) released_at(g, ids + tid, width, K, j, [&](int32_t, bool whatever) { (whatever ? always : served)++; });
-    always = wave_sum(always); served = wave_sum(served);
+    read_rows<true>(g, row, table, ids, blockIdx.y * width, width, blockIdx.y == 0u, row0, K, M, shift);
+    Gone gone{0ull, 0ull};
+    if (tid < width && j < M) gone = gone_at(g, ids + tid, width, K, j);
+    const uint32_t always = wave_sum((uint32_t)__popcll(gone.always)), served = wave_sum((uint32_t)__popcll(gone.served));
     if ((tid & 63u) == 0u) { part[0][tid >> 6] = always; part[1][tid >> 6] = served; }
     __syncthreads();
     if (blockIdx.y == 0u && tid < K) forks[row0 + tid] = g.fork[tid];
@@ -197,33 +220,31 @@ __device__ __forceinline__ Served served_of(const GroupNeed &n, uint32_t before,
     return Served{asks, end, n.pages != kTooLong && (asks == 0u || end <= free)};
 }
 
-// The whole workgroup works out the sums over the requests [0, g0); need(i) and back(i, served) are a request's own.
-template <typename Need, typename Given>
-__device__ __forceinline__ Sums sums_before(uint32_t g0, uint32_t free, uint32_t N, uint32_t *part, bool releases, Need need, Given back)
+// The workgroup's sums of five values of its threads; `part` is 5 * kPageWaves words of LDS.
+struct Five { uint32_t x[5]; };
+__device__ __forceinline__ Five block_sums(Five v, uint32_t *part)
 {
-    Sums s{0u, 0u, 0u, 0u};
-    for (uint32_t i0 = 0; i0 < g0; i0 += kPageThreads) {
-        const uint32_t i = i0 + threadIdx.x;
-        const GroupNeed n = i < g0 ? need(i) : GroupNeed{0u, 0u};
-        const uint32_t asks = served_of(n, 0u, 0u, N).asks;
-        uint32_t all;
-        const uint32_t end = block_scan(asks, part, &all);
-        const Served v = served_of(n, add(s.pages, end - asks), free, N);
-        s.pages = add(s.pages, all);
-        (void)block_scan(v.yes ? asks : 0u, part, &all);
-        s.used += all;
-        if (releases) { (void)block_scan(i < g0 ? back(i, v.yes) : 0u, part, &all); s.released += all; }
-        (void)block_scan(n.tokens, part, &all);
-        s.tokens += all;
+#pragma unroll
+    for (uint32_t i = 0; i < 5u; i++) v.x[i] = wave_sum(v.x[i]);
+    __syncthreads();
+    if ((threadIdx.x & 63u) == 0u)
+#pragma unroll
+        for (uint32_t i = 0; i < 5u; i++) part[i * kPageWaves + (threadIdx.x >> 6)] = v.x[i];
+    __syncthreads();
+#pragma unroll
+    for (uint32_t i = 0; i < 5u; i++) {
+        v.x[i] = 0u;
+#pragma unroll
+        for (uint32_t w = 0; w < kPageWaves; w++) v.x[i] += part[i * kPageWaves + w];
     }
-    return s;
+    return v;
 }
 
 // Without parents: requests of one row.
 __global__ void __launch_bounds__(kPageThreads)
 page_kernel(const PageArgs a)
 {
-    __shared__ uint32_t part[kPageWaves];
+    __shared__ uint32_t part[5u * kPageWaves];
     const uint32_t tid = threadIdx.x, page = 1u << a.shift;
     const uint32_t r0 = blockIdx.x * a.per, r1 = a.rows - r0 < a.per ? a.rows : r0 + a.per;
     const uint64_t taken = a.counters[0], given = a.counters[1];
@@ -233,7 +254,18 @@ page_kernel(const PageArgs a)
         const uint32_t have = (length + page - 1u) >> a.shift, want = (uint32_t)(((uint64_t)length + count + page - 1u) >> a.shift);
         return GroupNeed{want > a.M ? kTooLong : want - have, count};
     };
-    Sums s = sums_before(r0, free, a.N, part, false, need_of, [](uint32_t, bool) { return 0u; });
+    Sums s{0u, 0u, 0u, 0u};
+    Five own{{0u, 0u, 0u, 0u, 0u}};                   // the thread's share: pages handed out, tokens
+    for (uint32_t i0 = 0; i0 < r0; i0 += kPageThreads) {
+        const GroupNeed n = i0 + tid < r0 ? need_of(i0 + tid) : GroupNeed{0u, 0u};
+        const uint32_t asks = served_of(n, 0u, 0u, a.N).asks;
+        uint32_t all;
+        const uint32_t end = block_scan(asks, part, &all);
+        own.x[0] += served_of(n, add(s.pages, end - asks), free, a.N).yes ? asks : 0u;
+        own.x[1] += n.tokens;
+        s.pages = add(s.pages, all);
+    }
+    if (r0) { own = block_sums(own, part); s.used = own.x[0]; s.tokens = own.x[1]; }
     for (uint32_t r = r0; r < r1; r++) {
         const GroupNeed n = need_of(r);
         const Served v = served_of(n, s.pages, free, a.N);
@@ -268,35 +300,75 @@ page_beam_kernel(const PageArgs a)
 {
     extern __shared__ int32_t ids[];
     __shared__ Rows g;
-    __shared__ uint32_t part[kPageWaves], begins[2][kBeamMax];
+    __shared__ uint32_t part[5u * kPageWaves], begins[2][kBeamMax], flags[kPageThreads];
     const uint32_t tid = threadIdx.x, page = 1u << a.shift, K = a.K, G = a.rows / K, width = columns_of(K), j0 = blockIdx.y * width, j = j0 + tid, chunks = gridDim.y;
     const uint32_t g0 = blockIdx.x * a.per, g1 = G - g0 < a.per ? G : g0 + a.per;
     const uint64_t taken = a.counters[0], given = a.counters[1];
     const uint32_t free = given <= taken ? 0u : given - taken < a.N ? (uint32_t)(given - taken) : a.N;
     const uint32_t head = (uint32_t)(taken % a.N), tail = (uint32_t)(given % a.N);
-    auto back_of = [&](uint32_t i, uint32_t n, bool served) {       // of the request's first n chunks
-        uint32_t x = 0;
-        for (uint32_t c = 0; c < n; c++) { const Back b = a.back[(size_t)i * chunks + c]; x += b.always + (served ? b.served : 0u); }
-        return x;
-    };
+    // Asked for at once: the columns, the rows of the workgroup's first request, and of the requests before it what the first rounds below look at.
+    constexpr uint32_t kAhead = 4;
+    RowLoads row = load_row(a.lens, a.counts, a.parents, a.forks, g0 * K, K);
+    GroupNeed need = a.needs[g0];
+    Back mine = tid < chunks ? a.back[(size_t)g0 * chunks + tid] : Back{0u, 0u};
+    const GroupNeed first_need = tid < g0 ? a.needs[tid] : GroupNeed{0u, 0u};
+    const uint32_t first_entries = (g0 < kPageThreads ? g0 : kPageThreads) * chunks;
+    Back first_back[kAhead];
+#pragma unroll
+    for (uint32_t q = 0; q < kAhead; q++) first_back[q] = tid + q * kPageThreads < first_entries ? a.back[tid + q * kPageThreads] : Back{0u, 0u};
     read_columns(ids, a.table, g0 * K, K, a.M, j0, width);
-    Sums s = sums_before(g0, free, a.N, part, true, [&](uint32_t i) { return a.needs[i]; }, [&](uint32_t i, bool served) { return back_of(i, chunks, served); });
+    Sums s{0u, 0u, 0u, 0u};
+    Five own{{0u, 0u, 0u, 0u, 0u}};                   // the thread's share: pages handed out, tokens, pages given back; those of the own request, and before these columns
+    for (uint32_t i0 = 0; i0 < g0; i0 += kPageThreads) {
+        const uint32_t n_groups = g0 - i0 < kPageThreads ? g0 - i0 : kPageThreads, entries = n_groups * chunks;
+        const GroupNeed n = !i0 ? first_need : tid < n_groups ? a.needs[i0 + tid] : GroupNeed{0u, 0u};
+        const uint32_t asks = served_of(n, 0u, 0u, a.N).asks;
+        uint32_t all;
+        const uint32_t end = block_scan(asks, part, &all);
+        const bool yes = served_of(n, add(s.pages, end - asks), free, a.N).yes;
+        own.x[0] += yes ? asks : 0u;
+        own.x[1] += n.tokens;
+        s.pages = add(s.pages, all);
+        flags[tid] = yes;
+        __syncthreads();
+        auto back = [&](uint32_t e, const Back &b) { own.x[2] += b.always + (b.served && flags[e / chunks] ? b.served : 0u); };
+        if (!i0)
+#pragma unroll
+            for (uint32_t q = 0; q < kAhead; q++) if (tid + q * kPageThreads < entries) back(tid + q * kPageThreads, first_back[q]);
+        for (uint32_t e = tid + (i0 ? 0u : kAhead * kPageThreads); e < entries; e += kPageThreads) back(e, a.back[(size_t)i0 * chunks + e]);
+    }
     for (uint32_t i = g0; i < g1; i++) {
-        const GroupNeed n = a.needs[i];
-        const Served v = served_of(n, s.pages, free, a.N);
         const uint32_t row0 = i * K;
-        if (i != g0) { __syncthreads(); read_columns(ids, a.table, row0, K, a.M, j0, width); }
-        const Back mine = a.back[(size_t)i * chunks + blockIdx.y];
-        const uint32_t back = back_of(i, chunks, v.yes), before = back_of(i, blockIdx.y, v.yes);
-        read_rows<false>(g, a.table, a.lens, a.counts, a.parents, a.forks, row0, K, a.M, a.shift);
+        if (i != g0) {
+            __syncthreads();
+            row = load_row(a.lens, a.counts, a.parents, a.forks, row0, K);
+            need = a.needs[i];
+            mine = tid < chunks ? a.back[(size_t)i * chunks + tid] : Back{0u, 0u};
+            read_columns(ids, a.table, row0, K, a.M, j0, width);
+        }
+        const GroupNeed n = need;
+        const Served v = served_of(n, s.pages, free, a.N);
+        own.x[3] = own.x[4] = 0u;
+        for (uint32_t c = tid; c < chunks; c += kPageThreads) {
+            const Back b = c == tid ? mine : a.back[(size_t)i * chunks + c];
+            const uint32_t x = b.always + (v.yes ? b.served : 0u);
+            own.x[3] += x;
+            if (c < blockIdx.y) own.x[4] += x;
+        }
+        const Five sums = block_sums(own, part);
+        if (i == g0) { s.used = sums.x[0]; s.tokens = sums.x[1]; s.released = sums.x[2]; }
+        const uint32_t back = sums.x[3], before = sums.x[4];
+        read_rows<false>(g, row, a.table, ids, j0, width, false, row0, K, a.M, a.shift);
         if (tid < K) {                                // where each row's pages and tokens begin
             uint32_t p = s.pages, t = s.tokens;
+#pragma unroll 8
             for (uint32_t k = 0; k < tid; k++) { p += g.need[k]; t += g.count[k]; }
             begins[0][tid] = p; begins[1][tid] = t;
         }
         __syncthreads();
         auto page_of = [&](uint32_t k, uint32_t at) { return a.ring[ring_at(head, begins[0][k] + at, a.N)]; };
         if (tid < width)
+#pragma unroll 4
             for (uint32_t k = 0; k < K; k++) {
                 const uint32_t have = g.have[k], fork = v.yes ? g.fork[k] : 0u;
                 if (j >= (v.yes ? g.want[k] : have)) continue;
@@ -321,13 +393,14 @@ page_beam_kernel(const PageArgs a)
                 if ((tid & 63u) == 0u) { a.lens_out[r] = (int32_t)(v.yes ? length + g.count[k] : length); a.starts[r] = (int32_t)first; }
             }
         }
-        if (mine.always || (v.yes && mine.served)) {
+        if (back) {
             // pages go back by place in the tables, then by row
-            uint32_t count = 0, all;
-            if (tid < width && j < a.M) released_at(g, ids + tid, width, K, j, [&](int32_t, bool whatever) { count += whatever || v.yes; });
-            uint32_t at = s.released + before + block_scan(count, part, &all) - count;
-            if (count)
-                released_at(g, ids + tid, width, K, j, [&](int32_t id, bool whatever) { if (whatever || v.yes) a.ring[ring_at(tail, at++, a.N)] = id; });
+            Gone gone{0ull, 0ull};
+            if (tid < width && j < a.M) gone = gone_at(g, ids + tid, width, K, j);
+            unsigned long long rows = gone.always | (v.yes ? gone.served : 0ull);
+            const uint32_t count = (uint32_t)__popcll(rows);
+            uint32_t all, at = s.released + before + block_scan(count, part, &all) - count;
+            for (; rows; rows &= rows - 1ull) a.ring[ring_at(tail, at++, a.N)] = ids[(uint32_t)__builtin_ctzll(rows) * width + tid];
         }
         s.pages = v.end;
         if (v.yes) s.used += v.asks;

@@ -117,6 +117,7 @@ int wg_cache_append(const void *d_k, const void *d_v, uint32_t tokens, uint32_t 
         WG_WANT(shift_of(page_tokens), "page_tokens must be 16, 32 or 64");
         WG_WANT((uint64_t)pages * page_tokens <= 0x7FFFFFFFull, "slots above 2^31 - 1");
         WG_WANT(by_sixteen(d_k, k_token_stride, k_head_stride) && by_sixteen(d_v, v_token_stride, v_head_stride), "keys and values must lie at multiples of 16 bytes");
+        WG_WANT(k_token_stride >= 0 && v_token_stride >= 0 && k_token_stride < 1 << 24 && v_token_stride < 1 << 24, "tokens must lie 0 to 2^24 - 1 elements apart");
         WG_WANT(aligned(d_k_cache, 16) && aligned(d_v_cache, 16), "the cache must be 16-byte aligned");
         return launch_cache_append(d_k, d_v, tokens, heads, dim, k_token_stride, k_head_stride, v_token_stride, v_head_stride, d_slots, d_origins, d_k_cache,
                                    d_v_cache, d_k_scale, d_v_scale, pages, shift_of(page_tokens), static_cast<hipStream_t>(stream));

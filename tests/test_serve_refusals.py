@@ -57,7 +57,8 @@ def test_cache_append():
     refused("wg_cache_append", "wg_cache_append", good, [
         dict([(k, None)]) for k in ("k", "v", "slots", "k_cache", "v_cache", "k_scale", "v_scale")] + [
         dict(tokens=0), dict(heads=0), dict(pages=0), dict(heads=65536), dict(dim=96), dict(dim=512), dict(page=24), dict(pages=1 << 27), dict(k0=129), dict(v1=4),
-        dict(k=C.c_void_p(4104)), dict(v=C.c_void_p(4098)), dict(k_cache=C.c_void_p(4104)), dict(v_cache=C.c_void_p(4104)), dict(tokens=1 << 31)])
+        dict(k=C.c_void_p(4104)), dict(v=C.c_void_p(4098)), dict(k_cache=C.c_void_p(4104)), dict(v_cache=C.c_void_p(4104)), dict(tokens=1 << 31),
+        dict(k0=1 << 24), dict(v0=-128)])
 
 
 def test_cache_attend():
