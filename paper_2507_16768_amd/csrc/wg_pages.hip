@@ -29,18 +29,18 @@ static __host__ __device__ inline uint32_t columns_of(uint32_t K) { return K <= 
 
 // The rows of a request before the step, after they took over their parents' tables.
 struct Rows {
-    int32_t source[kBeamMax];                        // the row of the request whose table it takes; -1: none
-    uint32_t old[kBeamMax];                          // tokens of the old row
-    uint32_t length[kBeamMax], have[kBeamMax], count[kBeamMax];    // of the new row: tokens, pages, tokens to come
-    uint32_t fork[kBeamMax];                         // the new row copies its begun page
-    uint32_t need[kBeamMax], want[kBeamMax];         // of the new row: pages to be handed out, pages in all
+    // of the new row: the row of the request whose table it takes (-1: none), its pages, its pages in all with the step, the place of a begun page that it
+    // copies (kNoFork: none)
+    int4 rows[kBeamMax];
+    uint32_t length[kBeamMax], count[kBeamMax], need[kBeamMax];    // its tokens, tokens to come, pages to be handed out
     // of the old row: its pages; those of them that some child has (all or none); those that a child goes on with (all but a begun one that all children copy)
     uint4 ends[kBeamMax];
 };
+constexpr uint32_t kNoFork = 0xFFFFFFFFu;
 
 __device__ __forceinline__ uint32_t tokens_of(int32_t n, uint32_t most) { return n < 0 ? 0u : (uint32_t)n < most ? (uint32_t)n : most; }
 
-// The request's columns [j0, j0 + width) to LDS, row by row, a column to a thread; nobody else reads it.
+// The request's columns [j0, j0 + width) to LDS, row by row, a column to a thread.
 __device__ __forceinline__ void read_columns(int32_t *ids, const int32_t *table, uint32_t row0, uint32_t K, uint32_t M, uint32_t j0, uint32_t width)
 {
     const uint32_t tid = threadIdx.x, j = j0 + tid;
@@ -64,46 +64,48 @@ __device__ __forceinline__ RowLoads load_row(const int32_t *lens, const int32_t 
     return k < K ? RowLoads{parents[r], lens[r], counts[r], forks ? forks[r] : 0u} : RowLoads{0, 0, 0, 0u};
 }
 
-// Fills in g.  kFind: and finds the forks (else they came with x): those that begin in the columns [j0, j0 + width), which lie in ids, and with `all` the others too.
-// The whole workgroup calls it; it ends behind a barrier.
+// Fills in g.  kFind: and finds the forks (else they came with x): those that begin in the columns [j0, j0 + width), which lie in ids, and with `all` the others
+// too.  The first wavefront does it, a lane to a row, with the rows' values out of its registers.  The whole workgroup calls it, behind a barrier after
+// read_columns where forks are to be found; it ends behind a barrier.
 template <bool kFind>
 __device__ __forceinline__ void read_rows(Rows &g, const RowLoads &x, const int32_t *table, const int32_t *ids, uint32_t j0, uint32_t width, bool all, uint32_t row0, uint32_t K,
                                           uint32_t M, uint32_t shift)
 {
     const uint32_t k = threadIdx.x, page = 1u << shift;
-    if (k < K) {
+    if (k < 64u) {
+        const bool row = k < K;
         const int32_t p = x.parent - (int32_t)row0;
-        g.source[k] = (uint32_t)p < K ? p : -1;
-        g.old[k] = tokens_of(x.len, M << shift);
-        g.count[k] = tokens_of(x.count, 0x7FFFFFFFu);
-        g.fork[k] = x.fork;
-    }
-    __syncthreads();
-    if (k < K) {
-        g.length[k] = g.source[k] < 0 ? 0u : g.old[g.source[k]];
-        g.have[k] = (g.length[k] + page - 1u) >> shift;
-    }
-    if (kFind) {
-        __syncthreads();
-        // a begun page that another row has too
-        for (uint32_t i = threadIdx.x; i < K * K; i += kPageThreads) {
-            const uint32_t mine = i / K, other = i % K, c = g.length[mine] >> shift;
-            if (mine == other || !g.count[mine] || !(g.length[mine] & (page - 1u)) || g.have[other] <= c) continue;
-            const uint32_t a = (uint32_t)g.source[mine], b = (uint32_t)g.source[other];
-            if (c - j0 < width) { if (ids[a * width + c - j0] == ids[b * width + c - j0]) g.fork[mine] = 1u; }
-            else if (all && table[(size_t)(row0 + a) * M + c] == table[(size_t)(row0 + b) * M + c]) g.fork[mine] = 1u;
+        const int32_t source = row && (uint32_t)p < K ? p : -1;
+        const uint32_t old = row ? tokens_of(x.len, M << shift) : 0u, count = tokens_of(x.count, 0x7FFFFFFFu), parents = (uint32_t)__shfl((int32_t)old, source < 0 ? 0 : source);
+        const uint32_t length = source < 0 ? 0u : parents, have = (length + page - 1u) >> shift, col = length >> shift;
+        const bool begun = row && count && (length & (page - 1u));
+        uint32_t fork = x.fork;
+        if (kFind) {
+            fork = 0u;
+#pragma unroll 4
+            for (uint32_t r = 0; r < K; r++) {            // a begun page that another row has too
+                const uint32_t c = (uint32_t)__builtin_amdgcn_readlane((int32_t)col, r), mine = (uint32_t)__builtin_amdgcn_readlane(source, r);
+                const bool here = c - j0 < width, there = have > c && k != r;
+                if (!here && !all) continue;
+                int32_t id = 0, of = 0;
+                if (there) {
+                    id = here ? ids[(uint32_t)source * width + c - j0] : table[(size_t)(row0 + (uint32_t)source) * M + c];
+                    of = (int32_t)mine < 0 ? 0 : here ? ids[mine * width + c - j0] : table[(size_t)(row0 + mine) * M + c];
+                }
+                const bool shared = __ballot(there && id == of) != 0ull;
+                if (k == r) fork = begun && shared;
+            }
         }
-        __syncthreads();
-    }
-    if (k < K) {
         bool child = false, copied = true;
 #pragma unroll 8
         for (uint32_t c = 0; c < K; c++)
-            if (g.source[c] == (int32_t)k) { child = true; copied &= g.fork[c] != 0u; }
-        const uint32_t pages = (g.old[k] + page - 1u) >> shift;
-        g.ends[k] = uint4{pages, child ? pages : 0u, child ? (copied ? g.old[k] >> shift : pages) : 0u, 0u};
-        g.want[k] = (uint32_t)(((uint64_t)g.length[k] + g.count[k] + page - 1u) >> shift);
-        g.need[k] = g.fork[k] + g.want[k] - g.have[k];
+            if (__builtin_amdgcn_readlane(source, c) == (int32_t)k) { child = true; copied &= __builtin_amdgcn_readlane((int32_t)fork, c) != 0; }
+        if (row) {
+            const uint32_t pages = (old + page - 1u) >> shift, want = (uint32_t)(((uint64_t)length + count + page - 1u) >> shift);
+            g.ends[k] = uint4{pages, child ? pages : 0u, child ? (copied ? old >> shift : pages) : 0u, 0u};
+            g.rows[k] = int4{source, (int32_t)have, (int32_t)want, (int32_t)(fork ? col : kNoFork)};
+            g.length[k] = length; g.count[k] = count; g.need[k] = (fork ? 1u : 0u) + want - have;
+        }
     }
     __syncthreads();
 }
@@ -113,6 +115,32 @@ struct Gone { unsigned long long always, served; };
 __device__ __forceinline__ Gone gone_at(const Rows &g, const int32_t *ids, uint32_t width, uint32_t K, uint32_t j)
 {
     Gone r{0ull, 0ull};
+    if (K <= 8u) {
+        // eight rows out of registers (by the loop below, trips to LDS one after the other, twice as long: 2.7 us for eight beams)
+        int32_t id[8];
+        uint32_t in = 0, referred = 0, kept = 0;      // the rows whose tables reach so far; as far as a child has them; as far as one goes on with them
+#pragma unroll
+        for (uint32_t o = 0; o < 8u; o++) {
+            const uint32_t k = o < K ? o : 0u;
+            const uint4 e = g.ends[k];
+            id[o] = ids[k * width];
+            in |= (uint32_t)(o < K && j < e.x) << o;
+            referred |= (uint32_t)(o < K && j < e.y) << o;
+            kept |= (uint32_t)(o < K && j < e.z) << o;
+        }
+        uint32_t always = 0, served = 0;
+#pragma unroll
+        for (uint32_t b = 0; b < 8u; b++) {
+            uint32_t same = 0;
+#pragma unroll
+            for (uint32_t o = 0; o < 8u; o++) same |= (uint32_t)(id[o] == id[b]) << o;
+            same &= in;
+            const bool gone = (same >> b & 1u) && !(same & ((1u << b) - 1u)) && !(same & kept);
+            if (gone) { if (same & referred) served |= 1u << b; else always |= 1u << b; }
+        }
+        r.always = always; r.served = served;
+        return r;
+    }
     // (a child goes on with the others)
     unsigned long long look = 0;
 #pragma unroll 8
@@ -167,13 +195,14 @@ page_count_kernel(const int32_t *__restrict__ table, const int32_t *__restrict__
     const uint32_t tid = threadIdx.x, row0 = blockIdx.x * K, width = columns_of(K), j = blockIdx.y * width + tid;
     const RowLoads row = load_row(lens, counts, parents, nullptr, row0, K);
     read_columns(ids, table, row0, K, M, blockIdx.y * width, width);
+    __syncthreads();
     read_rows<true>(g, row, table, ids, blockIdx.y * width, width, blockIdx.y == 0u, row0, K, M, shift);
     Gone gone{0ull, 0ull};
     if (tid < width && j < M) gone = gone_at(g, ids + tid, width, K, j);
     const uint32_t always = wave_sum((uint32_t)__popcll(gone.always)), served = wave_sum((uint32_t)__popcll(gone.served));
     if ((tid & 63u) == 0u) { part[0][tid >> 6] = always; part[1][tid >> 6] = served; }
     __syncthreads();
-    if (blockIdx.y == 0u && tid < K) forks[row0 + tid] = g.fork[tid];
+    if (blockIdx.y == 0u && tid < K) forks[row0 + tid] = (uint32_t)g.rows[tid].w != kNoFork;
     if (tid) return;
     Back b{0u, 0u};
     for (uint32_t w = 0; w < kPageWaves; w++) { b.always += part[0][w]; b.served += part[1][w]; }
@@ -181,10 +210,11 @@ page_count_kernel(const int32_t *__restrict__ table, const int32_t *__restrict__
     if (blockIdx.y) return;
     GroupNeed n{0u, 0u};
     bool fits = true;
+#pragma unroll 8
     for (uint32_t k = 0; k < K; k++) {
         n.tokens += g.count[k];
         n.pages += g.need[k];
-        fits &= g.want[k] <= M;
+        fits &= (uint32_t)g.rows[k].z <= M;
     }
     if (!fits) n.pages = kTooLong;
     needs[blockIdx.x] = n;
@@ -368,29 +398,30 @@ page_beam_kernel(const PageArgs a)
         __syncthreads();
         auto page_of = [&](uint32_t k, uint32_t at) { return a.ring[ring_at(head, begins[0][k] + at, a.N)]; };
         if (tid < width)
-#pragma unroll 4
+#pragma unroll 8
             for (uint32_t k = 0; k < K; k++) {
-                const uint32_t have = g.have[k], fork = v.yes ? g.fork[k] : 0u;
-                if (j >= (v.yes ? g.want[k] : have)) continue;
-                int32_t id;
-                if (j >= have) id = page_of(k, fork + j - have);
-                else if (fork && j == (g.length[k] >> a.shift)) id = page_of(k, 0u);
-                else id = ids[(uint32_t)g.source[k] * width + tid];
+                const int4 row = g.rows[k];               // source, pages, pages with the step, place of the fork
+                const uint32_t have = (uint32_t)row.y, fork = v.yes ? (uint32_t)row.w : kNoFork;
+                if (j >= (v.yes ? (uint32_t)row.z : have)) continue;
+                int32_t id = ids[(row.x < 0 ? 0u : (uint32_t)row.x) * width + tid];
+                if (j >= have) id = page_of(k, (fork != kNoFork ? 1u : 0u) + j - have);
+                else if (j == fork) id = page_of(k, 0u);
                 a.table_out[(size_t)(row0 + k) * a.M + j] = id;
             }
         if (blockIdx.y == 0u) {
             for (uint32_t k = tid >> 6; k < K; k += kPageWaves) {
-                const uint32_t length = g.length[k], have = g.have[k], fork = v.yes ? g.fork[k] : 0u, col = length >> a.shift, first = begins[1][k], r = row0 + k;
-                const int32_t *from = a.table + (size_t)(row0 + (g.source[k] < 0 ? 0u : (uint32_t)g.source[k])) * a.M;
-                auto page_at = [&](uint32_t c) { return c >= have ? page_of(k, fork + c - have) : fork && c == col ? page_of(k, 0u) : from[c]; };
-                for (uint32_t t = tid & 63u; t < g.count[k]; t += 64u) {
+                const int4 row = g.rows[k];
+                const uint32_t length = g.length[k], count = g.count[k], have = (uint32_t)row.y, fork = v.yes ? (uint32_t)row.w : kNoFork, first = begins[1][k], r = row0 + k;
+                const int32_t *from = a.table + (size_t)(row0 + (row.x < 0 ? 0u : (uint32_t)row.x)) * a.M;
+                auto page_at = [&](uint32_t c) { return c >= have ? page_of(k, (fork != kNoFork ? 1u : 0u) + c - have) : c == fork ? page_of(k, 0u) : from[c]; };
+                for (uint32_t t = tid & 63u; t < count; t += 64u) {
                     const uint32_t at = first + t, pos = length + t;
                     if (at >= a.tokens || at < first) break;
                     a.positions[at] = (int32_t)pos;
                     a.slots[at] = v.yes ? page_at(pos >> a.shift) << a.shift | (int32_t)(pos & (page - 1u)) : -1;
-                    a.origins[at] = t == 0u && fork ? from[col] : -1;
+                    a.origins[at] = t == 0u && fork != kNoFork ? from[fork] : -1;
                 }
-                if ((tid & 63u) == 0u) { a.lens_out[r] = (int32_t)(v.yes ? length + g.count[k] : length); a.starts[r] = (int32_t)first; }
+                if ((tid & 63u) == 0u) { a.lens_out[r] = (int32_t)(v.yes ? length + count : length); a.starts[r] = (int32_t)first; }
             }
         }
         if (back) {
