@@ -7,8 +7,7 @@
 // share of them is among the row's K best by (x, lower token): no score is made for any other token.  The logits are read once: a
 // thread keeps a running maximum and the sum of its tokens' exp against it, rescaled where the maximum moves.
 //
-// beam_rows_kernel: a workgroup of 1,024 threads takes a row, or one of `parts` shares of it, and leaves m, Z and the K best tokens
-// as keys.  beam_merge_kernel: a workgroup takes a request, joins the parts' m and Z and ranks the K * parts * K keys by their scores.
+// beam_rows_kernel: a workgroup of 256 threads takes one of `parts` shares of a row, and leaves m, Z and the K best tokens as keys.  beam_merge_kernel: a workgroup takes a request, joins the parts' m and Z and ranks the K * parts * K keys by their scores.
 #include <hip/hip_runtime.h>
 
 #include <cfloat>
@@ -28,12 +27,13 @@ __device__ __forceinline__ float exp_of(float x) { return __builtin_amdgcn_exp2f
 // V terms of at most 1, in a thousand partial sums: relative error some 1e-6 at the most).
 struct PartSum { float top, sum; };
 
+constexpr uint32_t kRowThreads = 256, kRowWaves = kRowThreads / 64u, kRowSeg = 1024, kRowCand = 512;
 struct BeamShared {
-    uint32_t words[kSegWords + 1u];                  // the staged mask
-    unsigned long long cand[kCand];                  // the candidates: rank << 32 | ~id
-    uint32_t threads[kThreads];                      // threads that hold candidates
-    uint32_t least[kWaves];
-    float top[kWaves], sum[kWaves];
+    uint32_t words[kRowSeg + 1u];                    // the staged mask
+    unsigned long long cand[kRowCand];               // the candidates: rank << 32 | ~id
+    uint32_t threads[kRowThreads];                   // threads that hold candidates
+    uint32_t least[kRowWaves];
+    float top[kRowWaves], sum[kRowWaves];
     uint32_t n, n_threads;
 };
 
@@ -61,11 +61,27 @@ __device__ __forceinline__ Numbers<4> numbers(const uint4 &v, uint32_t m, uint32
     return r;
 }
 
+// bound_of, where wavefronts may have next to nothing: then the most of what each one's k best reach.  (A row's last part, or a request with dead beams, gave no bound
+// at all, and everything was ranked: 55 us instead of 8 for the step after 16 prompts.)
+template <uint32_t kN>
+__device__ __forceinline__ uint32_t bound_of_some(uint32_t own, uint32_t k, uint32_t *least)
+{
+    uint32_t bound = bound_of<kN>(own, k, least);
+    if (bound) return bound;
+    __syncthreads();
+    const uint32_t mine = nth_of_wave(own, k);
+    if ((threadIdx.x & 63u) == 0u) least[threadIdx.x >> 6] = mine;
+    __syncthreads();
+#pragma unroll
+    for (uint32_t w = 0; w < kN; w++) bound = least[w] > bound ? least[w] : bound;
+    return bound;
+}
+
 __device__ __forceinline__ const uint32_t *mask_of(const uint32_t *mask, uint32_t row, uint32_t W) { return mask + (size_t)row * W; }
 __device__ __forceinline__ NoMask mask_of(NoMask none, uint32_t, uint32_t) { return none; }
 
 template <typename Elem, bool kWhole, typename Mask>
-__global__ void __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(8)))
+__global__ void __launch_bounds__(kRowThreads) __attribute__((amdgpu_waves_per_eu(8)))
 beam_rows_kernel(const Elem *__restrict__ logits, int64_t row_stride, uint32_t V, uint32_t W, Mask bitmask,
                  const float *__restrict__ scores, uint32_t K, unsigned long long *__restrict__ lists, PartSum *__restrict__ sums)
 {
@@ -74,7 +90,7 @@ beam_rows_kernel(const Elem *__restrict__ logits, int64_t row_stride, uint32_t V
     const uint32_t b = blockIdx.y, tid = threadIdx.x;
     unsigned long long *out = lists + ((size_t)b * gridDim.x + blockIdx.x) * K;
     if (!(scores[b] > -__builtin_inff())) {          // (NaN too) a beam that is not there
-        for (uint32_t i = tid; i < K; i += kThreads) out[i] = 0ull;
+        for (uint32_t i = tid; i < K; i += kRowThreads) out[i] = 0ull;
         if (tid == 0) sums[(size_t)b * gridDim.x + blockIdx.x] = PartSum{-FLT_MAX, 0.f};
         return;
     }
@@ -87,7 +103,7 @@ beam_rows_kernel(const Elem *__restrict__ logits, int64_t row_stride, uint32_t V
     float best = -__builtin_inff(), second = best, top = -FLT_MAX, sum = 0.f;
     uint32_t where = 0, held_mask = 0;
     uint4 held{0u, 0u, 0u, 0u};
-    stream_row(r, mask, W, sh.words, lo, hi, [&](uint32_t p, const uint4 &v, uint32_t m) {
+    stream_row<kRowThreads, kRowSeg>(r, mask, W, sh.words, lo, hi, [&](uint32_t p, const uint4 &v, uint32_t m) {
         const auto y = numbers(v, m, Elem(0));
         float x = y.x[0];
 #pragma unroll
@@ -110,7 +126,7 @@ beam_rows_kernel(const Elem *__restrict__ logits, int64_t row_stride, uint32_t V
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o);
     if ((tid & 63u) == 0u) { sh.top[tid >> 6] = wave_top; sh.sum[tid >> 6] = sum; }
-    const uint32_t bound = bound_of<kWaves>(own, K, sh.least);
+    const uint32_t bound = bound_of_some<kRowWaves>(own, K, sh.least);
     const float value = __builtin_fmaxf(bound ? bound_value(bound) : -FLT_MAX, -FLT_MAX);
     auto put = [&](const uint4 &v, uint32_t p, uint32_t m) {
         uint32_t take = reaching(v, m, 1u, value, Elem(0));
@@ -118,7 +134,7 @@ beam_rows_kernel(const Elem *__restrict__ logits, int64_t row_stride, uint32_t V
             const uint32_t i = (uint32_t)__builtin_ctz(take);
             take &= take - 1u;
             const uint32_t at = atomicAdd(&sh.n, 1u);
-            if (at < kCand) sh.cand[at] = key_of(r, v, p, i);
+            if (at < kRowCand) sh.cand[at] = key_of(r, v, p, i);
         }
     };
     // Candidates: the allowed tokens at or above the bound, most of them in the one piece that their thread holds; the pieces of threads that
@@ -130,24 +146,24 @@ beam_rows_kernel(const Elem *__restrict__ logits, int64_t row_stride, uint32_t V
     __syncthreads();
     if (tid == 0) {
         float t = sh.top[0], z = 0.f;
-        for (uint32_t w = 1; w < kWaves; w++) t = __builtin_fmaxf(t, sh.top[w]);
-        for (uint32_t w = 0; w < kWaves; w++) z += sh.sum[w] * exp_of(sh.top[w] - t);
+        for (uint32_t w = 1; w < kRowWaves; w++) t = __builtin_fmaxf(t, sh.top[w]);
+        for (uint32_t w = 0; w < kRowWaves; w++) z += sh.sum[w] * exp_of(sh.top[w] - t);
         sums[(size_t)b * gridDim.x + blockIdx.x] = PartSum{t, z};
     }
-    const uint32_t n_own = hi - lo, per = (n_own + kThreads - 1u) / kThreads, items = sh.n_threads * per;
-    for (uint32_t i = tid; i < items; i += kThreads) {
-        const uint32_t of = i / per, p = lo + sh.threads[of] + (i - of * per) * kThreads;
+    const uint32_t n_own = hi - lo, per = (n_own + kRowThreads - 1u) / kRowThreads, items = sh.n_threads * per;
+    for (uint32_t i = tid; i < items; i += kRowThreads) {
+        const uint32_t of = i / per, p = lo + sh.threads[of] + (i - of * per) * kRowThreads;
         const uint32_t m = p < hi ? piece_mask(r, mask, W, p) : 0u;
         if (m) put(r.piece(r.window(p, 1u), 0u), p, m);
     }
     __syncthreads();
     const uint32_t n = sh.n;
-    if (n > kCand) {
+    if (n > kRowCand) {
         // Hundreds of tokens tie.  K rounds, the best key below the last one each time.
         unsigned long long last = ~0ull;
         for (uint32_t q = 0; q < K; q++) {
             unsigned long long most = 0ull;
-            for (uint32_t p = lo + tid; p < hi; p += kThreads) {
+            for (uint32_t p = lo + tid; p < hi; p += kRowThreads) {
                 const uint32_t m = piece_mask(r, mask, W, p);
                 if (!m) continue;
                 const uint4 v = r.piece(r.window(p, 1u), 0u);
@@ -165,67 +181,87 @@ beam_rows_kernel(const Elem *__restrict__ logits, int64_t row_stride, uint32_t V
             if ((tid & 63u) == 0u) sh.cand[tid >> 6] = most;
             __syncthreads();
             last = sh.cand[0];
-            for (uint32_t w = 1; w < kWaves; w++) last = sh.cand[w] > last ? sh.cand[w] : last;
+            for (uint32_t w = 1; w < kRowWaves; w++) last = sh.cand[w] > last ? sh.cand[w] : last;
             if (tid == 0) out[q] = last;
         }
         return;
     }
-    rank_keys<kThreads>(sh.cand, n, K, [&](uint32_t at, unsigned long long key) { out[at] = key; });
-    for (uint32_t i = n + tid; i < K; i += kThreads) out[i] = 0ull;
+    rank_keys<kRowThreads>(sh.cand, n, K, [&](uint32_t at, unsigned long long key) { out[at] = key; });
+    for (uint32_t i = n + tid; i < K; i += kRowThreads) out[i] = 0ull;
 }
 
 // ---------------------------------------------------------------------------------------------
 constexpr uint32_t kMergeThreads = 256, kMergeWaves = kMergeThreads / 64u, kMergeCand = 1024;
+constexpr uint32_t kMergeHeld = 8;                   // keys of a thread that stay in registers
+constexpr uint32_t kMergeSums = 1024;                // parts of a request's rows whose sums are joined out of LDS
 
-// A request's continuations from its rows' lists.  Time: a few trips to memory and LDS, one after the other.
+// A request's continuations from its rows' lists.  Its time is trips to memory and between wavefronts, one after the other: all that it reads is asked for at once.
 __global__ void __launch_bounds__(kMergeThreads)
 beam_merge_kernel(const unsigned long long *__restrict__ lists, const PartSum *__restrict__ sums, uint32_t K, uint32_t parts,
                   const float *__restrict__ scores, const wg_state_t *__restrict__ states, float *__restrict__ scores_out,
                   int32_t *__restrict__ parents, int32_t *__restrict__ tokens, wg_state_t *__restrict__ states_out)
 {
     __shared__ unsigned long long cand[kMergeCand], cand_key[kMergeCand];      // order key of the score << 32 | ~beam; the row's key
+    __shared__ PartSum part[kMergeSums];
     __shared__ float row_top[kBeamMax], row_log[kBeamMax], row_score[kBeamMax];
+    __shared__ wg_state_t row_state[kBeamMax];
     __shared__ unsigned long long pair[2][kMergeWaves];
     __shared__ uint32_t least[kMergeWaves], n_cand;
-    const uint32_t tid = threadIdx.x, row0 = blockIdx.x * K, n = K * parts * K;
-    const unsigned long long *list = lists + (size_t)row0 * parts * K;
-    for (uint32_t k = tid; k < K; k += kMergeThreads) {
-        const PartSum *of = sums + (size_t)(row0 + k) * parts;
-        float t = of[0].top, z = 0.f;
-        for (uint32_t p = 1; p < parts; p++) t = __builtin_fmaxf(t, of[p].top);
-        for (uint32_t p = 0; p < parts; p++) z += of[p].sum * exp_of(of[p].top - t);
-        row_top[k] = t; row_log[k] = __builtin_amdgcn_logf(z) * kLn2; row_score[k] = scores[row0 + k];
+    const uint32_t tid = threadIdx.x, row0 = blockIdx.x * K, n = K * parts * K, entries = K * parts;
+    const unsigned long long *list = lists + (size_t)row0 * (parts * K);
+    const PartSum *sum = sums + (size_t)row0 * parts;
+    const bool staged = entries <= kMergeSums, held = n <= kMergeHeld * kMergeThreads;
+    // The i-th key: in order of rank, the lists' best first.  The wavefronts take them in turn, so that each has as many good ones as another and few reach the bound.  (List by list, a
+    // wavefront had some rows only, and where those were bad all keys were ranked: 27 us for 32 requests of eight beams.)
+    const uint32_t place = (tid & 63u) * kMergeWaves + (tid >> 6);
+    auto list_at = [&](uint32_t i) { return i % entries * K + i / entries; };
+    unsigned long long key[kMergeHeld];
+#pragma unroll
+    for (uint32_t q = 0; q < kMergeHeld; q++) key[q] = held && place + q * kMergeThreads < n ? list[list_at(place + q * kMergeThreads)] : 0ull;
+    for (uint32_t i = tid; staged && i < entries; i += kMergeThreads) part[i] = sum[i];
+    if (tid < K) {
+        row_score[tid] = scores[row0 + tid];
+        if (states) row_state[tid] = states[row0 + tid];
     }
     if (tid == 0) n_cand = 0u;
     __syncthreads();
-    auto score_of = [&](unsigned long long key, uint32_t beam) {
-        const uint32_t order = (uint32_t)(key >> 32) - 1u;
+    if (tid < K) {
+        const PartSum *of = staged ? part + tid * parts : sum + tid * parts;
+        float t = -FLT_MAX, z = 0.f;
+#pragma unroll 8
+        for (uint32_t p = 0; p < parts; p++) t = __builtin_fmaxf(t, of[p].top);
+#pragma unroll 8
+        for (uint32_t p = 0; p < parts; p++) z += of[p].sum * exp_of(of[p].top - t);
+        row_top[tid] = t; row_log[tid] = __builtin_amdgcn_logf(z) * kLn2;
+    }
+    __syncthreads();
+    auto score_of = [&](unsigned long long k, uint32_t beam) {
+        const uint32_t order = (uint32_t)(k >> 32) - 1u;
         const float x = __builtin_fminf(__uint_as_float((order & 0x80000000u) ? order & 0x7FFFFFFFu : ~order), FLT_MAX);
         return row_score[beam] + ((x - row_top[beam]) - row_log[beam]);
     };
-    // the key of a continuation, 0 where there is none
-    auto key_at = [&](uint32_t i, unsigned long long *key) {
-        *key = i < n ? list[i] : 0ull;
-        if (!*key) return 0ull;
-        const uint32_t beam = i / (parts * K);
-        const float s = score_of(*key, beam);
+    // what ranks the continuation i of a key, 0 where there is none
+    auto rank_at = [&](uint32_t i, unsigned long long k) {
+        if (!k) return 0ull;
+        const uint32_t beam = i % entries / parts;
+        const float s = score_of(k, beam);
         return s > -__builtin_inff() ? (unsigned long long)order_key(__float_as_uint(s)) << 32 | (0xFFFFFFFFu - beam) : 0ull;
     };
+    unsigned long long rank[kMergeHeld];
     uint32_t own = 0;
-    for (uint32_t i = tid; i < n; i += kMergeThreads) {
-        unsigned long long key;
-        const uint32_t high = (uint32_t)(key_at(i, &key) >> 32);
-        own = high > own ? high : own;
-    }
-    const uint32_t bound = bound_of<kMergeWaves>(own, K, least);
-    for (uint32_t i = tid; i < n; i += kMergeThreads) {
-        unsigned long long key;
-        const unsigned long long s = key_at(i, &key);
-        if (s && (uint32_t)(s >> 32) >= bound) {
-            const uint32_t at = atomicAdd(&n_cand, 1u);
-            if (at < kMergeCand) { cand[at] = s; cand_key[at] = key; }
-        }
-    }
+    auto raise = [&](unsigned long long r) { const uint32_t high = (uint32_t)(r >> 32); own = high > own ? high : own; };
+#pragma unroll
+    for (uint32_t q = 0; q < kMergeHeld; q++) { rank[q] = rank_at(place + q * kMergeThreads, key[q]); raise(rank[q]); }
+    for (uint32_t i = place; !held && i < n; i += kMergeThreads) raise(rank_at(i, list[list_at(i)]));
+    const uint32_t bound = bound_of_some<kMergeWaves>(own, K, least);
+    auto put = [&](unsigned long long r, unsigned long long k) {
+        if (!r || (uint32_t)(r >> 32) < bound) return;
+        const uint32_t at = atomicAdd(&n_cand, 1u);
+        if (at < kMergeCand) { cand[at] = r; cand_key[at] = k; }
+    };
+#pragma unroll
+    for (uint32_t q = 0; q < kMergeHeld; q++) put(rank[q], key[q]);
+    for (uint32_t i = place; !held && i < n; i += kMergeThreads) { const unsigned long long k = list[list_at(i)]; put(rank_at(i, k), k); }
     __syncthreads();
     uint32_t c = n_cand;
     if (c > kMergeCand) {
@@ -234,16 +270,15 @@ beam_merge_kernel(const unsigned long long *__restrict__ lists, const PartSum *_
         __syncthreads();
         for (uint32_t q = 0; q < K; q++) {
             unsigned long long best = 0ull, best_key = 0ull;
-            auto see = [&](unsigned long long s, unsigned long long key) {
-                if (s > best || (s == best && key > best_key)) { best = s; best_key = key; }
+            auto see = [&](unsigned long long r, unsigned long long k) {
+                if (r > best || (r == best && k > best_key)) { best = r; best_key = k; }
             };
             for (uint32_t i = tid; i < n; i += kMergeThreads) {
-                unsigned long long key;
-                const unsigned long long s = key_at(i, &key);
-                if (s < last || (s == last && key < last_key)) see(s, key);
+                const unsigned long long k = list[list_at(i)], r = rank_at(i, k);
+                if (r < last || (r == last && k < last_key)) see(r, k);
             }
 #pragma unroll
-            for (int o = 32; o > 0; o >>= 1) { const unsigned long long s = __shfl_xor(best, o), key = __shfl_xor(best_key, o); see(s, key); }
+            for (int o = 32; o > 0; o >>= 1) { const unsigned long long r = __shfl_xor(best, o), k = __shfl_xor(best_key, o); see(r, k); }
             if ((tid & 63u) == 0u) { pair[0][tid >> 6] = best; pair[1][tid >> 6] = best_key; }
             __syncthreads();
             for (uint32_t w = 0; w < kMergeWaves; w++) see(pair[0][w], pair[1][w]);
@@ -256,16 +291,17 @@ beam_merge_kernel(const unsigned long long *__restrict__ lists, const PartSum *_
     // ranked by counting, eight lanes to a continuation
     const uint32_t sub = tid & 7u;
     for (uint32_t i = tid >> 3; i < c; i += kMergeThreads / 8u) {
-        const unsigned long long s = cand[i], key = cand_key[i];
+        const unsigned long long s = cand[i], k = cand_key[i];
         uint32_t better = 0;
-        for (uint32_t q = sub; q < c; q += 8u) better += cand[q] > s || (cand[q] == s && cand_key[q] > key);
+#pragma unroll 4
+        for (uint32_t q = sub; q < c; q += 8u) better += cand[q] > s || (cand[q] == s && cand_key[q] > k);
         better += __shfl_xor(better, 1); better += __shfl_xor(better, 2); better += __shfl_xor(better, 4);
         if (sub == 0u && better < K) {
             const uint32_t beam = 0xFFFFFFFFu - (uint32_t)s, row = row0 + better;
-            scores_out[row] = score_of(key, beam);
+            scores_out[row] = score_of(k, beam);
             parents[row] = (int32_t)(row0 + beam);
-            tokens[row] = (int32_t)(0xFFFFFFFFu - (uint32_t)key);
-            if (states) states_out[row] = states[row0 + beam];
+            tokens[row] = (int32_t)(0xFFFFFFFFu - (uint32_t)k);
+            if (states) states_out[row] = row_state[beam];
         }
     }
     for (uint32_t i = c + tid; i < K; i += kMergeThreads) {           // fewer continuations than beams
@@ -276,12 +312,15 @@ beam_merge_kernel(const unsigned long long *__restrict__ lists, const PartSum *_
     }
 }
 
-// Workgroups of a row: about two per compute unit, with at least 8,192 tokens each.
-uint32_t beam_parts(uint32_t rows, uint32_t V)
+// Workgroups of a row: about eight per compute unit in all, with at least 2,048 tokens each.  A multiple of eight where it can be: workgroups go to the chip's eight XCDs in turn, and
+// each then has its share of every row, however the rows' masks differ.  The merge's keys stay within what its threads hold, or 8 parts.
+uint32_t beam_parts(uint32_t rows, uint32_t V, uint32_t K)
 {
-    const uint32_t most = (V + 8191u) / 8192u, want = 512u / rows;
-    const uint32_t parts = want < most ? want : most;
-    return parts < 1u ? 1u : parts > kBeamParts ? kBeamParts : parts;
+    const uint32_t most = (V + 2047u) / 2048u, want = 2048u / rows < 8u ? 8u : 2048u / rows, held = kMergeHeld * kMergeThreads / (K * K), room = held < 8u ? 8u : held;
+    uint32_t parts = want < most ? want : most;
+    if (parts > room) parts = room;
+    if (parts > kBeamParts) parts = kBeamParts;
+    return parts >= 8u ? parts / 8u * 8u : parts;
 }
 
 template <typename Elem, typename Mask>
@@ -289,7 +328,7 @@ static hipError_t beam_rows(const Elem *logits, uint32_t rows, uint32_t V, int64
                             unsigned long long *lists, PartSum *sums, hipStream_t s)
 {
     const bool whole = reinterpret_cast<uintptr_t>(logits) % sizeof(Elem) == 0u;
-    return launch(whole ? beam_rows_kernel<Elem, true, Mask> : beam_rows_kernel<Elem, false, Mask>, dim3(beam_parts(rows, V), rows), dim3(kThreads), 0, s, nullptr,
+    return launch(whole ? beam_rows_kernel<Elem, true, Mask> : beam_rows_kernel<Elem, false, Mask>, dim3(beam_parts(rows, V, K), rows), dim3(kRowThreads), 0, s, nullptr,
                   logits, row_stride, V, (V + 31u) / 32u, mask, scores, K, lists, sums);
 }
 
@@ -297,7 +336,7 @@ hipError_t launch_beam_select(const void *logits, int dtype, uint32_t rows, uint
                               const float *scores, const wg_state_t *states, float *scores_out, int32_t *parents, int32_t *tokens,
                               wg_state_t *states_out, void *workspace, hipStream_t s)
 {
-    const uint32_t parts = beam_parts(rows, V);
+    const uint32_t parts = beam_parts(rows, V, K);
     unsigned long long *lists = static_cast<unsigned long long *>(workspace);
     PartSum *sums = reinterpret_cast<PartSum *>(lists + (size_t)rows * parts * K);
     auto first = [&](auto *x) {

@@ -69,25 +69,26 @@ __device__ __forceinline__ uint32_t mask_word(const uint32_t *mask, uint32_t W, 
     return skew ? (hi << skew) | ((i ? word(i - 1u) : 0u) >> (32u - skew)) : hi;
 }
 
-// The words [w0, w0 + nw) of the same, nw up to kSegWords, to LDS, and a zero behind them; all of a thread's in flight together.
+// The words [w0, w0 + nw) of the same, nw up to kSeg, to LDS, and a zero behind them; all of a thread's in flight together.
 // The whole workgroup calls it.
+template <uint32_t kT, uint32_t kSeg>
 __device__ __forceinline__ void stage_mask(const uint32_t *mask, uint32_t W, uint32_t V, uint32_t skew, uint32_t w0, uint32_t nw, uint32_t *words)
 {
-    constexpr uint32_t kMost = kSegWords / kThreads;
+    constexpr uint32_t kMost = kSeg / kT;
     const Window win = window_of(mask + w0, (W > w0 ? W - w0 < nw ? W - w0 : nw : 0u) * 4u);
     const uint32_t tid = threadIdx.x, last = W - 1u - w0, tail = V & 31u ? (1u << (V & 31u)) - 1u : 0xFFFFFFFFu;
     uint32_t x[kMost], y[kMost];
 #pragma unroll
     for (uint32_t j = 0; j < kMost; j++) {
         x[j] = 0u; y[j] = 0u;
-        if (j * kThreads >= nw) continue;
-        x[j] = word_at(win, (tid + j * kThreads) * 4u);
-        if (skew) y[j] = tid + j * kThreads ? word_at(win, (tid + j * kThreads - 1u) * 4u) : w0 ? mask[w0 - 1u] : 0u;
+        if (j * kT >= nw) continue;
+        x[j] = word_at(win, (tid + j * kT) * 4u);
+        if (skew) y[j] = tid + j * kT ? word_at(win, (tid + j * kT - 1u) * 4u) : w0 ? mask[w0 - 1u] : 0u;
     }
 #pragma unroll
     for (uint32_t j = 0; j < kMost; j++) {
-        const uint32_t i = tid + j * kThreads;
-        if (j * kThreads >= nw) break;
+        const uint32_t i = tid + j * kT;
+        if (j * kT >= nw) break;
         if (i == last) x[j] &= tail;
         if (skew) x[j] = x[j] << skew | (i == last + 1u ? y[j] & tail : y[j]) >> (32u - skew);
         if (i < nw) words[i] = x[j];
@@ -102,9 +103,10 @@ __device__ __forceinline__ uint32_t mask_word(NoMask, uint32_t W, uint32_t V, ui
     auto word = [&](uint32_t w) { return w >= W ? 0u : w == W - 1u && (V & 31u) ? (1u << (V & 31u)) - 1u : 0xFFFFFFFFu; };
     return skew ? (word(i) << skew) | ((i ? word(i - 1u) : 0u) >> (32u - skew)) : word(i);
 }
+template <uint32_t kT, uint32_t kSeg>
 __device__ __forceinline__ void stage_mask(NoMask none, uint32_t W, uint32_t V, uint32_t skew, uint32_t w0, uint32_t nw, uint32_t *words)
 {
-    for (uint32_t i = threadIdx.x; i <= nw; i += kThreads) words[i] = i < nw ? mask_word(none, W, V, skew, w0 + i) : 0u;
+    for (uint32_t i = threadIdx.x; i <= nw; i += kT) words[i] = i < nw ? mask_word(none, W, V, skew, w0 + i) : 0u;
 }
 
 // The allowed tokens of piece p, from the mask as it lies in memory.
@@ -143,19 +145,19 @@ __device__ __forceinline__ float piece_max(const uint4 &v, uint32_t m, uint32_t)
 }
 
 // Streams the pieces [lo, hi) of the row, lo a multiple of 32: what(p, piece, allowed tokens) for every
-// piece of the thread that has an allowed token, in ascending order.  `words` is kSegWords + 1
-// words of LDS.  The whole workgroup calls it.
-template <typename Elem, bool kWhole, typename Mask, typename F>
+// piece of the thread that has an allowed token, in ascending order.  `words` is kSeg + 1
+// words of LDS.  The whole workgroup, of kT threads, calls it.
+template <uint32_t kT = kThreads, uint32_t kSeg = kSegWords, typename Elem, bool kWhole, typename Mask, typename F>
 __device__ __forceinline__ void stream_row(const Row<Elem, kWhole> &r, Mask mask, uint32_t W, uint32_t *words,
                                            uint32_t lo, uint32_t hi, F what)
 {
-    constexpr uint32_t kPer = Row<Elem, kWhole>::kPer, kSegPieces = kSegWords * 32u / kPer;
+    constexpr uint32_t kPer = Row<Elem, kWhole>::kPer, kSegPieces = kSeg * 32u / kPer;
     const uint32_t tid = threadIdx.x;
     for (uint32_t s0 = lo; s0 < hi; s0 += kSegPieces) {
         const uint32_t n = hi - s0 < kSegPieces ? hi - s0 : kSegPieces;
         const uint32_t w0 = s0 / (32u / kPer), nw = (n * kPer + 31u) / 32u;
         if (s0 != lo) __syncthreads();                     // the segment before is done with the LDS
-        stage_mask(mask, W, r.V, r.skew, w0, nw, words);
+        stage_mask<kT, kSeg>(mask, W, r.V, r.skew, w0, nw, words);
         __syncthreads();
         const uint32_t none = nw * (32u / kPer);           // a piece of the zero behind the words
         auto allowed = [&](uint32_t q) {
@@ -166,16 +168,16 @@ __device__ __forceinline__ void stream_row(const Row<Elem, kWhole> &r, Mask mask
         // Up to three pieces of a thread are one round: the loop below takes two more for nothing (the greedy choice, mixed, us, before there was
         // the loop / with it alone / so: V = 8,000, B = 1 3.9 / 4.3 / 3.7, 256 4.5 / 5.1 / 4.3; a row of 151,936 tokens in eight shares 5.6 / 6.3 / 5.8).
         constexpr uint32_t kRound = 3u;
-        if (n <= kThreads * kRound) {
+        if (n <= kT * kRound) {
             const Window win = r.window(s0, n);
             uint32_t mm[kRound];
             uint4 vv[kRound];
 #pragma unroll
-            for (uint32_t j = 0; j < kRound; j++) mm[j] = allowed(tid + j * kThreads);
+            for (uint32_t j = 0; j < kRound; j++) mm[j] = allowed(tid + j * kT);
 #pragma unroll
-            for (uint32_t j = 0; j < kRound; j++) vv[j] = r.piece(win, mm[j] ? (tid + j * kThreads) * 16u : kNowhere);
+            for (uint32_t j = 0; j < kRound; j++) vv[j] = r.piece(win, mm[j] ? (tid + j * kT) * 16u : kNowhere);
 #pragma unroll
-            for (uint32_t j = 0; j < kRound; j++) if (mm[j]) what(s0 + tid + j * kThreads, vv[j], mm[j]);
+            for (uint32_t j = 0; j < kRound; j++) if (mm[j]) what(s0 + tid + j * kT, vv[j], mm[j]);
             continue;
         }
         constexpr uint32_t kHalf = kWhole ? 3u : 2u;       // (of five words each, three are 3 % slower)
@@ -184,22 +186,22 @@ __device__ __forceinline__ void stream_row(const Row<Elem, kWhole> &r, Mask mask
         uint4 v[2][kHalf];
         auto request = [&](uint32_t (&mm)[kHalf], uint4 (&vv)[kHalf], uint32_t q0) {
 #pragma unroll
-            for (uint32_t j = 0; j < kHalf; j++) mm[j] = allowed(q0 + j * kThreads);
+            for (uint32_t j = 0; j < kHalf; j++) mm[j] = allowed(q0 + j * kT);
 #pragma unroll
-            for (uint32_t j = 0; j < kHalf; j++) vv[j] = r.piece(win, mm[j] ? (q0 + j * kThreads) * 16u : kNowhere);
+            for (uint32_t j = 0; j < kHalf; j++) vv[j] = r.piece(win, mm[j] ? (q0 + j * kT) * 16u : kNowhere);
         };
         auto look = [&](const uint32_t (&mm)[kHalf], const uint4 (&vv)[kHalf], uint32_t q0) {
 #pragma unroll
             for (uint32_t j = 0; j < kHalf; j++)
-                if (mm[j]) what(s0 + q0 + j * kThreads, vv[j], mm[j]);
+                if (mm[j]) what(s0 + q0 + j * kT, vv[j], mm[j]);
         };
         request(m[0], v[0], tid);
 #pragma nounroll
-        for (uint32_t q0 = tid; q0 < n; q0 += kThreads * kHalf * 2u) {
-            request(m[1], v[1], q0 + kThreads * kHalf);
+        for (uint32_t q0 = tid; q0 < n; q0 += kT * kHalf * 2u) {
+            request(m[1], v[1], q0 + kT * kHalf);
             look(m[0], v[0], q0);
-            request(m[0], v[0], q0 + kThreads * kHalf * 2u);
-            look(m[1], v[1], q0 + kThreads * kHalf);
+            request(m[0], v[0], q0 + kT * kHalf * 2u);
+            look(m[1], v[1], q0 + kT * kHalf);
         }
     }
 }

@@ -39,8 +39,8 @@ bool aligned(const void *p, uintptr_t n) { return reinterpret_cast<uintptr_t>(p)
 extern "C" {
 
 uint64_t wg_beam_select_workspace(uint32_t rows, uint32_t V, uint32_t beams) {
-    if (rows == 0 || V == 0) return 0;
-    return (uint64_t)rows * beam_parts(rows, V) * (beams + 1ull) * 8ull;
+    if (rows == 0 || V == 0 || beams == 0 || beams > kBeamMax) return 0;
+    return (uint64_t)rows * beam_parts(rows, V, beams) * (beams + 1ull) * 8ull;
 }
 
 int wg_beam_select(const void *d_logits, wg_dtype_t dtype, uint32_t rows, uint32_t V, int64_t row_stride_elems, const uint32_t *d_bitmask,

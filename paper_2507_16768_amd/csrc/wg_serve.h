@@ -10,7 +10,7 @@ namespace wg {
 constexpr uint32_t kBeamMax = 64;            // most beams of a request
 constexpr uint32_t kBeamParts = 32;          // most workgroups of a row
 constexpr uint32_t kMostRows = 65535;        // rows of a call: a dimension of the grid
-uint32_t beam_parts(uint32_t rows, uint32_t V);
+uint32_t beam_parts(uint32_t rows, uint32_t V, uint32_t K);
 hipError_t launch_beam_select(const void *logits, int dtype, uint32_t rows, uint32_t V, int64_t row_stride, const uint32_t *bitmask, uint32_t K,
                               const float *scores, const wg_state_t *states, float *scores_out, int32_t *parents, int32_t *tokens,
                               wg_state_t *states_out, void *workspace, hipStream_t s);

@@ -24,7 +24,7 @@ def refused(call, name, good, cases):
 
 def test_beam_select():
     need = wg.beam_select_workspace(8, 2000, 4)
-    assert need == 8 * 1 * 5 * 8 and wg.beam_select_workspace(0, 5, 1) == 0 and wg.beam_select_workspace(4, 32000, 4) == 4 * 4 * 5 * 8
+    assert need == 8 * 1 * 5 * 8 and wg.beam_select_workspace(0, 5, 1) == 0 and wg.beam_select_workspace(4, 5, 0) == 0 and wg.beam_select_workspace(4, 32000, 4) == 4 * 16 * 5 * 8
     good = dict(logits=P, dtype=0, rows=8, V=2000, stride=2000, mask=P, beams=4, scores=P, states=P, out=Q, parents=Q, tokens=Q, out_states=Q,
                 work=Q, bytes=need, stream=None)
     refused("wg_beam_select", "wg_beam_select", good, [
