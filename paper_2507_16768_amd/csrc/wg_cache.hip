@@ -352,19 +352,40 @@ __device__ __forceinline__ Word4 first_bytes(Word4 v, uint32_t n)
     }
     return v;
 }
-template <uint32_t kParts>
-__device__ __forceinline__ bool has_nan(const Word4 (&v)[kParts])
+// The NaNs among sixteen bytes, a byte of 1 (0x38 in the format) for each: their low seven bits are ones, one more carries into the eighth.
+__device__ __forceinline__ Word4 nans_of(Word4 v)
 {
-    uint32_t any = 0;                                // a byte is NaN where its low seven bits are ones: one more carries into the eighth
 #pragma unroll
-    for (uint32_t p = 0; p < kParts; p++)
+    for (uint32_t w = 0; w < 4u; w++) v[w] = (((v[w] & 0x7F7F7F7Fu) + 0x01010101u) >> 7 & 0x01010101u) * 0x38u;
+    return v;
+}
+// The same sixteen bytes with zeros in their place.
+__device__ __forceinline__ Word4 without_nans(Word4 v)
+{
 #pragma unroll
-        for (uint32_t w = 0; w < 4u; w++) any |= (v[p][w] & 0x7F7F7F7Fu) + 0x01010101u;
-    return any & 0x80808080u;
+    for (uint32_t w = 0; w < 4u; w++) v[w] &= ~((((v[w] & 0x7F7F7F7Fu) + 0x01010101u) >> 7 & 0x01010101u) * 0xFFu);
+    return v;
+}
+// A NaN where a query sees one among the values of sixteen keys for each of the lanes' dims, a zero elsewhere: the product of what is NaN and what the query sees.
+__device__ __forceinline__ Float4 nans_seen(Word4 v, uint32_t seen)
+{
+    const Word4 nans = nans_of(v);
+    Float4 n{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (uint32_t u = 0; u < 2u; u++) {
+        Word4 ones;
+#pragma unroll
+        for (uint32_t e = 0; e < 4u; e++) ones[e] = (u * 8u + 2u * e < seen ? 0x3C00u : 0u) | (u * 8u + 2u * e + 1u < seen ? 0x3C000000u : 0u);
+        n = __builtin_amdgcn_mfma_f32_16x16x32_f16(widened16(nans[u * 2u], nans[u * 2u + 1u]), __builtin_bit_cast(Short8, ones), n, 0, 0, 0);
+    }
+#pragma unroll
+    for (uint32_t e = 0; e < 4u; e++) n[e] = n[e] > 0.f ? __builtin_nanf("") : 0.f;
+    return n;
 }
 
-// Where a tile lies: the request whose tiles it is among, from the places at which the requests' tokens begin.  Request r's tiles begin at
-// starts[r] * group / 16 + r, which leaves room for each one's last, begun tile.  A wavefront asks 64 requests at a time.
+// Where a tile of kTile rows lies: the request whose tiles it is among, from the places at which the requests' tokens begin.  Request r's tiles begin at
+// starts[r] * group / kTile + r, which leaves room for each one's last, begun tile.  A wavefront asks 64 requests at a time.
+template <uint32_t kTile>
 __device__ __forceinline__ uint32_t request_of(const AttendArgs &a, uint32_t tile)
 {
     const uint32_t lane = threadIdx.x & 63u;
@@ -382,16 +403,17 @@ __device__ __forceinline__ uint32_t request_of(const AttendArgs &a, uint32_t til
 
 struct TileOf { uint32_t row, first, last, begin, count; int32_t before; };      // query rows [first, last) of a request with `count` tokens from `begin` on, behind `before` others
 
+template <uint32_t kTile, bool kLastFirst = false>
 __device__ __forceinline__ bool tile_of(const AttendArgs &a, uint32_t tile, uint32_t *len, TileOf *out)
 {
-    const uint32_t r = request_of(a, tile);
+    const uint32_t r = request_of<kTile>(a, tile);
     const uint32_t b = (uint32_t)a.starts[r] < a.tokens ? (uint32_t)a.starts[r] : a.tokens, e0 = (uint32_t)a.starts[r + 1u], e = e0 < b ? b : e0 < a.tokens ? e0 : a.tokens;
     const uint32_t at = tile - ((uint32_t)((uint64_t)b * a.group / kTile) + r), all = (e - b) * a.group;
     const uint32_t most = a.columns << a.shift, l = (uint32_t)(a.lens[r] < 0 ? 0 : a.lens[r]);
     *len = l < most ? l : most;
     if (tile < (uint32_t)((uint64_t)b * a.group / kTile) + r || (uint64_t)at * kTile >= all) return false;
     out->row = r; out->begin = b; out->count = e - b;
-    out->first = at * kTile;
+    out->first = (kLastFirst ? (all - 1u) / kTile - at : at) * kTile;
     out->last = all - out->first < kTile ? all : out->first + kTile;
     out->before = (int32_t)*len - (int32_t)(e - b);
     return true;
@@ -417,7 +439,7 @@ attend_kernel(const AttendArgs a)
     const uint32_t split = blockIdx.z, h = blockIdx.y, P = 1u << a.shift;
     uint32_t len;
     TileOf t;
-    if (!tile_of(a, blockIdx.x, &len, &t)) return;
+    if (!tile_of<kTile>(a, blockIdx.x, &len, &t)) return;
     const uint32_t sees_most = seen_by(t, t.last - 1u, a.group), blocks = (sees_most + kBlock - 1u) / kBlock;
     uint32_t per;
     const uint32_t shares = shares_of(blocks, a.splits, &per);
@@ -481,7 +503,14 @@ attend_kernel(const AttendArgs a)
             // values behind the row's end are whatever the pages held: they must not be NaN times a weight of zero
             const uint32_t there = mine >= len ? 0u : len - mine < 16u ? len - mine : 16u;
 #pragma unroll
-            for (uint32_t p = 0; p < kParts; p++) vw[p] = first_bytes(vw[p], there);
+            for (uint32_t p = 0; p < kParts; p++) {
+                vw[p] = first_bytes(vw[p], there);
+                // a NaN among the values reaches the queries that see it, and as a weight of zero times it no other
+                const Word4 clean = without_nans(vw[p]);
+                const bool nan = ((clean[0] ^ vw[p][0]) | (clean[1] ^ vw[p][1]) | (clean[2] ^ vw[p][2]) | (clean[3] ^ vw[p][3])) != 0u;
+                if (__ballot(nan)) o[p] += nans_seen(vw[p], mine >= sees ? 0u : sees - mine < 16u ? sees - mine : 16u);
+                vw[p] = clean;
+            }
         }
         if (__ballot(next != top)) {
             const float shrink = __builtin_amdgcn_exp2f(top - (next > -__builtin_inff() ? next : 0.f));
@@ -500,21 +529,6 @@ attend_kernel(const AttendArgs a)
                 sum += w[e] * v_inverse;
             }
             weights[u] = __builtin_bit_cast(Short8, Word4{pk_f16(w[0], w[1]), pk_f16(w[2], w[3]), pk_f16(w[4], w[5]), pk_f16(w[6], w[7])});
-        }
-        if (edge && __ballot(has_nan(vw))) {
-            // A NaN among the values, and queries that do not see all of them: each query has a product of its own, of what it sees.
-            for (uint32_t n = 0; n < kTile; n++) {
-                const uint32_t limit = __shfl(sees, n), mine_seen = mine >= limit ? 0u : limit - mine < 16u ? limit - mine : 16u;
-#pragma unroll
-                for (uint32_t p = 0; p < kParts; p++) {
-                    const Word4 v = first_bytes(vw[p], mine_seen);
-                    Float4 one{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                    for (uint32_t u = 0; u < 2u; u++) one = __builtin_amdgcn_mfma_f32_16x16x32_f16(widened16(v[u * 2u], v[u * 2u + 1u]), weights[u], one, 0, 0, 0);
-                    if (m == n) o[p] += one;
-                }
-            }
-            continue;
         }
 #pragma unroll
         for (uint32_t u = 0; u < 2u; u++)
@@ -553,7 +567,7 @@ attend_kernel(const AttendArgs a)
         if (d0 == 0u) { to[kD] = all; to[kD + 1u] = total; }
         return;
     }
-    const float by = total > 0.f ? 1.f / total : 0.f;            // (a row that sees nothing: zeros)
+    const float by = total > 0.f ? 1.f / total : total == total ? 0.f : total;            // (a row that sees nothing: zeros)
 #pragma unroll
     for (uint32_t d = 0; d < kPer; d += 2u) reinterpret_cast<uint32_t *>(a.out + at * kD + d0)[d / 2u] = pk_bf16(acc[d] * by, acc[d + 1u] * by);
 }
@@ -567,7 +581,7 @@ attend_join_kernel(const AttendArgs a)
     // by tile, to know how many shares it has
     uint32_t len, per;
     TileOf t;
-    if (!tile_of(a, blockIdx.x, &len, &t)) return;
+    if (!tile_of<kTile>(a, blockIdx.x, &len, &t)) return;
     const uint32_t sees_most = seen_by(t, t.last - 1u, a.group), shares = shares_of((sees_most + kBlock - 1u) / kBlock, a.splits, &per);
     if (shares < 2u || head >= a.heads * kTile) return;
     const uint32_t h = head / kTile, r = t.first + head % kTile;
@@ -590,7 +604,7 @@ attend_join_kernel(const AttendArgs a)
 #pragma unroll
         for (uint32_t d = 0; d < kOwn; d++) acc[d] += by * p[lane * kOwn + d];
     }
-    const float by = l > 0.f ? 1.f / l : 0.f;
+    const float by = l > 0.f ? 1.f / l : l == l ? 0.f : l;
     uint16_t *out = a.out + at * kD + lane * kOwn;
     if (kOwn == 1u) out[0] = (uint16_t)pk_bf16(acc[0] * by, 0.f);
     else
@@ -598,11 +612,257 @@ attend_join_kernel(const AttendArgs a)
         for (uint32_t d = 0; d < kOwn; d += 2u) reinterpret_cast<uint32_t *>(out)[d / 2u] = pk_bf16(acc[d] * by, acc[(d + 1u) % kOwn] * by);
 }
 
+// ---------------------------------------------------------------------------------------------
+// attention of many rows of a request: prompts.  A wavefront holds kTiles tiles of 16 query rows, four of them share their keys, 64 at a time, through LDS.  Bound
+// by the vector unit: exp and what goes with it of every score, and the cache's numbers turned into what the products take.  So the keys are not
+// turned into anything: scores come from the product of 8-bit numbers, with the queries as sums of two such numbers.  A bfloat16 number has 8 bits of
+// mantissa: four of them, rounded, are one, the rest is another, 2^5 times as large; with each row brought to its largest in [128, 256) that is exact down to 2^-15 of
+// the row's largest number, and what is smaller is off by 2^-24 of that.  The two products take as long as one in bfloat16 does.
+//
+// The running maximum is not followed from block to block: weights are relative to a base, float16 up to 2^15, and the base moves only
+// where a score would leave that range, to put the largest at 2^8.
+//
+// In LDS keys and values lie as in their pages, but for the places of the sixteen bytes of a row: eight lanes that read together find eight different ones.
+typedef int Int8 __attribute__((ext_vector_type(8)));
+constexpr float kRoom = 15.f, kAim = 8.f;            // log2 of the largest weight, and of the largest where the base moves to
+
+// Sixteen bytes c of row `key` of the keys: where they lie in their row.
+template <uint32_t kD>
+__device__ __forceinline__ uint32_t key_place(uint32_t key, uint32_t c)
+{
+    return kD == 64u ? c ^ ((key >> 1 & 1u) | (key >> 4 & 1u) << 1) : c ^ ((key & 3u) | (key >> 4 & 1u) << 2);
+}
+__device__ __forceinline__ uint32_t value_place(uint32_t dim, uint32_t c) { return c ^ (dim >> 1 & 3u); }
+
+template <uint32_t kD, uint32_t kTiles>
+__global__ void __launch_bounds__(kAttendWaves * 64u, 2)
+attend_wide_kernel(const AttendArgs a)
+{
+    constexpr uint32_t kSteps = kD / 32u, kParts = kD / 16u, kRows = kAttendWaves * kTile * kTiles, kThreads = kAttendWaves * 64u;
+    constexpr bool kBytes = kD >= 128u;              // scores from 8-bit numbers: products of 128 of them
+    constexpr uint32_t kLoads = kD * kBlock / (16u * kThreads);            // sixteen bytes of a thread, of keys and of values each
+    __shared__ Word4 keys[2][kD * kBlock / 16u], values[2][kD * kBlock / 16u];
+    const uint32_t tid = threadIdx.x, lane = tid & 63u, wave = __builtin_amdgcn_readfirstlane(tid >> 6), m = lane & 15u, g = lane >> 4;
+    const uint32_t h = blockIdx.x, P = 1u << a.shift;
+    uint32_t len;
+    TileOf t;
+    if (!tile_of<kRows, true>(a, blockIdx.y, &len, &t)) return;
+    const uint32_t blocks = (seen_by(t, t.last - 1u, a.group) + kBlock - 1u) / kBlock;
+    const int32_t *table = a.table + (size_t)t.row * a.columns;
+    const uint32_t last_column = a.columns - 1u;
+    auto page_at = [&](uint32_t key) {
+        const uint32_t c = key >> a.shift, id = (uint32_t)table[c < last_column ? c : last_column];
+        return id < a.pages ? id : 0u;               // (what lies behind a row's pages is masked, and must be somewhere)
+    };
+    // the wavefront's rows
+    const uint32_t w0 = t.first + wave * (kTile * kTiles);
+    const bool working = w0 < t.last;
+    uint32_t sees[kTiles];
+    float q_scale[kTiles];
+    Int8 q_high[kTiles][kBytes ? kD / 128u : 1u], q_low[kTiles][kBytes ? kD / 128u : 1u];
+    Half8 q_half[kTiles][kBytes ? 1u : kSteps];
+#pragma unroll
+    for (uint32_t n = 0; n < kTiles; n++) {
+        const uint32_t i = w0 + n * kTile + m < t.last ? w0 + n * kTile + m : t.last - 1u;
+        sees[n] = seen_by(t, i, a.group);
+        const uint16_t *q = a.q + (int64_t)(t.begin + i / a.group) * a.q_token + (int64_t)(h * a.group + i % a.group) * a.q_head + g * (kD / 4u);
+        q_scale[n] = a.scale;
+        if (!kBytes) {
+#pragma unroll
+            for (uint32_t k = 0; k < (kBytes ? 1u : kSteps); k++) q_half[n][k] = __builtin_bit_cast(Half8, *reinterpret_cast<const Word4 *>(q + k * 8u));
+            continue;
+        }
+        Word4 raw[kD / 32u];
+        float top = 0.f;
+#pragma unroll
+        for (uint32_t k = 0; k < kD / 32u; k++) {
+            raw[k] = *reinterpret_cast<const Word4 *>(q + k * 8u);
+#pragma unroll
+            for (uint32_t e = 0; e < 4u; e++) { top = top_of(top, low(raw[k][e])); top = top_of(top, high(raw[k][e])); }
+        }
+        top = __builtin_fmaxf(top, __shfl_xor(top, 16));
+        top = __builtin_fmaxf(top, __shfl_xor(top, 32));
+        const int e = 134 - (int)(__float_as_uint(top) >> 23), exponent = top > 0.f ? (e > 126 ? 126 : e) : 0;
+        const float up = __uint_as_float((uint32_t)(exponent + 127) << 23);
+        q_scale[n] = a.scale * __uint_as_float((uint32_t)(127 - exponent) << 23);
+#pragma unroll
+        for (uint32_t k = 0; k < kD / 32u; k++)
+#pragma unroll
+            for (uint32_t e2 = 0; e2 < 2u; e2++) {
+                const uint32_t x = raw[k][2u * e2], y = raw[k][2u * e2 + 1u];
+                const float v[4] = {low(x) * up, high(x) * up, low(y) * up, high(y) * up};
+                const uint32_t first = to_bytes(v[0], v[1], v[2], v[3]);
+                const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)first, false), hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)first, true);
+                q_high[n][k / 4u][k % 4u * 2u + e2] = (int)first;
+                q_low[n][k / 4u][k % 4u * 2u + e2] = (int)to_bytes((v[0] - lo[0]) * 32.f, (v[1] - lo[1]) * 32.f, (v[2] - hi[0]) * 32.f, (v[3] - hi[1]) * 32.f);
+            }
+    }
+    const uint32_t sees_least = working ? seen_by(t, w0, a.group) : 0u, sees_most = working ? seen_by(t, w0 + kTile * kTiles < t.last ? w0 + kTile * kTiles - 1u : t.last - 1u, a.group) : 0u;
+    Float4 o[kTiles][kParts];
+    float base[kTiles], sum[kTiles];
+#pragma unroll
+    for (uint32_t n = 0; n < kTiles; n++) {
+        base[n] = -__builtin_inff(); sum[n] = 0.f;
+#pragma unroll
+        for (uint32_t p = 0; p < kParts; p++) o[n][p] = Float4{0.f, 0.f, 0.f, 0.f};
+    }
+    // What a thread brings of a block: sixteen bytes at a time, to the places one behind the other; and the lane's scales of it.
+    const uint32_t value_dim = tid / 4u, value_chunk = value_place(value_dim, tid % 4u);
+    Word4 next_k[kLoads], next_v[kLoads];
+    float next_ks = 0.f, next_vs = 0.f;
+    uint32_t page_k[kLoads], page_v, page_s;
+    auto ask_pages = [&](uint32_t b) {
+#pragma unroll
+        for (uint32_t j = 0; j < kLoads; j++) page_k[j] = page_at(b * kBlock + (((j * kThreads + tid) * 16u / kD) & ~15u));
+        page_v = page_at(b * kBlock + value_chunk * 16u);
+        page_s = page_at(b * kBlock + g * 16u);
+    };
+    auto ask = [&](uint32_t b) {
+#pragma unroll
+        for (uint32_t j = 0; j < kLoads; j++) {
+            const uint32_t key = (j * kThreads + tid) * 16u / kD, c = key_place<kD>(key, (j * kThreads + tid) % (kD / 16u));
+            next_k[j] = *reinterpret_cast<const Word4 *>(a.k_cache + (((size_t)page_k[j] * a.heads + h) * P + ((b * kBlock + key) & (P - 1u))) * kD + c * 16u);
+            next_v[j] = *reinterpret_cast<const Word4 *>(a.v_cache + (((size_t)page_v * a.heads + h) * kD + j * (kThreads / 4u) + value_dim) * P + ((b * kBlock + value_chunk * 16u) & (P - 1u)));
+        }
+        next_ks = a.k_scale[(size_t)page_s * a.heads + h];
+        next_vs = a.v_scale[(size_t)page_s * a.heads + h];
+    };
+    auto put = [&](uint32_t to) {
+#pragma unroll
+        for (uint32_t j = 0; j < kLoads; j++) { keys[to][j * kThreads + tid] = next_k[j]; values[to][j * kThreads + tid] = next_v[j]; }
+    };
+    if (blocks) {
+        ask_pages(0u);
+        ask(0u);
+        if (blocks > 1u) ask_pages(1u);
+        put(0u);
+    }
+    for (uint32_t b = 0; b < blocks; b++) {
+        const float ks = next_ks;
+        // (a page of zeros may have a scale of zero; what lies behind a row's pages may have any)
+        const float vs = __builtin_fmaxf(next_vs, 0x1p-64f), v_log = __builtin_amdgcn_logf(vs), v_inverse = __builtin_amdgcn_rcpf(vs);
+        __syncthreads();
+        const uint32_t at = b & 1u, key0 = b * kBlock, mine = key0 + g * 16u;
+        if (b + 1u < blocks) {
+            ask(b + 1u);
+            if (b + 2u < blocks) ask_pages(b + 2u);
+        }
+        if (working && key0 < sees_most) {
+            const bool edge = key0 + kBlock > sees_least;            // a query of the wavefront does not see all of the block
+            Float4 s[kTiles][4];
+#pragma unroll
+            for (uint32_t n = 0; n < 4u; n++) {
+                const uint32_t key = (m >> 2) * 16u + n * 4u + (m & 3u);
+                Word4 kw[kD / 64u];
+#pragma unroll
+                for (uint32_t j = 0; j < kD / 64u; j++) kw[j] = keys[at][key * (kD / 16u) + key_place<kD>(key, g * (kD / 64u) + j)];
+#pragma unroll
+                for (uint32_t i = 0; i < kTiles; i++) s[i][n] = Float4{0.f, 0.f, 0.f, 0.f};
+                if (kBytes) {
+#pragma unroll
+                    for (uint32_t k = 0; k < kD / 128u; k++) {
+                        const Word4 x = kw[(2u * k) % (kD / 64u)], y = kw[(2u * k + 1u) % (kD / 64u)];
+                        const Int8 bytes{(int)x[0], (int)x[1], (int)x[2], (int)x[3], (int)y[0], (int)y[1], (int)y[2], (int)y[3]};
+#pragma unroll
+                        for (uint32_t i = 0; i < kTiles; i++) {
+                            // (scales of 1 and, for the smaller summands, 2^-5)
+                            s[i][n] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(bytes, q_low[i][k], s[i][n], 0, 0, 0, 127, 0, 122);
+                            s[i][n] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(bytes, q_high[i][k], s[i][n], 0, 0, 0, 127, 0, 127);
+                        }
+                    }
+                } else
+#pragma unroll
+                    for (uint32_t k = 0; k < kSteps; k++) {
+                        const Half8 x = widened(kw[k / 2u % (kD / 64u)][k % 2u * 2u], kw[k / 2u % (kD / 64u)][k % 2u * 2u + 1u]);
+#pragma unroll
+                        for (uint32_t i = 0; i < kTiles; i++) s[i][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, q_half[i][k % (kBytes ? 1u : kSteps)], s[i][n], 0, 0, 0);
+                    }
+            }
+            Short8 weights[kTiles][2];
+#pragma unroll
+            for (uint32_t i = 0; i < kTiles; i++) {
+                const float by = ks * q_scale[i], add = v_log - (base[i] > -__builtin_inff() ? base[i] : 0.f);
+                float high = -__builtin_inff();
+#pragma unroll
+                for (uint32_t n = 0; n < 4u; n++)
+#pragma unroll
+                    for (uint32_t e = 0; e < 4u; e++) {
+                        s[i][n][e] = __builtin_fmaf(s[i][n][e], by, add);
+                        if (edge && mine + n * 4u + e >= sees[i]) s[i][n][e] = -__builtin_inff();
+                        high = __builtin_fmaxf(high, s[i][n][e]);
+                    }
+                const bool begun = base[i] > -__builtin_inff();
+                if (__ballot(high > kRoom || (!begun && high > -__builtin_inff()))) {
+                    high = __builtin_fmaxf(high, __shfl_xor(high, 16));
+                    high = __builtin_fmaxf(high, __shfl_xor(high, 32));
+                    const bool moves = high > kRoom || (!begun && high > -__builtin_inff());
+                    const float by_how_much = moves ? high - kAim : 0.f, shrink = begun ? __builtin_amdgcn_exp2f(-by_how_much) : 1.f;
+                    if (moves) base[i] = (begun ? base[i] : 0.f) + by_how_much;
+                    sum[i] *= shrink;
+#pragma unroll
+                    for (uint32_t p = 0; p < kParts; p++) o[i][p] *= shrink;
+#pragma unroll
+                    for (uint32_t n = 0; n < 4u; n++) s[i][n] -= by_how_much;
+                }
+#pragma unroll
+                for (uint32_t u = 0; u < 2u; u++) {
+                    float w[8];
+#pragma unroll
+                    for (uint32_t e = 0; e < 8u; e++) {
+                        w[e] = __builtin_amdgcn_exp2f(s[i][u * 2u + e / 4u][e % 4u]);
+                        sum[i] = __builtin_fmaf(w[e], v_inverse, sum[i]);
+                    }
+                    weights[i][u] = __builtin_bit_cast(Short8, Word4{pk_f16(w[0], w[1]), pk_f16(w[2], w[3]), pk_f16(w[4], w[5]), pk_f16(w[6], w[7])});
+                }
+            }
+            const uint32_t there = mine >= len ? 0u : len - mine < 16u ? len - mine : 16u;
+#pragma unroll
+            for (uint32_t p = 0; p < kParts; p++) {
+                Word4 v = values[at][(p * 16u + m) * 4u + value_place(m, g)];
+                if (edge) {
+                    v = first_bytes(v, there);           // what lies behind the row's end must not be NaN times a weight of zero
+                    // a NaN among the values reaches the queries that see it, and as a weight of zero times it no other
+                    const Word4 clean = without_nans(v);
+                    const bool nan = ((clean[0] ^ v[0]) | (clean[1] ^ v[1]) | (clean[2] ^ v[2]) | (clean[3] ^ v[3])) != 0u;
+                    if (__ballot(nan))
+#pragma unroll
+                        for (uint32_t i = 0; i < kTiles; i++) o[i][p] += nans_seen(v, mine >= sees[i] ? 0u : sees[i] - mine < 16u ? sees[i] - mine : 16u);
+                    v = clean;
+                }
+#pragma unroll
+                for (uint32_t u = 0; u < 2u; u++) {
+                    const Short8 x = widened16(v[u * 2u], v[u * 2u + 1u]);
+#pragma unroll
+                    for (uint32_t i = 0; i < kTiles; i++) o[i][p] = __builtin_amdgcn_mfma_f32_16x16x32_f16(x, weights[i][u], o[i][p], 0, 0, 0);
+                }
+            }
+        }
+        if (b + 1u < blocks) put(at ^ 1u);           // (its last reader is behind this round's barrier)
+    }
+#pragma unroll
+    for (uint32_t i = 0; i < kTiles; i++) {
+        float total = sum[i];
+        total += __shfl_xor(total, 16);
+        total += __shfl_xor(total, 32);
+        const uint32_t r = w0 + i * kTile + m;
+        if (r >= t.last) continue;
+        const float by = total > 0.f ? 1.f / total : total == total ? 0.f : total;           // (a row that sees nothing: zeros)
+        uint16_t *out = a.out + ((size_t)(t.begin + r / a.group) * (a.heads * a.group) + h * a.group + r % a.group) * kD + g * 4u;
+#pragma unroll
+        for (uint32_t p = 0; p < kParts; p++)
+            *reinterpret_cast<Word2 *>(out + p * 16u) = Word2{pk_bf16(o[i][p][0] * by, o[i][p][1] * by), pk_bf16(o[i][p][2] * by, o[i][p][3] * by)};
+    }
+}
+
 static uint32_t tiles_of(uint32_t tokens, uint32_t rows, uint32_t group) { return (uint32_t)((uint64_t)tokens * group / kTile) + rows; }
+
+// Whether a request has query rows enough, on average, to fill a wavefront's two tiles.
+static bool attend_is_wide(uint32_t tokens, uint32_t rows, uint32_t group) { return (uint64_t)tokens * group >= 64ull * rows; }
 
 // Shares of a tile's keys: workgroups for four of them on every compute unit, 64 shares at most.
 uint32_t attend_splits(uint32_t tokens, uint32_t rows, uint32_t heads, uint32_t group, uint32_t columns, uint32_t shift)
 {
+    if (attend_is_wide(tokens, rows, group)) return 1u;
     const uint64_t tiles = (uint64_t)(tokens < rows ? tokens : rows) * ((group + kTile - 1u) / kTile) * heads;
     const uint64_t all = tokens > rows ? (uint64_t)tokens * group / kTile * heads : tiles, n = all > tiles ? all : tiles;
     const uint64_t want = (1024u + n - 1u) / n, blocks = (((uint64_t)columns << shift) + kBlock - 1u) / kBlock, most = (blocks + kLeastBlocks - 1u) / kLeastBlocks;
@@ -617,7 +877,14 @@ hipError_t launch_cache_attend(const void *q, uint32_t tokens, uint32_t heads, u
     const uint32_t splits = attend_splits(tokens, rows, heads, group, columns, shift), tiles = tiles_of(tokens, rows, group);
     const AttendArgs a{static_cast<const uint16_t *>(q), q_token, q_head, k_cache, v_cache, k_scale, v_scale, table, lens, starts, static_cast<uint16_t *>(out),
                        static_cast<float *>(workspace), scale * 1.44269504088896340736f, tokens, rows, heads, group, columns, pages, shift, splits, tiles};
-    const dim3 grid(tiles, heads, splits), block(kAttendWaves * 64u);
+    const dim3 block(kAttendWaves * 64u);
+    if (attend_is_wide(tokens, rows, group)) {
+        const uint32_t per = kAttendWaves * kTile * (dim == 256u ? 1u : 2u);
+        // (heads first: workgroups go to the XCDs in turn, and those of a head find its keys in their L2)
+        const dim3 wide(heads, (uint32_t)((uint64_t)tokens * group / per) + rows);
+        return launch(dim == 64u ? attend_wide_kernel<64, 2> : dim == 128u ? attend_wide_kernel<128, 2> : attend_wide_kernel<256, 1>, wide, block, 0, s, nullptr, a);
+    }
+    const dim3 grid(tiles, heads, splits);
     const hipError_t e = launch(dim == 64u ? attend_kernel<64> : dim == 128u ? attend_kernel<128> : attend_kernel<256>, grid, block, 0, s, nullptr, a);
     if (e != hipSuccess || splits == 1u) return e;
     return launch(dim == 64u ? attend_join_kernel<64> : dim == 128u ? attend_join_kernel<128> : attend_join_kernel<256>, dim3(tiles, heads * kTile / 4u), dim3(256), 0, s, nullptr, a);

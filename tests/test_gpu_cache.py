@@ -303,12 +303,43 @@ def test_a_long_row(L):
     check_attention(out, *attention(cache, x, table, lens, starts, 128 ** -0.5))
 
 
-@pytest.mark.parametrize("n", [130, 700])
-def test_a_long_prompt(n):
+@pytest.mark.parametrize("n,P,H,G,D", [(130, 32, 2, 4, 128), (700, 32, 2, 4, 128), (333, 16, 1, 7, 64), (150, 64, 3, 5, 256), (65, 16, 8, 1, 128), (260, 64, 1, 16, 64)])
+def test_a_long_prompt(n, P, H, G, D):
     torch, wg = _wg()
-    cache, table, lens, starts, q = case(4, 32, 2, 4, 128, [n + 77, 20, n], [n, 3, n // 2])
-    out, x = run(torch, wg, cache, table, lens, starts, q, 128 ** -0.5)
-    check_attention(out, *attention(cache, x, table, lens, starts, 128 ** -0.5))
+    cache, table, lens, starts, q = case(4, P, H, G, D, [n + 77, 20, n], [n, 3, n // 2])
+    # query rows of all sizes, and numbers of a row that are far below its largest
+    q *= 2.0 ** np.random.default_rng(1).integers(-3, 2, q.shape[:2] + (1,))
+    q[::3] *= 2.0 ** np.random.default_rng(2).integers(-24, 1, q[::3].shape)
+    q[5] = 0.0
+    out, x = run(torch, wg, cache, table, lens, starts, q, D ** -0.5, strided=G == 5)
+    check_attention(out, *attention(cache, x, table, lens, starts, D ** -0.5))
+
+
+@pytest.mark.parametrize("D,size", [(128, 1e30), (128, 1e-30), (256, 1e36), (64, 1e-37)])
+def test_queries_at_the_ends_of_the_range(D, size):
+    """What the scale brings back to the middle of it."""
+    torch, wg = _wg()
+    cache, table, lens, starts, q = case(9, 16, 1, 4, D, [90, 70], [90, 40])
+    out, x = run(torch, wg, cache, table, lens, starts, q * size, 0.1 / size)
+    check_attention(out, *attention(cache, x, table, lens, starts, 0.1 / size))
+
+
+def test_scores_that_rise_and_fall_along_a_prompt():
+    """The first keys far below the later ones, and far above; in tiles that see few of either."""
+    torch, wg = _wg()
+    D, n = 128, 400
+    for sign in (1, -1):
+        cache, table, lens, starts, q = case(10, 16, 1, 2, D, [n, n], [n, n])
+        for r in range(2):
+            for i in range(n):
+                p, o = table[r, i // 16], i % 16
+                cache.k[p, 0, o] = to_bytes(np.full(D, sign * (i / 8.0 if r else (i // 64) * 40.0 % 130)))
+                cache.ks[p, 0] = 1.0
+        q[:] = 0.0
+        q[:, :, 3] = 1.0
+        q[::2, 1, 3] = 0.01
+        out, x = run(torch, wg, cache, table, lens, starts, q, 1.0)
+        check_attention(out, *attention(cache, x, table, lens, starts, 1.0))
 
 
 def test_scores_that_are_far_apart_or_equal():
@@ -394,9 +425,9 @@ def test_same_bits_every_time_and_in_a_graph():
 def test_what_a_token_does_not_see_is_nothing_to_it():
     """A NaN or an infinity in a key or value reaches the tokens from its own on, and no other."""
     torch, wg = _wg()
-    for D, P in ((64, 16), (128, 32), (256, 64)):
-        n, L = 40, 70
-        cache, table, lens, starts, q = case(7, P, 1, 4, D, [L, L, L], [n, n, n])
+    for D, P, n, G in ((64, 16, 40, 4), (128, 32, 40, 4), (256, 64, 40, 4), (64, 64, 19, 1), (128, 16, 19, 2), (256, 32, 19, 2)):
+        L = 70
+        cache, table, lens, starts, q = case(7, P, 1, G, D, [L, L, L], [n, n, n])
         at = L - n + 17                                  # the 18th token's own key
         page, o = table[0, at // P], at % P
         cache.k[page, 0, o, 5] = 0x7F
@@ -405,7 +436,7 @@ def test_what_a_token_does_not_see_is_nothing_to_it():
         out, x = run(torch, wg, cache, table, lens, starts, q, D ** -0.5)
         got = torch.isnan(out).cpu().numpy()
         assert not got[:17].any() and got[17:n].all()
-        assert not got[n:n + 17].any() and got[n + 17:2 * n, :, 7].all() and got[n + 17:2 * n].sum() == (n - 17) * 4
+        assert not got[n:n + 17].any() and got[n + 17:2 * n, :, 7].all() and got[n + 17:2 * n].sum() == (n - 17) * G
         assert not got[2 * n:].any()
         clean = np.ones(out.shape, bool)
         clean[17:n] = False
