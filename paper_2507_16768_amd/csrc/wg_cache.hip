@@ -619,8 +619,8 @@ attend_join_kernel(const AttendArgs a)
 // mantissa: four of them, rounded, are one, the rest is another, 2^5 times as large; with each row brought to its largest in [128, 256) that is exact down to 2^-15 of
 // the row's largest number, and what is smaller is off by 2^-24 of that.  The two products take as long as one in bfloat16 does.
 //
-// The running maximum is not followed from block to block: weights are relative to a base, float16 up to 2^15, and the base moves only
-// where a score would leave that range, to put the largest at 2^8.
+// The running maximum is not followed from block to block: weights are relative to a base, and that moves only where one of them leaves float16's
+// range, which their sum shows, to put the largest at 2^8.
 //
 // In LDS keys and values lie as in their pages, but for the places of the sixteen bytes of a row: eight lanes that read together find eight different ones.
 typedef int Int8 __attribute__((ext_vector_type(8)));
@@ -633,6 +633,9 @@ __device__ __forceinline__ uint32_t key_place(uint32_t key, uint32_t c)
     return kD == 64u ? c ^ ((key >> 1 & 1u) | (key >> 4 & 1u) << 1) : c ^ ((key & 3u) | (key >> 4 & 1u) << 2);
 }
 __device__ __forceinline__ uint32_t value_place(uint32_t dim, uint32_t c) { return c ^ (dim >> 1 & 3u); }
+
+struct Yes { static constexpr bool value = true; };
+struct No { static constexpr bool value = false; };
 
 template <uint32_t kD, uint32_t kTiles>
 __global__ void __launch_bounds__(kAttendWaves * 64u, 2)
@@ -650,10 +653,6 @@ attend_wide_kernel(const AttendArgs a)
     const uint32_t blocks = (seen_by(t, t.last - 1u, a.group) + kBlock - 1u) / kBlock;
     const int32_t *table = a.table + (size_t)t.row * a.columns;
     const uint32_t last_column = a.columns - 1u;
-    auto page_at = [&](uint32_t key) {
-        const uint32_t c = key >> a.shift, id = (uint32_t)table[c < last_column ? c : last_column];
-        return id < a.pages ? id : 0u;               // (what lies behind a row's pages is masked, and must be somewhere)
-    };
     // the wavefront's rows
     const uint32_t w0 = t.first + wave * (kTile * kTiles);
     const bool working = w0 < t.last;
@@ -700,29 +699,46 @@ attend_wide_kernel(const AttendArgs a)
     const uint32_t sees_least = working ? seen_by(t, w0, a.group) : 0u, sees_most = working ? seen_by(t, w0 + kTile * kTiles < t.last ? w0 + kTile * kTiles - 1u : t.last - 1u, a.group) : 0u;
     Float4 o[kTiles][kParts];
     float base[kTiles], sum[kTiles];
+    bool begun[kTiles];                              // the lane's query has a base
 #pragma unroll
     for (uint32_t n = 0; n < kTiles; n++) {
-        base[n] = -__builtin_inff(); sum[n] = 0.f;
+        base[n] = 0.f; sum[n] = 0.f; begun[n] = false;
 #pragma unroll
         for (uint32_t p = 0; p < kParts; p++) o[n][p] = Float4{0.f, 0.f, 0.f, 0.f};
     }
-    // What a thread brings of a block: sixteen bytes at a time, to the places one behind the other; and the lane's scales of it.
-    const uint32_t value_dim = tid / 4u, value_chunk = value_place(value_dim, tid % 4u);
+    // What a thread brings of a block: sixteen bytes at a time, to the places one behind the other; and the lane's scales of it.  A block begins with a page, so
+    // that a thread's places in pages stay, and its columns go on by the pages of a block.
+    const size_t page_bytes = (size_t)a.heads * P * kD;
+    const uint8_t *k_head = a.k_cache + (size_t)h * P * kD, *v_head = a.v_cache + (size_t)h * P * kD;
+    const uint32_t value_dim = tid / 4u, value_chunk = value_place(value_dim, tid % 4u), column_step = kBlock >> a.shift;
+    uint32_t k_column[kLoads], k_at[kLoads], v_at[kLoads];
+#pragma unroll
+    for (uint32_t j = 0; j < kLoads; j++) {
+        const uint32_t key = (j * kThreads + tid) * 16u / kD, c = key_place<kD>(key, (j * kThreads + tid) % (kD / 16u));
+        k_column[j] = key >> a.shift;
+        k_at[j] = (key & (P - 1u)) * kD + c * 16u;
+        v_at[j] = (j * (kThreads / 4u) + value_dim) * P + (value_chunk * 16u & (P - 1u));
+    }
+    const uint32_t v_column = value_chunk * 16u >> a.shift, s_column = g * 16u >> a.shift;
     Word4 next_k[kLoads], next_v[kLoads];
     float next_ks = 0.f, next_vs = 0.f;
-    uint32_t page_k[kLoads], page_v, page_s;
-    auto ask_pages = [&](uint32_t b) {
-#pragma unroll
-        for (uint32_t j = 0; j < kLoads; j++) page_k[j] = page_at(b * kBlock + (((j * kThreads + tid) * 16u / kD) & ~15u));
-        page_v = page_at(b * kBlock + value_chunk * 16u);
-        page_s = page_at(b * kBlock + g * 16u);
+    uint32_t page_k[kLoads], page_v = 0, page_s = 0;
+    auto page_at = [&](uint32_t c) {
+        const uint32_t id = (uint32_t)table[c < last_column ? c : last_column];
+        return id < a.pages ? id : 0u;               // (what lies behind a row's pages is masked, and must be somewhere)
     };
-    auto ask = [&](uint32_t b) {
+    auto ask_pages = [&](uint32_t b) {
+        const uint32_t first = b * column_step;
+#pragma unroll
+        for (uint32_t j = 0; j < kLoads; j++) page_k[j] = page_at(first + k_column[j]);
+        page_v = page_at(first + v_column);
+        page_s = page_at(first + s_column);
+    };
+    auto ask = [&]() {
 #pragma unroll
         for (uint32_t j = 0; j < kLoads; j++) {
-            const uint32_t key = (j * kThreads + tid) * 16u / kD, c = key_place<kD>(key, (j * kThreads + tid) % (kD / 16u));
-            next_k[j] = *reinterpret_cast<const Word4 *>(a.k_cache + (((size_t)page_k[j] * a.heads + h) * P + ((b * kBlock + key) & (P - 1u))) * kD + c * 16u);
-            next_v[j] = *reinterpret_cast<const Word4 *>(a.v_cache + (((size_t)page_v * a.heads + h) * kD + j * (kThreads / 4u) + value_dim) * P + ((b * kBlock + value_chunk * 16u) & (P - 1u)));
+            next_k[j] = *reinterpret_cast<const Word4 *>(k_head + page_k[j] * page_bytes + k_at[j]);
+            next_v[j] = *reinterpret_cast<const Word4 *>(v_head + page_v * page_bytes + v_at[j]);
         }
         next_ks = a.k_scale[(size_t)page_s * a.heads + h];
         next_vs = a.v_scale[(size_t)page_s * a.heads + h];
@@ -731,113 +747,130 @@ attend_wide_kernel(const AttendArgs a)
 #pragma unroll
         for (uint32_t j = 0; j < kLoads; j++) { keys[to][j * kThreads + tid] = next_k[j]; values[to][j * kThreads + tid] = next_v[j]; }
     };
-    if (blocks) {
-        ask_pages(0u);
-        ask(0u);
-        if (blocks > 1u) ask_pages(1u);
-        put(0u);
-    }
-    for (uint32_t b = 0; b < blocks; b++) {
-        const float ks = next_ks;
+    // where the lane's keys and values lie in LDS
+    const uint32_t key_row = ((m >> 2) * 16u + (m & 3u)) * (kD / 16u), value_row = m * 4u + value_place(m, g);
+    // A block of keys; kEdge: some query of the wavefront does not see all of it.
+    auto look = [&](uint32_t b, float ks, float vs0, auto edge) {
+        constexpr bool kEdge = decltype(edge)::value;
+        const uint32_t at = b & 1u, mine = b * kBlock + g * 16u;
         // (a page of zeros may have a scale of zero; what lies behind a row's pages may have any)
-        const float vs = __builtin_fmaxf(next_vs, 0x1p-64f), v_log = __builtin_amdgcn_logf(vs), v_inverse = __builtin_amdgcn_rcpf(vs);
-        __syncthreads();
-        const uint32_t at = b & 1u, key0 = b * kBlock, mine = key0 + g * 16u;
-        if (b + 1u < blocks) {
-            ask(b + 1u);
-            if (b + 2u < blocks) ask_pages(b + 2u);
+        const float vs = __builtin_fmaxf(vs0, 0x1p-64f), v_log = __builtin_amdgcn_logf(vs), v_inverse = __builtin_amdgcn_rcpf(vs);
+        Float4 s[kTiles][4];
+#pragma unroll
+        for (uint32_t n = 0; n < 4u; n++) {
+            Word4 kw[kD / 64u];
+#pragma unroll
+            for (uint32_t j = 0; j < kD / 64u; j++) kw[j] = keys[at][key_row + n * 4u * (kD / 16u) + key_place<kD>((m >> 2) * 16u + (m & 3u), g * (kD / 64u) + j)];
+#pragma unroll
+            for (uint32_t i = 0; i < kTiles; i++) s[i][n] = Float4{0.f, 0.f, 0.f, 0.f};
+            if (kBytes) {
+#pragma unroll
+                for (uint32_t k = 0; k < kD / 128u; k++) {
+                    const Word4 x = kw[(2u * k) % (kD / 64u)], y = kw[(2u * k + 1u) % (kD / 64u)];
+                    const Int8 bytes{(int)x[0], (int)x[1], (int)x[2], (int)x[3], (int)y[0], (int)y[1], (int)y[2], (int)y[3]};
+#pragma unroll
+                    for (uint32_t i = 0; i < kTiles; i++)        // (scales of 1 and, for the smaller summands, 2^-5)
+                        s[i][n] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(bytes, q_low[i][k], s[i][n], 0, 0, 0, 127, 0, 122);
+#pragma unroll
+                    for (uint32_t i = 0; i < kTiles; i++)
+                        s[i][n] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(bytes, q_high[i][k], s[i][n], 0, 0, 0, 127, 0, 127);
+                }
+            } else
+#pragma unroll
+                for (uint32_t k = 0; k < kSteps; k++) {
+                    const Half8 x = widened(kw[k / 2u % (kD / 64u)][k % 2u * 2u], kw[k / 2u % (kD / 64u)][k % 2u * 2u + 1u]);
+#pragma unroll
+                    for (uint32_t i = 0; i < kTiles; i++) s[i][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, q_half[i][k % (kBytes ? 1u : kSteps)], s[i][n], 0, 0, 0);
+                }
         }
-        if (working && key0 < sees_most) {
-            const bool edge = key0 + kBlock > sees_least;            // a query of the wavefront does not see all of the block
-            Float4 s[kTiles][4];
+        Short8 weights[kTiles][2];
 #pragma unroll
-            for (uint32_t n = 0; n < 4u; n++) {
-                const uint32_t key = (m >> 2) * 16u + n * 4u + (m & 3u);
-                Word4 kw[kD / 64u];
+        for (uint32_t i = 0; i < kTiles; i++) {
+            const float by = ks * q_scale[i], add = v_log - (begun[i] ? base[i] : 0.f);
 #pragma unroll
-                for (uint32_t j = 0; j < kD / 64u; j++) kw[j] = keys[at][key * (kD / 16u) + key_place<kD>(key, g * (kD / 64u) + j)];
+            for (uint32_t n = 0; n < 4u; n++)
 #pragma unroll
-                for (uint32_t i = 0; i < kTiles; i++) s[i][n] = Float4{0.f, 0.f, 0.f, 0.f};
-                if (kBytes) {
+                for (uint32_t e = 0; e < 4u; e++) {
+                    s[i][n][e] = __builtin_fmaf(s[i][n][e], by, add);
+                    if (kEdge) s[i][n][e] = mine + n * 4u + e < sees[i] ? s[i][n][e] : -__builtin_inff();
+                }
+            // The weights, and their sum out of the numbers that the product takes.  A sum that is infinite says that the base has to move first.
+            float part;
+            auto weigh = [&]() {
+                part = 0.f;
 #pragma unroll
-                    for (uint32_t k = 0; k < kD / 128u; k++) {
-                        const Word4 x = kw[(2u * k) % (kD / 64u)], y = kw[(2u * k + 1u) % (kD / 64u)];
-                        const Int8 bytes{(int)x[0], (int)x[1], (int)x[2], (int)x[3], (int)y[0], (int)y[1], (int)y[2], (int)y[3]};
+                for (uint32_t u = 0; u < 2u; u++) {
+                    Word4 w;
 #pragma unroll
-                        for (uint32_t i = 0; i < kTiles; i++) {
-                            // (scales of 1 and, for the smaller summands, 2^-5)
-                            s[i][n] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(bytes, q_low[i][k], s[i][n], 0, 0, 0, 127, 0, 122);
-                            s[i][n] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(bytes, q_high[i][k], s[i][n], 0, 0, 0, 127, 0, 127);
-                        }
+                    for (uint32_t e = 0; e < 4u; e++) {
+                        const uint32_t two = pk_f16(__builtin_amdgcn_exp2f(s[i][u * 2u + e / 2u][e % 2u * 2u]), __builtin_amdgcn_exp2f(s[i][u * 2u + e / 2u][e % 2u * 2u + 1u]));
+                        part = __builtin_amdgcn_fdot2(__builtin_bit_cast(Short2, two), Short2{(_Float16)1.f, (_Float16)1.f}, part, false);
+                        w[e] = two;
                     }
-                } else
-#pragma unroll
-                    for (uint32_t k = 0; k < kSteps; k++) {
-                        const Half8 x = widened(kw[k / 2u % (kD / 64u)][k % 2u * 2u], kw[k / 2u % (kD / 64u)][k % 2u * 2u + 1u]);
-#pragma unroll
-                        for (uint32_t i = 0; i < kTiles; i++) s[i][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, q_half[i][k % (kBytes ? 1u : kSteps)], s[i][n], 0, 0, 0);
-                    }
-            }
-            Short8 weights[kTiles][2];
-#pragma unroll
-            for (uint32_t i = 0; i < kTiles; i++) {
-                const float by = ks * q_scale[i], add = v_log - (base[i] > -__builtin_inff() ? base[i] : 0.f);
+                    weights[i][u] = __builtin_bit_cast(Short8, w);
+                }
+            };
+            weigh();
+            if (__ballot(!begun[i] || !(part < __builtin_inff()))) {
                 float high = -__builtin_inff();
 #pragma unroll
                 for (uint32_t n = 0; n < 4u; n++)
 #pragma unroll
-                    for (uint32_t e = 0; e < 4u; e++) {
-                        s[i][n][e] = __builtin_fmaf(s[i][n][e], by, add);
-                        if (edge && mine + n * 4u + e >= sees[i]) s[i][n][e] = -__builtin_inff();
-                        high = __builtin_fmaxf(high, s[i][n][e]);
-                    }
-                const bool begun = base[i] > -__builtin_inff();
-                if (__ballot(high > kRoom || (!begun && high > -__builtin_inff()))) {
-                    high = __builtin_fmaxf(high, __shfl_xor(high, 16));
-                    high = __builtin_fmaxf(high, __shfl_xor(high, 32));
-                    const bool moves = high > kRoom || (!begun && high > -__builtin_inff());
-                    const float by_how_much = moves ? high - kAim : 0.f, shrink = begun ? __builtin_amdgcn_exp2f(-by_how_much) : 1.f;
-                    if (moves) base[i] = (begun ? base[i] : 0.f) + by_how_much;
-                    sum[i] *= shrink;
+                    for (uint32_t e = 0; e < 4u; e++) high = __builtin_fmaxf(high, s[i][n][e]);
+                high = __builtin_fmaxf(high, __shfl_xor(high, 16));
+                high = __builtin_fmaxf(high, __shfl_xor(high, 32));
+                const bool moves = begun[i] ? high > kRoom : high > -__builtin_inff();
+                const float how_much = moves ? high - kAim : 0.f, shrink = begun[i] ? __builtin_amdgcn_exp2f(-how_much) : 1.f;
+                base[i] += how_much;
+                begun[i] = begun[i] || moves;
+                sum[i] *= shrink;
 #pragma unroll
-                    for (uint32_t p = 0; p < kParts; p++) o[i][p] *= shrink;
+                for (uint32_t p = 0; p < kParts; p++) o[i][p] *= shrink;
 #pragma unroll
-                    for (uint32_t n = 0; n < 4u; n++) s[i][n] -= by_how_much;
-                }
-#pragma unroll
-                for (uint32_t u = 0; u < 2u; u++) {
-                    float w[8];
-#pragma unroll
-                    for (uint32_t e = 0; e < 8u; e++) {
-                        w[e] = __builtin_amdgcn_exp2f(s[i][u * 2u + e / 4u][e % 4u]);
-                        sum[i] = __builtin_fmaf(w[e], v_inverse, sum[i]);
-                    }
-                    weights[i][u] = __builtin_bit_cast(Short8, Word4{pk_f16(w[0], w[1]), pk_f16(w[2], w[3]), pk_f16(w[4], w[5]), pk_f16(w[6], w[7])});
-                }
+                for (uint32_t n = 0; n < 4u; n++) s[i][n] -= how_much;
+                weigh();
             }
-            const uint32_t there = mine >= len ? 0u : len - mine < 16u ? len - mine : 16u;
+            sum[i] = __builtin_fmaf(part, v_inverse, sum[i]);
+        }
+        const uint32_t there = !kEdge ? 16u : mine >= len ? 0u : len - mine < 16u ? len - mine : 16u;
 #pragma unroll
-            for (uint32_t p = 0; p < kParts; p++) {
-                Word4 v = values[at][(p * 16u + m) * 4u + value_place(m, g)];
-                if (edge) {
-                    v = first_bytes(v, there);           // what lies behind the row's end must not be NaN times a weight of zero
-                    // a NaN among the values reaches the queries that see it, and as a weight of zero times it no other
-                    const Word4 clean = without_nans(v);
-                    const bool nan = ((clean[0] ^ v[0]) | (clean[1] ^ v[1]) | (clean[2] ^ v[2]) | (clean[3] ^ v[3])) != 0u;
-                    if (__ballot(nan))
+        for (uint32_t p = 0; p < kParts; p++) {
+            Word4 v = values[at][p * 64u + value_row];
+            if (kEdge) {
+                v = first_bytes(v, there);           // what lies behind the row's end must not be NaN times a weight of zero
+                // a NaN among the values reaches the queries that see it, and as a weight of zero times it no other
+                const Word4 clean = without_nans(v);
+                const bool nan = ((clean[0] ^ v[0]) | (clean[1] ^ v[1]) | (clean[2] ^ v[2]) | (clean[3] ^ v[3])) != 0u;
+                if (__ballot(nan))
 #pragma unroll
-                        for (uint32_t i = 0; i < kTiles; i++) o[i][p] += nans_seen(v, mine >= sees[i] ? 0u : sees[i] - mine < 16u ? sees[i] - mine : 16u);
-                    v = clean;
-                }
+                    for (uint32_t i = 0; i < kTiles; i++) o[i][p] += nans_seen(v, mine >= sees[i] ? 0u : sees[i] - mine < 16u ? sees[i] - mine : 16u);
+                v = clean;
+            }
 #pragma unroll
-                for (uint32_t u = 0; u < 2u; u++) {
-                    const Short8 x = widened16(v[u * 2u], v[u * 2u + 1u]);
+            for (uint32_t u = 0; u < 2u; u++) {
+                const Short8 x = widened16(v[u * 2u], v[u * 2u + 1u]);
 #pragma unroll
-                    for (uint32_t i = 0; i < kTiles; i++) o[i][p] = __builtin_amdgcn_mfma_f32_16x16x32_f16(x, weights[i][u], o[i][p], 0, 0, 0);
-                }
+                for (uint32_t i = 0; i < kTiles; i++) o[i][p] = __builtin_amdgcn_mfma_f32_16x16x32_f16(x, weights[i][u], o[i][p], 0, 0, 0);
             }
         }
-        if (b + 1u < blocks) put(at ^ 1u);           // (its last reader is behind this round's barrier)
+    };
+    if (blocks) {
+        ask_pages(0u);
+        ask();
+        if (blocks > 1u) ask_pages(1u);
+        put(0u);
+    }
+    const uint32_t whole = sees_least / kBlock;      // blocks that all queries of the wavefront see
+    for (uint32_t b = 0; b < blocks; b++) {
+        const float ks = next_ks, vs = next_vs;
+        __syncthreads();
+        if (b + 1u < blocks) {
+            ask();
+            if (b + 2u < blocks) ask_pages(b + 2u);
+        }
+        if (b < whole) look(b, ks, vs, No{});
+        else if (b * kBlock < sees_most) look(b, ks, vs, Yes{});
+        if (b + 1u < blocks) put(b & 1u ^ 1u);       // (its last reader is behind this round's barrier)
     }
 #pragma unroll
     for (uint32_t i = 0; i < kTiles; i++) {
