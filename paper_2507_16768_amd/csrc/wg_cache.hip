@@ -363,11 +363,15 @@ __device__ __forceinline__ Word4 nans_of(Word4 v)
 __device__ __forceinline__ Word4 without_nans(Word4 v)
 {
 #pragma unroll
-    for (uint32_t w = 0; w < 4u; w++) v[w] &= ~((((v[w] & 0x7F7F7F7Fu) + 0x01010101u) >> 7 & 0x01010101u) * 0xFFu);
+    for (uint32_t w = 0; w < 4u; w++) {
+        const uint32_t top = ((v[w] & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u;
+        v[w] &= ~(top | (top - (top >> 7)));
+    }
     return v;
 }
-// A NaN where a query sees one among the values of sixteen keys for each of the lanes' dims, a zero elsewhere: the product of what is NaN and what the query sees.
-__device__ __forceinline__ Float4 nans_seen(Word4 v, uint32_t seen)
+__device__ __forceinline__ bool differ(Word4 a, Word4 b) { return ((a[0] ^ b[0]) | (a[1] ^ b[1]) | (a[2] ^ b[2]) | (a[3] ^ b[3])) != 0u; }
+// Which of a lane's four outputs (dims of a part, for its query) see a NaN among the values of sixteen keys, as bits: the product of what is NaN and what the query sees.
+__device__ __forceinline__ uint32_t nans_seen(Word4 v, uint32_t seen)
 {
     const Word4 nans = nans_of(v);
     Float4 n{0.f, 0.f, 0.f, 0.f};
@@ -378,9 +382,7 @@ __device__ __forceinline__ Float4 nans_seen(Word4 v, uint32_t seen)
         for (uint32_t e = 0; e < 4u; e++) ones[e] = (u * 8u + 2u * e < seen ? 0x3C00u : 0u) | (u * 8u + 2u * e + 1u < seen ? 0x3C000000u : 0u);
         n = __builtin_amdgcn_mfma_f32_16x16x32_f16(widened16(nans[u * 2u], nans[u * 2u + 1u]), __builtin_bit_cast(Short8, ones), n, 0, 0, 0);
     }
-#pragma unroll
-    for (uint32_t e = 0; e < 4u; e++) n[e] = n[e] > 0.f ? __builtin_nanf("") : 0.f;
-    return n;
+    return (n[0] > 0.f ? 1u : 0u) | (n[1] > 0.f ? 2u : 0u) | (n[2] > 0.f ? 4u : 0u) | (n[3] > 0.f ? 8u : 0u);
 }
 
 // Where a tile of kTile rows lies: the request whose tiles it is among, from the places at which the requests' tokens begin.  Request r's tiles begin at
@@ -507,8 +509,11 @@ attend_kernel(const AttendArgs a)
                 vw[p] = first_bytes(vw[p], there);
                 // a NaN among the values reaches the queries that see it, and as a weight of zero times it no other
                 const Word4 clean = without_nans(vw[p]);
-                const bool nan = ((clean[0] ^ vw[p][0]) | (clean[1] ^ vw[p][1]) | (clean[2] ^ vw[p][2]) | (clean[3] ^ vw[p][3])) != 0u;
-                if (__ballot(nan)) o[p] += nans_seen(vw[p], mine >= sees ? 0u : sees - mine < 16u ? sees - mine : 16u);
+                if (__ballot(differ(clean, vw[p]))) {
+                    const uint32_t bits = nans_seen(vw[p], mine >= sees ? 0u : sees - mine < 16u ? sees - mine : 16u);
+#pragma unroll
+                    for (uint32_t e = 0; e < 4u; e++) o[p][e] = bits >> e & 1u ? __builtin_nanf("") : o[p][e];
+                }
                 vw[p] = clean;
             }
         }
@@ -572,37 +577,65 @@ attend_kernel(const AttendArgs a)
     for (uint32_t d = 0; d < kPer; d += 2u) reinterpret_cast<uint32_t *>(a.out + at * kD + d0)[d / 2u] = pk_bf16(acc[d] * by, acc[d + 1u] * by);
 }
 
-// The shares of a tile's keys joined: a wavefront for a token and query head.
+// The shares of a tile's keys joined: a workgroup for a token and query head, its wavefronts a fourth of the shares each, all of a wavefront's in flight together.  (A wavefront for all
+// shares of a head, four at a time, took 8 us for 64 shares, now TODO.)
 template <uint32_t kD>
 __global__ void __launch_bounds__(256)
 attend_join_kernel(const AttendArgs a)
 {
-    const uint32_t lane = threadIdx.x & 63u, head = blockIdx.y * 4u + (threadIdx.x >> 6), Q = a.heads * a.group;
-    // by tile, to know how many shares it has
+    constexpr uint32_t kOwn = kD / 64u, kMost = 16u;                       // dims of a lane; shares of a wavefront
+    __shared__ float part[4][kD], ends[4][2];
+    const uint32_t lane = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), Q = a.heads * a.group;
     uint32_t len, per;
     TileOf t;
     if (!tile_of<kTile>(a, blockIdx.x, &len, &t)) return;
     const uint32_t sees_most = seen_by(t, t.last - 1u, a.group), shares = shares_of((sees_most + kBlock - 1u) / kBlock, a.splits, &per);
-    if (shares < 2u || head >= a.heads * kTile) return;
-    const uint32_t h = head / kTile, r = t.first + head % kTile;
-    if (r >= t.last) return;
+    const uint32_t h = blockIdx.y / kTile, r = t.first + blockIdx.y % kTile;
+    if (shares < 2u || r >= t.last) return;
     const size_t at = (size_t)(t.begin + r / a.group) * Q + h * a.group + r % a.group;
     const float *from = a.partial + at * a.splits * (kD + 2u);
-    constexpr uint32_t kOwn = kD / 64u;
-    float m = -__builtin_inff(), l = 0.f, acc[kOwn];
-    if (lane < shares) m = from[(size_t)lane * (kD + 2u) + kD];
+    float v[kMost][kOwn], tops[kMost], sums[kMost];
 #pragma unroll
-    for (int s = 32; s > 0; s >>= 1) m = __builtin_fmaxf(m, __shfl_xor(m, s));
+    for (uint32_t k = 0; k < kMost; k++) {
+        const uint32_t share = wave + 4u * k;
+        tops[k] = -__builtin_inff(); sums[k] = 0.f;
+#pragma unroll
+        for (uint32_t d = 0; d < kOwn; d++) v[k][d] = 0.f;
+        if (share >= shares) continue;
+        const float *p = from + (size_t)share * (kD + 2u);
+        tops[k] = p[kD]; sums[k] = p[kD + 1u];
+#pragma unroll
+        for (uint32_t d = 0; d < kOwn; d++) v[k][d] = p[lane * kOwn + d];
+    }
+    float m = -__builtin_inff(), l = 0.f, acc[kOwn];
+#pragma unroll
+    for (uint32_t k = 0; k < kMost; k++) m = __builtin_fmaxf(m, tops[k]);
     const float base = m > -__builtin_inff() ? m : 0.f;
 #pragma unroll
     for (uint32_t d = 0; d < kOwn; d++) acc[d] = 0.f;
-#pragma unroll 4
-    for (uint32_t k = 0; k < shares; k++) {
-        const float *p = from + (size_t)k * (kD + 2u);
-        const float by = __builtin_amdgcn_exp2f(p[kD] - base);
-        l += by * p[kD + 1u];
 #pragma unroll
-        for (uint32_t d = 0; d < kOwn; d++) acc[d] += by * p[lane * kOwn + d];
+    for (uint32_t k = 0; k < kMost; k++) {
+        const float by = __builtin_amdgcn_exp2f(tops[k] - base);
+        l += by * sums[k];
+#pragma unroll
+        for (uint32_t d = 0; d < kOwn; d++) acc[d] += by * v[k][d];
+    }
+#pragma unroll
+    for (uint32_t d = 0; d < kOwn; d++) part[wave][lane * kOwn + d] = acc[d];
+    if (lane == 0u) { ends[wave][0] = m; ends[wave][1] = l; }
+    __syncthreads();
+    if (wave) return;
+    m = __builtin_fmaxf(__builtin_fmaxf(ends[0][0], ends[1][0]), __builtin_fmaxf(ends[2][0], ends[3][0]));
+    const float all = m > -__builtin_inff() ? m : 0.f;
+    l = 0.f;
+#pragma unroll
+    for (uint32_t d = 0; d < kOwn; d++) acc[d] = 0.f;
+#pragma unroll
+    for (uint32_t w = 0; w < 4u; w++) {
+        const float by = __builtin_amdgcn_exp2f(ends[w][0] - all);
+        l += by * ends[w][1];
+#pragma unroll
+        for (uint32_t d = 0; d < kOwn; d++) acc[d] += by * part[w][lane * kOwn + d];
     }
     const float by = l > 0.f ? 1.f / l : l == l ? 0.f : l;
     uint16_t *out = a.out + at * kD + lane * kOwn;
@@ -634,6 +667,10 @@ __device__ __forceinline__ uint32_t key_place(uint32_t key, uint32_t c)
 }
 __device__ __forceinline__ uint32_t value_place(uint32_t dim, uint32_t c) { return c ^ (dim >> 1 & 3u); }
 
+// LDS is read here and not earlier: asked for all at once, a block's keys and values do not fit the registers, and what is put into memory for them waits behind the
+// next block's loads.
+__device__ __forceinline__ void ds_fence() { __builtin_amdgcn_sched_barrier(0x1F); }
+
 struct Yes { static constexpr bool value = true; };
 struct No { static constexpr bool value = false; };
 
@@ -642,9 +679,12 @@ __global__ void __launch_bounds__(kAttendWaves * 64u, 2)
 attend_wide_kernel(const AttendArgs a)
 {
     constexpr uint32_t kSteps = kD / 32u, kParts = kD / 16u, kRows = kAttendWaves * kTile * kTiles, kThreads = kAttendWaves * 64u;
+    static_assert(kAttendWaves == kBlock / 16u, "a wavefront for sixteen keys");
+    constexpr uint32_t kAhead = kD == 256u ? 1u : 2u, kValuesAhead = 4u;         // tiles of keys and parts of values that are asked for in LDS before they are needed
     constexpr bool kBytes = kD >= 128u;              // scores from 8-bit numbers: products of 128 of them
     constexpr uint32_t kLoads = kD * kBlock / (16u * kThreads);            // sixteen bytes of a thread, of keys and of values each
     __shared__ Word4 keys[2][kD * kBlock / 16u], values[2][kD * kBlock / 16u];
+    __shared__ Float2 scales[2][kBlock / 16u];
     const uint32_t tid = threadIdx.x, lane = tid & 63u, wave = __builtin_amdgcn_readfirstlane(tid >> 6), m = lane & 15u, g = lane >> 4;
     const uint32_t h = blockIdx.x, P = 1u << a.shift;
     uint32_t len;
@@ -700,118 +740,140 @@ attend_wide_kernel(const AttendArgs a)
     Float4 o[kTiles][kParts];
     float base[kTiles], sum[kTiles];
     bool begun[kTiles];                              // the lane's query has a base
+    uint64_t nans[kTiles];                           // its outputs that have seen a NaN
 #pragma unroll
     for (uint32_t n = 0; n < kTiles; n++) {
-        base[n] = 0.f; sum[n] = 0.f; begun[n] = false;
+        base[n] = 0.f; sum[n] = 0.f; begun[n] = false; nans[n] = 0ull;
 #pragma unroll
         for (uint32_t p = 0; p < kParts; p++) o[n][p] = Float4{0.f, 0.f, 0.f, 0.f};
     }
-    // What a thread brings of a block: sixteen bytes at a time, to the places one behind the other; and the lane's scales of it.  A block begins with a page, so
-    // that a thread's places in pages stay, and its columns go on by the pages of a block.
-    const size_t page_bytes = (size_t)a.heads * P * kD;
+    // What a thread brings of a block, sixteen bytes at a time.  A wavefront's keys are among sixteen neighbours, its values those of sixteen, so that it has one page of
+    // each, and an address is a page's, in scalar registers, and a place that stays (by lanes, addresses were a third of a block's vector instructions).  A block
+    // begins with a page.
+    const uint64_t page_bytes = (uint64_t)a.heads * P * kD;
     const uint8_t *k_head = a.k_cache + (size_t)h * P * kD, *v_head = a.v_cache + (size_t)h * P * kD;
-    const uint32_t value_dim = tid / 4u, value_chunk = value_place(value_dim, tid % 4u), column_step = kBlock >> a.shift;
-    uint32_t k_column[kLoads], k_at[kLoads], v_at[kLoads];
+    const uint32_t column_step = kBlock >> a.shift;
+    uint32_t k_at[kLoads], v_at[kLoads], v_to[kLoads];
 #pragma unroll
     for (uint32_t j = 0; j < kLoads; j++) {
-        const uint32_t key = (j * kThreads + tid) * 16u / kD, c = key_place<kD>(key, (j * kThreads + tid) % (kD / 16u));
-        k_column[j] = key >> a.shift;
-        k_at[j] = (key & (P - 1u)) * kD + c * 16u;
-        v_at[j] = (j * (kThreads / 4u) + value_dim) * P + (value_chunk * 16u & (P - 1u));
+        const uint32_t key = (j * kThreads + tid) * 16u / kD, dim = j * 64u + lane;
+        k_at[j] = (key & (P - 1u)) * kD + key_place<kD>(key, (j * kThreads + tid) % (kD / 16u)) * 16u;
+        v_at[j] = dim * P + (wave * 16u & (P - 1u));
+        v_to[j] = dim * 4u + value_place(dim, wave);
     }
-    const uint32_t v_column = value_chunk * 16u >> a.shift, s_column = g * 16u >> a.shift;
     Word4 next_k[kLoads], next_v[kLoads];
     float next_ks = 0.f, next_vs = 0.f;
-    uint32_t page_k[kLoads], page_v = 0, page_s = 0;
-    auto page_at = [&](uint32_t c) {
-        const uint32_t id = (uint32_t)table[c < last_column ? c : last_column];
-        return id < a.pages ? id : 0u;               // (what lies behind a row's pages is masked, and must be somewhere)
-    };
+    uint32_t page_k[kLoads], page_v = 0;
+    auto page_at = [&](uint32_t c) { return (uint32_t)table[c < last_column ? c : last_column]; };
+    // (what lies behind a row's pages is masked, and must be somewhere.  Looked at where it is used, a block later: where it is asked for that is a wait for all that was asked for
+    // before, and took a fifth of the time)
+    auto page_of = [&](uint32_t asked) { const uint32_t id = (uint32_t)__builtin_amdgcn_readfirstlane((int)asked); return id < a.pages ? id : 0u; };
     auto ask_pages = [&](uint32_t b) {
         const uint32_t first = b * column_step;
 #pragma unroll
-        for (uint32_t j = 0; j < kLoads; j++) page_k[j] = page_at(first + k_column[j]);
-        page_v = page_at(first + v_column);
-        page_s = page_at(first + s_column);
+        for (uint32_t j = 0; j < kLoads; j++) page_k[j] = page_at(first + ((j * kThreads + wave * 64u) * 16u / kD >> a.shift));
+        page_v = page_at(first + (wave * 16u >> a.shift));
     };
     auto ask = [&]() {
 #pragma unroll
         for (uint32_t j = 0; j < kLoads; j++) {
-            next_k[j] = *reinterpret_cast<const Word4 *>(k_head + page_k[j] * page_bytes + k_at[j]);
-            next_v[j] = *reinterpret_cast<const Word4 *>(v_head + page_v * page_bytes + v_at[j]);
+            const uint8_t *k_page = k_head + page_of(page_k[j]) * page_bytes;
+            next_k[j] = *reinterpret_cast<const Word4 *>(k_page + k_at[j]);
         }
-        next_ks = a.k_scale[(size_t)page_s * a.heads + h];
-        next_vs = a.v_scale[(size_t)page_s * a.heads + h];
+        const uint32_t page = page_of(page_v);
+        const uint8_t *v_page = v_head + page * page_bytes;
+#pragma unroll
+        for (uint32_t j = 0; j < kLoads; j++) next_v[j] = *reinterpret_cast<const Word4 *>(v_page + v_at[j]);
+        next_ks = a.k_scale[(size_t)page * a.heads + h];
+        next_vs = a.v_scale[(size_t)page * a.heads + h];
     };
     auto put = [&](uint32_t to) {
 #pragma unroll
-        for (uint32_t j = 0; j < kLoads; j++) { keys[to][j * kThreads + tid] = next_k[j]; values[to][j * kThreads + tid] = next_v[j]; }
+        for (uint32_t j = 0; j < kLoads; j++) {
+            keys[to][j * kThreads + tid] = next_k[j];
+            values[to][v_to[j]] = next_v[j];
+        }
+        if (lane == 0u) scales[to][wave] = Float2{next_ks, next_vs};
     };
     // where the lane's keys and values lie in LDS
     const uint32_t key_row = ((m >> 2) * 16u + (m & 3u)) * (kD / 16u), value_row = m * 4u + value_place(m, g);
     // A block of keys; kEdge: some query of the wavefront does not see all of it.
-    auto look = [&](uint32_t b, float ks, float vs0, auto edge) {
+    auto look = [&](uint32_t b, auto edge) {
         constexpr bool kEdge = decltype(edge)::value;
         const uint32_t at = b & 1u, mine = b * kBlock + g * 16u;
         // (a page of zeros may have a scale of zero; what lies behind a row's pages may have any)
-        const float vs = __builtin_fmaxf(vs0, 0x1p-64f), v_log = __builtin_amdgcn_logf(vs), v_inverse = __builtin_amdgcn_rcpf(vs);
+        const Float2 scale = scales[at][g];
+        const float ks = scale[0], vs = __builtin_fmaxf(scale[1], 0x1p-64f), v_log = __builtin_amdgcn_logf(vs), v_inverse = __builtin_amdgcn_rcpf(vs);
         Float4 s[kTiles][4];
+        Word4 weights[kTiles][2];
+        float part[kTiles], by[kTiles], add[kTiles];
 #pragma unroll
-        for (uint32_t n = 0; n < 4u; n++) {
-            Word4 kw[kD / 64u];
+        for (uint32_t i = 0; i < kTiles; i++) { by[i] = ks * q_scale[i]; add[i] = v_log - (begun[i] ? base[i] : 0.f); part[i] = 0.f; }
+        // The weights of four keys, and their sum out of the numbers that the product takes.
+        auto weigh = [&](uint32_t i, uint32_t n) {
 #pragma unroll
-            for (uint32_t j = 0; j < kD / 64u; j++) kw[j] = keys[at][key_row + n * 4u * (kD / 16u) + key_place<kD>((m >> 2) * 16u + (m & 3u), g * (kD / 64u) + j)];
+            for (uint32_t e = 0; e < 2u; e++) {
+                const uint32_t two = pk_f16(__builtin_amdgcn_exp2f(s[i][n][2u * e]), __builtin_amdgcn_exp2f(s[i][n][2u * e + 1u]));
+                part[i] = __builtin_amdgcn_fdot2(__builtin_bit_cast(Short2, two), Short2{(_Float16)1.f, (_Float16)1.f}, part[i], false);
+                weights[i][n / 2u][n % 2u * 2u + e] = two;
+            }
+        };
+        // (weights of four keys while the products of the next four are under way)
+        Word4 kw[4][kD / 64u];
+        auto key_words = [&](uint32_t n, Word4 (&w)[kD / 64u]) {
 #pragma unroll
-            for (uint32_t i = 0; i < kTiles; i++) s[i][n] = Float4{0.f, 0.f, 0.f, 0.f};
-            if (kBytes) {
+            for (uint32_t j = 0; j < kD / 64u; j++) w[j] = keys[at][key_row + n * 4u * (kD / 16u) + key_place<kD>((m >> 2) * 16u + (m & 3u), g * (kD / 64u) + j)];
+        };
 #pragma unroll
-                for (uint32_t k = 0; k < kD / 128u; k++) {
-                    const Word4 x = kw[(2u * k) % (kD / 64u)], y = kw[(2u * k + 1u) % (kD / 64u)];
-                    const Int8 bytes{(int)x[0], (int)x[1], (int)x[2], (int)x[3], (int)y[0], (int)y[1], (int)y[2], (int)y[3]};
+        for (uint32_t n = 0; n < kAhead; n++) key_words(n, kw[n]);
 #pragma unroll
-                    for (uint32_t i = 0; i < kTiles; i++)        // (scales of 1 and, for the smaller summands, 2^-5)
-                        s[i][n] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(bytes, q_low[i][k], s[i][n], 0, 0, 0, 127, 0, 122);
+        for (uint32_t n = 0; n < 5u; n++) {
+            if (n < 4u) {
+                if (n + kAhead < 4u) key_words(n + kAhead, kw[n + kAhead]);
+                ds_fence();
 #pragma unroll
-                    for (uint32_t i = 0; i < kTiles; i++)
-                        s[i][n] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(bytes, q_high[i][k], s[i][n], 0, 0, 0, 127, 0, 127);
-                }
-            } else
+                for (uint32_t i = 0; i < kTiles; i++) s[i][n] = Float4{0.f, 0.f, 0.f, 0.f};
+                if (kBytes) {
 #pragma unroll
-                for (uint32_t k = 0; k < kSteps; k++) {
-                    const Half8 x = widened(kw[k / 2u % (kD / 64u)][k % 2u * 2u], kw[k / 2u % (kD / 64u)][k % 2u * 2u + 1u]);
+                    for (uint32_t k = 0; k < kD / 128u; k++) {
+                        const Word4 x = kw[n][(2u * k) % (kD / 64u)], y = kw[n][(2u * k + 1u) % (kD / 64u)];
+                        const Int8 bytes{(int)x[0], (int)x[1], (int)x[2], (int)x[3], (int)y[0], (int)y[1], (int)y[2], (int)y[3]};
 #pragma unroll
-                    for (uint32_t i = 0; i < kTiles; i++) s[i][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, q_half[i][k % (kBytes ? 1u : kSteps)], s[i][n], 0, 0, 0);
-                }
-        }
-        Short8 weights[kTiles][2];
+                        for (uint32_t i = 0; i < kTiles; i++)        // (scales of 1 and, for the smaller summands, 2^-5)
+                            s[i][n] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(bytes, q_low[i][k], s[i][n], 0, 0, 0, 127, 0, 122);
 #pragma unroll
-        for (uint32_t i = 0; i < kTiles; i++) {
-            const float by = ks * q_scale[i], add = v_log - (begun[i] ? base[i] : 0.f);
+                        for (uint32_t i = 0; i < kTiles; i++)
+                            s[i][n] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(bytes, q_high[i][k], s[i][n], 0, 0, 0, 127, 0, 127);
+                    }
+                } else
 #pragma unroll
-            for (uint32_t n = 0; n < 4u; n++)
+                    for (uint32_t k = 0; k < kSteps; k++) {
+                        const Half8 x = widened(kw[n][k / 2u % (kD / 64u)][k % 2u * 2u], kw[n][k / 2u % (kD / 64u)][k % 2u * 2u + 1u]);
 #pragma unroll
-                for (uint32_t e = 0; e < 4u; e++) {
-                    s[i][n][e] = __builtin_fmaf(s[i][n][e], by, add);
-                    if (kEdge) s[i][n][e] = mine + n * 4u + e < sees[i] ? s[i][n][e] : -__builtin_inff();
-                }
-            // The weights, and their sum out of the numbers that the product takes.  A sum that is infinite says that the base has to move first.
-            float part;
-            auto weigh = [&]() {
-                part = 0.f;
+                        for (uint32_t i = 0; i < kTiles; i++) s[i][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, q_half[i][k % (kBytes ? 1u : kSteps)], s[i][n], 0, 0, 0);
+                    }
+            }
+            if (n)
 #pragma unroll
-                for (uint32_t u = 0; u < 2u; u++) {
-                    Word4 w;
+                for (uint32_t i = 0; i < kTiles; i++) {
 #pragma unroll
                     for (uint32_t e = 0; e < 4u; e++) {
-                        const uint32_t two = pk_f16(__builtin_amdgcn_exp2f(s[i][u * 2u + e / 2u][e % 2u * 2u]), __builtin_amdgcn_exp2f(s[i][u * 2u + e / 2u][e % 2u * 2u + 1u]));
-                        part = __builtin_amdgcn_fdot2(__builtin_bit_cast(Short2, two), Short2{(_Float16)1.f, (_Float16)1.f}, part, false);
-                        w[e] = two;
+                        const float x = __builtin_fmaf(s[i][n - 1u][e], by[i], add[i]);
+                        s[i][n - 1u][e] = !kEdge || mine + (n - 1u) * 4u + e < sees[i] ? x : -__builtin_inff();
                     }
-                    weights[i][u] = __builtin_bit_cast(Short8, w);
+                    weigh(i, n - 1u);
                 }
-            };
-            weigh();
-            if (__ballot(!begun[i] || !(part < __builtin_inff()))) {
+        }
+        // values are asked for some parts ahead
+        Word4 words[kParts];
+#pragma unroll
+        for (uint32_t p = 0; p < kValuesAhead; p++) words[p] = values[at][p * 64u + value_row];
+        bool moves = false;                          // a sum that is infinite says that the base has to move first
+#pragma unroll
+        for (uint32_t i = 0; i < kTiles; i++) moves |= !begun[i] || !(part[i] < __builtin_inff());
+        if (__ballot(moves))
+#pragma unroll
+            for (uint32_t i = 0; i < kTiles; i++) {
                 float high = -__builtin_inff();
 #pragma unroll
                 for (uint32_t n = 0; n < 4u; n++)
@@ -819,40 +881,47 @@ attend_wide_kernel(const AttendArgs a)
                     for (uint32_t e = 0; e < 4u; e++) high = __builtin_fmaxf(high, s[i][n][e]);
                 high = __builtin_fmaxf(high, __shfl_xor(high, 16));
                 high = __builtin_fmaxf(high, __shfl_xor(high, 32));
-                const bool moves = begun[i] ? high > kRoom : high > -__builtin_inff();
-                const float how_much = moves ? high - kAim : 0.f, shrink = begun[i] ? __builtin_amdgcn_exp2f(-how_much) : 1.f;
+                const bool move = begun[i] ? high > kRoom : high > -__builtin_inff();
+                const float how_much = move ? high - kAim : 0.f, shrink = begun[i] ? __builtin_amdgcn_exp2f(-how_much) : 1.f;
                 base[i] += how_much;
-                begun[i] = begun[i] || moves;
+                begun[i] = begun[i] || move;
                 sum[i] *= shrink;
 #pragma unroll
                 for (uint32_t p = 0; p < kParts; p++) o[i][p] *= shrink;
+                part[i] = 0.f;
 #pragma unroll
-                for (uint32_t n = 0; n < 4u; n++) s[i][n] -= how_much;
-                weigh();
+                for (uint32_t n = 0; n < 4u; n++) { s[i][n] -= how_much; weigh(i, n); }
             }
-            sum[i] = __builtin_fmaf(part, v_inverse, sum[i]);
-        }
+#pragma unroll
+        for (uint32_t i = 0; i < kTiles; i++) sum[i] = __builtin_fmaf(part[i], v_inverse, sum[i]);
         const uint32_t there = !kEdge ? 16u : mine >= len ? 0u : len - mine < 16u ? len - mine : 16u;
+        bool nan = false;
 #pragma unroll
         for (uint32_t p = 0; p < kParts; p++) {
-            Word4 v = values[at][p * 64u + value_row];
+            Word4 v = words[p];
+            if (p + kValuesAhead < kParts) words[p + kValuesAhead] = values[at][(p + kValuesAhead) * 64u + value_row];
+            ds_fence();
             if (kEdge) {
                 v = first_bytes(v, there);           // what lies behind the row's end must not be NaN times a weight of zero
-                // a NaN among the values reaches the queries that see it, and as a weight of zero times it no other
                 const Word4 clean = without_nans(v);
-                const bool nan = ((clean[0] ^ v[0]) | (clean[1] ^ v[1]) | (clean[2] ^ v[2]) | (clean[3] ^ v[3])) != 0u;
-                if (__ballot(nan))
-#pragma unroll
-                    for (uint32_t i = 0; i < kTiles; i++) o[i][p] += nans_seen(v, mine >= sees[i] ? 0u : sees[i] - mine < 16u ? sees[i] - mine : 16u);
+                nan |= differ(clean, v);
                 v = clean;
             }
 #pragma unroll
             for (uint32_t u = 0; u < 2u; u++) {
                 const Short8 x = widened16(v[u * 2u], v[u * 2u + 1u]);
 #pragma unroll
-                for (uint32_t i = 0; i < kTiles; i++) o[i][p] = __builtin_amdgcn_mfma_f32_16x16x32_f16(x, weights[i][u], o[i][p], 0, 0, 0);
+                for (uint32_t i = 0; i < kTiles; i++) o[i][p] = __builtin_amdgcn_mfma_f32_16x16x32_f16(x, __builtin_bit_cast(Short8, weights[i][u]), o[i][p], 0, 0, 0);
             }
         }
+        // a NaN among the values reaches the queries that see it, and as a weight of zero times it no other
+        if (kEdge && __ballot(nan))
+#pragma nounroll
+            for (uint32_t p = 0; p < kParts; p++) {
+                const Word4 v = first_bytes(values[at][p * 64u + value_row], there);
+#pragma unroll
+                for (uint32_t i = 0; i < kTiles; i++) nans[i] |= (uint64_t)nans_seen(v, mine >= sees[i] ? 0u : sees[i] - mine < 16u ? sees[i] - mine : 16u) << (4u * p);
+            }
     };
     if (blocks) {
         ask_pages(0u);
@@ -860,18 +929,23 @@ attend_wide_kernel(const AttendArgs a)
         if (blocks > 1u) ask_pages(1u);
         put(0u);
     }
-    const uint32_t whole = sees_least / kBlock;      // blocks that all queries of the wavefront see
-    for (uint32_t b = 0; b < blocks; b++) {
-        const float ks = next_ks, vs = next_vs;
+    // Blocks that all queries of the wavefront see, then the others, in loops of their own: registers that the second has no room for must not be waited for in the first.
+    // (The wavefronts meet at a barrier for every block, in whichever loop each is.)
+    const uint32_t whole = sees_least / kBlock;
+    auto step = [&](uint32_t b, auto edge) {
         __syncthreads();
         if (b + 1u < blocks) {
             ask();
             if (b + 2u < blocks) ask_pages(b + 2u);
         }
-        if (b < whole) look(b, ks, vs, No{});
-        else if (b * kBlock < sees_most) look(b, ks, vs, Yes{});
+        if (!decltype(edge)::value || b * kBlock < sees_most) look(b, edge);
         if (b + 1u < blocks) put(b & 1u ^ 1u);       // (its last reader is behind this round's barrier)
-    }
+    };
+    uint32_t b = 0;
+#pragma nounroll
+    for (; b < whole; b++) step(b, No{});
+#pragma nounroll
+    for (; b < blocks; b++) step(b, Yes{});
 #pragma unroll
     for (uint32_t i = 0; i < kTiles; i++) {
         float total = sum[i];
@@ -882,8 +956,12 @@ attend_wide_kernel(const AttendArgs a)
         const float by = total > 0.f ? 1.f / total : total == total ? 0.f : total;           // (a row that sees nothing: zeros)
         uint16_t *out = a.out + ((size_t)(t.begin + r / a.group) * (a.heads * a.group) + h * a.group + r % a.group) * kD + g * 4u;
 #pragma unroll
-        for (uint32_t p = 0; p < kParts; p++)
-            *reinterpret_cast<Word2 *>(out + p * 16u) = Word2{pk_bf16(o[i][p][0] * by, o[i][p][1] * by), pk_bf16(o[i][p][2] * by, o[i][p][3] * by)};
+        for (uint32_t p = 0; p < kParts; p++) {
+            float x[4];
+#pragma unroll
+            for (uint32_t e = 0; e < 4u; e++) x[e] = nans[i] >> (4u * p + e) & 1u ? __builtin_nanf("") : o[i][p][e] * by;
+            *reinterpret_cast<Word2 *>(out + p * 16u) = Word2{pk_bf16(x[0], x[1]), pk_bf16(x[2], x[3])};
+        }
     }
 }
 
@@ -920,7 +998,7 @@ hipError_t launch_cache_attend(const void *q, uint32_t tokens, uint32_t heads, u
     const dim3 grid(tiles, heads, splits);
     const hipError_t e = launch(dim == 64u ? attend_kernel<64> : dim == 128u ? attend_kernel<128> : attend_kernel<256>, grid, block, 0, s, nullptr, a);
     if (e != hipSuccess || splits == 1u) return e;
-    return launch(dim == 64u ? attend_join_kernel<64> : dim == 128u ? attend_join_kernel<128> : attend_join_kernel<256>, dim3(tiles, heads * kTile / 4u), dim3(256), 0, s, nullptr, a);
+    return launch(dim == 64u ? attend_join_kernel<64> : dim == 128u ? attend_join_kernel<128> : attend_join_kernel<256>, dim3(tiles, heads * kTile), dim3(256), 0, s, nullptr, a);
 }
 
 }  // namespace wg
