@@ -307,7 +307,7 @@ hipError_t launch_cache_append(const void *k, const void *v, uint32_t tokens, ui
 // whatever the scales, and go into the second product as float16, up to 2^14: 11 bits of precision down to 2^-28 of the largest.  (In bfloat16 they had 8,
 // which was as large an error as the output's own rounding.)
 //
-// Lane l of a wavefront holds, of 64 keys: of K, for m = l % 16, key (m / 4) * 16 + u * 8 + t * 4 + m % 4 in tile (u, t), the dims of its quarter l / 16;
+// Lane l of a wavefront holds, of 64 keys: of K, for m = l % 16, key (m / 4) * 16 + u * 8 + t * 4 + m % 4 in tile (u, t), of every 64 dims those of its quarter l / 16;
 // after S^T of tile (u, t), the scores of query l % 16 and the keys (l / 16) * 16 + u * 8 + t * 4 + 0 .. 3; of V, for dim l % 16 of 16, the keys
 // (l / 16) * 16 + 0 .. 15.  Sixteen neighbouring keys lie in one page.
 struct AttendArgs {
@@ -318,12 +318,14 @@ struct AttendArgs {
     const int32_t *table, *lens, *starts;
     uint16_t *out;                                   // [token][head][dim]
     float *partial;                                  // [token][head][split][dim + 2]
+    uint32_t *shares;                                // [token]: shares of its keys
     float scale;                                     // of the scores, times log2(e)
     uint32_t tokens, rows, heads, group, columns, pages, shift, splits, tiles;
 };
 constexpr uint32_t kAttendWaves = 4, kBlock = 64, kTile = 16;
 constexpr float kHeadroom = 14.f;                    // weights go up to 2^14
 constexpr uint32_t kLeastBlocks = 4;                 // blocks of a share: one for each wavefront
+constexpr uint32_t kShares = 1024;                   // shares in all, about
 
 typedef _Float16 Short2 __attribute__((ext_vector_type(2)));
 typedef _Float16 Short8 __attribute__((ext_vector_type(8)));
@@ -403,6 +405,13 @@ __device__ __forceinline__ uint32_t request_of(const AttendArgs &a, uint32_t til
     return __builtin_amdgcn_readfirstlane(lo);
 }
 
+// Tokens of a row in the cache, as many as its table has pages for.
+__device__ __forceinline__ uint32_t tokens_of_row(const AttendArgs &a, uint32_t r)
+{
+    const uint32_t most = a.columns << a.shift, l = (uint32_t)(a.lens[r] < 0 ? 0 : a.lens[r]);
+    return l < most ? l : most;
+}
+
 struct TileOf { uint32_t row, first, last, begin, count; int32_t before; };      // query rows [first, last) of a request with `count` tokens from `begin` on, behind `before` others
 
 template <uint32_t kTile, bool kLastFirst = false>
@@ -411,8 +420,7 @@ __device__ __forceinline__ bool tile_of(const AttendArgs &a, uint32_t tile, uint
     const uint32_t r = request_of<kTile>(a, tile);
     const uint32_t b = (uint32_t)a.starts[r] < a.tokens ? (uint32_t)a.starts[r] : a.tokens, e0 = (uint32_t)a.starts[r + 1u], e = e0 < b ? b : e0 < a.tokens ? e0 : a.tokens;
     const uint32_t at = tile - ((uint32_t)((uint64_t)b * a.group / kTile) + r), all = (e - b) * a.group;
-    const uint32_t most = a.columns << a.shift, l = (uint32_t)(a.lens[r] < 0 ? 0 : a.lens[r]);
-    *len = l < most ? l : most;
+    *len = tokens_of_row(a, r);
     if (tile < (uint32_t)((uint64_t)b * a.group / kTile) + r || (uint64_t)at * kTile >= all) return false;
     out->row = r; out->begin = b; out->count = e - b;
     out->first = (kLastFirst ? (all - 1u) / kTile - at : at) * kTile;
@@ -420,12 +428,23 @@ __device__ __forceinline__ bool tile_of(const AttendArgs &a, uint32_t tile, uint
     out->before = (int32_t)*len - (int32_t)(e - b);
     return true;
 }
-// Shares that a tile's keys are cut into, and the blocks of each.
-__device__ __forceinline__ uint32_t shares_of(uint32_t blocks, uint32_t splits, uint32_t *per)
+// Shares that a tile's keys are cut into, and the blocks of each: shares of one size, whatever the rows' lengths, so that the workgroups that the chip holds at a time have as
+// much to do as one another (as many shares of each row, 128 rows of 2,000 to 8,000 tokens took 154 us without joining, in one share each 167; so TODO).
+__device__ __forceinline__ uint32_t shares_of(const AttendArgs &a, uint32_t blocks, uint32_t *per)
 {
-    const uint32_t most = (blocks + kLeastBlocks - 1u) / kLeastBlocks, n = most < splits ? (most ? most : 1u) : splits;
+    *per = blocks;
+    if (a.splits == 1u || !blocks) return 1u;
+    uint32_t all = 0;                                // blocks of all rows (1,024 of them at most where keys are cut)
+    for (uint32_t r = threadIdx.x & 63u; r < a.rows; r += 64u) all += (tokens_of_row(a, r) + kBlock - 1u) / kBlock;
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) all += __shfl_xor(all, o);
+    all = __builtin_amdgcn_readfirstlane(all);
+    const uint64_t work = (uint64_t)all * a.heads * ((a.group + kTile - 1u) / kTile);
+    uint32_t share = (uint32_t)((work + kShares - 1u) / kShares);
+    share = share < kLeastBlocks ? kLeastBlocks : share;
+    const uint32_t want = (blocks + share - 1u) / share, n = want < a.splits ? want : a.splits;
     *per = (blocks + n - 1u) / n;
-    return *per ? (blocks + *per - 1u) / *per : 1u;
+    return (blocks + *per - 1u) / *per;
 }
 // Keys that query row i of the tile sees.
 __device__ __forceinline__ uint32_t seen_by(const TileOf &t, uint32_t i, uint32_t group) { const int32_t n = t.before + (int32_t)(i / group) + 1; return n < 0 ? 0u : (uint32_t)n; }
@@ -444,7 +463,8 @@ attend_kernel(const AttendArgs a)
     if (!tile_of<kTile>(a, blockIdx.x, &len, &t)) return;
     const uint32_t sees_most = seen_by(t, t.last - 1u, a.group), blocks = (sees_most + kBlock - 1u) / kBlock;
     uint32_t per;
-    const uint32_t shares = shares_of(blocks, a.splits, &per);
+    const uint32_t shares = shares_of(a, blocks, &per);
+    if (a.splits > 1u && h == 0u && split == 0u && tid < kTile && t.first + tid < t.last) a.shares[t.begin + (t.first + tid) / a.group] = shares;
     if (split >= shares) return;
     const uint32_t b0 = split * per, b1 = blocks - b0 < per ? blocks : b0 + per;
     // the lane's query row (a row behind the last is the last again, and is not stored)
@@ -453,21 +473,21 @@ attend_kernel(const AttendArgs a)
     const uint16_t *q = a.q + (int64_t)(t.begin + i / a.group) * a.q_token + (int64_t)(h * a.group + i % a.group) * a.q_head;
     Half8 qf[kSteps];
 #pragma unroll
-    for (uint32_t s = 0; s < kSteps; s++) qf[s] = __builtin_bit_cast(Half8, *reinterpret_cast<const Word4 *>(q + g * (kD / 4u) + s * 8u));
+    for (uint32_t s = 0; s < kSteps; s++) qf[s] = __builtin_bit_cast(Half8, *reinterpret_cast<const Word4 *>(q + s / 2u * 64u + g * 16u + s % 2u * 8u));
     const int32_t *table = a.table + (size_t)t.row * a.columns;
     const uint32_t last_column = a.columns - 1u;
-    auto page_at = [&](uint32_t key) {
-        const uint32_t c = key >> a.shift, id = (uint32_t)table[c < last_column ? c : last_column];
-        return id < a.pages ? id : 0u;               // (what lies behind a row's pages is masked, and must be somewhere)
-    };
+    auto page_at = [&](uint32_t key) { const uint32_t c = key >> a.shift; return (uint32_t)table[c < last_column ? c : last_column]; };
+    auto page_of = [&](uint32_t id) { return id < a.pages ? id : 0u; };      // (what lies behind a row's pages is masked, and must be somewhere)
+    // (asked for a block ahead)
+    uint32_t k_next = page_at((b0 + wave) * kBlock + (m >> 2) * 16u), v_next = page_at((b0 + wave) * kBlock + g * 16u);
     Float4 o[kParts];
 #pragma unroll
     for (uint32_t p = 0; p < kParts; p++) o[p] = Float4{0.f, 0.f, 0.f, 0.f};
     float top = -__builtin_inff(), sum = 0.f;        // of the lane's query; the sum of the lane's own keys
     for (uint32_t b = b0 + wave; b < b1; b += kAttendWaves) {
         const uint32_t key0 = b * kBlock, mine = key0 + g * 16u, theirs = key0 + (m >> 2) * 16u;
-        const uint32_t k_page = page_at(theirs), v_page = page_at(mine);
-        const uint8_t *kp = a.k_cache + (((size_t)k_page * a.heads + h) * P + (theirs & (P - 1u)) + (m & 3u)) * kD + g * (kD / 4u);
+        const uint32_t k_page = page_of(k_next), v_page = page_of(v_next);
+        const uint8_t *kp = a.k_cache + (((size_t)k_page * a.heads + h) * P + (theirs & (P - 1u)) + (m & 3u)) * kD + g * 16u;
         const uint8_t *vp = a.v_cache + (((size_t)v_page * a.heads + h) * kD + m) * P + (mine & (P - 1u));
         const float ks = a.k_scale[(size_t)v_page * a.heads + h] * a.scale;
         // (a page of zeros may have a scale of zero; what lies behind a row's pages may have any)
@@ -476,10 +496,11 @@ attend_kernel(const AttendArgs a)
 #pragma unroll
         for (uint32_t n = 0; n < 4u; n++)
 #pragma unroll
-            for (uint32_t j = 0; j < kD / 64u; j++) kw[n][j] = *reinterpret_cast<const Word4 *>(kp + n * 4u * kD + j * 16u);
+            for (uint32_t j = 0; j < kD / 64u; j++) kw[n][j] = *reinterpret_cast<const Word4 *>(kp + n * 4u * kD + j * 64u);
         Word4 vw[kParts];
 #pragma unroll
         for (uint32_t p = 0; p < kParts; p++) vw[p] = *reinterpret_cast<const Word4 *>(vp + (size_t)p * 16u * P);
+        k_next = page_at(theirs + kAttendWaves * kBlock); v_next = page_at(mine + kAttendWaves * kBlock);
         Float4 s[4];
 #pragma unroll
         for (uint32_t n = 0; n < 4u; n++) {
@@ -577,27 +598,23 @@ attend_kernel(const AttendArgs a)
     for (uint32_t d = 0; d < kPer; d += 2u) reinterpret_cast<uint32_t *>(a.out + at * kD + d0)[d / 2u] = pk_bf16(acc[d] * by, acc[d + 1u] * by);
 }
 
-// The shares of a tile's keys joined: a workgroup for a token and query head, its wavefronts a fourth of the shares each, all of a wavefront's in flight together.  (A wavefront for all
-// shares of a head, four at a time, took 8 us for 64 shares, now TODO.)
-template <uint32_t kD>
+// The shares of a token's keys joined: kWaves wavefronts for each query head, all that one reads in flight together.  (A wavefront for a head of 64 shares, four at a time, took 8 us,
+// four take 3.5; for two shares of 28 heads of 128 tokens, 16 us by four wavefronts, 4 by one.)
+template <uint32_t kD, uint32_t kWaves>
 __global__ void __launch_bounds__(256)
 attend_join_kernel(const AttendArgs a)
 {
-    constexpr uint32_t kOwn = kD / 64u, kMost = 16u;                       // dims of a lane; shares of a wavefront
+    constexpr uint32_t kOwn = kD / 64u, kMost = 16u, kHeads = 4u / kWaves; // dims of a lane; shares of a wavefront; heads of a workgroup
     __shared__ float part[4][kD], ends[4][2];
     const uint32_t lane = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), Q = a.heads * a.group;
-    uint32_t len, per;
-    TileOf t;
-    if (!tile_of<kTile>(a, blockIdx.x, &len, &t)) return;
-    const uint32_t sees_most = seen_by(t, t.last - 1u, a.group), shares = shares_of((sees_most + kBlock - 1u) / kBlock, a.splits, &per);
-    const uint32_t h = blockIdx.y / kTile, r = t.first + blockIdx.y % kTile;
-    if (shares < 2u || r >= t.last) return;
-    const size_t at = (size_t)(t.begin + r / a.group) * Q + h * a.group + r % a.group;
+    const uint32_t head = blockIdx.y * kHeads + wave / kWaves, first = wave % kWaves, shares = a.shares[blockIdx.x];
+    if (shares < 2u || (kWaves == 1u && head >= Q)) return;
+    const size_t at = (size_t)blockIdx.x * Q + head;
     const float *from = a.partial + at * a.splits * (kD + 2u);
     float v[kMost][kOwn], tops[kMost], sums[kMost];
 #pragma unroll
     for (uint32_t k = 0; k < kMost; k++) {
-        const uint32_t share = wave + 4u * k;
+        const uint32_t share = first + kWaves * k;
         tops[k] = -__builtin_inff(); sums[k] = 0.f;
 #pragma unroll
         for (uint32_t d = 0; d < kOwn; d++) v[k][d] = 0.f;
@@ -620,22 +637,24 @@ attend_join_kernel(const AttendArgs a)
 #pragma unroll
         for (uint32_t d = 0; d < kOwn; d++) acc[d] += by * v[k][d];
     }
+    if (kWaves > 1u) {
 #pragma unroll
-    for (uint32_t d = 0; d < kOwn; d++) part[wave][lane * kOwn + d] = acc[d];
-    if (lane == 0u) { ends[wave][0] = m; ends[wave][1] = l; }
-    __syncthreads();
-    if (wave) return;
-    m = __builtin_fmaxf(__builtin_fmaxf(ends[0][0], ends[1][0]), __builtin_fmaxf(ends[2][0], ends[3][0]));
-    const float all = m > -__builtin_inff() ? m : 0.f;
-    l = 0.f;
+        for (uint32_t d = 0; d < kOwn; d++) part[wave][lane * kOwn + d] = acc[d];
+        if (lane == 0u) { ends[wave][0] = m; ends[wave][1] = l; }
+        __syncthreads();
+        if (wave) return;
+        m = __builtin_fmaxf(__builtin_fmaxf(ends[0][0], ends[1][0]), __builtin_fmaxf(ends[2][0], ends[3][0]));
+        const float all = m > -__builtin_inff() ? m : 0.f;
+        l = 0.f;
 #pragma unroll
-    for (uint32_t d = 0; d < kOwn; d++) acc[d] = 0.f;
+        for (uint32_t d = 0; d < kOwn; d++) acc[d] = 0.f;
 #pragma unroll
-    for (uint32_t w = 0; w < 4u; w++) {
-        const float by = __builtin_amdgcn_exp2f(ends[w][0] - all);
-        l += by * ends[w][1];
+        for (uint32_t w = 0; w < 4u; w++) {
+            const float by = __builtin_amdgcn_exp2f(ends[w][0] - all);
+            l += by * ends[w][1];
 #pragma unroll
-        for (uint32_t d = 0; d < kOwn; d++) acc[d] += by * part[w][lane * kOwn + d];
+            for (uint32_t d = 0; d < kOwn; d++) acc[d] += by * part[w][lane * kOwn + d];
+        }
     }
     const float by = l > 0.f ? 1.f / l : l == l ? 0.f : l;
     uint16_t *out = a.out + at * kD + lane * kOwn;
@@ -970,13 +989,15 @@ static uint32_t tiles_of(uint32_t tokens, uint32_t rows, uint32_t group) { retur
 // Whether a request has query rows enough, on average, to fill a wavefront's two tiles.
 static bool attend_is_wide(uint32_t tokens, uint32_t rows, uint32_t group) { return (uint64_t)tokens * group >= 64ull * rows; }
 
-// Shares of a tile's keys: workgroups for four of them on every compute unit, 64 shares at most.
+// The most shares of a tile's keys.  Where each row's keys in one share make four times as many workgroups as there are to be shares, the chip evens them out by itself; else a row may
+// have four times its part of them, 64 at most.
 uint32_t attend_splits(uint32_t tokens, uint32_t rows, uint32_t heads, uint32_t group, uint32_t columns, uint32_t shift)
 {
     if (attend_is_wide(tokens, rows, group)) return 1u;
     const uint64_t tiles = (uint64_t)(tokens < rows ? tokens : rows) * ((group + kTile - 1u) / kTile) * heads;
     const uint64_t all = tokens > rows ? (uint64_t)tokens * group / kTile * heads : tiles, n = all > tiles ? all : tiles;
-    const uint64_t want = (1024u + n - 1u) / n, blocks = (((uint64_t)columns << shift) + kBlock - 1u) / kBlock, most = (blocks + kLeastBlocks - 1u) / kLeastBlocks;
+    if (n >= 4u * kShares || rows > 1024u) return 1u;
+    const uint64_t want = 4u * ((kShares + n - 1u) / n), blocks = (((uint64_t)columns << shift) + kBlock - 1u) / kBlock, most = (blocks + kLeastBlocks - 1u) / kLeastBlocks;
     const uint64_t splits = want < most ? want : most;
     return splits < 1u ? 1u : splits > 64u ? 64u : (uint32_t)splits;
 }
@@ -987,7 +1008,7 @@ hipError_t launch_cache_attend(const void *q, uint32_t tokens, uint32_t heads, u
 {
     const uint32_t splits = attend_splits(tokens, rows, heads, group, columns, shift), tiles = tiles_of(tokens, rows, group);
     const AttendArgs a{static_cast<const uint16_t *>(q), q_token, q_head, k_cache, v_cache, k_scale, v_scale, table, lens, starts, static_cast<uint16_t *>(out),
-                       static_cast<float *>(workspace), scale * 1.44269504088896340736f, tokens, rows, heads, group, columns, pages, shift, splits, tiles};
+                       static_cast<float *>(workspace), static_cast<uint32_t *>(workspace) + (size_t)tokens * heads * group * splits * (dim + 2u), scale * 1.44269504088896340736f, tokens, rows, heads, group, columns, pages, shift, splits, tiles};
     const dim3 block(kAttendWaves * 64u);
     if (attend_is_wide(tokens, rows, group)) {
         const uint32_t per = kAttendWaves * kTile * (dim == 256u ? 1u : 2u);
@@ -998,7 +1019,10 @@ hipError_t launch_cache_attend(const void *q, uint32_t tokens, uint32_t heads, u
     const dim3 grid(tiles, heads, splits);
     const hipError_t e = launch(dim == 64u ? attend_kernel<64> : dim == 128u ? attend_kernel<128> : attend_kernel<256>, grid, block, 0, s, nullptr, a);
     if (e != hipSuccess || splits == 1u) return e;
-    return launch(dim == 64u ? attend_join_kernel<64> : dim == 128u ? attend_join_kernel<128> : attend_join_kernel<256>, dim3(tiles, heads * kTile), dim3(256), 0, s, nullptr, a);
+    const bool many = splits > 16u;                  // more than a wavefront takes
+    const dim3 joins(tokens, many ? heads * group : (heads * group + 3u) / 4u);
+    return launch(dim == 64u ? (many ? attend_join_kernel<64, 4> : attend_join_kernel<64, 1>) : dim == 128u ? (many ? attend_join_kernel<128, 4> : attend_join_kernel<128, 1>)
+                  : many ? attend_join_kernel<256, 4> : attend_join_kernel<256, 1>, joins, dim3(256), 0, s, nullptr, a);
 }
 
 }  // namespace wg

@@ -127,7 +127,7 @@ int wg_cache_append(const void *d_k, const void *d_v, uint32_t tokens, uint32_t 
 uint64_t wg_cache_attend_workspace(uint32_t tokens, uint32_t rows, uint32_t q_heads, uint32_t heads, uint32_t dim, uint32_t columns, uint32_t page_tokens) {
     if (!tokens || !rows || !heads || q_heads < heads || !columns || !shift_of(page_tokens)) return 0;
     const uint64_t splits = attend_splits(tokens, rows, heads, q_heads / heads, columns, shift_of(page_tokens));
-    return splits < 2u ? 0u : (uint64_t)tokens * q_heads * splits * (dim + 2u) * 4u;
+    return splits < 2u ? 0u : ((uint64_t)tokens * q_heads * splits * (dim + 2u) + tokens) * 4u;
 }
 
 int wg_cache_attend(const void *d_q, uint32_t tokens, uint32_t q_heads, uint32_t heads, uint32_t dim, int64_t q_token_stride, int64_t q_head_stride,
