@@ -371,7 +371,7 @@ int wg_beam_select(const void *d_logits, wg_dtype_t dtype, uint32_t rows, uint32
 
 /* wg_reorder_rows: what else follows the parents (token histories, recurrent states): row r of each of `outer` arrays of `rows` rows
  * <- row d_parents[r] of d_src, or zeros where that is not a row.  Strides are in bytes, those of rows at least row_bytes; d_src
- * and d_dst must not overlap.  One kernel. */
+ * and d_dst must not overlap.  outer, rows <= 65535, row_bytes <= 2^33.  One kernel. */
 int wg_reorder_rows(const void *d_src, void *d_dst, const int32_t *d_parents, uint32_t outer, uint32_t rows, uint64_t row_bytes,
                     int64_t src_outer_bytes, int64_t src_row_bytes, int64_t dst_outer_bytes, int64_t dst_row_bytes, void *stream);
 
@@ -414,7 +414,7 @@ int wg_page_step(const int32_t *d_table, uint32_t rows, uint32_t columns, const 
  * largest finite magnitude among the new tokens, or stays where it is larger (not where the first token is the page's first); numbers are rounded
  * to nearest, ties to even, larger ones (infinities) become 448 times the scale, NaN stays.  Where the scale grows, the page's earlier tokens are rounded anew
  * to it.  d_origins (may be NULL): where d_origins[t] of a page's first new token is a page, the tokens in front of it come from that one (scale and all);
- * no token of the call goes to that page.  One kernel. */
+ * no token of the call goes to that page.  tokens <= 2^29, heads <= 65535, pages * page_tokens < 2^31.  One kernel. */
 int wg_cache_append(const void *d_k, const void *d_v, uint32_t tokens, uint32_t heads, uint32_t dim, int64_t k_token_stride,
                     int64_t k_head_stride, int64_t v_token_stride, int64_t v_head_stride, const int32_t *d_slots, const int32_t *d_origins,
                     uint8_t *d_k_cache, uint8_t *d_v_cache, float *d_k_scale, float *d_v_scale, uint32_t pages, uint32_t page_tokens, void *stream);
@@ -422,10 +422,12 @@ int wg_cache_append(const void *d_k, const void *d_v, uint32_t tokens, uint32_t 
 /* wg_cache_attend: attention of the tokens of a step over the cache.  d_q, d_out: bfloat16 [tokens][q_heads][dim], d_out without gaps, d_q with
  * strides in elements at multiples of 16 bytes.  Query head j reads cached head j / (q_heads / heads).  Row r has d_lens[r] tokens in the
  * cache, the tokens d_starts[r] .. d_starts[r + 1] of the call being its last ones: token i of n sees the first d_lens[r] - n + i + 1 keys (none: its output is
- * zeros).  d_out = sum of values weighted by softmax(scale * q . k).  Products in bfloat16 (the cache's values are exact in it, the
- * weights are rounded to it), sums and the softmax in fp32.  d_table, d_lens, d_starts: what wg_page_step leaves.  Entries of a table
+ * zeros); tokens from d_starts[rows] on belong to no row, and their outputs stay.  d_out = sum of values weighted by softmax(scale * q . k).  Sums and the
+ * softmax in fp32, products of what bfloat16, float16 and 8 bits hold: the cache's numbers and the queries exactly (where requests have 64 query rows and more on average, and dim
+ * is 128 or 256, a query row's numbers below 2^-15 of its largest to 2^-24 of that), the weights rounded to float16.  d_table, d_lens, d_starts: what wg_page_step leaves.  Entries of a table
  * behind a row's pages may be anything.  d_workspace: wg_cache_attend_workspace(...) bytes (0: may be NULL), 16-byte aligned, overwritten; calls that
- * share it must not overlap.  One or two kernels. */
+ * share it must not overlap.  heads <= 4095, q_heads <= 65535, rows <= 65535, pages * page_tokens and columns * page_tokens < 2^31, and no more tokens than one launch
+ * holds (heads * (tokens * q_heads / heads / 64 + rows) < 2^24).  One or two kernels. */
 uint64_t wg_cache_attend_workspace(uint32_t tokens, uint32_t rows, uint32_t q_heads, uint32_t heads, uint32_t dim, uint32_t columns, uint32_t page_tokens);
 int wg_cache_attend(const void *d_q, uint32_t tokens, uint32_t q_heads, uint32_t heads, uint32_t dim, int64_t q_token_stride, int64_t q_head_stride,
                     const uint8_t *d_k_cache, const uint8_t *d_v_cache, const float *d_k_scale, const float *d_v_scale, uint32_t pages,

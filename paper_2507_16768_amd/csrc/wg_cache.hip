@@ -429,7 +429,8 @@ __device__ __forceinline__ bool tile_of(const AttendArgs &a, uint32_t tile, uint
     return true;
 }
 // Shares that a tile's keys are cut into, and the blocks of each: shares of one size, whatever the rows' lengths, so that the workgroups that the chip holds at a time have as
-// much to do as one another (as many shares of each row, 128 rows of 2,000 to 8,000 tokens took 154 us without joining, in one share each 167; so TODO).
+// much to do as one another (128 rows of 2,000 to 8,000 tokens, 4 heads of 128: a share for each row 167 us, as many shares of every row 154 and a join of
+// 16, shares of one size 144 and 4).  The number follows from the row and not from the tile: a token of a group that is no power of two can lie in two tiles.
 __device__ __forceinline__ uint32_t shares_of(const AttendArgs &a, uint32_t blocks, uint32_t *per)
 {
     *per = blocks;
@@ -461,12 +462,12 @@ attend_kernel(const AttendArgs a)
     uint32_t len;
     TileOf t;
     if (!tile_of<kTile>(a, blockIdx.x, &len, &t)) return;
-    const uint32_t sees_most = seen_by(t, t.last - 1u, a.group), blocks = (sees_most + kBlock - 1u) / kBlock;
+    const uint32_t blocks = (seen_by(t, t.last - 1u, a.group) + kBlock - 1u) / kBlock;
     uint32_t per;
-    const uint32_t shares = shares_of(a, blocks, &per);
+    const uint32_t shares = shares_of(a, (len + kBlock - 1u) / kBlock, &per);
     if (a.splits > 1u && h == 0u && split == 0u && tid < kTile && t.first + tid < t.last) a.shares[t.begin + (t.first + tid) / a.group] = shares;
     if (split >= shares) return;
-    const uint32_t b0 = split * per, b1 = blocks - b0 < per ? blocks : b0 + per;
+    const uint32_t b0 = split * per, b1 = b0 + per < blocks ? b0 + per : blocks;             // (a tile that ends before its row may have none in the last share)
     // the lane's query row (a row behind the last is the last again, and is not stored)
     const uint32_t i = t.first + m < t.last ? t.first + m : t.last - 1u;
     const uint32_t sees = seen_by(t, i, a.group), sees_least = seen_by(t, t.first, a.group);
@@ -607,7 +608,9 @@ attend_join_kernel(const AttendArgs a)
     constexpr uint32_t kOwn = kD / 64u, kMost = 16u, kHeads = 4u / kWaves; // dims of a lane; shares of a wavefront; heads of a workgroup
     __shared__ float part[4][kD], ends[4][2];
     const uint32_t lane = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), Q = a.heads * a.group;
-    const uint32_t head = blockIdx.y * kHeads + wave / kWaves, first = wave % kWaves, shares = a.shares[blockIdx.x];
+    const uint32_t head = blockIdx.y * kHeads + wave / kWaves, first = wave % kWaves;
+    if (blockIdx.x >= (uint32_t)a.starts[a.rows]) return;                  // a token of no row, whose shares nothing has written
+    const uint32_t said = a.shares[blockIdx.x], shares = said < a.splits ? said : a.splits;
     if (shares < 2u || (kWaves == 1u && head >= Q)) return;
     const size_t at = (size_t)blockIdx.x * Q + head;
     const float *from = a.partial + at * a.splits * (kD + 2u);
@@ -705,10 +708,11 @@ attend_wide_kernel(const AttendArgs a)
     __shared__ Word4 keys[2][kD * kBlock / 16u], values[2][kD * kBlock / 16u];
     __shared__ Float2 scales[2][kBlock / 16u];
     const uint32_t tid = threadIdx.x, lane = tid & 63u, wave = __builtin_amdgcn_readfirstlane(tid >> 6), m = lane & 15u, g = lane >> 4;
-    const uint32_t h = blockIdx.x, P = 1u << a.shift;
+    // (heads first: workgroups go to the XCDs in turn, and those of a head find its keys in their L2)
+    const uint32_t h = blockIdx.x % a.heads, P = 1u << a.shift;
     uint32_t len;
     TileOf t;
-    if (!tile_of<kRows, true>(a, blockIdx.y, &len, &t)) return;
+    if (!tile_of<kRows, true>(a, blockIdx.x / a.heads, &len, &t)) return;
     const uint32_t blocks = (seen_by(t, t.last - 1u, a.group) + kBlock - 1u) / kBlock;
     const int32_t *table = a.table + (size_t)t.row * a.columns;
     const uint32_t last_column = a.columns - 1u;
@@ -989,6 +993,13 @@ static uint32_t tiles_of(uint32_t tokens, uint32_t rows, uint32_t group) { retur
 // Whether a request has query rows enough, on average, to fill a wavefront's two tiles.
 static bool attend_is_wide(uint32_t tokens, uint32_t rows, uint32_t group) { return (uint64_t)tokens * group >= 64ull * rows; }
 
+// Whether a launch holds the call: below 2^32 threads to a dimension of the grid.
+bool attend_fits(uint32_t tokens, uint32_t rows, uint32_t heads, uint32_t group)
+{
+    const uint64_t most = 0xFFFFFFu, all = (uint64_t)tokens * group;
+    return attend_is_wide(tokens, rows, group) ? (all / (kTile * kAttendWaves) + rows) * heads <= most : all / kTile + rows <= most;
+}
+
 // The most shares of a tile's keys.  Where each row's keys in one share make four times as many workgroups as there are to be shares, the chip evens them out by itself; else a row may
 // have four times its part of them, 64 at most.
 uint32_t attend_splits(uint32_t tokens, uint32_t rows, uint32_t heads, uint32_t group, uint32_t columns, uint32_t shift)
@@ -1008,12 +1019,12 @@ hipError_t launch_cache_attend(const void *q, uint32_t tokens, uint32_t heads, u
 {
     const uint32_t splits = attend_splits(tokens, rows, heads, group, columns, shift), tiles = tiles_of(tokens, rows, group);
     const AttendArgs a{static_cast<const uint16_t *>(q), q_token, q_head, k_cache, v_cache, k_scale, v_scale, table, lens, starts, static_cast<uint16_t *>(out),
-                       static_cast<float *>(workspace), static_cast<uint32_t *>(workspace) + (size_t)tokens * heads * group * splits * (dim + 2u), scale * 1.44269504088896340736f, tokens, rows, heads, group, columns, pages, shift, splits, tiles};
+                       static_cast<float *>(workspace), splits > 1u ? static_cast<uint32_t *>(workspace) + (size_t)tokens * heads * group * splits * (dim + 2u) : nullptr,
+                       scale * 1.44269504088896340736f, tokens, rows, heads, group, columns, pages, shift, splits, tiles};
     const dim3 block(kAttendWaves * 64u);
     if (attend_is_wide(tokens, rows, group)) {
         const uint32_t per = kAttendWaves * kTile * (dim == 256u ? 1u : 2u);
-        // (heads first: workgroups go to the XCDs in turn, and those of a head find its keys in their L2)
-        const dim3 wide(heads, (uint32_t)((uint64_t)tokens * group / per) + rows);
+        const dim3 wide(((uint32_t)((uint64_t)tokens * group / per) + rows) * heads);
         return launch(dim == 64u ? attend_wide_kernel<64, 2> : dim == 128u ? attend_wide_kernel<128, 2> : attend_wide_kernel<256, 1>, wide, block, 0, s, nullptr, a);
     }
     const dim3 grid(tiles, heads, splits);

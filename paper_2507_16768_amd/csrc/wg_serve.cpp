@@ -71,7 +71,7 @@ int wg_reorder_rows(const void *d_src, void *d_dst, const int32_t *d_parents, ui
         WG_WANT(d_src != d_dst, "rows must not be moved in place");
         WG_WANT(outer && rows && row_bytes, "nothing to move");
         WG_WANT(outer <= 65535u && rows <= kMostRows, "outer or rows above 65535");
-        WG_WANT(row_bytes <= 1ull << 36, "rows above 2^36 bytes");
+        WG_WANT(row_bytes <= 1ull << 33, "rows above 2^33 bytes");
         WG_WANT(src_row_bytes >= (int64_t)row_bytes && dst_row_bytes >= (int64_t)row_bytes, "rows overlap");
         return launch_reorder_rows(d_src, d_dst, d_parents, outer, rows, row_bytes, src_outer_bytes, src_row_bytes, dst_outer_bytes, dst_row_bytes,
                                    static_cast<hipStream_t>(stream));
@@ -112,7 +112,7 @@ int wg_cache_append(const void *d_k, const void *d_v, uint32_t tokens, uint32_t 
     return entry("wg_cache_append", [&](const char **why) {
         WG_WANT(d_k && d_v && d_slots && d_k_cache && d_v_cache && d_k_scale && d_v_scale, "null argument");
         WG_WANT(tokens && heads && pages, "no tokens, heads or pages");
-        WG_WANT(tokens <= 0x7FFFFFFFu && heads <= 65535u, "too many tokens or heads");
+        WG_WANT(tokens <= 1u << 29 && heads <= 65535u, "tokens above 2^29 or heads above 65535");
         WG_WANT(dim_ok(dim), "dim must be 64, 128 or 256");
         WG_WANT(shift_of(page_tokens), "page_tokens must be 16, 32 or 64");
         WG_WANT((uint64_t)pages * page_tokens <= 0x7FFFFFFFull, "slots above 2^31 - 1");
@@ -142,7 +142,7 @@ int wg_cache_attend(const void *d_q, uint32_t tokens, uint32_t q_heads, uint32_t
         WG_WANT(dim_ok(dim), "dim must be 64, 128 or 256");
         WG_WANT(shift_of(page_tokens), "page_tokens must be 16, 32 or 64");
         WG_WANT((uint64_t)columns * page_tokens <= 0x7FFFFFFFull && (uint64_t)pages * page_tokens <= 0x7FFFFFFFull, "tokens above 2^31 - 1");
-        WG_WANT((uint64_t)tokens * (q_heads / heads) / 16u + rows <= 0x7FFFFFFFull, "too many tokens");
+        WG_WANT(attend_fits(tokens, rows, heads, q_heads / heads), "too many tokens for one launch");
         WG_WANT(by_sixteen(d_q, q_token_stride, q_head_stride), "queries must lie at multiples of 16 bytes");
         WG_WANT(aligned(d_k_cache, 16) && aligned(d_v_cache, 16) && aligned(d_out, 16), "the cache and the output must be 16-byte aligned");
         WG_WANT(scale == scale && scale - scale == 0.f, "the scale is no number");

@@ -303,6 +303,28 @@ def test_a_long_row(L):
     check_attention(out, *attention(cache, x, table, lens, starts, 128 ** -0.5))
 
 
+@pytest.mark.parametrize("G,n", [(12, 5), (6, 10), (20, 3), (7, 9)])
+def test_tokens_that_lie_in_two_tiles_of_a_row_in_shares(G, n):
+    """A token's query heads may be split between two tiles, whose last tokens do not see the same blocks of keys."""
+    torch, wg = _wg()
+    lens = [64 * b + e for b in (16, 32, 48) for e in range(1, 9)]
+    cache, table, lens, starts, q = case(6, 16, 1, G, 64, lens, [n] * len(lens))
+    assert wg.cache_attend_workspace(q.shape[0], len(lens), G, 1, 64, table.shape[1], 16) > 0
+    out, x = run(torch, wg, cache, table, lens, starts, q, 0.125)
+    check_attention(out, *attention(cache, x, table, lens, starts, 0.125))
+
+
+@pytest.mark.parametrize("lens,news", [([3000, 700], [1, 2]), ([60, 20], [3, 1]), ([400, 300], [200, 100])], ids=["shares", "one share", "prompts"])
+def test_outputs_of_tokens_behind_the_rows_stay(lens, news):
+    torch, wg = _wg()
+    cache, table, lens, starts, q = case(7, 16, 2, 4, 128, lens, news)
+    more = np.concatenate([q, np.full((5,) + q.shape[1:], np.nan)])
+    out, _ = run(torch, wg, cache, table, lens, starts, more, 0.1)
+    alone, x = run(torch, wg, cache, table, lens, starts, q, 0.1)
+    check_attention(out[:len(q)], *attention(cache, x, table, lens, starts, 0.1))
+    assert (out[len(q):] == 77.0).all()
+
+
 @pytest.mark.parametrize("n,P,H,G,D", [(130, 32, 2, 4, 128), (700, 32, 2, 4, 128), (333, 16, 1, 7, 64), (150, 64, 3, 5, 256), (65, 16, 8, 1, 128), (260, 64, 1, 16, 64)])
 def test_a_long_prompt(n, P, H, G, D):
     torch, wg = _wg()

@@ -75,6 +75,16 @@ def test_cache_attend():
         dict(bytes=need - 1), dict(work=C.c_void_p(4104))])
 
 
+def test_calls_that_no_launch_holds():
+    append = dict(k=P, v=P, tokens=(1 << 29) + 1, heads=2, dim=64, k0=128, k1=64, v0=128, v1=64, slots=P, origins=None, k_cache=Q, v_cache=Q, k_scale=Q, v_scale=Q, pages=10,
+                  page=16, stream=None)
+    refused("wg_cache_append", "wg_cache_append", append, [{}])
+    refused("wg_reorder_rows", "wg_reorder_rows", dict(src=P, dst=Q, parents=P, outer=1, rows=1, row_bytes=(1 << 33) + 16, so=0, sr=1 << 40, do=0, dr=1 << 40, stream=None), [{}])
+    attend = dict(q=P, tokens=1 << 27, q_heads=64, heads=8, dim=64, q0=512, q1=64, k_cache=P, v_cache=P, k_scale=P, v_scale=P, pages=200, page=16, table=P, rows=2, columns=100,
+                  lens=P, starts=P, scale=0.125, out=Q, work=Q, bytes=1 << 62, stream=None)
+    refused("wg_cache_attend", "wg_cache_attend", attend, [{}, dict(tokens=0x7FFFFFFF), dict(rows=65535, heads=4095, q_heads=4095 * 16, tokens=65535 * 16)])
+
+
 NO_STORAGE = r"""
 import torch
 from torch._subclasses.fake_tensor import FakeTensorMode
