@@ -320,12 +320,13 @@ struct AttendArgs {
     float *partial;                                  // [token][head][split][dim + 2]
     uint32_t *shares;                                // [token]: shares of its keys
     float scale;                                     // of the scores, times log2(e)
-    uint32_t tokens, rows, heads, group, columns, pages, shift, splits, tiles;
+    uint32_t tokens, rows, heads, group, columns, pages, shift, splits, least;
 };
 constexpr uint32_t kAttendWaves = 4, kBlock = 64, kTile = 16;
 constexpr float kHeadroom = 14.f;                    // weights go up to 2^14
-constexpr uint32_t kLeastBlocks = 4;                 // blocks of a share: one for each wavefront
-constexpr uint32_t kShares = 1024;                   // shares in all, about
+constexpr uint32_t kLeastBlocks = 16, kFewRows = 8192;       // blocks of a share: half as many of prompts with few query rows
+constexpr uint32_t kShares = 1024, kWideShares = 512;        // shares in all, about; of the kernel for many rows, as many as the chip holds at a time
+constexpr __host__ __device__ uint32_t wide_rows(uint32_t dim) { return kAttendWaves * kTile * (dim == 256u ? 1u : 2u); }    // query rows of a workgroup of it
 
 typedef _Float16 Short2 __attribute__((ext_vector_type(2)));
 typedef _Float16 Short8 __attribute__((ext_vector_type(8)));
@@ -431,18 +432,22 @@ __device__ __forceinline__ bool tile_of(const AttendArgs &a, uint32_t tile, uint
 // Shares that a tile's keys are cut into, and the blocks of each: shares of one size, whatever the rows' lengths, so that the workgroups that the chip holds at a time have as
 // much to do as one another (128 rows of 2,000 to 8,000 tokens, 4 heads of 128: a share for each row 167 us, as many shares of every row 154 and a join of
 // 16, shares of one size 144 and 4).  The number follows from the row and not from the tile: a token of a group that is no power of two can lie in two tiles.
+template <uint32_t kRows, bool kWide>
 __device__ __forceinline__ uint32_t shares_of(const AttendArgs &a, uint32_t blocks, uint32_t *per)
 {
+    constexpr uint32_t kAll = kWide ? kWideShares : kShares;
     *per = blocks;
     if (a.splits == 1u || !blocks) return 1u;
-    uint32_t all = 0;                                // blocks of all rows (1,024 of them at most where keys are cut)
-    for (uint32_t r = threadIdx.x & 63u; r < a.rows; r += 64u) all += (tokens_of_row(a, r) + kBlock - 1u) / kBlock;
+    uint64_t all = 0;                                // blocks of all rows' tiles (1,024 rows at most where keys are cut; few have tokens enough for a second tile, but with many of them)
+    for (uint32_t r = threadIdx.x & 63u; r < a.rows; r += 64u) {
+        const uint32_t tokens = kWide ? (uint32_t)a.starts[r + 1u] - (uint32_t)a.starts[r] : 1u;
+        all += (uint64_t)((tokens_of_row(a, r) + kBlock - 1u) / kBlock) * (uint32_t)(((uint64_t)tokens * a.group + kRows - 1u) / kRows);
+    }
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) all += __shfl_xor(all, o);
-    all = __builtin_amdgcn_readfirstlane(all);
-    const uint64_t work = (uint64_t)all * a.heads * ((a.group + kTile - 1u) / kTile);
-    uint32_t share = (uint32_t)((work + kShares - 1u) / kShares);
-    share = share < kLeastBlocks ? kLeastBlocks : share;
+    const uint64_t work = all * a.heads;
+    uint32_t share = __builtin_amdgcn_readfirstlane((uint32_t)((work + kAll - 1u) / kAll < blocks ? (work + kAll - 1u) / kAll : blocks));
+    share = share < a.least ? a.least : share;
     const uint32_t want = (blocks + share - 1u) / share, n = want < a.splits ? want : a.splits;
     *per = (blocks + n - 1u) / n;
     return (blocks + *per - 1u) / *per;
@@ -464,7 +469,7 @@ attend_kernel(const AttendArgs a)
     if (!tile_of<kTile>(a, blockIdx.x, &len, &t)) return;
     const uint32_t blocks = (seen_by(t, t.last - 1u, a.group) + kBlock - 1u) / kBlock;
     uint32_t per;
-    const uint32_t shares = shares_of(a, (len + kBlock - 1u) / kBlock, &per);
+    const uint32_t shares = shares_of<kTile, false>(a, (len + kBlock - 1u) / kBlock, &per);
     if (a.splits > 1u && h == 0u && split == 0u && tid < kTile && t.first + tid < t.last) a.shares[t.begin + (t.first + tid) / a.group] = shares;
     if (split >= shares) return;
     const uint32_t b0 = split * per, b1 = b0 + per < blocks ? b0 + per : blocks;             // (a tile that ends before its row may have none in the last share)
@@ -697,10 +702,11 @@ struct Yes { static constexpr bool value = true; };
 struct No { static constexpr bool value = false; };
 
 template <uint32_t kD, uint32_t kTiles>
-__global__ void __launch_bounds__(kAttendWaves * 64u, 2)
+__global__ void __launch_bounds__(kAttendWaves * 64u, kD == 64u ? 3 : 2)      // (heads of 64: 32 prompts of 64 tokens 57 us, with the registers for two only 85)
 attend_wide_kernel(const AttendArgs a)
 {
     constexpr uint32_t kSteps = kD / 32u, kParts = kD / 16u, kRows = kAttendWaves * kTile * kTiles, kThreads = kAttendWaves * 64u;
+    static_assert(kRows == wide_rows(kD) && kRows <= kThreads, "as the host counts them");
     static_assert(kAttendWaves == kBlock / 16u, "a wavefront for sixteen keys");
     constexpr uint32_t kAhead = kD == 256u ? 1u : 2u, kValuesAhead = 4u;         // tiles of keys and parts of values that are asked for in LDS before they are needed
     constexpr bool kBytes = kD >= 128u;              // scores from 8-bit numbers: products of 128 of them
@@ -713,7 +719,12 @@ attend_wide_kernel(const AttendArgs a)
     uint32_t len;
     TileOf t;
     if (!tile_of<kRows, true>(a, blockIdx.x / a.heads, &len, &t)) return;
-    const uint32_t blocks = (seen_by(t, t.last - 1u, a.group) + kBlock - 1u) / kBlock;
+    const uint32_t split = blockIdx.y;
+    uint32_t per;
+    const uint32_t shares = shares_of<kRows, true>(a, (len + kBlock - 1u) / kBlock, &per);
+    if (a.splits > 1u && h == 0u && split == 0u && tid < kRows && t.first + tid < t.last) a.shares[t.begin + (t.first + tid) / a.group] = shares;
+    if (split >= shares) return;
+    const uint32_t seen = (seen_by(t, t.last - 1u, a.group) + kBlock - 1u) / kBlock, b0 = split * per, blocks = b0 + per < seen ? b0 + per : seen;     // (blocks: where they end)
     const int32_t *table = a.table + (size_t)t.row * a.columns;
     const uint32_t last_column = a.columns - 1u;
     // the wavefront's rows
@@ -946,15 +957,15 @@ attend_wide_kernel(const AttendArgs a)
                 for (uint32_t i = 0; i < kTiles; i++) nans[i] |= (uint64_t)nans_seen(v, mine >= sees[i] ? 0u : sees[i] - mine < 16u ? sees[i] - mine : 16u) << (4u * p);
             }
     };
-    if (blocks) {
-        ask_pages(0u);
+    if (b0 < blocks) {
+        ask_pages(b0);
         ask();
-        if (blocks > 1u) ask_pages(1u);
-        put(0u);
+        if (b0 + 1u < blocks) ask_pages(b0 + 1u);
+        put(b0 & 1u);
     }
     // Blocks that all queries of the wavefront see, then the others, in loops of their own: registers that the second has no room for must not be waited for in the first.
     // (The wavefronts meet at a barrier for every block, in whichever loop each is.)
-    const uint32_t whole = sees_least / kBlock;
+    const uint32_t whole = sees_least / kBlock < blocks ? sees_least / kBlock : blocks;
     auto step = [&](uint32_t b, auto edge) {
         __syncthreads();
         if (b + 1u < blocks) {
@@ -964,7 +975,7 @@ attend_wide_kernel(const AttendArgs a)
         if (!decltype(edge)::value || b * kBlock < sees_most) look(b, edge);
         if (b + 1u < blocks) put(b & 1u ^ 1u);       // (its last reader is behind this round's barrier)
     };
-    uint32_t b = 0;
+    uint32_t b = b0;
 #pragma nounroll
     for (; b < whole; b++) step(b, No{});
 #pragma nounroll
@@ -976,8 +987,20 @@ attend_wide_kernel(const AttendArgs a)
         total += __shfl_xor(total, 32);
         const uint32_t r = w0 + i * kTile + m;
         if (r >= t.last) continue;
+        const size_t row = (size_t)(t.begin + r / a.group) * (a.heads * a.group) + h * a.group + r % a.group;
+        if (shares > 1u) {
+            float *to = a.partial + (row * a.splits + split) * (kD + 2u);
+#pragma unroll
+            for (uint32_t p = 0; p < kParts; p++)
+#pragma unroll
+                for (uint32_t e = 0; e < 4u; e += 2u)
+                    *reinterpret_cast<Float2 *>(to + p * 16u + g * 4u + e) =
+                        Float2{nans[i] >> (4u * p + e) & 1u ? __builtin_nanf("") : o[i][p][e], nans[i] >> (4u * p + e + 1u) & 1u ? __builtin_nanf("") : o[i][p][e + 1u]};
+            if (g == 0u) *reinterpret_cast<Float2 *>(to + kD) = Float2{begun[i] ? base[i] : -__builtin_inff(), total};
+            continue;
+        }
         const float by = total > 0.f ? 1.f / total : total == total ? 0.f : total;           // (a row that sees nothing: zeros)
-        uint16_t *out = a.out + ((size_t)(t.begin + r / a.group) * (a.heads * a.group) + h * a.group + r % a.group) * kD + g * 4u;
+        uint16_t *out = a.out + row * kD + g * 4u;
 #pragma unroll
         for (uint32_t p = 0; p < kParts; p++) {
             float x[4];
@@ -990,25 +1013,42 @@ attend_wide_kernel(const AttendArgs a)
 
 static uint32_t tiles_of(uint32_t tokens, uint32_t rows, uint32_t group) { return (uint32_t)((uint64_t)tokens * group / kTile) + rows; }
 
-// Whether a request has query rows enough, on average, to fill a wavefront's two tiles.
-static bool attend_is_wide(uint32_t tokens, uint32_t rows, uint32_t group) { return (uint64_t)tokens * group >= 64ull * rows; }
+// Whether requests have query rows enough, on average, for the kernel that holds many of them, which costs a request with few as much as one with its tile full.  With 8
+// heads of 128 and 4 query heads each, 32 rows of 2,000 tokens took 40 us in the other one and 51 in this for 16 query rows each, 57 and 52 for 32, 95 and 67 for
+// 64, 192 and 112 for 256; 4 such rows 17 and 22 for 32, 22 and 24 for 64, 43 and 37 for 256.  Heads of 64, whose scores come from bfloat16 in both: 32 and 40 for 32, 52 and 52 for 64.
+static bool attend_is_wide(uint32_t tokens, uint32_t rows, uint32_t group, uint32_t dim) { return (uint64_t)tokens * group >= (dim == 64u ? 64ull : 32ull) * rows; }
 
 // Whether a launch holds the call: below 2^32 threads to a dimension of the grid.
-bool attend_fits(uint32_t tokens, uint32_t rows, uint32_t heads, uint32_t group)
+bool attend_fits(uint32_t tokens, uint32_t rows, uint32_t heads, uint32_t group, uint32_t dim)
 {
     const uint64_t most = 0xFFFFFFu, all = (uint64_t)tokens * group;
-    return attend_is_wide(tokens, rows, group) ? (all / (kTile * kAttendWaves) + rows) * heads <= most : all / kTile + rows <= most;
+    return attend_is_wide(tokens, rows, group, dim) ? (all / (kTile * kAttendWaves) + rows) * heads <= most : all / kTile + rows <= most;
+}
+
+// Blocks that a share has at least: a share more is partial results of all query rows to write and read, and a second kernel.  With 4 blocks, one for each wavefront, 256 rows of 300 tokens
+// took 49 us for 39 with 16, and 4 rows of 2,000 13.6 for 16.7.  Prompts, whose shares take longer for as many blocks: a prompt of 1,000 tokens, 32 query heads over 8, took 31 us
+// in one share and 42 in two of 8 blocks; 16 new tokens of each of 4 rows of 2,000 33 us in shares of 16 blocks and 24 of 8.
+static uint32_t least_blocks(uint32_t tokens, uint32_t rows, uint32_t heads, uint32_t group, uint32_t dim)
+{
+    return attend_is_wide(tokens, rows, group, dim) && (uint64_t)tokens * group * heads <= kFewRows ? kLeastBlocks / 2u : kLeastBlocks;
 }
 
 // The most shares of a tile's keys.  Where each row's keys in one share make four times as many workgroups as there are to be shares, the chip evens them out by itself; else a row may
-// have four times its part of them, 64 at most.
-uint32_t attend_splits(uint32_t tokens, uint32_t rows, uint32_t heads, uint32_t group, uint32_t columns, uint32_t shift)
+// have four times its part of them, 64 at most.  Prompts are cut where they leave half of the chip or more idle, to fill it: 64 query rows of each of 8 heads behind 20,000 tokens took 405 us in one share, 30 in 20; a prompt of
+// 512 tokens behind 7,500, 175 and 98 in three.
+uint32_t attend_splits(uint32_t tokens, uint32_t rows, uint32_t heads, uint32_t group, uint32_t dim, uint32_t columns, uint32_t shift)
 {
-    if (attend_is_wide(tokens, rows, group)) return 1u;
-    const uint64_t tiles = (uint64_t)(tokens < rows ? tokens : rows) * ((group + kTile - 1u) / kTile) * heads;
-    const uint64_t all = tokens > rows ? (uint64_t)tokens * group / kTile * heads : tiles, n = all > tiles ? all : tiles;
-    if (n >= 4u * kShares || rows > 1024u) return 1u;
-    const uint64_t want = 4u * ((kShares + n - 1u) / n), blocks = (((uint64_t)columns << shift) + kBlock - 1u) / kBlock, most = (blocks + kLeastBlocks - 1u) / kLeastBlocks;
+    if (rows > 1024u) return 1u;
+    const uint64_t blocks = (((uint64_t)columns << shift) + kBlock - 1u) / kBlock, requests = tokens < rows ? tokens : rows;
+    const bool many = attend_is_wide(tokens, rows, group, dim);
+    const uint64_t least = least_blocks(tokens, rows, heads, group, dim), most = (blocks + least - 1u) / least;
+    uint64_t want;
+    if (many) want = kWideShares / (((uint64_t)tokens * group / wide_rows(dim) + requests) * heads);
+    else {
+        const uint64_t tiles = requests * ((group + kTile - 1u) / kTile) * heads;
+        const uint64_t all = tokens > rows ? (uint64_t)tokens * group / kTile * heads : tiles, n = all > tiles ? all : tiles;
+        want = n >= 4u * kShares ? 1u : 4u * ((kShares + n - 1u) / n);
+    }
     const uint64_t splits = want < most ? want : most;
     return splits < 1u ? 1u : splits > 64u ? 64u : (uint32_t)splits;
 }
@@ -1017,18 +1057,17 @@ hipError_t launch_cache_attend(const void *q, uint32_t tokens, uint32_t heads, u
                                const uint8_t *v_cache, const float *k_scale, const float *v_scale, uint32_t pages, uint32_t shift, const int32_t *table,
                                uint32_t rows, uint32_t columns, const int32_t *lens, const int32_t *starts, float scale, void *out, void *workspace, hipStream_t s)
 {
-    const uint32_t splits = attend_splits(tokens, rows, heads, group, columns, shift), tiles = tiles_of(tokens, rows, group);
+    const uint32_t splits = attend_splits(tokens, rows, heads, group, dim, columns, shift);
     const AttendArgs a{static_cast<const uint16_t *>(q), q_token, q_head, k_cache, v_cache, k_scale, v_scale, table, lens, starts, static_cast<uint16_t *>(out),
                        static_cast<float *>(workspace), splits > 1u ? static_cast<uint32_t *>(workspace) + (size_t)tokens * heads * group * splits * (dim + 2u) : nullptr,
-                       scale * 1.44269504088896340736f, tokens, rows, heads, group, columns, pages, shift, splits, tiles};
+                       scale * 1.44269504088896340736f, tokens, rows, heads, group, columns, pages, shift, splits,
+                       least_blocks(tokens, rows, heads, group, dim)};
     const dim3 block(kAttendWaves * 64u);
-    if (attend_is_wide(tokens, rows, group)) {
-        const uint32_t per = kAttendWaves * kTile * (dim == 256u ? 1u : 2u);
-        const dim3 wide(((uint32_t)((uint64_t)tokens * group / per) + rows) * heads);
-        return launch(dim == 64u ? attend_wide_kernel<64, 2> : dim == 128u ? attend_wide_kernel<128, 2> : attend_wide_kernel<256, 1>, wide, block, 0, s, nullptr, a);
-    }
-    const dim3 grid(tiles, heads, splits);
-    const hipError_t e = launch(dim == 64u ? attend_kernel<64> : dim == 128u ? attend_kernel<128> : attend_kernel<256>, grid, block, 0, s, nullptr, a);
+    hipError_t e;
+    if (attend_is_wide(tokens, rows, group, dim)) {
+        const dim3 wide(((uint32_t)((uint64_t)tokens * group / wide_rows(dim)) + rows) * heads, splits);
+        e = launch(dim == 64u ? attend_wide_kernel<64, 2> : dim == 128u ? attend_wide_kernel<128, 2> : attend_wide_kernel<256, 1>, wide, block, 0, s, nullptr, a);
+    } else e = launch(dim == 64u ? attend_kernel<64> : dim == 128u ? attend_kernel<128> : attend_kernel<256>, dim3(tiles_of(tokens, rows, group), heads, splits), block, 0, s, nullptr, a);
     if (e != hipSuccess || splits == 1u) return e;
     const bool many = splits > 16u;                  // more than a wavefront takes
     const dim3 joins(tokens, many ? heads * group : (heads * group + 3u) / 4u);

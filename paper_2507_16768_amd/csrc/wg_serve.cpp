@@ -126,7 +126,7 @@ int wg_cache_append(const void *d_k, const void *d_v, uint32_t tokens, uint32_t 
 
 uint64_t wg_cache_attend_workspace(uint32_t tokens, uint32_t rows, uint32_t q_heads, uint32_t heads, uint32_t dim, uint32_t columns, uint32_t page_tokens) {
     if (!tokens || !rows || !heads || q_heads < heads || !columns || !shift_of(page_tokens)) return 0;
-    const uint64_t splits = attend_splits(tokens, rows, heads, q_heads / heads, columns, shift_of(page_tokens));
+    const uint64_t splits = attend_splits(tokens, rows, heads, q_heads / heads, dim, columns, shift_of(page_tokens));
     return splits < 2u ? 0u : ((uint64_t)tokens * q_heads * splits * (dim + 2u) + tokens) * 4u;
 }
 
@@ -142,7 +142,7 @@ int wg_cache_attend(const void *d_q, uint32_t tokens, uint32_t q_heads, uint32_t
         WG_WANT(dim_ok(dim), "dim must be 64, 128 or 256");
         WG_WANT(shift_of(page_tokens), "page_tokens must be 16, 32 or 64");
         WG_WANT((uint64_t)columns * page_tokens <= 0x7FFFFFFFull && (uint64_t)pages * page_tokens <= 0x7FFFFFFFull, "tokens above 2^31 - 1");
-        WG_WANT(attend_fits(tokens, rows, heads, q_heads / heads), "too many tokens for one launch");
+        WG_WANT(attend_fits(tokens, rows, heads, q_heads / heads, dim), "too many tokens for one launch");
         WG_WANT(by_sixteen(d_q, q_token_stride, q_head_stride), "queries must lie at multiples of 16 bytes");
         WG_WANT(aligned(d_k_cache, 16) && aligned(d_v_cache, 16) && aligned(d_out, 16), "the cache and the output must be 16-byte aligned");
         WG_WANT(scale == scale && scale - scale == 0.f, "the scale is no number");

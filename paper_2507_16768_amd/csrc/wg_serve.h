@@ -25,9 +25,9 @@ hipError_t launch_cache_append(const void *k, const void *v, uint32_t tokens, ui
                                int64_t v_head, const int32_t *slots, const int32_t *origins, uint8_t *k_cache, uint8_t *v_cache, float *k_scale,
                                float *v_scale, uint32_t pages, uint32_t shift, hipStream_t s);
 // Whether one launch holds the call.
-bool attend_fits(uint32_t tokens, uint32_t rows, uint32_t heads, uint32_t group);
+bool attend_fits(uint32_t tokens, uint32_t rows, uint32_t heads, uint32_t group, uint32_t dim);
 // Shares that a tile's keys may be cut into; each leaves dim + 2 floats for every token and query head.
-uint32_t attend_splits(uint32_t tokens, uint32_t rows, uint32_t heads, uint32_t group, uint32_t columns, uint32_t shift);
+uint32_t attend_splits(uint32_t tokens, uint32_t rows, uint32_t heads, uint32_t group, uint32_t dim, uint32_t columns, uint32_t shift);
 hipError_t launch_cache_attend(const void *q, uint32_t tokens, uint32_t heads, uint32_t group, uint32_t dim, int64_t q_token, int64_t q_head, const uint8_t *k_cache,
                                const uint8_t *v_cache, const float *k_scale, const float *v_scale, uint32_t pages, uint32_t shift, const int32_t *table,
                                uint32_t rows, uint32_t columns, const int32_t *lens, const int32_t *starts, float scale, void *out, void *workspace, hipStream_t s);

@@ -337,6 +337,27 @@ def test_a_long_prompt(n, P, H, G, D):
     check_attention(out, *attention(cache, x, table, lens, starts, D ** -0.5))
 
 
+@pytest.mark.parametrize("P,H,G,D", [(16, 64, 2, 64), (32, 64, 2, 128), (64, 32, 2, 256)])
+def test_prompts_that_fill_the_chip(P, H, G, D):
+    """Enough of them for no row's keys to be cut."""
+    torch, wg = _wg()
+    cache, table, lens, starts, q = case(8, P, H, G, D, [270, 100], [260, 33])
+    assert wg.cache_attend_workspace(q.shape[0], 2, H * G, H, D, table.shape[1], P) == 0
+    out, x = run(torch, wg, cache, table, lens, starts, q, D ** -0.5)
+    check_attention(out, *attention(cache, x, table, lens, starts, D ** -0.5))
+
+
+@pytest.mark.parametrize("P,H,G,D", [(16, 2, 4, 64), (32, 1, 12, 128), (64, 1, 5, 256)])
+def test_prompts_behind_long_rows(P, H, G, D):
+    """Few query rows and many keys: the rows' keys are cut, one row's into more shares than another's."""
+    torch, wg = _wg()
+    lens, news = [5000, 1090, 70, 0, 3], [61, 66, 50, 0, 1]
+    cache, table, lens, starts, q = case(9, P, H, G, D, lens, news)
+    assert wg.cache_attend_workspace(q.shape[0], len(lens), H * G, H, D, table.shape[1], P) > 0
+    out, x = run(torch, wg, cache, table, lens, starts, q, D ** -0.5)
+    check_attention(out, *attention(cache, x, table, lens, starts, D ** -0.5))
+
+
 @pytest.mark.parametrize("D,size", [(128, 1e30), (128, 1e-30), (256, 1e36), (64, 1e-37)])
 def test_queries_at_the_ends_of_the_range(D, size):
     """What the scale brings back to the middle of it."""

@@ -64,7 +64,7 @@ def test_cache_append():
 def test_cache_attend():
     shape = dict(tokens=2, rows=2, q_heads=8, heads=2, dim=64, columns=100, page_tokens=16)
     need = wg.cache_attend_workspace(**shape)
-    assert need == (2 * 8 * 7 * 66 + 2) * 4 and wg.cache_attend_workspace(**dict(shape, columns=8)) == 0 and wg.cache_attend_workspace(**dict(shape, heads=0)) == 0
+    assert need == (2 * 8 * 2 * 66 + 2) * 4 and wg.cache_attend_workspace(**dict(shape, columns=8)) == 0 and wg.cache_attend_workspace(**dict(shape, heads=0)) == 0
     good = dict(q=P, tokens=2, q_heads=8, heads=2, dim=64, q0=512, q1=64, k_cache=P, v_cache=P, k_scale=P, v_scale=P, pages=200, page=16, table=P, rows=2, columns=100,
                 lens=P, starts=P, scale=0.125, out=Q, work=Q, bytes=need, stream=None)
     refused("wg_cache_attend", "wg_cache_attend", good, [
