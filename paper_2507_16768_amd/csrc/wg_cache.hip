@@ -1034,7 +1034,7 @@ static uint32_t least_blocks(uint32_t tokens, uint32_t rows, uint32_t heads, uin
 }
 
 // The most shares of a tile's keys.  Where each row's keys in one share make four times as many workgroups as there are to be shares, the chip evens them out by itself; else a row may
-// have four times its part of them, 64 at most.  Prompts are cut where they leave half of the chip or more idle, to fill it: 64 query rows of each of 8 heads behind 20,000 tokens took 405 us in one share, 30 in 20; a prompt of
+// have four times its part of them, 64 at most.  Prompts are cut where they leave half of the chip or more idle, to fill it: 64 query rows of each of 8 heads behind 20,000 tokens took 405 us in one share, 30 in 39; a prompt of
 // 512 tokens behind 7,500, 175 and 98 in three.
 uint32_t attend_splits(uint32_t tokens, uint32_t rows, uint32_t heads, uint32_t group, uint32_t dim, uint32_t columns, uint32_t shift)
 {

@@ -4,7 +4,7 @@
 // All of it is whole numbers: prefix sums over rows of pages needed, pages released and tokens.  Bound by launches and trips to memory, not by
 // bytes: rows wait for the sums of the rows before them, which every workgroup works out by itself from the lengths (a few KB in the L2) in place of
 // waiting for another.  Where rows follow parents, a first kernel counts what each request needs and releases (page_count_kernel); the second
-// (page_beam_kernel) sums that up and writes.  A workgroup of either takes 256 columns of a request's tables, which it holds in LDS: a thread's loads of all rows are
+// (page_beam_kernel) sums that up and writes.  A workgroup of either takes up to 256 columns of a request's tables, which it holds in LDS: a thread's loads of eight rows are
 // in flight together, and what it looks for among the rows of a column it finds there.
 //
 // A row's new table is its parent's whole one, so that within a request a page is referred to at one place of the tables only, and an old row with a
@@ -24,8 +24,11 @@ struct GroupNeed { uint32_t pages, tokens; };
 struct Back { uint32_t always, served; };
 constexpr uint32_t kTooLong = 0xFFFFFFFFu;
 
-// Columns that a workgroup takes of a request's tables: as many as it has threads, half as many where the rows would fill more than 32 KB of LDS.
-static __host__ __device__ inline uint32_t columns_of(uint32_t K) { return K <= 32u ? kPageThreads : kPageThreads / 2u; }
+// Threads that share a column of a request's tables, and with it the rows whose pages are looked for among the others: each has eight of them at the most.  (A thread
+// for a column of any number of rows took 256 us for 8 requests of 64 beams and 512 columns, eight take 75; for 32 requests of 16 beams 50, two take 28.)  A workgroup takes as
+// many columns as that leaves it.  kFew: up to eight rows, of kernels that know it (18.4 us without, 17.7 with, for 32 requests of eight beams).
+static __host__ __device__ inline uint32_t sharers_of(uint32_t K) { return K <= 8u ? 1u : K <= 16u ? 2u : K <= 32u ? 4u : 8u; }
+static __host__ __device__ inline uint32_t columns_of(uint32_t K) { return kPageThreads / sharers_of(K); }
 
 // The rows of a request before the step, after they took over their parents' tables.
 struct Rows {
@@ -40,20 +43,20 @@ constexpr uint32_t kNoFork = 0xFFFFFFFFu;
 
 __device__ __forceinline__ uint32_t tokens_of(int32_t n, uint32_t most) { return n < 0 ? 0u : (uint32_t)n < most ? (uint32_t)n : most; }
 
-// The request's columns [j0, j0 + width) to LDS, row by row, a column to a thread.
+// The request's columns [j0, j0 + width) to LDS, row by row.
 __device__ __forceinline__ void read_columns(int32_t *ids, const int32_t *table, uint32_t row0, uint32_t K, uint32_t M, uint32_t j0, uint32_t width)
 {
-    const uint32_t tid = threadIdx.x, j = j0 + tid;
-    if (tid >= width || j >= M) return;
-    uint32_t k = 0;
-    for (; k + 8u <= K; k += 8u) {
+    const uint32_t tid = threadIdx.x, c = tid & (width - 1u), j = j0 + c, step = kPageThreads / width;
+    if (j >= M) return;
+    uint32_t k = tid / width;
+    for (; k + 7u * step < K; k += 8u * step) {
         int32_t x[8];
 #pragma unroll
-        for (uint32_t i = 0; i < 8u; i++) x[i] = table[(size_t)(row0 + k + i) * M + j];
+        for (uint32_t i = 0; i < 8u; i++) x[i] = table[(size_t)(row0 + k + i * step) * M + j];
 #pragma unroll
-        for (uint32_t i = 0; i < 8u; i++) ids[(k + i) * width + tid] = x[i];
+        for (uint32_t i = 0; i < 8u; i++) ids[(k + i * step) * width + c] = x[i];
     }
-    for (; k < K; k++) ids[k * width + tid] = table[(size_t)(row0 + k) * M + j];
+    for (; k < K; k += step) ids[k * width + c] = table[(size_t)(row0 + k) * M + j];
 }
 
 // What a thread k < K asks for of its row, early.
@@ -110,12 +113,14 @@ __device__ __forceinline__ void read_rows(Rows &g, const RowLoads &x, const int3
     __syncthreads();
 }
 
-// The old rows whose page at column j goes back, as bits: whatever becomes of the request, and where it is served besides.  ids: the thread's column.
+// The old rows whose page at column j goes back, as bits: whatever becomes of the request, and where it is served besides.  ids: the column.  Of several threads of a
+// column each one answers for the rows that are `turn` modulo their number.
 struct Gone { unsigned long long always, served; };
-__device__ __forceinline__ Gone gone_at(const Rows &g, const int32_t *ids, uint32_t width, uint32_t K, uint32_t j)
+template <bool kFew>
+__device__ __forceinline__ Gone gone_at(const Rows &g, const int32_t *ids, uint32_t width, uint32_t K, uint32_t j, uint32_t turn)
 {
     Gone r{0ull, 0ull};
-    if (K <= 8u) {
+    if (kFew) {
         // eight rows out of registers (by the loop below, trips to LDS one after the other, twice as long: 2.7 us for eight beams)
         int32_t id[8];
         uint32_t in = 0, referred = 0, kept = 0;      // the rows whose tables reach so far; as far as a child has them; as far as one goes on with them
@@ -141,24 +146,30 @@ __device__ __forceinline__ Gone gone_at(const Rows &g, const int32_t *ids, uint3
         r.always = always; r.served = served;
         return r;
     }
-    // (a child goes on with the others)
-    unsigned long long look = 0;
+    unsigned long long in = 0, referred = 0, kept = 0;
 #pragma unroll 8
-    for (uint32_t b = 0; b < K; b++) { const uint4 e = g.ends[b]; if (j < e.x && j >= e.z) look |= 1ull << b; }
-    while (look) {
-        const uint32_t b = (uint32_t)__builtin_ctzll(look);
-        look &= look - 1ull;
+    for (uint32_t o = 0; o < K; o++) {
+        const uint4 e = g.ends[o];
+        in |= (unsigned long long)(j < e.x) << o;
+        referred |= (unsigned long long)(j < e.y) << o;
+        kept |= (unsigned long long)(j < e.z) << o;
+    }
+    const uint32_t sharers = kPageThreads / width;
+    for (uint32_t b = turn; b < K; b += sharers) {
+        if (!((in & ~kept) >> b & 1ull)) continue;    // (a child goes on with the others)
         const int32_t id = ids[b * width];
-        bool first = true, referred = false, kept = false;
-#pragma unroll 4
-        for (uint32_t o = 0; o < K; o++) {
-            const uint4 e = g.ends[o];
-            const bool same = ids[o * width] == id && j < e.x;
-            first &= !(same && o < b);
-            referred |= same && j < e.y;
-            kept |= same && j < e.z;
+        unsigned long long same = 0;
+        uint32_t o = 0;
+        for (; o + 8u <= K; o += 8u) {
+            uint32_t eight = 0;
+#pragma unroll
+            for (uint32_t i = 0; i < 8u; i++) eight |= (uint32_t)(ids[(o + i) * width] == id) << i;
+            same |= (unsigned long long)eight << o;
         }
-        if (first && !kept) { if (referred) r.served |= 1ull << b; else r.always |= 1ull << b; }
+        for (; o < K; o++) same |= (unsigned long long)(ids[o * width] == id) << o;
+        same &= in;
+        if ((same & ((1ull << b) - 1ull)) || (same & kept)) continue;
+        if (same & referred) r.served |= 1ull << b; else r.always |= 1ull << b;
     }
     return r;
 }
@@ -185,6 +196,7 @@ __device__ __forceinline__ uint32_t block_scan(uint32_t x, uint32_t *part, uint3
     return x + before;
 }
 
+template <bool kFew>
 __global__ void __launch_bounds__(kPageThreads)
 page_count_kernel(const int32_t *__restrict__ table, const int32_t *__restrict__ lens, const int32_t *__restrict__ counts, const int32_t *__restrict__ parents,
                   uint32_t K, uint32_t M, uint32_t shift, GroupNeed *__restrict__ needs, uint32_t *__restrict__ forks, Back *__restrict__ back)
@@ -192,13 +204,13 @@ page_count_kernel(const int32_t *__restrict__ table, const int32_t *__restrict__
     extern __shared__ int32_t ids[];
     __shared__ Rows g;
     __shared__ uint32_t part[2][kPageWaves];
-    const uint32_t tid = threadIdx.x, row0 = blockIdx.x * K, width = columns_of(K), j = blockIdx.y * width + tid;
+    const uint32_t tid = threadIdx.x, row0 = blockIdx.x * K, width = kFew ? kPageThreads : columns_of(K), sharers = kPageThreads / width, c = tid / sharers, j = blockIdx.y * width + c;
     const RowLoads row = load_row(lens, counts, parents, nullptr, row0, K);
     read_columns(ids, table, row0, K, M, blockIdx.y * width, width);
     __syncthreads();
     read_rows<true>(g, row, table, ids, blockIdx.y * width, width, blockIdx.y == 0u, row0, K, M, shift);
     Gone gone{0ull, 0ull};
-    if (tid < width && j < M) gone = gone_at(g, ids + tid, width, K, j);
+    if (j < M) gone = gone_at<kFew>(g, ids + c, width, K, j, tid % sharers);
     const uint32_t always = wave_sum((uint32_t)__popcll(gone.always)), served = wave_sum((uint32_t)__popcll(gone.served));
     if ((tid & 63u) == 0u) { part[0][tid >> 6] = always; part[1][tid >> 6] = served; }
     __syncthreads();
@@ -325,13 +337,14 @@ page_kernel(const PageArgs a)
 }
 
 // With parents: a workgroup takes some columns of a request's tables; the one of the first columns also the tokens.
+template <bool kFew>
 __global__ void __launch_bounds__(kPageThreads)
 page_beam_kernel(const PageArgs a)
 {
     extern __shared__ int32_t ids[];
     __shared__ Rows g;
     __shared__ uint32_t part[5u * kPageWaves], begins[2][kBeamMax], flags[kPageThreads];
-    const uint32_t tid = threadIdx.x, page = 1u << a.shift, K = a.K, G = a.rows / K, width = columns_of(K), j0 = blockIdx.y * width, j = j0 + tid, chunks = gridDim.y;
+    const uint32_t tid = threadIdx.x, page = 1u << a.shift, K = a.K, G = a.rows / K, width = kFew ? kPageThreads : columns_of(K), sharers = kPageThreads / width, j0 = blockIdx.y * width, chunks = gridDim.y;
     const uint32_t g0 = blockIdx.x * a.per, g1 = G - g0 < a.per ? G : g0 + a.per;
     const uint64_t taken = a.counters[0], given = a.counters[1];
     const uint32_t free = given <= taken ? 0u : given - taken < a.N ? (uint32_t)(given - taken) : a.N;
@@ -397,17 +410,19 @@ page_beam_kernel(const PageArgs a)
         }
         __syncthreads();
         auto page_of = [&](uint32_t k, uint32_t at) { return a.ring[ring_at(head, begins[0][k] + at, a.N)]; };
-        if (tid < width)
-#pragma unroll 8
-            for (uint32_t k = 0; k < K; k++) {
+        {
+            const uint32_t c = tid & (width - 1u), j = j0 + c;
+#pragma unroll 4
+            for (uint32_t k = tid / width; k < K; k += sharers) {
                 const int4 row = g.rows[k];               // source, pages, pages with the step, place of the fork
                 const uint32_t have = (uint32_t)row.y, fork = v.yes ? (uint32_t)row.w : kNoFork;
                 if (j >= (v.yes ? (uint32_t)row.z : have)) continue;
-                int32_t id = ids[(row.x < 0 ? 0u : (uint32_t)row.x) * width + tid];
+                int32_t id = ids[(row.x < 0 ? 0u : (uint32_t)row.x) * width + c];
                 if (j >= have) id = page_of(k, (fork != kNoFork ? 1u : 0u) + j - have);
                 else if (j == fork) id = page_of(k, 0u);
                 a.table_out[(size_t)(row0 + k) * a.M + j] = id;
             }
+        }
         if (blockIdx.y == 0u) {
             for (uint32_t k = tid >> 6; k < K; k += kPageWaves) {
                 const int4 row = g.rows[k];
@@ -427,11 +442,14 @@ page_beam_kernel(const PageArgs a)
         if (back) {
             // pages go back by place in the tables, then by row
             Gone gone{0ull, 0ull};
-            if (tid < width && j < a.M) gone = gone_at(g, ids + tid, width, K, j);
+            const uint32_t c = tid / sharers, turn = tid % sharers;
+            if (j0 + c < a.M) gone = gone_at<kFew>(g, ids + c, width, K, j0 + c, turn);
             unsigned long long rows = gone.always | (v.yes ? gone.served : 0ull);
+            for (uint32_t o = 1; o < sharers; o <<= 1) rows |= __shfl_xor(rows, o);
+            if (turn) rows = 0ull;                    // (the first one writes them)
             const uint32_t count = (uint32_t)__popcll(rows);
             uint32_t all, at = s.released + before + block_scan(count, part, &all) - count;
-            for (; rows; rows &= rows - 1ull) a.ring[ring_at(tail, at++, a.N)] = ids[(uint32_t)__builtin_ctzll(rows) * width + tid];
+            for (; rows; rows &= rows - 1ull) a.ring[ring_at(tail, at++, a.N)] = ids[(uint32_t)__builtin_ctzll(rows) * width + c];
         }
         s.pages = v.end;
         if (v.yes) s.used += v.asks;
@@ -462,16 +480,18 @@ hipError_t launch_page_step(const int32_t *table, uint32_t rows, uint32_t column
     GroupNeed *needs = static_cast<GroupNeed *>(workspace);
     Back *back = reinterpret_cast<Back *>(needs + G);
     uint32_t *forks = reinterpret_cast<uint32_t *>(back + (size_t)G * chunks);
-    // every workgroup goes over all requests before its own: at most 512 of them for the same columns
-    const uint32_t per = (G + 511u) / 512u;
+    // every workgroup goes over all requests before its own: at most 2,048 of them for the same columns (of 4,096 requests of
+    // four beams: 81 us with 512, 65 with 2,048)
+    const uint32_t per = (G + 2047u) / 2048u;
     const PageArgs a{table, lens, counts, parents, ring, counters, table_out, lens_out, starts, slots, positions, origins, counters_out,
                      needs, forks, back, rows, K, columns, shift, pages, tokens, per};
     const dim3 block(kPageThreads);
     if (!parents) return launch(page_kernel, dim3((G + per - 1u) / per), block, 0, s, nullptr, a);
+    const bool few = K <= 8u;
     const uint32_t lds = K * columns_of(K) * 4u;
-    const hipError_t e = launch(page_count_kernel, dim3(G, chunks), block, lds, s, nullptr, table, lens, counts, parents, K, columns, shift, needs, forks, back);
+    const hipError_t e = launch(few ? page_count_kernel<true> : page_count_kernel<false>, dim3(G, chunks), block, lds, s, nullptr, table, lens, counts, parents, K, columns, shift, needs, forks, back);
     if (e != hipSuccess) return e;
-    return launch(page_beam_kernel, dim3((G + per - 1u) / per, chunks), block, lds, s, nullptr, a);
+    return launch(few ? page_beam_kernel<true> : page_beam_kernel<false>, dim3((G + per - 1u) / per, chunks), block, lds, s, nullptr, a);
 }
 
 }  // namespace wg

@@ -94,7 +94,7 @@ int wg_page_step(const int32_t *d_table, uint32_t rows, uint32_t columns, const 
         WG_WANT(shift_of(page_tokens), "page_tokens must be 16, 32 or 64");
         WG_WANT((uint64_t)columns * page_tokens <= 0x7FFFFFFFull && (uint64_t)pages * page_tokens <= 0x7FFFFFFFull && tokens <= 0x7FFFFFFFu, "tokens above 2^31 - 1");
         WG_WANT(beams && beams <= kBeamMax && rows % beams == 0, "beams must be 1 .. 64 and divide rows");
-        WG_WANT(!d_parents || columns <= 65535u * 128u, "columns above 8388480 with parents");
+        WG_WANT(!d_parents || columns <= 65535u * 32u, "columns above 2097120 with parents");
         WG_WANT(d_parents || beams == 1u, "beams without parents");
         WG_WANT(!d_parents || d_table != d_table_out, "rows that follow parents must not be written in place");
         WG_WANT(d_lens != d_lens_out && d_counters != d_counters_out, "lengths and counters must not be written in place");

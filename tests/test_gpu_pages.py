@@ -138,7 +138,7 @@ def test_rows_without_beams(R, P, M, in_place):
 
 
 @pytest.mark.parametrize("K,G,P,M", [(1, 5, 16, 20), (2, 3, 16, 12), (4, 20, 16, 40), (5, 7, 32, 20), (8, 64, 16, 30), (64, 2, 16, 12), (3, 200, 16, 10), (8, 3, 16, 700),
-                                     (40, 3, 16, 300), (2, 700, 16, 6)])
+                                     (40, 3, 16, 300), (2, 700, 16, 6), (9, 3, 16, 290), (16, 5, 32, 130), (17, 4, 16, 70), (32, 3, 16, 65), (33, 3, 16, 33), (64, 2, 16, 100)])
 def test_beams_follow_their_parents(K, G, P, M):
     torch, wg = _wg()
     rng = np.random.default_rng(K * 100 + G)

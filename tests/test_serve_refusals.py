@@ -41,7 +41,7 @@ def test_reorder_rows():
 
 def test_page_step():
     need = wg.page_step_workspace(8, 4, 10)
-    assert need == 2 * (8 + 8) + 8 * 4 and wg.page_step_workspace(8, 0, 10) == 0 and wg.page_step_workspace(64, 64, 300) == 8 + 3 * 8 + 64 * 4
+    assert need == 2 * (8 + 8) + 8 * 4 and wg.page_step_workspace(8, 0, 10) == 0 and wg.page_step_workspace(64, 64, 300) == 8 + 10 * 8 + 64 * 4
     good = dict(table=P, rows=8, columns=10, lens=P, counts=P, parents=P, beams=4, page=16, ring=P, pages=100, counters=P, table_out=Q, lens_out=Q, starts=Q, slots=Q,
                 positions=Q, origins=Q, tokens=8, counters_out=Q, work=Q, bytes=need, stream=None)
     refused("wg_page_step", "wg_page_step", good, [
