@@ -210,14 +210,15 @@ beam_merge_kernel(const unsigned long long *__restrict__ lists, const PartSum *_
     const uint32_t tid = threadIdx.x, row0 = blockIdx.x * K, n = K * parts * K, entries = K * parts;
     const unsigned long long *list = lists + (size_t)row0 * (parts * K);
     const PartSum *sum = sums + (size_t)row0 * parts;
-    const bool staged = entries <= kMergeSums, held = n <= kMergeHeld * kMergeThreads;
+    const bool staged = entries <= kMergeSums;
+    constexpr uint32_t kRound = kMergeHeld * kMergeThreads;
     // The i-th key: in order of rank, the lists' best first.  The wavefronts take them in turn, so that each has as many good ones as another and few reach the bound.  (List by list, a
     // wavefront had some rows only, and where those were bad all keys were ranked: 27 us for 32 requests of eight beams.)
     const uint32_t place = (tid & 63u) * kMergeWaves + (tid >> 6);
     auto list_at = [&](uint32_t i) { return i % entries * K + i / entries; };
     unsigned long long key[kMergeHeld];
 #pragma unroll
-    for (uint32_t q = 0; q < kMergeHeld; q++) key[q] = held && place + q * kMergeThreads < n ? list[list_at(place + q * kMergeThreads)] : 0ull;
+    for (uint32_t q = 0; q < kMergeHeld; q++) key[q] = place + q * kMergeThreads < n ? list[list_at(place + q * kMergeThreads)] : 0ull;
     for (uint32_t i = tid; staged && i < entries; i += kMergeThreads) part[i] = sum[i];
     if (tid < K) {
         row_score[tid] = scores[row0 + tid];
@@ -252,16 +253,26 @@ beam_merge_kernel(const unsigned long long *__restrict__ lists, const PartSum *_
     auto raise = [&](unsigned long long r) { const uint32_t high = (uint32_t)(r >> 32); own = high > own ? high : own; };
 #pragma unroll
     for (uint32_t q = 0; q < kMergeHeld; q++) { rank[q] = rank_at(place + q * kMergeThreads, key[q]); raise(rank[q]); }
-    for (uint32_t i = place; !held && i < n; i += kMergeThreads) raise(rank_at(i, list[list_at(i)]));
     const uint32_t bound = bound_of_some<kMergeWaves>(own, K, least);
     auto put = [&](unsigned long long r, unsigned long long k) {
-        if (!r || (uint32_t)(r >> 32) < bound) return;
+        if (!r || (uint32_t)(r >> 32) < bound) return false;
         const uint32_t at = atomicAdd(&n_cand, 1u);
         if (at < kMergeCand) { cand[at] = r; cand_key[at] = k; }
+        return true;
     };
 #pragma unroll
     for (uint32_t q = 0; q < kMergeHeld; q++) put(rank[q], key[q]);
-    for (uint32_t i = place; !held && i < n; i += kMergeThreads) { const unsigned long long k = list[list_at(i)]; put(rank_at(i, k), k); }
+    // The others, of requests with many beams, a round of keys at a time.  A list's keys do not get better, so that a rank that reaches the bound in no list ends the search; a
+    // round has a whole rank (the host sees to that).  (With all keys for the bound and all again
+    // against it a request of 64 beams on 32,000 tokens took 110 us, for 27.)
+    for (uint32_t i0 = kRound; i0 < n; i0 += kRound) {
+        bool some = false;
+#pragma unroll
+        for (uint32_t q = 0; q < kMergeHeld; q++) { const uint32_t i = i0 + place + q * kMergeThreads; key[q] = i < n ? list[list_at(i)] : 0ull; }
+#pragma unroll
+        for (uint32_t q = 0; q < kMergeHeld; q++) some |= put(rank_at(i0 + place + q * kMergeThreads, key[q]), key[q]);
+        if (!__syncthreads_or(some)) break;
+    }
     __syncthreads();
     uint32_t c = n_cand;
     if (c > kMergeCand) {
@@ -313,9 +324,11 @@ beam_merge_kernel(const unsigned long long *__restrict__ lists, const PartSum *_
 }
 
 // Workgroups of a row: about eight per compute unit in all, with at least 2,048 tokens each.  A multiple of eight where it can be: workgroups go to the chip's eight XCDs in turn, and
-// each then has its share of every row, however the rows' masks differ.  The merge's keys stay within what its threads hold, or 8 parts.
+// each then has its share of every row, however the rows' masks differ.  The merge's keys stay within what its threads hold, or 8 parts, which leaves two ranks of a
+// request's lists to a round of them.
 uint32_t beam_parts(uint32_t rows, uint32_t V, uint32_t K)
 {
+    static_assert(2u * 8u * kBeamMax <= kMergeHeld * kMergeThreads, "a round of the merge has a whole rank");
     const uint32_t most = (V + 2047u) / 2048u, want = 2048u / rows < 8u ? 8u : 2048u / rows, held = kMergeHeld * kMergeThreads / (K * K), room = held < 8u ? 8u : held;
     uint32_t parts = want < most ? want : most;
     if (parts > room) parts = room;

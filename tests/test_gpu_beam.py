@@ -131,6 +131,21 @@ def test_the_best_continuations(G, K, V, masked, dtype):
     check(call.host(), states, call.states.cpu().numpy(), want, s, K, exact_ids=dtype == "f32" and apart(want, s, K))
 
 
+@pytest.mark.parametrize("K,V", [(64, 40000), (33, 16500), (20, 100003), (17, 20000)])
+def test_many_beams_whose_best_come_from_one_place(K, V):
+    """All of a request's continuations out of one beam's neighbouring tokens, out of one beam, and out of all alike."""
+    torch, wg = _wg()
+    x, allowed, scores, rng = data(K, 3, K, V, "f32")
+    x[K // 2, 700:700 + 2 * K] += 30 + np.arange(2 * K, dtype=np.float32) / 8
+    scores[K + 3] += 60
+    scores[2 * K:] = -7.0
+    want, s = definition(x.astype(np.float64), allowed, scores.astype(np.float64), K)
+    states = rng.integers(1, 1 << 30, (3 * K, 2)).astype(np.int32)
+    call = Call(torch, wg, 3 * K, V, K)
+    call.run(device_logits(torch, x, "f32"), None, torch.from_numpy(scores).cuda(), torch.from_numpy(states).cuda())
+    check(call.host(), states, call.states.cpu().numpy(), want, s, K, exact_ids=apart(want, s, K))
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_rows_anywhere_in_memory_and_on_another_stream(dtype):
     torch, wg = _wg()
