@@ -255,7 +255,7 @@ __device__ __forceinline__ void append_one(const AppendArgs &a, const Run &run, 
 
 constexpr uint32_t kAppendWaves = 4;
 template <uint32_t kD>
-__global__ void __launch_bounds__(kAppendWaves * 64u) __attribute__((amdgpu_waves_per_eu(4)))
+__global__ void __launch_bounds__(kAppendWaves * 64u) __attribute__((amdgpu_waves_per_eu(kD == 256u ? 3 : 4)))
 append_kernel(const AppendArgs a)
 {
     const uint32_t lane = threadIdx.x & 63u, P = 1u << a.shift, first = blockIdx.x * 64u, t = first + lane;
@@ -279,7 +279,7 @@ append_kernel(const AppendArgs a)
         const uint32_t follow = ~rest ? (uint32_t)__builtin_ctzll(~rest) : 64u;
         const uint32_t s = __builtin_amdgcn_readlane(slot, at), from = __builtin_amdgcn_readlane(origin, at), page = s >> a.shift;
         const Run run{first + at, page, from < a.pages ? from : page, s & (P - 1u), follow + 1u};
-        if (run.n == 1u) {
+        if (__builtin_expect(run.n == 1u, 0)) {      // (what there are no registers for then waits in this branch, not in the other: 11,000 tokens of prompts 21.2 us without, 19.4 with)
             if (which) append_one<kD, true>(a, run, h);
             else append_one<kD, false>(a, run, h);
         } else if (which) append_run<kD, true>(a, run, h);
