@@ -3,7 +3,7 @@
 //
 // Values lie transposed so that both products of attention find what a lane multiplies in one piece: with scores as S^T = K Q^T (rows: keys), the lane that
 // holds the scores of some keys after the first product is the one that needs their weights in the second, O^T = V^T P^T.  Nothing is exchanged between lanes
-// in between, and no LDS is used but to join wavefronts.
+// in between.
 #include <hip/hip_runtime.h>
 
 #include <cfloat>
@@ -58,7 +58,8 @@ __device__ __forceinline__ float scale_for(float top)
 // A wavefront looks at 64 tokens' slots and at the 64 behind them, a lane each, and finds the runs that begin among the first by ballots: prompts have few of them, rows
 // that take a token each have 64.  (A wavefront for every token, head and kind, of which all but those of first tokens left at once, took 99 us for 11,000 tokens
 // of prompts, 8 heads of 128.)  Runs are dealt out to as many wavefronts as the chip holds.  A run's numbers are read twice, the second time out of the
-// caches: held in registers they cost half of the wavefronts, and time.
+// caches: held in registers they cost half of the wavefronts, and time.  Bound by memory where there are many: those tokens take 21.7 us, 75 MB at 3.5 TB/s; a token for each of
+// 256 rows, with forks among them, 6.1, a launch and four trips to memory.  Half or twice as many wavefronts change that by less than 2 us.
 struct AppendArgs {
     const uint16_t *x[2];                            // keys, values: [token][head][dim]
     int64_t token_stride[2], head_stride[2];         // elements
@@ -306,6 +307,9 @@ hipError_t launch_cache_append(const void *k, const void *v, uint32_t tokens, ui
 // summand of the scores, log2(vs), so that the running maximum is that of what the weights are with it; the sum takes them without, times 1 / vs.  Weights are then at most 1,
 // whatever the scales, and go into the second product as float16, up to 2^14: 11 bits of precision down to 2^-28 of the largest.  (In bfloat16 they had 8,
 // which was as large an error as the output's own rounding.)
+//
+// Bound by memory: a token for each of 128 rows of 2,000 to 8,000 tokens, 28 query heads over 4 of 128, 148 us with the join (677 MB, 4.6 TB/s; a copy reaches 5.0); one of 30,000 tokens, 32 over 8,
+// 17 us, of which the join, a launch and the shares' own join are 5.
 //
 // Lane l of a wavefront holds, of 64 keys: of K, for m = l % 16, key (m / 4) * 16 + u * 8 + t * 4 + m % 4 in tile (u, t), of every 64 dims those of its quarter l / 16;
 // after S^T of tile (u, t), the scores of query l % 16 and the keys (l / 16) * 16 + u * 8 + t * 4 + 0 .. 3; of V, for dim l % 16 of 16, the keys
@@ -681,6 +685,10 @@ attend_join_kernel(const AttendArgs a)
 //
 // The running maximum is not followed from block to block: weights are relative to a base, and that moves only where one of them leaves float16's
 // range, which their sum shows, to put the largest at 2^8.
+//
+// 2,000 tokens each of 4 prompts behind up to 2,048, 32 query heads over 8 of 128: 229 us, 873 TFLOP/s (a large library product in bfloat16: 1,313).  The vector unit is busy for 59 % of the
+// cycles and the matrix unit for 39: the two wavefronts of a SIMD hardly get to use both at once.  One tile of rows and three or four wavefronts to a SIMD took 1.1 times as
+// long, four tiles and one wavefront 2.3 times.
 //
 // In LDS keys and values lie as in their pages, but for the places of the sixteen bytes of a row: eight lanes that read together find eight different ones.
 typedef int Int8 __attribute__((ext_vector_type(8)));

@@ -9,6 +9,8 @@
 //
 // A row's new table is its parent's whole one, so that within a request a page is referred to at one place of the tables only, and an old row with a
 // child keeps all of its pages but for a begun one that all of its children copy.  Only what lies in the tables of rows without children is compared.
+//
+// 256 rows without parents 3.9 us; 64 requests of eight beams with 1,024 columns 6.0 and 11.2 (2.6 MB read and written: 0.5 us of a copy).
 #include <hip/hip_runtime.h>
 
 #include "wg_launch.h"
