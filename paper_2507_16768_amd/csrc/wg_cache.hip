@@ -57,9 +57,10 @@ __device__ __forceinline__ float scale_for(float top)
 //
 // A wavefront looks at 64 tokens' slots and at the 64 behind them, a lane each, and finds the runs that begin among the first by ballots: prompts have few of them, rows
 // that take a token each have 64.  (A wavefront for every token, head and kind, of which all but those of first tokens left at once, took 99 us for 11,000 tokens
-// of prompts, 8 heads of 128.)  Runs are dealt out to as many wavefronts as the chip holds.  A run's numbers are read twice, the second time out of the
-// caches: held in registers they cost half of the wavefronts, and time.  Bound by memory where there are many: those tokens take 21.7 us, 75 MB at 3.5 TB/s; a token for each of
-// 256 rows, with forks among them, 6.1, a launch and four trips to memory.  Half or twice as many wavefronts change that by less than 2 us.
+// of prompts, 8 heads of 128.)  Runs are dealt out to as many wavefronts as the chip holds.  A run's numbers are looked at twice, the second time out of LDS, or
+// of the caches where a run is longer than 8 KB (60,000 tokens 84 us, all out of the caches 96, where 79 MB were read for 50; held in registers 108, for half of the wavefronts).  Those
+// 11,000 tokens take 20.7 us, 75 MB at 3.7 TB/s: each run waits for its loads, its largest magnitude and its stores one after the other; a token for each of
+// 256 rows, with forks among them, 6.4, a launch and four trips to memory.  Half or twice as many wavefronts change that by less than 2 us.
 struct AppendArgs {
     const uint16_t *x[2];                            // keys, values: [token][head][dim]
     int64_t token_stride[2], head_stride[2];         // elements
@@ -78,8 +79,10 @@ constexpr uint32_t kFar = 0xF0000000u;
 // Where a run's tokens go: tokens o .. o + n of a page, behind `o` earlier ones that lie in page `source`.
 struct Run { uint32_t token, page, source, o, n; };
 
-template <uint32_t kD, bool kValues>
-__device__ __forceinline__ void append_run(const AppendArgs &a, const Run &run, uint32_t h)
+// kStash: a run is 8 KB at the most, and the wavefront keeps them in LDS, each lane its own words, for the second pass.
+constexpr uint32_t kStashWords = 2048;
+template <uint32_t kD, bool kValues, bool kStash>
+__device__ __forceinline__ void append_run(const AppendArgs &a, const Run &run, uint32_t h, uint32_t *stash)
 {
     constexpr uint32_t kWhich = kValues ? 1u : 0u;
     constexpr uint32_t kLanes = kD / 8u, kTokens = 64u / kLanes;           // keys: eight dims to a lane, so many tokens to a load
@@ -106,6 +109,14 @@ __device__ __forceinline__ void append_run(const AppendArgs &a, const Run &run, 
         else
             for (uint32_t i = 0; i < kWords; i++) w[i] = __builtin_amdgcn_raw_buffer_load_b32(win, at + 4u * i, 0, 0);
     };
+    // what the first pass has put aside, or the same load once more
+    auto again_at = [&](uint32_t token, uint32_t (&w)[kLoadWords]) {
+        if (!kStash) { load(token, w); return; }
+        const bool there = token < n;
+        const uint32_t at = ((there ? token / kLoadTokens : 0u) * 64u + lane) * kLoadWords;
+#pragma unroll
+        for (uint32_t k = 0; k < kLoadWords; k++) w[k] = there ? stash[at + k] : 0u;
+    };
     const float was = o ? a.scale[kWhich][(size_t)run.source * a.heads + h] : 0.f;
     constexpr uint32_t kRound = kValues ? 16u : 4u;                        // loads in flight together
     float top = 0.f;
@@ -118,6 +129,12 @@ __device__ __forceinline__ void append_run(const AppendArgs &a, const Run &run, 
         for (uint32_t j = 0; j < kRound; j++)
 #pragma unroll
             for (uint32_t k = 0; k < kLoadWords; k++) { top = top_of(top, low(w[j][k])); top = top_of(top, high(w[j][k])); }
+        if (kStash)
+#pragma unroll
+            for (uint32_t j = 0; j < kRound; j++)
+                if (i + j * kLoadTokens < n)
+#pragma unroll
+                    for (uint32_t k = 0; k < kLoadWords; k++) stash[((i / kLoadTokens + j) * 64u + lane) * kLoadWords + k] = w[j][k];
     }
 #pragma unroll
     for (int s = 32; s > 0; s >>= 1) top = __builtin_fmaxf(top, __shfl_xor(top, s));
@@ -137,7 +154,7 @@ __device__ __forceinline__ void append_run(const AppendArgs &a, const Run &run, 
         for (uint32_t i = 0; i < n; i += kRound * kLoadTokens) {
             uint32_t w[kRound][kLoadWords];
 #pragma unroll
-            for (uint32_t j = 0; j < kRound; j++) load(i + j * kLoadTokens, w[j]);
+            for (uint32_t j = 0; j < kRound; j++) again_at(i + j * kLoadTokens, w[j]);
 #pragma unroll
             for (uint32_t j = 0; j < kRound; j++) {
                 const uint32_t token = i + j * kLoadTokens + own_token;
@@ -157,7 +174,7 @@ __device__ __forceinline__ void append_run(const AppendArgs &a, const Run &run, 
     for (uint32_t c = begin & ~15u; c < end; c += 16u) {
         uint32_t w[16][kLoadWords];
 #pragma unroll
-        for (uint32_t i = 0; i < 16u; i++) load(c + i - o, w[i]);          // (in front of the run's tokens a number of none, as behind them)
+        for (uint32_t i = 0; i < 16u; i++) again_at(c + i - o, w[i]);          // (in front of the run's tokens a number of none, as behind them)
 #pragma unroll
         for (uint32_t d = 0; d < kOwn; d++) {
             uint8_t *out = to + (size_t)(own_dim + d) * P + c;
@@ -255,10 +272,12 @@ __device__ __forceinline__ void append_one(const AppendArgs &a, const Run &run, 
 }
 
 constexpr uint32_t kAppendWaves = 4;
-template <uint32_t kD>
+template <uint32_t kD, bool kStash>
 __global__ void __launch_bounds__(kAppendWaves * 64u) __attribute__((amdgpu_waves_per_eu(kD == 256u ? 3 : 4)))
 append_kernel(const AppendArgs a)
 {
+    __shared__ __attribute__((aligned(16))) uint32_t stashes[kStash ? kAppendWaves * kStashWords : 1u];
+    uint32_t *stash = stashes + (kStash ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * kStashWords : 0u);
     const uint32_t lane = threadIdx.x & 63u, P = 1u << a.shift, first = blockIdx.x * 64u, t = first + lane;
     const uint32_t none = 0xFFFFFFFFu;
     const uint32_t slot = t < a.tokens ? (uint32_t)a.slots[t] : none, later = t + 64u < a.tokens ? (uint32_t)a.slots[t + 64u] : none;
@@ -280,11 +299,11 @@ append_kernel(const AppendArgs a)
         const uint32_t follow = ~rest ? (uint32_t)__builtin_ctzll(~rest) : 64u;
         const uint32_t s = __builtin_amdgcn_readlane(slot, at), from = __builtin_amdgcn_readlane(origin, at), page = s >> a.shift;
         const Run run{first + at, page, from < a.pages ? from : page, s & (P - 1u), follow + 1u};
-        if (__builtin_expect(run.n == 1u, 0)) {      // (what there are no registers for then waits in this branch, not in the other: 11,000 tokens of prompts 21.2 us without, 19.4 with)
+        if (__builtin_expect(run.n == 1u, 0)) {      // (registers that there is no room for are then put aside in this branch, not in the other: 1.8 us of 21)
             if (which) append_one<kD, true>(a, run, h);
             else append_one<kD, false>(a, run, h);
-        } else if (which) append_run<kD, true>(a, run, h);
-        else append_run<kD, false>(a, run, h);
+        } else if (which) append_run<kD, true, kStash>(a, run, h, stash);
+        else append_run<kD, false, kStash>(a, run, h, stash);
     }
 }
 
@@ -297,7 +316,10 @@ hipError_t launch_cache_append(const void *k, const void *v, uint32_t tokens, ui
     // some 8,192 wavefronts, no more than there can be runs
     const uint32_t blocks = (tokens + 63u) / 64u, want = (2048u + blocks - 1u) / blocks, most = (64u * heads * 2u + kAppendWaves - 1u) / kAppendWaves;
     const dim3 grid(blocks, want < most ? want : most), block(kAppendWaves * 64u);
-    return launch(dim == 64u ? append_kernel<64> : dim == 128u ? append_kernel<128> : append_kernel<256>, grid, block, 0, s, nullptr, a);
+    // (heads of 64, whose runs are half as long, take 11.4 us for 8,000 tokens by reading again and 12.5 with LDS)
+    const bool small = (dim << shift) * 2u <= kStashWords * 4u;
+    return launch(dim == 64u ? append_kernel<64, false> : dim == 128u ? (small ? append_kernel<128, true> : append_kernel<128, false>)
+                  : small ? append_kernel<256, true> : append_kernel<256, false>, grid, block, 0, s, nullptr, a);
 }
 
 // ---------------------------------------------------------------------------------------------
