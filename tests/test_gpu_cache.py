@@ -337,6 +337,16 @@ def test_a_long_prompt(n, P, H, G, D):
     check_attention(out, *attention(cache, x, table, lens, starts, D ** -0.5))
 
 
+@pytest.mark.parametrize("H,G,D,n", [(2, 2, 64, 1), (1, 16, 128, 2), (1, 3, 256, 1)])
+def test_more_rows_than_have_their_keys_cut(H, G, D, n):
+    torch, wg = _wg()
+    rng = np.random.default_rng(D)
+    lens = rng.integers(n, 90, 1100).tolist()
+    cache, table, lens, starts, q = case(10, 16, H, G, D, lens, [n] * len(lens))
+    out, x = run(torch, wg, cache, table, lens, starts, q, D ** -0.5)
+    check_attention(out, *attention(cache, x, table, lens, starts, D ** -0.5))
+
+
 @pytest.mark.parametrize("P,H,G,D", [(16, 64, 2, 64), (32, 64, 2, 128), (64, 32, 2, 256)])
 def test_prompts_that_fill_the_chip(P, H, G, D):
     """Enough of them for no row's keys to be cut."""
