@@ -7,6 +7,7 @@
 #include <hip/hip_runtime.h>
 
 #include <cfloat>
+#include <type_traits>
 
 #include "wg_buffer.h"
 #include "wg_launch.h"
@@ -343,7 +344,7 @@ struct AttendArgs {
     const float *k_scale, *v_scale;
     const int32_t *table, *lens, *starts;
     uint16_t *out;                                   // [token][head][dim]
-    float *partial;                                  // [token][head][split][dim + 2]
+    float *partial;                                  // [token][head][split][dim + 2]: a share's output, what its sum is relative to (log2), its sum
     uint32_t *shares;                                // [token]: shares of its keys
     float scale;                                     // of the scores, times log2(e)
     uint32_t tokens, rows, heads, group, columns, pages, shift, splits, least;
@@ -620,20 +621,20 @@ attend_kernel(const AttendArgs a)
         for (uint32_t d = 0; d < kPer; d++) acc[d] += by * join_o[w][row][d0 + d];
     }
     const size_t at = (size_t)(t.begin + r / a.group) * (a.heads * a.group) + h * a.group + r % a.group;
+    const float by = total > 0.f ? 1.f / total : total == total ? 0.f : total;            // (a row that sees nothing: zeros)
     if (shares > 1u) {
         float *to = a.partial + (at * a.splits + split) * (kD + 2u);
 #pragma unroll
-        for (uint32_t d = 0; d < kPer; d++) to[d0 + d] = acc[d];
+        for (uint32_t d = 0; d < kPer; d++) to[d0 + d] = acc[d] * by;
         if (d0 == 0u) { to[kD] = all; to[kD + 1u] = total; }
         return;
     }
-    const float by = total > 0.f ? 1.f / total : total == total ? 0.f : total;            // (a row that sees nothing: zeros)
 #pragma unroll
     for (uint32_t d = 0; d < kPer; d += 2u) reinterpret_cast<uint32_t *>(a.out + at * kD + d0)[d / 2u] = pk_bf16(acc[d] * by, acc[d + 1u] * by);
 }
 
-// The shares of a token's keys joined: kWaves wavefronts for each query head, all that one reads in flight together.  (A wavefront for a head of 64 shares, four at a time, took 8 us,
-// four take 3.5; for two shares of 28 heads of 128 tokens, 16 us by four wavefronts, 4 by one.)
+// The shares of a token's keys joined, each an output of its own with its sum: kWaves wavefronts for each query head, all that one reads in flight together.  (A wavefront for a
+// head of 64 shares, four at a time, took 8 us, four take 3.5; for two shares of 28 heads of 128 tokens, 16 us by four wavefronts, 4 by one.)
 template <uint32_t kD, uint32_t kWaves>
 __global__ void __launch_bounds__(256)
 attend_join_kernel(const AttendArgs a)
@@ -667,12 +668,12 @@ attend_join_kernel(const AttendArgs a)
 #pragma unroll
     for (uint32_t d = 0; d < kOwn; d++) acc[d] = 0.f;
 #pragma unroll
-    for (uint32_t k = 0; k < kMost; k++) {
-        const float by = __builtin_amdgcn_exp2f(tops[k] - base);
-        l += by * sums[k];
+    for (uint32_t k = 0; k < kMost; k++) { sums[k] *= __builtin_amdgcn_exp2f(tops[k] - base); l += sums[k]; }
+    const float by = l > 0.f ? 1.f / l : l == l ? 0.f : l;
 #pragma unroll
-        for (uint32_t d = 0; d < kOwn; d++) acc[d] += by * v[k][d];
-    }
+    for (uint32_t k = 0; k < kMost; k++)
+#pragma unroll
+        for (uint32_t d = 0; d < kOwn; d++) acc[d] += sums[k] * by * v[k][d];
     if (kWaves > 1u) {
 #pragma unroll
         for (uint32_t d = 0; d < kOwn; d++) part[wave][lane * kOwn + d] = acc[d];
@@ -681,23 +682,22 @@ attend_join_kernel(const AttendArgs a)
         if (wave) return;
         m = __builtin_fmaxf(__builtin_fmaxf(ends[0][0], ends[1][0]), __builtin_fmaxf(ends[2][0], ends[3][0]));
         const float all = m > -__builtin_inff() ? m : 0.f;
-        l = 0.f;
+        float of[4], joined = 0.f;
+#pragma unroll
+        for (uint32_t w = 0; w < 4u; w++) { of[w] = ends[w][1] * __builtin_amdgcn_exp2f(ends[w][0] - all); joined += of[w]; }
+        const float by_all = joined > 0.f ? 1.f / joined : joined == joined ? 0.f : joined;
 #pragma unroll
         for (uint32_t d = 0; d < kOwn; d++) acc[d] = 0.f;
 #pragma unroll
-        for (uint32_t w = 0; w < 4u; w++) {
-            const float by = __builtin_amdgcn_exp2f(ends[w][0] - all);
-            l += by * ends[w][1];
+        for (uint32_t w = 0; w < 4u; w++)
 #pragma unroll
-            for (uint32_t d = 0; d < kOwn; d++) acc[d] += by * part[w][lane * kOwn + d];
-        }
+            for (uint32_t d = 0; d < kOwn; d++) acc[d] += of[w] * by_all * part[w][lane * kOwn + d];
     }
-    const float by = l > 0.f ? 1.f / l : l == l ? 0.f : l;
     uint16_t *out = a.out + at * kD + lane * kOwn;
-    if (kOwn == 1u) out[0] = (uint16_t)pk_bf16(acc[0] * by, 0.f);
+    if (kOwn == 1u) out[0] = (uint16_t)pk_bf16(acc[0], 0.f);
     else
 #pragma unroll
-        for (uint32_t d = 0; d < kOwn; d += 2u) reinterpret_cast<uint32_t *>(out)[d / 2u] = pk_bf16(acc[d] * by, acc[(d + 1u) % kOwn] * by);
+        for (uint32_t d = 0; d < kOwn; d += 2u) reinterpret_cast<uint32_t *>(out)[d / 2u] = pk_bf16(acc[d], acc[(d + 1u) % kOwn]);
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -707,8 +707,11 @@ attend_join_kernel(const AttendArgs a)
 // mantissa: four of them, rounded, are one, the rest is another, 2^5 times as large; with each row brought to its largest in [128, 256) that is exact down to 2^-15 of
 // the row's largest number, and what is smaller is off by 2^-24 of that.  The two products take as long as one in bfloat16 does.
 //
-// The running maximum is not followed from block to block: weights are relative to a base, and that moves only where one of them leaves float16's
-// range, which their sum shows, to put the largest at 2^8.
+// The running maximum is not followed from block to block: the softmax's terms e = 2^(score - base) are relative to a base, and that moves only where they get large, which
+// their sum shows.  The weights in the second product are e * vs * 2^up, with vs the scale of the page's values: `up`, of each query, puts the largest of them at 2^8 where the base
+// moves.  One exp makes a weight, of score - base + lift, lift = log2(vs) + up; the sum is that of the fp32 weights times 2^-lift, which is that of the terms.  Pages of values far below
+// the others (of zeros: they have the least scale) have a lift far below zero; that is held at -80, where a weight of e <= 2^40 is nothing in float16 and a term above 2^-46 is
+// something in fp32.  So the terms keep their sum whatever the scales are.  (Summed as float16 holds them, such pages' keys went missing.)
 //
 // 2,000 tokens each of 4 prompts behind up to 2,048, 32 query heads over 8 of 128: 229 us, 873 TFLOP/s (a large library product in bfloat16: 1,313).  The vector unit is busy for 59 % of the
 // cycles and the matrix unit for 39: the two wavefronts of a SIMD hardly get to use both at once.  One tile of rows and three or four wavefronts to a SIMD took 1.1 times as
@@ -716,7 +719,9 @@ attend_join_kernel(const AttendArgs a)
 //
 // In LDS keys and values lie as in their pages, but for the places of the sixteen bytes of a row: eight lanes that read together find eight different ones.
 typedef int Int8 __attribute__((ext_vector_type(8)));
-constexpr float kRoom = 15.f, kAim = 8.f;            // log2 of the largest weight, and of the largest where the base moves to
+constexpr float kMostSum = 65504.f, kMostTerms = 0x1p40f;    // sums of a lane's sixteen weights, and of what they are without the values' scale, from which on a base moves
+constexpr float kRoom = 11.f, kAim = 8.f;            // log2 of the largest weight that stays where a base moves (sixteen of them are 2^15), and of the largest of the others
+constexpr float kLeastLift = -80.f, kMostLift = 120.f;
 
 // Sixteen bytes c of row `key` of the keys: where they lie in their row.
 template <uint32_t kD>
@@ -740,7 +745,9 @@ attend_wide_kernel(const AttendArgs a)
     constexpr uint32_t kSteps = kD / 32u, kParts = kD / 16u, kRows = kAttendWaves * kTile * kTiles, kThreads = kAttendWaves * 64u;
     static_assert(kRows == wide_rows(kD) && kRows <= kThreads, "as the host counts them");
     static_assert(kAttendWaves == kBlock / 16u, "a wavefront for sixteen keys");
-    constexpr uint32_t kAhead = kD == 256u ? 1u : 2u, kValuesAhead = 4u;         // tiles of keys and parts of values that are asked for in LDS before they are needed
+    constexpr uint32_t kAhead = kD == 256u ? 1u : 2u, kValuesAhead = kD == 64u ? 2u : 4u;         // tiles of keys and parts of values that are asked for in LDS before they are needed (heads
+    // of 64 with four parts: 32 prompts of 64 tokens behind 1,936, 79 us for 58, as what waits in registers is put into memory)
+    typedef std::conditional_t<kD == 256u, uint64_t, uint32_t> Bits;
     constexpr bool kBytes = kD >= 128u;              // scores from 8-bit numbers: products of 128 of them
     constexpr uint32_t kLoads = kD * kBlock / (16u * kThreads);            // sixteen bytes of a thread, of keys and of values each
     __shared__ Word4 keys[2][kD * kBlock / 16u], values[2][kD * kBlock / 16u];
@@ -804,12 +811,12 @@ attend_wide_kernel(const AttendArgs a)
     }
     const uint32_t sees_least = working ? seen_by(t, w0, a.group) : 0u, sees_most = working ? seen_by(t, w0 + kTile * kTiles < t.last ? w0 + kTile * kTiles - 1u : t.last - 1u, a.group) : 0u;
     Float4 o[kTiles][kParts];
-    float base[kTiles], sum[kTiles];
+    float base[kTiles], sum[kTiles], up[kTiles];
     bool begun[kTiles];                              // the lane's query has a base
-    uint64_t nans[kTiles];                           // its outputs that have seen a NaN
+    Bits nans[kTiles];                               // its outputs that have seen a NaN
 #pragma unroll
     for (uint32_t n = 0; n < kTiles; n++) {
-        base[n] = 0.f; sum[n] = 0.f; begun[n] = false; nans[n] = 0ull;
+        base[n] = 0.f; sum[n] = 0.f; up[n] = 0.f; begun[n] = false; nans[n] = 0u;
 #pragma unroll
         for (uint32_t p = 0; p < kParts; p++) o[n][p] = Float4{0.f, 0.f, 0.f, 0.f};
     }
@@ -869,19 +876,22 @@ attend_wide_kernel(const AttendArgs a)
         const uint32_t at = b & 1u, mine = b * kBlock + g * 16u;
         // (a page of zeros may have a scale of zero; what lies behind a row's pages may have any)
         const Float2 scale = scales[at][g];
-        const float ks = scale[0], vs = __builtin_fmaxf(scale[1], 0x1p-64f), v_log = __builtin_amdgcn_logf(vs), v_inverse = __builtin_amdgcn_rcpf(vs);
+        const float ks = scale[0];
+        auto log_of = [](float vs) { return __builtin_amdgcn_logf(__builtin_fmaxf(vs, 0x1p-64f)); };
         Float4 s[kTiles][4];
         Word4 weights[kTiles][2];
         float part[kTiles], by[kTiles], add[kTiles];
+        auto lift_of = [&](uint32_t i, float v_log) { return __builtin_amdgcn_fmed3f(v_log + up[i], kLeastLift, kMostLift); };
 #pragma unroll
-        for (uint32_t i = 0; i < kTiles; i++) { by[i] = ks * q_scale[i]; add[i] = v_log - (begun[i] ? base[i] : 0.f); part[i] = 0.f; }
-        // The weights of four keys, and their sum out of the numbers that the product takes.
+        for (uint32_t i = 0; i < kTiles; i++) { by[i] = ks * q_scale[i]; add[i] = lift_of(i, log_of(scale[1])) - base[i]; part[i] = 0.f; }
+        // The weights of four keys, and their sum.
         auto weigh = [&](uint32_t i, uint32_t n) {
 #pragma unroll
             for (uint32_t e = 0; e < 2u; e++) {
-                const uint32_t two = pk_f16(__builtin_amdgcn_exp2f(s[i][n][2u * e]), __builtin_amdgcn_exp2f(s[i][n][2u * e + 1u]));
-                part[i] = __builtin_amdgcn_fdot2(__builtin_bit_cast(Short2, two), Short2{(_Float16)1.f, (_Float16)1.f}, part[i], false);
-                weights[i][n / 2u][n % 2u * 2u + e] = two;
+                const float x = __builtin_amdgcn_exp2f(s[i][n][2u * e]), y = __builtin_amdgcn_exp2f(s[i][n][2u * e + 1u]);
+                part[i] += x;
+                part[i] += y;
+                weights[i][n / 2u][n % 2u * 2u + e] = pk_f16(x, y);
             }
         };
         // (weights of four keys while the products of the next four are under way)
@@ -934,32 +944,52 @@ attend_wide_kernel(const AttendArgs a)
         Word4 words[kParts];
 #pragma unroll
         for (uint32_t p = 0; p < kValuesAhead; p++) words[p] = values[at][p * 64u + value_row];
-        bool moves = false;                          // a sum that is infinite says that the base has to move first
+        float terms[kTiles];                         // sums without the scale
+        bool moves = false;                          // (a NaN says so too)
 #pragma unroll
-        for (uint32_t i = 0; i < kTiles; i++) moves |= !begun[i] || !(part[i] < __builtin_inff());
-        if (__ballot(moves))
+        for (uint32_t i = 0; i < kTiles; i++) {
+            terms[i] = part[i] * __builtin_amdgcn_exp2f(-(add[i] + base[i]));
+            moves |= !begun[i] || !(part[i] <= kMostSum) || !(terms[i] <= kMostTerms);
+        }
+        if (__ballot(moves)) {
+            // (Read again but for heads of 128, where registers have room for it until here: a prompt of 512 tokens behind 7,500, heads of 64, 128 and 256, 86, 99 and 122 us
+            // with it held, 79, 102 and 116 without.)
+            const float v_log = log_of(kD == 128u ? scale[1] : *const_cast<const volatile float *>(reinterpret_cast<const float *>(&scales[at][g]) + 1));
 #pragma unroll
             for (uint32_t i = 0; i < kTiles; i++) {
-                float high = -__builtin_inff();
+                // log2 of the largest term, and of the largest weight (where the lift is held, of what it were without)
+                float term = -__builtin_inff();
 #pragma unroll
                 for (uint32_t n = 0; n < 4u; n++)
 #pragma unroll
-                    for (uint32_t e = 0; e < 4u; e++) high = __builtin_fmaxf(high, s[i][n][e]);
-                high = __builtin_fmaxf(high, __shfl_xor(high, 16));
-                high = __builtin_fmaxf(high, __shfl_xor(high, 32));
-                const bool move = begun[i] ? high > kRoom : high > -__builtin_inff();
-                const float how_much = move ? high - kAim : 0.f, shrink = begun[i] ? __builtin_amdgcn_exp2f(-how_much) : 1.f;
-                base[i] += how_much;
-                begun[i] = begun[i] || move;
-                sum[i] *= shrink;
+                    for (uint32_t e = 0; e < 4u; e++) term = __builtin_fmaxf(term, s[i][n][e]);
+                const float was = add[i] + base[i];
+                term -= was;
+                float weight = term + (v_log + up[i]);
+                term = __builtin_fmaxf(term, __shfl_xor(term, 16));
+                weight = __builtin_fmaxf(weight, __shfl_xor(weight, 16));
+                term = __builtin_fmaxf(term, __shfl_xor(term, 32));
+                weight = __builtin_fmaxf(weight, __shfl_xor(weight, 32));
+                // the base goes to the largest term, so that none is above 1; weights follow that, but for those that have to come down
+                const bool some = term > -__builtin_inff();
+                const float by_base = begun[i] ? __builtin_fmaxf(term, 0.f) : some ? term : 0.f;
+                const float by_weight = weight > (begun[i] ? kRoom : -__builtin_inff()) ? weight - kAim : 0.f;
+                sum[i] *= begun[i] ? __builtin_amdgcn_exp2f(-by_base) : 1.f;
+                const float shrink = begun[i] ? __builtin_amdgcn_exp2f(-by_weight) : 1.f;
 #pragma unroll
                 for (uint32_t p = 0; p < kParts; p++) o[i][p] *= shrink;
+                base[i] += by_base;
+                up[i] += by_base - by_weight;
+                begun[i] = begun[i] || some;
+                const float lift = lift_of(i, v_log), change = lift - was - by_base;
                 part[i] = 0.f;
 #pragma unroll
-                for (uint32_t n = 0; n < 4u; n++) { s[i][n] -= how_much; weigh(i, n); }
+                for (uint32_t n = 0; n < 4u; n++) { s[i][n] += change; weigh(i, n); }
+                terms[i] = part[i] * __builtin_amdgcn_exp2f(-lift);
             }
+        }
 #pragma unroll
-        for (uint32_t i = 0; i < kTiles; i++) sum[i] = __builtin_fmaf(part[i], v_inverse, sum[i]);
+        for (uint32_t i = 0; i < kTiles; i++) sum[i] += terms[i];
         const uint32_t there = !kEdge ? 16u : mine >= len ? 0u : len - mine < 16u ? len - mine : 16u;
         bool nan = false;
 #pragma unroll
@@ -986,7 +1016,7 @@ attend_wide_kernel(const AttendArgs a)
             for (uint32_t p = 0; p < kParts; p++) {
                 const Word4 v = first_bytes(values[at][p * 64u + value_row], there);
 #pragma unroll
-                for (uint32_t i = 0; i < kTiles; i++) nans[i] |= (uint64_t)nans_seen(v, mine >= sees[i] ? 0u : sees[i] - mine < 16u ? sees[i] - mine : 16u) << (4u * p);
+                for (uint32_t i = 0; i < kTiles; i++) nans[i] |= (Bits)nans_seen(v, mine >= sees[i] ? 0u : sees[i] - mine < 16u ? sees[i] - mine : 16u) << (4u * p);
             }
     };
     if (b0 < blocks) {
@@ -1020,26 +1050,20 @@ attend_wide_kernel(const AttendArgs a)
         const uint32_t r = w0 + i * kTile + m;
         if (r >= t.last) continue;
         const size_t row = (size_t)(t.begin + r / a.group) * (a.heads * a.group) + h * a.group + r % a.group;
+        const float by = total > 0.f ? 1.f / total : total == total ? 0.f : total, down = __builtin_amdgcn_exp2f(-up[i]);      // (a row that sees nothing: zeros)
+        auto out_at = [&](uint32_t p, uint32_t e) { return nans[i] >> (4u * p + e) & 1u ? __builtin_nanf("") : o[i][p][e] * by * down; };
         if (shares > 1u) {
             float *to = a.partial + (row * a.splits + split) * (kD + 2u);
 #pragma unroll
             for (uint32_t p = 0; p < kParts; p++)
 #pragma unroll
-                for (uint32_t e = 0; e < 4u; e += 2u)
-                    *reinterpret_cast<Float2 *>(to + p * 16u + g * 4u + e) =
-                        Float2{nans[i] >> (4u * p + e) & 1u ? __builtin_nanf("") : o[i][p][e], nans[i] >> (4u * p + e + 1u) & 1u ? __builtin_nanf("") : o[i][p][e + 1u]};
+                for (uint32_t e = 0; e < 4u; e += 2u) *reinterpret_cast<Float2 *>(to + p * 16u + g * 4u + e) = Float2{out_at(p, e), out_at(p, e + 1u)};
             if (g == 0u) *reinterpret_cast<Float2 *>(to + kD) = Float2{begun[i] ? base[i] : -__builtin_inff(), total};
             continue;
         }
-        const float by = total > 0.f ? 1.f / total : total == total ? 0.f : total;           // (a row that sees nothing: zeros)
         uint16_t *out = a.out + row * kD + g * 4u;
 #pragma unroll
-        for (uint32_t p = 0; p < kParts; p++) {
-            float x[4];
-#pragma unroll
-            for (uint32_t e = 0; e < 4u; e++) x[e] = nans[i] >> (4u * p + e) & 1u ? __builtin_nanf("") : o[i][p][e] * by;
-            *reinterpret_cast<Word2 *>(out + p * 16u) = Word2{pk_bf16(x[0], x[1]), pk_bf16(x[2], x[3])};
-        }
+        for (uint32_t p = 0; p < kParts; p++) *reinterpret_cast<Word2 *>(out + p * 16u) = Word2{pk_bf16(out_at(p, 0u), out_at(p, 1u)), pk_bf16(out_at(p, 2u), out_at(p, 3u))};
     }
 }
 

@@ -520,3 +520,65 @@ def test_weights_that_are_small_beside_the_largest():
         scale = float(np.log(2.0))
         out, x = run(torch, wg, cache, table, lens, starts, q, scale)
         check_attention(out, *attention(cache, x, table, lens, starts, scale))
+
+
+# ---- pages whose values differ in scale ---------------------------------------------------------
+# A weight is held as float16 and with it the scale of its page's values, the largest of a query at 2^8 or more: what is below 2^-25 is lost from the products, and with
+# n keys of at most 448 that is n * 448 * 2^-25 beside 2^8 times the largest key's own value: below 2^-15 of the sum of magnitudes for the thousands of keys here, whose
+# values are 2^4 on average.  The sum of the weights is fp32 and loses nothing.  The bounds above hold as they are.
+SMALL = {"zeros": (2.0 ** -64, True), "zeros without a scale": (0.0, True), "far below": (2.0 ** -40, False), "below": (2.0 ** -30, False)}
+
+
+def small_pages(cache, table, r, which, kind, times=1.0):
+    """Some of row r's pages have values of zero, or of a scale far below the others'."""
+    scale, zeros = SMALL[kind]
+    for j in which:
+        p = table[r, j]
+        if zeros:
+            cache.v[p] = 0
+        cache.vs[p] = scale * times
+
+
+def places(n, where):
+    """The first pages, the last ones, every other one, all but one."""
+    return {"first": range(n // 2), "last": range(n // 2, n), "every other": range(1, n, 2), "all but one": [j for j in range(n) if j != 1]}[where]
+
+
+@pytest.mark.parametrize("where", ["first", "last", "every other", "all but one"])
+@pytest.mark.parametrize("kind", list(SMALL))
+@pytest.mark.parametrize("P,H,G,D", [(16, 1, 4, 64), (32, 2, 2, 128), (64, 1, 4, 256), (16, 1, 4, 128)])
+def test_prompts_over_pages_of_small_values(P, H, G, D, kind, where):
+    torch, wg = _wg()
+    lens, news = [300, 200, 130], [190, 70, 130]
+    cache, table, lens, starts, q = case(11, P, H, G, D, lens, news)
+    cache.vs[cache.vs > 0] = 2.0 ** -4
+    for r, L in enumerate(lens):
+        small_pages(cache, table, r, places(-(-int(L) // P), where), kind)
+    out, x = run(torch, wg, cache, table, lens, starts, q, D ** -0.5)
+    check_attention(out, *attention(cache, x, table, lens, starts, D ** -0.5))
+
+
+@pytest.mark.parametrize("where", ["last", "all but one"])
+@pytest.mark.parametrize("P,H,G,D", [(16, 2, 4, 64), (32, 1, 12, 128), (64, 1, 5, 256)])
+def test_prompts_behind_long_rows_of_small_values(P, H, G, D, where):
+    """The same where a row's keys are cut: shares of zeros alone are among them."""
+    torch, wg = _wg()
+    lens, news = [5000, 1090, 70], [61, 66, 50]
+    cache, table, lens, starts, q = case(12, P, H, G, D, lens, news)
+    assert wg.cache_attend_workspace(q.shape[0], len(lens), H * G, H, D, table.shape[1], P) > 0
+    for r, L in enumerate(lens):
+        small_pages(cache, table, r, places(-(-int(L) // P), where), "zeros")
+    out, x = run(torch, wg, cache, table, lens, starts, q, D ** -0.5)
+    check_attention(out, *attention(cache, x, table, lens, starts, D ** -0.5))
+
+
+def test_a_prompt_and_single_tokens_agree():
+    """The last token of a prompt over pages of zeros, by itself and among the prompt's."""
+    torch, wg = _wg()
+    cache, table, lens, starts, q = case(13, 16, 1, 4, 128, [160], [160])
+    small_pages(cache, table, 0, range(4, 10), "zeros")
+    whole, x = run(torch, wg, cache, table, lens, starts, q, 0.1)
+    alone, _ = run(torch, wg, cache, table, lens, np.array([0, 1], np.int32), q[-1:], 0.1)
+    want, size = attention(cache, x, table, lens, starts, 0.1)
+    check_attention(whole, want, size)
+    check_attention(alone, want[-1:], size[-1:])
