@@ -326,10 +326,11 @@ hipError_t launch_cache_append(const void *k, const void *v, uint32_t tokens, ui
 // ---------------------------------------------------------------------------------------------
 // attention.  A tile is 16 query rows of a request and a cached head: its tokens times the query heads that share the head.  A workgroup takes a share of a
 // tile's keys, its wavefronts 64 keys at a time in turn: 16 bytes to a lane and load straight into registers, turned into bfloat16 there (exactly), scores,
-// a running maximum and sum, weights, weighted values.  A page's scales multiply scores and weights, not its values: that of its values as a
-// summand of the scores, log2(vs), so that the running maximum is that of what the weights are with it; the sum takes them without, times 1 / vs.  Weights are then at most 1,
-// whatever the scales, and go into the second product as float16, up to 2^14: 11 bits of precision down to 2^-28 of the largest.  (In bfloat16 they had 8,
-// which was as large an error as the output's own rounding.)
+// a running maximum and sum, weights, weighted values.  A page's scales multiply scores and weights, not its values.  There are two running maxima for it: `top` of the scores,
+// which the softmax's terms e = 2^(score - top) and their sum are relative to, and `most` of score + log2(vs), of what the weights e * vs are with the scale of their page's values.
+// Weights go into the second product as float16, the largest at 2^14: 11 bits of precision down to 2^-28 of the largest.  (In bfloat16 they had 8,
+// which was as large an error as the output's own rounding.)  One exp makes a weight, of score - top + lift, with lift = log2(vs) + top - most + 14 of the page; the sum is that of the
+// fp32 weights times 2^-lift.  Far below the others, as a page of zeros, which has the least scale, a lift is held at -80: such a weight is nothing in float16 and something in the sum.
 //
 // Bound by memory: a token for each of 128 rows of 2,000 to 8,000 tokens, 28 query heads over 4 of 128, 148 us with the join (677 MB, 4.6 TB/s; a copy reaches 5.0); one of 30,000 tokens, 32 over 8,
 // 17 us, of which the join, a launch and the shares' own join are 5.
@@ -351,6 +352,7 @@ struct AttendArgs {
 };
 constexpr uint32_t kAttendWaves = 4, kBlock = 64, kTile = 16;
 constexpr float kHeadroom = 14.f;                    // weights go up to 2^14
+constexpr float kLeastLift = -80.f, kMostLift = 120.f;       // (above: of terms below 2^-104)
 constexpr uint32_t kLeastBlocks = 16, kFewRows = 8192;       // blocks of a share: half as many of prompts with few query rows
 // Shares in all, about (512, 768, 1,024 and 2,048: 64 rows of 2,000 tokens 58, 54, 54 and 54 us, 200 of 1,000 99, 99, 99 and 113); of the kernel for many rows, as many as the chip
 // holds at a time (256, 512 and 1,024: a prompt of 512 tokens behind 7,500 175, 98 and 100 us, 128 query rows of 32 rows of 2,000 tokens 73, 73 and 94).
@@ -490,7 +492,7 @@ attend_kernel(const AttendArgs a)
 {
     constexpr uint32_t kSteps = kD / 32u, kParts = kD / 16u;
     __shared__ float join_o[kAttendWaves][kTile][kD + 4u];
-    __shared__ float join_m[kAttendWaves][kTile], join_l[kAttendWaves][kTile];
+    __shared__ float join_m[kAttendWaves][kTile], join_w[kAttendWaves][kTile], join_l[kAttendWaves][kTile];
     const uint32_t tid = threadIdx.x, lane = tid & 63u, wave = __builtin_amdgcn_readfirstlane(tid >> 6), m = lane & 15u, g = lane >> 4;
     const uint32_t split = blockIdx.z, h = blockIdx.y, P = 1u << a.shift;
     uint32_t len;
@@ -518,7 +520,7 @@ attend_kernel(const AttendArgs a)
     Float4 o[kParts];
 #pragma unroll
     for (uint32_t p = 0; p < kParts; p++) o[p] = Float4{0.f, 0.f, 0.f, 0.f};
-    float top = -__builtin_inff(), sum = 0.f;        // of the lane's query; the sum of the lane's own keys
+    float top = -__builtin_inff(), most = top, sum = 0.f;    // of the lane's query; the sum of the lane's own keys
     for (uint32_t b = b0 + wave; b < b1; b += kAttendWaves) {
         const uint32_t key0 = b * kBlock, mine = key0 + g * 16u, theirs = key0 + (m >> 2) * 16u;
         const uint32_t k_page = page_of(k_next), v_page = page_of(v_next);
@@ -526,7 +528,7 @@ attend_kernel(const AttendArgs a)
         const uint8_t *vp = a.v_cache + (((size_t)v_page * a.heads + h) * kD + m) * P + (mine & (P - 1u));
         const float ks = a.k_scale[(size_t)v_page * a.heads + h] * a.scale;
         // (a page of zeros may have a scale of zero; what lies behind a row's pages may have any)
-        const float vs = __builtin_fmaxf(a.v_scale[(size_t)v_page * a.heads + h], 0x1p-64f), v_log = __builtin_amdgcn_logf(vs), v_inverse = __builtin_amdgcn_rcpf(vs);
+        const float v_log = __builtin_amdgcn_logf(__builtin_fmaxf(a.v_scale[(size_t)v_page * a.heads + h], 0x1p-64f));
         Word4 kw[4][kD / 64u];
 #pragma unroll
         for (uint32_t n = 0; n < 4u; n++)
@@ -550,13 +552,18 @@ attend_kernel(const AttendArgs a)
         for (uint32_t n = 0; n < 4u; n++)
 #pragma unroll
             for (uint32_t e = 0; e < 4u; e++) {
-                s[n][e] = s[n][e] * ks + v_log;
+                s[n][e] *= ks;
                 if (edge && mine + n * 4u + e >= sees) s[n][e] = -__builtin_inff();
                 high = __builtin_fmaxf(high, s[n][e]);
             }
+        float large = high + v_log;
         high = __builtin_fmaxf(high, __shfl_xor(high, 16));
+        large = __builtin_fmaxf(large, __shfl_xor(large, 16));
         high = __builtin_fmaxf(high, __shfl_xor(high, 32));
-        const float next = __builtin_fmaxf(top, high), base = next > -__builtin_inff() ? next - kHeadroom : 0.f;
+        large = __builtin_fmaxf(large, __shfl_xor(large, 32));
+        // (relative to 0 where nothing has been seen: all weights are zero there)
+        const float next = __builtin_fmaxf(top, high), base = next > -__builtin_inff() ? next : 0.f, next_most = __builtin_fmaxf(most, large);
+        const float lift = __builtin_amdgcn_fmed3f(v_log + (next_most > -__builtin_inff() ? base - next_most : 0.f) + kHeadroom, kLeastLift, kMostLift), from = lift - base;
         if (edge) {
             // values behind the row's end are whatever the pages held: they must not be NaN times a weight of zero
             const uint32_t there = mine >= len ? 0u : len - mine < 16u ? len - mine : 16u;
@@ -573,24 +580,26 @@ attend_kernel(const AttendArgs a)
                 vw[p] = clean;
             }
         }
-        if (__ballot(next != top)) {
-            const float shrink = __builtin_amdgcn_exp2f(top - (next > -__builtin_inff() ? next : 0.f));
-            sum *= shrink;
+        if (__ballot(next != top || next_most != most)) {
+            sum *= __builtin_amdgcn_exp2f(top - base);
+            const float shrink = __builtin_amdgcn_exp2f(most - (next_most > -__builtin_inff() ? next_most : 0.f));
 #pragma unroll
             for (uint32_t p = 0; p < kParts; p++) o[p] *= shrink;
         }
-        top = next;
+        top = next; most = next_most;
+        float part = 0.f;
         Short8 weights[2];
 #pragma unroll
         for (uint32_t u = 0; u < 2u; u++) {
             float w[8];
 #pragma unroll
             for (uint32_t e = 0; e < 8u; e++) {
-                w[e] = __builtin_amdgcn_exp2f(s[u * 2u + e / 4u][e % 4u] - base);
-                sum += w[e] * v_inverse;
+                w[e] = __builtin_amdgcn_exp2f(s[u * 2u + e / 4u][e % 4u] + from);
+                part += w[e];
             }
             weights[u] = __builtin_bit_cast(Short8, Word4{pk_f16(w[0], w[1]), pk_f16(w[2], w[3]), pk_f16(w[4], w[5]), pk_f16(w[6], w[7])});
         }
+        sum = __builtin_fmaf(part, __builtin_amdgcn_exp2f(-lift), sum);
 #pragma unroll
         for (uint32_t u = 0; u < 2u; u++)
 #pragma unroll
@@ -600,37 +609,39 @@ attend_kernel(const AttendArgs a)
     sum += __shfl_xor(sum, 16);
     sum += __shfl_xor(sum, 32);
     // the wavefronts' shares joined
-    if (g == 0u) { join_m[wave][m] = top; join_l[wave][m] = sum; }
+    if (g == 0u) { join_m[wave][m] = top; join_w[wave][m] = most; join_l[wave][m] = sum; }
 #pragma unroll
     for (uint32_t p = 0; p < kParts; p++) *reinterpret_cast<Float4 *>(&join_o[wave][m][p * 16u + g * 4u]) = o[p];
     __syncthreads();
     constexpr uint32_t kPer = kTile * kD / (kAttendWaves * 64u);          // neighbouring dims of a thread
     const uint32_t row = tid * kPer / kD, d0 = tid * kPer % kD, r = t.first + row;
     if (r >= t.last) return;
-    float all = -__builtin_inff(), total = 0.f, acc[kPer];
+    float all = -__builtin_inff(), all_most = all, total = 0.f, acc[kPer];
 #pragma unroll
-    for (uint32_t w = 0; w < kAttendWaves; w++) all = __builtin_fmaxf(all, join_m[w][row]);
-    const float base = all > -__builtin_inff() ? all : 0.f;
+    for (uint32_t w = 0; w < kAttendWaves; w++) { all = __builtin_fmaxf(all, join_m[w][row]); all_most = __builtin_fmaxf(all_most, join_w[w][row]); }
+    const float base = all > -__builtin_inff() ? all : 0.f, most_base = all_most > -__builtin_inff() ? all_most : 0.f;
 #pragma unroll
     for (uint32_t d = 0; d < kPer; d++) acc[d] = 0.f;
 #pragma unroll
     for (uint32_t w = 0; w < kAttendWaves; w++) {
-        const float by = __builtin_amdgcn_exp2f(join_m[w][row] - base);
-        total += by * join_l[w][row];
+        total += __builtin_amdgcn_exp2f(join_m[w][row] - base) * join_l[w][row];
+        const float by = __builtin_amdgcn_exp2f(join_w[w][row] - most_base);
 #pragma unroll
         for (uint32_t d = 0; d < kPer; d++) acc[d] += by * join_o[w][row][d0 + d];
     }
     const size_t at = (size_t)(t.begin + r / a.group) * (a.heads * a.group) + h * a.group + r % a.group;
-    const float by = total > 0.f ? 1.f / total : total == total ? 0.f : total;            // (a row that sees nothing: zeros)
+    const float by = total > 0.f ? 1.f / total : total == total ? 0.f : total, up = __builtin_amdgcn_exp2f(most_base - base - kHeadroom);     // (a row that sees nothing: zeros)
+#pragma unroll
+    for (uint32_t d = 0; d < kPer; d++) acc[d] = acc[d] * by * up;
     if (shares > 1u) {
         float *to = a.partial + (at * a.splits + split) * (kD + 2u);
 #pragma unroll
-        for (uint32_t d = 0; d < kPer; d++) to[d0 + d] = acc[d] * by;
+        for (uint32_t d = 0; d < kPer; d++) to[d0 + d] = acc[d];
         if (d0 == 0u) { to[kD] = all; to[kD + 1u] = total; }
         return;
     }
 #pragma unroll
-    for (uint32_t d = 0; d < kPer; d += 2u) reinterpret_cast<uint32_t *>(a.out + at * kD + d0)[d / 2u] = pk_bf16(acc[d] * by, acc[d + 1u] * by);
+    for (uint32_t d = 0; d < kPer; d += 2u) reinterpret_cast<uint32_t *>(a.out + at * kD + d0)[d / 2u] = pk_bf16(acc[d], acc[d + 1u]);
 }
 
 // The shares of a token's keys joined, each an output of its own with its sum: kWaves wavefronts for each query head, all that one reads in flight together.  (A wavefront for a
@@ -721,7 +732,6 @@ attend_join_kernel(const AttendArgs a)
 typedef int Int8 __attribute__((ext_vector_type(8)));
 constexpr float kMostSum = 65504.f, kMostTerms = 0x1p40f;    // sums of a lane's sixteen weights, and of what they are without the values' scale, from which on a base moves
 constexpr float kRoom = 11.f, kAim = 8.f;            // log2 of the largest weight that stays where a base moves (sixteen of them are 2^15), and of the largest of the others
-constexpr float kLeastLift = -80.f, kMostLift = 120.f;
 
 // Sixteen bytes c of row `key` of the keys: where they lie in their row.
 template <uint32_t kD>

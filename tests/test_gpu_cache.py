@@ -582,3 +582,17 @@ def test_a_prompt_and_single_tokens_agree():
     want, size = attention(cache, x, table, lens, starts, 0.1)
     check_attention(whole, want, size)
     check_attention(alone, want[-1:], size[-1:])
+
+
+@pytest.mark.parametrize("where", ["first", "last", "every other", "all but one"])
+@pytest.mark.parametrize("P,H,G,D,lens,news", [(16, 1, 4, 64, [300, 200], [1, 2]), (32, 2, 7, 128, [5000, 300], [1, 1]), (64, 1, 3, 256, [300, 700], [1, 1]),
+                                               (16, 1, 4, 64, [300, 200], [100, 90]), (32, 1, 12, 128, [5000, 70], [61, 50]), (64, 1, 5, 256, [200, 100], [100, 20])])
+def test_pages_of_zeros_beside_very_large_values(P, H, G, D, lens, news, where):
+    """What float32 holds of a scale: 2^90 beside the least one."""
+    torch, wg = _wg()
+    cache, table, lens, starts, q = case(14, P, H, G, D, lens, news)
+    cache.vs[cache.vs > 0] = 2.0 ** 90
+    for r, L in enumerate(lens):
+        small_pages(cache, table, r, places(-(-int(L) // P), where), "zeros")
+    out, x = run(torch, wg, cache, table, lens, starts, q, D ** -0.5)
+    check_attention(out, *attention(cache, x, table, lens, starts, D ** -0.5))
