@@ -419,6 +419,16 @@ __device__ __forceinline__ uint32_t nans_seen(Word4 v, uint32_t seen)
     return (n[0] > 0.f ? 1u : 0u) | (n[1] > 0.f ? 2u : 0u) | (n[2] > 0.f ? 4u : 0u) | (n[3] > 0.f ? 8u : 0u);
 }
 
+// Eight numbers of a query (bfloat16), infinities as NaN: a score that is infinite makes the softmax none, also where all of them are -inf, which would look like a query that sees
+// nothing, and where the numbers are taken in 8 bits, which have no infinity.
+__device__ __forceinline__ Word4 query_words(const uint16_t *q)
+{
+    Word4 v = *reinterpret_cast<const Word4 *>(q);
+#pragma unroll
+    for (uint32_t w = 0; w < 4u; w++) v[w] |= ((v[w] & 0x7F807F80u) + 0x00800080u & 0x80008000u) >> 9;      // (an exponent of ones carries into the sign's place)
+    return v;
+}
+
 // Where a tile of kTile rows lies: the request whose tiles it is among, from the places at which the requests' tokens begin.  Request r's tiles begin at
 // starts[r] * group / kTile + r, which leaves room for each one's last, begun tile.  A wavefront asks 64 requests at a time.
 template <uint32_t kTile>
@@ -510,7 +520,7 @@ attend_kernel(const AttendArgs a)
     const uint16_t *q = a.q + (int64_t)(t.begin + i / a.group) * a.q_token + (int64_t)(h * a.group + i % a.group) * a.q_head;
     Half8 qf[kSteps];
 #pragma unroll
-    for (uint32_t s = 0; s < kSteps; s++) qf[s] = __builtin_bit_cast(Half8, *reinterpret_cast<const Word4 *>(q + s / 2u * 64u + g * 16u + s % 2u * 8u));
+    for (uint32_t s = 0; s < kSteps; s++) qf[s] = __builtin_bit_cast(Half8, query_words(q + s / 2u * 64u + g * 16u + s % 2u * 8u));
     const int32_t *table = a.table + (size_t)t.row * a.columns;
     const uint32_t last_column = a.columns - 1u;
     auto page_at = [&](uint32_t key) { const uint32_t c = key >> a.shift; return (uint32_t)table[c < last_column ? c : last_column]; };
@@ -791,14 +801,14 @@ attend_wide_kernel(const AttendArgs a)
         q_scale[n] = a.scale;
         if (!kBytes) {
 #pragma unroll
-            for (uint32_t k = 0; k < (kBytes ? 1u : kSteps); k++) q_half[n][k] = __builtin_bit_cast(Half8, *reinterpret_cast<const Word4 *>(q + k * 8u));
+            for (uint32_t k = 0; k < (kBytes ? 1u : kSteps); k++) q_half[n][k] = __builtin_bit_cast(Half8, query_words(q + k * 8u));
             continue;
         }
         Word4 raw[kD / 32u];
         float top = 0.f;
 #pragma unroll
         for (uint32_t k = 0; k < kD / 32u; k++) {
-            raw[k] = *reinterpret_cast<const Word4 *>(q + k * 8u);
+            raw[k] = query_words(q + k * 8u);
 #pragma unroll
             for (uint32_t e = 0; e < 4u; e++) { top = top_of(top, low(raw[k][e])); top = top_of(top, high(raw[k][e])); }
         }

@@ -596,3 +596,31 @@ def test_pages_of_zeros_beside_very_large_values(P, H, G, D, lens, news, where):
         small_pages(cache, table, r, places(-(-int(L) // P), where), "zeros")
     out, x = run(torch, wg, cache, table, lens, starts, q, D ** -0.5)
     check_attention(out, *attention(cache, x, table, lens, starts, D ** -0.5))
+
+
+@pytest.mark.parametrize("D", [64, 128, 256])
+@pytest.mark.parametrize("n", [1, 2, 40])
+def test_queries_with_numbers_that_are_none(D, n):
+    """An infinity or a NaN in a query makes its output NaN (infinite scores less their infinite maximum are none) and no other; a query that sees nothing has zeros."""
+    torch, wg = _wg()
+    G, lens = 4, [90, 70, 0, 1500]
+    cache, table, lens, starts, q = case(15, 16, 1, G, D, lens, [n] * len(lens))
+    cache.k[table[1, 0], 0, :, 5] = to_bytes(np.full(16, -2.0))            # numbers of one sign, of both, zeros
+    for j in range(5):
+        cache.k[table[1, j], 0, :, 9] = to_bytes(np.full(16, -1.5))
+        cache.k[table[0, j], 0, :, 9] = 0
+    bad = np.zeros(q.shape[:2], bool)
+    for r, L in enumerate(lens):
+        t = int(starts[r + 1]) - 1
+        q[t, 0, 9], q[t, 1, 9], q[t, 2, 5] = np.inf, -np.inf, np.nan
+        bad[t, :3] = L > 0
+        if n > 2:
+            q[t - 7, 3, D - 1] = np.inf
+            bad[t - 7, 3] = L > 0
+    out, x = run(torch, wg, cache, table, lens, starts, q, D ** -0.5)
+    got = torch.isnan(out).cpu().numpy()
+    assert (got == bad[:, :, None]).all(), np.argwhere(got != bad[:, :, None])[:4].tolist()
+    assert float(out[starts[2]:starts[3]].abs().max()) == 0.0
+    want, size = attention(cache, np.where(np.isfinite(x), x, 0.0), table, lens, starts, D ** -0.5)
+    keep = ~bad
+    check_attention(out[torch.from_numpy(keep).cuda()], want[keep], size[keep])
