@@ -454,7 +454,7 @@ __device__ __forceinline__ uint32_t tokens_of_row(const AttendArgs &a, uint32_t 
     return l < most ? l : most;
 }
 
-struct TileOf { uint32_t row, first, last, begin, count; int32_t before; };      // query rows [first, last) of a request with `count` tokens from `begin` on, behind `before` others
+struct TileOf { uint32_t row, first, last, begin; int32_t before; };      // query rows [first, last) of a request whose tokens are those from `begin` on, behind `before` others
 
 template <uint32_t kTile, bool kLastFirst = false>
 __device__ __forceinline__ bool tile_of(const AttendArgs &a, uint32_t tile, uint32_t *len, TileOf *out)
@@ -464,10 +464,10 @@ __device__ __forceinline__ bool tile_of(const AttendArgs &a, uint32_t tile, uint
     const uint32_t at = tile - ((uint32_t)((uint64_t)b * a.group / kTile) + r), all = (e - b) * a.group;
     *len = tokens_of_row(a, r);
     if (tile < (uint32_t)((uint64_t)b * a.group / kTile) + r || (uint64_t)at * kTile >= all) return false;
-    out->row = r; out->begin = b; out->count = e - b;
+    out->row = r; out->begin = b;
     out->first = (kLastFirst ? (all - 1u) / kTile - at : at) * kTile;
     out->last = all - out->first < kTile ? all : out->first + kTile;
-    out->before = (int32_t)*len - (int32_t)(e - b);
+    out->before = (int32_t)*len - (int32_t)(e0 < b ? 0u : e0 - b);       // (with the row's tokens that the call does not have)
     return true;
 }
 // Shares that a tile's keys are cut into, and the blocks of each: shares of one size, whatever the rows' lengths, so that the workgroups that the chip holds at a time have as

@@ -624,3 +624,14 @@ def test_queries_with_numbers_that_are_none(D, n):
     want, size = attention(cache, np.where(np.isfinite(x), x, 0.0), table, lens, starts, D ** -0.5)
     keep = ~bad
     check_attention(out[torch.from_numpy(keep).cuda()], want[keep], size[keep])
+
+
+@pytest.mark.parametrize("G,D,lens,news,cut", [(4, 128, [300, 200, 90], [100, 80, 90], 130), (4, 64, [300, 200, 90], [100, 80, 90], 37), (2, 256, [90, 300], [64, 200], 100),
+                                               (4, 128, [300, 200], [5, 4], 7), (3, 64, [2000, 300], [3, 2], 2), (12, 128, [5000, 70], [61, 50], 50)])
+def test_fewer_tokens_than_the_rows_take(G, D, lens, news, cut):
+    """The first tokens of a step by themselves: the rows' lengths and starts say where they are, and what they see does not change."""
+    torch, wg = _wg()
+    cache, table, lens, starts, q = case(16, 16, 1, G, D, lens, news)
+    out, x = run(torch, wg, cache, table, lens, starts, q[:cut], D ** -0.5)
+    want, size = attention(cache, bf16(torch, q)[1], table, lens, starts, D ** -0.5)
+    check_attention(out, want[:cut], size[:cut])
