@@ -422,11 +422,10 @@ int wg_cache_append(const void *d_k, const void *d_v, uint32_t tokens, uint32_t 
 /* wg_cache_attend: attention of the tokens of a step over the cache.  d_q, d_out: bfloat16 [tokens][q_heads][dim], d_out without gaps, d_q with
  * strides in elements at multiples of 16 bytes.  Query head j reads cached head j / (q_heads / heads).  Row r has d_lens[r] tokens in the
  * cache, the tokens d_starts[r] .. d_starts[r + 1] of the call being its last ones: token i of n sees the first d_lens[r] - n + i + 1 keys (none: its output is
- * zeros); tokens from d_starts[rows] on belong to no row, and their outputs stay; with fewer
- * tokens than that the first ones see what they see in the whole call.  d_out = sum of values weighted by softmax(scale * q . k).  An infinity or a
- * NaN in a query makes its output NaN.  Sums and the
- * softmax in fp32, products of what bfloat16, float16 and 8 bits hold: the cache's numbers and the queries exactly (where requests have 64 query rows and more on average, and dim
- * is 128 or 256, a query row's numbers below 2^-15 of its largest to 2^-24 of that), the weights rounded to float16.  d_table, d_lens, d_starts: what wg_page_step leaves.  Entries of a table
+ * zeros); tokens from d_starts[rows] on belong to no row, and their outputs stay; with fewer tokens than that the first ones see what they see in
+ * the whole call.  d_out = sum of values weighted by softmax(scale * q . k).  An infinity or a NaN in a query makes its output NaN.  Sums and the softmax in
+ * fp32, products of what bfloat16, float16 and 8 bits hold: the cache's numbers and the queries exactly (where tokens * q_heads / heads is at least 32 * rows, and dim
+ * is 128 or 256, a query row's numbers below 2^-14 of its largest to 2^-22 of that), the weights rounded to float16.  d_table, d_lens, d_starts: what wg_page_step leaves.  Entries of a table
  * behind a row's pages may be anything.  d_workspace: wg_cache_attend_workspace(...) bytes (0: may be NULL), 16-byte aligned, overwritten; calls that
  * share it must not overlap.  heads <= 4095, q_heads <= 65535, rows <= 65535, pages * page_tokens and columns * page_tokens < 2^31, and no more tokens than one launch
  * holds (heads * (tokens * q_heads / heads / 64 + rows) < 2^24).  One or two kernels. */

@@ -725,8 +725,8 @@ attend_join_kernel(const AttendArgs a)
 // attention of many rows of a request: prompts.  A wavefront holds kTiles tiles of 16 query rows, four of them share their keys, 64 at a time, through LDS.  Bound
 // by the vector unit: exp and what goes with it of every score, and the cache's numbers turned into what the products take.  So the keys are not
 // turned into anything: scores come from the product of 8-bit numbers, with the queries as sums of two such numbers.  A bfloat16 number has 8 bits of
-// mantissa: four of them, rounded, are one, the rest is another, 2^5 times as large; with each row brought to its largest in [128, 256) that is exact down to 2^-15 of
-// the row's largest number, and what is smaller is off by 2^-24 of that.  The two products take as long as one in bfloat16 does.
+// mantissa: four of them, rounded, are one, the rest is another, 2^5 times as large; with each row brought to its largest in [128, 256) that is exact for numbers from 2^-7 on,
+// 2^-14 of the row's largest, and what is smaller is off by 2^-15, 2^-22 of that, at the most.  The two products take as long as one in bfloat16 does.
 //
 // The running maximum is not followed from block to block: the softmax's terms e = 2^(score - base) are relative to a base, and that moves only where they get large, which
 // their sum shows.  The weights in the second product are e * vs * 2^up, with vs the scale of the page's values: `up`, of each query, puts the largest of them at 2^8 where the base

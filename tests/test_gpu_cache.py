@@ -635,3 +635,31 @@ def test_fewer_tokens_than_the_rows_take(G, D, lens, news, cut):
     out, x = run(torch, wg, cache, table, lens, starts, q[:cut], D ** -0.5)
     want, size = attention(cache, bf16(torch, q)[1], table, lens, starts, D ** -0.5)
     check_attention(out, want[:cut], size[:cut])
+
+
+def sum_of_two(x):
+    """A row of bfloat16 numbers as the header says that calls with 32 query rows and more to a row of the table take it: the largest in [128, 256), sums of two
+    8-bit numbers, the second 2^-5 of what it is."""
+    e = np.floor(np.log2(np.abs(x).max(-1, keepdims=True))) - 7
+    y = x / 2.0 ** e
+    first = NUMBERS[to_bytes(y)]
+    return (first + NUMBERS[to_bytes((y - first) * 32)] / 32) * 2.0 ** e
+
+
+@pytest.mark.parametrize("D,n", [(128, 8), (256, 16), (128, 7), (64, 8)])
+def test_what_queries_are_rounded_to(D, n):
+    """One large number of a query meets keys of zeros, and its small ones keys that tell what they are: as they are below the limit and for heads of 64, else in two parts."""
+    torch, wg = _wg()
+    cache, table, lens, starts, q = case(17, 16, 1, 4, D, [40, 40], [n, n])
+    cache.k[:, :, :, 0] = 0
+    cache.ks[cache.ks > 0] = 2.0 ** 13
+    q *= 2.0 ** -16
+    q[:, :, 0] = 1.9
+    out, x = run(torch, wg, cache, table, lens, starts, q, D ** -0.5)
+    parts = sum_of_two(x)
+    off = np.abs(parts - x).max()
+    assert 2.0 ** -24 < off <= 2.0 ** -22
+    taken = parts if D != 64 and n * 4 >= 32 else x
+    check_attention(out, *attention(cache, taken, table, lens, starts, D ** -0.5))
+    other, size = attention(cache, x if taken is parts else parts, table, lens, starts, D ** -0.5)
+    assert (np.abs(out.double().cpu().numpy() - other) > 2 * (2.0 ** -8 * size + 2.0 ** -9 * np.abs(other))).any()
