@@ -28,8 +28,10 @@ namespace wg {
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 __device__ __forceinline__ float exp_of(float x) { return __builtin_amdgcn_exp2f(x * kLog2e); }
 
-// What a part leaves besides its keys: +inf counts as the largest number, so that top and every difference from it are finite; sum is in 32 bits (at most
-// V terms of at most 1, in a thousand partial sums: relative error some 1e-6 at the most).
+// What a part leaves besides its keys: +inf counts as the largest number, so that top and every difference from it are finite.  The sum is in 32 bits.  A thread adds up to V / 2,048 + 16
+// terms of at most 1 one after the other (a row has eight parts of 256 threads at the least, or as many as it has 2,048 tokens), rescales their sum for every four or eight of them, and
+// some 50 additions join those of threads, wavefronts and parts.  Each is off by 2^-24 of the sum at the most and an exp by 2^-22, all together by (V / 1,600 + 80) * 2^-24: 1e-5 for
+// 151,936 tokens, 2e-2 for the most that a row may have, where errors all have one sign.
 struct PartSum { float top, sum; };
 
 // (256 threads: the first of these takes 33 us with 512, the third the same)

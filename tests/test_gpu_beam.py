@@ -316,3 +316,18 @@ def test_rows_of_a_larger_array_follow_too():
     wg.reorder_rows(src, parents, dst, axis=1)
     want = src[:, parents.clamp(min=0).long()] * (parents >= 0).int()[None, :, None]
     assert torch.equal(dst, want) and int(out[:, :, :7].abs().sum()) == 0 and int(out[:, :, 32:].abs().sum()) == 0
+
+
+@pytest.mark.parametrize("R,V,dtype", [(1, 40_000_003, "f32"), (256, 200_003, "bf16"), (64, 700_001, "bf16"), (1, 60_000_000, "bf16")])
+def test_the_sum_over_a_large_vocabulary(R, V, dtype):
+    """One beam a request: the score is its row's largest logit less the log of the sum, which is off by what the header says; the score's three roundings on top."""
+    torch, wg = _wg()
+    g = torch.Generator(device="cuda").manual_seed(V)
+    x = torch.randn((R, V), generator=g, device="cuda").to(torch.float32 if dtype == "f32" else torch.bfloat16)
+    call = Call(torch, wg, R, V, 1, states=False)
+    call.run(x, None, torch.zeros(R, device="cuda"), None)
+    for r in range(0, R, 37):
+        y = x[r].double()
+        want = float(y.max() - torch.logsumexp(y, 0))
+        assert abs(float(call.scores[r]) - want) <= (V / 1600 + 80) * 2.0 ** -24 + 2e-7 * abs(want)
+        assert int(call.tokens[r]) == int((y == y.max()).nonzero()[0])
