@@ -425,7 +425,8 @@ int wg_cache_append(const void *d_k, const void *d_v, uint32_t tokens, uint32_t 
  * zeros); tokens from d_starts[rows] on belong to no row, and their outputs stay; with fewer tokens than that the first ones see what they see in
  * the whole call.  d_out = sum of values weighted by softmax(scale * q . k).  An infinity or a NaN in a query makes its output NaN.  Sums and the softmax in
  * fp32, products of what bfloat16, float16 and 8 bits hold: the cache's numbers and the queries exactly (where tokens * q_heads / heads is at least 32 * rows, and dim
- * is 128 or 256, a query row's numbers below 2^-14 of its largest to 2^-22 of that), the weights rounded to float16.  d_table, d_lens, d_starts: what wg_page_step leaves.  Entries of a table
+ * is 128 or 256, a query row's numbers below 2^-14 of its largest to 2^-22 of that), the weights times the scale of their values
+ * rounded to float16, those below 2^-33 of a query's largest to nothing (not in the sum).  d_table, d_lens, d_starts: what wg_page_step leaves.  Entries of a table
  * behind a row's pages may be anything.  d_workspace: wg_cache_attend_workspace(...) bytes (0: may be NULL), 16-byte aligned, overwritten; calls that
  * share it must not overlap.  heads <= 4095, q_heads <= 65535, rows <= 65535, pages * page_tokens and columns * page_tokens < 2^31, and no more tokens than one launch
  * holds (heads * (tokens * q_heads / heads / 64 + rows) < 2^24).  One or two kernels. */

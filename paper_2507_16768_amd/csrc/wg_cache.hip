@@ -352,7 +352,7 @@ struct AttendArgs {
 };
 constexpr uint32_t kAttendWaves = 4, kBlock = 64, kTile = 16;
 constexpr float kHeadroom = 14.f;                    // weights go up to 2^14
-constexpr float kLeastLift = -80.f, kMostLift = 120.f;       // (above: of terms below 2^-104)
+constexpr float kLeastLift = -80.f, kMostLift = 1000.f;      // (above: of scales that are infinite, in pages that nothing sees)
 constexpr uint32_t kLeastBlocks = 16, kFewRows = 8192;       // blocks of a share: half as many of prompts with few query rows
 // Shares in all, about (512, 768, 1,024 and 2,048: 64 rows of 2,000 tokens 58, 54, 54 and 54 us, 200 of 1,000 99, 99, 99 and 113); of the kernel for many rows, as many as the chip
 // holds at a time (256, 512 and 1,024: a prompt of 512 tokens behind 7,500 175, 98 and 100 us, 128 query rows of 32 rows of 2,000 tokens 73, 73 and 94).
@@ -640,9 +640,9 @@ attend_kernel(const AttendArgs a)
         for (uint32_t d = 0; d < kPer; d++) acc[d] += by * join_o[w][row][d0 + d];
     }
     const size_t at = (size_t)(t.begin + r / a.group) * (a.heads * a.group) + h * a.group + r % a.group;
-    const float by = total > 0.f ? 1.f / total : total == total ? 0.f : total, up = __builtin_amdgcn_exp2f(most_base - base - kHeadroom);     // (a row that sees nothing: zeros)
+    const float by = total > 0.f ? 1.f / total : total == total ? 0.f : total, up = __builtin_amdgcn_exp2f((most_base - base - kHeadroom) * 0.5f);     // (a row that sees nothing: zeros; up twice, as its square may be below all numbers)
 #pragma unroll
-    for (uint32_t d = 0; d < kPer; d++) acc[d] = acc[d] * by * up;
+    for (uint32_t d = 0; d < kPer; d++) acc[d] = acc[d] * by * up * up;
     if (shares > 1u) {
         float *to = a.partial + (at * a.splits + split) * (kD + 2u);
 #pragma unroll
@@ -1070,8 +1070,8 @@ attend_wide_kernel(const AttendArgs a)
         const uint32_t r = w0 + i * kTile + m;
         if (r >= t.last) continue;
         const size_t row = (size_t)(t.begin + r / a.group) * (a.heads * a.group) + h * a.group + r % a.group;
-        const float by = total > 0.f ? 1.f / total : total == total ? 0.f : total, down = __builtin_amdgcn_exp2f(-up[i]);      // (a row that sees nothing: zeros)
-        auto out_at = [&](uint32_t p, uint32_t e) { return nans[i] >> (4u * p + e) & 1u ? __builtin_nanf("") : o[i][p][e] * by * down; };
+        const float by = total > 0.f ? 1.f / total : total == total ? 0.f : total, down = __builtin_amdgcn_exp2f(up[i] * -0.5f);      // (a row that sees nothing: zeros; down twice, as its square may be below all numbers)
+        auto out_at = [&](uint32_t p, uint32_t e) { return nans[i] >> (4u * p + e) & 1u ? __builtin_nanf("") : o[i][p][e] * by * down * down; };
         if (shares > 1u) {
             float *to = a.partial + (row * a.splits + split) * (kD + 2u);
 #pragma unroll

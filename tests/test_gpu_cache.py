@@ -663,3 +663,29 @@ def test_what_queries_are_rounded_to(D, n):
     check_attention(out, *attention(cache, taken, table, lens, starts, D ** -0.5))
     other, size = attention(cache, x if taken is parts else parts, table, lens, starts, D ** -0.5)
     assert (np.abs(out.double().cpu().numpy() - other) > 2 * (2.0 ** -8 * size + 2.0 ** -9 * np.abs(other))).any()
+
+
+@pytest.mark.parametrize("high,others", [(20.0, 0), (40.0, 0), (80.0, 0), (80.0, 90)])
+@pytest.mark.parametrize("D,lens,news", [(64, [300, 200], [1, 2]), (128, [2500, 200], [1, 2]), (64, [300, 200], [200, 90]), (128, [300, 200], [200, 90]), (256, [300, 200], [200, 90]),
+                                         (128, [2500, 200], [70, 90])])
+def test_pages_of_zeros_with_the_highest_scores(D, lens, news, high, others):
+    """What the other pages leave beside them is as small as their terms.  Here the largest weight, of a score e^80 times the others' and the least scale, may be on a page of
+    zeros, and the sum of magnitudes says nothing of it: what is below 2^-33 of it is lost, for len keys of at most 448."""
+    torch, wg = _wg()
+    cache, table, lens, starts, q = case(18, 16, 1, 4, D, lens, news)
+    cache.ks[cache.ks > 0] = 1.0
+    cache.vs[cache.vs > 0] *= np.float32(2.0 ** others)
+    for r, L in enumerate(lens):
+        for i in range(int(L)):
+            page = table[r, i // 16]
+            cache.k[page, 0, i % 16] = to_bytes(np.full(D, high if i // 16 % 3 == 2 else i % 16 / 8.0))
+        small_pages(cache, table, r, range(2, -(-int(L) // 16), 3), "zeros")
+    q[:] = 0.0
+    q[:, :, 3] = 1.0
+    q[::2, 1, 3] = -1.0
+    out, x = run(torch, wg, cache, table, lens, starts, q, 1.0)
+    want, size = attention(cache, x, table, lens, starts, 1.0)
+    off = np.abs(out.double().cpu().numpy() - want)
+    lost = 2500 * 448 * 2.0 ** -33 * 2.0 ** -64
+    assert (off <= 2.0 ** -8 * size + 2.0 ** -9 * np.abs(want) + lost).all(), float((off / (size + lost)).max())
+    assert others == 0 or (np.abs(want) > 1e3 * lost).mean() > 0.9
