@@ -354,8 +354,8 @@ constexpr uint32_t kAttendWaves = 4, kBlock = 64, kTile = 16;
 constexpr float kHeadroom = 14.f;                    // weights go up to 2^14
 constexpr float kLeastLift = -80.f, kMostLift = 1000.f;      // (above: of scales that are infinite, in pages that nothing sees)
 constexpr uint32_t kLeastBlocks = 16, kFewRows = 8192;       // blocks of a share: half as many of prompts with few query rows
-// Shares in all, about (512, 768, 1,024 and 2,048: 64 rows of 2,000 tokens 58, 54, 54 and 54 us, 200 of 1,000 99, 99, 99 and 113); of the kernel for many rows, as many as the chip
-// holds at a time (256, 512 and 1,024: a prompt of 512 tokens behind 7,500 175, 98 and 100 us, 128 query rows of 32 rows of 2,000 tokens 73, 73 and 94).
+// Shares in all, about (512, 768, 1,024 and 2,048: 64 rows of 2,000 tokens 55, 51, 51 and 51 us, 200 of 1,000 86, 85, 85 and 86); of the kernel for many rows, as many as the chip
+// holds at a time (256, 512 and 1,024: a prompt of 512 tokens behind 7,500 174, 104 and 105 us, 128 query rows of 32 rows of 2,000 tokens 74, 74 and 95).
 constexpr uint32_t kShares = 1024, kWideShares = 512;
 constexpr __host__ __device__ uint32_t wide_rows(uint32_t dim) { return kAttendWaves * kTile * (dim == 256u ? 1u : 2u); }    // query rows of a workgroup of it
 
@@ -734,7 +734,7 @@ attend_join_kernel(const AttendArgs a)
 // the others (of zeros: they have the least scale) have a lift far below zero; that is held at -80, where a weight of e <= 2^40 is nothing in float16 and a term above 2^-46 is
 // something in fp32.  So the terms keep their sum whatever the scales are.  (Summed as float16 holds them, such pages' keys went missing.)
 //
-// 2,000 tokens each of 4 prompts behind up to 2,048, 32 query heads over 8 of 128: 229 us, 873 TFLOP/s (a large library product in bfloat16: 1,313).  The vector unit is busy for 59 % of the
+// 2,000 tokens each of 4 prompts behind up to 2,048, 32 query heads over 8 of 128: 227 us, 881 TFLOP/s (a large library product in bfloat16: 1,313).  The vector unit is busy for 63 % of the
 // cycles and the matrix unit for 39: the two wavefronts of a SIMD hardly get to use both at once.  One tile of rows and three or four wavefronts to a SIMD took 1.1 times as
 // long, four tiles and one wavefront 2.3 times.
 //
@@ -759,14 +759,14 @@ struct Yes { static constexpr bool value = true; };
 struct No { static constexpr bool value = false; };
 
 template <uint32_t kD, uint32_t kTiles>
-__global__ void __launch_bounds__(kAttendWaves * 64u, kD == 64u ? 3 : 2)      // (heads of 64: 32 prompts of 64 tokens 57 us, with the registers for two only 85)
+__global__ void __launch_bounds__(kAttendWaves * 64u, kD == 64u ? 3 : 2)      // (heads of 64: 64 tokens of each of 32 rows of 2,000 60 us, with the registers for two only 81)
 attend_wide_kernel(const AttendArgs a)
 {
     constexpr uint32_t kSteps = kD / 32u, kParts = kD / 16u, kRows = kAttendWaves * kTile * kTiles, kThreads = kAttendWaves * 64u;
     static_assert(kRows == wide_rows(kD) && kRows <= kThreads, "as the host counts them");
     static_assert(kAttendWaves == kBlock / 16u, "a wavefront for sixteen keys");
     constexpr uint32_t kAhead = kD == 256u ? 1u : 2u, kValuesAhead = kD == 64u ? 2u : 4u;         // tiles of keys and parts of values that are asked for in LDS before they are needed (heads
-    // of 64 with four parts: 32 prompts of 64 tokens behind 1,936, 79 us for 58, as what waits in registers is put into memory)
+    // of 64 with four parts: 64 tokens of each of 32 rows of 2,000 77 us for 60, as what waits in registers is put into memory)
     typedef std::conditional_t<kD == 256u, uint64_t, uint32_t> Bits;
     constexpr bool kBytes = kD >= 128u;              // scores from 8-bit numbers: products of 128 of them
     constexpr uint32_t kLoads = kD * kBlock / (16u * kThreads);            // sixteen bytes of a thread, of keys and of values each
@@ -972,8 +972,8 @@ attend_wide_kernel(const AttendArgs a)
             moves |= !begun[i] || !(part[i] <= kMostSum) || !(terms[i] <= kMostTerms);
         }
         if (__ballot(moves)) {
-            // (Read again but for heads of 128, where registers have room for it until here: a prompt of 512 tokens behind 7,500, heads of 64, 128 and 256, 86, 99 and 122 us
-            // with it held, 79, 102 and 116 without.)
+            // (Read again but for heads of 128, where registers have room for it until here: a prompt of 512 tokens behind 7,500, heads of 64, 128 and 256, 86, 103 and 125 us
+            // with it held, 81, 106 and 118 without.)
             const float v_log = log_of(kD == 128u ? scale[1] : *const_cast<const volatile float *>(reinterpret_cast<const float *>(&scales[at][g]) + 1));
 #pragma unroll
             for (uint32_t i = 0; i < kTiles; i++) {
@@ -1090,8 +1090,8 @@ attend_wide_kernel(const AttendArgs a)
 static uint32_t tiles_of(uint32_t tokens, uint32_t rows, uint32_t group) { return (uint32_t)((uint64_t)tokens * group / kTile) + rows; }
 
 // Whether requests have query rows enough, on average, for the kernel that holds many of them, which costs a request with few as much as one with its tile full.  With 8
-// heads of 128 and 4 query heads each, 32 rows of 2,000 tokens took 40 us in the other one and 51 in this for 16 query rows each, 57 and 52 for 32, 95 and 67 for
-// 64, 192 and 112 for 256; 4 such rows 17 and 22 for 32, 22 and 24 for 64, 43 and 37 for 256.  Heads of 64, whose scores come from bfloat16 in both: 32 and 40 for 32, 52 and 52 for 64.
+// heads of 128 and 4 query heads each, 32 rows of 2,000 tokens took 40 us in the other one and 51 in this for 16 query rows each, 55 and 52 for 32, 92 and 70 for
+// 64, 188 and 115 for 256; 4 such rows 16 and 23 for 32, 24 and 24 for 64, 42 and 38 for 256.  Heads of 64, whose scores come from bfloat16 in both: 33 and 38 for 32, 54 and 54 for 64.
 static bool attend_is_wide(uint32_t tokens, uint32_t rows, uint32_t group, uint32_t dim) { return (uint64_t)tokens * group >= (dim == 64u ? 64ull : 32ull) * rows; }
 
 // Whether a launch holds the call: below 2^32 threads to a dimension of the grid.
@@ -1102,16 +1102,16 @@ bool attend_fits(uint32_t tokens, uint32_t rows, uint32_t heads, uint32_t group,
 }
 
 // Blocks that a share has at least: a share more is partial results of all query rows to write and read, and a second kernel.  With 4 blocks, one for each wavefront, 256 rows of 300 tokens
-// took 49 us for 39 with 16, and 4 rows of 2,000 13.6 for 16.7.  Prompts, whose shares take longer for as many blocks: a prompt of 1,000 tokens, 32 query heads over 8, took 31 us
-// in one share and 42 in two of 8 blocks; 16 new tokens of each of 4 rows of 2,000 33 us in shares of 16 blocks and 24 of 8.
+// took 48 us for 38 with 16, and 4 rows of 2,000 11.7 for 14.3.  Prompts, whose shares take longer for as many blocks: a prompt of 1,000 tokens, 32 query heads over 8, took 31 us
+// in one share and 45 in two of 8 blocks; 16 new tokens of each of 4 rows of 2,000 33 us in shares of 16 blocks and 24 of 8.
 static uint32_t least_blocks(uint32_t tokens, uint32_t rows, uint32_t heads, uint32_t group, uint32_t dim)
 {
     return attend_is_wide(tokens, rows, group, dim) && (uint64_t)tokens * group * heads <= kFewRows ? kLeastBlocks / 2u : kLeastBlocks;
 }
 
 // The most shares of a tile's keys.  Where each row's keys in one share make four times as many workgroups as there are to be shares, the chip evens them out by itself; else a row may
-// have four times its part of them, 64 at most.  Prompts are cut where they leave half of the chip or more idle, to fill it: 64 query rows of each of 8 heads behind 20,000 tokens took 405 us in one share, 30 in 39; a prompt of
-// 512 tokens behind 7,500, 175 and 98 in three.
+// have four times its part of them, 64 at most.  Prompts are cut where they leave half of the chip or more idle, to fill it: 64 query rows of each of 8 heads behind 20,000 tokens took 407 us in one share, 31 in 39; a prompt of
+// 512 tokens behind 7,500, 175 and 104 in three.
 uint32_t attend_splits(uint32_t tokens, uint32_t rows, uint32_t heads, uint32_t group, uint32_t dim, uint32_t columns, uint32_t shift)
 {
     if (rows > 1024u) return 1u;
