@@ -436,6 +436,66 @@ int wg_cache_attend(const void *d_q, uint32_t tokens, uint32_t q_heads, uint32_t
                     uint32_t page_tokens, const int32_t *d_table, uint32_t rows, uint32_t columns, const int32_t *d_lens, const int32_t *d_starts,
                     float scale, void *d_out, void *d_workspace, uint64_t workspace_bytes, void *stream);
 
+/* ---- rotary positions -----------------------------------------------------------------------
+ * wg_rotate: pairs of a head's numbers turned by the angle that its token's position (wg_page_step leaves it) times the pair's frequency makes: with c and s the
+ * angle's cosine and sine times `magnitude`, (x, y) becomes (x c - y s, x s + y c).  The pairs are made of the first `rotated` numbers of every head, those
+ * behind stay: pair i is numbers i and i + rotated / 2, or, interleaved, 2 i and 2 i + 1.  d_frequencies: rotated / 2 of them, radians a position, fp64 (the angle is taken in 64
+ * bits; turning in fp32, rounded once).  d_q [tokens][q_heads][dim] and d_k [tokens][k_heads][dim] (k_heads 0: none, NULL) of `dtype`; strides in elements, any
+ * alignment, but 16 bytes at a time where everything lies at multiples of 16.  d_q_out may be d_q, d_k_out may be d_k, with the same strides; else no output is or overlaps an input.
+ * 2 <= rotated <= dim <= 1024, rotated even, at most 4096 heads of each.  One kernel.
+ *
+ * wg_rotary_frequencies (host): the frequencies base^(-2 i / rotated) into host_out, for contexts `factor` times as long as the `original` one that a model was trained on: a pair that
+ * turns at least `high` times over the original context keeps its frequency, one that turns at most `low` times has it divided by the factor, between them the two are mixed, in
+ * proportion to the turns or (log_ramp) to their logarithm.  factor 1: none of it (original, low and high are not looked at).  low infinite: all are divided. */
+int wg_rotate(const void *d_q, const void *d_k, wg_dtype_t dtype, uint32_t tokens, uint32_t q_heads, uint32_t k_heads, uint32_t dim, uint32_t rotated, int interleaved,
+              int64_t q_token_stride, int64_t q_head_stride, int64_t k_token_stride, int64_t k_head_stride, const int32_t *d_positions, const double *d_frequencies,
+              float magnitude, void *d_q_out, int64_t q_out_token_stride, int64_t q_out_head_stride, void *d_k_out, int64_t k_out_token_stride,
+              int64_t k_out_head_stride, void *stream);
+int wg_rotary_frequencies(double *host_out, uint32_t rotated, double base, double factor, double original, double low, double high, int log_ramp);
+
+/* ---- a cache of latent vectors --------------------------------------------------------------
+ * For models whose keys and values all come from one latent vector a token: of every token the vector, `latent` numbers (256 or 512) that all heads share, and a shared key of 64
+ * numbers that carries the position (wg_rotate).  Pages as above: d_c_cache [pages][page_tokens][latent] in bfloat16 (d_c_scale NULL) or in 8 bits (e4m3) with a scale for each token,
+ * d_c_scale [pages][page_tokens] fp32; d_r_cache [pages][page_tokens][64] bfloat16.
+ *
+ * wg_latent_append: token t's vector and shared key (bfloat16, strides of tokens in elements, at multiples of 16 bytes) go to slot d_slots[t]; a slot outside [0, pages * page_tokens)
+ * takes none; no slot is given twice.  In 8 bits a token's scale is the least power of two, 2^-64 at least, times which 448 reaches the vector's largest finite magnitude; numbers are rounded to
+ * nearest, ties to even, infinities become 448 times the scale, NaN stays.  d_origins (may be NULL), as wg_page_step leaves them: where d_origins[t] is a page, the tokens in front of token t's
+ * slot in its page come from the same places of that one; no token of the call goes to that page, or in front of token t in its own.  tokens <= 2^29, pages * page_tokens < 2^31.  One kernel.
+ *
+ * wg_latent_read: the first d_starts[r + 1] - d_starts[r] cached tokens of row r of d_table, in bfloat16, into rows d_starts[r] .. of d_c_out and d_r_out (strides in elements, at multiples of
+ * 16 bytes): what prompts behind a cached prefix expand into keys and values (numbers in 8 bits times their scale, which is exact; above what bfloat16 holds, an infinity).  d_starts does not descend; rows from d_starts[rows] on stay, and so do
+ * those in front of d_starts[0].  A token whose page is no page or lies behind the table reads as zeros.  tokens: rows that d_c_out has, < 2^31.  rows <= 65535.  One kernel. */
+int wg_latent_append(const void *d_c, const void *d_r, uint32_t tokens, uint32_t latent, int64_t c_token_stride, int64_t r_token_stride, const int32_t *d_slots,
+                     const int32_t *d_origins, void *d_c_cache, void *d_r_cache, float *d_c_scale, uint32_t pages, uint32_t page_tokens, void *stream);
+int wg_latent_read(const void *d_c_cache, const void *d_r_cache, const float *d_c_scale, uint32_t latent, uint32_t pages, uint32_t page_tokens, const int32_t *d_table,
+                   uint32_t rows, uint32_t columns, const int32_t *d_starts, uint32_t tokens, void *d_c_out, int64_t c_token_stride, void *d_r_out, int64_t r_token_stride, void *stream);
+
+/* wg_latent_attend: attention of the tokens of a step over the cached vectors themselves.  With c_j and r_j what is cached of token j, token t's output of head h is the sum of the c_j weighted by
+ * softmax over j of scale * (q_c . c_j + q_r . r_j): d_q_c [tokens][heads][latent] (a head's query, multiplied beforehand by what makes keys from vectors) and d_q_r
+ * [tokens][heads][64], both bfloat16 with strides in elements at multiples of 16 bytes; d_out bfloat16 [tokens][heads][latent] without gaps (what makes a head's values from vectors is applied to it
+ * afterwards).  d_table, d_lens, d_starts, and which keys a token sees, as for wg_cache_attend: row r has d_lens[r] tokens in the cache, the tokens d_starts[r] .. d_starts[r + 1] of the
+ * call being its last ones; token i of n sees the first d_lens[r] - n + i + 1 (none: its output is zeros); tokens from d_starts[rows] on belong to no row, and their outputs stay.  Products of
+ * bfloat16 numbers (those in 8 bits times their scale exactly), sums and softmax in fp32; weights are rounded to bfloat16 and divided by the sum of the rounded ones.  An infinity or a NaN in a vector that a token sees makes
+ * its output NaN, in part or as a whole, and is nothing to a token that does not see it.  A page number of a row's tokens that is none reads as zeros; entries behind them may be anything.
+ * d_workspace: wg_latent_attend_workspace(...) bytes (0: may be NULL), 16-byte aligned, overwritten; calls that share it must not overlap.  heads <= 4096, rows <= 65535, pages *
+ * page_tokens and columns * page_tokens < 2^31, tokens * heads < 2^31 and no more tokens than one launch holds (tokens * heads / 16 + rows < 2^24).  One or two kernels.
+ *
+ * wg_latent_prompt: the same attention with keys and values of every head made beforehand from the vectors (wg_latent_read, then a product), which takes a fraction of the operations where
+ * many tokens see the same keys.  d_q_n [tokens][heads][dim] and d_q_r [tokens][heads][64] are the two parts of the queries, d_k_n and d_v [keys][heads][dim] the keys' own part and the values, d_k_r [keys][64] the shared part; bfloat16, strides in
+ * elements at multiples of 16 bytes; dim is 64 or 128.  Row r has the queries d_starts[r] .. d_starts[r + 1] and the keys d_key_starts[r] .. d_key_starts[r + 1], its queries being the last of them: query i of n sees
+ * the first m - n + i + 1 of its m keys (none: zeros); tokens from d_starts[rows] on belong to no row, and their outputs stay.  d_out bfloat16 [tokens][heads][dim] without gaps.  Rounding as above; an infinity or a NaN in a value that a
+ * token sees makes that output infinite or NaN and is nothing to a token that does not see it.  Both starts do not descend.  heads <= 4096, rows <= 65535, tokens and keys < 2^31, tokens * heads < 2^31.  One or two kernels. */
+uint64_t wg_latent_attend_workspace(uint32_t tokens, uint32_t rows, uint32_t heads, uint32_t latent, uint32_t columns, uint32_t page_tokens);
+int wg_latent_attend(const void *d_q_c, const void *d_q_r, uint32_t tokens, uint32_t heads, uint32_t latent, int64_t c_token_stride, int64_t c_head_stride, int64_t r_token_stride,
+                     int64_t r_head_stride, const void *d_c_cache, const void *d_r_cache, const float *d_c_scale, uint32_t pages, uint32_t page_tokens, const int32_t *d_table, uint32_t rows,
+                     uint32_t columns, const int32_t *d_lens, const int32_t *d_starts, float scale, void *d_out, void *d_workspace, uint64_t workspace_bytes, void *stream);
+uint64_t wg_latent_prompt_workspace(uint32_t tokens, uint32_t rows, uint32_t heads, uint32_t dim, uint32_t keys);
+int wg_latent_prompt(const void *d_q_n, const void *d_q_r, const void *d_k_n, const void *d_k_r, const void *d_v, uint32_t tokens, uint32_t keys, uint32_t heads, uint32_t dim,
+                     int64_t q_n_token_stride, int64_t q_n_head_stride, int64_t q_r_token_stride, int64_t q_r_head_stride, int64_t k_n_token_stride, int64_t k_n_head_stride,
+                     int64_t k_r_token_stride, int64_t v_token_stride, int64_t v_head_stride, uint32_t rows, const int32_t *d_starts, const int32_t *d_key_starts, float scale,
+                     void *d_out, void *d_workspace, uint64_t workspace_bytes, void *stream);
+
 /* ---- introspection (these synchronise the device) ---------------------------------------- */
 /* (Counters are read in two small copies, whatever the number of keys; rows_in_use is counted by a launch while
  * the cache has a row for every key.) */

@@ -66,6 +66,7 @@ EXPORTS = [
     "wg_masked_topk_static", "wg_masked_topk_static_capacity", "wg_profile_apply_mask", "wg_forced_bytes",
     "wg_beam_select", "wg_beam_select_workspace", "wg_reorder_rows",
     "wg_page_step", "wg_page_step_workspace", "wg_cache_append", "wg_cache_attend", "wg_cache_attend_workspace",
+    "wg_rotate", "wg_rotary_frequencies", "wg_latent_append", "wg_latent_read", "wg_latent_attend", "wg_latent_attend_workspace", "wg_latent_prompt", "wg_latent_prompt_workspace",
 ]
 
 
@@ -140,6 +141,16 @@ def load_library():
     L.wg_cache_attend_workspace.argtypes = [u32] * 7
     L.wg_cache_attend_workspace.restype = u64
     L.wg_cache_attend.argtypes = [vp, u32, u32, u32, u32, i64, i64, vp, vp, vp, vp, u32, u32, vp, u32, u32, vp, vp, C.c_float, vp, vp, u64, vp]
+    L.wg_rotate.argtypes = [vp, vp, C.c_int, u32, u32, u32, u32, u32, C.c_int, i64, i64, i64, i64, vp, vp, C.c_float, vp, i64, i64, vp, i64, i64, vp]
+    L.wg_rotary_frequencies.argtypes = [C.POINTER(C.c_double), u32] + [C.c_double] * 5 + [C.c_int]
+    L.wg_latent_append.argtypes = [vp, vp, u32, u32, i64, i64, vp, vp, vp, vp, vp, u32, u32, vp]
+    L.wg_latent_read.argtypes = [vp, vp, vp, u32, u32, u32, vp, u32, u32, vp, u32, vp, i64, vp, i64, vp]
+    L.wg_latent_attend_workspace.argtypes = [u32] * 6
+    L.wg_latent_attend_workspace.restype = u64
+    L.wg_latent_attend.argtypes = [vp, vp, u32, u32, u32, i64, i64, i64, i64, vp, vp, vp, u32, u32, vp, u32, u32, vp, vp, C.c_float, vp, vp, u64, vp]
+    L.wg_latent_prompt_workspace.argtypes = [u32] * 5
+    L.wg_latent_prompt_workspace.restype = u64
+    L.wg_latent_prompt.argtypes = [vp] * 5 + [u32] * 4 + [i64] * 9 + [u32, vp, vp, C.c_float, vp, vp, u64, vp]
     L.wg_cache_clear.argtypes = [vp, vp]
     L.wg_cache_stats.argtypes = [vp, C.POINTER(_Stats)]
     L.wg_error_count.argtypes = [vp, C.POINTER(u64)]
@@ -492,3 +503,48 @@ def cache_attend(q, k_cache, v_cache, k_scale, v_scale, table, lens, starts, sca
     """wg_cache_attend: q and out bfloat16 [T, q_heads, dim], the cache as for cache_append, table int32 [R, columns], lens [R] and
     starts [R + 1] as page_step leaves them."""
     (_native or _load_native()).cache_attend(q, k_cache, v_cache, k_scale, v_scale, table, lens, starts, scale, out, workspace, stream)
+
+
+def rotary_frequencies(rotated, base=10000.0, factor=1.0, original=0.0, low=1.0, high=4.0, log_ramp=False):
+    """wg_rotary_frequencies: the frequencies of rotated / 2 pairs, float64 on the host."""
+    out = np.empty(max(int(rotated) // 2, 1), dtype=np.float64)
+    _check(load_library().wg_rotary_frequencies(out.ctypes.data_as(C.POINTER(C.c_double)), int(rotated), base, factor, original, low, high, 1 if log_ramp else 0))
+    return out
+
+
+def rotate(q, k, positions, frequencies, q_out, k_out, interleaved=False, magnitude=1.0, stream=None):
+    """wg_rotate: q and q_out [T, q_heads, dim], k and k_out [T, k_heads, dim] or both None, float32 or bfloat16, positions int32 [T], frequencies float64
+    [rotated / 2] on the device.  The outputs may be the inputs."""
+    (_native or _load_native()).rotate(q, k, positions, frequencies, q_out, k_out, interleaved, magnitude, stream)
+
+
+def latent_append(c, r, slots, origins, c_cache, r_cache, c_scale, stream=None):
+    """wg_latent_append: c bfloat16 [T, latent], r bfloat16 [T, 64], slots and origins (or None) int32 [T], c_cache [pages, page_tokens, latent] float8_e4m3fn with
+    c_scale float32 [pages, page_tokens], or bfloat16 with c_scale None, r_cache bfloat16 [pages, page_tokens, 64]."""
+    (_native or _load_native()).latent_append(c, r, slots, origins, c_cache, r_cache, c_scale, stream)
+
+
+def latent_read(c_cache, r_cache, c_scale, table, starts, c_out, r_out, stream=None):
+    """wg_latent_read: the cache as for latent_append, table int32 [R, columns], starts int32 [R + 1], c_out bfloat16 [N, latent], r_out bfloat16 [N, 64]."""
+    (_native or _load_native()).latent_read(c_cache, r_cache, c_scale, table, starts, c_out, r_out, stream)
+
+
+def latent_attend_workspace(tokens, rows, heads, latent, columns, page_tokens):
+    """wg_latent_attend_workspace: bytes of device workspace a latent_attend call of this shape needs."""
+    return int(load_library().wg_latent_attend_workspace(tokens, rows, heads, latent, columns, page_tokens))
+
+
+def latent_attend(q_c, q_r, c_cache, r_cache, c_scale, table, lens, starts, scale, out, workspace=None, stream=None):
+    """wg_latent_attend: q_c and out bfloat16 [T, heads, latent], q_r bfloat16 [T, heads, 64], the cache as for latent_append, table int32 [R, columns], lens [R] and
+    starts [R + 1] as page_step leaves them."""
+    (_native or _load_native()).latent_attend(q_c, q_r, c_cache, r_cache, c_scale, table, lens, starts, scale, out, workspace, stream)
+
+
+def latent_prompt_workspace(tokens, rows, heads, dim, keys):
+    """wg_latent_prompt_workspace: bytes of device workspace a latent_prompt call of this shape needs."""
+    return int(load_library().wg_latent_prompt_workspace(tokens, rows, heads, dim, keys))
+
+
+def latent_prompt(q_n, q_r, k_n, k_r, v, starts, key_starts, scale, out, workspace=None, stream=None):
+    """wg_latent_prompt: q_n and out bfloat16 [T, heads, dim], q_r [T, heads, 64], k_n and v [N, heads, dim], k_r [N, 64], starts and key_starts int32 [R + 1]."""
+    (_native or _load_native()).latent_prompt(q_n, q_r, k_n, k_r, v, starts, key_starts, scale, out, workspace, stream)

@@ -6,8 +6,8 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libwgrammar.so")
 SOURCES = ["wg_api.cpp", "wg_lower.cpp", "wg_regex.cpp", "wg_vocab_index.cpp", "wg_kernels.hip", "wg_sample.hip",
-           "wg_serve.cpp", "wg_beam.hip", "wg_pages.hip", "wg_cache.hip"]
-HEADERS = ["wg_internal.h", "wg_buffer.h", "wg_device.h", "wg_launch.h", "wg_order.h", "wg_row.h", "wg_serve.h", os.path.join("..", "..", "include", "wg.h")]
+           "wg_serve.cpp", "wg_beam.hip", "wg_pages.hip", "wg_cache.hip", "wg_rotate.hip", "wg_latent.hip", "wg_latent_attend.hip"]
+HEADERS = ["wg_internal.h", "wg_buffer.h", "wg_device.h", "wg_launch.h", "wg_number.h", "wg_order.h", "wg_row.h", "wg_serve.h", os.path.join("..", "..", "include", "wg.h")]
 # a kernel's first dwords of arguments are in scalar registers when its wavefronts begin
 PRELOADED_DWORDS = 14
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared", "-Wall",

@@ -1,0 +1,159 @@
+// A cache of latent vectors for gfx950: of every token one vector of C numbers that all heads share, and a shared key of 64 numbers that carries the position.  Pages of P
+// tokens: latent vectors [page][token][C] in bfloat16, or in 8 bits with a scale for each token, [page][token]; shared keys [page][token][64] in bfloat16.
+#include <hip/hip_runtime.h>
+
+#include "wg_launch.h"
+#include "wg_number.h"
+#include "wg_serve.h"
+
+namespace wg {
+
+constexpr uint32_t kLatentThreads = 256, kLatentWaves = 4;
+
+// ---------------------------------------------------------------------------------------------
+// append.  A wavefront for each token.  A token has a scale of its own, so nothing that is in the cache is rounded again; what comes along from another page is copied as it is, by all
+// wavefronts of the workgroup (63 tokens of 644 bytes at the most).
+struct LatentAppendArgs {
+    const uint16_t *c, *r;
+    int64_t c_token, r_token;                        // strides, elements
+    const int32_t *slots, *origins;
+    uint8_t *c_cache;
+    uint16_t *r_cache;
+    float *scale;
+    uint32_t tokens, pages, shift, per;              // per: tokens of a workgroup
+};
+
+__device__ __forceinline__ void copy_words(void *to, const void *from, uint32_t words, uint32_t tid)
+{
+#pragma unroll 4
+    for (uint32_t i = tid; i < words; i += kLatentThreads) static_cast<Word4 *>(to)[i] = static_cast<const Word4 *>(from)[i];
+}
+
+template <uint32_t kC, bool kBytes>
+__global__ void __launch_bounds__(kLatentThreads)
+latent_append_kernel(const LatentAppendArgs a)
+{
+    constexpr uint32_t kOwn = kC / 64u, kRow = kC * (kBytes ? 1u : 2u);    // dims of a lane; bytes of a token
+    const uint32_t tid = threadIdx.x, lane = tid & 63u, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const uint32_t first = blockIdx.x * a.per, t = first + wave;
+    if (wave < a.per && t < a.tokens) {
+        const uint32_t slot = (uint32_t)a.slots[t];
+        uint32_t w[kOwn / 2u];
+        const uint32_t *x = reinterpret_cast<const uint32_t *>(a.c + (int64_t)t * a.c_token) + lane * (kOwn / 2u);
+#pragma unroll
+        for (uint32_t i = 0; i < kOwn / 2u; i++) w[i] = x[i];
+        const uint32_t r = lane < 32u ? reinterpret_cast<const uint32_t *>(a.r + (int64_t)t * a.r_token)[lane] : 0u;
+        if (slot >> a.shift < a.pages) {
+            uint32_t *to = reinterpret_cast<uint32_t *>(a.c_cache + (size_t)slot * kRow) + lane * (kRow / 256u);
+            if (kBytes) {
+                float top = 0.f;
+#pragma unroll
+                for (uint32_t i = 0; i < kOwn / 2u; i++) { top = top_of(top, low(w[i])); top = top_of(top, high(w[i])); }
+#pragma unroll
+                for (int s = 32; s > 0; s >>= 1) top = __builtin_fmaxf(top, __shfl_xor(top, s));
+                const float scale = scale_for(top), inverse = 1.f / scale;
+                if (lane == 0u) a.scale[slot] = scale;
+#pragma unroll
+                for (uint32_t i = 0; i < kOwn / 4u; i++)
+                    to[i] = to_bytes(low(w[2u * i]) * inverse, high(w[2u * i]) * inverse, low(w[2u * i + 1u]) * inverse, high(w[2u * i + 1u]) * inverse);
+            } else
+#pragma unroll
+                for (uint32_t i = 0; i < kOwn / 2u; i++) to[i] = w[i];
+            if (lane < 32u) reinterpret_cast<uint32_t *>(a.r_cache + (size_t)slot * kLatentKey)[lane] = r;
+        }
+    }
+    if (!a.origins) return;
+    for (uint32_t i = 0; i < a.per && first + i < a.tokens; i++) {
+        const uint32_t origin = (uint32_t)a.origins[first + i], slot = (uint32_t)a.slots[first + i], page = slot >> a.shift, o = slot & ((1u << a.shift) - 1u);
+        if (origin >= a.pages || page >= a.pages || !o || origin == page) continue;
+        const size_t from = (size_t)origin << a.shift, to = (size_t)page << a.shift;
+        copy_words(a.c_cache + to * kRow, a.c_cache + from * kRow, o * (kRow / 16u), tid);
+        copy_words(a.r_cache + to * kLatentKey, a.r_cache + from * kLatentKey, o * (kLatentKey / 8u), tid);
+        if (kBytes && tid < o) a.scale[to + tid] = a.scale[from + tid];
+    }
+}
+
+hipError_t launch_latent_append(const void *c, const void *r, uint32_t tokens, uint32_t latent, int64_t c_token, int64_t r_token, const int32_t *slots, const int32_t *origins,
+                                void *c_cache, void *r_cache, float *scale, uint32_t pages, uint32_t shift, hipStream_t s)
+{
+    const uint32_t per = tokens <= 1024u ? 1u : kLatentWaves;
+    const LatentAppendArgs a{static_cast<const uint16_t *>(c), static_cast<const uint16_t *>(r), c_token, r_token, slots, origins, static_cast<uint8_t *>(c_cache),
+                             static_cast<uint16_t *>(r_cache), scale, tokens, pages, shift, per};
+    return launch(latent == 512u ? (scale ? latent_append_kernel<512, true> : latent_append_kernel<512, false>) : scale ? latent_append_kernel<256, true> : latent_append_kernel<256, false>,
+                  dim3((tokens + per - 1u) / per), dim3(kLatentThreads), 0, s, nullptr, a);
+}
+
+// ---------------------------------------------------------------------------------------------
+// read.  A wavefront takes 16 tokens behind one another; a lane of the workgroup finds a token's row and slot.
+struct LatentReadArgs {
+    const uint8_t *c_cache;
+    const uint16_t *r_cache;
+    const float *scale;
+    const int32_t *table, *starts;
+    uint16_t *c_out, *r_out;
+    int64_t c_token, r_token;
+    uint32_t rows, columns, tokens, pages, shift;
+};
+constexpr uint32_t kReadTokens = 16;
+
+template <uint32_t kC, bool kBytes>
+__global__ void __launch_bounds__(kLatentThreads)
+latent_read_kernel(const LatentReadArgs a)
+{
+    constexpr uint32_t kOwn = kC / 64u, kRow = kC * (kBytes ? 1u : 2u), kWords = kRow / 256u;
+    const uint32_t tid = threadIdx.x, lane = tid & 63u, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const uint32_t base = (blockIdx.x * kLatentWaves + wave) * kReadTokens, t = base + lane;
+    // the last row that begins at the token or before
+    uint32_t slot = 0xFFFFFFFFu;
+    bool there = lane < kReadTokens && t < a.tokens && t < (uint32_t)a.starts[a.rows] && t >= (uint32_t)a.starts[0];
+    if (there) {
+        uint32_t lo = 0, n = a.rows;
+        while (n > 1u) { const uint32_t half = n / 2u; if ((uint32_t)a.starts[lo + half] <= t) { lo += half; n -= half; } else n = half; }
+        const uint32_t i = t - (uint32_t)a.starts[lo], column = i >> a.shift;
+        if (column < a.columns) {
+            const uint32_t page = (uint32_t)a.table[(size_t)lo * a.columns + column];
+            if (page < a.pages) slot = page << a.shift | (i & ((1u << a.shift) - 1u));
+        }
+    }
+    const uint32_t known = (uint32_t)__ballot(there);
+    const float own_scale = kBytes && slot != 0xFFFFFFFFu ? a.scale[slot] : 0.f;
+    uint32_t w[kReadTokens][kWords], r[kReadTokens];
+#pragma unroll
+    for (uint32_t i = 0; i < kReadTokens; i++) {
+        const uint32_t at = __builtin_amdgcn_readlane(slot, i);
+        const bool real = at != 0xFFFFFFFFu;
+        const uint32_t *from = reinterpret_cast<const uint32_t *>(a.c_cache + (size_t)(real ? at : 0u) * kRow) + lane * kWords;
+#pragma unroll
+        for (uint32_t k = 0; k < kWords; k++) w[i][k] = real ? from[k] : 0u;
+        r[i] = real && lane < 32u ? reinterpret_cast<const uint32_t *>(a.r_cache + (size_t)at * kLatentKey)[lane] : 0u;
+    }
+#pragma unroll
+    for (uint32_t i = 0; i < kReadTokens; i++) {
+        if (!(known >> i & 1u)) continue;
+        uint32_t *to = reinterpret_cast<uint32_t *>(a.c_out + (int64_t)(base + i) * a.c_token) + lane * (kOwn / 2u);
+        if (kBytes) {
+            const float scale = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(own_scale), i));
+#pragma unroll
+            for (uint32_t k = 0; k < kWords; k++) {
+                const auto x = __builtin_amdgcn_cvt_pk_f32_fp8((int)w[i][k], false), y = __builtin_amdgcn_cvt_pk_f32_fp8((int)w[i][k], true);
+                to[2u * k] = pk_bf16(x[0] * scale, x[1] * scale);
+                to[2u * k + 1u] = pk_bf16(y[0] * scale, y[1] * scale);
+            }
+        } else
+#pragma unroll
+            for (uint32_t k = 0; k < kWords; k++) to[k] = w[i][k];
+        if (lane < 32u) reinterpret_cast<uint32_t *>(a.r_out + (int64_t)(base + i) * a.r_token)[lane] = r[i];
+    }
+}
+
+hipError_t launch_latent_read(const void *c_cache, const void *r_cache, const float *scale, uint32_t latent, uint32_t pages, uint32_t shift, const int32_t *table, uint32_t rows,
+                              uint32_t columns, const int32_t *starts, uint32_t tokens, void *c_out, int64_t c_token, void *r_out, int64_t r_token, hipStream_t s)
+{
+    const LatentReadArgs a{static_cast<const uint8_t *>(c_cache), static_cast<const uint16_t *>(r_cache), scale, table, starts, static_cast<uint16_t *>(c_out),
+                           static_cast<uint16_t *>(r_out), c_token, r_token, rows, columns, tokens, pages, shift};
+    const uint32_t per = kLatentWaves * kReadTokens;
+    return launch(latent == 512u ? (scale ? latent_read_kernel<512, true> : latent_read_kernel<512, false>) : scale ? latent_read_kernel<256, true> : latent_read_kernel<256, false>,
+                  dim3((tokens + per - 1u) / per), dim3(kLatentThreads), 0, s, nullptr, a);
+}
+
+}  // namespace wg

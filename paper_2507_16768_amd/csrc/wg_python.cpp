@@ -39,7 +39,7 @@ bool device(const at::Tensor &t, at::ScalarType dtype, const char *name) {
     if (!t.is_cuda() || !t.is_contiguous()) return bad(PyExc_ValueError, std::string(name) + " must be a contiguous device tensor");
     if (t.scalar_type() != dtype)
         return bad(PyExc_ValueError, std::string(name) + " must have dtype torch." + (dtype == at::kInt ? "int32" : dtype == at::kLong ? "int64" :
-                                     dtype == at::kByte ? "uint8" : dtype == at::kFloat ? "float32" : "bfloat16"));
+                                     dtype == at::kByte ? "uint8" : dtype == at::kFloat ? "float32" : dtype == at::kDouble ? "float64" : "bfloat16"));
     return true;
 }
 bool shape2(const at::Tensor &t, int64_t a, int64_t b) { return t.dim() == 2 && t.size(0) == a && t.size(1) == b; }
@@ -384,6 +384,129 @@ PyObject *cache_attend(PyObject *, PyObject *const *a, Py_ssize_t n) {
     }));
 }
 
+// A [T, heads, dim] float32 or bfloat16 device tensor with unit inner stride, of the first one's type.
+bool turned_ok(const at::Tensor &t, at::ScalarType dtype, const char *name) {
+    if (t.dim() != 3 || !t.is_cuda() || t.scalar_type() != dtype || (t.size(2) != 1 && t.stride(2) != 1))
+        return bad(PyExc_ValueError, std::string(name) + " must be a [T, heads, dim] device tensor with unit inner stride, of the dtype of q");
+    return fits32(t, 0) && fits32(t, 1) && fits32(t, 2);
+}
+
+// rotate(q, k or None, positions, frequencies, q_out, k_out or None, interleaved, magnitude, stream)
+PyObject *rotate(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    const at::Tensor *q, *k = nullptr, *po, *fr, *qo, *ko = nullptr; void *s;
+    if (!count(n, 9) || !tensor(a[0], &q, "q") || (a[1] != Py_None && !tensor(a[1], &k, "k")) || !tensor(a[2], &po, "positions") || !tensor(a[3], &fr, "frequencies") ||
+        !tensor(a[4], &qo, "q_out") || (a[5] != Py_None && !tensor(a[5], &ko, "k_out"))) return nullptr;
+    const int beside = PyObject_IsTrue(a[6]);
+    const double magnitude = PyFloat_AsDouble(a[7]);
+    if (PyErr_Occurred()) return nullptr;
+    const at::ScalarType type = q->scalar_type();
+    if (type != at::kFloat && type != at::kBFloat16) { bad(PyExc_ValueError, "q must be float32 or bfloat16"); return nullptr; }
+    if (!k != !ko) { bad(PyExc_ValueError, "keys go in and out, or neither"); return nullptr; }
+    if (!turned_ok(*q, type, "q") || !turned_ok(*qo, type, "q_out") || (k && (!turned_ok(*k, type, "k") || !turned_ok(*ko, type, "k_out")))) return nullptr;
+    const int64_t T = q->size(0), D = q->size(2);
+    if (qo->sizes() != q->sizes() || (k && (ko->sizes() != k->sizes() || k->size(0) != T || k->size(2) != D))) {
+        bad(PyExc_ValueError, "the outputs must have their inputs' shapes, and q and k the same tokens and dim");
+        return nullptr;
+    }
+    if (!shape1(*po, T) || fr->dim() != 1) { bad(PyExc_ValueError, "positions must be [T] and frequencies [rotated / 2]"); return nullptr; }
+    if (fr->size(0) > D) { bad(PyExc_ValueError, "more frequencies than pairs"); return nullptr; }
+    if (!device(*po, at::kInt, "positions") || !device(*fr, at::kDouble, "frequencies") || !stream_of(a[8], &s)) return nullptr;
+    const uint32_t pairs = rows(*fr), K = k ? (uint32_t)k->size(1) : 0u;
+    return result(unlocked([=, qp = q->data_ptr(), kp = k ? k->data_ptr() : nullptr, dt = type == at::kFloat ? WG_F32 : WG_BF16, H = (uint32_t)q->size(1), q0 = step_of(*q, 0), q1 = step_of(*q, 1),
+                            k0 = k ? step_of(*k, 0) : 0, k1 = k ? step_of(*k, 1) : 0, positions = ints(*po), frequencies = static_cast<const double *>(fr->data_ptr()), qop = qo->data_ptr(),
+                            kop = k ? ko->data_ptr() : nullptr, qo0 = step_of(*qo, 0), qo1 = step_of(*qo, 1), ko0 = k ? step_of(*ko, 0) : 0, ko1 = k ? step_of(*ko, 1) : 0] {
+        return wg_rotate(qp, kp, dt, (uint32_t)T, H, K, (uint32_t)D, 2u * pairs, beside, q0, q1, k0, k1, positions, frequencies, (float)magnitude, qop, qo0, qo1, kop, ko0, ko1, s);
+    }));
+}
+
+// The cache of latent vectors [pages, page_tokens, latent], shared keys [pages, page_tokens, 64] and scales [pages, page_tokens] or None.
+struct Latents { void *c, *r; float *scale; uint32_t pages, page_tokens, latent; };
+bool latents_of(PyObject *const *a, Latents *out) {
+    const at::Tensor *c, *r, *sc = nullptr;
+    if (!tensor(a[0], &c, "c_cache") || !tensor(a[1], &r, "r_cache") || (a[2] != Py_None && !tensor(a[2], &sc, "c_scale"))) return false;
+    if (c->dim() != 3 || r->dim() != 3 || r->size(0) != c->size(0) || r->size(1) != c->size(1) || r->size(2) != 64 || (sc && !shape2(*sc, c->size(0), c->size(1))))
+        return bad(PyExc_ValueError, "c_cache must be [pages, page_tokens, latent], r_cache [pages, page_tokens, 64] and c_scale [pages, page_tokens]");
+    if (c->scalar_type() != (sc ? at::kFloat8_e4m3fn : at::kBFloat16)) return bad(PyExc_ValueError, "c_cache must have dtype torch.float8_e4m3fn, with c_scale, or torch.bfloat16, without");
+    if (!device(*c, c->scalar_type(), "c_cache") || !device(*r, at::kBFloat16, "r_cache") || (sc && !device(*sc, at::kFloat, "c_scale"))) return false;
+    for (int64_t d = 0; d < 3; d++) if (!fits32(*c, d)) return false;
+    *out = Latents{c->data_ptr(), r->data_ptr(), sc ? static_cast<float *>(sc->data_ptr()) : nullptr, (uint32_t)c->size(0), (uint32_t)c->size(1), (uint32_t)c->size(2)};
+    return true;
+}
+// A [T, dim] bfloat16 device tensor with unit inner stride.
+bool vectors_ok(const at::Tensor &t, int64_t dim, const char *name) {
+    if (t.dim() != 2 || !t.is_cuda() || t.scalar_type() != at::kBFloat16 || t.stride(1) != 1 || t.size(1) != dim)
+        return bad(PyExc_ValueError, std::string(name) + " must be a [T, " + std::to_string(dim) + "] bfloat16 device tensor with unit inner stride");
+    return fits32(t, 0);
+}
+
+// latent_append(c, r, slots, origins or None, c_cache, r_cache, c_scale or None, stream)
+PyObject *latent_append(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    const at::Tensor *c, *r, *sl, *og = nullptr; void *s; Latents l;
+    if (!count(n, 8) || !tensor(a[0], &c, "c") || !tensor(a[1], &r, "r") || !tensor(a[2], &sl, "slots") || (a[3] != Py_None && !tensor(a[3], &og, "origins")) || !latents_of(a + 4, &l) ||
+        !vectors_ok(*c, l.latent, "c") || !vectors_ok(*r, 64, "r")) return nullptr;
+    const int64_t T = c->size(0);
+    if (r->size(0) != T || !shape1(*sl, T) || (og && !shape1(*og, T))) { bad(PyExc_ValueError, "c must be [T, latent], r [T, 64], slots and origins [T]"); return nullptr; }
+    if (!device(*sl, at::kInt, "slots") || (og && !device(*og, at::kInt, "origins")) || !stream_of(a[7], &s)) return nullptr;
+    return result(unlocked([=, cp = c->data_ptr(), rp = r->data_ptr(), c0 = step_of(*c, 0), r0 = step_of(*r, 0), slots = ints(*sl), origins = og ? ints(*og) : nullptr] {
+        return wg_latent_append(cp, rp, (uint32_t)T, l.latent, c0, r0, slots, origins, l.c, l.r, l.scale, l.pages, l.page_tokens, s);
+    }));
+}
+
+// latent_read(c_cache, r_cache, c_scale or None, table, starts, c_out, r_out, stream)
+PyObject *latent_read(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    const at::Tensor *tb, *st, *c, *r; void *s; Latents l;
+    if (!count(n, 8) || !latents_of(a, &l) || !tensor(a[3], &tb, "table") || !tensor(a[4], &st, "starts") || !tensor(a[5], &c, "c_out") || !tensor(a[6], &r, "r_out") ||
+        !vectors_ok(*c, l.latent, "c_out") || !vectors_ok(*r, 64, "r_out")) return nullptr;
+    if (tb->dim() != 2 || !shape1(*st, tb->size(0) + 1) || r->size(0) != c->size(0)) { bad(PyExc_ValueError, "table must be [R, columns], starts [R + 1], c_out and r_out of the same tokens"); return nullptr; }
+    if (!device(*tb, at::kInt, "table") || !device(*st, at::kInt, "starts") || !fits32(*tb, 0) || !fits32(*tb, 1) || !stream_of(a[7], &s)) return nullptr;
+    return result(unlocked([=, table = ints(*tb), R = rows(*tb), M = (uint32_t)tb->size(1), starts = ints(*st), T = rows(*c), cp = c->data_ptr(), rp = r->data_ptr(), c0 = step_of(*c, 0),
+                            r0 = step_of(*r, 0)] {
+        return wg_latent_read(l.c, l.r, l.scale, l.latent, l.pages, l.page_tokens, table, R, M, starts, T, cp, c0, rp, r0, s);
+    }));
+}
+
+// latent_attend(q_c, q_r, c_cache, r_cache, c_scale or None, table, lens, starts, scale, out, workspace or None, stream)
+PyObject *latent_attend(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    const at::Tensor *q, *r, *tb, *le, *st, *ou; void *s, *work; uint64_t bytes; Latents l;
+    if (!count(n, 12) || !tensor(a[0], &q, "q_c") || !tensor(a[1], &r, "q_r") || !latents_of(a + 2, &l) || !tensor(a[5], &tb, "table") || !tensor(a[6], &le, "lens") ||
+        !tensor(a[7], &st, "starts") || !tensor(a[9], &ou, "out") || !work_of(a[10], &work, &bytes) || !heads_ok(*q, "q_c") || !heads_ok(*r, "q_r")) return nullptr;
+    const double scale = PyFloat_AsDouble(a[8]);
+    if (PyErr_Occurred()) return nullptr;
+    if (q->size(2) != l.latent || ou->sizes() != q->sizes() || r->size(0) != q->size(0) || r->size(1) != q->size(1) || r->size(2) != 64) {
+        bad(PyExc_ValueError, "q_c and out must be [T, heads, latent] with the cache's latent, q_r [T, heads, 64]");
+        return nullptr;
+    }
+    if (tb->dim() != 2 || !shape1(*le, tb->size(0)) || !shape1(*st, tb->size(0) + 1)) { bad(PyExc_ValueError, "table must be [R, columns], lens [R] and starts [R + 1]"); return nullptr; }
+    if (!device(*tb, at::kInt, "table") || !device(*le, at::kInt, "lens") || !device(*st, at::kInt, "starts") || !device(*ou, at::kBFloat16, "out") || !fits32(*tb, 0) || !fits32(*tb, 1) ||
+        !stream_of(a[11], &s)) return nullptr;
+    return result(unlocked([=, qp = q->data_ptr(), rp = r->data_ptr(), T = rows(*q), H = (uint32_t)q->size(1), q0 = step_of(*q, 0), q1 = step_of(*q, 1), r0 = step_of(*r, 0), r1 = step_of(*r, 1),
+                            table = ints(*tb), R = rows(*tb), M = (uint32_t)tb->size(1), lens = ints(*le), starts = ints(*st), out = ou->data_ptr()] {
+        return wg_latent_attend(qp, rp, T, H, l.latent, q0, q1, r0, r1, l.c, l.r, l.scale, l.pages, l.page_tokens, table, R, M, lens, starts, (float)scale, out, work, bytes, s);
+    }));
+}
+
+// latent_prompt(q_n, q_r, k_n, k_r, v, starts, key_starts, scale, out, workspace or None, stream)
+PyObject *latent_prompt(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    const at::Tensor *q, *r, *k, *kr, *v, *st, *ks, *ou; void *s, *work; uint64_t bytes;
+    if (!count(n, 11) || !tensor(a[0], &q, "q_n") || !tensor(a[1], &r, "q_r") || !tensor(a[2], &k, "k_n") || !tensor(a[3], &kr, "k_r") || !tensor(a[4], &v, "v") || !tensor(a[5], &st, "starts") ||
+        !tensor(a[6], &ks, "key_starts") || !tensor(a[8], &ou, "out") || !work_of(a[9], &work, &bytes) || !heads_ok(*q, "q_n") || !heads_ok(*r, "q_r") || !heads_ok(*k, "k_n") ||
+        !heads_ok(*v, "v") || !vectors_ok(*kr, 64, "k_r")) return nullptr;
+    const double scale = PyFloat_AsDouble(a[7]);
+    if (PyErr_Occurred()) return nullptr;
+    if (ou->sizes() != q->sizes() || r->size(0) != q->size(0) || r->size(1) != q->size(1) || r->size(2) != 64 || k->sizes() != v->sizes() || k->size(1) != q->size(1) || k->size(2) != q->size(2) ||
+        kr->size(0) != k->size(0)) {
+        bad(PyExc_ValueError, "q_n and out must be [T, heads, dim], q_r [T, heads, 64], k_n and v [N, heads, dim], k_r [N, 64]");
+        return nullptr;
+    }
+    if (st->dim() != 1 || st->size(0) < 2 || !shape1(*ks, st->size(0))) { bad(PyExc_ValueError, "starts and key_starts must be [R + 1]"); return nullptr; }
+    if (!device(*st, at::kInt, "starts") || !device(*ks, at::kInt, "key_starts") || !device(*ou, at::kBFloat16, "out") || !fits32(*q, 2) || !stream_of(a[10], &s)) return nullptr;
+    return result(unlocked([=, qp = q->data_ptr(), rp = r->data_ptr(), kp = k->data_ptr(), krp = kr->data_ptr(), vp = v->data_ptr(), T = rows(*q), N = rows(*k), H = (uint32_t)q->size(1),
+                            D = (uint32_t)q->size(2), q0 = step_of(*q, 0), q1 = step_of(*q, 1), r0 = step_of(*r, 0), r1 = step_of(*r, 1), k0 = step_of(*k, 0), k1 = step_of(*k, 1),
+                            kr0 = step_of(*kr, 0), v0 = step_of(*v, 0), v1 = step_of(*v, 1), R = rows(*st) - 1u, starts = ints(*st), key_starts = ints(*ks), out = ou->data_ptr()] {
+        return wg_latent_prompt(qp, rp, kp, krp, vp, T, N, H, D, q0, q1, r0, r1, k0, k1, kr0, v0, v1, R, starts, key_starts, (float)scale, out, work, bytes, s);
+    }));
+}
+
 // add_instances(handle, texts, args or None, starts address, its rows, stream): sequences of template texts and of
 // argument mappings.  The C call reads the strings in place and without the lock, when other threads may
 // change the caller's lists and dictionaries, and a conversion to bytes may run Python code that does:
@@ -467,7 +590,8 @@ PyObject *set_error(PyObject *, PyObject *cls) {
 #define FAST(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(guarded<name>)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {FAST(fill_masks), FAST(advance), FAST(advance_fill_masks), FAST(decode_step), FAST(forced_bytes), FAST(cache_clear),
                          FAST(apply_mask), FAST(masked_argmax), FAST(masked_topk), FAST(select_tokens), FAST(add_instances), FAST(beam_select), FAST(reorder_rows),
-                         FAST(page_step), FAST(cache_append), FAST(cache_attend),
+                         FAST(page_step), FAST(cache_append), FAST(cache_attend), FAST(rotate), FAST(latent_append), FAST(latent_read), FAST(latent_attend),
+                         FAST(latent_prompt),
                          {"set_error", set_error, METH_O, nullptr}, {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_native", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -1,0 +1,151 @@
+// Rotary positions for gfx950: pairs of a head's numbers turned by the angle position * frequency.
+#include <hip/hip_runtime.h>
+
+#include "wg_launch.h"
+#include "wg_number.h"
+#include "wg_serve.h"
+
+namespace wg {
+
+constexpr uint32_t kRotateThreads = 256;
+
+struct RotateArgs {
+    const void *x[2];                                // queries, keys: [token][head][dim]
+    void *out[2];
+    int64_t x_token[2], x_head[2], out_token[2], out_head[2];              // strides, elements
+    const int32_t *positions;
+    const double *frequencies;
+    float magnitude;
+    uint32_t tokens, heads[2], dim, pairs, per, units, turned_units;       // per: tokens of a workgroup
+};
+
+// Sine and cosine of position * frequency.  The angle is made in 64 bits, in quarters of a turn: at position 2^20 a frequency of 1 in 32 bits would leave an
+// angle that is off by 2^-4.  What is left after the whole quarters, at most an eighth of a turn either way, goes into the functions' series (the first terms that are left out are
+// below 2^-28 there).
+__device__ __forceinline__ float2 cos_sin(int32_t position, double frequency)
+{
+    const double quarters = (double)position * (frequency * 0.63661977236758134308), whole = __builtin_rint(quarters);
+    const float x = (float)((quarters - whole) * 1.57079632679489661923), y = x * x;
+    const uint32_t k = (uint32_t)(int32_t)(whole - 4.0 * __builtin_floor(whole * 0.25));
+    const float s = x + x * y * (-1.f / 6.f + y * (1.f / 120.f + y * (-1.f / 5040.f + y * (1.f / 362880.f))));
+    const float c = 1.f + y * (-0.5f + y * (1.f / 24.f + y * (-1.f / 720.f + y * (1.f / 40320.f + y * (-1.f / 3628800.f)))));
+    const float a = k & 1u ? s : c, b = k & 1u ? c : s;
+    return make_float2(k == 1u || k == 2u ? -a : a, k & 2u ? -b : b);
+}
+
+// kN numbers of a head, 16 bytes of them or one.
+template <typename T, uint32_t kN> struct Numbers;
+template <> struct Numbers<uint16_t, 8> {
+    static __device__ __forceinline__ void load(const uint16_t *p, float (&v)[8])
+    {
+        const Word4 w = *reinterpret_cast<const Word4 *>(p);
+#pragma unroll
+        for (uint32_t i = 0; i < 4u; i++) { v[2u * i] = low(w[i]); v[2u * i + 1u] = high(w[i]); }
+    }
+    static __device__ __forceinline__ void store(uint16_t *p, const float (&v)[8])
+    {
+        *reinterpret_cast<Word4 *>(p) = Word4{pk_bf16(v[0], v[1]), pk_bf16(v[2], v[3]), pk_bf16(v[4], v[5]), pk_bf16(v[6], v[7])};
+    }
+};
+template <> struct Numbers<float, 4> {
+    static __device__ __forceinline__ void load(const float *p, float (&v)[4])
+    {
+        const Float4 w = *reinterpret_cast<const Float4 *>(p);
+#pragma unroll
+        for (uint32_t i = 0; i < 4u; i++) v[i] = w[i];
+    }
+    static __device__ __forceinline__ void store(float *p, const float (&v)[4]) { *reinterpret_cast<Float4 *>(p) = Float4{v[0], v[1], v[2], v[3]}; }
+};
+template <> struct Numbers<uint16_t, 1> {
+    static __device__ __forceinline__ void load(const uint16_t *p, float (&v)[1]) { v[0] = __uint_as_float((uint32_t)*p << 16); }
+    static __device__ __forceinline__ void store(uint16_t *p, const float (&v)[1]) { *p = (uint16_t)pk_bf16(v[0], 0.f); }
+};
+template <> struct Numbers<float, 1> {
+    static __device__ __forceinline__ void load(const float *p, float (&v)[1]) { v[0] = *p; }
+    static __device__ __forceinline__ void store(float *p, const float (&v)[1]) { *p = v[0]; }
+};
+
+// A workgroup makes the sines and cosines of a few tokens once, in LDS, and turns the numbers of all heads with them (heads are dealt out to more workgroups where there
+// are few tokens).  A unit is what a thread takes at once: two pieces of 16 bytes that are turned together (kBeside: one piece of neighbouring pairs), or, behind the pairs, one that is
+// copied.  Bound by memory.
+template <typename T, uint32_t kN, bool kBeside>
+__global__ void __launch_bounds__(kRotateThreads)
+rotate_kernel(const RotateArgs a)
+{
+    extern __shared__ float2 turns[];                // [token][pair]
+    const uint32_t first = blockIdx.x * a.per, n = a.tokens - first < a.per ? a.tokens - first : a.per;
+    for (uint32_t i = threadIdx.x; i < n * a.pairs; i += kRotateThreads) {
+        const uint32_t t = i / a.pairs;
+        const float2 cs = cos_sin(a.positions[first + t], a.frequencies[i - t * a.pairs]);
+        turns[i] = make_float2(cs.x * a.magnitude, cs.y * a.magnitude);
+    }
+    __syncthreads();
+    const uint32_t heads = a.heads[0] + a.heads[1], all = n * heads * a.units;
+    for (uint32_t i = blockIdx.y * kRotateThreads + threadIdx.x; i < all; i += gridDim.y * kRotateThreads) {
+        const uint32_t head_of = i / a.units, u = i - head_of * a.units, t = head_of / heads, h0 = head_of - t * heads;
+        const uint32_t which = h0 >= a.heads[0] ? 1u : 0u, h = which ? h0 - a.heads[0] : h0;
+        const T *x = static_cast<const T *>(a.x[which]) + (int64_t)(first + t) * a.x_token[which] + (int64_t)h * a.x_head[which];
+        T *out = static_cast<T *>(a.out[which]) + (int64_t)(first + t) * a.out_token[which] + (int64_t)h * a.out_head[which];
+        const float2 *turn = turns + t * a.pairs;
+        if (u >= a.turned_units) {                   // behind the pairs
+            const uint32_t d = 2u * a.pairs + (u - a.turned_units) * kN;
+            float v[kN];
+            if (x == out) continue;
+            Numbers<T, kN>::load(x + d, v);
+            Numbers<T, kN>::store(out + d, v);
+        } else if (kBeside && kN > 1u) {
+            float v[kN];
+            Numbers<T, kN>::load(x + u * kN, v);
+#pragma unroll
+            for (uint32_t k = 0; k < kN / 2u; k++) {
+                const float2 cs = turn[u * (kN / 2u) + k];
+                const float p = v[2u * k], q = v[(2u * k + 1u) % kN];
+                v[2u * k] = p * cs.x - q * cs.y; v[(2u * k + 1u) % kN] = p * cs.y + q * cs.x;
+            }
+            Numbers<T, kN>::store(out + u * kN, v);
+        } else {
+            const uint32_t d = kBeside ? 2u * u : u * kN, e = kBeside ? d + 1u : d + a.pairs;
+            float v[kN], w[kN];
+            Numbers<T, kN>::load(x + d, v);
+            Numbers<T, kN>::load(x + e, w);
+#pragma unroll
+            for (uint32_t k = 0; k < kN; k++) {
+                const float2 cs = turn[u * kN + k];
+                const float p = v[k], q = w[k];
+                v[k] = p * cs.x - q * cs.y; w[k] = p * cs.y + q * cs.x;
+            }
+            Numbers<T, kN>::store(out + d, v);
+            Numbers<T, kN>::store(out + e, w);
+        }
+    }
+}
+
+hipError_t launch_rotate(const void *q, const void *k, int dtype, uint32_t tokens, uint32_t q_heads, uint32_t k_heads, uint32_t dim, uint32_t rotated, bool interleaved,
+                         const int64_t (&strides)[8], const int32_t *positions, const double *frequencies, float magnitude, void *q_out, void *k_out, hipStream_t s)
+{
+    RotateArgs a{{q, k}, {q_out, k_out}, {strides[0], strides[2]}, {strides[1], strides[3]}, {strides[4], strides[6]}, {strides[5], strides[7]},
+                 positions, frequencies, magnitude, tokens, {q_heads, k_heads}, dim, rotated / 2u, 0, 0, 0};
+    const bool f32 = dtype == WG_F32;
+    const uint32_t n = f32 ? 4u : 8u, bytes = f32 ? 4u : 2u;
+    // by 16 bytes where all pieces lie at multiples of them
+    bool wide = dim % n == 0 && (interleaved ? rotated % n == 0 : a.pairs % n == 0);
+    for (const int64_t stride : strides) wide = wide && stride % n == 0;
+    for (const void *p : {q, k, static_cast<const void *>(q_out), static_cast<const void *>(k_out)}) wide = wide && reinterpret_cast<uintptr_t>(p) % (n * bytes) == 0;
+    const uint32_t piece = wide ? n : 1u;
+    a.turned_units = wide && interleaved ? rotated / piece : a.pairs / piece;
+    a.units = a.turned_units + (dim - rotated) / piece;
+    const uint32_t fit = kRotateThreads / a.pairs;
+    a.per = fit < 1u ? 1u : fit > 16u ? 16u : fit;
+    if (a.per > tokens) a.per = tokens;
+    // workgroups for each share of tokens: the chip filled, as far as there is something for each thread to do
+    const uint32_t blocks = (tokens + a.per - 1u) / a.per;
+    const uint64_t all = (uint64_t)a.per * (q_heads + k_heads) * a.units;
+    const uint64_t most = (all + kRotateThreads - 1u) / kRotateThreads, want = (1024u + blocks - 1u) / blocks;
+    const dim3 grid(blocks, (uint32_t)(want < most ? want : most)), block(kRotateThreads);
+    const uint32_t lds = a.per * a.pairs * (uint32_t)sizeof(float2);
+    return launch(f32 ? (wide ? (interleaved ? rotate_kernel<float, 4, true> : rotate_kernel<float, 4, false>) : interleaved ? rotate_kernel<float, 1, true> : rotate_kernel<float, 1, false>)
+                  : wide ? (interleaved ? rotate_kernel<uint16_t, 8, true> : rotate_kernel<uint16_t, 8, false>) : interleaved ? rotate_kernel<uint16_t, 1, true> : rotate_kernel<uint16_t, 1, false>,
+                  grid, block, lds, s, nullptr, a);
+}
+
+}  // namespace wg

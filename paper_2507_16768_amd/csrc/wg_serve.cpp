@@ -1,6 +1,7 @@
-// C ABI of beam selection, page tables and the 8-bit paged cache: argument checks and launches.
+// C ABI of beam selection, page tables, rotary positions and the paged caches: argument checks and launches.
 #include <hip/hip_runtime.h>
 
+#include <cmath>
 #include <new>
 #include <string>
 
@@ -29,6 +30,7 @@ template <typename F> int entry(const char *who, F f) {
 // log2 of a page's tokens: 16, 32 or 64; 0 for anything else
 uint32_t shift_of(uint32_t page_tokens) { return page_tokens == 16u ? 4u : page_tokens == 32u ? 5u : page_tokens == 64u ? 6u : 0u; }
 bool dim_ok(uint32_t dim) { return dim == 64u || dim == 128u || dim == 256u; }
+bool latent_ok(uint32_t latent) { return latent == 256u || latent == 512u; }
 // Rows of numbers in 16 bits that are read 16 bytes at a time.
 bool by_sixteen(const void *p, int64_t token, int64_t head) { return reinterpret_cast<uintptr_t>(p) % 16 == 0 && token % 8 == 0 && head % 8 == 0; }
 
@@ -151,6 +153,142 @@ int wg_cache_attend(const void *d_q, uint32_t tokens, uint32_t q_heads, uint32_t
         WG_WANT(aligned(d_workspace, 16), "the workspace must be 16-byte aligned");
         return launch_cache_attend(d_q, tokens, heads, q_heads / heads, dim, q_token_stride, q_head_stride, d_k_cache, d_v_cache, d_k_scale, d_v_scale, pages,
                                    shift_of(page_tokens), d_table, rows, columns, d_lens, d_starts, scale, d_out, d_workspace, static_cast<hipStream_t>(stream));
+    });
+}
+
+int wg_rotate(const void *d_q, const void *d_k, wg_dtype_t dtype, uint32_t tokens, uint32_t q_heads, uint32_t k_heads, uint32_t dim, uint32_t rotated, int interleaved,
+              int64_t q_token_stride, int64_t q_head_stride, int64_t k_token_stride, int64_t k_head_stride, const int32_t *d_positions, const double *d_frequencies,
+              float magnitude, void *d_q_out, int64_t q_out_token_stride, int64_t q_out_head_stride, void *d_k_out, int64_t k_out_token_stride,
+              int64_t k_out_head_stride, void *stream) {
+    return entry("wg_rotate", [&](const char **why) {
+        WG_WANT(d_q && d_positions && d_frequencies && d_q_out && (!k_heads || (d_k && d_k_out)), "null argument");
+        WG_WANT(tokens && q_heads, "no tokens or heads");
+        WG_WANT(dtype == WG_F32 || dtype == WG_BF16, "unknown dtype");
+        WG_WANT(tokens <= 0x7FFFFFFFu && q_heads <= 4096u && k_heads <= 4096u, "tokens above 2^31 - 1 or heads above 4096");
+        WG_WANT(dim <= 1024u && rotated >= 2u && rotated <= dim && rotated % 2u == 0u, "rotated must be even, 2 .. dim, and dim 1024 at most");
+        WG_WANT(magnitude == magnitude && magnitude - magnitude == 0.f, "the magnitude is no number");
+        const uintptr_t size = dtype == WG_F32 ? 4u : 2u;
+        WG_WANT(aligned(d_q, size) && aligned(d_q_out, size) && (!k_heads || (aligned(d_k, size) && aligned(d_k_out, size))) && aligned(d_frequencies, 8), "numbers must lie at multiples of their size");
+        WG_WANT((d_q != d_q_out || (q_token_stride == q_out_token_stride && q_head_stride == q_out_head_stride)) &&
+                (!k_heads || d_k != d_k_out || (k_token_stride == k_out_token_stride && k_head_stride == k_out_head_stride)), "in place the strides must agree");
+        WG_WANT(!k_heads || (d_q_out != d_k_out && d_q_out != d_k && d_k_out != d_q), "queries and keys must not be one another's output");
+        const bool keys = k_heads != 0u;
+        const int64_t strides[8] = {q_token_stride, q_head_stride, keys ? k_token_stride : 0, keys ? k_head_stride : 0,
+                                    q_out_token_stride, q_out_head_stride, keys ? k_out_token_stride : 0, keys ? k_out_head_stride : 0};
+        return launch_rotate(d_q, keys ? d_k : nullptr, dtype, tokens, q_heads, k_heads, dim, rotated, interleaved != 0, strides, d_positions, d_frequencies, magnitude, d_q_out,
+                             keys ? d_k_out : nullptr, static_cast<hipStream_t>(stream));
+    });
+}
+
+int wg_rotary_frequencies(double *host_out, uint32_t rotated, double base, double factor, double original, double low, double high, int log_ramp) {
+    return entry("wg_rotary_frequencies", [&](const char **why) {
+        WG_WANT(host_out, "null argument");
+        WG_WANT(rotated >= 2u && rotated % 2u == 0u && rotated <= 1024u, "rotated must be even, 2 .. 1024");
+        WG_WANT(base > 0.0 && base - base == 0.0 && factor >= 1.0 && factor - factor == 0.0, "base must be above 0 and factor 1 at least");
+        const bool all = low > 0.0 && std::isinf(low);
+        WG_WANT(factor == 1.0 || all || (original > 0.0 && original - original == 0.0 && low >= 0.0 && high > low && high - high == 0.0 && (!log_ramp || low > 0.0)),
+                "a ramp wants original above 0 and 0 <= low < high (0 < low over the logarithm)");
+        for (uint32_t i = 0; i < rotated / 2u; i++) {
+            const double f = std::pow(base, -2.0 * i / rotated);
+            double kept = 1.0;
+            if (factor != 1.0) {
+                const double turns = original * f / 6.28318530717958647693;
+                kept = all ? 0.0 : log_ramp ? std::log(turns / low) / std::log(high / low) : (turns - low) / (high - low);
+                kept = kept < 0.0 ? 0.0 : kept > 1.0 ? 1.0 : kept;
+            }
+            host_out[i] = kept * f + (1.0 - kept) * f / factor;
+        }
+        return hipSuccess;
+    });
+}
+
+int wg_latent_append(const void *d_c, const void *d_r, uint32_t tokens, uint32_t latent, int64_t c_token_stride, int64_t r_token_stride, const int32_t *d_slots,
+                     const int32_t *d_origins, void *d_c_cache, void *d_r_cache, float *d_c_scale, uint32_t pages, uint32_t page_tokens, void *stream) {
+    return entry("wg_latent_append", [&](const char **why) {
+        WG_WANT(d_c && d_r && d_slots && d_c_cache && d_r_cache, "null argument");
+        WG_WANT(tokens && pages, "no tokens or pages");
+        WG_WANT(tokens <= 1u << 29, "tokens above 2^29");
+        WG_WANT(latent_ok(latent), "latent must be 256 or 512");
+        WG_WANT(shift_of(page_tokens), "page_tokens must be 16, 32 or 64");
+        WG_WANT((uint64_t)pages * page_tokens <= 0x7FFFFFFFull, "slots above 2^31 - 1");
+        WG_WANT(by_sixteen(d_c, c_token_stride, 0) && by_sixteen(d_r, r_token_stride, 0), "vectors and shared keys must lie at multiples of 16 bytes");
+        WG_WANT(aligned(d_c_cache, 16) && aligned(d_r_cache, 16) && aligned(d_c_scale, 4), "the cache must be 16-byte aligned");
+        return launch_latent_append(d_c, d_r, tokens, latent, c_token_stride, r_token_stride, d_slots, d_origins, d_c_cache, d_r_cache, d_c_scale, pages, shift_of(page_tokens),
+                                    static_cast<hipStream_t>(stream));
+    });
+}
+
+int wg_latent_read(const void *d_c_cache, const void *d_r_cache, const float *d_c_scale, uint32_t latent, uint32_t pages, uint32_t page_tokens, const int32_t *d_table,
+                   uint32_t rows, uint32_t columns, const int32_t *d_starts, uint32_t tokens, void *d_c_out, int64_t c_token_stride, void *d_r_out, int64_t r_token_stride, void *stream) {
+    return entry("wg_latent_read", [&](const char **why) {
+        WG_WANT(d_c_cache && d_r_cache && d_table && d_starts && d_c_out && d_r_out, "null argument");
+        WG_WANT(tokens && rows && columns && pages, "no tokens, rows, columns or pages");
+        WG_WANT(tokens <= 0x7FFFFFFFu && rows <= kMostRows, "tokens above 2^31 - 1 or rows above 65535");
+        WG_WANT(latent_ok(latent), "latent must be 256 or 512");
+        WG_WANT(shift_of(page_tokens), "page_tokens must be 16, 32 or 64");
+        WG_WANT((uint64_t)columns * page_tokens <= 0x7FFFFFFFull && (uint64_t)pages * page_tokens <= 0x7FFFFFFFull, "tokens above 2^31 - 1");
+        WG_WANT(by_sixteen(d_c_out, c_token_stride, 0) && by_sixteen(d_r_out, r_token_stride, 0), "vectors and shared keys must lie at multiples of 16 bytes");
+        WG_WANT(aligned(d_c_cache, 16) && aligned(d_r_cache, 16) && aligned(d_c_scale, 4), "the cache must be 16-byte aligned");
+        return launch_latent_read(d_c_cache, d_r_cache, d_c_scale, latent, pages, shift_of(page_tokens), d_table, rows, columns, d_starts, tokens, d_c_out, c_token_stride, d_r_out,
+                                  r_token_stride, static_cast<hipStream_t>(stream));
+    });
+}
+
+uint64_t wg_latent_attend_workspace(uint32_t tokens, uint32_t rows, uint32_t heads, uint32_t latent, uint32_t columns, uint32_t page_tokens) {
+    if (!tokens || !rows || !heads || !columns || !shift_of(page_tokens)) return 0;
+    const uint64_t splits = latent_attend_splits(tokens, rows, heads, columns, shift_of(page_tokens));
+    return splits < 2u ? 0u : ((uint64_t)tokens * heads * splits * (latent + 2u) + tokens) * 4u;
+}
+
+int wg_latent_attend(const void *d_q_c, const void *d_q_r, uint32_t tokens, uint32_t heads, uint32_t latent, int64_t c_token_stride, int64_t c_head_stride, int64_t r_token_stride,
+                     int64_t r_head_stride, const void *d_c_cache, const void *d_r_cache, const float *d_c_scale, uint32_t pages, uint32_t page_tokens, const int32_t *d_table, uint32_t rows,
+                     uint32_t columns, const int32_t *d_lens, const int32_t *d_starts, float scale, void *d_out, void *d_workspace, uint64_t workspace_bytes, void *stream) {
+    return entry("wg_latent_attend", [&](const char **why) {
+        WG_WANT(d_q_c && d_q_r && d_c_cache && d_r_cache && d_table && d_lens && d_starts && d_out, "null argument");
+        WG_WANT(tokens && rows && columns && pages && heads, "no tokens, rows, columns, pages or heads");
+        WG_WANT(tokens <= 0x7FFFFFFFu && rows <= kMostRows && heads <= 4096u && (uint64_t)tokens * heads <= 0x7FFFFFFFull, "too many tokens, rows or heads");
+        WG_WANT(latent_ok(latent), "latent must be 256 or 512");
+        WG_WANT(shift_of(page_tokens), "page_tokens must be 16, 32 or 64");
+        WG_WANT((uint64_t)columns * page_tokens <= 0x7FFFFFFFull && (uint64_t)pages * page_tokens <= 0x7FFFFFFFull, "tokens above 2^31 - 1");
+        WG_WANT(latent_attend_fits(tokens, rows, heads), "too many tokens for one launch");
+        WG_WANT(by_sixteen(d_q_c, c_token_stride, c_head_stride) && by_sixteen(d_q_r, r_token_stride, r_head_stride), "queries must lie at multiples of 16 bytes");
+        WG_WANT(aligned(d_c_cache, 16) && aligned(d_r_cache, 16) && aligned(d_c_scale, 4) && aligned(d_out, 16), "the cache and the output must be 16-byte aligned");
+        WG_WANT(scale == scale && scale - scale == 0.f, "the scale is no number");
+        const uint64_t need = wg_latent_attend_workspace(tokens, rows, heads, latent, columns, page_tokens);
+        WG_WANT(!need || (d_workspace && workspace_bytes >= need), "the workspace is too small (wg_latent_attend_workspace)");
+        WG_WANT(aligned(d_workspace, 16), "the workspace must be 16-byte aligned");
+        const int64_t strides[4] = {c_token_stride, c_head_stride, r_token_stride, r_head_stride};
+        return launch_latent_attend(d_q_c, d_q_r, tokens, heads, latent, strides, d_c_cache, d_r_cache, d_c_scale, pages, shift_of(page_tokens), d_table, rows, columns, d_lens, d_starts,
+                                    scale, d_out, d_workspace, static_cast<hipStream_t>(stream));
+    });
+}
+
+uint64_t wg_latent_prompt_workspace(uint32_t tokens, uint32_t rows, uint32_t heads, uint32_t dim, uint32_t keys) {
+    if (!tokens || !rows || !heads || !keys) return 0;
+    const uint64_t splits = latent_prompt_splits(tokens, rows, heads, keys);
+    return splits < 2u ? 0u : ((uint64_t)tokens * heads * splits * (dim + 2u) + tokens) * 4u;
+}
+
+int wg_latent_prompt(const void *d_q_n, const void *d_q_r, const void *d_k_n, const void *d_k_r, const void *d_v, uint32_t tokens, uint32_t keys, uint32_t heads, uint32_t dim,
+                     int64_t q_n_token_stride, int64_t q_n_head_stride, int64_t q_r_token_stride, int64_t q_r_head_stride, int64_t k_n_token_stride, int64_t k_n_head_stride,
+                     int64_t k_r_token_stride, int64_t v_token_stride, int64_t v_head_stride, uint32_t rows, const int32_t *d_starts, const int32_t *d_key_starts, float scale,
+                     void *d_out, void *d_workspace, uint64_t workspace_bytes, void *stream) {
+    return entry("wg_latent_prompt", [&](const char **why) {
+        WG_WANT(d_q_n && d_q_r && d_k_n && d_k_r && d_v && d_starts && d_key_starts && d_out, "null argument");
+        WG_WANT(tokens && rows && keys && heads, "no tokens, rows, keys or heads");
+        WG_WANT(tokens <= 0x7FFFFFFFu && keys <= 0x7FFFFFFFu && rows <= kMostRows && heads <= 4096u && (uint64_t)tokens * heads <= 0x7FFFFFFFull, "too many tokens, keys, rows or heads");
+        WG_WANT(dim == 64u || dim == 128u, "dim must be 64 or 128");
+        WG_WANT(latent_prompt_fits(tokens, rows), "too many tokens for one launch");
+        WG_WANT(by_sixteen(d_q_n, q_n_token_stride, q_n_head_stride) && by_sixteen(d_q_r, q_r_token_stride, q_r_head_stride) && by_sixteen(d_k_n, k_n_token_stride, k_n_head_stride) &&
+                by_sixteen(d_k_r, k_r_token_stride, 0) && by_sixteen(d_v, v_token_stride, v_head_stride), "queries, keys and values must lie at multiples of 16 bytes");
+        WG_WANT(aligned(d_out, 16), "the output must be 16-byte aligned");
+        WG_WANT(scale == scale && scale - scale == 0.f, "the scale is no number");
+        const uint64_t need = wg_latent_prompt_workspace(tokens, rows, heads, dim, keys);
+        WG_WANT(!need || (d_workspace && workspace_bytes >= need), "the workspace is too small (wg_latent_prompt_workspace)");
+        WG_WANT(aligned(d_workspace, 16), "the workspace must be 16-byte aligned");
+        const int64_t strides[9] = {q_n_token_stride, q_n_head_stride, q_r_token_stride, q_r_head_stride, k_n_token_stride, k_n_head_stride, k_r_token_stride, v_token_stride, v_head_stride};
+        return launch_latent_prompt(d_q_n, d_q_r, d_k_n, d_k_r, d_v, tokens, keys, heads, dim, strides, rows, d_starts, d_key_starts, scale, d_out, d_workspace,
+                                    static_cast<hipStream_t>(stream));
     });
 }
 
