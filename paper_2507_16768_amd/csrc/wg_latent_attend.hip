@@ -93,21 +93,33 @@ __device__ __forceinline__ Word2 wider(uint32_t four, float scale)
     return Word2{__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(four, scale, false)),
                  __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(four, scale, true))};
 }
-// Whether one of eight numbers is none or infinite; the numbers with zeros in their place; ones where such are.
-__device__ __forceinline__ uint32_t odd_bits(uint32_t two) { return (((two & 0x7F807F80u) + 0x00800080u) & 0x80008000u); }      // (an exponent of ones carries into the sign's place)
+// Numbers that are none or infinite, as bits: an exponent of ones carries into the sign's place.
+__device__ __forceinline__ uint32_t odd_bits(uint32_t two) { return ((two & 0x7F807F80u) + 0x00800080u) & 0x80008000u; }
 __device__ __forceinline__ bool any_odd(Word4 v) { return (odd_bits(v[0]) | odd_bits(v[1]) | odd_bits(v[2]) | odd_bits(v[3])) != 0u; }
-__device__ __forceinline__ void split_odd(Half8 x, Half8 *clean, Half8 *odd)
+// Eight numbers of key `key` with zeros in the place of those; `from` keeps the first key that has one.
+__device__ __forceinline__ Word4 without_odd(Word4 v, uint32_t key, uint32_t *from)
 {
-    Word4 v = __builtin_bit_cast(Word4, x), o;
+    if (any_odd(v)) atomicMin(from, key);
+#pragma unroll
+    for (uint32_t w = 0; w < 4u; w++) { const uint32_t b = odd_bits(v[w]); v[w] &= ~(b | (b - (b >> 15))); }
+    return v;
+}
+// The same for each dim by itself, from dim d on.
+__device__ __forceinline__ Word4 without_odd_dims(Word4 v, uint32_t key, uint32_t d, uint32_t *from)
+{
+    if (!any_odd(v)) return v;
 #pragma unroll
     for (uint32_t w = 0; w < 4u; w++) {
-        const uint32_t b = odd_bits(v[w]), mask = b | (b - (b >> 15));
-        v[w] &= ~mask;
-        o[w] = mask & 0x3F803F80u;
+        const uint32_t b = odd_bits(v[w]);
+        if (b & 0x8000u) atomicMin(from + d + 2u * w, key);
+        if (b >> 31) atomicMin(from + d + 2u * w + 1u, key);
+        v[w] &= ~(b | (b - (b >> 15)));
     }
-    *clean = __builtin_bit_cast(Half8, v);
-    *odd = __builtin_bit_cast(Half8, o);
+    return v;
 }
+
+// What is read in the place of a key that there is none of.
+__device__ __attribute__((aligned(16))) const uint8_t kZeros[1024] = {};
 
 // What a wavefront holds of its kM tiles of 16 queries: of query m of each, the base and its own part of the sum, and outputs, dims 4 g .. 4 g + 3 of each of kParts.
 template <uint32_t kM, uint32_t kParts>
@@ -200,18 +212,18 @@ __device__ __forceinline__ uint32_t cached_tokens(const LatentAttendArgs &a, uin
     return l < most ? l : most;
 }
 
-template <uint32_t kC, bool kBytes, uint32_t kM, uint32_t kGroups>
-__global__ void __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(1, 1)))
+template <uint32_t kC, bool kBytes, uint32_t kM, uint32_t kGroups, uint32_t kW>
+__global__ void __launch_bounds__(kW * 64u) __attribute__((amdgpu_waves_per_eu(kW / 4u, kW / 4u)))
 latent_attend_kernel(const LatentAttendArgs a)
 {
-    constexpr uint32_t kKeyGroups = kWaves / kGroups, kKeys = 32u * kKeyGroups, kRows = 16u * kM * kGroups;
+    constexpr uint32_t kKeyGroups = kW / kGroups, kKeys = 32u * kKeyGroups, kRows = 16u * kM * kGroups;
     constexpr uint32_t kSteps = (kC + kTop) / 32u, kParts = kC / 16u, kPitch = kC + kTop + 8u;
-    constexpr uint32_t kRow = kC * (kBytes ? 1u : 2u), kPer = 1024u / kRow, kStage = kKeys / kWaves;      // bytes of a vector; keys of a wavefront's load; keys that it brings
-    constexpr uint32_t kLoads = kStage / kPer, kTops = kStage / 8u;
-    constexpr uint32_t kJoinPitch = kC + 4u, kTileBytes = kKeys * kPitch * 2u, kJoinBytes = kKeyGroups > 1u ? kWaves * 16u * kJoinPitch * 4u : 0u;
+    constexpr uint32_t kRow = kC * (kBytes ? 1u : 2u), kPer = 1024u / kRow, kStage = kKeys / kW;          // bytes of a vector; keys of a wavefront's load; keys that it brings
+    constexpr uint32_t kLoads = kStage / kPer, kTops = (kStage + 7u) / 8u;
+    constexpr uint32_t kJoinPitch = kC + 4u, kTileBytes = kKeys * kPitch * 2u, kJoinBytes = kKeyGroups > 1u ? kW * 16u * kJoinPitch * 4u : 0u;
     __shared__ __attribute__((aligned(16))) uint8_t room[kTileBytes > kJoinBytes ? kTileBytes : kJoinBytes];
-    __shared__ uint32_t odd[2];
-    __shared__ float join_base[kWaves][16], join_sum[kWaves][16];
+    __shared__ uint32_t odd_from;                                          // the first key with a number that is none, of those that some rows do not see
+    __shared__ float join_base[kW][16], join_sum[kW][16];
     uint16_t *keys = reinterpret_cast<uint16_t *>(room);
     const uint32_t tid = threadIdx.x, lane = tid & 63u, wave = __builtin_amdgcn_readfirstlane(tid >> 6), m = lane & 15u, g = lane >> 4;
     const uint32_t split = blockIdx.y, P = 1u << a.shift, heads = a.of.heads;
@@ -231,6 +243,35 @@ latent_attend_kernel(const LatentAttendArgs a)
     const uint32_t seen_least = seen_by(t.first), seen_most = seen_by(t.last - 1u);
     const uint32_t from = split * per * kAttendBlock, to0 = shares > 1u ? from + per * kAttendBlock : seen_most, to = to0 < seen_most ? to0 : seen_most;
 
+    // The wavefront's keys of a block: lane i knows the slot of the i-th.
+    auto slot_of = [&](uint32_t block) {
+        const uint32_t at = block + wave * kStage + lane;
+        if (lane >= kStage || at >= to) return kNone;
+        const uint32_t page = (uint32_t)a.table[(size_t)t.row * a.columns + (at >> a.shift)];
+        return page < a.pages ? page << a.shift | (at & (P - 1u)) : kNone;
+    };
+    Word4 raw[kLoads], tops[kTops];
+    float scales[kBytes ? kLoads : 1u];
+    auto fetch = [&](uint32_t slots) {
+#pragma unroll
+        for (uint32_t i = 0; i < kLoads; i++) {
+            const uint32_t slot = kPer == 1u ? __builtin_amdgcn_readlane(slots, i) : __shfl(slots, i * kPer + lane / (64u / kPer));
+            const uint8_t *row = slot != kNone ? a.c_cache + (size_t)slot * kRow : kZeros;
+            raw[i] = *reinterpret_cast<const Word4 *>(row + lane % (64u / kPer) * 16u);
+            if (kBytes) scales[i % (kBytes ? kLoads : 1u)] = *(slot != kNone ? a.scale + slot : reinterpret_cast<const float *>(kZeros));
+        }
+#pragma unroll
+        for (uint32_t i = 0; i < kTops; i++) {
+            const uint32_t slot = __shfl(slots, i * 8u + lane / 8u);
+            tops[i] = *reinterpret_cast<const Word4 *>((slot != kNone ? a.r_cache + (size_t)slot * kTop : reinterpret_cast<const uint16_t *>(kZeros)) + lane % 8u * 8u);
+        }
+    };
+    uint32_t ahead = 0;
+    if (from < to) {
+        fetch(slot_of(from));
+        ahead = slot_of(from + kKeys);
+    }
+
     // queries: a row behind the last is the last again, and is not stored
     const uint32_t group = wave % kGroups, key_group = wave / kGroups;
     Half8 q[kM][kSteps];
@@ -246,65 +287,29 @@ latent_attend_kernel(const LatentAttendArgs a)
     }
     Sums<kM, kParts> sums;
     sums.clear();
-
-    // The wavefront's keys of a block: lane i knows the slot of the i-th.
-    auto slot_of = [&](uint32_t block) {
-        const uint32_t at = block + wave * kStage + lane;
-        if (lane >= kStage || at >= to) return kNone;
-        const uint32_t page = (uint32_t)a.table[(size_t)t.row * a.columns + (at >> a.shift)];
-        return page < a.pages ? page << a.shift | (at & (P - 1u)) : kNone;
-    };
-    Word4 raw[kLoads], tops[kTops];
-    float scales[kBytes ? kLoads : 1u];
-    auto fetch = [&](uint32_t slots) {
-#pragma unroll
-        for (uint32_t i = 0; i < kLoads; i++) {
-            const uint32_t slot = kPer == 1u ? __builtin_amdgcn_readlane(slots, i) : __shfl(slots, i * kPer + lane / (64u / kPer));
-            raw[i] = Word4{0u, 0u, 0u, 0u};
-            if (kBytes) scales[i % (kBytes ? kLoads : 1u)] = 1.f;
-            if (slot != kNone) {
-                raw[i] = *reinterpret_cast<const Word4 *>(a.c_cache + (size_t)slot * kRow + lane % (64u / kPer) * 16u);
-                if (kBytes) scales[i % (kBytes ? kLoads : 1u)] = a.scale[slot];
-            }
-        }
-#pragma unroll
-        for (uint32_t i = 0; i < kTops; i++) {
-            const uint32_t slot = __shfl(slots, i * 8u + lane / 8u);
-            tops[i] = Word4{0u, 0u, 0u, 0u};
-            if (slot != kNone) tops[i] = *reinterpret_cast<const Word4 *>(a.r_cache + (size_t)slot * kTop + lane % 8u * 8u);
-        }
-    };
-    if (tid == 0u) { odd[0] = 0u; odd[1] = 0u; }
+    if (tid == 0u) odd_from = kNone;
     __syncthreads();
-    uint32_t ahead = 0;
-    if (from < to) {
-        fetch(slot_of(from));
-        ahead = slot_of(from + kKeys);
-    }
-    uint32_t turn = 0;
-    for (uint32_t block = from; block < to; block += kKeys, turn ^= 1u) {
+    for (uint32_t block = from; block < to; block += kKeys) {
         const bool partly = block + kKeys > seen_least;                    // some of the tile's rows do not see all of the block's keys
-        bool found = false;
 #pragma unroll
         for (uint32_t i = 0; i < kLoads; i++) {
             const uint32_t key = wave * kStage + i * kPer + lane / (64u / kPer), at = lane % (64u / kPer);
             if (kBytes) {
                 const float scale = scales[i % (kBytes ? kLoads : 1u)];
                 const Word2 w0 = wider(raw[i][0], scale), w1 = wider(raw[i][1], scale), w2 = wider(raw[i][2], scale), w3 = wider(raw[i][3], scale);
-                const Word4 x{w0[0], w0[1], w1[0], w1[1]}, y{w2[0], w2[1], w3[0], w3[1]};
+                Word4 x{w0[0], w0[1], w1[0], w1[1]}, y{w2[0], w2[1], w3[0], w3[1]};
+                if (partly) { x = without_odd(x, block + key, &odd_from); y = without_odd(y, block + key, &odd_from); }
                 Word4 *put = reinterpret_cast<Word4 *>(keys + key * kPitch + at * 16u);
                 put[0] = x; put[1] = y;
-                if (partly) found = found || any_odd(x) || any_odd(y);
             } else {
+                if (partly) raw[i] = without_odd(raw[i], block + key, &odd_from);
                 *reinterpret_cast<Word4 *>(keys + key * kPitch + at * 8u) = raw[i];
-                if (partly) found = found || any_odd(raw[i]);
             }
         }
+        if (kStage >= 8u || lane < kStage * 8u)
 #pragma unroll
-        for (uint32_t i = 0; i < kTops; i++) *reinterpret_cast<Word4 *>(keys + (wave * kStage + i * 8u + lane / 8u) * kPitch + kC + lane % 8u * 8u) = tops[i];
-        if (found) odd[turn] = 1u;
+            for (uint32_t i = 0; i < kTops; i++) *reinterpret_cast<Word4 *>(keys + (wave * kStage + i * 8u + lane / 8u) * kPitch + kC + lane % 8u * 8u) = tops[i];
         __syncthreads();
-        if (tid == 0u) odd[turn ^ 1u] = 0u;
         if (block + kKeys < to) {
             fetch(ahead);
             ahead = slot_of(block + 2u * kKeys);
@@ -339,41 +344,19 @@ latent_attend_kernel(const LatentAttendArgs a)
             Half8 p[1][kM];
             sums.template weigh<1>(s, p);
             const uint16_t *column = mine + (g * 8u + m / 4u) * kPitch + m % 4u * 4u;
-            if (__builtin_expect(!odd[turn], 1)) {
 #pragma unroll
-                for (uint32_t d = 0; d < kParts; d++) {
-                    const Half8 v = both(column_of(column + d * 16u), column_of(column + 4u * kPitch + d * 16u));
+            for (uint32_t d = 0; d < kParts; d++) {
+                const Half8 v = both(column_of(column + d * 16u), column_of(column + 4u * kPitch + d * 16u));
 #pragma unroll
-                    for (uint32_t n = 0; n < kM; n++) sums.acc[d][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, p[0][n], sums.acc[d][n], 0, 0, 0);
-                }
-            } else {
-                // An infinity or a NaN among vectors that some of the rows do not see: it makes none of the outputs of those that do, and is nothing to the others.
-                Half8 one[kM];
-#pragma unroll
-                for (uint32_t n = 0; n < kM; n++) {
-                    Word4 w;
-#pragma unroll
-                    for (uint32_t j = 0; j < 4u; j++) w[j] = (at + 2u * j < sees[n] ? 0x3F80u : 0u) | (at + 2u * j + 1u < sees[n] ? 0x3F800000u : 0u);
-                    one[n] = __builtin_bit_cast(Half8, w);
-                }
-#pragma unroll
-                for (uint32_t d = 0; d < kParts; d++) {
-                    Half8 v, o;
-                    split_odd(both(column_of(column + d * 16u), column_of(column + 4u * kPitch + d * 16u)), &v, &o);
-#pragma unroll
-                    for (uint32_t n = 0; n < kM; n++) {
-                        sums.acc[d][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, p[0][n], sums.acc[d][n], 0, 0, 0);
-                        const Float4 hits = __builtin_amdgcn_mfma_f32_16x16x32_bf16(o, one[n], Float4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
-#pragma unroll
-                        for (uint32_t e = 0; e < 4u; e++) sums.acc[d][n][e] = hits[e] > 0.f ? __builtin_nanf("") : sums.acc[d][n][e];
-                    }
-                }
+                for (uint32_t n = 0; n < kM; n++) sums.acc[d][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, p[0][n], sums.acc[d][n], 0, 0, 0);
             }
         }
         __syncthreads();
     }
 
-    // out: this share's output by itself, or the whole
+    // out: this share's output by itself, or the whole.  (Numbers that are none have been left out of the sums of rows that see only some of a block's keys: what a row that sees them makes of them
+    // is none.)
+    const uint32_t odd = odd_from;
     auto put = [&](uint32_t i, uint32_t d, Float4 v) {                     // dims d .. d + 3 of query row i
         const size_t at = (size_t)t.begin * heads + i;
         if (shares > 1u) *reinterpret_cast<Float4 *>(a.partial + (at * a.of.splits + split) * kC + d) = v;
@@ -385,7 +368,8 @@ latent_attend_kernel(const LatentAttendArgs a)
     };
 #pragma unroll
     for (uint32_t n = 0; n < kM; n++) {
-        const float sum = sums.whole_sum(n);
+        float sum = sums.whole_sum(n);
+        if (odd < sees[n]) sum = __builtin_nanf("");
         const uint32_t own = t.first + (group * kM + n) * 16u + m;
         if (kKeyGroups == 1u) {
             const bool any = sees[n] > from;
@@ -404,7 +388,7 @@ latent_attend_kernel(const LatentAttendArgs a)
         if (g == 0u) { join_base[wave][m] = sums.base[n]; join_sum[wave][m] = sum; }
         __syncthreads();
         // rows of all groups, four dims to a thread
-        for (uint32_t u = tid; u < kGroups * 16u * (kC / 4u); u += kThreads) {
+        for (uint32_t u = tid; u < kGroups * 16u * (kC / 4u); u += kW * 64u) {
             const uint32_t d = u % (kC / 4u) * 4u, row = u / (kC / 4u) % 16u, of = u / (kC / 4u) / 16u, i = t.first + (of * kM + n) * 16u + row;
             if (i >= t.last) continue;
             float base = -__builtin_inff(), total = 0.f;
@@ -537,7 +521,7 @@ static hipError_t launch_latent(const LatentAttendArgs &a, hipStream_t s)
 {
     const uint32_t rows = attend_rows(a.of.tokens, a.of.rows, a.of.heads);
     const dim3 grid((uint32_t)((uint64_t)a.of.tokens * a.of.heads / rows) + a.of.rows, a.of.splits);
-    const hipError_t e = launch(rows == 128u ? latent_attend_kernel<kC, kBytes, 2, 4> : latent_attend_kernel<kC, kBytes, 1, 1>, grid, dim3(kThreads), 0, s, nullptr, a);
+    const hipError_t e = launch(rows == 128u ? latent_attend_kernel<kC, kBytes, 1, 8, 8> : latent_attend_kernel<kC, kBytes, 1, 1, 4>, grid, dim3(rows == 128u ? 512u : 256u), 0, s, nullptr, a);
     if (e != hipSuccess || a.of.splits == 1u) return e;
     return launch_join<kC>(JoinArgs{a.partial, a.ends, a.shares, a.of.starts + a.of.rows, a.out, a.of.heads, a.of.splits}, a.of.tokens, s);
 }
@@ -580,13 +564,13 @@ __device__ __forceinline__ uint32_t keys_of(const LatentPromptArgs &a, uint32_t 
 }
 
 template <uint32_t kD>
-__global__ void __launch_bounds__(kThreads)
+__global__ void __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2)))
 latent_prompt_kernel(const LatentPromptArgs a)
 {
     constexpr uint32_t kM = 2u, kSteps = (kD + kTop) / 32u, kParts = kD / 16u, kPitch = kD + kTop + 8u, kValuePitch = kD + 8u, kStage = kPromptKeys / kWaves;
     constexpr uint32_t kPer = 512u / kD, kLoads = kStage / kPer, kTops = kStage / 8u;
     __shared__ __attribute__((aligned(16))) uint16_t keys[kPromptKeys * kPitch], values[kPromptKeys * kValuePitch];
-    __shared__ uint32_t odd[2];
+    __shared__ uint32_t odd_from[kD], any_from;       // of each dim, the first key whose value is none, of those that some rows do not see; the first of all
     const uint32_t tid = threadIdx.x, lane = tid & 63u, wave = __builtin_amdgcn_readfirstlane(tid >> 6), m = lane & 15u, g = lane >> 4;
     const uint32_t head = blockIdx.y, split = blockIdx.z;
     Tile t;
@@ -638,25 +622,25 @@ latent_prompt_kernel(const LatentPromptArgs a)
             if (key < to) tops[i] = *reinterpret_cast<const Word4 *>(k_r + (int64_t)key * a.kr_token + lane % 8u * 8u);
         }
     };
-    if (tid == 0u) { odd[0] = 0u; odd[1] = 0u; }
+    if (tid < kD) odd_from[tid] = kNone;
+    if (tid == 0u) any_from = kNone;
     __syncthreads();
     if (from < to) fetch(from);
-    uint32_t turn = 0;
-    for (uint32_t block = from; block < to; block += kPromptKeys, turn ^= 1u) {
+    for (uint32_t block = from; block < to; block += kPromptKeys) {
         const bool partly = block + kPromptKeys > seen_least;
-        bool found = false;
 #pragma unroll
         for (uint32_t i = 0; i < kLoads; i++) {
             const uint32_t key = wave * kStage + i * kPer + lane / (64u / kPer), d = lane % (64u / kPer) * 8u;
+            if (partly && any_odd(raw_v[i])) {
+                atomicMin(&any_from, block + key);
+                raw_v[i] = without_odd_dims(raw_v[i], block + key, d, odd_from);
+            }
             *reinterpret_cast<Word4 *>(keys + key * kPitch + d) = raw[i];
             *reinterpret_cast<Word4 *>(values + key * kValuePitch + d) = raw_v[i];
-            if (partly) found = found || any_odd(raw_v[i]);
         }
 #pragma unroll
         for (uint32_t i = 0; i < kTops; i++) *reinterpret_cast<Word4 *>(keys + (wave * kStage + i * 8u + lane / 8u) * kPitch + kD + lane % 8u * 8u) = tops[i];
-        if (found) odd[turn] = 1u;
         __syncthreads();
-        if (tid == 0u) odd[turn ^ 1u] = 0u;
         if (block + kPromptKeys < to) fetch(block + kPromptKeys);
         Float4 score[2][2][kM];
         const uint16_t *row = keys + (m / 4u * 8u + m % 4u) * kPitch + g * 8u;
@@ -691,43 +675,15 @@ latent_prompt_kernel(const LatentPromptArgs a)
         Half8 p[2][kM];
         sums.template weigh<2>(s, p);
         const uint16_t *column = values + (g * 8u + m / 4u) * kValuePitch + m % 4u * 4u;
-        if (__builtin_expect(!odd[turn], 1)) {
 #pragma unroll
-            for (uint32_t d = 0; d < kParts; d++)
+        for (uint32_t d = 0; d < kParts; d++)
 #pragma unroll
-                for (uint32_t k = 0; k < 2u; k++) {
-                    const uint16_t *of = column + k * 32u * kValuePitch + d * 16u;
-                    const Half8 x = both(column_of(of), column_of(of + 4u * kValuePitch));
+            for (uint32_t k = 0; k < 2u; k++) {
+                const uint16_t *of = column + k * 32u * kValuePitch + d * 16u;
+                const Half8 x = both(column_of(of), column_of(of + 4u * kValuePitch));
 #pragma unroll
-                    for (uint32_t n = 0; n < kM; n++) sums.acc[d][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, p[k][n], sums.acc[d][n], 0, 0, 0);
-                }
-        } else {
-            Half8 one[2][kM];
-#pragma unroll
-            for (uint32_t k = 0; k < 2u; k++)
-#pragma unroll
-                for (uint32_t n = 0; n < kM; n++) {
-                    Word4 w;
-#pragma unroll
-                    for (uint32_t j = 0; j < 4u; j++) w[j] = (at + k * 32u + 2u * j < sees[n] ? 0x3F80u : 0u) | (at + k * 32u + 2u * j + 1u < sees[n] ? 0x3F800000u : 0u);
-                    one[k][n] = __builtin_bit_cast(Half8, w);
-                }
-#pragma unroll
-            for (uint32_t d = 0; d < kParts; d++)
-#pragma unroll
-                for (uint32_t k = 0; k < 2u; k++) {
-                    const uint16_t *of = column + k * 32u * kValuePitch + d * 16u;
-                    Half8 x, o;
-                    split_odd(both(column_of(of), column_of(of + 4u * kValuePitch)), &x, &o);
-#pragma unroll
-                    for (uint32_t n = 0; n < kM; n++) {
-                        sums.acc[d][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, p[k][n], sums.acc[d][n], 0, 0, 0);
-                        const Float4 hits = __builtin_amdgcn_mfma_f32_16x16x32_bf16(o, one[k][n], Float4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
-#pragma unroll
-                        for (uint32_t e = 0; e < 4u; e++) sums.acc[d][n][e] = hits[e] > 0.f ? __builtin_nanf("") : sums.acc[d][n][e];
-                    }
-                }
-        }
+                for (uint32_t n = 0; n < kM; n++) sums.acc[d][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, p[k][n], sums.acc[d][n], 0, 0, 0);
+            }
         __syncthreads();
     }
 #pragma unroll
@@ -740,7 +696,10 @@ latent_prompt_kernel(const LatentPromptArgs a)
         const size_t at = (size_t)(t.begin + own) * a.of.heads + head;
 #pragma unroll
         for (uint32_t d = 0; d < kParts; d++) {
-            const Float4 v = sums.acc[d][n] * by;
+            Float4 v = sums.acc[d][n] * by;
+            if (any_from != kNone)
+#pragma unroll
+                for (uint32_t e = 0; e < 4u; e++) v[e] = odd_from[d * 16u + g * 4u + e] < sees[n] ? __builtin_nanf("") : v[e];
             if (shares > 1u) *reinterpret_cast<Float4 *>(a.partial + (at * a.of.splits + split) * kD + d * 16u + g * 4u) = v;
             else *reinterpret_cast<Word2 *>(a.out + at * kD + d * 16u + g * 4u) = Word2{pk_bf16(v[0], v[1]), pk_bf16(v[2], v[3])};
         }
