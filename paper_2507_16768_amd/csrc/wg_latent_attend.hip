@@ -24,22 +24,37 @@ constexpr uint32_t kThreads = 256, kWaves = 4, kTop = 64;
 constexpr float kLift = 8.f;                         // how far above the base a score may be, log2
 constexpr uint32_t kNone = 0xFFFFFFFFu;
 
-// Requests and their tokens: query rows [starts[r], starts[r + 1]) of request r are its last ones.
+// Requests and their query tokens: tokens [starts[r], starts[r + 1]) of the call are request r's last ones.
 struct Requests {
     const int32_t *starts;
-    uint32_t rows, tokens, heads, splits, least;     // splits: the most shares of a row's keys; least: blocks of a share
+    uint32_t rows, tokens, heads;
+    uint32_t chunks;                                 // workgroups that all work is dealt out to; 0: one for each tile
 };
+struct Tile { uint32_t row, first, last, begin, count; int32_t before; };  // query rows [first, last) of request `row`, whose tokens of the call begin at `begin`, behind `before` others (count: all of them)
 
-// Where a tile of kRows query rows lies (`heads` rows to a token): request r's tiles begin at starts[r] * heads / kRows + r, which leaves room for each one's last, begun tile.  A
-// wavefront asks 64 requests at a time.
-struct Tile { uint32_t row, first, last, begin; int32_t before; };         // query rows [first, last) of request `row`, its tokens those from `begin` on, behind `before` others
+__device__ __forceinline__ uint32_t start_of(const Requests &a, uint32_t r) { const uint32_t t = (uint32_t)a.starts[r]; return t < a.tokens ? t : a.tokens; }
+__device__ __forceinline__ uint32_t tokens_of(const Requests &a, uint32_t r) { const uint32_t b = start_of(a, r), e = start_of(a, r + 1u); return e < b ? 0u : e - b; }
 
+// Tile `tile` of request r, of kRows query rows, `per` to a token; false: there is none.
 template <uint32_t kRows>
-__device__ __forceinline__ bool tile_of(const Requests &a, uint32_t heads, uint32_t tile, Tile *out, uint32_t *count)
+__device__ __forceinline__ bool tile_at(const Requests &a, uint32_t per, uint32_t r, uint32_t tile, Tile *out)
+{
+    const uint32_t n = tokens_of(a, r), all = n * per, e = (uint32_t)a.starts[r + 1u];
+    out->row = r; out->begin = start_of(a, r);
+    if ((uint64_t)tile * kRows >= all) return false;
+    out->first = tile * kRows;
+    out->last = all - out->first < kRows ? all : out->first + kRows;
+    out->count = e - out->begin;                     // (with the request's tokens that the call does not have)
+    return true;
+}
+
+// The request whose tiles tile `tile` of the call is among: request r's begin at starts[r] * per / kRows + r, which leaves room for each one's last, begun tile.  A wavefront asks 64
+// requests at a time.
+template <uint32_t kRows>
+__device__ __forceinline__ bool tile_of(const Requests &a, uint32_t per, uint32_t tile, Tile *out)
 {
     const uint32_t lane = threadIdx.x & 63u;
-    auto start = [&](uint32_t r) { const uint32_t t = (uint32_t)a.starts[r]; return t < a.tokens ? t : a.tokens; };
-    auto begins = [&](uint32_t r) { return (uint32_t)((uint64_t)start(r) * heads / kRows) + r; };
+    auto begins = [&](uint32_t r) { return (uint32_t)((uint64_t)start_of(a, r) * per / kRows) + r; };
     uint32_t lo = 0, n = a.rows;
     while (n > 1u) {
         const uint32_t step = (n + 63u) / 64u, r = lo + lane * step;
@@ -49,33 +64,48 @@ __device__ __forceinline__ bool tile_of(const Requests &a, uint32_t heads, uint3
         lo += k * step;
     }
     lo = __builtin_amdgcn_readfirstlane(lo);
-    const uint32_t b = start(lo), e0 = (uint32_t)a.starts[lo + 1u], e = e0 < b ? b : e0 < a.tokens ? e0 : a.tokens, first_tile = begins(lo), all = (e - b) * heads;
-    if (tile < first_tile || (uint64_t)(tile - first_tile) * kRows >= all) return false;
-    out->row = lo; out->begin = b;
-    out->first = (tile - first_tile) * kRows;
-    out->last = all - out->first < kRows ? all : out->first + kRows;
-    *count = e0 < b ? 0u : e0 - b;                   // (with the request's tokens that the call does not have)
-    return true;
+    const uint32_t first = begins(lo);
+    return tile >= first && tile_at<kRows>(a, per, lo, tile - first, out);
 }
 
-// Blocks of keys to a share: shares of one size, whatever the rows' lengths, so that the workgroups have as much to do as one another.  The number follows from the row and not from the tile,
-// as a token's rows may lie in two tiles.  tiles(r): query tiles of row r; blocks(r): blocks of its keys.
+// All work dealt out: blocks of keys of the tiles of the requests, one behind the other, in chunks of one size, a workgroup each, so that all have as much to do whatever the rows' lengths
+// are.  A chunk takes the end of a tile, whole ones, and the beginning of another; what is part of a tile only goes to the workspace and is joined by another kernel.  Chunk w's part of a tile
+// that has begun before it lies in place 2 w there, one of a tile that begins in it in place 2 w + 1.
+struct Chunk { uint32_t at, end, size, row, off; };  // blocks [at, end) of all work; `at` is block `off` of request `row`
+
 template <typename F>
-__device__ __forceinline__ uint32_t shares_of(const Requests &a, uint32_t blocks, uint32_t *per, F work_of)
+__device__ __forceinline__ bool chunk_of(const Requests &a, uint32_t w, F work_of, Chunk *out)
 {
-    *per = blocks;
-    if (a.splits == 1u || !blocks) return 1u;
-    uint64_t all = 0;
-    for (uint32_t r = threadIdx.x & 63u; r < a.rows; r += 64u) all += work_of(r);
+    const uint32_t lane = threadIdx.x & 63u;
+    uint32_t all = 0;
+    for (uint32_t r = lane; r < a.rows; r += 64u) all += work_of(r);
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) all += __shfl_xor(all, o);
-    uint64_t share64 = (all + kAttendShares - 1u) / kAttendShares;
-    uint32_t share = __builtin_amdgcn_readfirstlane((uint32_t)(share64 < blocks ? share64 : blocks));
-    share = share < a.least ? a.least : share;
-    const uint32_t want = (blocks + share - 1u) / share, n = want < a.splits ? want : a.splits;
-    *per = (blocks + n - 1u) / n;
-    return (blocks + *per - 1u) / *per;
+    all = __builtin_amdgcn_readfirstlane(all);
+    const uint32_t even = (all + a.chunks - 1u) / a.chunks, size = even < kAttendLeast ? kAttendLeast : even;
+    out->size = size;
+    out->at = w * size;
+    if (w >= a.chunks || out->at >= all) return false;
+    out->end = all - out->at < size ? all : out->at + size;
+    uint32_t ahead = 0;                              // work of the requests in front
+    for (uint32_t base = 0;; base += 64u) {
+        const uint32_t own = base + lane < a.rows ? work_of(base + lane) : 0u;
+        uint32_t sum = own;
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) { const uint32_t x = __shfl_up(sum, o); sum += lane >= (uint32_t)o ? x : 0u; }
+        const unsigned long long behind = __ballot(ahead + sum > out->at);
+        if (behind) {
+            const uint32_t k = (uint32_t)__builtin_ctzll(behind);
+            out->row = base + k;
+            out->off = out->at - (ahead + __builtin_amdgcn_readlane(sum, k) - __builtin_amdgcn_readlane(own, k));
+            return true;
+        }
+        ahead += __builtin_amdgcn_readlane(sum, 63);
+    }
 }
+
+// Where the parts of a query row lie: its first chunk and its place in the tile, and how many chunks.
+struct Parts { uint32_t chunk_and_row, chunks; };
 
 // Four rows' sixteen numbers, a column of four to each lane: `at` is the lane's four of a row.
 __device__ __forceinline__ Short4 column_of(const uint16_t *at)
@@ -118,8 +148,42 @@ __device__ __forceinline__ Word4 without_odd_dims(Word4 v, uint32_t key, uint32_
     return v;
 }
 
+// A load from device memory.  (Of an address that is one of two the compiler knows only that it is some address, and a load from there counts as one from LDS too: the waits for operands
+// out of LDS would be waits for memory.)
+template <typename T> __device__ __forceinline__ T from_memory(const void *p) { return *(const __attribute__((address_space(1))) T *)p; }
+
 // What is read in the place of a key that there is none of.
 __device__ __attribute__((aligned(16))) const uint8_t kZeros[1024] = {};
+
+// kN operands out of LDS, load(i, place), each for products, use(i, place): kAhead of them are asked for before the kAhead in front of them are used.  (Left to itself the compiler asks for one,
+// waits, and uses it.)
+template <uint32_t kN, uint32_t kAhead, typename L, typename U>
+__device__ __forceinline__ void pipelined(L load, U use)
+{
+    constexpr uint32_t kRounds = (kN + kAhead - 1u) / kAhead;
+#pragma unroll
+    for (uint32_t i = 0; i < kAhead && i < kN; i++) load(i, i);
+#pragma unroll
+    for (uint32_t b = 0; b < kRounds; b++) {
+#pragma unroll
+        for (uint32_t i = 0; i < kAhead; i++)
+            if ((b + 1u) * kAhead + i < kN) load((b + 1u) * kAhead + i, (b + 1u) % 2u * kAhead + i);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (uint32_t i = 0; i < kAhead; i++)
+            if (b * kAhead + i < kN) use(b * kAhead + i, b % 2u * kAhead + i);
+        __builtin_amdgcn_sched_barrier(0);
+    }
+}
+
+// The largest over lanes l, l ^ 16, l ^ 32 and l ^ 48.
+__device__ __forceinline__ float most_of_rows(float x)
+{
+    const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    x = __builtin_fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+    const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return __builtin_fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
 
 // What a wavefront holds of its kM tiles of 16 queries: of query m of each, the base and its own part of the sum, and outputs, dims 4 g .. 4 g + 3 of each of kParts.
 template <uint32_t kM, uint32_t kParts>
@@ -139,31 +203,15 @@ struct Sums {
     template <uint32_t kGroups>
     __device__ __forceinline__ void weigh(const float (&s)[kGroups][kM][8], Half8 (&p)[kGroups][kM])
     {
-        float top[kM];
-        bool grows = false;
 #pragma unroll
         for (uint32_t t = 0; t < kM; t++) {
-            top[t] = -__builtin_inff();
+            float n = base[t];
 #pragma unroll
-            for (uint32_t k = 0; k < kGroups; k++)
-#pragma unroll
-                for (uint32_t j = 0; j < 8u; j++) top[t] = __builtin_fmaxf(top[t], s[k][t][j]);
-            grows = grows || top[t] > base[t] + kLift;
-        }
-        if (__ballot(grows)) {
-#pragma unroll
-            for (uint32_t t = 0; t < kM; t++) {
-                float n = __builtin_fmaxf(top[t], __shfl_xor(top[t], 16));
-                n = __builtin_fmaxf(base[t], __builtin_fmaxf(n, __shfl_xor(n, 32)));
-                const float by = base[t] > -__builtin_inff() ? __builtin_amdgcn_exp2f(base[t] - n) : 0.f;
-                base[t] = n; sum[t] *= by;
-#pragma unroll
-                for (uint32_t d = 0; d < kParts; d++) acc[d][t] *= by;
-            }
-        }
-#pragma unroll
-        for (uint32_t t = 0; t < kM; t++) {
-            const float from = base[t] > -__builtin_inff() ? base[t] : 0.f;
+            for (uint32_t k = 0; k < kGroups; k++) n = __builtin_fmaxf(n, __builtin_fmaxf(__builtin_fmaxf(__builtin_fmaxf(s[k][t][0], s[k][t][1]), __builtin_fmaxf(s[k][t][2], s[k][t][3])),
+                                                                                          __builtin_fmaxf(__builtin_fmaxf(s[k][t][4], s[k][t][5]), __builtin_fmaxf(s[k][t][6], s[k][t][7]))));
+            n = most_of_rows(n);
+            const float from = n > -__builtin_inff() ? n : 0.f, by = __builtin_amdgcn_exp2f(base[t] - from);
+            base[t] = n; sum[t] *= by;
 #pragma unroll
             for (uint32_t k = 0; k < kGroups; k++) {
                 Word4 w;
@@ -174,6 +222,8 @@ struct Sums {
                 }
                 p[k][t] = __builtin_bit_cast(Half8, w);
             }
+#pragma unroll
+            for (uint32_t d = 0; d < kParts; d++) acc[d][t] *= by;
         }
     }
     // The queries' sums over all lanes.
@@ -189,8 +239,8 @@ __device__ __forceinline__ float share_of_sum(float sum, bool sees) { return sum
 constexpr float kEmpty = -1.f;                       // the sum of a share in which a query sees keys whose scores are all -inf
 
 // ---------------------------------------------------------------------------------------------
-// Attention over the cached vectors.  A workgroup takes 16 * kM * kGroups query rows (tokens times heads) of a request and a share of its keys; its wavefronts are kGroups groups of rows
-// times 4 / kGroups groups of keys.  All keys of a block, 32 for each group, go through LDS: from memory into registers, while the block before is worked on, and turned into bfloat16 (exactly) on the way.
+// Attention over the cached vectors.  A workgroup's eight wavefronts are kGroups groups of 16 query rows (tokens times heads), times kCols groups of the vectors' columns (for which
+// scores are made again), times groups of 32 keys.  A block's keys go through LDS: from memory into registers, while the block before is worked on, and turned into bfloat16 (exactly) on the way.
 struct LatentAttendArgs {
     Requests of;
     const uint16_t *q_c, *q_r;
@@ -200,8 +250,8 @@ struct LatentAttendArgs {
     const float *scale;                              // of each token; null: the vectors are bfloat16
     const int32_t *table, *lens;
     uint16_t *out;                                   // [token][head][C]
-    float *partial, *ends;                           // [token][head][split][C]; [token][head][split][2]: base and sum
-    uint32_t *shares;                                // [token]: shares of its keys
+    float *partial, *ends;                           // [chunk][2][row of a tile][C]; [chunk][2][row of a tile][2]: base and sum
+    Parts *parts;                                    // [token][head]
     float factor;                                    // of the scores, times log2(e)
     uint32_t columns, pages, shift;
 };
@@ -211,245 +261,253 @@ __device__ __forceinline__ uint32_t cached_tokens(const LatentAttendArgs &a, uin
     const uint32_t most = a.columns << a.shift, l = (uint32_t)(a.lens[r] < 0 ? 0 : a.lens[r]);
     return l < most ? l : most;
 }
+__device__ __forceinline__ uint32_t blocks_of(uint32_t keys) { return keys ? (keys + kAttendBlock - 1u) / kAttendBlock : 1u; }
 
-template <uint32_t kC, bool kBytes, uint32_t kM, uint32_t kGroups, uint32_t kW>
-__global__ void __launch_bounds__(kW * 64u) __attribute__((amdgpu_waves_per_eu(kW / 4u, kW / 4u)))
+template <uint32_t kC, bool kBytes, uint32_t kGroups, uint32_t kCols>
+__global__ void __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2)))
 latent_attend_kernel(const LatentAttendArgs a)
 {
-    constexpr uint32_t kKeyGroups = kW / kGroups, kKeys = 32u * kKeyGroups, kRows = 16u * kM * kGroups;
-    constexpr uint32_t kSteps = (kC + kTop) / 32u, kParts = kC / 16u, kPitch = kC + kTop + 8u;
+    constexpr uint32_t kW = 8u, kKeyGroups = kW / (kGroups * kCols), kKeys = 32u * kKeyGroups, kRows = 16u * kGroups;
+    constexpr uint32_t kSteps = (kC + kTop) / 32u, kParts = kC / 16u / kCols, kPitch = kC + kTop + 8u;
     constexpr uint32_t kRow = kC * (kBytes ? 1u : 2u), kPer = 1024u / kRow, kStage = kKeys / kW;          // bytes of a vector; keys of a wavefront's load; keys that it brings
-    constexpr uint32_t kLoads = kStage / kPer, kTops = (kStage + 7u) / 8u;
-    constexpr uint32_t kJoinPitch = kC + 4u, kTileBytes = kKeys * kPitch * 2u, kJoinBytes = kKeyGroups > 1u ? kW * 16u * kJoinPitch * 4u : 0u;
+    constexpr uint32_t kLoads = kStage / kPer, kTops = (kStage + 7u) / 8u, kAhead = kC == 512u ? 2u : 4u, kPut = kC == 512u && kGroups == 8u ? 6u : 0u, kKept = kSteps - kPut;
+    constexpr uint32_t kJoinPitch = kC + 4u, kTileBytes = kKeys * kPitch * 2u, kJoinBytes = kKeyGroups > 1u ? kKeyGroups * kRows * kJoinPitch * 4u : 0u;
     __shared__ __attribute__((aligned(16))) uint8_t room[kTileBytes > kJoinBytes ? kTileBytes : kJoinBytes];
     __shared__ uint32_t odd_from;                                          // the first key with a number that is none, of those that some rows do not see
-    __shared__ float join_base[kW][16], join_sum[kW][16];
+    __shared__ float join_base[kKeyGroups][kRows], join_sum[kKeyGroups][kRows];
+    __shared__ Half8 q_rest[kPut ? kW * kPut * 64u : 1u];                  // the last steps of the queries, each lane its own: there are no registers for them
     uint16_t *keys = reinterpret_cast<uint16_t *>(room);
     const uint32_t tid = threadIdx.x, lane = tid & 63u, wave = __builtin_amdgcn_readfirstlane(tid >> 6), m = lane & 15u, g = lane >> 4;
-    const uint32_t split = blockIdx.y, P = 1u << a.shift, heads = a.of.heads;
+    const uint32_t group = wave % kGroups, column_group = wave / kGroups % kCols, key_group = wave / (kGroups * kCols);
+    const uint32_t P = 1u << a.shift, heads = a.of.heads;
+    auto tiles = [&](uint32_t r) { return (uint32_t)(((uint64_t)tokens_of(a.of, r) * heads + kRows - 1u) / kRows); };
     Tile t;
-    uint32_t count;
-    if (!tile_of<kRows>(a.of, heads, blockIdx.x, &t, &count)) return;
-    const uint32_t len = cached_tokens(a, t.row);
-    t.before = (int32_t)len - (int32_t)count;
-    uint32_t per;
-    const uint32_t shares = shares_of(a.of, (len + kAttendBlock - 1u) / kAttendBlock, &per, [&](uint32_t r) {
-        const uint32_t n = (uint32_t)a.of.starts[r + 1u] - (uint32_t)a.of.starts[r];
-        return (uint64_t)((cached_tokens(a, r) + kAttendBlock - 1u) / kAttendBlock) * (((uint64_t)n * heads + kRows - 1u) / kRows);
-    });
-    if (a.of.splits > 1u && split == 0u && tid < kRows && t.first + tid < t.last) a.shares[t.begin + (t.first + tid) / heads] = shares;
-    if (split >= shares) return;
-    auto seen_by = [&](uint32_t i) { const int32_t n = t.before + (int32_t)(i / heads) + 1; return n < 0 ? 0u : (uint32_t)n; };
-    const uint32_t seen_least = seen_by(t.first), seen_most = seen_by(t.last - 1u);
-    const uint32_t from = split * per * kAttendBlock, to0 = shares > 1u ? from + per * kAttendBlock : seen_most, to = to0 < seen_most ? to0 : seen_most;
-
-    // The wavefront's keys of a block: lane i knows the slot of the i-th.
-    auto slot_of = [&](uint32_t block) {
-        const uint32_t at = block + wave * kStage + lane;
-        if (lane >= kStage || at >= to) return kNone;
-        const uint32_t page = (uint32_t)a.table[(size_t)t.row * a.columns + (at >> a.shift)];
-        return page < a.pages ? page << a.shift | (at & (P - 1u)) : kNone;
-    };
-    Word4 raw[kLoads], tops[kTops];
-    float scales[kBytes ? kLoads : 1u];
-    auto fetch = [&](uint32_t slots) {
-#pragma unroll
-        for (uint32_t i = 0; i < kLoads; i++) {
-            const uint32_t slot = kPer == 1u ? __builtin_amdgcn_readlane(slots, i) : __shfl(slots, i * kPer + lane / (64u / kPer));
-            const uint8_t *row = slot != kNone ? a.c_cache + (size_t)slot * kRow : kZeros;
-            raw[i] = *reinterpret_cast<const Word4 *>(row + lane % (64u / kPer) * 16u);
-            if (kBytes) scales[i % (kBytes ? kLoads : 1u)] = *(slot != kNone ? a.scale + slot : reinterpret_cast<const float *>(kZeros));
+    Chunk c{0u, 1u, 0u, 0u, 0u};
+    if (a.of.chunks ? !chunk_of(a.of, blockIdx.x, [&](uint32_t r) { return tiles(r) * blocks_of(cached_tokens(a, r)); }, &c) : !tile_of<kRows>(a.of, heads, blockIdx.x, &t)) return;
+    while (c.at < c.end) {
+        // the next part of a tile: blocks [b0, b0 + n) of its `blocks`
+        uint32_t b0 = 0, n = 1u, blocks = 1u, begins = 0;                  // begins: where the tile's blocks do, among all
+        if (a.of.chunks) {
+            const uint32_t work = tiles(c.row) * (blocks = blocks_of(cached_tokens(a, c.row))), tile = c.off / blocks;
+            if (!work) { c.row++; continue; }                              // (off is 0)
+            (void)tile_at<kRows>(a.of, heads, c.row, tile, &t);
+            b0 = c.off - tile * blocks;
+            n = blocks - b0 < c.end - c.at ? blocks - b0 : c.end - c.at;
+            begins = c.at - b0;
+            c.off += n;
+            if (c.off >= work) { c.off = 0; c.row++; }
         }
-#pragma unroll
-        for (uint32_t i = 0; i < kTops; i++) {
-            const uint32_t slot = __shfl(slots, i * 8u + lane / 8u);
-            tops[i] = *reinterpret_cast<const Word4 *>((slot != kNone ? a.r_cache + (size_t)slot * kTop : reinterpret_cast<const uint16_t *>(kZeros)) + lane % 8u * 8u);
-        }
-    };
-    uint32_t ahead = 0;
-    if (from < to) {
-        fetch(slot_of(from));
-        ahead = slot_of(from + kKeys);
-    }
+        const uint32_t len = cached_tokens(a, t.row);
+        t.before = (int32_t)len - (int32_t)t.count;
+        const bool whole = n == blocks;
+        const uint32_t place = 2u * blockIdx.x + (b0 ? 0u : 1u), row_first = t.first;
+        if (a.of.chunks && b0 == 0u && tid < kRows && t.first + tid < t.last)
+            a.parts[(size_t)t.begin * heads + t.first + tid] = Parts{blockIdx.x | tid << 16, whole ? 1u : (begins + blocks - 1u) / c.size - blockIdx.x + 1u};
+        c.at += n;
+        auto seen_by = [&](uint32_t i) { const int32_t k = t.before + (int32_t)(i / heads) + 1; return k < 0 ? 0u : (uint32_t)k; };
+        const uint32_t seen_least = seen_by(t.first), seen_most = seen_by(t.last - 1u);
+        const uint32_t from = b0 * kAttendBlock, to0 = whole ? seen_most : from + n * kAttendBlock, to = to0 < seen_most ? to0 : seen_most;
 
-    // queries: a row behind the last is the last again, and is not stored
-    const uint32_t group = wave % kGroups, key_group = wave / kGroups;
-    Half8 q[kM][kSteps];
-    uint32_t sees[kM];
+        // The wavefront's keys of a block: lane i knows the slot of the i-th.  A page's number is asked for a block ahead of the keys, and looked at when they are asked for: before that,
+        // the wait for it would be one for all that has been asked for earlier.
+        const int32_t *pages_of_row = a.table + (size_t)t.row * a.columns;
+        auto page_of = [&](uint32_t block) {
+            const uint32_t at = block + wave * kStage + lane % kStage;
+            return from_memory<uint32_t>(at < to ? static_cast<const void *>(pages_of_row + (at >> a.shift)) : kZeros);
+        };
+        auto slot_of = [&](uint32_t block, uint32_t page) {
+            const uint32_t at = block + wave * kStage + lane;
+            return lane < kStage && at < to && page < a.pages ? page << a.shift | (at & (P - 1u)) : kNone;
+        };
+        Word4 raw[kLoads], tops[kTops];
+        float scales[kBytes ? kLoads : 1u];
+        auto fetch = [&](uint32_t slots) {
 #pragma unroll
-    for (uint32_t n = 0; n < kM; n++) {
-        const uint32_t i0 = t.first + (group * kM + n) * 16u + m, i = i0 < t.last ? i0 : t.last - 1u, token = t.begin + i / heads, head = i % heads;
-        const uint16_t *c = a.q_c + (int64_t)token * a.c_token + (int64_t)head * a.c_head + g * 8u, *r = a.q_r + (int64_t)token * a.r_token + (int64_t)head * a.r_head + g * 8u;
-#pragma unroll
-        for (uint32_t s = 0; s < kSteps; s++) q[n][s] = *reinterpret_cast<const Half8 *>(s < kC / 32u ? c + s * 32u : r + (s - kC / 32u) * 32u);
-        const uint32_t all = seen_by(i);
-        sees[n] = all < to ? all : to;
-    }
-    Sums<kM, kParts> sums;
-    sums.clear();
-    if (tid == 0u) odd_from = kNone;
-    __syncthreads();
-    for (uint32_t block = from; block < to; block += kKeys) {
-        const bool partly = block + kKeys > seen_least;                    // some of the tile's rows do not see all of the block's keys
-#pragma unroll
-        for (uint32_t i = 0; i < kLoads; i++) {
-            const uint32_t key = wave * kStage + i * kPer + lane / (64u / kPer), at = lane % (64u / kPer);
-            if (kBytes) {
-                const float scale = scales[i % (kBytes ? kLoads : 1u)];
-                const Word2 w0 = wider(raw[i][0], scale), w1 = wider(raw[i][1], scale), w2 = wider(raw[i][2], scale), w3 = wider(raw[i][3], scale);
-                Word4 x{w0[0], w0[1], w1[0], w1[1]}, y{w2[0], w2[1], w3[0], w3[1]};
-                if (partly) { x = without_odd(x, block + key, &odd_from); y = without_odd(y, block + key, &odd_from); }
-                Word4 *put = reinterpret_cast<Word4 *>(keys + key * kPitch + at * 16u);
-                put[0] = x; put[1] = y;
-            } else {
-                if (partly) raw[i] = without_odd(raw[i], block + key, &odd_from);
-                *reinterpret_cast<Word4 *>(keys + key * kPitch + at * 8u) = raw[i];
+            for (uint32_t i = 0; i < kLoads; i++) {
+                const uint32_t slot = kPer == 1u ? __builtin_amdgcn_readlane(slots, i) : __shfl(slots, i * kPer + lane / (64u / kPer));
+                const uint8_t *row = slot != kNone ? a.c_cache + (size_t)slot * kRow : kZeros;
+                raw[i] = from_memory<Word4>(row + lane % (64u / kPer) * 16u);
+                if (kBytes) scales[i % (kBytes ? kLoads : 1u)] = from_memory<float>(slot != kNone ? static_cast<const void *>(a.scale + slot) : kZeros);
             }
-        }
-        if (kStage >= 8u || lane < kStage * 8u)
 #pragma unroll
-            for (uint32_t i = 0; i < kTops; i++) *reinterpret_cast<Word4 *>(keys + (wave * kStage + i * 8u + lane / 8u) * kPitch + kC + lane % 8u * 8u) = tops[i];
+            for (uint32_t i = 0; i < kTops; i++) {
+                const uint32_t slot = __shfl(slots, i * 8u + lane / 8u);
+                tops[i] = from_memory<Word4>((slot != kNone ? reinterpret_cast<const uint8_t *>(a.r_cache) + (size_t)slot * (kTop * 2u) : kZeros) + lane % 8u * 16u);
+            }
+        };
+        uint32_t ahead = 0;
+        if (from < to) {
+            const uint32_t first = page_of(from);
+            ahead = page_of(from + kKeys);
+            fetch(slot_of(from, first));
+        }
+
+        // queries: a row behind the last is the last again, and is not stored
+        Half8 q[kKept];
+        uint32_t sees;
+        {
+            const uint32_t i0 = t.first + group * 16u + m, i = i0 < t.last ? i0 : t.last - 1u, token = t.begin + i / heads, head = i % heads;
+            const uint16_t *c = a.q_c + (int64_t)token * a.c_token + (int64_t)head * a.c_head + g * 8u, *r = a.q_r + (int64_t)token * a.r_token + (int64_t)head * a.r_head + g * 8u;
+#pragma unroll
+            for (uint32_t s = 0; s < kSteps; s++) {
+                const Half8 x = *reinterpret_cast<const Half8 *>(s < kC / 32u ? c + s * 32u : r + (s - kC / 32u) * 32u);
+                if (s < kKept) q[s % kKept] = x;
+                else q_rest[(wave * kPut + s - kKept) * 64u + lane] = x;
+            }
+            const uint32_t all = seen_by(i);
+            sees = all < to ? all : to;
+        }
+        Sums<1, kParts> sums;
+        sums.clear();
+        if (tid == 0u) odd_from = kNone;
         __syncthreads();
-        if (block + kKeys < to) {
-            fetch(ahead);
-            ahead = slot_of(block + 2u * kKeys);
-        }
-        if (block + key_group * 32u < to) {
-            const uint16_t *mine = keys + key_group * 32u * kPitch;
-            Float4 score[2][kM];
+        for (uint32_t block = from; block < to; block += kKeys) {
+            const bool partly = block + kKeys > seen_least;                    // some of the tile's rows do not see all of the block's keys
 #pragma unroll
-            for (uint32_t u = 0; u < 2u; u++)
-#pragma unroll
-                for (uint32_t n = 0; n < kM; n++) score[u][n] = Float4{0.f, 0.f, 0.f, 0.f};
-            const uint16_t *row = mine + (m / 4u * 8u + m % 4u) * kPitch + g * 8u;
-#pragma unroll
-            for (uint32_t s = 0; s < kSteps; s++)
-#pragma unroll
-                for (uint32_t u = 0; u < 2u; u++) {
-                    const Half8 k = *reinterpret_cast<const Half8 *>(row + u * 4u * kPitch + s * 32u);
-#pragma unroll
-                    for (uint32_t n = 0; n < kM; n++) score[u][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, q[n][s], score[u][n], 0, 0, 0);
+            for (uint32_t i = 0; i < kLoads; i++) {
+                const uint32_t key = wave * kStage + i * kPer + lane / (64u / kPer), at = lane % (64u / kPer);
+                if (kBytes) {
+                    const float scale = scales[i % (kBytes ? kLoads : 1u)];
+                    const Word2 w0 = wider(raw[i][0], scale), w1 = wider(raw[i][1], scale), w2 = wider(raw[i][2], scale), w3 = wider(raw[i][3], scale);
+                    Word4 x{w0[0], w0[1], w1[0], w1[1]}, y{w2[0], w2[1], w3[0], w3[1]};
+                    if (partly) { x = without_odd(x, block + key, &odd_from); y = without_odd(y, block + key, &odd_from); }
+                    Word4 *put = reinterpret_cast<Word4 *>(keys + key * kPitch + at * 16u);
+                    put[0] = x; put[1] = y;
+                } else {
+                    if (partly) raw[i] = without_odd(raw[i], block + key, &odd_from);
+                    *reinterpret_cast<Word4 *>(keys + key * kPitch + at * 8u) = raw[i];
                 }
-            float s[1][kM][8];
+            }
+            if (kStage >= 8u || lane < kStage * 8u)
+#pragma unroll
+                for (uint32_t i = 0; i < kTops; i++) *reinterpret_cast<Word4 *>(keys + (wave * kStage + i * 8u + lane / 8u) * kPitch + kC + lane % 8u * 8u) = tops[i];
+            __syncthreads();
+            if (block + kKeys < to) {
+                const uint32_t slots = slot_of(block + kKeys, ahead);
+                ahead = page_of(block + 2u * kKeys);
+                fetch(slots);
+            }
+            const uint16_t *mine = keys + key_group * 32u * kPitch, *row = mine + (m / 4u * 8u + m % 4u) * kPitch + g * 8u;
+            Float4 score[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+            Half8 k[2][kAhead];
+            pipelined<2u * kSteps, kAhead>([&](uint32_t i, uint32_t at) { k[at / kAhead][at % kAhead] = *reinterpret_cast<const Half8 *>(row + i % 2u * 4u * kPitch + i / 2u * 32u); },
+                                           [&](uint32_t i, uint32_t at) {
+                                               const Half8 x = i / 2u < kKept ? q[i / 2u % kKept] : q_rest[(wave * kPut + i / 2u - kKept) * 64u + lane];
+                                               score[i % 2u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k[at / kAhead][at % kAhead], x, score[i % 2u], 0, 0, 0);
+                                           });
+            float s[1][1][8];
             const uint32_t at = block + key_group * 32u + g * 8u;
 #pragma unroll
-            for (uint32_t n = 0; n < kM; n++)
-#pragma unroll
-                for (uint32_t j = 0; j < 8u; j++) s[0][n][j] = score[j / 4u][n][j % 4u] * a.factor;
+            for (uint32_t j = 0; j < 8u; j++) s[0][0][j] = score[j / 4u][j % 4u] * a.factor;
             if (partly || block + kKeys > to)
 #pragma unroll
-                for (uint32_t n = 0; n < kM; n++)
-#pragma unroll
-                    for (uint32_t j = 0; j < 8u; j++) s[0][n][j] = at + j < sees[n] ? s[0][n][j] : -__builtin_inff();
-            Half8 p[1][kM];
+                for (uint32_t j = 0; j < 8u; j++) s[0][0][j] = at + j < sees ? s[0][0][j] : -__builtin_inff();
+            Half8 p[1][1];
             sums.template weigh<1>(s, p);
-            const uint16_t *column = mine + (g * 8u + m / 4u) * kPitch + m % 4u * 4u;
-#pragma unroll
-            for (uint32_t d = 0; d < kParts; d++) {
-                const Half8 v = both(column_of(column + d * 16u), column_of(column + 4u * kPitch + d * 16u));
-#pragma unroll
-                for (uint32_t n = 0; n < kM; n++) sums.acc[d][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, p[0][n], sums.acc[d][n], 0, 0, 0);
-            }
+            const uint16_t *column = mine + (g * 8u + m / 4u) * kPitch + column_group * (kC / kCols) + m % 4u * 4u;
+            pipelined<kParts, kAhead>([&](uint32_t d, uint32_t at) { k[at / kAhead][at % kAhead] = both(column_of(column + d * 16u), column_of(column + 4u * kPitch + d * 16u)); },
+                                      [&](uint32_t d, uint32_t at) { sums.acc[d][0] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k[at / kAhead][at % kAhead], p[0][0], sums.acc[d][0], 0, 0, 0); });
+            __syncthreads();
         }
-        __syncthreads();
-    }
 
-    // out: this share's output by itself, or the whole.  (Numbers that are none have been left out of the sums of rows that see only some of a block's keys: what a row that sees them makes of them
-    // is none.)
-    const uint32_t odd = odd_from;
-    auto put = [&](uint32_t i, uint32_t d, Float4 v) {                     // dims d .. d + 3 of query row i
-        const size_t at = (size_t)t.begin * heads + i;
-        if (shares > 1u) *reinterpret_cast<Float4 *>(a.partial + (at * a.of.splits + split) * kC + d) = v;
-        else *reinterpret_cast<Word2 *>(a.out + at * kC + d) = Word2{pk_bf16(v[0], v[1]), pk_bf16(v[2], v[3])};
-    };
-    auto end = [&](uint32_t i, float base, float sum, bool any) {
-        float *to_ends = a.ends + (((size_t)t.begin * heads + i) * a.of.splits + split) * 2u;
-        to_ends[0] = base; to_ends[1] = any && sum == 0.f ? kEmpty : sum;
-    };
-#pragma unroll
-    for (uint32_t n = 0; n < kM; n++) {
-        float sum = sums.whole_sum(n);
-        if (odd < sees[n]) sum = __builtin_nanf("");
-        const uint32_t own = t.first + (group * kM + n) * 16u + m;
+        // Out: this part by itself, or the whole.  (Numbers that are none have been left out of the sums of rows that see only some of a block's keys: what a row that sees them makes of them
+        // is none.)
+        const uint32_t odd = odd_from;
+        const float sum = sums.whole_sum(0);
+        auto put = [&](uint32_t i, uint32_t d, Float4 v) {                 // dims d .. d + 3 of query row i of the tile
+            if (whole) *reinterpret_cast<Word2 *>(a.out + ((size_t)t.begin * heads + row_first + i) * kC + d) = Word2{pk_bf16(v[0], v[1]), pk_bf16(v[2], v[3])};
+            else *reinterpret_cast<Float4 *>(a.partial + ((size_t)place * kRows + i) * kC + d) = v;
+        };
+        auto finish = [&](uint32_t i, float base, float sum_of, float *by) {   // what the row's outputs are multiplied by
+            const uint32_t all = seen_by(row_first + i), end = all < to ? all : to;
+            const float l = odd < end ? __builtin_nanf("") : sum_of;
+            *by = share_of_sum(l, end > from && whole);
+            return Float2{base, end > from && l == 0.f ? kEmpty : l};
+        };
         if (kKeyGroups == 1u) {
-            const bool any = sees[n] > from;
-            const float by = share_of_sum(sum, any && shares == 1u);
-            if (own < t.last) {
+            const uint32_t i = group * 16u + m;
+            float by;
+            const Float2 ends = finish(i, sums.base[0], sum, &by);
+            if (row_first + i < t.last) {
 #pragma unroll
-                for (uint32_t d = 0; d < kParts; d++) put(own, d * 16u + g * 4u, sums.acc[d][n] * by);
-                if (shares > 1u && g == 0u) end(own, sums.base[n], sum, any);
+                for (uint32_t d = 0; d < kParts; d++) put(i, column_group * (kC / kCols) + d * 16u + g * 4u, sums.acc[d][0] * by);
+                if (!whole && g == 0u && column_group == 0u) *reinterpret_cast<Float2 *>(a.ends + ((size_t)place * kRows + i) * 2u) = ends;
             }
+            __syncthreads();
             continue;
         }
         float *join = reinterpret_cast<float *>(room);
-        if (n) __syncthreads();
+        const uint32_t own = key_group * kRows + group * 16u + m;
 #pragma unroll
-        for (uint32_t d = 0; d < kParts; d++) *reinterpret_cast<Float4 *>(join + (wave * 16u + m) * kJoinPitch + d * 16u + g * 4u) = sums.acc[d][n];
-        if (g == 0u) { join_base[wave][m] = sums.base[n]; join_sum[wave][m] = sum; }
+        for (uint32_t d = 0; d < kParts; d++) *reinterpret_cast<Float4 *>(join + own * kJoinPitch + column_group * (kC / kCols) + d * 16u + g * 4u) = sums.acc[d][0];
+        if (g == 0u && column_group == 0u) { join_base[key_group][group * 16u + m] = sums.base[0]; join_sum[key_group][group * 16u + m] = sum; }
         __syncthreads();
-        // rows of all groups, four dims to a thread
-        for (uint32_t u = tid; u < kGroups * 16u * (kC / 4u); u += kW * 64u) {
-            const uint32_t d = u % (kC / 4u) * 4u, row = u / (kC / 4u) % 16u, of = u / (kC / 4u) / 16u, i = t.first + (of * kM + n) * 16u + row;
-            if (i >= t.last) continue;
+        // four dims of a row to a thread
+        for (uint32_t u = tid; u < kRows * (kC / 4u); u += kW * 64u) {
+            const uint32_t d = u % (kC / 4u) * 4u, i = u / (kC / 4u);
+            if (row_first + i >= t.last) continue;
             float base = -__builtin_inff(), total = 0.f;
 #pragma unroll
-            for (uint32_t w = 0; w < kKeyGroups; w++) base = __builtin_fmaxf(base, join_base[w * kGroups + of][row]);
+            for (uint32_t w = 0; w < kKeyGroups; w++) base = __builtin_fmaxf(base, join_base[w][i]);
             const float rel = base > -__builtin_inff() ? base : 0.f;
             Float4 v{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (uint32_t w = 0; w < kKeyGroups; w++) {
-                const float by = __builtin_amdgcn_exp2f(join_base[w * kGroups + of][row] - rel);
-                total += by * join_sum[w * kGroups + of][row];
-                v += by * *reinterpret_cast<const Float4 *>(join + ((w * kGroups + of) * 16u + row) * kJoinPitch + d);
+                const float by = __builtin_amdgcn_exp2f(join_base[w][i] - rel);
+                total += by * join_sum[w][i];
+                v += by * *reinterpret_cast<const Float4 *>(join + (w * kRows + i) * kJoinPitch + d);
             }
-            const uint32_t all = seen_by(i);
-            const bool any = (all < to ? all : to) > from;
-            put(i, d, v * share_of_sum(total, any && shares == 1u));
-            if (shares > 1u && d == 0u) end(i, base, total, any);
+            float by;
+            const Float2 ends = finish(i, base, total, &by);
+            put(i, d, v * by);
+            if (!whole && d == 0u) *reinterpret_cast<Float2 *>(a.ends + ((size_t)place * kRows + i) * 2u) = ends;
         }
+        __syncthreads();
     }
 }
 
-// The shares of a query row joined, each an output of its own with its sum: kJoinWaves wavefronts for each.
+// The parts of a query row joined, each an output of its own with its sum: kJoinWaves wavefronts for each.
 struct JoinArgs {
     const float *partial, *ends;
-    const uint32_t *shares;
-    const int32_t *total;                            // starts[rows]: tokens that belong to a row
+    const Parts *parts;
+    const int32_t *starts;
     uint16_t *out;
-    uint32_t heads, splits;
+    uint32_t requests, heads, chunks, rows;          // rows: of a tile
 };
 template <uint32_t kD, uint32_t kJoinWaves>
-__global__ void __launch_bounds__(kThreads)
+__global__ void __launch_bounds__(256)
 latent_join_kernel(const JoinArgs a)
 {
-    constexpr uint32_t kOwn = kD / 64u, kHeads = kWaves / kJoinWaves, kRound = 8u;
-    __shared__ float part[kJoinWaves > 1u ? kWaves : 1u][kD];
+    constexpr uint32_t kOwn = kD / 64u, kHeads = 4u / kJoinWaves, kRound = 8u;
+    __shared__ float part[kJoinWaves > 1u ? 4u : 1u][kD];
     const uint32_t lane = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const uint32_t token = blockIdx.x, head = blockIdx.y * kHeads + wave / kJoinWaves, first = wave % kJoinWaves;
-    if (token >= (uint32_t)*a.total) return;         // a token of no row, whose shares nothing has written
-    const uint32_t said = a.shares[token], shares = said < a.splits ? said : a.splits;
-    if (shares < 2u || (kJoinWaves == 1u && head >= a.heads)) return;
+    if (token < (uint32_t)a.starts[0] || token >= (uint32_t)a.starts[a.requests] || head >= a.heads) return;          // (a token of no row has no parts)
     const size_t at = (size_t)token * a.heads + head;
-    const float *ends = a.ends + at * a.splits * 2u;
+    const Parts p = a.parts[at];
+    const uint32_t chunk = p.chunk_and_row & 0xFFFFu, row = p.chunk_and_row >> 16;
+    if (p.chunks < 2u || row >= a.rows || chunk >= a.chunks) return;
+    const uint32_t n = p.chunks < a.chunks - chunk ? p.chunks : a.chunks - chunk;
+    auto place = [&](uint32_t i) { return (size_t)(i ? 2u * (chunk + i) : 2u * chunk + 1u) * a.rows + row; };
+    auto ends = [&](uint32_t i) { return *reinterpret_cast<const Float2 *>(a.ends + place(i) * 2u); };
     float base = -__builtin_inff(), total = 0.f;
     bool any = false;
-    for (uint32_t i = lane; i < shares; i += 64u) base = __builtin_fmaxf(base, ends[2u * i]);
+    for (uint32_t i = lane; i < n; i += 64u) base = __builtin_fmaxf(base, ends(i)[0]);
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) base = __builtin_fmaxf(base, __shfl_xor(base, o));
     const float rel = base > -__builtin_inff() ? base : 0.f;
-    for (uint32_t i = lane; i < shares; i += 64u) {
-        const float sum = ends[2u * i + 1u];
-        any = any || sum == kEmpty;
-        if (sum != kEmpty) total += sum * __builtin_amdgcn_exp2f(ends[2u * i] - rel);
+    for (uint32_t i = lane; i < n; i += 64u) {
+        const Float2 e = ends(i);
+        any = any || e[1] == kEmpty;
+        if (e[1] != kEmpty && e[1] != 0.f) total += e[1] * __builtin_amdgcn_exp2f(e[0] - rel);
     }
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) total += __shfl_xor(total, o);
     const float by = share_of_sum(total, __ballot(any) != 0ull);
-    const float *from = a.partial + at * a.splits * kD + lane * kOwn;
     float acc[kOwn];
 #pragma unroll
     for (uint32_t d = 0; d < kOwn; d++) acc[d] = 0.f;
-    for (uint32_t i0 = first; i0 < shares; i0 += kRound * kJoinWaves) {
+    for (uint32_t i0 = first; i0 < n; i0 += kRound * kJoinWaves) {
         float v[kRound][kOwn], w[kRound];
 #pragma unroll
         for (uint32_t k = 0; k < kRound; k++) {
@@ -457,12 +515,13 @@ latent_join_kernel(const JoinArgs a)
             w[k] = 0.f;
 #pragma unroll
             for (uint32_t d = 0; d < kOwn; d++) v[k][d] = 0.f;
-            if (i >= shares) continue;
-            const float sum = ends[2u * i + 1u];
-            w[k] = sum == 0.f || sum == kEmpty ? 0.f : sum * __builtin_amdgcn_exp2f(ends[2u * i] - rel) * by;
-            if (sum == 0.f || sum == kEmpty) continue;
+            if (i >= n) continue;
+            const Float2 e = ends(i);
+            if (e[1] == 0.f || e[1] == kEmpty) continue;
+            w[k] = e[1] * __builtin_amdgcn_exp2f(e[0] - rel) * by;
+            const float *from = a.partial + place(i) * kD + lane * kOwn;
 #pragma unroll
-            for (uint32_t d = 0; d < kOwn; d++) v[k][d] = from[(size_t)i * kD + d];
+            for (uint32_t d = 0; d < kOwn; d++) v[k][d] = from[d];
         }
 #pragma unroll
         for (uint32_t k = 0; k < kRound; k++)
@@ -471,17 +530,17 @@ latent_join_kernel(const JoinArgs a)
     }
     if (kJoinWaves > 1u) {
 #pragma unroll
-        for (uint32_t d = 0; d < kOwn; d++) part[wave % (kJoinWaves > 1u ? kWaves : 1u)][lane * kOwn + d] = acc[d];
+        for (uint32_t d = 0; d < kOwn; d++) part[wave % (kJoinWaves > 1u ? 4u : 1u)][lane * kOwn + d] = acc[d];
         __syncthreads();
         if (wave) return;
 #pragma unroll
         for (uint32_t d = 0; d < kOwn; d++) {
             acc[d] = 0.f;
 #pragma unroll
-            for (uint32_t w = 0; w < kWaves; w++) acc[d] += part[w % (kJoinWaves > 1u ? kWaves : 1u)][lane * kOwn + d];
+            for (uint32_t w = 0; w < 4u; w++) acc[d] += part[w % (kJoinWaves > 1u ? 4u : 1u)][lane * kOwn + d];
         }
     }
-    if (total == 0.f && by != by)
+    if (total == 0.f && by != by)                    // (scores that are all -inf)
 #pragma unroll
         for (uint32_t d = 0; d < kOwn; d++) acc[d] = by;
     uint16_t *out = a.out + at * kD + lane * kOwn;
@@ -491,51 +550,71 @@ latent_join_kernel(const JoinArgs a)
         for (uint32_t d = 0; d < kOwn; d += 2u) reinterpret_cast<Word *>(out)[d / 2u] = pk_bf16(acc[d], acc[(d + 1u) % kOwn]);
 }
 
-template <uint32_t kD>
-static hipError_t launch_join(const JoinArgs &j, uint32_t tokens, hipStream_t s)
+// Whether all work is dealt out, over how many workgroups, and the workspace's parts.  (tiles, blocks: the most there can be)
+struct Plan { uint32_t chunks; uint64_t partial, ends, parts; };
+static Plan plan_of(uint64_t tiles, uint64_t blocks, uint32_t rows, uint32_t tile_rows, uint32_t dim, uint32_t slots, uint64_t outputs)
 {
-    if (j.splits > 8u) return launch(latent_join_kernel<kD, 4>, dim3(tokens, j.heads), dim3(kThreads), 0, s, nullptr, j);
-    return launch(latent_join_kernel<kD, 1>, dim3(tokens, (j.heads + kWaves - 1u) / kWaves), dim3(kThreads), 0, s, nullptr, j);
+    Plan p{0u, 0u, 0u, 0u};
+    if (rows > 1024u || blocks < 2u || tiles >= 2u * slots || tiles * blocks > 0x7FFFFFFFull) return p;
+    const uint64_t most = (tiles * blocks + kAttendLeast - 1u) / kAttendLeast;
+    p.chunks = (uint32_t)(most < slots ? most : slots);
+    p.partial = (uint64_t)p.chunks * 2u * tile_rows * dim;
+    p.ends = (uint64_t)p.chunks * 2u * tile_rows * 2u;
+    p.parts = outputs * 2u;
+    return p;
+}
+uint64_t plan_bytes(const Plan &p) { return (p.partial + p.ends + p.parts) * 4u; }
+
+template <uint32_t kD>
+static hipError_t launch_join(const JoinArgs &j, uint32_t tokens, bool many, hipStream_t s)
+{
+    if (many) return launch(latent_join_kernel<kD, 4>, dim3(tokens, j.heads), dim3(256), 0, s, nullptr, j);
+    return launch(latent_join_kernel<kD, 1>, dim3(tokens, (j.heads + 3u) / 4u), dim3(256), 0, s, nullptr, j);
 }
 
-static uint32_t wide_of(uint32_t tokens, uint32_t rows, uint32_t heads) { return (uint64_t)tokens * heads >= 64ull * rows ? 1u : 0u; }
-static uint32_t attend_rows(uint32_t tokens, uint32_t rows, uint32_t heads) { return wide_of(tokens, rows, heads) ? 128u : 16u; }
+// Query rows of a tile: 16, 32, 64 or 128, as many as a request has.
+static uint32_t attend_rows(uint32_t tokens, uint32_t rows, uint32_t heads)
+{
+    const uint64_t n = (uint64_t)tokens * heads, r = rows < tokens ? rows : tokens;
+    return n <= 16u * r ? 16u : n <= 32u * r ? 32u : n <= 64u * r ? 64u : 128u;
+}
+static uint64_t attend_tiles(uint32_t tokens, uint32_t rows, uint32_t heads) { return (uint64_t)tokens * heads / attend_rows(tokens, rows, heads) + (rows < tokens ? rows : tokens); }
 
 bool latent_attend_fits(uint32_t tokens, uint32_t rows, uint32_t heads)
 {
-    return (uint64_t)tokens * heads / attend_rows(tokens, rows, heads) + rows <= 0xFFFFFFu;
+    return (uint64_t)tokens * heads / attend_rows(tokens, rows, heads) + rows <= 0x7FFFFFu;
 }
 
-uint32_t latent_attend_splits(uint32_t tokens, uint32_t rows, uint32_t heads, uint32_t columns, uint32_t shift)
+static Plan attend_plan(uint32_t tokens, uint32_t rows, uint32_t heads, uint32_t latent, uint32_t columns, uint32_t shift)
 {
-    if (rows > 1024u) return 1u;
-    const uint64_t blocks = (((uint64_t)columns << shift) + kAttendBlock - 1u) / kAttendBlock, requests = tokens < rows ? tokens : rows;
-    const uint64_t n0 = (uint64_t)tokens * heads / attend_rows(tokens, rows, heads), n = n0 > requests ? n0 : requests;
-    const uint64_t want = n >= 4u * kAttendShares ? 1u : 4u * ((kAttendShares + n - 1u) / n), most = (blocks + kAttendLeast - 1u) / kAttendLeast;
-    const uint64_t splits = want < most ? want : most;
-    return splits < 1u ? 1u : splits > 128u ? 128u : (uint32_t)splits;
+    const uint64_t blocks = (((uint64_t)columns << shift) + kAttendBlock - 1u) / kAttendBlock;
+    return plan_of(attend_tiles(tokens, rows, heads), blocks, rows, attend_rows(tokens, rows, heads), latent, kAttendSlots, (uint64_t)tokens * heads);
+}
+uint64_t latent_attend_bytes(uint32_t tokens, uint32_t rows, uint32_t heads, uint32_t latent, uint32_t columns, uint32_t shift)
+{
+    return plan_bytes(attend_plan(tokens, rows, heads, latent, columns, shift));
 }
 
 template <uint32_t kC, bool kBytes>
 static hipError_t launch_latent(const LatentAttendArgs &a, hipStream_t s)
 {
     const uint32_t rows = attend_rows(a.of.tokens, a.of.rows, a.of.heads);
-    const dim3 grid((uint32_t)((uint64_t)a.of.tokens * a.of.heads / rows) + a.of.rows, a.of.splits);
-    const hipError_t e = launch(rows == 128u ? latent_attend_kernel<kC, kBytes, 1, 8, 8> : latent_attend_kernel<kC, kBytes, 1, 1, 4>, grid, dim3(rows == 128u ? 512u : 256u), 0, s, nullptr, a);
-    if (e != hipSuccess || a.of.splits == 1u) return e;
-    return launch_join<kC>(JoinArgs{a.partial, a.ends, a.shares, a.of.starts + a.of.rows, a.out, a.of.heads, a.of.splits}, a.of.tokens, s);
+    const dim3 grid(a.of.chunks ? a.of.chunks : (uint32_t)((uint64_t)a.of.tokens * a.of.heads / rows) + a.of.rows);
+    const hipError_t e = launch(rows == 16u ? latent_attend_kernel<kC, kBytes, 1, 2> : rows == 32u ? latent_attend_kernel<kC, kBytes, 2, 2> : rows == 64u ? latent_attend_kernel<kC, kBytes, 4, 2>
+                                : latent_attend_kernel<kC, kBytes, 8, 1>, grid, dim3(512), 0, s, nullptr, a);
+    if (e != hipSuccess || !a.of.chunks) return e;
+    return launch_join<kC>(JoinArgs{a.partial, a.ends, a.parts, a.of.starts, a.out, a.of.rows, a.of.heads, a.of.chunks, rows}, a.of.tokens, a.of.chunks > 8u * a.of.rows, s);
 }
 
 hipError_t launch_latent_attend(const void *q_c, const void *q_r, uint32_t tokens, uint32_t heads, uint32_t latent, const int64_t (&strides)[4], const void *c_cache, const void *r_cache,
                                 const float *scale, uint32_t pages, uint32_t shift, const int32_t *table, uint32_t rows, uint32_t columns, const int32_t *lens,
                                 const int32_t *starts, float factor, void *out, void *workspace, hipStream_t s)
 {
-    const uint32_t splits = latent_attend_splits(tokens, rows, heads, columns, shift);
-    float *partial = static_cast<float *>(workspace), *ends = partial + (splits > 1u ? (size_t)tokens * heads * splits * latent : 0u);
-    const LatentAttendArgs a{{starts, rows, tokens, heads, splits, kAttendLeast}, static_cast<const uint16_t *>(q_c), static_cast<const uint16_t *>(q_r),
+    const Plan p = attend_plan(tokens, rows, heads, latent, columns, shift);
+    float *partial = static_cast<float *>(workspace), *ends = partial + p.partial;
+    const LatentAttendArgs a{{starts, rows, tokens, heads, p.chunks}, static_cast<const uint16_t *>(q_c), static_cast<const uint16_t *>(q_r),
                              strides[0], strides[1], strides[2], strides[3], static_cast<const uint8_t *>(c_cache), static_cast<const uint16_t *>(r_cache), scale, table, lens,
-                             static_cast<uint16_t *>(out), partial, ends, reinterpret_cast<uint32_t *>(ends + (splits > 1u ? (size_t)tokens * heads * splits * 2u : 0u)),
-                             factor * 1.44269504088896340736f, columns, pages, shift};
+                             static_cast<uint16_t *>(out), partial, ends, reinterpret_cast<Parts *>(ends + p.ends), factor * 1.44269504088896340736f, columns, pages, shift};
     if (latent == 512u) return scale ? launch_latent<512, true>(a, s) : launch_latent<512, false>(a, s);
     return scale ? launch_latent<256, true>(a, s) : launch_latent<256, false>(a, s);
 }
@@ -549,8 +628,8 @@ struct LatentPromptArgs {
     int64_t qn_token, qn_head, qr_token, qr_head, kn_token, kn_head, kr_token, v_token, v_head;
     const int32_t *key_starts;
     uint16_t *out;                                   // [token][head][D]
-    float *partial, *ends;
-    uint32_t *shares;
+    float *partial, *ends;                           // as in LatentAttendArgs
+    Parts *parts;
     float factor;
     uint32_t keys;
 };
@@ -572,23 +651,37 @@ latent_prompt_kernel(const LatentPromptArgs a)
     __shared__ __attribute__((aligned(16))) uint16_t keys[kPromptKeys * kPitch], values[kPromptKeys * kValuePitch];
     __shared__ uint32_t odd_from[kD], any_from;       // of each dim, the first key whose value is none, of those that some rows do not see; the first of all
     const uint32_t tid = threadIdx.x, lane = tid & 63u, wave = __builtin_amdgcn_readfirstlane(tid >> 6), m = lane & 15u, g = lane >> 4;
-    const uint32_t head = blockIdx.y, split = blockIdx.z;
+    const uint32_t heads = a.of.heads;
+    auto tiles = [&](uint32_t r) { return (tokens_of(a.of, r) + kPromptRows - 1u) / kPromptRows; };
+    auto blocks_at = [&](uint32_t r) { uint32_t none; return blocks_of(keys_of(a, r, &none)); };
     Tile t;
-    uint32_t count, begin;
-    if (!tile_of<kPromptRows>(a.of, 1u, blockIdx.x, &t, &count)) return;
+    Chunk c{0u, 1u, 0u, 0u, 0u};
+    uint32_t head = blockIdx.x % heads;
+    if (a.of.chunks ? !chunk_of(a.of, blockIdx.x, [&](uint32_t r) { return tiles(r) * heads * blocks_at(r); }, &c) : !tile_of<kPromptRows>(a.of, 1u, blockIdx.x / heads, &t)) return;
+    if (!a.of.chunks) (void)tile_at<kPromptRows>(a.of, 1u, t.row, tiles(t.row) - 1u - t.first / kPromptRows, &t);             // the last, which see the most keys, first
+    while (c.at < c.end) {
+    uint32_t b0 = 0, n_blocks = 1u, blocks = 1u, begins = 0, begin;
+    if (a.of.chunks) {
+        const uint32_t work = tiles(c.row) * heads * (blocks = blocks_at(c.row)), unit = c.off / blocks;
+        if (!work) { c.row++; continue; }            // (off is 0)
+        head = unit % heads;
+        (void)tile_at<kPromptRows>(a.of, 1u, c.row, unit / heads, &t);
+        b0 = c.off - unit * blocks;
+        n_blocks = blocks - b0 < c.end - c.at ? blocks - b0 : c.end - c.at;
+        begins = c.at - b0;
+        c.off += n_blocks;
+        if (c.off >= work) { c.off = 0; c.row++; }
+    }
     const uint32_t len = keys_of(a, t.row, &begin);
-    t.before = (int32_t)len - (int32_t)count;
-    uint32_t per;
-    const uint32_t shares = shares_of(a.of, (len + kAttendBlock - 1u) / kAttendBlock, &per, [&](uint32_t r) {
-        const uint32_t n = (uint32_t)a.of.starts[r + 1u] - (uint32_t)a.of.starts[r];
-        uint32_t none;
-        return (uint64_t)((keys_of(a, r, &none) + kAttendBlock - 1u) / kAttendBlock) * ((n + kPromptRows - 1u) / kPromptRows) * a.of.heads;
-    });
-    if (a.of.splits > 1u && split == 0u && head == 0u && tid < kPromptRows && t.first + tid < t.last) a.shares[t.begin + t.first + tid] = shares;
-    if (split >= shares) return;
-    auto seen_by = [&](uint32_t i) { const int32_t n = t.before + (int32_t)i + 1; return n < 0 ? 0u : (uint32_t)n; };
+    t.before = (int32_t)len - (int32_t)t.count;
+    const bool whole = n_blocks == blocks;
+    const uint32_t place = 2u * blockIdx.x + (b0 ? 0u : 1u);
+    if (a.of.chunks && b0 == 0u && tid < kPromptRows && t.first + tid < t.last)
+        a.parts[(size_t)(t.begin + t.first + tid) * heads + head] = Parts{blockIdx.x | tid << 16, whole ? 1u : (begins + blocks - 1u) / c.size - blockIdx.x + 1u};
+    c.at += n_blocks;
+    auto seen_by = [&](uint32_t i) { const int32_t k = t.before + (int32_t)i + 1; return k < 0 ? 0u : (uint32_t)k; };
     const uint32_t seen_least = seen_by(t.first), seen_most = seen_by(t.last - 1u);
-    const uint32_t from = split * per * kAttendBlock, to0 = shares > 1u ? from + per * kAttendBlock : seen_most, to = to0 < seen_most ? to0 : seen_most;
+    const uint32_t from = b0 * kAttendBlock, to0 = whole ? seen_most : from + n_blocks * kAttendBlock, to = to0 < seen_most ? to0 : seen_most;
     Half8 q[kM][kSteps];
     uint32_t sees[kM];
 #pragma unroll
@@ -622,10 +715,10 @@ latent_prompt_kernel(const LatentPromptArgs a)
             if (key < to) tops[i] = *reinterpret_cast<const Word4 *>(k_r + (int64_t)key * a.kr_token + lane % 8u * 8u);
         }
     };
+    if (from < to) fetch(from);
     if (tid < kD) odd_from[tid] = kNone;
     if (tid == 0u) any_from = kNone;
     __syncthreads();
-    if (from < to) fetch(from);
     for (uint32_t block = from; block < to; block += kPromptKeys) {
         const bool partly = block + kPromptKeys > seen_least;
 #pragma unroll
@@ -691,50 +784,47 @@ latent_prompt_kernel(const LatentPromptArgs a)
         const float sum = sums.whole_sum(n);
         const uint32_t own = t.first + (wave * kM + n) * 16u + m;
         const bool any = sees[n] > from;
-        const float by = share_of_sum(sum, any && shares == 1u);
+        const float by = share_of_sum(sum, any && whole);
         if (own >= t.last) continue;
-        const size_t at = (size_t)(t.begin + own) * a.of.heads + head;
+        const size_t at = (size_t)(t.begin + own) * heads + head, part = (size_t)place * kPromptRows + own - t.first;
 #pragma unroll
         for (uint32_t d = 0; d < kParts; d++) {
             Float4 v = sums.acc[d][n] * by;
             if (any_from != kNone)
 #pragma unroll
                 for (uint32_t e = 0; e < 4u; e++) v[e] = odd_from[d * 16u + g * 4u + e] < sees[n] ? __builtin_nanf("") : v[e];
-            if (shares > 1u) *reinterpret_cast<Float4 *>(a.partial + (at * a.of.splits + split) * kD + d * 16u + g * 4u) = v;
-            else *reinterpret_cast<Word2 *>(a.out + at * kD + d * 16u + g * 4u) = Word2{pk_bf16(v[0], v[1]), pk_bf16(v[2], v[3])};
+            if (whole) *reinterpret_cast<Word2 *>(a.out + at * kD + d * 16u + g * 4u) = Word2{pk_bf16(v[0], v[1]), pk_bf16(v[2], v[3])};
+            else *reinterpret_cast<Float4 *>(a.partial + part * kD + d * 16u + g * 4u) = v;
         }
-        if (shares > 1u && g == 0u) {
-            float *to_ends = a.ends + (at * a.of.splits + split) * 2u;
-            to_ends[0] = sums.base[n]; to_ends[1] = any && sum == 0.f ? kEmpty : sum;
-        }
+        if (!whole && g == 0u) *reinterpret_cast<Float2 *>(a.ends + part * 2u) = Float2{sums.base[n], any && sum == 0.f ? kEmpty : sum};
+    }
+    __syncthreads();
     }
 }
 
-bool latent_prompt_fits(uint32_t tokens, uint32_t rows) { return (uint64_t)tokens / kPromptRows + rows <= 0xFFFFFFu; }
+bool latent_prompt_fits(uint32_t tokens, uint32_t rows, uint32_t heads) { return ((uint64_t)tokens / kPromptRows + rows) * heads <= 0xFFFFFFu; }
 
-uint32_t latent_prompt_splits(uint32_t tokens, uint32_t rows, uint32_t heads, uint32_t keys)
+static Plan prompt_plan(uint32_t tokens, uint32_t rows, uint32_t heads, uint32_t dim, uint32_t keys)
 {
-    if (rows > 1024u) return 1u;
-    const uint64_t blocks = ((uint64_t)keys + kAttendBlock - 1u) / kAttendBlock, requests = tokens < rows ? tokens : rows;
-    const uint64_t n = ((uint64_t)tokens / kPromptRows + requests) * heads;
-    const uint64_t want = kAttendShares * 2u / n, most = (blocks + kAttendLeast - 1u) / kAttendLeast, splits = want < most ? want : most;
-    return splits < 1u ? 1u : splits > 64u ? 64u : (uint32_t)splits;
+    const uint64_t tiles = ((uint64_t)tokens / kPromptRows + (rows < tokens ? rows : tokens)) * heads, blocks = ((uint64_t)keys + kAttendBlock - 1u) / kAttendBlock;
+    return plan_of(tiles, blocks, rows, kPromptRows, dim, kPromptSlots, (uint64_t)tokens * heads);
 }
+uint64_t latent_prompt_bytes(uint32_t tokens, uint32_t rows, uint32_t heads, uint32_t dim, uint32_t keys) { return plan_bytes(prompt_plan(tokens, rows, heads, dim, keys)); }
 
 hipError_t launch_latent_prompt(const void *q_n, const void *q_r, const void *k_n, const void *k_r, const void *v, uint32_t tokens, uint32_t keys, uint32_t heads, uint32_t dim,
                                 const int64_t (&strides)[9], uint32_t rows, const int32_t *starts, const int32_t *key_starts, float factor, void *out, void *workspace, hipStream_t s)
 {
-    const uint32_t splits = latent_prompt_splits(tokens, rows, heads, keys);
-    float *partial = static_cast<float *>(workspace), *ends = partial + (splits > 1u ? (size_t)tokens * heads * splits * dim : 0u);
-    auto halves = [](const void *p) { return static_cast<const uint16_t *>(p); };
-    const LatentPromptArgs a{{starts, rows, tokens, heads, splits, kAttendLeast}, halves(q_n), halves(q_r), halves(k_n), halves(k_r), halves(v),
+    const Plan p = prompt_plan(tokens, rows, heads, dim, keys);
+    float *partial = static_cast<float *>(workspace), *ends = partial + p.partial;
+    auto halves = [](const void *x) { return static_cast<const uint16_t *>(x); };
+    const LatentPromptArgs a{{starts, rows, tokens, heads, p.chunks}, halves(q_n), halves(q_r), halves(k_n), halves(k_r), halves(v),
                              strides[0], strides[1], strides[2], strides[3], strides[4], strides[5], strides[6], strides[7], strides[8], key_starts, static_cast<uint16_t *>(out),
-                             partial, ends, reinterpret_cast<uint32_t *>(ends + (splits > 1u ? (size_t)tokens * heads * splits * 2u : 0u)), factor * 1.44269504088896340736f, keys};
-    const dim3 grid(tokens / kPromptRows + rows, heads, splits);
+                             partial, ends, reinterpret_cast<Parts *>(ends + p.ends), factor * 1.44269504088896340736f, keys};
+    const dim3 grid(p.chunks ? p.chunks : (tokens / kPromptRows + rows) * heads);
     const hipError_t e = launch(dim == 128u ? latent_prompt_kernel<128> : latent_prompt_kernel<64>, grid, dim3(kThreads), 0, s, nullptr, a);
-    if (e != hipSuccess || splits == 1u) return e;
-    const JoinArgs j{a.partial, a.ends, a.shares, starts + rows, a.out, heads, splits};
-    return dim == 128u ? launch_join<128>(j, tokens, s) : launch_join<64>(j, tokens, s);
+    if (e != hipSuccess || !p.chunks) return e;
+    const JoinArgs j{a.partial, a.ends, a.parts, starts, a.out, rows, heads, p.chunks, kPromptRows};
+    return dim == 128u ? launch_join<128>(j, tokens, false, s) : launch_join<64>(j, tokens, false, s);
 }
 
 }  // namespace wg

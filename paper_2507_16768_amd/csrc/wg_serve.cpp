@@ -236,8 +236,7 @@ int wg_latent_read(const void *d_c_cache, const void *d_r_cache, const float *d_
 
 uint64_t wg_latent_attend_workspace(uint32_t tokens, uint32_t rows, uint32_t heads, uint32_t latent, uint32_t columns, uint32_t page_tokens) {
     if (!tokens || !rows || !heads || !columns || !shift_of(page_tokens)) return 0;
-    const uint64_t splits = latent_attend_splits(tokens, rows, heads, columns, shift_of(page_tokens));
-    return splits < 2u ? 0u : ((uint64_t)tokens * heads * splits * (latent + 2u) + tokens) * 4u;
+    return latent_attend_bytes(tokens, rows, heads, latent, columns, shift_of(page_tokens));
 }
 
 int wg_latent_attend(const void *d_q_c, const void *d_q_r, uint32_t tokens, uint32_t heads, uint32_t latent, int64_t c_token_stride, int64_t c_head_stride, int64_t r_token_stride,
@@ -265,8 +264,7 @@ int wg_latent_attend(const void *d_q_c, const void *d_q_r, uint32_t tokens, uint
 
 uint64_t wg_latent_prompt_workspace(uint32_t tokens, uint32_t rows, uint32_t heads, uint32_t dim, uint32_t keys) {
     if (!tokens || !rows || !heads || !keys) return 0;
-    const uint64_t splits = latent_prompt_splits(tokens, rows, heads, keys);
-    return splits < 2u ? 0u : ((uint64_t)tokens * heads * splits * (dim + 2u) + tokens) * 4u;
+    return latent_prompt_bytes(tokens, rows, heads, dim, keys);
 }
 
 int wg_latent_prompt(const void *d_q_n, const void *d_q_r, const void *d_k_n, const void *d_k_r, const void *d_v, uint32_t tokens, uint32_t keys, uint32_t heads, uint32_t dim,
@@ -278,7 +276,7 @@ int wg_latent_prompt(const void *d_q_n, const void *d_q_r, const void *d_k_n, co
         WG_WANT(tokens && rows && keys && heads, "no tokens, rows, keys or heads");
         WG_WANT(tokens <= 0x7FFFFFFFu && keys <= 0x7FFFFFFFu && rows <= kMostRows && heads <= 4096u && (uint64_t)tokens * heads <= 0x7FFFFFFFull, "too many tokens, keys, rows or heads");
         WG_WANT(dim == 64u || dim == 128u, "dim must be 64 or 128");
-        WG_WANT(latent_prompt_fits(tokens, rows), "too many tokens for one launch");
+        WG_WANT(latent_prompt_fits(tokens, rows, heads), "too many tokens for one launch");
         WG_WANT(by_sixteen(d_q_n, q_n_token_stride, q_n_head_stride) && by_sixteen(d_q_r, q_r_token_stride, q_r_head_stride) && by_sixteen(d_k_n, k_n_token_stride, k_n_head_stride) &&
                 by_sixteen(d_k_r, k_r_token_stride, 0) && by_sixteen(d_v, v_token_stride, v_head_stride), "queries, keys and values must lie at multiples of 16 bytes");
         WG_WANT(aligned(d_out, 16), "the output must be 16-byte aligned");

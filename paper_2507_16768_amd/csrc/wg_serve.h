@@ -41,17 +41,16 @@ hipError_t launch_latent_append(const void *c, const void *r, uint32_t tokens, u
                                 void *c_cache, void *r_cache, float *scale, uint32_t pages, uint32_t shift, hipStream_t s);
 hipError_t launch_latent_read(const void *c_cache, const void *r_cache, const float *scale, uint32_t latent, uint32_t pages, uint32_t shift, const int32_t *table, uint32_t rows,
                               uint32_t columns, const int32_t *starts, uint32_t tokens, void *c_out, int64_t c_token, void *r_out, int64_t r_token, hipStream_t s);
-// Keys of a block, blocks of a share at least, and shares in all, about.
-constexpr uint32_t kAttendBlock = 128, kAttendLeast = 2, kAttendShares = 256;
+// Keys of a block, blocks of a chunk of work at least, and chunks at most: as many workgroups as the chip holds at a time.
+constexpr uint32_t kAttendBlock = 128, kAttendLeast = 2, kAttendSlots = 256, kPromptSlots = 512;
 bool latent_attend_fits(uint32_t tokens, uint32_t rows, uint32_t heads);
-// Shares that a row's keys may be cut into; each leaves an output in fp32, a base and a sum for every token and head.
-uint32_t latent_attend_splits(uint32_t tokens, uint32_t rows, uint32_t heads, uint32_t columns, uint32_t shift);
+uint64_t latent_attend_bytes(uint32_t tokens, uint32_t rows, uint32_t heads, uint32_t latent, uint32_t columns, uint32_t shift);
 // strides: of tokens and heads of q_c and q_r.
 hipError_t launch_latent_attend(const void *q_c, const void *q_r, uint32_t tokens, uint32_t heads, uint32_t latent, const int64_t (&strides)[4], const void *c_cache, const void *r_cache,
                                 const float *scale, uint32_t pages, uint32_t shift, const int32_t *table, uint32_t rows, uint32_t columns, const int32_t *lens,
                                 const int32_t *starts, float factor, void *out, void *workspace, hipStream_t s);
-bool latent_prompt_fits(uint32_t tokens, uint32_t rows);
-uint32_t latent_prompt_splits(uint32_t tokens, uint32_t rows, uint32_t heads, uint32_t keys);
+bool latent_prompt_fits(uint32_t tokens, uint32_t rows, uint32_t heads);
+uint64_t latent_prompt_bytes(uint32_t tokens, uint32_t rows, uint32_t heads, uint32_t dim, uint32_t keys);
 // strides: of tokens and heads of q_n, q_r and k_n, of tokens of k_r, of tokens and heads of v.
 hipError_t launch_latent_prompt(const void *q_n, const void *q_r, const void *k_n, const void *k_r, const void *v, uint32_t tokens, uint32_t keys, uint32_t heads, uint32_t dim,
                                 const int64_t (&strides)[9], uint32_t rows, const int32_t *starts, const int32_t *key_starts, float factor, void *out, void *workspace, hipStream_t s);
