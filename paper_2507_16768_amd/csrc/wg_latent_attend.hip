@@ -152,6 +152,9 @@ __device__ __forceinline__ Word4 without_odd_dims(Word4 v, uint32_t key, uint32_
 // out of LDS would be waits for memory.)
 template <typename T> __device__ __forceinline__ T from_memory(const void *p) { return *(const __attribute__((address_space(1))) T *)p; }
 
+// x, which the compiler is not to know anything about.
+__device__ __forceinline__ uint32_t anew(uint32_t x) { asm volatile("" : "+v"(x)); return x; }
+
 // What is read in the place of a key that there is none of.
 __device__ __attribute__((aligned(16))) const uint8_t kZeros[1024] = {};
 
@@ -268,16 +271,16 @@ __global__ void __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))
 latent_attend_kernel(const LatentAttendArgs a)
 {
     constexpr uint32_t kW = 8u, kKeyGroups = kW / (kGroups * kCols), kKeys = 32u * kKeyGroups, kRows = 16u * kGroups;
-    constexpr uint32_t kSteps = (kC + kTop) / 32u, kParts = kC / 16u / kCols, kPitch = kC + kTop + 8u;
+    constexpr uint32_t kSteps = (kC + kTop) / 32u, kParts = kC / 16u / kCols, kPitch = kC + kTop + 16u, kGroupPitch = 32u * kPitch + 144u;
     constexpr uint32_t kRow = kC * (kBytes ? 1u : 2u), kPer = 1024u / kRow, kStage = kKeys / kW;          // bytes of a vector; keys of a wavefront's load; keys that it brings
-    constexpr uint32_t kLoads = kStage / kPer, kTops = (kStage + 7u) / 8u, kAhead = kC == 512u ? 2u : 4u, kPut = kC == 512u && kGroups == 8u ? 6u : 0u, kKept = kSteps - kPut;
-    constexpr uint32_t kJoinPitch = kC + 4u, kTileBytes = kKeys * kPitch * 2u, kJoinBytes = kKeyGroups > 1u ? kKeyGroups * kRows * kJoinPitch * 4u : 0u;
-    __shared__ __attribute__((aligned(16))) uint8_t room[kTileBytes > kJoinBytes ? kTileBytes : kJoinBytes];
+    constexpr uint32_t kLoads = kStage / kPer, kTops = (kStage + 7u) / 8u, kAhead = kC == 512u ? 2u : 4u, kPut = kC == 512u && kGroups == 8u ? 8u : 0u, kKept = kSteps - kPut;
+    constexpr uint32_t kJoinPitch = kC + 4u, kTile = kKeyGroups * kGroupPitch, kTileBytes = kTile * 2u, kJoinBytes = kKeyGroups > 1u ? kKeyGroups * kRows * kJoinPitch * 4u : 0u;
+    __shared__ __attribute__((aligned(16))) uint8_t room[2u * kTileBytes > kJoinBytes ? 2u * kTileBytes : kJoinBytes];   // two blocks of keys: one that is worked on, one that comes
     __shared__ uint32_t odd_from;                                          // the first key with a number that is none, of those that some rows do not see
     __shared__ float join_base[kKeyGroups][kRows], join_sum[kKeyGroups][kRows];
     __shared__ Half8 q_rest[kPut ? kW * kPut * 64u : 1u];                  // the last steps of the queries, each lane its own: there are no registers for them
     uint16_t *keys = reinterpret_cast<uint16_t *>(room);
-    const uint32_t tid = threadIdx.x, lane = tid & 63u, wave = __builtin_amdgcn_readfirstlane(tid >> 6), m = lane & 15u, g = lane >> 4;
+    const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const uint32_t group = wave % kGroups, column_group = wave / kGroups % kCols, key_group = wave / (kGroups * kCols);
     const uint32_t P = 1u << a.shift, heads = a.of.heads;
     auto tiles = [&](uint32_t r) { return (uint32_t)(((uint64_t)tokens_of(a.of, r) * heads + kRows - 1u) / kRows); };
@@ -285,6 +288,8 @@ latent_attend_kernel(const LatentAttendArgs a)
     Chunk c{0u, 1u, 0u, 0u, 0u};
     if (a.of.chunks ? !chunk_of(a.of, blockIdx.x, [&](uint32_t r) { return tiles(r) * blocks_of(cached_tokens(a, r)); }, &c) : !tile_of<kRows>(a.of, heads, blockIdx.x, &t)) return;
     while (c.at < c.end) {
+        // (What follows from the thread's number is made anew for each part: kept over the parts it would take registers from the loop over keys.)
+        const uint32_t tid = anew(threadIdx.x), lane = tid & 63u, m = lane & 15u, g = lane >> 4;
         // the next part of a tile: blocks [b0, b0 + n) of its `blocks`
         uint32_t b0 = 0, n = 1u, blocks = 1u, begins = 0;                  // begins: where the tile's blocks do, among all
         if (a.of.chunks) {
@@ -335,12 +340,41 @@ latent_attend_kernel(const LatentAttendArgs a)
                 tops[i] = from_memory<Word4>((slot != kNone ? reinterpret_cast<const uint8_t *>(a.r_cache) + (size_t)slot * (kTop * 2u) : kZeros) + lane % 8u * 16u);
             }
         };
+        // Keys of a block into LDS.  A group of 32 keys has 16 bytes more than its rows would take behind every eighth, and a half more behind the sixteenth, so that what sixteen lanes read at a
+        // time, the same place of rows 0 .. 3, 8 .. 11, 16 .. 19 and 24 .. 27 or 32 bytes of four neighbouring rows, lies in different banks.
+        auto row_at = [&](uint32_t key) { return key / 32u * kGroupPitch + key % 32u * kPitch + (key & 8u ? 72u : 0u) + (key & 16u ? 64u : 0u); };
+        auto stage = [&](uint32_t block, uint16_t *to_keys) {
+            const bool partly = block + kKeys > seen_least;                // some of the tile's rows do not see all of the block's keys
+#pragma unroll
+            for (uint32_t i = 0; i < kLoads; i++) {
+                const uint32_t key = wave * kStage + i * kPer + lane / (64u / kPer), at = lane % (64u / kPer);
+                if (kBytes) {
+                    const float scale = scales[i % (kBytes ? kLoads : 1u)];
+                    const Word2 w0 = wider(raw[i][0], scale), w1 = wider(raw[i][1], scale), w2 = wider(raw[i][2], scale), w3 = wider(raw[i][3], scale);
+                    Word4 x{w0[0], w0[1], w1[0], w1[1]}, y{w2[0], w2[1], w3[0], w3[1]};
+                    if (partly) { x = without_odd(x, block + key, &odd_from); y = without_odd(y, block + key, &odd_from); }
+                    Word4 *put = reinterpret_cast<Word4 *>(to_keys + row_at(key) + at * 16u);
+                    put[0] = x; put[1] = y;
+                } else {
+                    if (partly) raw[i] = without_odd(raw[i], block + key, &odd_from);
+                    *reinterpret_cast<Word4 *>(to_keys + row_at(key) + at * 8u) = raw[i];
+                }
+            }
+            if (kStage >= 8u || lane < kStage * 8u)
+#pragma unroll
+                for (uint32_t i = 0; i < kTops; i++) *reinterpret_cast<Word4 *>(to_keys + row_at(wave * kStage + i * 8u + lane / 8u) + kC + lane % 8u * 8u) = tops[i];
+        };
         uint32_t ahead = 0;
         if (from < to) {
             const uint32_t first = page_of(from);
             ahead = page_of(from + kKeys);
             fetch(slot_of(from, first));
         }
+        auto fetch_next = [&](uint32_t block) {
+            const uint32_t slots = slot_of(block, ahead);
+            ahead = page_of(block + kKeys);
+            fetch(slots);
+        };
 
         // queries: a row behind the last is the last again, and is not stored
         Half8 q[kKept];
@@ -361,33 +395,14 @@ latent_attend_kernel(const LatentAttendArgs a)
         sums.clear();
         if (tid == 0u) odd_from = kNone;
         __syncthreads();
-        for (uint32_t block = from; block < to; block += kKeys) {
-            const bool partly = block + kKeys > seen_least;                    // some of the tile's rows do not see all of the block's keys
-#pragma unroll
-            for (uint32_t i = 0; i < kLoads; i++) {
-                const uint32_t key = wave * kStage + i * kPer + lane / (64u / kPer), at = lane % (64u / kPer);
-                if (kBytes) {
-                    const float scale = scales[i % (kBytes ? kLoads : 1u)];
-                    const Word2 w0 = wider(raw[i][0], scale), w1 = wider(raw[i][1], scale), w2 = wider(raw[i][2], scale), w3 = wider(raw[i][3], scale);
-                    Word4 x{w0[0], w0[1], w1[0], w1[1]}, y{w2[0], w2[1], w3[0], w3[1]};
-                    if (partly) { x = without_odd(x, block + key, &odd_from); y = without_odd(y, block + key, &odd_from); }
-                    Word4 *put = reinterpret_cast<Word4 *>(keys + key * kPitch + at * 16u);
-                    put[0] = x; put[1] = y;
-                } else {
-                    if (partly) raw[i] = without_odd(raw[i], block + key, &odd_from);
-                    *reinterpret_cast<Word4 *>(keys + key * kPitch + at * 8u) = raw[i];
-                }
-            }
-            if (kStage >= 8u || lane < kStage * 8u)
-#pragma unroll
-                for (uint32_t i = 0; i < kTops; i++) *reinterpret_cast<Word4 *>(keys + (wave * kStage + i * 8u + lane / 8u) * kPitch + kC + lane % 8u * 8u) = tops[i];
+        if (from < to) {
+            stage(from, keys);
+            if (from + kKeys < to) fetch_next(from + kKeys);
+        }
+        uint32_t turn = 0;
+        for (uint32_t block = from; block < to; block += kKeys, turn ^= 1u) {
             __syncthreads();
-            if (block + kKeys < to) {
-                const uint32_t slots = slot_of(block + kKeys, ahead);
-                ahead = page_of(block + 2u * kKeys);
-                fetch(slots);
-            }
-            const uint16_t *mine = keys + key_group * 32u * kPitch, *row = mine + (m / 4u * 8u + m % 4u) * kPitch + g * 8u;
+            const uint16_t *mine = keys + turn * kTile + key_group * kGroupPitch, *row = mine + row_at(m / 4u * 8u + m % 4u) + g * 8u;
             Float4 score[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
             Half8 k[2][kAhead];
             pipelined<2u * kSteps, kAhead>([&](uint32_t i, uint32_t at) { k[at / kAhead][at % kAhead] = *reinterpret_cast<const Half8 *>(row + i % 2u * 4u * kPitch + i / 2u * 32u); },
@@ -399,16 +414,20 @@ latent_attend_kernel(const LatentAttendArgs a)
             const uint32_t at = block + key_group * 32u + g * 8u;
 #pragma unroll
             for (uint32_t j = 0; j < 8u; j++) s[0][0][j] = score[j / 4u][j % 4u] * a.factor;
-            if (partly || block + kKeys > to)
+            if (block + kKeys > seen_least || block + kKeys > to)
 #pragma unroll
                 for (uint32_t j = 0; j < 8u; j++) s[0][0][j] = at + j < sees ? s[0][0][j] : -__builtin_inff();
             Half8 p[1][1];
             sums.template weigh<1>(s, p);
-            const uint16_t *column = mine + (g * 8u + m / 4u) * kPitch + column_group * (kC / kCols) + m % 4u * 4u;
+            if (block + kKeys < to) {
+                stage(block + kKeys, keys + (turn ^ 1u) * kTile);
+                if (block + 2u * kKeys < to) fetch_next(block + 2u * kKeys);
+            }
+            const uint16_t *column = mine + row_at(g * 8u + m / 4u) + column_group * (kC / kCols) + m % 4u * 4u;
             pipelined<kParts, kAhead>([&](uint32_t d, uint32_t at) { k[at / kAhead][at % kAhead] = both(column_of(column + d * 16u), column_of(column + 4u * kPitch + d * 16u)); },
                                       [&](uint32_t d, uint32_t at) { sums.acc[d][0] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k[at / kAhead][at % kAhead], p[0][0], sums.acc[d][0], 0, 0, 0); });
-            __syncthreads();
         }
+        __syncthreads();
 
         // Out: this part by itself, or the whole.  (Numbers that are none have been left out of the sums of rows that see only some of a block's keys: what a row that sees them makes of them
         // is none.)
@@ -600,7 +619,7 @@ static hipError_t launch_latent(const LatentAttendArgs &a, hipStream_t s)
 {
     const uint32_t rows = attend_rows(a.of.tokens, a.of.rows, a.of.heads);
     const dim3 grid(a.of.chunks ? a.of.chunks : (uint32_t)((uint64_t)a.of.tokens * a.of.heads / rows) + a.of.rows);
-    const hipError_t e = launch(rows == 16u ? latent_attend_kernel<kC, kBytes, 1, 2> : rows == 32u ? latent_attend_kernel<kC, kBytes, 2, 2> : rows == 64u ? latent_attend_kernel<kC, kBytes, 4, 2>
+    const hipError_t e = launch(rows == 16u ? latent_attend_kernel<kC, kBytes, 1, 4> : rows == 32u ? latent_attend_kernel<kC, kBytes, 2, 2> : rows == 64u ? latent_attend_kernel<kC, kBytes, 4, 2>
                                 : latent_attend_kernel<kC, kBytes, 8, 1>, grid, dim3(512), 0, s, nullptr, a);
     if (e != hipSuccess || !a.of.chunks) return e;
     return launch_join<kC>(JoinArgs{a.partial, a.ends, a.parts, a.of.starts, a.out, a.of.rows, a.of.heads, a.of.chunks, rows}, a.of.tokens, a.of.chunks > 8u * a.of.rows, s);
