@@ -212,9 +212,14 @@ struct Sums {
 #pragma unroll
             for (uint32_t k = 0; k < kGroups; k++) n = __builtin_fmaxf(n, __builtin_fmaxf(__builtin_fmaxf(__builtin_fmaxf(s[k][t][0], s[k][t][1]), __builtin_fmaxf(s[k][t][2], s[k][t][3])),
                                                                                           __builtin_fmaxf(__builtin_fmaxf(s[k][t][4], s[k][t][5]), __builtin_fmaxf(s[k][t][6], s[k][t][7]))));
-            n = most_of_rows(n);
-            const float from = n > -__builtin_inff() ? n : 0.f, by = __builtin_amdgcn_exp2f(base[t] - from);
-            base[t] = n; sum[t] *= by;
+            if (__ballot(n > base[t] + kLift)) {
+                n = most_of_rows(n);
+                const float by = __builtin_amdgcn_exp2f(base[t] - (n > -__builtin_inff() ? n : 0.f));
+                base[t] = n; sum[t] *= by;
+#pragma unroll
+                for (uint32_t d = 0; d < kParts; d++) acc[d][t] *= by;
+            }
+            const float from = base[t] > -__builtin_inff() ? base[t] : 0.f;
 #pragma unroll
             for (uint32_t k = 0; k < kGroups; k++) {
                 Word4 w;
@@ -225,8 +230,6 @@ struct Sums {
                 }
                 p[k][t] = __builtin_bit_cast(Half8, w);
             }
-#pragma unroll
-            for (uint32_t d = 0; d < kParts; d++) acc[d][t] *= by;
         }
     }
     // The queries' sums over all lanes.
@@ -395,19 +398,22 @@ latent_attend_kernel(const LatentAttendArgs a)
         sums.clear();
         if (tid == 0u) odd_from = kNone;
         __syncthreads();
-        if (from < to) {
-            stage(from, keys);
-            if (from + kKeys < to) fetch_next(from + kKeys);
-        }
+        if (from < to) stage(from, keys);
+        // (vmcnt(0): the queries are here before anything else is asked for.  A wait for them in the loop would be one for the keys that come)
+        __builtin_amdgcn_s_waitcnt(0x0F70);
+        if (from + kKeys < to) fetch_next(from + kKeys);
         uint32_t turn = 0;
         for (uint32_t block = from; block < to; block += kKeys, turn ^= 1u) {
             __syncthreads();
             const uint16_t *mine = keys + turn * kTile + key_group * kGroupPitch, *row = mine + row_at(m / 4u * 8u + m % 4u) + g * 8u;
             Float4 score[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
-            Half8 k[2][kAhead];
-            pipelined<2u * kSteps, kAhead>([&](uint32_t i, uint32_t at) { k[at / kAhead][at % kAhead] = *reinterpret_cast<const Half8 *>(row + i % 2u * 4u * kPitch + i / 2u * 32u); },
+            Half8 k[2][kAhead], rest[2][(kAhead + 1u) / 2u];
+            pipelined<2u * kSteps, kAhead>([&](uint32_t i, uint32_t at) {
+                                               k[at / kAhead][at % kAhead] = *reinterpret_cast<const Half8 *>(row + i % 2u * 4u * kPitch + i / 2u * 32u);
+                                               if (i / 2u >= kKept && i % 2u == 0u) rest[at / kAhead][at % kAhead / 2u] = q_rest[(wave * kPut + i / 2u - kKept) * 64u + lane];
+                                           },
                                            [&](uint32_t i, uint32_t at) {
-                                               const Half8 x = i / 2u < kKept ? q[i / 2u % kKept] : q_rest[(wave * kPut + i / 2u - kKept) * 64u + lane];
+                                               const Half8 x = i / 2u < kKept ? q[i / 2u % kKept] : rest[at / kAhead][at % kAhead / 2u];
                                                score[i % 2u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k[at / kAhead][at % kAhead], x, score[i % 2u], 0, 0, 0);
                                            });
             float s[1][1][8];
