@@ -499,14 +499,16 @@ struct JoinArgs {
     uint16_t *out;
     uint32_t requests, heads, chunks, rows;          // rows: of a tile
 };
-template <uint32_t kD, uint32_t kJoinWaves>
+// A workgroup takes 64 * kOwn dims of kHeads heads of a token, 4 / kHeads wavefronts to a head: few parts are a wavefront's, all dims of a row and all parts asked for together; many are
+// dealt out to four wavefronts, which take 64 dims, so that as many workgroups are at it.
+template <uint32_t kD, bool kMany>
 __global__ void __launch_bounds__(256)
 latent_join_kernel(const JoinArgs a)
 {
-    constexpr uint32_t kOwn = kD / 64u, kHeads = 4u / kJoinWaves, kRound = 8u;
-    __shared__ float part[kJoinWaves > 1u ? 4u : 1u][kD];
+    constexpr uint32_t kOwn = kMany ? 1u : kD / 64u, kShare = kMany ? 4u : 1u, kHeads = 4u / kShare, kRound = kMany ? 32u : 4u;
+    __shared__ float part[4][64];
     const uint32_t lane = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const uint32_t token = blockIdx.x, head = blockIdx.y * kHeads + wave / kJoinWaves, first = wave % kJoinWaves;
+    const uint32_t token = blockIdx.x, head = blockIdx.y * kHeads + wave / kShare, first = wave % kShare, d0 = (kMany ? blockIdx.z * 64u : 0u) + lane * kOwn;
     if (token < (uint32_t)a.starts[0] || token >= (uint32_t)a.starts[a.requests] || head >= a.heads) return;          // (a token of no row has no parts)
     const size_t at = (size_t)token * a.heads + head;
     const Parts p = a.parts[at];
@@ -514,61 +516,60 @@ latent_join_kernel(const JoinArgs a)
     if (p.chunks < 2u || row >= a.rows || chunk >= a.chunks) return;
     const uint32_t n = p.chunks < a.chunks - chunk ? p.chunks : a.chunks - chunk;
     auto place = [&](uint32_t i) { return (size_t)(i ? 2u * (chunk + i) : 2u * chunk + 1u) * a.rows + row; };
-    auto ends = [&](uint32_t i) { return *reinterpret_cast<const Float2 *>(a.ends + place(i) * 2u); };
+    // a lane for each part, 64 at a time: what it weighs
     float base = -__builtin_inff(), total = 0.f;
     bool any = false;
-    for (uint32_t i = lane; i < n; i += 64u) base = __builtin_fmaxf(base, ends(i)[0]);
+    float acc[kOwn];
 #pragma unroll
-    for (int o = 32; o > 0; o >>= 1) base = __builtin_fmaxf(base, __shfl_xor(base, o));
-    const float rel = base > -__builtin_inff() ? base : 0.f;
-    for (uint32_t i = lane; i < n; i += 64u) {
-        const Float2 e = ends(i);
+    for (uint32_t d = 0; d < kOwn; d++) acc[d] = 0.f;
+    for (uint32_t i0 = 0; i0 < n; i0 += 64u) {
+        const Float2 e = i0 + lane < n ? *reinterpret_cast<const Float2 *>(a.ends + place(i0 + lane) * 2u) : Float2{-__builtin_inff(), 0.f};
+        const uint32_t more = n - i0 < 64u ? n - i0 : 64u;
+        float v[kRound][kOwn];
+        auto ask = [&](uint32_t k0) {
+#pragma unroll
+            for (uint32_t k = 0; k < kRound; k++) {
+                const uint32_t i = k0 + k * kShare;
+                const float *from = a.partial + place(i0 + (i < more ? i : 0u)) * kD + d0;
+#pragma unroll
+                for (uint32_t d = 0; d < kOwn; d++) v[k][d] = from[d];
+            }
+        };
+        ask(first);
+        float top = __builtin_fmaxf(base, e[0]);
+#pragma unroll
+        for (int o = 32; o > 0; o >>= 1) top = __builtin_fmaxf(top, __shfl_xor(top, o));
+        const float rel = top > -__builtin_inff() ? top : 0.f, by = __builtin_amdgcn_exp2f(base - rel);
         any = any || e[1] == kEmpty;
-        if (e[1] != kEmpty && e[1] != 0.f) total += e[1] * __builtin_amdgcn_exp2f(e[0] - rel);
+        const float w = e[1] == kEmpty || e[1] == 0.f ? 0.f : e[1] * __builtin_amdgcn_exp2f(e[0] - rel);
+        total = total * by + w;
+        base = top;
+#pragma unroll
+        for (uint32_t d = 0; d < kOwn; d++) acc[d] *= by;
+        for (uint32_t k0 = first; k0 < more; k0 += kRound * kShare) {
+            if (k0 != first) ask(k0);
+#pragma unroll
+            for (uint32_t k = 0; k < kRound; k++) {
+                const uint32_t i = k0 + k * kShare;
+                const float wk = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(w), i < 64u ? i : 63u));
+                if (i >= more || wk == 0.f) continue;                      // (a part that weighs nothing may be anything)
+#pragma unroll
+                for (uint32_t d = 0; d < kOwn; d++) acc[d] += wk * v[k][d];
+            }
+        }
     }
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) total += __shfl_xor(total, o);
     const float by = share_of_sum(total, __ballot(any) != 0ull);
-    float acc[kOwn];
-#pragma unroll
-    for (uint32_t d = 0; d < kOwn; d++) acc[d] = 0.f;
-    for (uint32_t i0 = first; i0 < n; i0 += kRound * kJoinWaves) {
-        float v[kRound][kOwn], w[kRound];
-#pragma unroll
-        for (uint32_t k = 0; k < kRound; k++) {
-            const uint32_t i = i0 + k * kJoinWaves;
-            w[k] = 0.f;
-#pragma unroll
-            for (uint32_t d = 0; d < kOwn; d++) v[k][d] = 0.f;
-            if (i >= n) continue;
-            const Float2 e = ends(i);
-            if (e[1] == 0.f || e[1] == kEmpty) continue;
-            w[k] = e[1] * __builtin_amdgcn_exp2f(e[0] - rel) * by;
-            const float *from = a.partial + place(i) * kD + lane * kOwn;
-#pragma unroll
-            for (uint32_t d = 0; d < kOwn; d++) v[k][d] = from[d];
-        }
-#pragma unroll
-        for (uint32_t k = 0; k < kRound; k++)
-#pragma unroll
-            for (uint32_t d = 0; d < kOwn; d++) acc[d] += w[k] * v[k][d];
-    }
-    if (kJoinWaves > 1u) {
-#pragma unroll
-        for (uint32_t d = 0; d < kOwn; d++) part[wave % (kJoinWaves > 1u ? 4u : 1u)][lane * kOwn + d] = acc[d];
+    if (kMany) {
+        part[wave][lane] = acc[0];
         __syncthreads();
         if (wave) return;
-#pragma unroll
-        for (uint32_t d = 0; d < kOwn; d++) {
-            acc[d] = 0.f;
-#pragma unroll
-            for (uint32_t w = 0; w < 4u; w++) acc[d] += part[w % (kJoinWaves > 1u ? 4u : 1u)][lane * kOwn + d];
-        }
+        acc[0] = part[0][lane] + part[1][lane] + part[2][lane] + part[3][lane];
     }
-    if (total == 0.f && by != by)                    // (scores that are all -inf)
 #pragma unroll
-        for (uint32_t d = 0; d < kOwn; d++) acc[d] = by;
-    uint16_t *out = a.out + at * kD + lane * kOwn;
+    for (uint32_t d = 0; d < kOwn; d++) acc[d] *= by;                      // (nothing but -inf: 0 times none)
+    uint16_t *out = a.out + at * kD + d0;
     if (kOwn == 1u) out[0] = (uint16_t)pk_bf16(acc[0], 0.f);
     else
 #pragma unroll
@@ -593,8 +594,8 @@ uint64_t plan_bytes(const Plan &p) { return (p.partial + p.ends + p.parts) * 4u;
 template <uint32_t kD>
 static hipError_t launch_join(const JoinArgs &j, uint32_t tokens, bool many, hipStream_t s)
 {
-    if (many) return launch(latent_join_kernel<kD, 4>, dim3(tokens, j.heads), dim3(256), 0, s, nullptr, j);
-    return launch(latent_join_kernel<kD, 1>, dim3(tokens, (j.heads + 3u) / 4u), dim3(256), 0, s, nullptr, j);
+    if (many) return launch(latent_join_kernel<kD, true>, dim3(tokens, j.heads, kD / 64u), dim3(256), 0, s, nullptr, j);
+    return launch(latent_join_kernel<kD, false>, dim3(tokens, (j.heads + 3u) / 4u), dim3(256), 0, s, nullptr, j);
 }
 
 // Query rows of a tile: 16, 32, 64 or 128, as many as a request has.
@@ -628,7 +629,8 @@ static hipError_t launch_latent(const LatentAttendArgs &a, hipStream_t s)
     const hipError_t e = launch(rows == 16u ? latent_attend_kernel<kC, kBytes, 1, 4> : rows == 32u ? latent_attend_kernel<kC, kBytes, 2, 2> : rows == 64u ? latent_attend_kernel<kC, kBytes, 4, 2>
                                 : latent_attend_kernel<kC, kBytes, 8, 1>, grid, dim3(512), 0, s, nullptr, a);
     if (e != hipSuccess || !a.of.chunks) return e;
-    return launch_join<kC>(JoinArgs{a.partial, a.ends, a.parts, a.of.starts, a.out, a.of.rows, a.of.heads, a.of.chunks, rows}, a.of.tokens, a.of.chunks > 8u * a.of.rows, s);
+    return launch_join<kC>(JoinArgs{a.partial, a.ends, a.parts, a.of.starts, a.out, a.of.rows, a.of.heads, a.of.chunks, rows}, a.of.tokens,
+                           a.of.chunks > 32u * attend_tiles(a.of.tokens, a.of.rows, a.of.heads), s);
 }
 
 hipError_t launch_latent_attend(const void *q_c, const void *q_r, uint32_t tokens, uint32_t heads, uint32_t latent, const int64_t (&strides)[4], const void *c_cache, const void *r_cache,
@@ -671,12 +673,12 @@ template <uint32_t kD>
 __global__ void __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2)))
 latent_prompt_kernel(const LatentPromptArgs a)
 {
-    constexpr uint32_t kM = 2u, kSteps = (kD + kTop) / 32u, kParts = kD / 16u, kPitch = kD + kTop + 8u, kValuePitch = kD + 8u, kStage = kPromptKeys / kWaves;
-    constexpr uint32_t kPer = 512u / kD, kLoads = kStage / kPer, kTops = kStage / 8u;
-    __shared__ __attribute__((aligned(16))) uint16_t keys[kPromptKeys * kPitch], values[kPromptKeys * kValuePitch];
+    constexpr uint32_t kM = 2u, kSteps = (kD + kTop) / 32u, kParts = kD / 16u, kPitch = kD + kTop + 16u, kGroupPitch = 32u * kPitch + 144u, kValuePitch = kD + 16u, kValueGroup = 32u * kValuePitch + 144u,
+                       kStage = kPromptKeys / kWaves;
+    constexpr uint32_t kPer = 512u / kD, kLoads = kStage / kPer, kTops = kStage / 8u, kAhead = 3u;
+    __shared__ __attribute__((aligned(16))) uint16_t keys[kPromptKeys / 32u * kGroupPitch], values[kPromptKeys / 32u * kValueGroup];
     __shared__ uint32_t odd_from[kD], any_from;       // of each dim, the first key whose value is none, of those that some rows do not see; the first of all
-    const uint32_t tid = threadIdx.x, lane = tid & 63u, wave = __builtin_amdgcn_readfirstlane(tid >> 6), m = lane & 15u, g = lane >> 4;
-    const uint32_t heads = a.of.heads;
+    const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), heads = a.of.heads;
     auto tiles = [&](uint32_t r) { return (tokens_of(a.of, r) + kPromptRows - 1u) / kPromptRows; };
     auto blocks_at = [&](uint32_t r) { uint32_t none; return blocks_of(keys_of(a, r, &none)); };
     Tile t;
@@ -685,153 +687,155 @@ latent_prompt_kernel(const LatentPromptArgs a)
     if (a.of.chunks ? !chunk_of(a.of, blockIdx.x, [&](uint32_t r) { return tiles(r) * heads * blocks_at(r); }, &c) : !tile_of<kPromptRows>(a.of, 1u, blockIdx.x / heads, &t)) return;
     if (!a.of.chunks) (void)tile_at<kPromptRows>(a.of, 1u, t.row, tiles(t.row) - 1u - t.first / kPromptRows, &t);             // the last, which see the most keys, first
     while (c.at < c.end) {
-    uint32_t b0 = 0, n_blocks = 1u, blocks = 1u, begins = 0, begin;
-    if (a.of.chunks) {
-        const uint32_t work = tiles(c.row) * heads * (blocks = blocks_at(c.row)), unit = c.off / blocks;
-        if (!work) { c.row++; continue; }            // (off is 0)
-        head = unit % heads;
-        (void)tile_at<kPromptRows>(a.of, 1u, c.row, unit / heads, &t);
-        b0 = c.off - unit * blocks;
-        n_blocks = blocks - b0 < c.end - c.at ? blocks - b0 : c.end - c.at;
-        begins = c.at - b0;
-        c.off += n_blocks;
-        if (c.off >= work) { c.off = 0; c.row++; }
-    }
-    const uint32_t len = keys_of(a, t.row, &begin);
-    t.before = (int32_t)len - (int32_t)t.count;
-    const bool whole = n_blocks == blocks;
-    const uint32_t place = 2u * blockIdx.x + (b0 ? 0u : 1u);
-    if (a.of.chunks && b0 == 0u && tid < kPromptRows && t.first + tid < t.last)
-        a.parts[(size_t)(t.begin + t.first + tid) * heads + head] = Parts{blockIdx.x | tid << 16, whole ? 1u : (begins + blocks - 1u) / c.size - blockIdx.x + 1u};
-    c.at += n_blocks;
-    auto seen_by = [&](uint32_t i) { const int32_t k = t.before + (int32_t)i + 1; return k < 0 ? 0u : (uint32_t)k; };
-    const uint32_t seen_least = seen_by(t.first), seen_most = seen_by(t.last - 1u);
-    const uint32_t from = b0 * kAttendBlock, to0 = whole ? seen_most : from + n_blocks * kAttendBlock, to = to0 < seen_most ? to0 : seen_most;
-    Half8 q[kM][kSteps];
-    uint32_t sees[kM];
+        const uint32_t tid = anew(threadIdx.x), lane = tid & 63u, m = lane & 15u, g = lane >> 4;
+        uint32_t b0 = 0, n_blocks = 1u, blocks = 1u, begins = 0, begin;
+        if (a.of.chunks) {
+            const uint32_t work = tiles(c.row) * heads * (blocks = blocks_at(c.row)), unit = c.off / blocks;
+            if (!work) { c.row++; continue; }                              // (off is 0)
+            head = unit % heads;
+            (void)tile_at<kPromptRows>(a.of, 1u, c.row, unit / heads, &t);
+            b0 = c.off - unit * blocks;
+            n_blocks = blocks - b0 < c.end - c.at ? blocks - b0 : c.end - c.at;
+            begins = c.at - b0;
+            c.off += n_blocks;
+            if (c.off >= work) { c.off = 0; c.row++; }
+        }
+        const uint32_t len = keys_of(a, t.row, &begin);
+        t.before = (int32_t)len - (int32_t)t.count;
+        const bool whole = n_blocks == blocks;
+        const uint32_t place = 2u * blockIdx.x + (b0 ? 0u : 1u);
+        if (a.of.chunks && b0 == 0u && tid < kPromptRows && t.first + tid < t.last)
+            a.parts[(size_t)(t.begin + t.first + tid) * heads + head] = Parts{blockIdx.x | tid << 16, whole ? 1u : (begins + blocks - 1u) / c.size - blockIdx.x + 1u};
+        c.at += n_blocks;
+        auto seen_by = [&](uint32_t i) { const int32_t k = t.before + (int32_t)i + 1; return k < 0 ? 0u : (uint32_t)k; };
+        const uint32_t seen_least = seen_by(t.first), seen_most = seen_by(t.last - 1u);
+        const uint32_t from = b0 * kAttendBlock, to0 = whole ? seen_most : from + n_blocks * kAttendBlock, to = to0 < seen_most ? to0 : seen_most;
+
+        Word4 raw[kLoads], tops[kTops], raw_v[kLoads];
+        const uint8_t *k_n = reinterpret_cast<const uint8_t *>(a.k_n + (int64_t)begin * a.kn_token + (int64_t)head * a.kn_head), *k_r = reinterpret_cast<const uint8_t *>(a.k_r + (int64_t)begin * a.kr_token),
+                      *v_of = reinterpret_cast<const uint8_t *>(a.v + (int64_t)begin * a.v_token + (int64_t)head * a.v_head);
+        auto fetch = [&](uint32_t block) {
 #pragma unroll
-    for (uint32_t n = 0; n < kM; n++) {
-        const uint32_t i0 = t.first + (wave * kM + n) * 16u + m, i = i0 < t.last ? i0 : t.last - 1u, token = t.begin + i;
-        const uint16_t *qn = a.q_n + (int64_t)token * a.qn_token + (int64_t)head * a.qn_head + g * 8u, *qr = a.q_r + (int64_t)token * a.qr_token + (int64_t)head * a.qr_head + g * 8u;
-#pragma unroll
-        for (uint32_t s = 0; s < kSteps; s++) q[n][s] = *reinterpret_cast<const Half8 *>(s < kD / 32u ? qn + s * 32u : qr + (s - kD / 32u) * 32u);
-        const uint32_t all = seen_by(i);
-        sees[n] = all < to ? all : to;
-    }
-    Sums<kM, kParts> sums;
-    sums.clear();
-    Word4 raw[kLoads], tops[kTops], raw_v[kLoads];
-    const uint16_t *k_n = a.k_n + (int64_t)begin * a.kn_token + (int64_t)head * a.kn_head, *k_r = a.k_r + (int64_t)begin * a.kr_token,
-                   *v_of = a.v + (int64_t)begin * a.v_token + (int64_t)head * a.v_head;
-    auto fetch = [&](uint32_t block) {
-#pragma unroll
-        for (uint32_t i = 0; i < kLoads; i++) {
-            const uint32_t key = block + wave * kStage + i * kPer + lane / (64u / kPer), d = lane % (64u / kPer) * 8u;
-            raw[i] = Word4{0u, 0u, 0u, 0u}; raw_v[i] = Word4{0u, 0u, 0u, 0u};
-            if (key < to) {
-                raw[i] = *reinterpret_cast<const Word4 *>(k_n + (int64_t)key * a.kn_token + d);
-                raw_v[i] = *reinterpret_cast<const Word4 *>(v_of + (int64_t)key * a.v_token + d);
+            for (uint32_t i = 0; i < kLoads; i++) {
+                const uint32_t key = block + wave * kStage + i * kPer + lane / (64u / kPer), d = lane % (64u / kPer) * 16u;
+                raw[i] = from_memory<Word4>(key < to ? k_n + (int64_t)key * a.kn_token * 2 + d : kZeros);
+                raw_v[i] = from_memory<Word4>(key < to ? v_of + (int64_t)key * a.v_token * 2 + d : kZeros);
             }
-        }
 #pragma unroll
-        for (uint32_t i = 0; i < kTops; i++) {
-            const uint32_t key = block + wave * kStage + i * 8u + lane / 8u;
-            tops[i] = Word4{0u, 0u, 0u, 0u};
-            if (key < to) tops[i] = *reinterpret_cast<const Word4 *>(k_r + (int64_t)key * a.kr_token + lane % 8u * 8u);
-        }
-    };
-    if (from < to) fetch(from);
-    if (tid < kD) odd_from[tid] = kNone;
-    if (tid == 0u) any_from = kNone;
-    __syncthreads();
-    for (uint32_t block = from; block < to; block += kPromptKeys) {
-        const bool partly = block + kPromptKeys > seen_least;
-#pragma unroll
-        for (uint32_t i = 0; i < kLoads; i++) {
-            const uint32_t key = wave * kStage + i * kPer + lane / (64u / kPer), d = lane % (64u / kPer) * 8u;
-            if (partly && any_odd(raw_v[i])) {
-                atomicMin(&any_from, block + key);
-                raw_v[i] = without_odd_dims(raw_v[i], block + key, d, odd_from);
+            for (uint32_t i = 0; i < kTops; i++) {
+                const uint32_t key = block + wave * kStage + i * 8u + lane / 8u;
+                tops[i] = from_memory<Word4>(key < to ? k_r + (int64_t)key * a.kr_token * 2 + lane % 8u * 16u : kZeros);
             }
-            *reinterpret_cast<Word4 *>(keys + key * kPitch + d) = raw[i];
-            *reinterpret_cast<Word4 *>(values + key * kValuePitch + d) = raw_v[i];
-        }
+        };
+        // (where keys and values lie in LDS: as in latent_attend_kernel)
+        auto row_at = [&](uint32_t key) { return key / 32u * kGroupPitch + key % 32u * kPitch + (key & 8u ? 72u : 0u) + (key & 16u ? 64u : 0u); };
+        auto value_at = [&](uint32_t key) { return key / 32u * kValueGroup + key % 32u * kValuePitch + (key & 8u ? 72u : 0u) + (key & 16u ? 64u : 0u); };
+        auto stage = [&](uint32_t block) {
+            const bool partly = block + kPromptKeys > seen_least;
 #pragma unroll
-        for (uint32_t i = 0; i < kTops; i++) *reinterpret_cast<Word4 *>(keys + (wave * kStage + i * 8u + lane / 8u) * kPitch + kD + lane % 8u * 8u) = tops[i];
-        __syncthreads();
-        if (block + kPromptKeys < to) fetch(block + kPromptKeys);
-        Float4 score[2][2][kM];
-        const uint16_t *row = keys + (m / 4u * 8u + m % 4u) * kPitch + g * 8u;
-#pragma unroll
-        for (uint32_t k = 0; k < 2u; k++)
-#pragma unroll
-            for (uint32_t u = 0; u < 2u; u++) {
-#pragma unroll
-                for (uint32_t n = 0; n < kM; n++) score[k][u][n] = Float4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                for (uint32_t s = 0; s < kSteps; s++) {
-                    const Half8 x = *reinterpret_cast<const Half8 *>(row + (k * 32u + u * 4u) * kPitch + s * 32u);
-#pragma unroll
-                    for (uint32_t n = 0; n < kM; n++) score[k][u][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, q[n][s], score[k][u][n], 0, 0, 0);
+            for (uint32_t i = 0; i < kLoads; i++) {
+                const uint32_t key = wave * kStage + i * kPer + lane / (64u / kPer), d = lane % (64u / kPer) * 8u;
+                if (partly && any_odd(raw_v[i])) {
+                    atomicMin(&any_from, block + key);
+                    raw_v[i] = without_odd_dims(raw_v[i], block + key, d, odd_from);
                 }
+                *reinterpret_cast<Word4 *>(keys + row_at(key) + d) = raw[i];
+                *reinterpret_cast<Word4 *>(values + value_at(key) + d) = raw_v[i];
             }
-        float s[2][kM][8];
-        const uint32_t at = block + g * 8u;
 #pragma unroll
-        for (uint32_t k = 0; k < 2u; k++)
+            for (uint32_t i = 0; i < kTops; i++) *reinterpret_cast<Word4 *>(keys + row_at(wave * kStage + i * 8u + lane / 8u) + kD + lane % 8u * 8u) = tops[i];
+        };
+        if (from < to) fetch(from);
+        Half8 q[kM][kSteps];
+        uint32_t sees[kM];
 #pragma unroll
-            for (uint32_t n = 0; n < kM; n++)
+        for (uint32_t n = 0; n < kM; n++) {
+            const uint32_t i0 = t.first + (wave * kM + n) * 16u + m, i = i0 < t.last ? i0 : t.last - 1u, token = t.begin + i;
+            const uint16_t *qn = a.q_n + (int64_t)token * a.qn_token + (int64_t)head * a.qn_head + g * 8u, *qr = a.q_r + (int64_t)token * a.qr_token + (int64_t)head * a.qr_head + g * 8u;
 #pragma unroll
-                for (uint32_t j = 0; j < 8u; j++) s[k][n][j] = score[k][j / 4u][n][j % 4u] * a.factor;
-        if (partly || block + kPromptKeys > to)
+            for (uint32_t s = 0; s < kSteps; s++) q[n][s] = *reinterpret_cast<const Half8 *>(s < kD / 32u ? qn + s * 32u : qr + (s - kD / 32u) * 32u);
+            const uint32_t all = seen_by(i);
+            sees[n] = all < to ? all : to;
+        }
+        Sums<kM, kParts> sums;
+        sums.clear();
+        if (tid < kD) odd_from[tid] = kNone;
+        if (tid == 0u) any_from = kNone;
+        __builtin_amdgcn_s_waitcnt(0x0F70);                                // (as in latent_attend_kernel)
+        __syncthreads();
+        for (uint32_t block = from; block < to; block += kPromptKeys) {
+            stage(block);
+            __syncthreads();
+            if (block + kPromptKeys < to) fetch(block + kPromptKeys);
+            Float4 score[2][2][kM];
+#pragma unroll
+            for (uint32_t i = 0; i < 4u * kM; i++) score[i / 2u / kM][i / kM % 2u][i % kM] = Float4{0.f, 0.f, 0.f, 0.f};
+            const uint16_t *row = keys + row_at(m / 4u * 8u + m % 4u) + g * 8u;
+            Half8 x[2][kAhead];
+            pipelined<4u * kSteps, kAhead>([&](uint32_t i, uint32_t at) { x[at / kAhead][at % kAhead] = *reinterpret_cast<const Half8 *>(row + i / 2u % 2u * kGroupPitch + i % 2u * 4u * kPitch + i / 4u * 32u); },
+                                           [&](uint32_t i, uint32_t at) {
+#pragma unroll
+                                               for (uint32_t n = 0; n < kM; n++)
+                                                   score[i / 2u % 2u][i % 2u][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x[at / kAhead][at % kAhead], q[n][i / 4u], score[i / 2u % 2u][i % 2u][n], 0, 0, 0);
+                                           });
+            float s[2][kM][8];
+            const uint32_t at = block + g * 8u;
 #pragma unroll
             for (uint32_t k = 0; k < 2u; k++)
 #pragma unroll
                 for (uint32_t n = 0; n < kM; n++)
 #pragma unroll
-                    for (uint32_t j = 0; j < 8u; j++) s[k][n][j] = at + k * 32u + j < sees[n] ? s[k][n][j] : -__builtin_inff();
-        Half8 p[2][kM];
-        sums.template weigh<2>(s, p);
-        const uint16_t *column = values + (g * 8u + m / 4u) * kValuePitch + m % 4u * 4u;
+                    for (uint32_t j = 0; j < 8u; j++) s[k][n][j] = score[k][j / 4u][n][j % 4u] * a.factor;
+            if (block + kPromptKeys > seen_least || block + kPromptKeys > to)
 #pragma unroll
-        for (uint32_t d = 0; d < kParts; d++)
+                for (uint32_t k = 0; k < 2u; k++)
 #pragma unroll
-            for (uint32_t k = 0; k < 2u; k++) {
-                const uint16_t *of = column + k * 32u * kValuePitch + d * 16u;
-                const Half8 x = both(column_of(of), column_of(of + 4u * kValuePitch));
+                    for (uint32_t n = 0; n < kM; n++)
 #pragma unroll
-                for (uint32_t n = 0; n < kM; n++) sums.acc[d][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, p[k][n], sums.acc[d][n], 0, 0, 0);
-            }
-        __syncthreads();
-    }
+                        for (uint32_t j = 0; j < 8u; j++) s[k][n][j] = at + k * 32u + j < sees[n] ? s[k][n][j] : -__builtin_inff();
+            Half8 p[2][kM];
+            sums.template weigh<2>(s, p);
+            const uint16_t *column = values + value_at(g * 8u + m / 4u) + m % 4u * 4u;
+            pipelined<2u * kParts, kAhead>([&](uint32_t i, uint32_t at) {
+                                               const uint16_t *of = column + i % 2u * kValueGroup + i / 2u * 16u;
+                                               x[at / kAhead][at % kAhead] = both(column_of(of), column_of(of + 4u * kValuePitch));
+                                           },
+                                           [&](uint32_t i, uint32_t at) {
 #pragma unroll
-    for (uint32_t n = 0; n < kM; n++) {
-        const float sum = sums.whole_sum(n);
-        const uint32_t own = t.first + (wave * kM + n) * 16u + m;
-        const bool any = sees[n] > from;
-        const float by = share_of_sum(sum, any && whole);
-        if (own >= t.last) continue;
-        const size_t at = (size_t)(t.begin + own) * heads + head, part = (size_t)place * kPromptRows + own - t.first;
-#pragma unroll
-        for (uint32_t d = 0; d < kParts; d++) {
-            Float4 v = sums.acc[d][n] * by;
-            if (any_from != kNone)
-#pragma unroll
-                for (uint32_t e = 0; e < 4u; e++) v[e] = odd_from[d * 16u + g * 4u + e] < sees[n] ? __builtin_nanf("") : v[e];
-            if (whole) *reinterpret_cast<Word2 *>(a.out + at * kD + d * 16u + g * 4u) = Word2{pk_bf16(v[0], v[1]), pk_bf16(v[2], v[3])};
-            else *reinterpret_cast<Float4 *>(a.partial + part * kD + d * 16u + g * 4u) = v;
+                                               for (uint32_t n = 0; n < kM; n++)
+                                                   sums.acc[i / 2u][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x[at / kAhead][at % kAhead], p[i % 2u][n], sums.acc[i / 2u][n], 0, 0, 0);
+                                           });
+            __syncthreads();
         }
-        if (!whole && g == 0u) *reinterpret_cast<Float2 *>(a.ends + part * 2u) = Float2{sums.base[n], any && sum == 0.f ? kEmpty : sum};
-    }
-    __syncthreads();
+#pragma unroll
+        for (uint32_t n = 0; n < kM; n++) {
+            const float sum = sums.whole_sum(n);
+            const uint32_t own = t.first + (wave * kM + n) * 16u + m;
+            const bool any = sees[n] > from;
+            const float by = share_of_sum(sum, any && whole);
+            if (own >= t.last) continue;
+            const size_t at = (size_t)(t.begin + own) * heads + head, part = (size_t)place * kPromptRows + own - t.first;
+#pragma unroll
+            for (uint32_t d = 0; d < kParts; d++) {
+                Float4 v = sums.acc[d][n] * by;
+                if (any_from != kNone)
+#pragma unroll
+                    for (uint32_t e = 0; e < 4u; e++) v[e] = odd_from[d * 16u + g * 4u + e] < sees[n] ? __builtin_nanf("") : v[e];
+                if (whole) *reinterpret_cast<Word2 *>(a.out + at * kD + d * 16u + g * 4u) = Word2{pk_bf16(v[0], v[1]), pk_bf16(v[2], v[3])};
+                else *reinterpret_cast<Float4 *>(a.partial + part * kD + d * 16u + g * 4u) = v;
+            }
+            if (!whole && g == 0u) *reinterpret_cast<Float2 *>(a.ends + part * 2u) = Float2{sums.base[n], any && sum == 0.f ? kEmpty : sum};
+        }
+        __syncthreads();
     }
 }
 
 bool latent_prompt_fits(uint32_t tokens, uint32_t rows, uint32_t heads) { return ((uint64_t)tokens / kPromptRows + rows) * heads <= 0xFFFFFFu; }
 
+static uint64_t prompt_tiles(uint32_t tokens, uint32_t rows, uint32_t heads) { return ((uint64_t)tokens / kPromptRows + (rows < tokens ? rows : tokens)) * heads; }
 static Plan prompt_plan(uint32_t tokens, uint32_t rows, uint32_t heads, uint32_t dim, uint32_t keys)
 {
-    const uint64_t tiles = ((uint64_t)tokens / kPromptRows + (rows < tokens ? rows : tokens)) * heads, blocks = ((uint64_t)keys + kAttendBlock - 1u) / kAttendBlock;
+    const uint64_t tiles = prompt_tiles(tokens, rows, heads), blocks = ((uint64_t)keys + kAttendBlock - 1u) / kAttendBlock;
     return plan_of(tiles, blocks, rows, kPromptRows, dim, kPromptSlots, (uint64_t)tokens * heads);
 }
 uint64_t latent_prompt_bytes(uint32_t tokens, uint32_t rows, uint32_t heads, uint32_t dim, uint32_t keys) { return plan_bytes(prompt_plan(tokens, rows, heads, dim, keys)); }
@@ -849,7 +853,8 @@ hipError_t launch_latent_prompt(const void *q_n, const void *q_r, const void *k_
     const hipError_t e = launch(dim == 128u ? latent_prompt_kernel<128> : latent_prompt_kernel<64>, grid, dim3(kThreads), 0, s, nullptr, a);
     if (e != hipSuccess || !p.chunks) return e;
     const JoinArgs j{a.partial, a.ends, a.parts, starts, a.out, rows, heads, p.chunks, kPromptRows};
-    return dim == 128u ? launch_join<128>(j, tokens, false, s) : launch_join<64>(j, tokens, false, s);
+    const bool many = p.chunks > 32u * prompt_tiles(tokens, rows, heads);
+    return dim == 128u ? launch_join<128>(j, tokens, many, s) : launch_join<64>(j, tokens, many, s);
 }
 
 }  // namespace wg
