@@ -476,14 +476,14 @@ int wg_latent_read(const void *d_c_cache, const void *d_r_cache, const float *d_
  * [tokens][heads][64], both bfloat16 with strides in elements at multiples of 16 bytes; d_out bfloat16 [tokens][heads][latent] without gaps (what makes a head's values from vectors is applied to it
  * afterwards).  d_table, d_lens, d_starts, and which keys a token sees, as for wg_cache_attend: row r has d_lens[r] tokens in the cache, the tokens d_starts[r] .. d_starts[r + 1] of the
  * call being its last ones; token i of n sees the first d_lens[r] - n + i + 1 (none: its output is zeros); tokens from d_starts[rows] on belong to no row, and their outputs stay.  Products of
- * bfloat16 numbers (those in 8 bits times their scale exactly), sums and softmax in fp32; weights are rounded to bfloat16 and divided by the sum of the rounded ones.  An infinity or a NaN in a vector that a token sees makes
+ * bfloat16 numbers (those in 8 bits times their scale exactly), sums and softmax in fp32; weights are rounded to bfloat16, their sum is taken before.  An infinity or a NaN in a vector that a token sees makes
  * its output NaN, in part or as a whole, and is nothing to a token that does not see it.  A page number of a row's tokens that is none reads as zeros; entries behind them may be anything.
  * d_workspace: wg_latent_attend_workspace(...) bytes (0: may be NULL), 16-byte aligned, overwritten; calls that share it must not overlap.  heads <= 4096, rows <= 65535, pages *
  * page_tokens and columns * page_tokens < 2^31, tokens * heads < 2^31 and no more tokens than one launch holds (tokens * heads / 16 + rows < 2^24).  One or two kernels.
  *
  * wg_latent_prompt: the same attention with keys and values of every head made beforehand from the vectors (wg_latent_read, then a product), which takes a fraction of the operations where
  * many tokens see the same keys.  d_q_n [tokens][heads][dim] and d_q_r [tokens][heads][64] are the two parts of the queries, d_k_n and d_v [keys][heads][dim] the keys' own part and the values, d_k_r [keys][64] the shared part; bfloat16, strides in
- * elements at multiples of 16 bytes; dim is 64 or 128.  Row r has the queries d_starts[r] .. d_starts[r + 1] and the keys d_key_starts[r] .. d_key_starts[r + 1], its queries being the last of them: query i of n sees
+ * elements at multiples of 16 bytes, keys and values less than 2^24 elements from one token to the next; dim is 64 or 128.  Row r has the queries d_starts[r] .. d_starts[r + 1] and the keys d_key_starts[r] .. d_key_starts[r + 1], its queries being the last of them: query i of n sees
  * the first m - n + i + 1 of its m keys (none: zeros); tokens from d_starts[rows] on belong to no row, and their outputs stay.  d_out bfloat16 [tokens][heads][dim] without gaps.  Rounding as above; an infinity or a NaN in a value that a
  * token sees makes that output infinite or NaN and is nothing to a token that does not see it.  Both starts do not descend.  heads <= 4096, rows <= 65535, tokens and keys < 2^31, tokens * heads < 2^31.  One or two kernels. */
 uint64_t wg_latent_attend_workspace(uint32_t tokens, uint32_t rows, uint32_t heads, uint32_t latent, uint32_t columns, uint32_t page_tokens);

@@ -7,10 +7,11 @@
 // by the transposing read: sixteen lanes that ask for four rows of sixteen numbers get a column of four each.
 //
 // The softmax is taken in one pass: weights e = 2^(score - base) relative to a base that moves only where a score is 8 above it, by their wavefront as a whole; so it
-// costs no exchange between lanes but where it moves.  Weights are rounded to bfloat16, as the values are that they multiply (values go as far as 2^127, which float16 would not hold), and
-// their sum, in fp32, is that of the rounded ones: weights off by 2^-8 at the most, by as much as the output's own rounding.
+// costs no exchange between lanes but where it moves.  Weights are rounded to bfloat16, as the values are that they multiply (values go as far as 2^127, which float16 would not hold): they
+// are off by 2^-8 at the most, as the output is by its own rounding.  Their sum, in fp32, is that of the weights before.
 #include <hip/hip_runtime.h>
 
+#include "wg_buffer.h"
 #include "wg_launch.h"
 #include "wg_number.h"
 #include "wg_serve.h"
@@ -32,6 +33,8 @@ struct Requests {
 };
 struct Tile { uint32_t row, first, last, begin, count; int32_t before; };  // query rows [first, last) of request `row`, whose tokens of the call begin at `begin`, behind `before` others (count: all of them)
 
+// What is the same for all lanes, though it comes by a load of each.
+__device__ __forceinline__ uint32_t uniform(uint32_t x) { return __builtin_amdgcn_readfirstlane(x); }
 __device__ __forceinline__ uint32_t start_of(const Requests &a, uint32_t r) { const uint32_t t = (uint32_t)a.starts[r]; return t < a.tokens ? t : a.tokens; }
 __device__ __forceinline__ uint32_t tokens_of(const Requests &a, uint32_t r) { const uint32_t b = start_of(a, r), e = start_of(a, r + 1u); return e < b ? 0u : e - b; }
 
@@ -39,8 +42,8 @@ __device__ __forceinline__ uint32_t tokens_of(const Requests &a, uint32_t r) { c
 template <uint32_t kRows>
 __device__ __forceinline__ bool tile_at(const Requests &a, uint32_t per, uint32_t r, uint32_t tile, Tile *out)
 {
-    const uint32_t n = tokens_of(a, r), all = n * per, e = (uint32_t)a.starts[r + 1u];
-    out->row = r; out->begin = start_of(a, r);
+    const uint32_t n = uniform(tokens_of(a, r)), all = n * per, e = uniform((uint32_t)a.starts[r + 1u]);
+    out->row = r; out->begin = uniform(start_of(a, r));
     if ((uint64_t)tile * kRows >= all) return false;
     out->first = tile * kRows;
     out->last = all - out->first < kRows ? all : out->first + kRows;
@@ -64,7 +67,7 @@ __device__ __forceinline__ bool tile_of(const Requests &a, uint32_t per, uint32_
         lo += k * step;
     }
     lo = __builtin_amdgcn_readfirstlane(lo);
-    const uint32_t first = begins(lo);
+    const uint32_t first = uniform(begins(lo));
     return tile >= first && tile_at<kRows>(a, per, lo, tile - first, out);
 }
 
@@ -97,7 +100,7 @@ __device__ __forceinline__ bool chunk_of(const Requests &a, uint32_t w, F work_o
         if (behind) {
             const uint32_t k = (uint32_t)__builtin_ctzll(behind);
             out->row = base + k;
-            out->off = out->at - (ahead + __builtin_amdgcn_readlane(sum, k) - __builtin_amdgcn_readlane(own, k));
+            out->off = uniform(out->at - (ahead + __builtin_amdgcn_readlane(sum, k) - __builtin_amdgcn_readlane(own, k)));
             return true;
         }
         ahead += __builtin_amdgcn_readlane(sum, 63);
@@ -179,6 +182,17 @@ __device__ __forceinline__ void pipelined(L load, U use)
     }
 }
 
+// Queries that give scores of the factor's sign, which then is 1 or above 0: with it 0 all are zeros.
+__device__ __forceinline__ Half8 signed_query(Half8 q, float factor)
+{
+    const uint32_t flip = factor < 0.f ? 0x80008000u : 0u, keep = factor == 0.f ? 0u : 0xFFFFFFFFu;
+    Word4 v = __builtin_bit_cast(Word4, q);
+#pragma unroll
+    for (uint32_t w = 0; w < 4u; w++) v[w] = (v[w] ^ flip) & keep;
+    return __builtin_bit_cast(Half8, v);
+}
+__device__ __forceinline__ float size_of(float factor) { return factor == 0.f ? 1.f : __builtin_fabsf(factor); }
+
 // The largest over lanes l, l ^ 16, l ^ 32 and l ^ 48.
 __device__ __forceinline__ float most_of_rows(float x)
 {
@@ -202,18 +216,20 @@ struct Sums {
             for (uint32_t d = 0; d < kParts; d++) acc[d][t] = Float4{0.f, 0.f, 0.f, 0.f};
         }
     }
-    // Scores (log2, -inf where nothing is seen) of kGroups times 32 keys into weights.
+    // Scores (-inf where nothing is seen) of kGroups times 32 keys into weights; factor, above 0, makes them scores in log2.
     template <uint32_t kGroups>
-    __device__ __forceinline__ void weigh(const float (&s)[kGroups][kM][8], Half8 (&p)[kGroups][kM])
+    __device__ __forceinline__ void weigh(const float (&s)[kGroups][kM][8], float factor, Half8 (&p)[kGroups][kM])
     {
 #pragma unroll
         for (uint32_t t = 0; t < kM; t++) {
-            float n = base[t];
+            float n = s[0][t][0];
 #pragma unroll
-            for (uint32_t k = 0; k < kGroups; k++) n = __builtin_fmaxf(n, __builtin_fmaxf(__builtin_fmaxf(__builtin_fmaxf(s[k][t][0], s[k][t][1]), __builtin_fmaxf(s[k][t][2], s[k][t][3])),
-                                                                                          __builtin_fmaxf(__builtin_fmaxf(s[k][t][4], s[k][t][5]), __builtin_fmaxf(s[k][t][6], s[k][t][7]))));
+            for (uint32_t k = 0; k < kGroups; k++)
+#pragma unroll
+                for (uint32_t j = 0; j < 8u; j++) n = __builtin_fmaxf(n, s[k][t][j]);
+            n *= factor;
             if (__ballot(n > base[t] + kLift)) {
-                n = most_of_rows(n);
+                n = __builtin_fmaxf(base[t], most_of_rows(n));
                 const float by = __builtin_amdgcn_exp2f(base[t] - (n > -__builtin_inff() ? n : 0.f));
                 base[t] = n; sum[t] *= by;
 #pragma unroll
@@ -225,8 +241,9 @@ struct Sums {
                 Word4 w;
 #pragma unroll
                 for (uint32_t j = 0; j < 4u; j++) {
-                    w[j] = pk_bf16(__builtin_amdgcn_exp2f(s[k][t][2u * j] - from), __builtin_amdgcn_exp2f(s[k][t][2u * j + 1u] - from));
-                    sum[t] += low(w[j]) + high(w[j]);
+                    const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(s[k][t][2u * j], factor, -from)), y = __builtin_amdgcn_exp2f(__builtin_fmaf(s[k][t][2u * j + 1u], factor, -from));
+                    w[j] = pk_bf16(x, y);
+                    sum[t] += x; sum[t] += y;
                 }
                 p[k][t] = __builtin_bit_cast(Half8, w);
             }
@@ -276,7 +293,7 @@ latent_attend_kernel(const LatentAttendArgs a)
     constexpr uint32_t kW = 8u, kKeyGroups = kW / (kGroups * kCols), kKeys = 32u * kKeyGroups, kRows = 16u * kGroups;
     constexpr uint32_t kSteps = (kC + kTop) / 32u, kParts = kC / 16u / kCols, kPitch = kC + kTop + 16u, kGroupPitch = 32u * kPitch + 144u;
     constexpr uint32_t kRow = kC * (kBytes ? 1u : 2u), kPer = 1024u / kRow, kStage = kKeys / kW;          // bytes of a vector; keys of a wavefront's load; keys that it brings
-    constexpr uint32_t kLoads = kStage / kPer, kTops = (kStage + 7u) / 8u, kAhead = kC == 512u ? 2u : 4u, kPut = kC == 512u && kGroups == 8u ? 8u : 0u, kKept = kSteps - kPut;
+    constexpr uint32_t kLoads = kStage / kPer, kTops = (kStage + 7u) / 8u, kAhead = kC == 512u ? 2u : 4u, kPut = kC == 512u && kGroups == 8u ? 10u : 0u, kKept = kSteps - kPut;
     constexpr uint32_t kJoinPitch = kC + 4u, kTile = kKeyGroups * kGroupPitch, kTileBytes = kTile * 2u, kJoinBytes = kKeyGroups > 1u ? kKeyGroups * kRows * kJoinPitch * 4u : 0u;
     __shared__ __attribute__((aligned(16))) uint8_t room[2u * kTileBytes > kJoinBytes ? 2u * kTileBytes : kJoinBytes];   // two blocks of keys: one that is worked on, one that comes
     __shared__ uint32_t odd_from;                                          // the first key with a number that is none, of those that some rows do not see
@@ -296,7 +313,7 @@ latent_attend_kernel(const LatentAttendArgs a)
         // the next part of a tile: blocks [b0, b0 + n) of its `blocks`
         uint32_t b0 = 0, n = 1u, blocks = 1u, begins = 0;                  // begins: where the tile's blocks do, among all
         if (a.of.chunks) {
-            const uint32_t work = tiles(c.row) * (blocks = blocks_of(cached_tokens(a, c.row))), tile = c.off / blocks;
+            const uint32_t work = uniform(tiles(c.row) * (blocks = uniform(blocks_of(cached_tokens(a, c.row))))), tile = c.off / blocks;
             if (!work) { c.row++; continue; }                              // (off is 0)
             (void)tile_at<kRows>(a.of, heads, c.row, tile, &t);
             b0 = c.off - tile * blocks;
@@ -305,7 +322,7 @@ latent_attend_kernel(const LatentAttendArgs a)
             c.off += n;
             if (c.off >= work) { c.off = 0; c.row++; }
         }
-        const uint32_t len = cached_tokens(a, t.row);
+        const uint32_t len = uniform(cached_tokens(a, t.row));
         t.before = (int32_t)len - (int32_t)t.count;
         const bool whole = n == blocks;
         const uint32_t place = 2u * blockIdx.x + (b0 ? 0u : 1u), row_first = t.first;
@@ -387,7 +404,7 @@ latent_attend_kernel(const LatentAttendArgs a)
             const uint16_t *c = a.q_c + (int64_t)token * a.c_token + (int64_t)head * a.c_head + g * 8u, *r = a.q_r + (int64_t)token * a.r_token + (int64_t)head * a.r_head + g * 8u;
 #pragma unroll
             for (uint32_t s = 0; s < kSteps; s++) {
-                const Half8 x = *reinterpret_cast<const Half8 *>(s < kC / 32u ? c + s * 32u : r + (s - kC / 32u) * 32u);
+                const Half8 x = signed_query(*reinterpret_cast<const Half8 *>(s < kC / 32u ? c + s * 32u : r + (s - kC / 32u) * 32u), a.factor);
                 if (s < kKept) q[s % kKept] = x;
                 else q_rest[(wave * kPut + s - kKept) * 64u + lane] = x;
             }
@@ -419,12 +436,12 @@ latent_attend_kernel(const LatentAttendArgs a)
             float s[1][1][8];
             const uint32_t at = block + key_group * 32u + g * 8u;
 #pragma unroll
-            for (uint32_t j = 0; j < 8u; j++) s[0][0][j] = score[j / 4u][j % 4u] * a.factor;
+            for (uint32_t j = 0; j < 8u; j++) s[0][0][j] = score[j / 4u][j % 4u];
             if (block + kKeys > seen_least || block + kKeys > to)
 #pragma unroll
                 for (uint32_t j = 0; j < 8u; j++) s[0][0][j] = at + j < sees ? s[0][0][j] : -__builtin_inff();
             Half8 p[1][1];
-            sums.template weigh<1>(s, p);
+            sums.template weigh<1>(s, size_of(a.factor), p);
             if (block + kKeys < to) {
                 stage(block + kKeys, keys + (turn ^ 1u) * kTile);
                 if (block + 2u * kKeys < to) fetch_next(block + 2u * kKeys);
@@ -675,24 +692,25 @@ latent_prompt_kernel(const LatentPromptArgs a)
 {
     constexpr uint32_t kM = 2u, kSteps = (kD + kTop) / 32u, kParts = kD / 16u, kPitch = kD + kTop + 16u, kGroupPitch = 32u * kPitch + 144u, kValuePitch = kD + 16u, kValueGroup = 32u * kValuePitch + 144u,
                        kStage = kPromptKeys / kWaves;
-    constexpr uint32_t kPer = 512u / kD, kLoads = kStage / kPer, kTops = kStage / 8u, kAhead = 3u;
+    constexpr uint32_t kPer = 512u / kD, kLoads = kStage / kPer, kTops = kStage / 8u, kAhead = 3u, kPut = kD == 128u ? 1u : 0u, kKept = kSteps - kPut;
     __shared__ __attribute__((aligned(16))) uint16_t keys[kPromptKeys / 32u * kGroupPitch], values[kPromptKeys / 32u * kValueGroup];
+    __shared__ Half8 q_rest[kPut ? kWaves * kM * kPut * 64u : 1u];         // (as in latent_attend_kernel)
     __shared__ uint32_t odd_from[kD], any_from;       // of each dim, the first key whose value is none, of those that some rows do not see; the first of all
     const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), heads = a.of.heads;
     auto tiles = [&](uint32_t r) { return (tokens_of(a.of, r) + kPromptRows - 1u) / kPromptRows; };
     auto blocks_at = [&](uint32_t r) { uint32_t none; return blocks_of(keys_of(a, r, &none)); };
     Tile t;
     Chunk c{0u, 1u, 0u, 0u, 0u};
-    uint32_t head = blockIdx.x % heads;
+    uint32_t head = uniform(blockIdx.x % heads);
     if (a.of.chunks ? !chunk_of(a.of, blockIdx.x, [&](uint32_t r) { return tiles(r) * heads * blocks_at(r); }, &c) : !tile_of<kPromptRows>(a.of, 1u, blockIdx.x / heads, &t)) return;
-    if (!a.of.chunks) (void)tile_at<kPromptRows>(a.of, 1u, t.row, tiles(t.row) - 1u - t.first / kPromptRows, &t);             // the last, which see the most keys, first
+    if (!a.of.chunks) (void)tile_at<kPromptRows>(a.of, 1u, t.row, uniform(tiles(t.row)) - 1u - t.first / kPromptRows, &t);             // the last, which see the most keys, first
     while (c.at < c.end) {
         const uint32_t tid = anew(threadIdx.x), lane = tid & 63u, m = lane & 15u, g = lane >> 4;
         uint32_t b0 = 0, n_blocks = 1u, blocks = 1u, begins = 0, begin;
         if (a.of.chunks) {
-            const uint32_t work = tiles(c.row) * heads * (blocks = blocks_at(c.row)), unit = c.off / blocks;
+            const uint32_t work = uniform(tiles(c.row) * heads * (blocks = uniform(blocks_at(c.row)))), unit = c.off / blocks;
             if (!work) { c.row++; continue; }                              // (off is 0)
-            head = unit % heads;
+            head = uniform(unit % heads);
             (void)tile_at<kPromptRows>(a.of, 1u, c.row, unit / heads, &t);
             b0 = c.off - unit * blocks;
             n_blocks = blocks - b0 < c.end - c.at ? blocks - b0 : c.end - c.at;
@@ -700,7 +718,8 @@ latent_prompt_kernel(const LatentPromptArgs a)
             c.off += n_blocks;
             if (c.off >= work) { c.off = 0; c.row++; }
         }
-        const uint32_t len = keys_of(a, t.row, &begin);
+        const uint32_t len = uniform(keys_of(a, t.row, &begin));
+        begin = uniform(begin);
         t.before = (int32_t)len - (int32_t)t.count;
         const bool whole = n_blocks == blocks;
         const uint32_t place = 2u * blockIdx.x + (b0 ? 0u : 1u);
@@ -712,20 +731,25 @@ latent_prompt_kernel(const LatentPromptArgs a)
         const uint32_t from = b0 * kAttendBlock, to0 = whole ? seen_most : from + n_blocks * kAttendBlock, to = to0 < seen_most ? to0 : seen_most;
 
         Word4 raw[kLoads], tops[kTops], raw_v[kLoads];
-        const uint8_t *k_n = reinterpret_cast<const uint8_t *>(a.k_n + (int64_t)begin * a.kn_token + (int64_t)head * a.kn_head), *k_r = reinterpret_cast<const uint8_t *>(a.k_r + (int64_t)begin * a.kr_token),
-                      *v_of = reinterpret_cast<const uint8_t *>(a.v + (int64_t)begin * a.v_token + (int64_t)head * a.v_head);
+        const uint32_t head_now = uniform(head);
+        const uint16_t *k_n = a.k_n + (int64_t)begin * a.kn_token + (int64_t)head_now * a.kn_head, *k_r = a.k_r + (int64_t)begin * a.kr_token, *v_of = a.v + (int64_t)begin * a.v_token + (int64_t)head_now * a.v_head;
+        // a block's rows as buffers: keys behind the last lie behind their ends, and read as zeros
+        auto rows_from = [&](const uint16_t *p, uint32_t block, int64_t token, uint32_t dim) {
+            const uint32_t n = to - block < kPromptKeys ? to - block : kPromptKeys;
+            return window_of(p + (int64_t)block * token, ((n - 1u) * (uint32_t)token + dim) * 2u);
+        };
+        auto four = [&](Window w, uint32_t at) { const FourWords x = __builtin_amdgcn_raw_buffer_load_b128(w, at, 0, 0); return Word4{x.x, x.y, x.z, x.w}; };
+        const uint32_t own_key = wave * kStage + lane / (64u / kPer), own_dim = lane % (64u / kPer) * 16u, own_top = (wave * kStage + lane / 8u) * (uint32_t)a.kr_token * 2u + lane % 8u * 16u;
+        const uint32_t own_k = own_key * (uint32_t)a.kn_token * 2u + own_dim, own_v = own_key * (uint32_t)a.v_token * 2u + own_dim;
         auto fetch = [&](uint32_t block) {
+            const Window kw = rows_from(k_n, block, a.kn_token, kD), vw = rows_from(v_of, block, a.v_token, kD), rw = rows_from(k_r, block, a.kr_token, kTop);
 #pragma unroll
             for (uint32_t i = 0; i < kLoads; i++) {
-                const uint32_t key = block + wave * kStage + i * kPer + lane / (64u / kPer), d = lane % (64u / kPer) * 16u;
-                raw[i] = from_memory<Word4>(key < to ? k_n + (int64_t)key * a.kn_token * 2 + d : kZeros);
-                raw_v[i] = from_memory<Word4>(key < to ? v_of + (int64_t)key * a.v_token * 2 + d : kZeros);
+                raw[i] = four(kw, own_k + i * kPer * (uint32_t)a.kn_token * 2u);
+                raw_v[i] = four(vw, own_v + i * kPer * (uint32_t)a.v_token * 2u);
             }
 #pragma unroll
-            for (uint32_t i = 0; i < kTops; i++) {
-                const uint32_t key = block + wave * kStage + i * 8u + lane / 8u;
-                tops[i] = from_memory<Word4>(key < to ? k_r + (int64_t)key * a.kr_token * 2 + lane % 8u * 16u : kZeros);
-            }
+            for (uint32_t i = 0; i < kTops; i++) tops[i] = four(rw, own_top + i * 8u * (uint32_t)a.kr_token * 2u);
         };
         // (where keys and values lie in LDS: as in latent_attend_kernel)
         auto row_at = [&](uint32_t key) { return key / 32u * kGroupPitch + key % 32u * kPitch + (key & 8u ? 72u : 0u) + (key & 16u ? 64u : 0u); };
@@ -746,14 +770,18 @@ latent_prompt_kernel(const LatentPromptArgs a)
             for (uint32_t i = 0; i < kTops; i++) *reinterpret_cast<Word4 *>(keys + row_at(wave * kStage + i * 8u + lane / 8u) + kD + lane % 8u * 8u) = tops[i];
         };
         if (from < to) fetch(from);
-        Half8 q[kM][kSteps];
+        Half8 q[kM][kKept];
         uint32_t sees[kM];
 #pragma unroll
         for (uint32_t n = 0; n < kM; n++) {
             const uint32_t i0 = t.first + (wave * kM + n) * 16u + m, i = i0 < t.last ? i0 : t.last - 1u, token = t.begin + i;
             const uint16_t *qn = a.q_n + (int64_t)token * a.qn_token + (int64_t)head * a.qn_head + g * 8u, *qr = a.q_r + (int64_t)token * a.qr_token + (int64_t)head * a.qr_head + g * 8u;
 #pragma unroll
-            for (uint32_t s = 0; s < kSteps; s++) q[n][s] = *reinterpret_cast<const Half8 *>(s < kD / 32u ? qn + s * 32u : qr + (s - kD / 32u) * 32u);
+            for (uint32_t s = 0; s < kSteps; s++) {
+                const Half8 x = signed_query(*reinterpret_cast<const Half8 *>(s < kD / 32u ? qn + s * 32u : qr + (s - kD / 32u) * 32u), a.factor);
+                if (s < kKept) q[n][s % kKept] = x;
+                else q_rest[((wave * kM + n) * kPut + s - kKept) * 64u + lane] = x;
+            }
             const uint32_t all = seen_by(i);
             sees[n] = all < to ? all : to;
         }
@@ -775,8 +803,10 @@ latent_prompt_kernel(const LatentPromptArgs a)
             pipelined<4u * kSteps, kAhead>([&](uint32_t i, uint32_t at) { x[at / kAhead][at % kAhead] = *reinterpret_cast<const Half8 *>(row + i / 2u % 2u * kGroupPitch + i % 2u * 4u * kPitch + i / 4u * 32u); },
                                            [&](uint32_t i, uint32_t at) {
 #pragma unroll
-                                               for (uint32_t n = 0; n < kM; n++)
-                                                   score[i / 2u % 2u][i % 2u][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x[at / kAhead][at % kAhead], q[n][i / 4u], score[i / 2u % 2u][i % 2u][n], 0, 0, 0);
+                                               for (uint32_t n = 0; n < kM; n++) {
+                                                   const Half8 y = i / 4u < kKept ? q[n][i / 4u % kKept] : q_rest[((wave * kM + n) * kPut + i / 4u - kKept) * 64u + lane];
+                                                   score[i / 2u % 2u][i % 2u][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x[at / kAhead][at % kAhead], y, score[i / 2u % 2u][i % 2u][n], 0, 0, 0);
+                                               }
                                            });
             float s[2][kM][8];
             const uint32_t at = block + g * 8u;
@@ -785,7 +815,7 @@ latent_prompt_kernel(const LatentPromptArgs a)
 #pragma unroll
                 for (uint32_t n = 0; n < kM; n++)
 #pragma unroll
-                    for (uint32_t j = 0; j < 8u; j++) s[k][n][j] = score[k][j / 4u][n][j % 4u] * a.factor;
+                    for (uint32_t j = 0; j < 8u; j++) s[k][n][j] = score[k][j / 4u][n][j % 4u];
             if (block + kPromptKeys > seen_least || block + kPromptKeys > to)
 #pragma unroll
                 for (uint32_t k = 0; k < 2u; k++)
@@ -794,7 +824,7 @@ latent_prompt_kernel(const LatentPromptArgs a)
 #pragma unroll
                         for (uint32_t j = 0; j < 8u; j++) s[k][n][j] = at + k * 32u + j < sees[n] ? s[k][n][j] : -__builtin_inff();
             Half8 p[2][kM];
-            sums.template weigh<2>(s, p);
+            sums.template weigh<2>(s, size_of(a.factor), p);
             const uint16_t *column = values + value_at(g * 8u + m / 4u) + m % 4u * 4u;
             pipelined<2u * kParts, kAhead>([&](uint32_t i, uint32_t at) {
                                                const uint16_t *of = column + i % 2u * kValueGroup + i / 2u * 16u;

@@ -279,6 +279,8 @@ int wg_latent_prompt(const void *d_q_n, const void *d_q_r, const void *d_k_n, co
         WG_WANT(latent_prompt_fits(tokens, rows, heads), "too many tokens for one launch");
         WG_WANT(by_sixteen(d_q_n, q_n_token_stride, q_n_head_stride) && by_sixteen(d_q_r, q_r_token_stride, q_r_head_stride) && by_sixteen(d_k_n, k_n_token_stride, k_n_head_stride) &&
                 by_sixteen(d_k_r, k_r_token_stride, 0) && by_sixteen(d_v, v_token_stride, v_head_stride), "queries, keys and values must lie at multiples of 16 bytes");
+        WG_WANT(k_n_token_stride >= 0 && k_r_token_stride >= 0 && v_token_stride >= 0 && k_n_token_stride < 1 << 24 && k_r_token_stride < 1 << 24 && v_token_stride < 1 << 24,
+                "keys and values must lie 0 to 2^24 - 1 elements apart");
         WG_WANT(aligned(d_out, 16), "the output must be 16-byte aligned");
         WG_WANT(scale == scale && scale - scale == 0.f, "the scale is no number");
         const uint64_t need = wg_latent_prompt_workspace(tokens, rows, heads, dim, keys);

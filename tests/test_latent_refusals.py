@@ -68,7 +68,7 @@ def test_latent_prompt():
     refused("wg_latent_prompt", good, [
         dict(q_n=None), dict(q_r=None), dict(k_n=None), dict(k_r=None), dict(v=None), dict(starts=None), dict(key_starts=None), dict(out=None), dict(work=None), dict(tokens=0), dict(keys=0),
         dict(heads=0), dict(heads=4097), dict(dim=96), dict(dim=256), dict(rows=0), dict(rows=65536), dict(tokens=1 << 31), dict(keys=1 << 31), dict(tokens=1 << 29, heads=4),
-        dict(qn0=769), dict(qn1=4), dict(qr0=4), dict(qr1=4), dict(kn0=4), dict(kn1=4), dict(kr0=4), dict(v0=4), dict(v1=4), dict(q_n=OFF), dict(q_r=OFF), dict(k_n=OFF), dict(k_r=OFF), dict(v=OFF),
+        dict(qn0=769), dict(qn1=4), dict(qr0=4), dict(qr1=4), dict(kn0=4), dict(kn1=4), dict(kr0=4), dict(v0=4), dict(v1=4), dict(kn0=1 << 24), dict(kr0=1 << 24), dict(v0=1 << 24), dict(kn0=-1024), dict(kr0=-64), dict(v0=-1024), dict(q_n=OFF), dict(q_r=OFF), dict(k_n=OFF), dict(k_r=OFF), dict(v=OFF),
         dict(out=OFF), dict(factor=math.nan), dict(bytes=need - 1), dict(work=OFF)])
 
 
