@@ -262,8 +262,8 @@ __device__ __forceinline__ float share_of_sum(float sum, bool sees) { return sum
 constexpr float kEmpty = -1.f;                       // the sum of a share in which a query sees keys whose scores are all -inf
 
 // ---------------------------------------------------------------------------------------------
-// Attention over the cached vectors.  A workgroup's eight wavefronts are kGroups groups of 16 query rows (tokens times heads), times kCols groups of the vectors' columns (for which
-// scores are made again), times groups of 32 keys.  A block's keys go through LDS: from memory into registers, while the block before is worked on, and turned into bfloat16 (exactly) on the way.
+// Attention over the cached vectors.  A workgroup's eight wavefronts are kGroups groups of 16 query rows (tokens times heads), times kCols groups of the vectors' columns (which make
+// the scores between them), times groups of 32 keys.  A block's keys go through LDS: from memory into registers, while the block before is worked on, and turned into bfloat16 (exactly) on the way.
 struct LatentAttendArgs {
     Requests of;
     const uint16_t *q_c, *q_r;
@@ -293,11 +293,13 @@ latent_attend_kernel(const LatentAttendArgs a)
     constexpr uint32_t kW = 8u, kKeyGroups = kW / (kGroups * kCols), kKeys = 32u * kKeyGroups, kRows = 16u * kGroups;
     constexpr uint32_t kSteps = (kC + kTop) / 32u, kParts = kC / 16u / kCols, kPitch = kC + kTop + 16u, kGroupPitch = 32u * kPitch + 144u;
     constexpr uint32_t kRow = kC * (kBytes ? 1u : 2u), kPer = 1024u / kRow, kStage = kKeys / kW;          // bytes of a vector; keys of a wavefront's load; keys that it brings
-    constexpr uint32_t kLoads = kStage / kPer, kTops = (kStage + 7u) / 8u, kAhead = kC == 512u ? 2u : 4u, kPut = kC == 512u && kGroups == 8u ? 10u : 0u, kKept = kSteps - kPut;
+    constexpr uint32_t kLoads = kStage / kPer, kTops = (kStage + 7u) / 8u, kAhead = kC == 512u && kGroups == 8u ? 2u : 4u, kPut = kC == 512u && kGroups == 8u ? 10u : 0u, kKept = kSteps - kPut;
     constexpr uint32_t kJoinPitch = kC + 4u, kTile = kKeyGroups * kGroupPitch, kTileBytes = kTile * 2u, kJoinBytes = kKeyGroups > 1u ? kKeyGroups * kRows * kJoinPitch * 4u : 0u;
+    constexpr bool kHalves = kCols > 1u;                                   // two wavefronts that take the same rows and keys make half of the scores each
     __shared__ __attribute__((aligned(16))) uint8_t room[2u * kTileBytes > kJoinBytes ? 2u * kTileBytes : kJoinBytes];   // two blocks of keys: one that is worked on, one that comes
     __shared__ uint32_t odd_from;                                          // the first key with a number that is none, of those that some rows do not see
     __shared__ float join_base[kKeyGroups][kRows], join_sum[kKeyGroups][kRows];
+    __shared__ Float4 halves[kHalves ? kW * 64u : 1u];                     // each lane's scores of half of the keys
     __shared__ Half8 q_rest[kPut ? kW * kPut * 64u : 1u];                  // the last steps of the queries, each lane its own: there are no registers for them
     uint16_t *keys = reinterpret_cast<uint16_t *>(room);
     const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -425,14 +427,27 @@ latent_attend_kernel(const LatentAttendArgs a)
             const uint16_t *mine = keys + turn * kTile + key_group * kGroupPitch, *row = mine + row_at(m / 4u * 8u + m % 4u) + g * 8u;
             Float4 score[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
             Half8 k[2][kAhead], rest[2][(kAhead + 1u) / 2u];
-            pipelined<2u * kSteps, kAhead>([&](uint32_t i, uint32_t at) {
-                                               k[at / kAhead][at % kAhead] = *reinterpret_cast<const Half8 *>(row + i % 2u * 4u * kPitch + i / 2u * 32u);
-                                               if (i / 2u >= kKept && i % 2u == 0u) rest[at / kAhead][at % kAhead / 2u] = q_rest[(wave * kPut + i / 2u - kKept) * 64u + lane];
-                                           },
-                                           [&](uint32_t i, uint32_t at) {
-                                               const Half8 x = i / 2u < kKept ? q[i / 2u % kKept] : rest[at / kAhead][at % kAhead / 2u];
-                                               score[i % 2u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k[at / kAhead][at % kAhead], x, score[i % 2u], 0, 0, 0);
-                                           });
+            if (kHalves) {
+                const uint32_t half = column_group % 2u;
+                const uint16_t *half_row = row + half * 4u * kPitch;
+                Float4 own[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};                          // (two sums, so that a product need not wait for the one before)
+                pipelined<kSteps, kAhead>([&](uint32_t i, uint32_t at) { k[at / kAhead][at % kAhead] = *reinterpret_cast<const Half8 *>(half_row + i * 32u); },
+                                          [&](uint32_t i, uint32_t at) { own[i % 2u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k[at / kAhead][at % kAhead], q[i % kKept], own[i % 2u], 0, 0, 0); });
+                own[0] += own[1];
+                halves[wave * 64u + lane] = own[0];
+                __syncthreads();
+                const Float4 other = halves[(wave ^ kGroups) * 64u + lane];
+#pragma unroll
+                for (uint32_t e = 0; e < 4u; e++) { score[0][e] = half ? other[e] : own[0][e]; score[1][e] = half ? own[0][e] : other[e]; }
+            } else
+                pipelined<2u * kSteps, kAhead>([&](uint32_t i, uint32_t at) {
+                                                   k[at / kAhead][at % kAhead] = *reinterpret_cast<const Half8 *>(row + i % 2u * 4u * kPitch + i / 2u * 32u);
+                                                   if (i / 2u >= kKept && i % 2u == 0u) rest[at / kAhead][at % kAhead / 2u] = q_rest[(wave * kPut + i / 2u - kKept) * 64u + lane];
+                                               },
+                                               [&](uint32_t i, uint32_t at) {
+                                                   const Half8 x = i / 2u < kKept ? q[i / 2u % kKept] : rest[at / kAhead][at % kAhead / 2u];
+                                                   score[i % 2u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k[at / kAhead][at % kAhead], x, score[i % 2u], 0, 0, 0);
+                                               });
             float s[1][1][8];
             const uint32_t at = block + key_group * 32u + g * 8u;
 #pragma unroll
