@@ -291,7 +291,7 @@ __global__ void __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))
 latent_attend_kernel(const LatentAttendArgs a)
 {
     constexpr uint32_t kW = 8u, kKeyGroups = kW / (kGroups * kCols), kKeys = 32u * kKeyGroups, kRows = 16u * kGroups;
-    constexpr uint32_t kSteps = (kC + kTop) / 32u, kParts = kC / 16u / kCols, kPitch = kC + kTop + 16u, kGroupPitch = 32u * kPitch + 144u;
+    constexpr uint32_t kSteps = (kC + kTop) / 32u, kParts = kC / 16u / kCols, kPitch = kC + kTop + 16u, kGroupPitch = 32u * kPitch + 192u;
     constexpr uint32_t kRow = kC * (kBytes ? 1u : 2u), kPer = 1024u / kRow, kStage = kKeys / kW;          // bytes of a vector; keys of a wavefront's load; keys that it brings
     constexpr uint32_t kLoads = kStage / kPer, kTops = (kStage + 7u) / 8u, kAhead = kC == 512u && kGroups == 8u ? 2u : 4u, kPut = kC == 512u && kGroups == 8u ? 10u : 0u, kKept = kSteps - kPut;
     constexpr uint32_t kJoinPitch = kC + 4u, kTile = kKeyGroups * kGroupPitch, kTileBytes = kTile * 2u, kJoinBytes = kKeyGroups > 1u ? kKeyGroups * kRows * kJoinPitch * 4u : 0u;
@@ -362,9 +362,10 @@ latent_attend_kernel(const LatentAttendArgs a)
                 tops[i] = from_memory<Word4>((slot != kNone ? reinterpret_cast<const uint8_t *>(a.r_cache) + (size_t)slot * (kTop * 2u) : kZeros) + lane % 8u * 16u);
             }
         };
-        // Keys of a block into LDS.  A group of 32 keys has 16 bytes more than its rows would take behind every eighth, and a half more behind the sixteenth, so that what sixteen lanes read at a
-        // time, the same place of rows 0 .. 3, 8 .. 11, 16 .. 19 and 24 .. 27 or 32 bytes of four neighbouring rows, lies in different banks.
-        auto row_at = [&](uint32_t key) { return key / 32u * kGroupPitch + key % 32u * kPitch + (key & 8u ? 72u : 0u) + (key & 16u ? 64u : 0u); };
+        // Keys of a block into LDS, which serves 16 lanes' sixteen bytes in a cycle, lanes 0 .. 3, 12 .. 15 and 20 .. 27 of 32 and the others of these, or 32 lanes' eight, from 64 banks.  So the
+        // operands of the first product, sixteen bytes of rows 0 .. 3, 8 .. 11, 16 .. 19 and 24 .. 27, and of the second, 32 bytes each of four rows and of the four that lie eight further, are
+        // to lie in different sixteenths of 256 bytes: a row takes 2 or 10 of them more than whole ones, and every eight rows have 8 more behind them.
+        auto row_at = [&](uint32_t key) { return key / 32u * kGroupPitch + key % 32u * kPitch + key % 32u / 8u * 64u; };
         auto stage = [&](uint32_t block, uint16_t *to_keys) {
             const bool partly = block + kKeys > seen_least;                // some of the tile's rows do not see all of the block's keys
 #pragma unroll
@@ -705,7 +706,7 @@ template <uint32_t kD>
 __global__ void __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2)))
 latent_prompt_kernel(const LatentPromptArgs a)
 {
-    constexpr uint32_t kM = 2u, kSteps = (kD + kTop) / 32u, kParts = kD / 16u, kPitch = kD + kTop + 16u, kGroupPitch = 32u * kPitch + 144u, kValuePitch = kD + 16u, kValueGroup = 32u * kValuePitch + 144u,
+    constexpr uint32_t kM = 2u, kSteps = (kD + kTop) / 32u, kParts = kD / 16u, kPitch = kD + kTop + 16u, kGroupPitch = 32u * kPitch + 192u, kValuePitch = kD + 16u, kValueGroup = 32u * kValuePitch + 192u,
                        kStage = kPromptKeys / kWaves;
     constexpr uint32_t kPer = 512u / kD, kLoads = kStage / kPer, kTops = kStage / 8u, kAhead = 3u, kPut = kD == 128u ? 1u : 0u, kKept = kSteps - kPut;
     __shared__ __attribute__((aligned(16))) uint16_t keys[kPromptKeys / 32u * kGroupPitch], values[kPromptKeys / 32u * kValueGroup];
@@ -767,8 +768,8 @@ latent_prompt_kernel(const LatentPromptArgs a)
             for (uint32_t i = 0; i < kTops; i++) tops[i] = four(rw, own_top + i * 8u * (uint32_t)a.kr_token * 2u);
         };
         // (where keys and values lie in LDS: as in latent_attend_kernel)
-        auto row_at = [&](uint32_t key) { return key / 32u * kGroupPitch + key % 32u * kPitch + (key & 8u ? 72u : 0u) + (key & 16u ? 64u : 0u); };
-        auto value_at = [&](uint32_t key) { return key / 32u * kValueGroup + key % 32u * kValuePitch + (key & 8u ? 72u : 0u) + (key & 16u ? 64u : 0u); };
+        auto row_at = [&](uint32_t key) { return key / 32u * kGroupPitch + key % 32u * kPitch + key % 32u / 8u * 64u; };
+        auto value_at = [&](uint32_t key) { return key / 32u * kValueGroup + key % 32u * kValuePitch + key % 32u / 8u * 64u; };
         auto stage = [&](uint32_t block) {
             const bool partly = block + kPromptKeys > seen_least;
 #pragma unroll
