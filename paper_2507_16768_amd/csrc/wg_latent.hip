@@ -84,7 +84,7 @@ hipError_t launch_latent_append(const void *c, const void *r, uint32_t tokens, u
 }
 
 // ---------------------------------------------------------------------------------------------
-// read.  A wavefront takes 16 tokens behind one another; a lane of the workgroup finds a token's row and slot.
+// read.  A wavefront takes 16 tokens behind one another, 4 where there are few; a lane of the workgroup finds a token's row and slot.
 struct LatentReadArgs {
     const uint8_t *c_cache;
     const uint16_t *r_cache;
@@ -94,9 +94,7 @@ struct LatentReadArgs {
     int64_t c_token, r_token;
     uint32_t rows, columns, tokens, pages, shift;
 };
-constexpr uint32_t kReadTokens = 16;
-
-template <uint32_t kC, bool kBytes>
+template <uint32_t kC, bool kBytes, uint32_t kReadTokens>
 __global__ void __launch_bounds__(kLatentThreads)
 latent_read_kernel(const LatentReadArgs a)
 {
@@ -151,9 +149,14 @@ hipError_t launch_latent_read(const void *c_cache, const void *r_cache, const fl
 {
     const LatentReadArgs a{static_cast<const uint8_t *>(c_cache), static_cast<const uint16_t *>(r_cache), scale, table, starts, static_cast<uint16_t *>(c_out),
                            static_cast<uint16_t *>(r_out), c_token, r_token, rows, columns, tokens, pages, shift};
-    const uint32_t per = kLatentWaves * kReadTokens;
-    return launch(latent == 512u ? (scale ? latent_read_kernel<512, true> : latent_read_kernel<512, false>) : scale ? latent_read_kernel<256, true> : latent_read_kernel<256, false>,
-                  dim3((tokens + per - 1u) / per), dim3(kLatentThreads), 0, s, nullptr, a);
+    const bool few = tokens <= 8192u;
+    const uint32_t per = kLatentWaves * (few ? 4u : 16u);
+    const dim3 grid((tokens + per - 1u) / per), block(kLatentThreads);
+    if (few)
+        return launch(latent == 512u ? (scale ? latent_read_kernel<512, true, 4> : latent_read_kernel<512, false, 4>) : scale ? latent_read_kernel<256, true, 4> : latent_read_kernel<256, false, 4>,
+                      grid, block, 0, s, nullptr, a);
+    return launch(latent == 512u ? (scale ? latent_read_kernel<512, true, 16> : latent_read_kernel<512, false, 16>) : scale ? latent_read_kernel<256, true, 16> : latent_read_kernel<256, false, 16>,
+                  grid, block, 0, s, nullptr, a);
 }
 
 }  // namespace wg

@@ -163,12 +163,13 @@ __device__ __attribute__((aligned(16))) const uint8_t kZeros[1024] = {};
 
 // kN operands out of LDS, load(i, place), each for products, use(i, place): kAhead of them are asked for before the kAhead in front of them are used.  (Left to itself the compiler asks for one,
 // waits, and uses it.)
-template <uint32_t kN, uint32_t kAhead, typename L, typename U>
-__device__ __forceinline__ void pipelined(L load, U use)
+template <uint32_t kN, uint32_t kAhead, bool kBegun = false, typename L, typename U>
+__device__ __forceinline__ void pipelined(L load, U use)                   // kBegun: the first kAhead have been asked for
 {
     constexpr uint32_t kRounds = (kN + kAhead - 1u) / kAhead;
+    if (!kBegun)
 #pragma unroll
-    for (uint32_t i = 0; i < kAhead && i < kN; i++) load(i, i);
+        for (uint32_t i = 0; i < kAhead && i < kN; i++) load(i, i);
 #pragma unroll
     for (uint32_t b = 0; b < kRounds; b++) {
 #pragma unroll
@@ -532,22 +533,23 @@ struct JoinArgs {
     uint16_t *out;
     uint32_t requests, heads, chunks, rows;          // rows: of a tile
 };
-// A workgroup takes 64 * kOwn dims of kHeads heads of a token, 4 / kHeads wavefronts to a head: few parts are a wavefront's, all dims of a row and all parts asked for together; many are
-// dealt out to four wavefronts, which take 64 dims, so that as many workgroups are at it.
+// Few parts of a row are a wavefront's, all dims and all parts asked for together.  Many are dealt out to the four wavefronts of a workgroup, 64 at a time, and the dims, 64 at a time, to
+// workgroups: 235 parts of 16 rows of 512 take 4.8 us instead of 8.4 with each 64 parts one after the other.
 template <uint32_t kD, bool kMany>
 __global__ void __launch_bounds__(256)
 latent_join_kernel(const JoinArgs a)
 {
     constexpr uint32_t kOwn = kMany ? 1u : kD / 64u, kShare = kMany ? 4u : 1u, kHeads = 4u / kShare, kRound = kMany ? 32u : 4u;
-    __shared__ float part[4][64];
+    __shared__ float part[4][64], tops[4], sums[4];
+    __shared__ uint32_t empties[4];
     const uint32_t lane = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const uint32_t token = blockIdx.x, head = blockIdx.y * kHeads + wave / kShare, first = wave % kShare, d0 = (kMany ? blockIdx.z * 64u : 0u) + lane * kOwn;
+    const uint32_t token = blockIdx.x, head = blockIdx.y * kHeads + wave / kShare, d0 = (kMany ? blockIdx.z * 64u : 0u) + lane * kOwn;
     if (token < (uint32_t)a.starts[0] || token >= (uint32_t)a.starts[a.requests] || head >= a.heads) return;          // (a token of no row has no parts)
     const size_t at = (size_t)token * a.heads + head;
     const Parts p = a.parts[at];
-    const uint32_t chunk = p.chunk_and_row & 0xFFFFu, row = p.chunk_and_row >> 16;
+    const uint32_t chunk = uniform(p.chunk_and_row & 0xFFFFu), row = uniform(p.chunk_and_row >> 16);
     if (p.chunks < 2u || row >= a.rows || chunk >= a.chunks) return;
-    const uint32_t n = p.chunks < a.chunks - chunk ? p.chunks : a.chunks - chunk;
+    const uint32_t n = uniform(p.chunks < a.chunks - chunk ? p.chunks : a.chunks - chunk);
     auto place = [&](uint32_t i) { return (size_t)(i ? 2u * (chunk + i) : 2u * chunk + 1u) * a.rows + row; };
     // a lane for each part, 64 at a time: what it weighs
     float base = -__builtin_inff(), total = 0.f;
@@ -555,20 +557,19 @@ latent_join_kernel(const JoinArgs a)
     float acc[kOwn];
 #pragma unroll
     for (uint32_t d = 0; d < kOwn; d++) acc[d] = 0.f;
-    for (uint32_t i0 = 0; i0 < n; i0 += 64u) {
+    for (uint32_t i0 = wave % kShare * 64u; i0 < n; i0 += 64u * kShare) {
         const Float2 e = i0 + lane < n ? *reinterpret_cast<const Float2 *>(a.ends + place(i0 + lane) * 2u) : Float2{-__builtin_inff(), 0.f};
         const uint32_t more = n - i0 < 64u ? n - i0 : 64u;
         float v[kRound][kOwn];
         auto ask = [&](uint32_t k0) {
 #pragma unroll
             for (uint32_t k = 0; k < kRound; k++) {
-                const uint32_t i = k0 + k * kShare;
-                const float *from = a.partial + place(i0 + (i < more ? i : 0u)) * kD + d0;
+                const float *from = a.partial + place(i0 + (k0 + k < more ? k0 + k : 0u)) * kD + d0;
 #pragma unroll
                 for (uint32_t d = 0; d < kOwn; d++) v[k][d] = from[d];
             }
         };
-        ask(first);
+        ask(0u);
         float top = __builtin_fmaxf(base, e[0]);
 #pragma unroll
         for (int o = 32; o > 0; o >>= 1) top = __builtin_fmaxf(top, __shfl_xor(top, o));
@@ -579,13 +580,12 @@ latent_join_kernel(const JoinArgs a)
         base = top;
 #pragma unroll
         for (uint32_t d = 0; d < kOwn; d++) acc[d] *= by;
-        for (uint32_t k0 = first; k0 < more; k0 += kRound * kShare) {
-            if (k0 != first) ask(k0);
+        for (uint32_t k0 = 0; k0 < more; k0 += kRound) {
+            if (k0) ask(k0);
 #pragma unroll
             for (uint32_t k = 0; k < kRound; k++) {
-                const uint32_t i = k0 + k * kShare;
-                const float wk = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(w), i < 64u ? i : 63u));
-                if (i >= more || wk == 0.f) continue;                      // (a part that weighs nothing may be anything)
+                const float wk = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(w), k0 + k < 64u ? k0 + k : 63u));
+                if (k0 + k >= more || wk == 0.f) continue;                 // (a part that weighs nothing may be anything)
 #pragma unroll
                 for (uint32_t d = 0; d < kOwn; d++) acc[d] += wk * v[k][d];
             }
@@ -593,13 +593,22 @@ latent_join_kernel(const JoinArgs a)
     }
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) total += __shfl_xor(total, o);
-    const float by = share_of_sum(total, __ballot(any) != 0ull);
+    bool empty = __ballot(any) != 0ull;
     if (kMany) {
         part[wave][lane] = acc[0];
+        if (lane == 0u) { tops[wave] = base; sums[wave] = total; empties[wave] = empty; }
         __syncthreads();
         if (wave) return;
-        acc[0] = part[0][lane] + part[1][lane] + part[2][lane] + part[3][lane];
+        const float top = __builtin_fmaxf(__builtin_fmaxf(tops[0], tops[1]), __builtin_fmaxf(tops[2], tops[3])), rel = top > -__builtin_inff() ? top : 0.f;
+        acc[0] = 0.f; total = 0.f;
+#pragma unroll
+        for (uint32_t w = 0; w < 4u; w++) {
+            const float by = __builtin_amdgcn_exp2f(tops[w] - rel);
+            acc[0] += by * part[w][lane]; total += by * sums[w];
+            empty = empty || empties[w];
+        }
     }
+    const float by = share_of_sum(total, empty);
 #pragma unroll
     for (uint32_t d = 0; d < kOwn; d++) acc[d] *= by;                      // (nothing but -inf: 0 times none)
     uint16_t *out = a.out + at * kD + d0;
@@ -693,7 +702,7 @@ struct LatentPromptArgs {
     float factor;
     uint32_t keys;
 };
-constexpr uint32_t kPromptRows = 128, kPromptKeys = 64;
+constexpr uint32_t kPromptRows = 128, kPromptKeys = 32;
 
 __device__ __forceinline__ uint32_t keys_of(const LatentPromptArgs &a, uint32_t r, uint32_t *begin)
 {
@@ -708,9 +717,8 @@ latent_prompt_kernel(const LatentPromptArgs a)
 {
     constexpr uint32_t kM = 2u, kSteps = (kD + kTop) / 32u, kParts = kD / 16u, kPitch = kD + kTop + 16u, kGroupPitch = 32u * kPitch + 192u, kValuePitch = kD + 16u, kValueGroup = 32u * kValuePitch + 192u,
                        kStage = kPromptKeys / kWaves;
-    constexpr uint32_t kPer = 512u / kD, kLoads = kStage / kPer, kTops = kStage / 8u, kAhead = 3u, kPut = kD == 128u ? 1u : 0u, kKept = kSteps - kPut;
-    __shared__ __attribute__((aligned(16))) uint16_t keys[kPromptKeys / 32u * kGroupPitch], values[kPromptKeys / 32u * kValueGroup];
-    __shared__ Half8 q_rest[kPut ? kWaves * kM * kPut * 64u : 1u];         // (as in latent_attend_kernel)
+    constexpr uint32_t kPer = 512u / kD, kLoads = kStage / kPer, kTops = kStage / 8u, kAhead = 4u;
+    __shared__ __attribute__((aligned(16))) uint16_t keys[2u * kGroupPitch], values[2u * kValueGroup];            // two blocks: one that is worked on, one that comes
     __shared__ uint32_t odd_from[kD], any_from;       // of each dim, the first key whose value is none, of those that some rows do not see; the first of all
     const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), heads = a.of.heads;
     auto tiles = [&](uint32_t r) { return (tokens_of(a.of, r) + kPromptRows - 1u) / kPromptRows; };
@@ -768,9 +776,9 @@ latent_prompt_kernel(const LatentPromptArgs a)
             for (uint32_t i = 0; i < kTops; i++) tops[i] = four(rw, own_top + i * 8u * (uint32_t)a.kr_token * 2u);
         };
         // (where keys and values lie in LDS: as in latent_attend_kernel)
-        auto row_at = [&](uint32_t key) { return key / 32u * kGroupPitch + key % 32u * kPitch + key % 32u / 8u * 64u; };
-        auto value_at = [&](uint32_t key) { return key / 32u * kValueGroup + key % 32u * kValuePitch + key % 32u / 8u * 64u; };
-        auto stage = [&](uint32_t block) {
+        auto row_at = [&](uint32_t key) { return key * kPitch + key / 8u * 64u; };
+        auto value_at = [&](uint32_t key) { return key * kValuePitch + key / 8u * 64u; };
+        auto stage = [&](uint32_t block, uint32_t turn) {
             const bool partly = block + kPromptKeys > seen_least;
 #pragma unroll
             for (uint32_t i = 0; i < kLoads; i++) {
@@ -779,14 +787,14 @@ latent_prompt_kernel(const LatentPromptArgs a)
                     atomicMin(&any_from, block + key);
                     raw_v[i] = without_odd_dims(raw_v[i], block + key, d, odd_from);
                 }
-                *reinterpret_cast<Word4 *>(keys + row_at(key) + d) = raw[i];
-                *reinterpret_cast<Word4 *>(values + value_at(key) + d) = raw_v[i];
+                *reinterpret_cast<Word4 *>(keys + turn * kGroupPitch + row_at(key) + d) = raw[i];
+                *reinterpret_cast<Word4 *>(values + turn * kValueGroup + value_at(key) + d) = raw_v[i];
             }
 #pragma unroll
-            for (uint32_t i = 0; i < kTops; i++) *reinterpret_cast<Word4 *>(keys + row_at(wave * kStage + i * 8u + lane / 8u) + kD + lane % 8u * 8u) = tops[i];
+            for (uint32_t i = 0; i < kTops; i++) *reinterpret_cast<Word4 *>(keys + turn * kGroupPitch + row_at(wave * kStage + i * 8u + lane / 8u) + kD + lane % 8u * 8u) = tops[i];
         };
         if (from < to) fetch(from);
-        Half8 q[kM][kKept];
+        Half8 q[kM][kSteps];
         uint32_t sees[kM];
 #pragma unroll
         for (uint32_t n = 0; n < kM; n++) {
@@ -794,9 +802,7 @@ latent_prompt_kernel(const LatentPromptArgs a)
             const uint16_t *qn = a.q_n + (int64_t)token * a.qn_token + (int64_t)head * a.qn_head + g * 8u, *qr = a.q_r + (int64_t)token * a.qr_token + (int64_t)head * a.qr_head + g * 8u;
 #pragma unroll
             for (uint32_t s = 0; s < kSteps; s++) {
-                const Half8 x = signed_query(*reinterpret_cast<const Half8 *>(s < kD / 32u ? qn + s * 32u : qr + (s - kD / 32u) * 32u), a.factor);
-                if (s < kKept) q[n][s % kKept] = x;
-                else q_rest[((wave * kM + n) * kPut + s - kKept) * 64u + lane] = x;
+                q[n][s] = signed_query(*reinterpret_cast<const Half8 *>(s < kD / 32u ? qn + s * 32u : qr + (s - kD / 32u) * 32u), a.factor);
             }
             const uint32_t all = seen_by(i);
             sees[n] = all < to ? all : to;
@@ -805,54 +811,55 @@ latent_prompt_kernel(const LatentPromptArgs a)
         sums.clear();
         if (tid < kD) odd_from[tid] = kNone;
         if (tid == 0u) any_from = kNone;
-        __builtin_amdgcn_s_waitcnt(0x0F70);                                // (as in latent_attend_kernel)
         __syncthreads();
-        for (uint32_t block = from; block < to; block += kPromptKeys) {
-            stage(block);
+        if (from < to) stage(from, 0u);
+        __builtin_amdgcn_s_waitcnt(0x0F70);                                // (as in latent_attend_kernel)
+        if (from + kPromptKeys < to) fetch(from + kPromptKeys);
+        uint32_t turn = 0;
+        for (uint32_t block = from; block < to; block += kPromptKeys, turn ^= 1u) {
             __syncthreads();
-            if (block + kPromptKeys < to) fetch(block + kPromptKeys);
-            Float4 score[2][2][kM];
+            Float4 score[2][kM];
 #pragma unroll
-            for (uint32_t i = 0; i < 4u * kM; i++) score[i / 2u / kM][i / kM % 2u][i % kM] = Float4{0.f, 0.f, 0.f, 0.f};
-            const uint16_t *row = keys + row_at(m / 4u * 8u + m % 4u) + g * 8u;
+            for (uint32_t i = 0; i < 2u * kM; i++) score[i / kM][i % kM] = Float4{0.f, 0.f, 0.f, 0.f};
+            const uint16_t *row = keys + turn * kGroupPitch + row_at(m / 4u * 8u + m % 4u) + g * 8u;
             Half8 x[2][kAhead];
-            pipelined<4u * kSteps, kAhead>([&](uint32_t i, uint32_t at) { x[at / kAhead][at % kAhead] = *reinterpret_cast<const Half8 *>(row + i / 2u % 2u * kGroupPitch + i % 2u * 4u * kPitch + i / 4u * 32u); },
-                                           [&](uint32_t i, uint32_t at) {
-#pragma unroll
-                                               for (uint32_t n = 0; n < kM; n++) {
-                                                   const Half8 y = i / 4u < kKept ? q[n][i / 4u % kKept] : q_rest[((wave * kM + n) * kPut + i / 4u - kKept) * 64u + lane];
-                                                   score[i / 2u % 2u][i % 2u][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x[at / kAhead][at % kAhead], y, score[i / 2u % 2u][i % 2u][n], 0, 0, 0);
-                                               }
-                                           });
-            float s[2][kM][8];
-            const uint32_t at = block + g * 8u;
-#pragma unroll
-            for (uint32_t k = 0; k < 2u; k++)
-#pragma unroll
-                for (uint32_t n = 0; n < kM; n++)
-#pragma unroll
-                    for (uint32_t j = 0; j < 8u; j++) s[k][n][j] = score[k][j / 4u][n][j % 4u];
-            if (block + kPromptKeys > seen_least || block + kPromptKeys > to)
-#pragma unroll
-                for (uint32_t k = 0; k < 2u; k++)
-#pragma unroll
-                    for (uint32_t n = 0; n < kM; n++)
-#pragma unroll
-                        for (uint32_t j = 0; j < 8u; j++) s[k][n][j] = at + k * 32u + j < sees[n] ? s[k][n][j] : -__builtin_inff();
-            Half8 p[2][kM];
-            sums.template weigh<2>(s, size_of(a.factor), p);
-            const uint16_t *column = values + value_at(g * 8u + m / 4u) + m % 4u * 4u;
-            pipelined<2u * kParts, kAhead>([&](uint32_t i, uint32_t at) {
-                                               const uint16_t *of = column + i % 2u * kValueGroup + i / 2u * 16u;
-                                               x[at / kAhead][at % kAhead] = both(column_of(of), column_of(of + 4u * kValuePitch));
-                                           },
+            pipelined<2u * kSteps, kAhead>([&](uint32_t i, uint32_t at) { x[at / kAhead][at % kAhead] = *reinterpret_cast<const Half8 *>(row + i % 2u * 4u * kPitch + i / 2u * 32u); },
                                            [&](uint32_t i, uint32_t at) {
 #pragma unroll
                                                for (uint32_t n = 0; n < kM; n++)
-                                                   sums.acc[i / 2u][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x[at / kAhead][at % kAhead], p[i % 2u][n], sums.acc[i / 2u][n], 0, 0, 0);
+                                                   score[i % 2u][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x[at / kAhead][at % kAhead], q[n][i / 2u], score[i % 2u][n], 0, 0, 0);
                                            });
-            __syncthreads();
+            float s[1][kM][8];
+            const uint32_t at = block + g * 8u;
+#pragma unroll
+            for (uint32_t n = 0; n < kM; n++)
+#pragma unroll
+                for (uint32_t j = 0; j < 8u; j++) s[0][n][j] = score[j / 4u][n][j % 4u];
+            if (block + kPromptKeys > seen_least || block + kPromptKeys > to)
+#pragma unroll
+                for (uint32_t n = 0; n < kM; n++)
+#pragma unroll
+                    for (uint32_t j = 0; j < 8u; j++) s[0][n][j] = at + j < sees[n] ? s[0][n][j] : -__builtin_inff();
+            // (the first values are on their way while the scores become weights)
+            const uint16_t *column = values + turn * kValueGroup + value_at(g * 8u + m / 4u) + m % 4u * 4u;
+            auto ask = [&](uint32_t d, uint32_t at) { x[at / kAhead][at % kAhead] = both(column_of(column + d * 16u), column_of(column + 4u * kValuePitch + d * 16u)); };
+#pragma unroll
+            for (uint32_t d = 0; d < kAhead; d++) ask(d, d);
+            __builtin_amdgcn_sched_barrier(0);
+            Half8 p[1][kM];
+            sums.template weigh<1>(s, size_of(a.factor), p);
+            if (block + kPromptKeys < to) {
+                stage(block + kPromptKeys, turn ^ 1u);
+                if (block + 2u * kPromptKeys < to) fetch(block + 2u * kPromptKeys);
+            }
+            pipelined<kParts, kAhead, true>(ask,
+                                      [&](uint32_t d, uint32_t at) {
+#pragma unroll
+                                          for (uint32_t n = 0; n < kM; n++)
+                                              sums.acc[d][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x[at / kAhead][at % kAhead], p[0][n], sums.acc[d][n], 0, 0, 0);
+                                      });
         }
+        __syncthreads();
 #pragma unroll
         for (uint32_t n = 0; n < kM; n++) {
             const float sum = sums.whole_sum(n);
