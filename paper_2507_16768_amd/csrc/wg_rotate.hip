@@ -44,7 +44,7 @@ template <> struct Numbers<uint16_t, 8> {
     }
     static __device__ __forceinline__ void store(uint16_t *p, const float (&v)[8])
     {
-        *reinterpret_cast<Word4 *>(p) = Word4{pk_bf16(v[0], v[1]), pk_bf16(v[2], v[3]), pk_bf16(v[4], v[5]), pk_bf16(v[6], v[7])};
+        __builtin_nontemporal_store(Word4{pk_bf16(v[0], v[1]), pk_bf16(v[2], v[3]), pk_bf16(v[4], v[5]), pk_bf16(v[6], v[7])}, reinterpret_cast<Word4 *>(p));
     }
 };
 template <> struct Numbers<float, 4> {
@@ -54,7 +54,7 @@ template <> struct Numbers<float, 4> {
 #pragma unroll
         for (uint32_t i = 0; i < 4u; i++) v[i] = w[i];
     }
-    static __device__ __forceinline__ void store(float *p, const float (&v)[4]) { *reinterpret_cast<Float4 *>(p) = Float4{v[0], v[1], v[2], v[3]}; }
+    static __device__ __forceinline__ void store(float *p, const float (&v)[4]) { __builtin_nontemporal_store(Float4{v[0], v[1], v[2], v[3]}, reinterpret_cast<Float4 *>(p)); }
 };
 template <> struct Numbers<uint16_t, 1> {
     static __device__ __forceinline__ void load(const uint16_t *p, float (&v)[1]) { v[0] = __uint_as_float((uint32_t)*p << 16); }
@@ -80,42 +80,54 @@ rotate_kernel(const RotateArgs a)
         turns[i] = make_float2(cs.x * a.magnitude, cs.y * a.magnitude);
     }
     __syncthreads();
-    const uint32_t heads = a.heads[0] + a.heads[1], all = n * heads * a.units;
-    for (uint32_t i = blockIdx.y * kRotateThreads + threadIdx.x; i < all; i += gridDim.y * kRotateThreads) {
-        const uint32_t head_of = i / a.units, u = i - head_of * a.units, t = head_of / heads, h0 = head_of - t * heads;
-        const uint32_t which = h0 >= a.heads[0] ? 1u : 0u, h = which ? h0 - a.heads[0] : h0;
-        const T *x = static_cast<const T *>(a.x[which]) + (int64_t)(first + t) * a.x_token[which] + (int64_t)h * a.x_head[which];
-        T *out = static_cast<T *>(a.out[which]) + (int64_t)(first + t) * a.out_token[which] + (int64_t)h * a.out_head[which];
-        const float2 *turn = turns + t * a.pairs;
-        if (u >= a.turned_units) {                   // behind the pairs
-            const uint32_t d = 2u * a.pairs + (u - a.turned_units) * kN;
-            float v[kN];
-            if (x == out) continue;
-            Numbers<T, kN>::load(x + d, v);
-            Numbers<T, kN>::store(out + d, v);
-        } else if (kBeside && kN > 1u) {
-            float v[kN];
-            Numbers<T, kN>::load(x + u * kN, v);
+    // A thread has one unit's place of a head; its heads' numbers (rows) are asked for kOnce at a time.
+    constexpr uint32_t kOnce = kN > 1u ? 4u : 1u;
+    const uint32_t heads = a.heads[0] + a.heads[1], rows = n * heads, at_once = kRotateThreads / a.units ? kRotateThreads / a.units : 1u, step = gridDim.y * at_once;
+    for (uint32_t u = threadIdx.x % (at_once * a.units) % a.units; threadIdx.x < at_once * a.units && u < a.units; u += kRotateThreads) {
+        const bool turned = u < a.turned_units;
+        const uint32_t d = turned ? (kBeside && kN == 1u ? 2u * u : u * kN) : 2u * a.pairs + (u - a.turned_units) * kN, e = d + (kBeside ? 1u : a.pairs);
+        const float2 *turn = turns + (kBeside && kN > 1u ? u * (kN / 2u) : u * kN);
+        auto place = [&](uint32_t r, const T **x, T **out) {
+            const uint32_t t = r / heads, h0 = r - t * heads, which = h0 >= a.heads[0] ? 1u : 0u, h = which ? h0 - a.heads[0] : h0;
+            *x = static_cast<const T *>(a.x[which]) + (int64_t)(first + t) * a.x_token[which] + (int64_t)h * a.x_head[which];
+            *out = static_cast<T *>(a.out[which]) + (int64_t)(first + t) * a.out_token[which] + (int64_t)h * a.out_head[which];
+            return t;
+        };
+        for (uint32_t r0 = blockIdx.y * at_once + threadIdx.x / a.units % at_once; r0 < rows; r0 += step * kOnce) {
+            float v[kOnce][kN], w[kOnce][kN];
+            T *out[kOnce];
+            uint32_t t[kOnce];
+            bool moved[kOnce];
 #pragma unroll
-            for (uint32_t k = 0; k < kN / 2u; k++) {
-                const float2 cs = turn[u * (kN / 2u) + k];
-                const float p = v[2u * k], q = v[(2u * k + 1u) % kN];
-                v[2u * k] = p * cs.x - q * cs.y; v[(2u * k + 1u) % kN] = p * cs.y + q * cs.x;
+            for (uint32_t j = 0; j < kOnce; j++) {
+                const uint32_t r = r0 + j * step;
+                const T *x;
+                t[j] = place(r < rows ? r : r0, &x, &out[j]);
+                moved[j] = r < rows && (turned || x != out[j]);
+                Numbers<T, kN>::load(x + d, v[j]);
+                if (turned && (!kBeside || kN == 1u)) Numbers<T, kN>::load(x + e, w[j]);
             }
-            Numbers<T, kN>::store(out + u * kN, v);
-        } else {
-            const uint32_t d = kBeside ? 2u * u : u * kN, e = kBeside ? d + 1u : d + a.pairs;
-            float v[kN], w[kN];
-            Numbers<T, kN>::load(x + d, v);
-            Numbers<T, kN>::load(x + e, w);
 #pragma unroll
-            for (uint32_t k = 0; k < kN; k++) {
-                const float2 cs = turn[u * kN + k];
-                const float p = v[k], q = w[k];
-                v[k] = p * cs.x - q * cs.y; w[k] = p * cs.y + q * cs.x;
+            for (uint32_t j = 0; j < kOnce; j++) {
+                if (!moved[j]) continue;
+                if (!turned) { Numbers<T, kN>::store(out[j] + d, v[j]); continue; }             // behind the pairs
+                const float2 *cs = turn + t[j] * a.pairs;
+                if (kBeside && kN > 1u) {
+#pragma unroll
+                    for (uint32_t k = 0; k < kN / 2u; k++) {
+                        const float p = v[j][2u * k], q = v[j][(2u * k + 1u) % kN];
+                        v[j][2u * k] = p * cs[k].x - q * cs[k].y; v[j][(2u * k + 1u) % kN] = p * cs[k].y + q * cs[k].x;
+                    }
+                } else {
+#pragma unroll
+                    for (uint32_t k = 0; k < kN; k++) {
+                        const float p = v[j][k], q = w[j][k];
+                        v[j][k] = p * cs[k].x - q * cs[k].y; w[j][k] = p * cs[k].y + q * cs[k].x;
+                    }
+                    Numbers<T, kN>::store(out[j] + e, w[j]);
+                }
+                Numbers<T, kN>::store(out[j] + d, v[j]);
             }
-            Numbers<T, kN>::store(out + d, v);
-            Numbers<T, kN>::store(out + e, w);
         }
     }
 }
