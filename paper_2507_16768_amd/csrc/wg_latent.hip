@@ -8,10 +8,10 @@
 
 namespace wg {
 
-constexpr uint32_t kLatentThreads = 256, kLatentWaves = 4;
+constexpr uint32_t kLatentThreads = 256, kLatentWaves = 4, kNoToken = 0xFFFFFFFFu;
 
 // ---------------------------------------------------------------------------------------------
-// append.  A wavefront for each token.  A token has a scale of its own, so nothing that is in the cache is rounded again; what comes along from another page is copied as it is, by all
+// append.  A wavefront for each token, or for four, all asked for at once, where there are many.  A token has a scale of its own, so nothing that is in the cache is rounded again; what comes along from another page is copied as it is, by all
 // wavefronts of the workgroup (63 tokens of 644 bytes at the most).
 struct LatentAppendArgs {
     const uint16_t *c, *r;
@@ -29,44 +29,53 @@ __device__ __forceinline__ void copy_words(void *to, const void *from, uint32_t 
     for (uint32_t i = tid; i < words; i += kLatentThreads) static_cast<Word4 *>(to)[i] = static_cast<const Word4 *>(from)[i];
 }
 
-template <uint32_t kC, bool kBytes>
+template <uint32_t kC, bool kBytes, uint32_t kTokens>
 __global__ void __launch_bounds__(kLatentThreads)
 latent_append_kernel(const LatentAppendArgs a)
 {
-    constexpr uint32_t kOwn = kC / 64u, kRow = kC * (kBytes ? 1u : 2u);    // dims of a lane; bytes of a token
+    constexpr uint32_t kOwn = kC / 64u, kWords = kOwn / 2u, kRow = kC * (kBytes ? 1u : 2u);               // dims of a lane; words; bytes of a token
     const uint32_t tid = threadIdx.x, lane = tid & 63u, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const uint32_t first = blockIdx.x * a.per, t = first + wave;
-    if (wave < a.per && t < a.tokens) {
-        const uint32_t slot = (uint32_t)a.slots[t];
-        uint32_t w[kOwn / 2u];
-        const uint32_t *x = reinterpret_cast<const uint32_t *>(a.c + (int64_t)t * a.c_token) + lane * (kOwn / 2u);
+    const uint32_t first = blockIdx.x * a.per;
+    uint32_t slot[kTokens], w[kTokens][kWords], r[kTokens];
 #pragma unroll
-        for (uint32_t i = 0; i < kOwn / 2u; i++) w[i] = x[i];
-        const uint32_t r = lane < 32u ? reinterpret_cast<const uint32_t *>(a.r + (int64_t)t * a.r_token)[lane] : 0u;
-        if (slot >> a.shift < a.pages) {
-            uint32_t *to = reinterpret_cast<uint32_t *>(a.c_cache + (size_t)slot * kRow) + lane * (kRow / 256u);
-            if (kBytes) {
-                float top = 0.f;
+    for (uint32_t k = 0; k < kTokens; k++) {
+        const uint32_t t = first + wave * kTokens + k;
+        const bool there = wave * kTokens + k < a.per && t < a.tokens;
+        const uint32_t at = there ? t : first;
+        slot[k] = there ? (uint32_t)a.slots[at] : kNoToken;
+        const uint32_t *x = reinterpret_cast<const uint32_t *>(a.c + (int64_t)at * a.c_token) + lane * kWords;
 #pragma unroll
-                for (uint32_t i = 0; i < kOwn / 2u; i++) { top = top_of(top, low(w[i])); top = top_of(top, high(w[i])); }
+        for (uint32_t i = 0; i < kWords; i++) w[k][i] = x[i];
+        r[k] = reinterpret_cast<const uint32_t *>(a.r + (int64_t)at * a.r_token)[lane & 31u];
+    }
 #pragma unroll
-                for (int s = 32; s > 0; s >>= 1) top = __builtin_fmaxf(top, __shfl_xor(top, s));
-                const float scale = scale_for(top), inverse = 1.f / scale;
-                if (lane == 0u) a.scale[slot] = scale;
+    for (uint32_t k = 0; k < kTokens; k++) {
+        if (slot[k] >> a.shift >= a.pages) continue;
+        uint32_t *to = reinterpret_cast<uint32_t *>(a.c_cache + (size_t)slot[k] * kRow) + lane * (kRow / 256u);
+        if (kBytes) {
+            float top = 0.f;
 #pragma unroll
-                for (uint32_t i = 0; i < kOwn / 4u; i++)
-                    to[i] = to_bytes(low(w[2u * i]) * inverse, high(w[2u * i]) * inverse, low(w[2u * i + 1u]) * inverse, high(w[2u * i + 1u]) * inverse);
-            } else
+            for (uint32_t i = 0; i < kWords; i++) { top = top_of(top, low(w[k][i])); top = top_of(top, high(w[k][i])); }
 #pragma unroll
-                for (uint32_t i = 0; i < kOwn / 2u; i++) to[i] = w[i];
-            if (lane < 32u) reinterpret_cast<uint32_t *>(a.r_cache + (size_t)slot * kLatentKey)[lane] = r;
-        }
+            for (int s = 32; s > 0; s >>= 1) top = __builtin_fmaxf(top, __shfl_xor(top, s));
+            const float scale = scale_for(top), inverse = 1.f / scale;
+            if (lane == 0u) a.scale[slot[k]] = scale;
+#pragma unroll
+            for (uint32_t i = 0; i < kOwn / 4u; i++)
+                to[i] = to_bytes(low(w[k][2u * i]) * inverse, high(w[k][2u * i]) * inverse, low(w[k][2u * i + 1u]) * inverse, high(w[k][2u * i + 1u]) * inverse);
+        } else
+#pragma unroll
+            for (uint32_t i = 0; i < kWords; i++) to[i] = w[k][i];
+        if (lane < 32u) reinterpret_cast<uint32_t *>(a.r_cache + (size_t)slot[k] * kLatentKey)[lane] = r[k];
     }
     if (!a.origins) return;
-    for (uint32_t i = 0; i < a.per && first + i < a.tokens; i++) {
-        const uint32_t origin = (uint32_t)a.origins[first + i], slot = (uint32_t)a.slots[first + i], page = slot >> a.shift, o = slot & ((1u << a.shift) - 1u);
-        if (origin >= a.pages || page >= a.pages || !o || origin == page) continue;
-        const size_t from = (size_t)origin << a.shift, to = (size_t)page << a.shift;
+    // tokens whose page has begun in another one: a lane looks at each
+    const uint32_t own = lane < a.per && first + lane < a.tokens ? first + lane : kNoToken;
+    const uint32_t own_origin = own != kNoToken ? (uint32_t)a.origins[own] : kNoToken, own_slot = own != kNoToken ? (uint32_t)a.slots[own] : kNoToken;
+    const bool taken = own_origin < a.pages && own_slot >> a.shift < a.pages && (own_slot & ((1u << a.shift) - 1u)) && own_origin != own_slot >> a.shift;
+    for (unsigned long long left = __ballot(taken); left; left &= left - 1ull) {
+        const uint32_t i = (uint32_t)__builtin_ctzll(left), origin = __builtin_amdgcn_readlane(own_origin, i), at = __builtin_amdgcn_readlane(own_slot, i), o = at & ((1u << a.shift) - 1u);
+        const size_t from = (size_t)origin << a.shift, to = (size_t)(at >> a.shift) << a.shift;
         copy_words(a.c_cache + to * kRow, a.c_cache + from * kRow, o * (kRow / 16u), tid);
         copy_words(a.r_cache + to * kLatentKey, a.r_cache + from * kLatentKey, o * (kLatentKey / 8u), tid);
         if (kBytes && tid < o) a.scale[to + tid] = a.scale[from + tid];
@@ -76,11 +85,16 @@ latent_append_kernel(const LatentAppendArgs a)
 hipError_t launch_latent_append(const void *c, const void *r, uint32_t tokens, uint32_t latent, int64_t c_token, int64_t r_token, const int32_t *slots, const int32_t *origins,
                                 void *c_cache, void *r_cache, float *scale, uint32_t pages, uint32_t shift, hipStream_t s)
 {
-    const uint32_t per = tokens <= 1024u ? 1u : kLatentWaves;
+    const bool many = tokens > 4096u;
+    const uint32_t per = tokens <= 1024u ? 1u : kLatentWaves * (many ? 4u : 1u);
     const LatentAppendArgs a{static_cast<const uint16_t *>(c), static_cast<const uint16_t *>(r), c_token, r_token, slots, origins, static_cast<uint8_t *>(c_cache),
                              static_cast<uint16_t *>(r_cache), scale, tokens, pages, shift, per};
-    return launch(latent == 512u ? (scale ? latent_append_kernel<512, true> : latent_append_kernel<512, false>) : scale ? latent_append_kernel<256, true> : latent_append_kernel<256, false>,
-                  dim3((tokens + per - 1u) / per), dim3(kLatentThreads), 0, s, nullptr, a);
+    const dim3 grid((tokens + per - 1u) / per), block(kLatentThreads);
+    if (many)
+        return launch(latent == 512u ? (scale ? latent_append_kernel<512, true, 4> : latent_append_kernel<512, false, 4>) : scale ? latent_append_kernel<256, true, 4> : latent_append_kernel<256, false, 4>,
+                      grid, block, 0, s, nullptr, a);
+    return launch(latent == 512u ? (scale ? latent_append_kernel<512, true, 1> : latent_append_kernel<512, false, 1>) : scale ? latent_append_kernel<256, true, 1> : latent_append_kernel<256, false, 1>,
+                  grid, block, 0, s, nullptr, a);
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -94,6 +108,14 @@ struct LatentReadArgs {
     int64_t c_token, r_token;
     uint32_t rows, columns, tokens, pages, shift;
 };
+// 8 or 16 bytes of a lane, past the caches' own.
+template <uint32_t kN>
+__device__ __forceinline__ void stream_words(uint32_t *to, const uint32_t (&w)[kN])
+{
+    if (kN == 4u) __builtin_nontemporal_store(Word4{w[0], w[1], w[2 % kN], w[3 % kN]}, reinterpret_cast<Word4 *>(to));
+    else __builtin_nontemporal_store(Word2{w[0], w[1]}, reinterpret_cast<Word2 *>(to));
+}
+
 template <uint32_t kC, bool kBytes, uint32_t kReadTokens>
 __global__ void __launch_bounds__(kLatentThreads)
 latent_read_kernel(const LatentReadArgs a)
@@ -128,18 +150,19 @@ latent_read_kernel(const LatentReadArgs a)
 #pragma unroll
     for (uint32_t i = 0; i < kReadTokens; i++) {
         if (!(known >> i & 1u)) continue;
-        uint32_t *to = reinterpret_cast<uint32_t *>(a.c_out + (int64_t)(base + i) * a.c_token) + lane * (kOwn / 2u);
+        uint32_t *to = reinterpret_cast<uint32_t *>(a.c_out + (int64_t)(base + i) * a.c_token) + lane * (kOwn / 2u), out[kOwn / 2u];
         if (kBytes) {
             const float scale = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(own_scale), i));
 #pragma unroll
             for (uint32_t k = 0; k < kWords; k++) {
                 const auto x = __builtin_amdgcn_cvt_pk_f32_fp8((int)w[i][k], false), y = __builtin_amdgcn_cvt_pk_f32_fp8((int)w[i][k], true);
-                to[2u * k] = pk_bf16(x[0] * scale, x[1] * scale);
-                to[2u * k + 1u] = pk_bf16(y[0] * scale, y[1] * scale);
+                out[2u * k] = pk_bf16(x[0] * scale, x[1] * scale);
+                out[2u * k + 1u] = pk_bf16(y[0] * scale, y[1] * scale);
             }
         } else
 #pragma unroll
-            for (uint32_t k = 0; k < kWords; k++) to[k] = w[i][k];
+            for (uint32_t k = 0; k < kWords; k++) out[k % (kOwn / 2u)] = w[i][k];
+        stream_words<kOwn / 2u>(to, out);
         if (lane < 32u) reinterpret_cast<uint32_t *>(a.r_out + (int64_t)(base + i) * a.r_token)[lane] = r[i];
     }
 }
