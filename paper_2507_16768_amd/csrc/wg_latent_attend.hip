@@ -91,7 +91,7 @@ __device__ __forceinline__ bool chunk_of(const Requests &a, uint32_t w, F work_o
     if (w >= a.chunks || out->at >= all) return false;
     out->end = all - out->at < size ? all : out->at + size;
     uint32_t ahead = 0;                              // work of the requests in front
-    for (uint32_t base = 0;; base += 64u) {
+    for (uint32_t base = 0; base < a.rows; base += 64u) {
         const uint32_t own = base + lane < a.rows ? work_of(base + lane) : 0u;
         uint32_t sum = own;
 #pragma unroll
@@ -105,6 +105,22 @@ __device__ __forceinline__ bool chunk_of(const Requests &a, uint32_t w, F work_o
         }
         ahead += __builtin_amdgcn_readlane(sum, 63);
     }
+    return false;
+}
+
+// The next part of a tile: blocks [b0, b0 + n) of its `blocks`, and how many chunks it lies in.  A tile counts as kTileCost blocks more, in front of its own: asking for its queries and storing its
+// outputs take that long.  false: the chunk ends among these.  (off: the chunk's place in the tile; work: of the request)
+__device__ __forceinline__ bool part_of(Chunk *c, uint32_t off, uint32_t blocks, uint32_t work, uint32_t *b0, uint32_t *n, uint32_t *chunks)
+{
+    const uint32_t whole = blocks + kTileCost, took = whole - off < c->end - c->at ? whole - off : c->end - c->at, end = off + took;
+    const uint32_t begins = c->at - off + kTileCost;                       // where the tile's own blocks do, among all
+    *b0 = off > kTileCost ? off - kTileCost : 0u;
+    *n = (end > kTileCost ? end - kTileCost : 0u) - *b0;
+    *chunks = (begins + blocks - 1u) / c->size - begins / c->size + 1u;
+    c->at += took;
+    c->off += took;
+    if (c->off >= work) { c->off = 0; c->row++; }
+    return *n != 0u;
 }
 
 // Where the parts of a query row lie: its first chunk and its place in the tile, and how many chunks.
@@ -309,29 +325,25 @@ latent_attend_kernel(const LatentAttendArgs a)
     auto tiles = [&](uint32_t r) { return (uint32_t)(((uint64_t)tokens_of(a.of, r) * heads + kRows - 1u) / kRows); };
     Tile t;
     Chunk c{0u, 1u, 0u, 0u, 0u};
-    if (a.of.chunks ? !chunk_of(a.of, blockIdx.x, [&](uint32_t r) { return tiles(r) * blocks_of(cached_tokens(a, r)); }, &c) : !tile_of<kRows>(a.of, heads, blockIdx.x, &t)) return;
-    while (c.at < c.end) {
+    if (a.of.chunks ? !chunk_of(a.of, blockIdx.x, [&](uint32_t r) { return tiles(r) * (blocks_of(cached_tokens(a, r)) + kTileCost); }, &c) : !tile_of<kRows>(a.of, heads, blockIdx.x, &t)) return;
+    while (c.at < c.end && c.row < a.of.rows) {
         // (What follows from the thread's number is made anew for each part: kept over the parts it would take registers from the loop over keys.)
         const uint32_t tid = anew(threadIdx.x), lane = tid & 63u, m = lane & 15u, g = lane >> 4;
         // the next part of a tile: blocks [b0, b0 + n) of its `blocks`
-        uint32_t b0 = 0, n = 1u, blocks = 1u, begins = 0;                  // begins: where the tile's blocks do, among all
+        uint32_t b0 = 0, n = 1u, blocks = 1u, chunks = 1u;                 // chunks: that the tile lies in
         if (a.of.chunks) {
-            const uint32_t work = uniform(tiles(c.row) * (blocks = uniform(blocks_of(cached_tokens(a, c.row))))), tile = c.off / blocks;
+            blocks = uniform(blocks_of(cached_tokens(a, c.row)));
+            const uint32_t tile = c.off / (blocks + kTileCost), work = uniform(tiles(c.row)) * (blocks + kTileCost);
             if (!work) { c.row++; continue; }                              // (off is 0)
             (void)tile_at<kRows>(a.of, heads, c.row, tile, &t);
-            b0 = c.off - tile * blocks;
-            n = blocks - b0 < c.end - c.at ? blocks - b0 : c.end - c.at;
-            begins = c.at - b0;
-            c.off += n;
-            if (c.off >= work) { c.off = 0; c.row++; }
-        }
+            if (!part_of(&c, c.off - tile * (blocks + kTileCost), blocks, work, &b0, &n, &chunks)) continue;
+        } else c.at++;
         const uint32_t len = uniform(cached_tokens(a, t.row));
         t.before = (int32_t)len - (int32_t)t.count;
         const bool whole = n == blocks;
         const uint32_t place = 2u * blockIdx.x + (b0 ? 0u : 1u), row_first = t.first;
         if (a.of.chunks && b0 == 0u && tid < kRows && t.first + tid < t.last)
-            a.parts[(size_t)t.begin * heads + t.first + tid] = Parts{blockIdx.x | tid << 16, whole ? 1u : (begins + blocks - 1u) / c.size - blockIdx.x + 1u};
-        c.at += n;
+            a.parts[(size_t)t.begin * heads + t.first + tid] = Parts{blockIdx.x | tid << 16, chunks};
         auto seen_by = [&](uint32_t i) { const int32_t k = t.before + (int32_t)(i / heads) + 1; return k < 0 ? 0u : (uint32_t)k; };
         const uint32_t seen_least = seen_by(t.first), seen_most = seen_by(t.last - 1u);
         const uint32_t from = b0 * kAttendBlock, to0 = whole ? seen_most : from + n * kAttendBlock, to = to0 < seen_most ? to0 : seen_most;
@@ -623,8 +635,8 @@ struct Plan { uint32_t chunks; uint64_t partial, ends, parts; };
 static Plan plan_of(uint64_t tiles, uint64_t blocks, uint32_t rows, uint32_t tile_rows, uint32_t dim, uint32_t slots, uint64_t outputs)
 {
     Plan p{0u, 0u, 0u, 0u};
-    if (rows > 1024u || blocks < 2u || tiles >= 2u * slots || tiles * blocks > 0x7FFFFFFFull) return p;
-    const uint64_t most = (tiles * blocks + kAttendLeast - 1u) / kAttendLeast;
+    if (rows > 1024u || blocks < 2u || tiles >= 2u * slots || tiles * (blocks + kTileCost) > 0x7FFFFFFFull) return p;
+    const uint64_t most = (tiles * (blocks + kTileCost) + kAttendLeast - 1u) / kAttendLeast;
     p.chunks = (uint32_t)(most < slots ? most : slots);
     p.partial = (uint64_t)p.chunks * 2u * tile_rows * dim;
     p.ends = (uint64_t)p.chunks * 2u * tile_rows * 2u;
@@ -726,30 +738,26 @@ latent_prompt_kernel(const LatentPromptArgs a)
     Tile t;
     Chunk c{0u, 1u, 0u, 0u, 0u};
     uint32_t head = uniform(blockIdx.x % heads);
-    if (a.of.chunks ? !chunk_of(a.of, blockIdx.x, [&](uint32_t r) { return tiles(r) * heads * blocks_at(r); }, &c) : !tile_of<kPromptRows>(a.of, 1u, blockIdx.x / heads, &t)) return;
+    if (a.of.chunks ? !chunk_of(a.of, blockIdx.x, [&](uint32_t r) { return tiles(r) * heads * (blocks_at(r) + kTileCost); }, &c) : !tile_of<kPromptRows>(a.of, 1u, blockIdx.x / heads, &t)) return;
     if (!a.of.chunks) (void)tile_at<kPromptRows>(a.of, 1u, t.row, uniform(tiles(t.row)) - 1u - t.first / kPromptRows, &t);             // the last, which see the most keys, first
-    while (c.at < c.end) {
+    while (c.at < c.end && c.row < a.of.rows) {
         const uint32_t tid = anew(threadIdx.x), lane = tid & 63u, m = lane & 15u, g = lane >> 4;
-        uint32_t b0 = 0, n_blocks = 1u, blocks = 1u, begins = 0, begin;
+        uint32_t b0 = 0, n_blocks = 1u, blocks = 1u, chunks = 1u, begin;
         if (a.of.chunks) {
-            const uint32_t work = uniform(tiles(c.row) * heads * (blocks = uniform(blocks_at(c.row)))), unit = c.off / blocks;
+            blocks = uniform(blocks_at(c.row));
+            const uint32_t unit = c.off / (blocks + kTileCost), work = uniform(tiles(c.row)) * heads * (blocks + kTileCost);
             if (!work) { c.row++; continue; }                              // (off is 0)
             head = uniform(unit % heads);
             (void)tile_at<kPromptRows>(a.of, 1u, c.row, unit / heads, &t);
-            b0 = c.off - unit * blocks;
-            n_blocks = blocks - b0 < c.end - c.at ? blocks - b0 : c.end - c.at;
-            begins = c.at - b0;
-            c.off += n_blocks;
-            if (c.off >= work) { c.off = 0; c.row++; }
-        }
+            if (!part_of(&c, c.off - unit * (blocks + kTileCost), blocks, work, &b0, &n_blocks, &chunks)) continue;
+        } else c.at++;
         const uint32_t len = uniform(keys_of(a, t.row, &begin));
         begin = uniform(begin);
         t.before = (int32_t)len - (int32_t)t.count;
         const bool whole = n_blocks == blocks;
         const uint32_t place = 2u * blockIdx.x + (b0 ? 0u : 1u);
         if (a.of.chunks && b0 == 0u && tid < kPromptRows && t.first + tid < t.last)
-            a.parts[(size_t)(t.begin + t.first + tid) * heads + head] = Parts{blockIdx.x | tid << 16, whole ? 1u : (begins + blocks - 1u) / c.size - blockIdx.x + 1u};
-        c.at += n_blocks;
+            a.parts[(size_t)(t.begin + t.first + tid) * heads + head] = Parts{blockIdx.x | tid << 16, chunks};
         auto seen_by = [&](uint32_t i) { const int32_t k = t.before + (int32_t)i + 1; return k < 0 ? 0u : (uint32_t)k; };
         const uint32_t seen_least = seen_by(t.first), seen_most = seen_by(t.last - 1u);
         const uint32_t from = b0 * kAttendBlock, to0 = whole ? seen_most : from + n_blocks * kAttendBlock, to = to0 < seen_most ? to0 : seen_most;

@@ -42,7 +42,7 @@ hipError_t launch_latent_append(const void *c, const void *r, uint32_t tokens, u
 hipError_t launch_latent_read(const void *c_cache, const void *r_cache, const float *scale, uint32_t latent, uint32_t pages, uint32_t shift, const int32_t *table, uint32_t rows,
                               uint32_t columns, const int32_t *starts, uint32_t tokens, void *c_out, int64_t c_token, void *r_out, int64_t r_token, hipStream_t s);
 // Keys of a block, blocks of a chunk of work at least, and chunks at most: as many workgroups as the chip holds at a time.
-constexpr uint32_t kAttendBlock = 128, kAttendLeast = 1, kAttendSlots = 256, kPromptSlots = 512;
+constexpr uint32_t kAttendBlock = 128, kAttendLeast = 1, kTileCost = 1, kAttendSlots = 256, kPromptSlots = 512;
 bool latent_attend_fits(uint32_t tokens, uint32_t rows, uint32_t heads);
 uint64_t latent_attend_bytes(uint32_t tokens, uint32_t rows, uint32_t heads, uint32_t latent, uint32_t columns, uint32_t shift);
 // strides: of tokens and heads of q_c and q_r.

@@ -467,6 +467,101 @@ def test_prompt_values_that_are_none(bad, at):
         assert fine.all()
 
 
+def test_attend_fewer_tokens_than_the_rows_have():
+    """A call with the first tokens of a step alone: they see what they see in the whole call.  And rows that begin behind the first token."""
+    for H, lens, counts in ((16, [700, 90, 3000], [3, 40, 200]), (128, [300, 2000], [2, 5])):
+        g = gen(H)
+        table, N = pages_of(g, lens, 32)
+        c_cache, r_cache, _ = new_cache(g, N, 32, 512, 16)
+        T = sum(counts)
+        q_c, q_r = bf16(g, T, H, 512), bf16(g, T, H, E)
+        starts, lens_t, out = ints(starts_of(counts)), ints(lens), torch.empty((T, H, 512), dtype=torch.bfloat16, device="cuda")
+        work = torch.empty(1 << 28, dtype=torch.uint8, device="cuda")
+        wg.latent_attend(q_c, q_r, c_cache, r_cache, None, table, lens_t, starts, 0.07, out, work)
+        v, r = values(c_cache, None), r_cache.view(-1, E).double()
+        for few in (1, counts[0], counts[0] + 1, T - 1):
+            part = torch.empty((few, H, 512), dtype=torch.bfloat16, device="cuda")
+            wg.latent_attend(q_c[:few], q_r[:few], c_cache, r_cache, None, table, lens_t, starts, 0.07, part, work)
+            at = 0
+            for row, n in enumerate(counts):
+                m = max(0, min(n, few - at))
+                if m:
+                    i = torch.arange(lens[row], device="cuda")
+                    slots = table[row].long()[i // 32] * 32 + i % 32
+                    seen = lens[row] - n + 1 + torch.arange(m, device="cuda")
+                    want, off = attention(torch.cat((q_c[at:at + m], q_r[at:at + m]), -1), torch.cat((v[slots], r[slots]), -1)[:, None], v[slots][:, None], seen, 0.07)
+                    assert ((part[at:at + m].double() - want).abs() <= off).all()
+                at += n
+        # the rows begin at token 5
+        moved = torch.full((T + 7, H, 512), 5.0, dtype=torch.bfloat16, device="cuda")
+        q_c2, q_r2 = torch.zeros((T + 7, H, 512), dtype=torch.bfloat16, device="cuda"), torch.zeros((T + 7, H, E), dtype=torch.bfloat16, device="cuda")
+        q_c2[5:5 + T], q_r2[5:5 + T] = q_c, q_r
+        wg.latent_attend(q_c2, q_r2, c_cache, r_cache, None, table, lens_t, starts + 5, 0.07, moved, work)
+        assert (moved[:5] == 5).all() and (moved[5 + T:] == 5).all()
+        at = 0
+        for row, n in enumerate(counts):
+            i = torch.arange(lens[row], device="cuda")
+            slots = table[row].long()[i // 32] * 32 + i % 32
+            seen = lens[row] - n + 1 + torch.arange(n, device="cuda")
+            want, off = attention(torch.cat((q_c[at:at + n], q_r[at:at + n]), -1), torch.cat((v[slots], r[slots]), -1)[:, None], v[slots][:, None], seen, 0.07)
+            assert ((moved[5 + at:5 + at + n].double() - want).abs() <= off).all()
+            at += n
+
+
+def test_prompt_fewer_tokens_and_shifted_rows():
+    g = gen(31)
+    H, D, counts, keys = 4, 128, [200, 30], [900, 31]
+    T, N = sum(counts), sum(keys)
+    q_n, q_r, k_n, k_r, v = bf16(g, T + 4, H, D), bf16(g, T + 4, H, E), bf16(g, N + 3, H, D), bf16(g, N + 3, E), bf16(g, N + 3, H, D)
+    work = torch.empty(1 << 26, dtype=torch.uint8, device="cuda")
+    for few in (T + 4, 150, 201):
+        out = torch.full((few, H, D), 5.0, dtype=torch.bfloat16, device="cuda")
+        wg.latent_prompt(q_n[:few], q_r[:few], k_n, k_r, v, ints([2, 202, 232]), ints([3, 903, 934]), 0.08, out, work)
+        assert (out[:2] == 5).all() and (out[232:] == 5).all()
+        for b, n, kb, m in ((2, 200, 3, 900), (202, 30, 903, 31)):
+            have = max(0, min(n, few - b))
+            if have:
+                seen = m - n + 1 + torch.arange(have, device="cuda")
+                k = torch.cat((k_n[kb:kb + m], k_r[kb:kb + m][:, None].expand(-1, H, -1)), -1)
+                want, off = attention(torch.cat((q_n[b:b + have], q_r[b:b + have]), -1), k, v[kb:kb + m], seen, 0.08)
+                assert ((out[b:b + have].double() - want).abs() <= off).all()
+
+
+def test_prompt_shared_and_broadcast_keys():
+    """Heads that share keys and values (a stride of 0), as one cached head read by many."""
+    g = gen(32)
+    q_n, q_r, k_n, k_r, v = bf16(g, 70, 6, 64), bf16(g, 70, 6, E), bf16(g, 300, 1, 64), bf16(g, 300, E), bf16(g, 300, 1, 64)
+    out = torch.empty((70, 6, 64), dtype=torch.bfloat16, device="cuda")
+    work = torch.empty(1 << 24, dtype=torch.uint8, device="cuda")
+    wg.latent_prompt(q_n, q_r, k_n.expand(-1, 6, -1), k_r, v.expand(-1, 6, -1), ints([0, 70]), ints([0, 300]), 0.1, out, work)
+    want, off = attention(torch.cat((q_n, q_r), -1), torch.cat((k_n, k_r[:, None]), -1).expand(-1, 6, -1), v.expand(-1, 6, -1), 231 + torch.arange(70, device="cuda"), 0.1)
+    assert ((out.double() - want).abs() <= off).all()
+
+
+@pytest.mark.parametrize("bits", [8, 16])
+def test_a_cache_behind_2_to_32_bytes(bits):
+    """Slots whose vectors lie more than 2^32 bytes from the first one's."""
+    P, C, H = 64, 512, 16
+    N = (1 << 32) // (P * C * (1 if bits == 8 else 2)) + 4
+    g = gen(bits)
+    c_cache = torch.empty((N, P, C), dtype=torch.float8_e4m3fn if bits == 8 else torch.bfloat16, device="cuda")
+    r_cache, scale = torch.empty((N, P, E), dtype=torch.bfloat16, device="cuda"), torch.empty((N, P), device="cuda") if bits == 8 else None
+    table = ints([[N - 1, 0, N - 3]])
+    i = torch.arange(170, device="cuda")
+    slots = table[0].long()[i // P] * P + i % P
+    c, r = bf16(g, 170, C), bf16(g, 170, E)
+    wg.latent_append(c, r, slots.to(torch.int32), None, c_cache, r_cache, scale)
+    c_out, r_out = torch.empty_like(c), torch.empty_like(r)
+    wg.latent_read(c_cache, r_cache, scale, table, ints([0, 170]), c_out, r_out)
+    kept = held(c)[0] * held(c)[1][:, None] if bits == 8 else c.double()
+    assert torch.equal(c_out.double(), kept.to(torch.bfloat16).double()) and torch.equal(r_out, r)
+    q_c, q_r, out = bf16(g, 1, H, C), bf16(g, 1, H, E), torch.empty((1, H, C), dtype=torch.bfloat16, device="cuda")
+    work = torch.empty(max(16, wg.latent_attend_workspace(1, 1, H, C, 3, P)), dtype=torch.uint8, device="cuda")
+    wg.latent_attend(q_c, q_r, c_cache, r_cache, scale, table, ints([170]), ints([0, 1]), 0.06, out, work)
+    want, off = attention(torch.cat((q_c, q_r), -1), torch.cat((kept, r.double()), -1)[:, None], kept[:, None], torch.tensor([170], device="cuda"), 0.06)
+    assert ((out.double() - want).abs() <= off).all()
+
+
 # ---- together -------------------------------------------------------------------------------------
 
 def test_calls_on_another_stream_and_in_graphs():
