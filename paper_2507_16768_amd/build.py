@@ -56,15 +56,26 @@ def build_native(verbose=False):
 
 
 def build(verbose=False):
+    """Each source by itself, several at a time, then linked."""
+    import concurrent.futures
+    import tempfile
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
-    tmp = LIB + ".%d.tmp" % os.getpid()
-    cmd = [hipcc] + FLAGS + ["-o", tmp] + [os.path.join(CSRC, f) for f in SOURCES]
-    if verbose:
-        print(" ".join(cmd))
-    r = subprocess.run(cmd, capture_output=True, text=True)
-    if r.returncode != 0:
-        raise RuntimeError("hipcc failed:\n" + r.stdout + r.stderr)
-    os.replace(tmp, LIB)
+
+    def run(cmd):
+        if verbose:
+            print(" ".join(cmd))
+        r = subprocess.run(cmd, capture_output=True, text=True)
+        if r.returncode != 0:
+            raise RuntimeError("hipcc failed:\n" + r.stdout + r.stderr)
+
+    with tempfile.TemporaryDirectory(dir=HERE, prefix=".objects.") as objects:
+        made = [os.path.join(objects, f + ".o") for f in SOURCES]
+        compile_flags = [f for f in FLAGS if f != "-shared" and not f.startswith("-Wl,")]
+        with concurrent.futures.ThreadPoolExecutor(max_workers=min(8, os.cpu_count() or 1)) as pool:
+            list(pool.map(lambda p: run([hipcc] + compile_flags + ["-c", os.path.join(CSRC, p[0]), "-o", p[1]]), zip(SOURCES, made)))
+        tmp = LIB + ".%d.tmp" % os.getpid()
+        run([hipcc] + FLAGS + ["-o", tmp] + made)
+        os.replace(tmp, LIB)
     build_native(verbose)
     return LIB
 
