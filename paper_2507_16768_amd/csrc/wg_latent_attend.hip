@@ -19,6 +19,7 @@
 namespace wg {
 
 typedef short Short4 __attribute__((ext_vector_type(4)));
+typedef float Float16 __attribute__((ext_vector_type(16)));
 typedef uint32_t Word __attribute__((may_alias));
 
 constexpr uint32_t kThreads = 256, kWaves = 4, kTop = 64;
@@ -727,10 +728,9 @@ template <uint32_t kD>
 __global__ void __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2)))
 latent_prompt_kernel(const LatentPromptArgs a)
 {
-    constexpr uint32_t kM = 2u, kSteps = (kD + kTop) / 32u, kParts = kD / 16u, kPitch = kD + kTop + 16u, kGroupPitch = 32u * kPitch + 192u, kValuePitch = kD + 16u, kValueGroup = 32u * kValuePitch + 192u,
-                       kStage = kPromptKeys / kWaves;
+    constexpr uint32_t kSteps = (kD + kTop) / 16u, kParts = kD / 32u, kPitch = kD + kTop + 8u, kValuePitch = kD + 32u, kStage = kPromptKeys / kWaves;
     constexpr uint32_t kPer = 512u / kD, kLoads = kStage / kPer, kTops = kStage / 8u, kAhead = 4u;
-    __shared__ __attribute__((aligned(16))) uint16_t keys[2u * kGroupPitch], values[2u * kValueGroup];            // two blocks: one that is worked on, one that comes
+    __shared__ __attribute__((aligned(16))) uint16_t keys[2u * 32u * kPitch], values[2u * 32u * kValuePitch];           // two blocks: one that is worked on, one that comes
     __shared__ uint32_t odd_from[kD], any_from;       // of each dim, the first key whose value is none, of those that some rows do not see; the first of all
     const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), heads = a.of.heads;
     auto tiles = [&](uint32_t r) { return (tokens_of(a.of, r) + kPromptRows - 1u) / kPromptRows; };
@@ -741,7 +741,7 @@ latent_prompt_kernel(const LatentPromptArgs a)
     if (a.of.chunks ? !chunk_of(a.of, blockIdx.x, [&](uint32_t r) { return tiles(r) * heads * (blocks_at(r) + kTileCost); }, &c) : !tile_of<kPromptRows>(a.of, 1u, blockIdx.x / heads, &t)) return;
     if (!a.of.chunks) (void)tile_at<kPromptRows>(a.of, 1u, t.row, uniform(tiles(t.row)) - 1u - t.first / kPromptRows, &t);             // the last, which see the most keys, first
     while (c.at < c.end && c.row < a.of.rows) {
-        const uint32_t tid = anew(threadIdx.x), lane = tid & 63u, m = lane & 15u, g = lane >> 4;
+        const uint32_t tid = anew(threadIdx.x), lane = tid & 63u, m = lane & 31u, h = lane >> 5;
         uint32_t b0 = 0, n_blocks = 1u, blocks = 1u, chunks = 1u, begin;
         if (a.of.chunks) {
             blocks = uniform(blocks_at(c.row));
@@ -783,9 +783,10 @@ latent_prompt_kernel(const LatentPromptArgs a)
 #pragma unroll
             for (uint32_t i = 0; i < kTops; i++) tops[i] = four(rw, own_top + i * 8u * (uint32_t)a.kr_token * 2u);
         };
-        // (where keys and values lie in LDS: as in latent_attend_kernel)
-        auto row_at = [&](uint32_t key) { return key * kPitch + key / 8u * 64u; };
-        auto value_at = [&](uint32_t key) { return key * kValuePitch + key / 8u * 64u; };
+        // Rows of keys take a sixteenth of 256 bytes more than whole eighths of that, rows of values four, so that what LDS serves in a cycle lies in different ones: of the first product rows 4 q .. 4 q + 3
+        // for q of 0, 3, 5, 6 or 1, 2, 4, 7, of the second 64 bytes each of four neighbouring rows.
+        auto row_at = [&](uint32_t key) { return key * kPitch; };
+        auto value_at = [&](uint32_t key) { return key * kValuePitch; };
         auto stage = [&](uint32_t block, uint32_t turn) {
             const bool partly = block + kPromptKeys > seen_least;
 #pragma unroll
@@ -795,97 +796,104 @@ latent_prompt_kernel(const LatentPromptArgs a)
                     atomicMin(&any_from, block + key);
                     raw_v[i] = without_odd_dims(raw_v[i], block + key, d, odd_from);
                 }
-                *reinterpret_cast<Word4 *>(keys + turn * kGroupPitch + row_at(key) + d) = raw[i];
-                *reinterpret_cast<Word4 *>(values + turn * kValueGroup + value_at(key) + d) = raw_v[i];
+                *reinterpret_cast<Word4 *>(keys + turn * 32u * kPitch + row_at(key) + d) = raw[i];
+                *reinterpret_cast<Word4 *>(values + turn * 32u * kValuePitch + value_at(key) + d) = raw_v[i];
             }
 #pragma unroll
-            for (uint32_t i = 0; i < kTops; i++) *reinterpret_cast<Word4 *>(keys + turn * kGroupPitch + row_at(wave * kStage + i * 8u + lane / 8u) + kD + lane % 8u * 8u) = tops[i];
+            for (uint32_t i = 0; i < kTops; i++) *reinterpret_cast<Word4 *>(keys + turn * 32u * kPitch + row_at(wave * kStage + i * 8u + lane / 8u) + kD + lane % 8u * 8u) = tops[i];
         };
         if (from < to) fetch(from);
-        Half8 q[kM][kSteps];
-        uint32_t sees[kM];
+        const uint32_t own = wave * 32u + m, i0 = t.first + own, i = i0 < t.last ? i0 : t.last - 1u;
+        Half8 q[kSteps];
+        {
+            const uint16_t *qn = a.q_n + (int64_t)(t.begin + i) * a.qn_token + (int64_t)head_now * a.qn_head + h * 8u, *qr = a.q_r + (int64_t)(t.begin + i) * a.qr_token + (int64_t)head_now * a.qr_head + h * 8u;
 #pragma unroll
-        for (uint32_t n = 0; n < kM; n++) {
-            const uint32_t i0 = t.first + (wave * kM + n) * 16u + m, i = i0 < t.last ? i0 : t.last - 1u, token = t.begin + i;
-            const uint16_t *qn = a.q_n + (int64_t)token * a.qn_token + (int64_t)head * a.qn_head + g * 8u, *qr = a.q_r + (int64_t)token * a.qr_token + (int64_t)head * a.qr_head + g * 8u;
-#pragma unroll
-            for (uint32_t s = 0; s < kSteps; s++) {
-                q[n][s] = signed_query(*reinterpret_cast<const Half8 *>(s < kD / 32u ? qn + s * 32u : qr + (s - kD / 32u) * 32u), a.factor);
-            }
-            const uint32_t all = seen_by(i);
-            sees[n] = all < to ? all : to;
+            for (uint32_t s = 0; s < kSteps; s++) q[s] = signed_query(*reinterpret_cast<const Half8 *>(s < kD / 16u ? qn + s * 16u : qr + (s - kD / 16u) * 16u), a.factor);
         }
-        Sums<kM, kParts> sums;
-        sums.clear();
+        const uint32_t all = seen_by(i), sees = all < to ? all : to;
+        Float16 acc[kParts];
+        float base = -__builtin_inff(), sum = 0.f;
+#pragma unroll
+        for (uint32_t d = 0; d < kParts; d++)
+#pragma unroll
+            for (uint32_t e = 0; e < 16u; e++) acc[d][e] = 0.f;
         if (tid < kD) odd_from[tid] = kNone;
         if (tid == 0u) any_from = kNone;
         __syncthreads();
         if (from < to) stage(from, 0u);
         __builtin_amdgcn_s_waitcnt(0x0F70);                                // (as in latent_attend_kernel)
         if (from + kPromptKeys < to) fetch(from + kPromptKeys);
+        const float factor = size_of(a.factor);
         uint32_t turn = 0;
         for (uint32_t block = from; block < to; block += kPromptKeys, turn ^= 1u) {
             __syncthreads();
-            Float4 score[2][kM];
+            // row r of the first product's tile is key 16 (r / 16) + 8 (r / 4 % 2) + 4 (r / 8 % 2) + r % 4: the lane then has the scores of keys 8 h .. 8 h + 7 of each sixteen
+            const uint16_t *row = keys + turn * 32u * kPitch + row_at(m / 16u * 16u + m / 4u % 2u * 8u + m / 8u % 2u * 4u + m % 4u) + h * 8u;
+            Float16 score;
 #pragma unroll
-            for (uint32_t i = 0; i < 2u * kM; i++) score[i / kM][i % kM] = Float4{0.f, 0.f, 0.f, 0.f};
-            const uint16_t *row = keys + turn * kGroupPitch + row_at(m / 4u * 8u + m % 4u) + g * 8u;
+            for (uint32_t e = 0; e < 16u; e++) score[e] = 0.f;
             Half8 x[2][kAhead];
-            pipelined<2u * kSteps, kAhead>([&](uint32_t i, uint32_t at) { x[at / kAhead][at % kAhead] = *reinterpret_cast<const Half8 *>(row + i % 2u * 4u * kPitch + i / 2u * 32u); },
-                                           [&](uint32_t i, uint32_t at) {
-#pragma unroll
-                                               for (uint32_t n = 0; n < kM; n++)
-                                                   score[i % 2u][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x[at / kAhead][at % kAhead], q[n][i / 2u], score[i % 2u][n], 0, 0, 0);
-                                           });
-            float s[1][kM][8];
-            const uint32_t at = block + g * 8u;
-#pragma unroll
-            for (uint32_t n = 0; n < kM; n++)
-#pragma unroll
-                for (uint32_t j = 0; j < 8u; j++) s[0][n][j] = score[j / 4u][n][j % 4u];
+            pipelined<kSteps, kAhead>([&](uint32_t i, uint32_t at) { x[at / kAhead][at % kAhead] = *reinterpret_cast<const Half8 *>(row + i * 16u); },
+                                      [&](uint32_t i, uint32_t at) { score = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x[at / kAhead][at % kAhead], q[i], score, 0, 0, 0); });
+            const uint32_t at = block + h * 8u;
             if (block + kPromptKeys > seen_least || block + kPromptKeys > to)
 #pragma unroll
-                for (uint32_t n = 0; n < kM; n++)
+                for (uint32_t e = 0; e < 16u; e++) score[e] = at + e / 8u * 16u + e % 8u < sees ? score[e] : -__builtin_inff();
+            float top = score[0];
 #pragma unroll
-                    for (uint32_t j = 0; j < 8u; j++) s[0][n][j] = at + j < sees[n] ? s[0][n][j] : -__builtin_inff();
-            // (the first values are on their way while the scores become weights)
-            const uint16_t *column = values + turn * kValueGroup + value_at(g * 8u + m / 4u) + m % 4u * 4u;
-            auto ask = [&](uint32_t d, uint32_t at) { x[at / kAhead][at % kAhead] = both(column_of(column + d * 16u), column_of(column + 4u * kValuePitch + d * 16u)); };
+            for (uint32_t e = 1; e < 16u; e++) top = __builtin_fmaxf(top, score[e]);
+            top *= factor;
+            if (__ballot(top > base + kLift)) {
+                const auto both_halves = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top), false, false);
+                top = __builtin_fmaxf(base, __builtin_fmaxf(__uint_as_float(both_halves[0]), __uint_as_float(both_halves[1])));
+                const float by = __builtin_amdgcn_exp2f(base - (top > -__builtin_inff() ? top : 0.f));
+                base = top; sum *= by;
 #pragma unroll
-            for (uint32_t d = 0; d < kAhead; d++) ask(d, d);
-            __builtin_amdgcn_sched_barrier(0);
-            Half8 p[1][kM];
-            sums.template weigh<1>(s, size_of(a.factor), p);
+                for (uint32_t d = 0; d < kParts; d++) acc[d] *= by;
+            }
+            const float rel = base > -__builtin_inff() ? base : 0.f;
+            Half8 p[2];
+#pragma unroll
+            for (uint32_t k = 0; k < 2u; k++) {
+                Word4 w;
+#pragma unroll
+                for (uint32_t j = 0; j < 4u; j++) {
+                    const float u = __builtin_amdgcn_exp2f(__builtin_fmaf(score[8u * k + 2u * j], factor, -rel)), v = __builtin_amdgcn_exp2f(__builtin_fmaf(score[8u * k + 2u * j + 1u], factor, -rel));
+                    w[j] = pk_bf16(u, v);
+                    sum += u; sum += v;
+                }
+                p[k] = __builtin_bit_cast(Half8, w);
+            }
             if (block + kPromptKeys < to) {
                 stage(block + kPromptKeys, turn ^ 1u);
                 if (block + 2u * kPromptKeys < to) fetch(block + 2u * kPromptKeys);
             }
-            pipelined<kParts, kAhead, true>(ask,
-                                      [&](uint32_t d, uint32_t at) {
-#pragma unroll
-                                          for (uint32_t n = 0; n < kM; n++)
-                                              sums.acc[d][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x[at / kAhead][at % kAhead], p[0][n], sums.acc[d][n], 0, 0, 0);
-                                      });
+            const uint16_t *column = values + turn * 32u * kValuePitch + value_at(h * 8u + lane % 16u / 4u) + lane / 16u % 2u * 16u + lane % 4u * 4u;
+            pipelined<2u * kParts, kAhead>([&](uint32_t i, uint32_t at) {
+                                               const uint16_t *of = column + i / kParts * 16u * kValuePitch + i % kParts * 32u;
+                                               x[at / kAhead][at % kAhead] = both(column_of(of), column_of(of + 4u * kValuePitch));
+                                           },
+                                           [&](uint32_t i, uint32_t at) { acc[i % kParts] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x[at / kAhead][at % kAhead], p[i / kParts], acc[i % kParts], 0, 0, 0); });
         }
         __syncthreads();
+        sum += __shfl_xor(sum, 32);
+        const bool any = sees > from;
+        const float by = share_of_sum(sum, any && whole);
+        if (i0 < t.last) {
+            const size_t at = (size_t)(t.begin + i0) * heads + head_now, part = (size_t)place * kPromptRows + own;
 #pragma unroll
-        for (uint32_t n = 0; n < kM; n++) {
-            const float sum = sums.whole_sum(n);
-            const uint32_t own = t.first + (wave * kM + n) * 16u + m;
-            const bool any = sees[n] > from;
-            const float by = share_of_sum(sum, any && whole);
-            if (own >= t.last) continue;
-            const size_t at = (size_t)(t.begin + own) * heads + head, part = (size_t)place * kPromptRows + own - t.first;
+            for (uint32_t d = 0; d < kParts; d++)
 #pragma unroll
-            for (uint32_t d = 0; d < kParts; d++) {
-                Float4 v = sums.acc[d][n] * by;
-                if (any_from != kNone)
+                for (uint32_t e = 0; e < 4u; e++) {
+                    const uint32_t dim = d * 32u + e * 8u + h * 4u;
+                    Float4 v{acc[d][4u * e] * by, acc[d][4u * e + 1u] * by, acc[d][4u * e + 2u] * by, acc[d][4u * e + 3u] * by};
+                    if (any_from != kNone)
 #pragma unroll
-                    for (uint32_t e = 0; e < 4u; e++) v[e] = odd_from[d * 16u + g * 4u + e] < sees[n] ? __builtin_nanf("") : v[e];
-                if (whole) *reinterpret_cast<Word2 *>(a.out + at * kD + d * 16u + g * 4u) = Word2{pk_bf16(v[0], v[1]), pk_bf16(v[2], v[3])};
-                else *reinterpret_cast<Float4 *>(a.partial + part * kD + d * 16u + g * 4u) = v;
-            }
-            if (!whole && g == 0u) *reinterpret_cast<Float2 *>(a.ends + part * 2u) = Float2{sums.base[n], any && sum == 0.f ? kEmpty : sum};
+                        for (uint32_t j = 0; j < 4u; j++) v[j] = odd_from[dim + j] < sees ? __builtin_nanf("") : v[j];
+                    if (whole) *reinterpret_cast<Word2 *>(a.out + at * kD + dim) = Word2{pk_bf16(v[0], v[1]), pk_bf16(v[2], v[3])};
+                    else *reinterpret_cast<Float4 *>(a.partial + part * kD + dim) = v;
+                }
+            if (!whole && h == 0u) *reinterpret_cast<Float2 *>(a.ends + part * 2u) = Float2{base, any && sum == 0.f ? kEmpty : sum};
         }
         __syncthreads();
     }
