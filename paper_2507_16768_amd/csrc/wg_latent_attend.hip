@@ -631,12 +631,14 @@ latent_join_kernel(const JoinArgs a)
         for (uint32_t d = 0; d < kOwn; d += 2u) reinterpret_cast<Word *>(out)[d / 2u] = pk_bf16(acc[d], acc[(d + 1u) % kOwn]);
 }
 
-// Whether all work is dealt out, over how many workgroups, and the workspace's parts.  (tiles, blocks: the most there can be)
+// Whether all work is dealt out, over how many workgroups, and the workspace's parts.  (tiles, blocks: the most there can be.)  Tiles of a request's many tokens see more keys the later they come, which the
+// chunks do not know: with twice as many as the chip holds at a time they are left to it; where requests have few tokens, as they decode, all work is dealt out however many there are (256 rows of 1,000 to
+// 4,000 tokens, 128 heads, a tile each: 541 us left to the chip, 307 dealt out).
 struct Plan { uint32_t chunks; uint64_t partial, ends, parts; };
-static Plan plan_of(uint64_t tiles, uint64_t blocks, uint32_t rows, uint32_t tile_rows, uint32_t dim, uint32_t slots, uint64_t outputs)
+static Plan plan_of(uint64_t tiles, uint64_t blocks, uint32_t rows, bool few, uint32_t tile_rows, uint32_t dim, uint32_t slots, uint64_t outputs)
 {
     Plan p{0u, 0u, 0u, 0u};
-    if (rows > 1024u || blocks < 2u || tiles >= 2u * slots || tiles * (blocks + kTileCost) > 0x7FFFFFFFull) return p;
+    if (rows > 1024u || blocks < 2u || (tiles >= 2u * slots && !few) || tiles * (blocks + kTileCost) > 0x7FFFFFFFull) return p;
     const uint64_t most = (tiles * (blocks + kTileCost) + kAttendLeast - 1u) / kAttendLeast;
     p.chunks = (uint32_t)(most < slots ? most : slots);
     p.partial = (uint64_t)p.chunks * 2u * tile_rows * dim;
@@ -644,7 +646,7 @@ static Plan plan_of(uint64_t tiles, uint64_t blocks, uint32_t rows, uint32_t til
     p.parts = outputs * 2u;
     return p;
 }
-uint64_t plan_bytes(const Plan &p) { return (p.partial + p.ends + p.parts) * 4u; }
+static uint64_t plan_bytes(const Plan &p) { return (p.partial + p.ends + p.parts) * 4u; }
 
 template <uint32_t kD>
 static hipError_t launch_join(const JoinArgs &j, uint32_t tokens, bool many, hipStream_t s)
@@ -669,7 +671,7 @@ bool latent_attend_fits(uint32_t tokens, uint32_t rows, uint32_t heads)
 static Plan attend_plan(uint32_t tokens, uint32_t rows, uint32_t heads, uint32_t latent, uint32_t columns, uint32_t shift)
 {
     const uint64_t blocks = (((uint64_t)columns << shift) + kAttendBlock - 1u) / kAttendBlock;
-    return plan_of(attend_tiles(tokens, rows, heads), blocks, rows, attend_rows(tokens, rows, heads), latent, kAttendSlots, (uint64_t)tokens * heads);
+    return plan_of(attend_tiles(tokens, rows, heads), blocks, rows, tokens <= 16u * rows, attend_rows(tokens, rows, heads), latent, kAttendSlots, (uint64_t)tokens * heads);
 }
 uint64_t latent_attend_bytes(uint32_t tokens, uint32_t rows, uint32_t heads, uint32_t latent, uint32_t columns, uint32_t shift)
 {
@@ -905,7 +907,7 @@ static uint64_t prompt_tiles(uint32_t tokens, uint32_t rows, uint32_t heads) { r
 static Plan prompt_plan(uint32_t tokens, uint32_t rows, uint32_t heads, uint32_t dim, uint32_t keys)
 {
     const uint64_t tiles = prompt_tiles(tokens, rows, heads), blocks = ((uint64_t)keys + kAttendBlock - 1u) / kAttendBlock;
-    return plan_of(tiles, blocks, rows, kPromptRows, dim, kPromptSlots, (uint64_t)tokens * heads);
+    return plan_of(tiles, blocks, rows, tokens <= kPromptRows * rows, kPromptRows, dim, kPromptSlots, (uint64_t)tokens * heads);
 }
 uint64_t latent_prompt_bytes(uint32_t tokens, uint32_t rows, uint32_t heads, uint32_t dim, uint32_t keys) { return plan_bytes(prompt_plan(tokens, rows, heads, dim, keys)); }
 

@@ -374,6 +374,14 @@ def test_attend_more_rows_than_have_their_keys_cut():
 
 
 @pytest.mark.parametrize("bits", [8, 16])
+@pytest.mark.parametrize("R,H,n", [(600, 16, 400), (520, 128, 300), (300, 48, 1400), (1024, 2, 150)])
+def test_attend_many_rows_of_few_tokens(bits, R, H, n):
+    """More tiles than the chip holds at a time, and rows of no tokens and of none cached among them."""
+    lens = [r * 7919 % n if r % 11 else 0 for r in range(R)]
+    run_attend(gen(R), lens, [(1, 1, 0, 2, 1)[r % 5] for r in range(R)], H, 512, bits, 64, columns=50)
+
+
+@pytest.mark.parametrize("bits", [8, 16])
 def test_attend_large_scores_and_scales(bits):
     """Scores in the hundreds, so that one key has all the weight, and vectors whose sizes differ by 2^12."""
     run_attend(gen(4), [300, 1000, 77], [1, 2, 3], 16, 512, bits, 32, factor=1.0)
@@ -442,6 +450,13 @@ def check_prompt(g, counts, keys, H, D, extra=0, factor=0.08, spoil=None):
     (1, [1000], [1000]), (5, [3, 600, 64], [1000, 601, 64]), (32, [200] * 6, [200] * 6), (2, [1] * 70, list(range(70)))])
 def test_prompt(D, H, counts, keys):
     for _ in check_prompt(gen(H + D), counts, keys, H, D, extra=2):
+        pass
+
+
+@pytest.mark.parametrize("H,R", [(16, 100), (4, 500), (2, 1030)])
+def test_prompt_many_rows_of_few_tokens(H, R):
+    counts = [(1, 4, 0, 7)[r % 4] for r in range(R)]
+    for _ in check_prompt(gen(H), counts, [r * 31 % 290 for r in range(R)], H, 128, extra=1):
         pass
 
 
