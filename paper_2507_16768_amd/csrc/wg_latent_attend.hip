@@ -312,7 +312,7 @@ latent_attend_kernel(const LatentAttendArgs a)
     constexpr uint32_t kSteps = (kC + kTop) / 32u, kParts = kC / 16u / kCols, kPitch = kC + kTop + 16u, kGroupPitch = 32u * kPitch + 192u;
     constexpr uint32_t kRow = kC * (kBytes ? 1u : 2u), kPer = 1024u / kRow, kStage = kKeys / kW;          // bytes of a vector; keys of a wavefront's load; keys that it brings
     constexpr uint32_t kLoads = kStage / kPer, kTops = (kStage + 7u) / 8u, kAhead = kC == 512u && kGroups == 8u ? 2u : 4u, kPut = kC == 512u && kGroups == 8u ? 10u : 0u, kKept = kSteps - kPut;
-    constexpr uint32_t kJoinPitch = kC + 4u, kTile = kKeyGroups * kGroupPitch, kTileBytes = kTile * 2u, kJoinBytes = kKeyGroups > 1u ? kKeyGroups * kRows * kJoinPitch * 4u : 0u;
+    constexpr uint32_t kJoinPitch = kC + 4u, kTile = kKeyGroups * kGroupPitch, kTileBytes = kTile * 2u, kJoinBytes = kKeyGroups > 1u ? kKeyGroups * kRows * kJoinPitch * 4u : kW * 16u * 132u * 4u;
     constexpr bool kHalves = kCols > 1u;                                   // two wavefronts that take the same rows and keys make half of the scores each
     __shared__ __attribute__((aligned(16))) uint8_t room[2u * kTileBytes > kJoinBytes ? 2u * kTileBytes : kJoinBytes];   // two blocks of keys: one that is worked on, one that comes
     __shared__ uint32_t odd_from;                                          // the first key with a number that is none, of those that some rows do not see
@@ -500,10 +500,21 @@ latent_attend_kernel(const LatentAttendArgs a)
             const uint32_t i = group * 16u + m;
             float by;
             const Float2 ends = finish(i, sums.base[0], sum, &by);
-            if (row_first + i < t.last) {
+            if (row_first + i < t.last && !whole && g == 0u && column_group == 0u) *reinterpret_cast<Float2 *>(a.ends + ((size_t)place * kRows + i) * 2u) = ends;
+            // Through LDS, 128 dims of the wavefront's 16 rows at a time, so that it stores 512 bytes beside each other.
+            float *turned = reinterpret_cast<float *>(room) + wave * (16u * 132u);
 #pragma unroll
-                for (uint32_t d = 0; d < kParts; d++) put(i, column_group * (kC / kCols) + d * 16u + g * 4u, sums.acc[d][0] * by);
-                if (!whole && g == 0u && column_group == 0u) *reinterpret_cast<Float2 *>(a.ends + ((size_t)place * kRows + i) * 2u) = ends;
+            for (uint32_t d0 = 0; d0 < kC / kCols; d0 += 128u) {
+#pragma unroll
+                for (uint32_t d = 0; d < 8u; d++) *reinterpret_cast<Float4 *>(turned + m * 132u + d * 16u + g * 4u) = sums.acc[d0 / 16u + d][0] * by;
+                __builtin_amdgcn_wave_barrier();
+#pragma unroll
+                for (uint32_t k = 0; k < 8u; k++) {
+                    const uint32_t row = k * 2u + lane / 32u;
+                    const Float4 v = *reinterpret_cast<const Float4 *>(turned + row * 132u + lane % 32u * 4u);
+                    if (row_first + group * 16u + row < t.last) put(group * 16u + row, column_group * (kC / kCols) + d0 + lane % 32u * 4u, v);
+                }
+                __builtin_amdgcn_wave_barrier();
             }
             __syncthreads();
             continue;
@@ -633,12 +644,13 @@ latent_join_kernel(const JoinArgs a)
 
 // Whether all work is dealt out, over how many workgroups, and the workspace's parts.  (tiles, blocks: the most there can be.)  Tiles of a request's many tokens see more keys the later they come, which the
 // chunks do not know: with twice as many as the chip holds at a time they are left to it; where requests have few tokens, as they decode, all work is dealt out however many there are (256 rows of 1,000 to
-// 4,000 tokens, 128 heads, a tile each: 541 us left to the chip, 307 dealt out).
+// 4,000 tokens, 128 heads, a tile each: 541 us left to the chip, 307 dealt out).  Below three blocks of keys a tile is a workgroup's: joining it would cost more than it saves (one token of a row of 200, 16
+// heads: 17.3 us dealt out, 16.2 by one; a prompt of 200, 8 heads: 15.3 and 12.0; with three blocks 16.3 and 18.0).
 struct Plan { uint32_t chunks; uint64_t partial, ends, parts; };
 static Plan plan_of(uint64_t tiles, uint64_t blocks, uint32_t rows, bool few, uint32_t tile_rows, uint32_t dim, uint32_t slots, uint64_t outputs)
 {
     Plan p{0u, 0u, 0u, 0u};
-    if (rows > 1024u || blocks < 2u || (tiles >= 2u * slots && !few) || tiles * (blocks + kTileCost) > 0x7FFFFFFFull) return p;
+    if (rows > 1024u || blocks < 3u || (tiles >= 2u * slots && !few) || tiles * (blocks + kTileCost) > 0x7FFFFFFFull) return p;
     const uint64_t most = (tiles * (blocks + kTileCost) + kAttendLeast - 1u) / kAttendLeast;
     p.chunks = (uint32_t)(most < slots ? most : slots);
     p.partial = (uint64_t)p.chunks * 2u * tile_rows * dim;
@@ -732,7 +744,9 @@ latent_prompt_kernel(const LatentPromptArgs a)
 {
     constexpr uint32_t kSteps = (kD + kTop) / 16u, kParts = kD / 32u, kPitch = kD + kTop + 8u, kValuePitch = kD + 32u, kStage = kPromptKeys / kWaves;
     constexpr uint32_t kPer = 512u / kD, kLoads = kStage / kPer, kTops = kStage / 8u, kAhead = 4u;
-    __shared__ __attribute__((aligned(16))) uint16_t keys[2u * 32u * kPitch], values[2u * 32u * kValuePitch];           // two blocks: one that is worked on, one that comes
+    constexpr uint32_t kBlocks = 2u * 32u * (kPitch + kValuePitch) * 2u, kTurned = 32u * 68u;
+    __shared__ __attribute__((aligned(16))) uint8_t room[kBlocks > kWaves * kTurned * 4u ? kBlocks : kWaves * kTurned * 4u];   // two blocks of keys and values: one that is worked on, one that comes
+    uint16_t *keys = reinterpret_cast<uint16_t *>(room), *values = keys + 2u * 32u * kPitch;
     __shared__ uint32_t odd_from[kD], any_from;       // of each dim, the first key whose value is none, of those that some rows do not see; the first of all
     const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), heads = a.of.heads;
     auto tiles = [&](uint32_t r) { return (tokens_of(a.of, r) + kPromptRows - 1u) / kPromptRows; };
@@ -881,21 +895,30 @@ latent_prompt_kernel(const LatentPromptArgs a)
         sum += __shfl_xor(sum, 32);
         const bool any = sees > from;
         const float by = share_of_sum(sum, any && whole);
-        if (i0 < t.last) {
-            const size_t at = (size_t)(t.begin + i0) * heads + head_now, part = (size_t)place * kPromptRows + own;
+        if (i0 < t.last && !whole && h == 0u) *reinterpret_cast<Float2 *>(a.ends + ((size_t)place * kPromptRows + own) * 2u) = Float2{base, any && sum == 0.f ? kEmpty : sum};
+        // through LDS (as in latent_attend_kernel), 64 dims of the wavefront's 32 rows at a time
+        float *turned = reinterpret_cast<float *>(room) + wave * kTurned;
 #pragma unroll
-            for (uint32_t d = 0; d < kParts; d++)
+        for (uint32_t d0 = 0; d0 < kD; d0 += 64u) {
 #pragma unroll
-                for (uint32_t e = 0; e < 4u; e++) {
-                    const uint32_t dim = d * 32u + e * 8u + h * 4u;
-                    Float4 v{acc[d][4u * e] * by, acc[d][4u * e + 1u] * by, acc[d][4u * e + 2u] * by, acc[d][4u * e + 3u] * by};
-                    if (any_from != kNone)
+            for (uint32_t d = 0; d < 64u; d += 8u) {
+                const uint32_t dim = d0 + d + h * 4u, of = (d0 + d) / 32u, e = d / 8u % 4u;
+                Float4 v{acc[of][4u * e] * by, acc[of][4u * e + 1u] * by, acc[of][4u * e + 2u] * by, acc[of][4u * e + 3u] * by};
+                if (any_from != kNone)
 #pragma unroll
-                        for (uint32_t j = 0; j < 4u; j++) v[j] = odd_from[dim + j] < sees ? __builtin_nanf("") : v[j];
-                    if (whole) *reinterpret_cast<Word2 *>(a.out + at * kD + dim) = Word2{pk_bf16(v[0], v[1]), pk_bf16(v[2], v[3])};
-                    else *reinterpret_cast<Float4 *>(a.partial + part * kD + dim) = v;
-                }
-            if (!whole && h == 0u) *reinterpret_cast<Float2 *>(a.ends + part * 2u) = Float2{base, any && sum == 0.f ? kEmpty : sum};
+                    for (uint32_t j = 0; j < 4u; j++) v[j] = odd_from[dim + j] < sees ? __builtin_nanf("") : v[j];
+                *reinterpret_cast<Float4 *>(turned + m * 68u + d + h * 4u) = v;
+            }
+            __builtin_amdgcn_wave_barrier();
+#pragma unroll
+            for (uint32_t k = 0; k < 8u; k++) {
+                const uint32_t i = k * 4u + lane / 16u, dim = d0 + lane % 16u * 4u;
+                const Float4 v = *reinterpret_cast<const Float4 *>(turned + i * 68u + lane % 16u * 4u);
+                if (t.first + wave * 32u + i >= t.last) continue;
+                if (whole) *reinterpret_cast<Word2 *>(a.out + ((size_t)(t.begin + t.first + wave * 32u + i) * heads + head_now) * kD + dim) = Word2{pk_bf16(v[0], v[1]), pk_bf16(v[2], v[3])};
+                else *reinterpret_cast<Float4 *>(a.partial + ((size_t)place * kPromptRows + wave * 32u + i) * kD + dim) = v;
+            }
+            __builtin_amdgcn_wave_barrier();
         }
         __syncthreads();
     }
