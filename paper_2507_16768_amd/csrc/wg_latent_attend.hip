@@ -175,6 +175,17 @@ template <typename T> __device__ __forceinline__ T from_memory(const void *p) { 
 // x, which the compiler is not to know anything about.
 __device__ __forceinline__ uint32_t anew(uint32_t x) { asm volatile("" : "+v"(x)); return x; }
 
+// x of lane first + which, `which` below kN.  (Without LDS, in which a shuffle waits for the keys that have been written there:
+// three rows' 200 tokens behind 1,500 in bfloat16, 24 heads, 43.2 us for 44.7.  Of 8-bit vectors, whose keys come two to a load, shuffles are the faster: 64 rows' 4 drafts, 16 heads, 89 us for 105.)
+template <uint32_t kN>
+__device__ __forceinline__ uint32_t of_groups(uint32_t x, uint32_t first, uint32_t which)
+{
+    uint32_t y = __builtin_amdgcn_readlane(x, first);
+#pragma unroll
+    for (uint32_t i = 1; i < kN; i++) { const uint32_t z = __builtin_amdgcn_readlane(x, first + i); y = which >= i ? z : y; }
+    return y;
+}
+
 // What is read in the place of a key that there is none of.
 __device__ __attribute__((aligned(16))) const uint8_t kZeros[1024] = {};
 
@@ -361,18 +372,18 @@ latent_attend_kernel(const LatentAttendArgs a)
             return lane < kStage && at < to && page < a.pages ? page << a.shift | (at & (P - 1u)) : kNone;
         };
         Word4 raw[kLoads], tops[kTops];
-        float scales[kBytes ? kLoads : 1u];
+        float scales = 0.f;                                                // lane i: of the i-th key
         auto fetch = [&](uint32_t slots) {
+            if (kBytes) scales = from_memory<float>(slots != kNone ? static_cast<const void *>(a.scale + slots) : kZeros);
 #pragma unroll
             for (uint32_t i = 0; i < kLoads; i++) {
-                const uint32_t slot = kPer == 1u ? __builtin_amdgcn_readlane(slots, i) : __shfl(slots, i * kPer + lane / (64u / kPer));
+                const uint32_t slot = kBytes && kPer > 1u ? (uint32_t)__shfl(slots, i * kPer + lane / (64u / kPer)) : of_groups<kPer>(slots, i * kPer, lane / (64u / kPer));
                 const uint8_t *row = slot != kNone ? a.c_cache + (size_t)slot * kRow : kZeros;
                 raw[i] = from_memory<Word4>(row + lane % (64u / kPer) * 16u);
-                if (kBytes) scales[i % (kBytes ? kLoads : 1u)] = from_memory<float>(slot != kNone ? static_cast<const void *>(a.scale + slot) : kZeros);
             }
 #pragma unroll
             for (uint32_t i = 0; i < kTops; i++) {
-                const uint32_t slot = __shfl(slots, i * 8u + lane / 8u);
+                const uint32_t slot = kBytes ? (uint32_t)__shfl(slots, i * 8u + lane / 8u) : of_groups<kStage < 8u ? kStage : 8u>(slots, i * 8u, lane / 8u);
                 tops[i] = from_memory<Word4>((slot != kNone ? reinterpret_cast<const uint8_t *>(a.r_cache) + (size_t)slot * (kTop * 2u) : kZeros) + lane % 8u * 16u);
             }
         };
@@ -386,7 +397,7 @@ latent_attend_kernel(const LatentAttendArgs a)
             for (uint32_t i = 0; i < kLoads; i++) {
                 const uint32_t key = wave * kStage + i * kPer + lane / (64u / kPer), at = lane % (64u / kPer);
                 if (kBytes) {
-                    const float scale = scales[i % (kBytes ? kLoads : 1u)];
+                    const float scale = __shfl(scales, i * kPer + lane / (64u / kPer));
                     const Word2 w0 = wider(raw[i][0], scale), w1 = wider(raw[i][1], scale), w2 = wider(raw[i][2], scale), w3 = wider(raw[i][3], scale);
                     Word4 x{w0[0], w0[1], w1[0], w1[1]}, y{w2[0], w2[1], w3[0], w3[1]};
                     if (partly) { x = without_odd(x, block + key, &odd_from); y = without_odd(y, block + key, &odd_from); }
