@@ -191,13 +191,12 @@ __device__ __attribute__((aligned(16))) const uint8_t kZeros[1024] = {};
 
 // kN operands out of LDS, load(i, place), each for products, use(i, place): kAhead of them are asked for before the kAhead in front of them are used.  (Left to itself the compiler asks for one,
 // waits, and uses it.)
-template <uint32_t kN, uint32_t kAhead, bool kBegun = false, typename L, typename U>
-__device__ __forceinline__ void pipelined(L load, U use)                   // kBegun: the first kAhead have been asked for
+template <uint32_t kN, uint32_t kAhead, typename L, typename U>
+__device__ __forceinline__ void pipelined(L load, U use)
 {
     constexpr uint32_t kRounds = (kN + kAhead - 1u) / kAhead;
-    if (!kBegun)
 #pragma unroll
-        for (uint32_t i = 0; i < kAhead && i < kN; i++) load(i, i);
+    for (uint32_t i = 0; i < kAhead && i < kN; i++) load(i, i);
 #pragma unroll
     for (uint32_t b = 0; b < kRounds; b++) {
 #pragma unroll
@@ -231,57 +230,45 @@ __device__ __forceinline__ float most_of_rows(float x)
     return __builtin_fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
 }
 
-// What a wavefront holds of its kM tiles of 16 queries: of query m of each, the base and its own part of the sum, and outputs, dims 4 g .. 4 g + 3 of each of kParts.
-template <uint32_t kM, uint32_t kParts>
+// What a wavefront holds of its 16 queries: of query m, the base and its own part of the sum, and outputs, dims 4 g .. 4 g + 3 of each of kParts.
+template <uint32_t kParts>
 struct Sums {
-    Float4 acc[kParts][kM];
-    float base[kM], sum[kM];
+    Float4 acc[kParts];
+    float base, sum;
     __device__ __forceinline__ void clear()
     {
+        base = -__builtin_inff(); sum = 0.f;
 #pragma unroll
-        for (uint32_t t = 0; t < kM; t++) {
-            base[t] = -__builtin_inff(); sum[t] = 0.f;
-#pragma unroll
-            for (uint32_t d = 0; d < kParts; d++) acc[d][t] = Float4{0.f, 0.f, 0.f, 0.f};
-        }
+        for (uint32_t d = 0; d < kParts; d++) acc[d] = Float4{0.f, 0.f, 0.f, 0.f};
     }
-    // Scores (-inf where nothing is seen) of kGroups times 32 keys into weights; factor, above 0, makes them scores in log2.
-    template <uint32_t kGroups>
-    __device__ __forceinline__ void weigh(const float (&s)[kGroups][kM][8], float factor, Half8 (&p)[kGroups][kM])
+    // Scores of eight keys (-inf where nothing is seen) into weights; factor, above 0, makes them scores in log2.
+    __device__ __forceinline__ Half8 weigh(const float (&s)[8], float factor)
     {
+        float n = s[0];
 #pragma unroll
-        for (uint32_t t = 0; t < kM; t++) {
-            float n = s[0][t][0];
+        for (uint32_t j = 0; j < 8u; j++) n = __builtin_fmaxf(n, s[j]);
+        n *= factor;
+        if (__ballot(n > base + kLift)) {
+            n = __builtin_fmaxf(base, most_of_rows(n));
+            const float by = __builtin_amdgcn_exp2f(base - (n > -__builtin_inff() ? n : 0.f));
+            base = n; sum *= by;
 #pragma unroll
-            for (uint32_t k = 0; k < kGroups; k++)
-#pragma unroll
-                for (uint32_t j = 0; j < 8u; j++) n = __builtin_fmaxf(n, s[k][t][j]);
-            n *= factor;
-            if (__ballot(n > base[t] + kLift)) {
-                n = __builtin_fmaxf(base[t], most_of_rows(n));
-                const float by = __builtin_amdgcn_exp2f(base[t] - (n > -__builtin_inff() ? n : 0.f));
-                base[t] = n; sum[t] *= by;
-#pragma unroll
-                for (uint32_t d = 0; d < kParts; d++) acc[d][t] *= by;
-            }
-            const float from = base[t] > -__builtin_inff() ? base[t] : 0.f;
-#pragma unroll
-            for (uint32_t k = 0; k < kGroups; k++) {
-                Word4 w;
-#pragma unroll
-                for (uint32_t j = 0; j < 4u; j++) {
-                    const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(s[k][t][2u * j], factor, -from)), y = __builtin_amdgcn_exp2f(__builtin_fmaf(s[k][t][2u * j + 1u], factor, -from));
-                    w[j] = pk_bf16(x, y);
-                    sum[t] += x; sum[t] += y;
-                }
-                p[k][t] = __builtin_bit_cast(Half8, w);
-            }
+            for (uint32_t d = 0; d < kParts; d++) acc[d] *= by;
         }
+        const float from = base > -__builtin_inff() ? base : 0.f;
+        Word4 w;
+#pragma unroll
+        for (uint32_t j = 0; j < 4u; j++) {
+            const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(s[2u * j], factor, -from)), y = __builtin_amdgcn_exp2f(__builtin_fmaf(s[2u * j + 1u], factor, -from));
+            w[j] = pk_bf16(x, y);
+            sum += x; sum += y;
+        }
+        return __builtin_bit_cast(Half8, w);
     }
     // The queries' sums over all lanes.
-    __device__ __forceinline__ float whole_sum(uint32_t t) const
+    __device__ __forceinline__ float whole_sum() const
     {
-        const float l = sum[t] + __shfl_xor(sum[t], 16);
+        const float l = sum + __shfl_xor(sum, 16);
         return l + __shfl_xor(l, 32);
     }
 };
@@ -439,7 +426,7 @@ latent_attend_kernel(const LatentAttendArgs a)
             const uint32_t all = seen_by(i);
             sees = all < to ? all : to;
         }
-        Sums<1, kParts> sums;
+        Sums<kParts> sums;
         sums.clear();
         if (tid == 0u) odd_from = kNone;
         __syncthreads();
@@ -474,29 +461,28 @@ latent_attend_kernel(const LatentAttendArgs a)
                                                    const Half8 x = i / 2u < kKept ? q[i / 2u % kKept] : rest[at / kAhead][at % kAhead / 2u];
                                                    score[i % 2u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k[at / kAhead][at % kAhead], x, score[i % 2u], 0, 0, 0);
                                                });
-            float s[1][1][8];
+            float s[8];
             const uint32_t at = block + key_group * 32u + g * 8u;
 #pragma unroll
-            for (uint32_t j = 0; j < 8u; j++) s[0][0][j] = score[j / 4u][j % 4u];
+            for (uint32_t j = 0; j < 8u; j++) s[j] = score[j / 4u][j % 4u];
             if (block + kKeys > seen_least || block + kKeys > to)
 #pragma unroll
-                for (uint32_t j = 0; j < 8u; j++) s[0][0][j] = at + j < sees ? s[0][0][j] : -__builtin_inff();
-            Half8 p[1][1];
-            sums.template weigh<1>(s, size_of(a.factor), p);
+                for (uint32_t j = 0; j < 8u; j++) s[j] = at + j < sees ? s[j] : -__builtin_inff();
+            const Half8 p = sums.weigh(s, size_of(a.factor));
             if (block + kKeys < to) {
                 stage(block + kKeys, keys + (turn ^ 1u) * kTile);
                 if (block + 2u * kKeys < to) fetch_next(block + 2u * kKeys);
             }
             const uint16_t *column = mine + row_at(g * 8u + m / 4u) + column_group * (kC / kCols) + m % 4u * 4u;
             pipelined<kParts, kAhead>([&](uint32_t d, uint32_t at) { k[at / kAhead][at % kAhead] = both(column_of(column + d * 16u), column_of(column + 4u * kPitch + d * 16u)); },
-                                      [&](uint32_t d, uint32_t at) { sums.acc[d][0] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k[at / kAhead][at % kAhead], p[0][0], sums.acc[d][0], 0, 0, 0); });
+                                      [&](uint32_t d, uint32_t at) { sums.acc[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k[at / kAhead][at % kAhead], p, sums.acc[d], 0, 0, 0); });
         }
         __syncthreads();
 
         // Out: this part by itself, or the whole.  (Numbers that are none have been left out of the sums of rows that see only some of a block's keys: what a row that sees them makes of them
         // is none.)
         const uint32_t odd = odd_from;
-        const float sum = sums.whole_sum(0);
+        const float sum = sums.whole_sum();
         auto put = [&](uint32_t i, uint32_t d, Float4 v) {                 // dims d .. d + 3 of query row i of the tile
             if (whole) *reinterpret_cast<Word2 *>(a.out + ((size_t)t.begin * heads + row_first + i) * kC + d) = Word2{pk_bf16(v[0], v[1]), pk_bf16(v[2], v[3])};
             else *reinterpret_cast<Float4 *>(a.partial + ((size_t)place * kRows + i) * kC + d) = v;
@@ -510,14 +496,14 @@ latent_attend_kernel(const LatentAttendArgs a)
         if (kKeyGroups == 1u) {
             const uint32_t i = group * 16u + m;
             float by;
-            const Float2 ends = finish(i, sums.base[0], sum, &by);
+            const Float2 ends = finish(i, sums.base, sum, &by);
             if (row_first + i < t.last && !whole && g == 0u && column_group == 0u) *reinterpret_cast<Float2 *>(a.ends + ((size_t)place * kRows + i) * 2u) = ends;
             // Through LDS, 128 dims of the wavefront's 16 rows at a time, so that it stores 512 bytes beside each other.
             float *turned = reinterpret_cast<float *>(room) + wave * (16u * 132u);
 #pragma unroll
             for (uint32_t d0 = 0; d0 < kC / kCols; d0 += 128u) {
 #pragma unroll
-                for (uint32_t d = 0; d < 8u; d++) *reinterpret_cast<Float4 *>(turned + m * 132u + d * 16u + g * 4u) = sums.acc[d0 / 16u + d][0] * by;
+                for (uint32_t d = 0; d < 8u; d++) *reinterpret_cast<Float4 *>(turned + m * 132u + d * 16u + g * 4u) = sums.acc[d0 / 16u + d] * by;
                 __builtin_amdgcn_wave_barrier();
 #pragma unroll
                 for (uint32_t k = 0; k < 8u; k++) {
@@ -533,8 +519,8 @@ latent_attend_kernel(const LatentAttendArgs a)
         float *join = reinterpret_cast<float *>(room);
         const uint32_t own = key_group * kRows + group * 16u + m;
 #pragma unroll
-        for (uint32_t d = 0; d < kParts; d++) *reinterpret_cast<Float4 *>(join + own * kJoinPitch + column_group * (kC / kCols) + d * 16u + g * 4u) = sums.acc[d][0];
-        if (g == 0u && column_group == 0u) { join_base[key_group][group * 16u + m] = sums.base[0]; join_sum[key_group][group * 16u + m] = sum; }
+        for (uint32_t d = 0; d < kParts; d++) *reinterpret_cast<Float4 *>(join + own * kJoinPitch + column_group * (kC / kCols) + d * 16u + g * 4u) = sums.acc[d];
+        if (g == 0u && column_group == 0u) { join_base[key_group][group * 16u + m] = sums.base; join_sum[key_group][group * 16u + m] = sum; }
         __syncthreads();
         // four dims of a row to a thread
         for (uint32_t u = tid; u < kRows * (kC / 4u); u += kW * 64u) {
