@@ -442,7 +442,7 @@ int wg_cache_attend(const void *d_q, uint32_t tokens, uint32_t q_heads, uint32_t
  * behind stay: pair i is numbers i and i + rotated / 2, or, interleaved, 2 i and 2 i + 1.  d_frequencies: rotated / 2 of them, radians a position, fp64 (the angle is taken in 64
  * bits; turning in fp32, rounded once).  d_q [tokens][q_heads][dim] and d_k [tokens][k_heads][dim] (k_heads 0: none, NULL) of `dtype`; strides in elements, any
  * alignment, but 16 bytes at a time where everything lies at multiples of 16.  d_q_out may be d_q, d_k_out may be d_k, with the same strides; else no output is or overlaps an input.
- * 2 <= rotated <= dim <= 1024, rotated even, at most 4096 heads of each.  One kernel.
+ * 2 <= rotated <= dim <= 1024, rotated even, at most 4096 heads of each, tokens < 2^24.  One kernel.
  *
  * wg_rotary_frequencies (host): the frequencies base^(-2 i / rotated) into host_out, for contexts `factor` times as long as the `original` one that a model was trained on: a pair that
  * turns at least `high` times over the original context keeps its frequency, one that turns at most `low` times has it divided by the factor, between them the two are mixed, in
@@ -460,12 +460,12 @@ int wg_rotary_frequencies(double *host_out, uint32_t rotated, double base, doubl
  *
  * wg_latent_append: token t's vector and shared key (bfloat16, strides of tokens in elements, at multiples of 16 bytes) go to slot d_slots[t]; a slot outside [0, pages * page_tokens)
  * takes none; no slot is given twice.  In 8 bits a token's scale is the least power of two, 2^-64 at least, times which 448 reaches the vector's largest finite magnitude; numbers are rounded to
- * nearest, ties to even, infinities become 448 times the scale, NaN stays.  d_origins (may be NULL), as wg_page_step leaves them: where d_origins[t] is a page, the tokens in front of token t's
- * slot in its page come from the same places of that one; no token of the call goes to that page, or in front of token t in its own.  tokens <= 2^29, pages * page_tokens < 2^31.  One kernel.
+ * nearest, ties to even, infinities become 448 times the scale, NaN stays.  (What reads the cache takes scales for powers of two.)  d_origins (may be NULL), as wg_page_step leaves them: where d_origins[t] is a page, the tokens in front of token t's
+ * slot in its page come from the same places of that one; no token of the call goes to that page, or in front of token t in its own.  tokens <= 2^27, pages * page_tokens < 2^31.  One kernel.
  *
  * wg_latent_read: the first d_starts[r + 1] - d_starts[r] cached tokens of row r of d_table, in bfloat16, into rows d_starts[r] .. of d_c_out and d_r_out (strides in elements, at multiples of
  * 16 bytes): what prompts behind a cached prefix expand into keys and values (numbers in 8 bits times their scale, which is exact; above what bfloat16 holds, an infinity).  d_starts does not descend; rows from d_starts[rows] on stay, and so do
- * those in front of d_starts[0].  A token whose page is no page or lies behind the table reads as zeros.  tokens: rows that d_c_out has, < 2^31.  rows <= 65535.  One kernel. */
+ * those in front of d_starts[0].  A token whose page is no page or lies behind the table reads as zeros.  tokens: rows that d_c_out has, <= 2^29.  rows <= 65535.  One kernel. */
 int wg_latent_append(const void *d_c, const void *d_r, uint32_t tokens, uint32_t latent, int64_t c_token_stride, int64_t r_token_stride, const int32_t *d_slots,
                      const int32_t *d_origins, void *d_c_cache, void *d_r_cache, float *d_c_scale, uint32_t pages, uint32_t page_tokens, void *stream);
 int wg_latent_read(const void *d_c_cache, const void *d_r_cache, const float *d_c_scale, uint32_t latent, uint32_t pages, uint32_t page_tokens, const int32_t *d_table,
@@ -479,13 +479,15 @@ int wg_latent_read(const void *d_c_cache, const void *d_r_cache, const float *d_
  * bfloat16 numbers (those in 8 bits times their scale exactly), sums and softmax in fp32; weights are rounded to bfloat16, their sum is taken before.  An infinity or a NaN in a vector that a token sees makes
  * its output NaN, in part or as a whole, and is nothing to a token that does not see it.  A page number of a row's tokens that is none reads as zeros; entries behind them may be anything.
  * d_workspace: wg_latent_attend_workspace(...) bytes (0: may be NULL), 16-byte aligned, overwritten; calls that share it must not overlap.  heads <= 4096, rows <= 65535, pages *
- * page_tokens and columns * page_tokens < 2^31, tokens * heads < 2^31 and no more tokens than one launch holds (tokens * heads / 16 + rows < 2^24).  One or two kernels.
+ * page_tokens and columns * page_tokens < 2^31, tokens * heads < 2^31, and no more than one launch holds: with n, the least of 16, 32, 64 and 128 that tokens * heads / min(rows, tokens) does not exceed, or 128,
+ * tokens * heads / n + rows < 2^23.  One or two kernels.
  *
  * wg_latent_prompt: the same attention with keys and values of every head made beforehand from the vectors (wg_latent_read, then a product), which takes a fraction of the operations where
  * many tokens see the same keys.  d_q_n [tokens][heads][dim] and d_q_r [tokens][heads][64] are the two parts of the queries, d_k_n and d_v [keys][heads][dim] the keys' own part and the values, d_k_r [keys][64] the shared part; bfloat16, strides in
  * elements at multiples of 16 bytes, keys and values less than 2^24 elements from one token to the next; dim is 64 or 128.  Row r has the queries d_starts[r] .. d_starts[r + 1] and the keys d_key_starts[r] .. d_key_starts[r + 1], its queries being the last of them: query i of n sees
  * the first m - n + i + 1 of its m keys (none: zeros); tokens from d_starts[rows] on belong to no row, and their outputs stay.  d_out bfloat16 [tokens][heads][dim] without gaps.  Rounding as above; an infinity or a NaN in a value that a
- * token sees makes that output infinite or NaN and is nothing to a token that does not see it.  Both starts do not descend.  heads <= 4096, rows <= 65535, tokens and keys < 2^31, tokens * heads < 2^31.  One or two kernels. */
+ * token sees makes that output infinite or NaN and is nothing to a token that does not see it.  Both starts do not descend.  d_workspace: wg_latent_prompt_workspace(...) bytes,
+ * as above.  heads <= 4096, rows <= 65535, tokens and keys < 2^31, tokens * heads < 2^31, (tokens / 128 + rows) * heads < 2^24.  One or two kernels. */
 uint64_t wg_latent_attend_workspace(uint32_t tokens, uint32_t rows, uint32_t heads, uint32_t latent, uint32_t columns, uint32_t page_tokens);
 int wg_latent_attend(const void *d_q_c, const void *d_q_r, uint32_t tokens, uint32_t heads, uint32_t latent, int64_t c_token_stride, int64_t c_head_stride, int64_t r_token_stride,
                      int64_t r_head_stride, const void *d_c_cache, const void *d_r_cache, const float *d_c_scale, uint32_t pages, uint32_t page_tokens, const int32_t *d_table, uint32_t rows,

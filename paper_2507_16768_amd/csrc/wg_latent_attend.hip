@@ -343,7 +343,7 @@ latent_attend_kernel(const LatentAttendArgs a)
         const uint32_t place = 2u * blockIdx.x + (b0 ? 0u : 1u), row_first = t.first;
         if (a.of.chunks && b0 == 0u && tid < kRows && t.first + tid < t.last)
             a.parts[(size_t)t.begin * heads + t.first + tid] = Parts{blockIdx.x | tid << 16, chunks};
-        auto seen_by = [&](uint32_t i) { const int32_t k = t.before + (int32_t)(i / heads) + 1; return k < 0 ? 0u : (uint32_t)k; };
+        auto seen_by = [&](uint32_t i) { const int32_t k = t.before + (int32_t)(i / heads) + 1; return k < 0 ? 0u : (uint32_t)k < len ? (uint32_t)k : len; };
         const uint32_t seen_least = seen_by(t.first), seen_most = seen_by(t.last - 1u);
         const uint32_t from = b0 * kAttendBlock, to0 = whole ? seen_most : from + n * kAttendBlock, to = to0 < seen_most ? to0 : seen_most;
 
@@ -771,7 +771,7 @@ latent_prompt_kernel(const LatentPromptArgs a)
         const uint32_t place = 2u * blockIdx.x + (b0 ? 0u : 1u);
         if (a.of.chunks && b0 == 0u && tid < kPromptRows && t.first + tid < t.last)
             a.parts[(size_t)(t.begin + t.first + tid) * heads + head] = Parts{blockIdx.x | tid << 16, chunks};
-        auto seen_by = [&](uint32_t i) { const int32_t k = t.before + (int32_t)i + 1; return k < 0 ? 0u : (uint32_t)k; };
+        auto seen_by = [&](uint32_t i) { const int32_t k = t.before + (int32_t)i + 1; return k < 0 ? 0u : (uint32_t)k < len ? (uint32_t)k : len; };
         const uint32_t seen_least = seen_by(t.first), seen_most = seen_by(t.last - 1u);
         const uint32_t from = b0 * kAttendBlock, to0 = whole ? seen_most : from + n_blocks * kAttendBlock, to = to0 < seen_most ? to0 : seen_most;
 

@@ -164,8 +164,9 @@ int wg_rotate(const void *d_q, const void *d_k, wg_dtype_t dtype, uint32_t token
         WG_WANT(d_q && d_positions && d_frequencies && d_q_out && (!k_heads || (d_k && d_k_out)), "null argument");
         WG_WANT(tokens && q_heads, "no tokens or heads");
         WG_WANT(dtype == WG_F32 || dtype == WG_BF16, "unknown dtype");
-        WG_WANT(tokens <= 0x7FFFFFFFu && q_heads <= 4096u && k_heads <= 4096u, "tokens above 2^31 - 1 or heads above 4096");
+        WG_WANT(q_heads <= 4096u && k_heads <= 4096u, "heads above 4096");
         WG_WANT(dim <= 1024u && rotated >= 2u && rotated <= dim && rotated % 2u == 0u, "rotated must be even, 2 .. dim, and dim 1024 at most");
+        WG_WANT(tokens < 1u << 24, "tokens above 2^24 - 1");
         WG_WANT(magnitude == magnitude && magnitude - magnitude == 0.f, "the magnitude is no number");
         const uintptr_t size = dtype == WG_F32 ? 4u : 2u;
         WG_WANT(aligned(d_q, size) && aligned(d_q_out, size) && (!k_heads || (aligned(d_k, size) && aligned(d_k_out, size))) && aligned(d_frequencies, 8), "numbers must lie at multiples of their size");
@@ -207,7 +208,7 @@ int wg_latent_append(const void *d_c, const void *d_r, uint32_t tokens, uint32_t
     return entry("wg_latent_append", [&](const char **why) {
         WG_WANT(d_c && d_r && d_slots && d_c_cache && d_r_cache, "null argument");
         WG_WANT(tokens && pages, "no tokens or pages");
-        WG_WANT(tokens <= 1u << 29, "tokens above 2^29");
+        WG_WANT(tokens <= 1u << 27, "tokens above 2^27");
         WG_WANT(latent_ok(latent), "latent must be 256 or 512");
         WG_WANT(shift_of(page_tokens), "page_tokens must be 16, 32 or 64");
         WG_WANT((uint64_t)pages * page_tokens <= 0x7FFFFFFFull, "slots above 2^31 - 1");
@@ -223,7 +224,7 @@ int wg_latent_read(const void *d_c_cache, const void *d_r_cache, const float *d_
     return entry("wg_latent_read", [&](const char **why) {
         WG_WANT(d_c_cache && d_r_cache && d_table && d_starts && d_c_out && d_r_out, "null argument");
         WG_WANT(tokens && rows && columns && pages, "no tokens, rows, columns or pages");
-        WG_WANT(tokens <= 0x7FFFFFFFu && rows <= kMostRows, "tokens above 2^31 - 1 or rows above 65535");
+        WG_WANT(tokens <= 1u << 29 && rows <= kMostRows, "tokens above 2^29 or rows above 65535");
         WG_WANT(latent_ok(latent), "latent must be 256 or 512");
         WG_WANT(shift_of(page_tokens), "page_tokens must be 16, 32 or 64");
         WG_WANT((uint64_t)columns * page_tokens <= 0x7FFFFFFFull && (uint64_t)pages * page_tokens <= 0x7FFFFFFFull, "tokens above 2^31 - 1");
@@ -252,7 +253,7 @@ int wg_latent_attend(const void *d_q_c, const void *d_q_r, uint32_t tokens, uint
         WG_WANT(latent_attend_fits(tokens, rows, heads), "too many tokens for one launch");
         WG_WANT(by_sixteen(d_q_c, c_token_stride, c_head_stride) && by_sixteen(d_q_r, r_token_stride, r_head_stride), "queries must lie at multiples of 16 bytes");
         WG_WANT(aligned(d_c_cache, 16) && aligned(d_r_cache, 16) && aligned(d_c_scale, 4) && aligned(d_out, 16), "the cache and the output must be 16-byte aligned");
-        WG_WANT(scale == scale && scale - scale == 0.f, "the scale is no number");
+        WG_WANT(scale * 1.5f - scale * 1.5f == 0.f, "the scale is no number, or too large");
         const uint64_t need = wg_latent_attend_workspace(tokens, rows, heads, latent, columns, page_tokens);
         WG_WANT(!need || (d_workspace && workspace_bytes >= need), "the workspace is too small (wg_latent_attend_workspace)");
         WG_WANT(aligned(d_workspace, 16), "the workspace must be 16-byte aligned");
@@ -282,7 +283,7 @@ int wg_latent_prompt(const void *d_q_n, const void *d_q_r, const void *d_k_n, co
         WG_WANT(k_n_token_stride >= 0 && k_r_token_stride >= 0 && v_token_stride >= 0 && k_n_token_stride < 1 << 24 && k_r_token_stride < 1 << 24 && v_token_stride < 1 << 24,
                 "keys and values must lie 0 to 2^24 - 1 elements apart");
         WG_WANT(aligned(d_out, 16), "the output must be 16-byte aligned");
-        WG_WANT(scale == scale && scale - scale == 0.f, "the scale is no number");
+        WG_WANT(scale * 1.5f - scale * 1.5f == 0.f, "the scale is no number, or too large");
         const uint64_t need = wg_latent_prompt_workspace(tokens, rows, heads, dim, keys);
         WG_WANT(!need || (d_workspace && workspace_bytes >= need), "the workspace is too small (wg_latent_prompt_workspace)");
         WG_WANT(aligned(d_workspace, 16), "the workspace must be 16-byte aligned");

@@ -25,7 +25,7 @@ def test_rotate():
     good = dict(q=P, k=P, dtype=1, tokens=4, q_heads=8, k_heads=2, dim=128, rotated=64, beside=0, q0=1024, q1=128, k0=256, k1=128, positions=P, frequencies=P, magnitude=1.0,
                 q_out=Q, qo0=1024, qo1=128, k_out=C.c_void_p(1 << 21), ko0=256, ko1=128, stream=None)
     refused("wg_rotate", good, [
-        dict(q=None), dict(k=None), dict(positions=None), dict(frequencies=None), dict(q_out=None), dict(k_out=None), dict(dtype=2), dict(tokens=0), dict(tokens=1 << 31),
+        dict(q=None), dict(k=None), dict(positions=None), dict(frequencies=None), dict(q_out=None), dict(k_out=None), dict(dtype=2), dict(tokens=0), dict(tokens=1 << 31), dict(tokens=1 << 24),
         dict(q_heads=0), dict(q_heads=4097), dict(k_heads=4097), dict(dim=1025), dict(dim=63), dict(rotated=0), dict(rotated=63), dict(rotated=130),
         dict(magnitude=math.nan), dict(magnitude=math.inf), dict(q=C.c_void_p(4097)), dict(q_out=C.c_void_p(4097)), dict(k=C.c_void_p(4097)), dict(frequencies=C.c_void_p(4100)),
         dict(q_out=P, qo0=2048), dict(q_out=P, qo1=64), dict(k_out=P, ko0=512), dict(k_out=Q), dict(dtype=0, q=C.c_void_p(4098))])
@@ -34,14 +34,14 @@ def test_rotate():
 def test_latent_append():
     good = dict(c=P, r=P, tokens=4, latent=512, c0=576, r0=576, slots=P, origins=P, c_cache=Q, r_cache=Q, scale=Q, pages=10, page_tokens=16, stream=None)
     refused("wg_latent_append", good, [
-        dict(c=None), dict(r=None), dict(slots=None), dict(c_cache=None), dict(r_cache=None), dict(tokens=0), dict(tokens=(1 << 29) + 1), dict(latent=128), dict(latent=576), dict(pages=0),
+        dict(c=None), dict(r=None), dict(slots=None), dict(c_cache=None), dict(r_cache=None), dict(tokens=0), dict(tokens=(1 << 29) + 1), dict(tokens=(1 << 27) + 1), dict(latent=128), dict(latent=576), dict(pages=0),
         dict(page_tokens=24), dict(pages=1 << 27), dict(c=OFF), dict(r=OFF), dict(c0=580), dict(r0=4), dict(c_cache=OFF), dict(r_cache=OFF), dict(scale=C.c_void_p(4098))])
 
 
 def test_latent_read():
     good = dict(c_cache=P, r_cache=P, scale=P, latent=256, pages=10, page_tokens=32, table=P, rows=3, columns=5, starts=P, tokens=100, c_out=Q, c0=256, r_out=Q, r0=64, stream=None)
     refused("wg_latent_read", good, [
-        dict(c_cache=None), dict(r_cache=None), dict(table=None), dict(starts=None), dict(c_out=None), dict(r_out=None), dict(tokens=0), dict(tokens=1 << 31), dict(rows=0), dict(rows=65536),
+        dict(c_cache=None), dict(r_cache=None), dict(table=None), dict(starts=None), dict(c_out=None), dict(r_out=None), dict(tokens=0), dict(tokens=1 << 31), dict(tokens=(1 << 29) + 1), dict(rows=0), dict(rows=65536),
         dict(columns=0), dict(columns=1 << 26), dict(latent=64), dict(page_tokens=8), dict(pages=0), dict(pages=1 << 26), dict(c_out=OFF), dict(r_out=OFF), dict(c0=250), dict(r0=68),
         dict(c_cache=OFF), dict(r_cache=OFF)])
 
@@ -56,7 +56,7 @@ def test_latent_attend():
         dict(q_c=None), dict(q_r=None), dict(c_cache=None), dict(r_cache=None), dict(table=None), dict(lens=None), dict(starts=None), dict(out=None), dict(work=None), dict(tokens=0),
         dict(heads=0), dict(heads=4097), dict(latent=320), dict(pages=0), dict(pages=1 << 25), dict(page_tokens=0), dict(rows=0), dict(rows=65536), dict(columns=0), dict(columns=1 << 25),
         dict(tokens=1 << 27, heads=16), dict(tokens=(1 << 27) - 1, heads=16, rows=65535), dict(c0=8190), dict(c1=508), dict(r0=1020), dict(r1=60), dict(q_c=OFF), dict(q_r=OFF), dict(c_cache=OFF),
-        dict(r_cache=OFF), dict(out=OFF), dict(factor=math.nan), dict(factor=-math.inf), dict(bytes=need - 1), dict(work=OFF)])
+        dict(r_cache=OFF), dict(out=OFF), dict(factor=math.nan), dict(factor=-math.inf), dict(factor=3e38), dict(bytes=need - 1), dict(work=OFF)])
 
 
 def test_latent_prompt():
@@ -69,7 +69,7 @@ def test_latent_prompt():
         dict(q_n=None), dict(q_r=None), dict(k_n=None), dict(k_r=None), dict(v=None), dict(starts=None), dict(key_starts=None), dict(out=None), dict(work=None), dict(tokens=0), dict(keys=0),
         dict(heads=0), dict(heads=4097), dict(dim=96), dict(dim=256), dict(rows=0), dict(rows=65536), dict(tokens=1 << 31), dict(keys=1 << 31), dict(tokens=1 << 29, heads=4),
         dict(qn0=769), dict(qn1=4), dict(qr0=4), dict(qr1=4), dict(kn0=4), dict(kn1=4), dict(kr0=4), dict(v0=4), dict(v1=4), dict(kn0=1 << 24), dict(kr0=1 << 24), dict(v0=1 << 24), dict(kn0=-1024), dict(kr0=-64), dict(v0=-1024), dict(q_n=OFF), dict(q_r=OFF), dict(k_n=OFF), dict(k_r=OFF), dict(v=OFF),
-        dict(out=OFF), dict(factor=math.nan), dict(bytes=need - 1), dict(work=OFF)])
+        dict(out=OFF), dict(factor=math.nan), dict(factor=-3e38), dict(heads=4096, rows=65535, keys=100), dict(bytes=need - 1), dict(work=OFF)])
 
 
 def test_frequencies():
