@@ -554,8 +554,9 @@ struct JoinArgs {
     uint16_t *out;
     uint32_t requests, heads, chunks, rows;          // rows: of a tile
 };
-// Few parts of a row are a wavefront's, all dims and all parts asked for together.  Many are dealt out to the four wavefronts of a workgroup, 64 at a time, and the dims, 64 at a time, to
-// workgroups: 235 parts of 16 rows of 512 take 4.8 us instead of 8.4 with each 64 parts one after the other.
+// Few parts of a row are a wavefront's, all dims and all parts asked for together.  Many are dealt out to the four wavefronts of a workgroup, 64 at a time, and the dims, 64 at a time, to workgroups.  16 heads, a token
+// a row, attention and this: one row of 30,000, cut into 235 parts, 24 us dealt out and 58 not; four rows of 16,000, 64 parts each, 26 and 31; ten of 8,000, 25 parts, 27.6 and 27.2; 64 of 4,000, 68 and 43.
+constexpr uint32_t kManyParts = 16;                  // parts of a tile, as many as can be (it is counted as two where requests fill one)
 template <uint32_t kD, bool kMany>
 __global__ void __launch_bounds__(256)
 latent_join_kernel(const JoinArgs a)
@@ -696,7 +697,7 @@ static hipError_t launch_latent(const LatentAttendArgs &a, hipStream_t s)
                                 : latent_attend_kernel<kC, kBytes, 8, 1>, grid, dim3(512), 0, s, nullptr, a);
     if (e != hipSuccess || !a.of.chunks) return e;
     return launch_join<kC>(JoinArgs{a.partial, a.ends, a.parts, a.of.starts, a.out, a.of.rows, a.of.heads, a.of.chunks, rows}, a.of.tokens,
-                           a.of.chunks > 32u * attend_tiles(a.of.tokens, a.of.rows, a.of.heads), s);
+                           a.of.chunks > kManyParts * attend_tiles(a.of.tokens, a.of.rows, a.of.heads), s);
 }
 
 hipError_t launch_latent_attend(const void *q_c, const void *q_r, uint32_t tokens, uint32_t heads, uint32_t latent, const int64_t (&strides)[4], const void *c_cache, const void *r_cache,
@@ -944,7 +945,7 @@ hipError_t launch_latent_prompt(const void *q_n, const void *q_r, const void *k_
     const hipError_t e = launch(dim == 128u ? latent_prompt_kernel<128> : latent_prompt_kernel<64>, grid, dim3(kThreads), 0, s, nullptr, a);
     if (e != hipSuccess || !p.chunks) return e;
     const JoinArgs j{a.partial, a.ends, a.parts, starts, a.out, rows, heads, p.chunks, kPromptRows};
-    const bool many = p.chunks > 32u * prompt_tiles(tokens, rows, heads);
+    const bool many = p.chunks > kManyParts * prompt_tiles(tokens, rows, heads);
     return dim == 128u ? launch_join<128>(j, tokens, many, s) : launch_join<64>(j, tokens, many, s);
 }
 

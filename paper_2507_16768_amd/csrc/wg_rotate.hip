@@ -7,7 +7,7 @@
 
 namespace wg {
 
-constexpr uint32_t kRotateThreads = 256;
+constexpr uint32_t kRotateThreads = 256, kOnce = 4;
 
 struct RotateArgs {
     const void *x[2];                                // queries, keys: [token][head][dim]
@@ -80,8 +80,8 @@ rotate_kernel(const RotateArgs a)
         turns[i] = make_float2(cs.x * a.magnitude, cs.y * a.magnitude);
     }
     __syncthreads();
-    // A thread has one unit's place of a head; its heads' numbers (rows) are asked for kOnce at a time.
-    constexpr uint32_t kOnce = kN > 1u ? 4u : 1u;
+    // A thread has one unit's place of a head; its heads' numbers (rows) are asked for kAsked at a time.
+    constexpr uint32_t kAsked = kN > 1u ? kOnce : 1u;
     const uint32_t heads = a.heads[0] + a.heads[1], rows = n * heads, at_once = kRotateThreads / a.units ? kRotateThreads / a.units : 1u, step = gridDim.y * at_once;
     for (uint32_t u = threadIdx.x % (at_once * a.units) % a.units; threadIdx.x < at_once * a.units && u < a.units; u += kRotateThreads) {
         const bool turned = u < a.turned_units;
@@ -93,13 +93,13 @@ rotate_kernel(const RotateArgs a)
             *out = static_cast<T *>(a.out[which]) + (int64_t)(first + t) * a.out_token[which] + (int64_t)h * a.out_head[which];
             return t;
         };
-        for (uint32_t r0 = blockIdx.y * at_once + threadIdx.x / a.units % at_once; r0 < rows; r0 += step * kOnce) {
-            float v[kOnce][kN], w[kOnce][kN];
-            T *out[kOnce];
-            uint32_t t[kOnce];
-            bool moved[kOnce];
+        for (uint32_t r0 = blockIdx.y * at_once + threadIdx.x / a.units % at_once; r0 < rows; r0 += step * kAsked) {
+            float v[kAsked][kN], w[kAsked][kN];
+            T *out[kAsked];
+            uint32_t t[kAsked];
+            bool moved[kAsked];
 #pragma unroll
-            for (uint32_t j = 0; j < kOnce; j++) {
+            for (uint32_t j = 0; j < kAsked; j++) {
                 const uint32_t r = r0 + j * step;
                 const T *x;
                 t[j] = place(r < rows ? r : r0, &x, &out[j]);
@@ -108,7 +108,7 @@ rotate_kernel(const RotateArgs a)
                 if (turned && (!kBeside || kN == 1u)) Numbers<T, kN>::load(x + e, w[j]);
             }
 #pragma unroll
-            for (uint32_t j = 0; j < kOnce; j++) {
+            for (uint32_t j = 0; j < kAsked; j++) {
                 if (!moved[j]) continue;
                 if (!turned) { Numbers<T, kN>::store(out[j] + d, v[j]); continue; }             // behind the pairs
                 const float2 *cs = turn + t[j] * a.pairs;
@@ -149,11 +149,12 @@ hipError_t launch_rotate(const void *q, const void *k, int dtype, uint32_t token
     const uint32_t fit = kRotateThreads / a.pairs;
     a.per = fit < 1u ? 1u : fit > 16u ? 16u : fit;
     if (a.per > tokens) a.per = tokens;
-    // workgroups for each share of tokens: the chip filled, as far as there is something for each thread to do
-    const uint32_t blocks = (tokens + a.per - 1u) / a.per;
-    const uint64_t all = (uint64_t)a.per * (q_heads + k_heads) * a.units;
-    const uint64_t most = (all + kRotateThreads - 1u) / kRotateThreads, want = (1024u + blocks - 1u) / blocks;
-    const dim3 grid(blocks, (uint32_t)(want < most ? want : most)), block(kRotateThreads);
+    // Workgroups for each share of tokens: by 16 bytes, so many that each thread has kOnce rows, all of which it asks for at once (700 tokens of 48 heads 5.0 us, with half as many to a thread 6.1; 7,001
+    // tokens 27.5, with three times as many 29.3); where these are few, or by single numbers, more, as far as there is something for each thread to do.
+    const uint32_t blocks = (tokens + a.per - 1u) / a.per, at_once = kRotateThreads / a.units ? kRotateThreads / a.units : 1u, rows = a.per * (q_heads + k_heads);
+    const uint32_t full = wide ? (rows + at_once * kOnce - 1u) / (at_once * kOnce) : 1u;
+    const uint64_t most = ((uint64_t)rows * a.units + kRotateThreads - 1u) / kRotateThreads, want = ((wide ? 256u : 1024u) + blocks - 1u) / blocks, least = want < most ? want : most;
+    const dim3 grid(blocks, full > least ? full : (uint32_t)least), block(kRotateThreads);
     const uint32_t lds = a.per * a.pairs * (uint32_t)sizeof(float2);
     return launch(f32 ? (wide ? (interleaved ? rotate_kernel<float, 4, true> : rotate_kernel<float, 4, false>) : interleaved ? rotate_kernel<float, 1, true> : rotate_kernel<float, 1, false>)
                   : wide ? (interleaved ? rotate_kernel<uint16_t, 8, true> : rotate_kernel<uint16_t, 8, false>) : interleaved ? rotate_kernel<uint16_t, 1, true> : rotate_kernel<uint16_t, 1, false>,
