@@ -33,28 +33,39 @@ __device__ __forceinline__ float2 cos_sin(int32_t position, double frequency)
     return make_float2(k == 1u || k == 2u ? -a : a, k & 2u ? -b : b);
 }
 
-// kN numbers of a head, 16 bytes of them or one.
+// kN numbers of a head, 16, 8 or 4 bytes of them or one.
 template <typename T, uint32_t kN> struct Numbers;
-template <> struct Numbers<uint16_t, 8> {
-    static __device__ __forceinline__ void load(const uint16_t *p, float (&v)[8])
+template <uint32_t kN> struct Numbers<uint16_t, kN> {
+    typedef uint32_t Words __attribute__((ext_vector_type(kN / 2u)));
+    static __device__ __forceinline__ void load(const uint16_t *p, float (&v)[kN])
     {
-        const Word4 w = *reinterpret_cast<const Word4 *>(p);
+        const Words w = *reinterpret_cast<const Words *>(p);
 #pragma unroll
-        for (uint32_t i = 0; i < 4u; i++) { v[2u * i] = low(w[i]); v[2u * i + 1u] = high(w[i]); }
+        for (uint32_t i = 0; i < kN / 2u; i++) { v[2u * i] = low(w[i]); v[2u * i + 1u] = high(w[i]); }
     }
-    static __device__ __forceinline__ void store(uint16_t *p, const float (&v)[8])
+    static __device__ __forceinline__ void store(uint16_t *p, const float (&v)[kN])
     {
-        __builtin_nontemporal_store(Word4{pk_bf16(v[0], v[1]), pk_bf16(v[2], v[3]), pk_bf16(v[4], v[5]), pk_bf16(v[6], v[7])}, reinterpret_cast<Word4 *>(p));
+        Words w;
+#pragma unroll
+        for (uint32_t i = 0; i < kN / 2u; i++) w[i] = pk_bf16(v[2u * i], v[2u * i + 1u]);
+        __builtin_nontemporal_store(w, reinterpret_cast<Words *>(p));
     }
 };
-template <> struct Numbers<float, 4> {
-    static __device__ __forceinline__ void load(const float *p, float (&v)[4])
+template <uint32_t kN> struct Numbers<float, kN> {
+    typedef float Floats __attribute__((ext_vector_type(kN)));
+    static __device__ __forceinline__ void load(const float *p, float (&v)[kN])
     {
-        const Float4 w = *reinterpret_cast<const Float4 *>(p);
+        const Floats w = *reinterpret_cast<const Floats *>(p);
 #pragma unroll
-        for (uint32_t i = 0; i < 4u; i++) v[i] = w[i];
+        for (uint32_t i = 0; i < kN; i++) v[i] = w[i];
     }
-    static __device__ __forceinline__ void store(float *p, const float (&v)[4]) { __builtin_nontemporal_store(Float4{v[0], v[1], v[2], v[3]}, reinterpret_cast<Float4 *>(p)); }
+    static __device__ __forceinline__ void store(float *p, const float (&v)[kN])
+    {
+        Floats w;
+#pragma unroll
+        for (uint32_t i = 0; i < kN; i++) w[i] = v[i];
+        __builtin_nontemporal_store(w, reinterpret_cast<Floats *>(p));
+    }
 };
 template <> struct Numbers<uint16_t, 1> {
     static __device__ __forceinline__ void load(const uint16_t *p, float (&v)[1]) { v[0] = __uint_as_float((uint32_t)*p << 16); }
@@ -66,7 +77,7 @@ template <> struct Numbers<float, 1> {
 };
 
 // A workgroup makes the sines and cosines of a few tokens once, in LDS, and turns the numbers of all heads with them (heads are dealt out to more workgroups where there
-// are few tokens).  A unit is what a thread takes at once: two pieces of 16 bytes that are turned together (kBeside: one piece of neighbouring pairs), or, behind the pairs, one that is
+// are few tokens).  A unit is what a thread takes at once: two pieces of up to 16 bytes that are turned together (kBeside: one piece of neighbouring pairs), or, behind the pairs, one that is
 // copied.  Bound by memory.
 template <typename T, uint32_t kN, bool kBeside>
 __global__ void __launch_bounds__(kRotateThreads)
@@ -138,27 +149,36 @@ hipError_t launch_rotate(const void *q, const void *k, int dtype, uint32_t token
     RotateArgs a{{q, k}, {q_out, k_out}, {strides[0], strides[2]}, {strides[1], strides[3]}, {strides[4], strides[6]}, {strides[5], strides[7]},
                  positions, frequencies, magnitude, tokens, {q_heads, k_heads}, dim, rotated / 2u, 0, 0, 0};
     const bool f32 = dtype == WG_F32;
-    const uint32_t n = f32 ? 4u : 8u, bytes = f32 ? 4u : 2u;
-    // by 16 bytes where all pieces lie at multiples of them
-    bool wide = dim % n == 0 && (interleaved ? rotated % n == 0 : a.pairs % n == 0);
-    for (const int64_t stride : strides) wide = wide && stride % n == 0;
-    for (const void *p : {q, k, static_cast<const void *>(q_out), static_cast<const void *>(k_out)}) wide = wide && reinterpret_cast<uintptr_t>(p) % (n * bytes) == 0;
-    const uint32_t piece = wide ? n : 1u;
+    // by 16, 8 or 4 bytes, as all pieces lie at multiples of them (20,000 tokens of 20 heads of 80 numbers, 20 of them turned, by 4 bytes: 45 us; by single numbers 110)
+    auto lies = [&](uint32_t n) {
+        bool fits = dim % n == 0 && (interleaved ? rotated % n == 0 : a.pairs % n == 0);
+        for (const int64_t stride : strides) fits = fits && stride % n == 0;
+        for (const void *p : {q, k, static_cast<const void *>(q_out), static_cast<const void *>(k_out)}) fits = fits && reinterpret_cast<uintptr_t>(p) % (n * (f32 ? 4u : 2u)) == 0;
+        return fits;
+    };
+    uint32_t piece = f32 ? 4u : 8u;
+    while (!lies(piece)) piece /= 2u;
+    const bool wide = piece > 1u;
     a.turned_units = wide && interleaved ? rotated / piece : a.pairs / piece;
     a.units = a.turned_units + (dim - rotated) / piece;
     const uint32_t fit = kRotateThreads / a.pairs;
     a.per = fit < 1u ? 1u : fit > 16u ? 16u : fit;
     if (a.per > tokens) a.per = tokens;
-    // Workgroups for each share of tokens: by 16 bytes, so many that each thread has kOnce rows, all of which it asks for at once (700 tokens of 48 heads 5.0 us, with half as many to a thread 6.1; 7,001
+    // Workgroups for each share of tokens: by more than a number, so many that each thread has kOnce rows, all of which it asks for at once (700 tokens of 48 heads 5.0 us, with half as many to a thread 6.1; 7,001
     // tokens 27.5, with three times as many 29.3); where these are few, or by single numbers, more, as far as there is something for each thread to do.
     const uint32_t blocks = (tokens + a.per - 1u) / a.per, at_once = kRotateThreads / a.units ? kRotateThreads / a.units : 1u, rows = a.per * (q_heads + k_heads);
     const uint32_t full = wide ? (rows + at_once * kOnce - 1u) / (at_once * kOnce) : 1u;
     const uint64_t most = ((uint64_t)rows * a.units + kRotateThreads - 1u) / kRotateThreads, want = ((wide ? 256u : 1024u) + blocks - 1u) / blocks, least = want < most ? want : most;
     const dim3 grid(blocks, full > least ? full : (uint32_t)least), block(kRotateThreads);
     const uint32_t lds = a.per * a.pairs * (uint32_t)sizeof(float2);
-    return launch(f32 ? (wide ? (interleaved ? rotate_kernel<float, 4, true> : rotate_kernel<float, 4, false>) : interleaved ? rotate_kernel<float, 1, true> : rotate_kernel<float, 1, false>)
-                  : wide ? (interleaved ? rotate_kernel<uint16_t, 8, true> : rotate_kernel<uint16_t, 8, false>) : interleaved ? rotate_kernel<uint16_t, 1, true> : rotate_kernel<uint16_t, 1, false>,
-                  grid, block, lds, s, nullptr, a);
+    auto go = [&](auto beside, auto straight) { return launch(interleaved ? beside : straight, grid, block, lds, s, nullptr, a); };
+    if (f32)
+        return piece == 4u ? go(rotate_kernel<float, 4, true>, rotate_kernel<float, 4, false>) : piece == 2u ? go(rotate_kernel<float, 2, true>, rotate_kernel<float, 2, false>)
+                                                                                                             : go(rotate_kernel<float, 1, true>, rotate_kernel<float, 1, false>);
+    return piece == 8u   ? go(rotate_kernel<uint16_t, 8, true>, rotate_kernel<uint16_t, 8, false>)
+           : piece == 4u ? go(rotate_kernel<uint16_t, 4, true>, rotate_kernel<uint16_t, 4, false>)
+           : piece == 2u ? go(rotate_kernel<uint16_t, 2, true>, rotate_kernel<uint16_t, 2, false>)
+                         : go(rotate_kernel<uint16_t, 1, true>, rotate_kernel<uint16_t, 1, false>);
 }
 
 }  // namespace wg

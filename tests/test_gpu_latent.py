@@ -52,7 +52,8 @@ def close_turned(got, x, positions, f, beside, magnitude):
 
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 @pytest.mark.parametrize("beside", [False, True])
-@pytest.mark.parametrize("T,Q,K,D,rotated", [(1, 32, 8, 128, 128), (3, 1, 0, 64, 64), (257, 5, 2, 80, 20), (70, 3, 3, 192, 64), (19, 2, 1, 7, 6), (33, 4, 1, 66, 2), (2, 1, 1, 1024, 1024), (1000, 16, 1, 64, 64)])
+@pytest.mark.parametrize("T,Q,K,D,rotated", [(1, 32, 8, 128, 128), (3, 1, 0, 64, 64), (257, 5, 2, 80, 20), (70, 3, 3, 192, 64), (19, 2, 1, 7, 6), (33, 4, 1, 66, 2), (2, 1, 1, 1024, 1024), (1000, 16, 1, 64, 64), (150, 4, 2, 80, 40), (61, 7, 1, 36, 12),
+                                               (3001, 24, 2, 80, 20), (9, 300, 5, 1022, 514)])
 def test_rotate(dtype, beside, T, Q, K, D, rotated):
     g = gen(T * D + beside)
     x = torch.randn((T, Q + K, D), generator=g, device="cuda").to(dtype)
