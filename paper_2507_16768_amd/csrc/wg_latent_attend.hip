@@ -665,23 +665,33 @@ static hipError_t launch_join(const JoinArgs &j, uint32_t tokens, bool many, hip
     return launch(latent_join_kernel<kD, false>, dim3(tokens, (j.heads + 3u) / 4u), dim3(256), 0, s, nullptr, j);
 }
 
-// Query rows of a tile: 16, 32, 64 or 128, as many as a request has.
-static uint32_t attend_rows(uint32_t tokens, uint32_t rows, uint32_t heads)
+static uint64_t attend_blocks(uint32_t columns, uint32_t shift) { return (((uint64_t)columns << shift) + kAttendBlock - 1u) / kAttendBlock; }
+static uint64_t tiles_of(uint32_t tokens, uint32_t rows, uint32_t heads, uint32_t tile) { return (uint64_t)tokens * heads / tile + (rows < tokens ? rows : tokens); }
+static uint32_t rows_of_request(uint32_t tokens, uint32_t rows, uint32_t heads)
 {
     const uint64_t n = (uint64_t)tokens * heads, r = rows < tokens ? rows : tokens;
     return n <= 16u * r ? 16u : n <= 32u * r ? 32u : n <= 64u * r ? 64u : 128u;
 }
-static uint64_t attend_tiles(uint32_t tokens, uint32_t rows, uint32_t heads) { return (uint64_t)tokens * heads / attend_rows(tokens, rows, heads) + (rows < tokens ? rows : tokens); }
-
-bool latent_attend_fits(uint32_t tokens, uint32_t rows, uint32_t heads)
+// Query rows of a tile: 16, 32, 64 or 128.  As many as a request has read its keys once (in bfloat16, 512 numbers: 100 rows of 4,000 tokens, 128 heads 118 us with 128, 144 with 64, 337 with 16; 64 of 8,000, 32 heads 92
+// with 32, 126 with 16, 116 with 128).  But a workgroup has its queries to ask for and its part to store however few keys it has, and where all tiles have only two blocks of keys for each
+// workgroup, or four, as far as the table's width tells, smaller ones are faster, whose parts are smaller (128 heads: one row of 2,000 tokens 21.5 us with 16, 27.5 with 128; four of 2,000 26 and 42; one of
+// 30,000 37 with 64, 42 with 128, 56 with 16; 50 tokens of a row of 4,000, 24 heads 39 with 64, 68 with 128).
+static uint32_t attend_rows(uint32_t tokens, uint32_t rows, uint32_t heads, uint64_t blocks)
 {
-    return (uint64_t)tokens * heads / attend_rows(tokens, rows, heads) + rows <= 0x7FFFFFu;
+    const uint32_t most = rows_of_request(tokens, rows, heads);
+    const uint64_t n = (uint64_t)tokens * heads;
+    for (uint32_t tile = 16u; tile < most; tile *= 2u)
+        if (((n + tile - 1u) / tile) * blocks <= (tile == 64u ? 4u : 2u) * kAttendSlots) return tile;
+    return most;
 }
+static uint64_t attend_tiles(uint32_t tokens, uint32_t rows, uint32_t heads, uint64_t blocks) { return tiles_of(tokens, rows, heads, attend_rows(tokens, rows, heads, blocks)); }
+
+bool latent_attend_fits(uint32_t tokens, uint32_t rows, uint32_t heads) { return (uint64_t)tokens * heads / rows_of_request(tokens, rows, heads) + rows <= 0x7FFFFFu; }
 
 static Plan attend_plan(uint32_t tokens, uint32_t rows, uint32_t heads, uint32_t latent, uint32_t columns, uint32_t shift)
 {
-    const uint64_t blocks = (((uint64_t)columns << shift) + kAttendBlock - 1u) / kAttendBlock;
-    return plan_of(attend_tiles(tokens, rows, heads), blocks, rows, tokens <= 16u * rows, attend_rows(tokens, rows, heads), latent, kAttendSlots, (uint64_t)tokens * heads);
+    const uint64_t blocks = attend_blocks(columns, shift);
+    return plan_of(attend_tiles(tokens, rows, heads, blocks), blocks, rows, tokens <= 16u * rows, attend_rows(tokens, rows, heads, blocks), latent, kAttendSlots, (uint64_t)tokens * heads);
 }
 uint64_t latent_attend_bytes(uint32_t tokens, uint32_t rows, uint32_t heads, uint32_t latent, uint32_t columns, uint32_t shift)
 {
@@ -691,13 +701,14 @@ uint64_t latent_attend_bytes(uint32_t tokens, uint32_t rows, uint32_t heads, uin
 template <uint32_t kC, bool kBytes>
 static hipError_t launch_latent(const LatentAttendArgs &a, hipStream_t s)
 {
-    const uint32_t rows = attend_rows(a.of.tokens, a.of.rows, a.of.heads);
+    const uint64_t blocks = attend_blocks(a.columns, a.shift);
+    const uint32_t rows = attend_rows(a.of.tokens, a.of.rows, a.of.heads, blocks);
     const dim3 grid(a.of.chunks ? a.of.chunks : (uint32_t)((uint64_t)a.of.tokens * a.of.heads / rows) + a.of.rows);
     const hipError_t e = launch(rows == 16u ? latent_attend_kernel<kC, kBytes, 1, 4> : rows == 32u ? latent_attend_kernel<kC, kBytes, 2, 2> : rows == 64u ? latent_attend_kernel<kC, kBytes, 4, 2>
                                 : latent_attend_kernel<kC, kBytes, 8, 1>, grid, dim3(512), 0, s, nullptr, a);
     if (e != hipSuccess || !a.of.chunks) return e;
     return launch_join<kC>(JoinArgs{a.partial, a.ends, a.parts, a.of.starts, a.out, a.of.rows, a.of.heads, a.of.chunks, rows}, a.of.tokens,
-                           a.of.chunks > kManyParts * attend_tiles(a.of.tokens, a.of.rows, a.of.heads), s);
+                           a.of.chunks > kManyParts * attend_tiles(a.of.tokens, a.of.rows, a.of.heads, blocks), s);
 }
 
 hipError_t launch_latent_attend(const void *q_c, const void *q_r, uint32_t tokens, uint32_t heads, uint32_t latent, const int64_t (&strides)[4], const void *c_cache, const void *r_cache,

@@ -364,6 +364,31 @@ def test_attend_in_shares(bits, H, lens, counts):
     run_attend(gen(H), lens, counts, H, 512, bits, 64, columns=300)
 
 
+@pytest.mark.parametrize("bits", [8, 16])
+@pytest.mark.parametrize("C", [256, 512])
+@pytest.mark.parametrize("columns", [2500, 200, 0])
+@pytest.mark.parametrize("H,P,lens,counts", [
+    (128, 16, [1, 2, 15, 16, 17, 31, 32, 33, 63, 64, 65, 127, 128, 129, 255, 256, 257, 300, 511, 513], [1] * 20), (64, 32, [700, 0, 33, 129, 1000], [1] * 5), (24, 16, [600, 77], [203, 77]),
+    (5, 16, [2000, 0, 1, 33], [13, 0, 0, 33]), (40, 64, [90], [90]), (32, 64, [1, 400, 64, 5], [1, 2, 1, 0]), (16, 64, [500, 40, 4, 1000], [4, 4, 4, 3])])
+def test_attend_tables_of_other_widths(bits, C, columns, H, P, lens, counts):
+    """How wide a table is decides over how many query rows a workgroup takes; what it holds behind the rows' tokens is nothing to them."""
+    run_attend(gen(H + P), lens, counts, H, C, bits, P, extra=1, columns=columns)
+
+
+@pytest.mark.parametrize("bad", [NAN, INF])
+@pytest.mark.parametrize("H,lens,counts,at", [(128, [200], [3], 198), (16, [130], [130], 100), (64, [64], [64], 33)])
+def test_attend_numbers_that_are_none_under_wide_tables(bad, H, lens, counts, at):
+    def spoil(c_cache, r_cache, scale, slots):
+        c_cache.view(-1, 512)[int(slots[0][at]), 5] = bad
+    for got, q, k, v, seen in check_attend(gen(at), lens, counts, H, 512, 16, 64, spoil=spoil, columns=2000):
+        v, k = v.clone(), k.clone()
+        v[at, :, 5], k[at, :, 5] = 0.0, 0.0
+        blind = seen <= at
+        want, off = attention(q[blind], k, v, seen[blind], 0.06)
+        assert ((got[blind].double() - want).abs() <= off).all()
+        assert got[~blind][..., 5].isnan().all()
+
+
 def test_attend_rows_without_tokens_and_many_rows():
     counts = [1 if r % 3 else 0 for r in range(150)]
     run_attend(gen(9), [(r * 37) % 290 if r % 5 else 0 for r in range(150)], counts, 16, 256, 8, 16)
