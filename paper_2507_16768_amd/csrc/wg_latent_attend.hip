@@ -280,6 +280,13 @@ constexpr float kEmpty = -1.f;                       // the sum of a share in wh
 // ---------------------------------------------------------------------------------------------
 // Attention over the cached vectors.  A workgroup's eight wavefronts are kGroups groups of 16 query rows (tokens times heads), times kCols groups of the vectors' columns (which make
 // the scores between them), times groups of 32 keys.  A block's keys go through LDS: from memory into registers, while the block before is worked on, and turned into bfloat16 (exactly) on the way.
+//
+// What bounds it.  100 rows of 1,000 to 4,000 tokens, 128 heads, bfloat16: 118 to 122 us, 590 to 614 TFLOP/s, an eighth of it joining.  Over its keys, 295 MB, it goes at 5.2 TB/s, what a copy reaches, 57 us; the
+// rest is that 256 workgroups, one on each compute unit, ask for 147 KB of queries for each of the two tiles or so that they have a part of, and store 256 KB for each part.  64 rows' 4 drafts, 16 heads, 8 bits: 88 us,
+// 6 of it joining (2.4 TB/s, 273 TFLOP/s): a block of 32 keys takes 3,900 cycles, of which the products are 1,100; the others are what comes one after the other in a block, the scores' exchange, the softmax, the keys to LDS.  One
+// row of 30,000, 16 heads, 8 bits: 22 us, 6 of it joining, a workgroup having one block of 128 keys: latencies, one behind the other, of lengths, page numbers, keys and stores.
+// Tried, and no faster: the keys' way to LDS beside the second product (124 us for 121; 172 with branches, whose waits are for everything), all queries asked for before one is used (123 for 123), wavefronts'
+// priorities, values asked for before the softmax; 32 query rows to a wavefront (its 256 accumulators leave no registers to scale them in).
 struct LatentAttendArgs {
     Requests of;
     const uint16_t *q_c, *q_r;
@@ -725,8 +732,14 @@ hipError_t launch_latent_attend(const void *q_c, const void *q_r, uint32_t token
 }
 
 // ---------------------------------------------------------------------------------------------
-// Attention of prompts over keys and values of every head.  A workgroup takes 128 tokens of a request, a head and a share of the keys, 32 tokens to a wavefront; keys and values go
-// through LDS 64 at a time.
+// Attention of prompts over keys and values of every head.  A workgroup takes 128 tokens of a request, a head and a share of the keys, 32 tokens to a wavefront, a query to a lane (products of 32 by 32, whose
+// operands out of LDS serve twice as many queries as those of 16 by 16: 138 us for 158); keys and values go through LDS 32 at a time, two workgroups on a compute unit (211 us with one).  Tiles of many tokens are
+// left to the chip, the last of a row first.
+//
+// What bounds it.  Four prompts of 800 to 2,000 tokens, 32 heads of 128: 139 to 147 us, 664 to 698 TFLOP/s (one of 16,000, 16 heads: 955; a large matrix product reaches 1,222).  Left out, the softmax's arithmetic would save
+// 18 us of it, the second product 26, the keys' way from memory 12: no part bounds it alone.  131 queries behind 9,000 keys, 16 heads: 41 us, 1.9 TB/s; its 32 tiles are cut, and what the parts cost adds.
+// Tried, and no faster: one block's softmax under the next one's products with three blocks in LDS (143 us for 143), tiles in order of their keys over all rows (146 for 146), 16 rows to a wavefront and four of
+// them to a SIMD (158).
 struct LatentPromptArgs {
     Requests of;
     const uint16_t *q_n, *q_r, *k_n, *k_r, *v;
@@ -849,6 +862,7 @@ latent_prompt_kernel(const LatentPromptArgs a)
         __builtin_amdgcn_s_waitcnt(0x0F70);                                // (as in latent_attend_kernel)
         if (from + kPromptKeys < to) fetch(from + kPromptKeys);
         const float factor = size_of(a.factor);
+        const bool some = uniform(t.first + wave * 32u) < t.last;            // a wavefront that has no query only brings keys (131 queries, 16 heads, behind 9,000 keys: 40.8 us for 42.8)
         uint32_t turn = 0;
         for (uint32_t block = from; block < to; block += kPromptKeys, turn ^= 1u) {
             __syncthreads();
@@ -857,42 +871,44 @@ latent_prompt_kernel(const LatentPromptArgs a)
             Float16 score;
 #pragma unroll
             for (uint32_t e = 0; e < 16u; e++) score[e] = 0.f;
-            Half8 x[2][kAhead];
-            pipelined<kSteps, kAhead>([&](uint32_t i, uint32_t at) { x[at / kAhead][at % kAhead] = *reinterpret_cast<const Half8 *>(row + i * 16u); },
-                                      [&](uint32_t i, uint32_t at) { score = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x[at / kAhead][at % kAhead], q[i], score, 0, 0, 0); });
-            const uint32_t at = block + h * 8u;
-            if (block + kPromptKeys > seen_least || block + kPromptKeys > to)
+            Half8 x[2][kAhead], p[2];
+            if (some) {
+                pipelined<kSteps, kAhead>([&](uint32_t i, uint32_t at) { x[at / kAhead][at % kAhead] = *reinterpret_cast<const Half8 *>(row + i * 16u); },
+                                          [&](uint32_t i, uint32_t at) { score = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x[at / kAhead][at % kAhead], q[i], score, 0, 0, 0); });
+                const uint32_t at = block + h * 8u;
+                if (block + kPromptKeys > seen_least || block + kPromptKeys > to)
 #pragma unroll
-                for (uint32_t e = 0; e < 16u; e++) score[e] = at + e / 8u * 16u + e % 8u < sees ? score[e] : -__builtin_inff();
-            float top = score[0];
+                    for (uint32_t e = 0; e < 16u; e++) score[e] = at + e / 8u * 16u + e % 8u < sees ? score[e] : -__builtin_inff();
+                float top = score[0];
 #pragma unroll
-            for (uint32_t e = 1; e < 16u; e++) top = __builtin_fmaxf(top, score[e]);
-            top *= factor;
-            if (__ballot(top > base + kLift)) {
-                const auto both_halves = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top), false, false);
-                top = __builtin_fmaxf(base, __builtin_fmaxf(__uint_as_float(both_halves[0]), __uint_as_float(both_halves[1])));
-                const float by = __builtin_amdgcn_exp2f(base - (top > -__builtin_inff() ? top : 0.f));
-                base = top; sum *= by;
+                for (uint32_t e = 1; e < 16u; e++) top = __builtin_fmaxf(top, score[e]);
+                top *= factor;
+                if (__ballot(top > base + kLift)) {
+                    const auto both_halves = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top), false, false);
+                    top = __builtin_fmaxf(base, __builtin_fmaxf(__uint_as_float(both_halves[0]), __uint_as_float(both_halves[1])));
+                    const float by = __builtin_amdgcn_exp2f(base - (top > -__builtin_inff() ? top : 0.f));
+                    base = top; sum *= by;
 #pragma unroll
-                for (uint32_t d = 0; d < kParts; d++) acc[d] *= by;
-            }
-            const float rel = base > -__builtin_inff() ? base : 0.f;
-            Half8 p[2];
-#pragma unroll
-            for (uint32_t k = 0; k < 2u; k++) {
-                Word4 w;
-#pragma unroll
-                for (uint32_t j = 0; j < 4u; j++) {
-                    const float u = __builtin_amdgcn_exp2f(__builtin_fmaf(score[8u * k + 2u * j], factor, -rel)), v = __builtin_amdgcn_exp2f(__builtin_fmaf(score[8u * k + 2u * j + 1u], factor, -rel));
-                    w[j] = pk_bf16(u, v);
-                    sum += u; sum += v;
+                    for (uint32_t d = 0; d < kParts; d++) acc[d] *= by;
                 }
-                p[k] = __builtin_bit_cast(Half8, w);
+                const float rel = base > -__builtin_inff() ? base : 0.f;
+#pragma unroll
+                for (uint32_t k = 0; k < 2u; k++) {
+                    Word4 w;
+#pragma unroll
+                    for (uint32_t j = 0; j < 4u; j++) {
+                        const float u = __builtin_amdgcn_exp2f(__builtin_fmaf(score[8u * k + 2u * j], factor, -rel)), v = __builtin_amdgcn_exp2f(__builtin_fmaf(score[8u * k + 2u * j + 1u], factor, -rel));
+                        w[j] = pk_bf16(u, v);
+                        sum += u; sum += v;
+                    }
+                    p[k] = __builtin_bit_cast(Half8, w);
+                }
             }
             if (block + kPromptKeys < to) {
                 stage(block + kPromptKeys, turn ^ 1u);
                 if (block + 2u * kPromptKeys < to) fetch(block + 2u * kPromptKeys);
             }
+            if (!some) continue;
             const uint16_t *column = values + turn * 32u * kValuePitch + value_at(h * 8u + lane % 16u / 4u) + lane / 16u % 2u * 16u + lane % 4u * 4u;
             pipelined<2u * kParts, kAhead>([&](uint32_t i, uint32_t at) {
                                                const uint16_t *of = column + i / kParts * 16u * kValuePitch + i % kParts * 32u;
