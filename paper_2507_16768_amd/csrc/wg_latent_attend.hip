@@ -81,8 +81,9 @@ template <typename F>
 __device__ __forceinline__ bool chunk_of(const Requests &a, uint32_t w, F work_of, Chunk *out)
 {
     const uint32_t lane = threadIdx.x & 63u;
-    uint32_t all = 0;
-    for (uint32_t r = lane; r < a.rows; r += 64u) all += work_of(r);
+    const uint32_t first = lane < a.rows ? work_of(lane) : 0u;             // (most calls have no more rows: asked for once)
+    uint32_t all = first;
+    for (uint32_t r = lane + 64u; r < a.rows; r += 64u) all += work_of(r);
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) all += __shfl_xor(all, o);
     all = __builtin_amdgcn_readfirstlane(all);
@@ -93,7 +94,7 @@ __device__ __forceinline__ bool chunk_of(const Requests &a, uint32_t w, F work_o
     out->end = all - out->at < size ? all : out->at + size;
     uint32_t ahead = 0;                              // work of the requests in front
     for (uint32_t base = 0; base < a.rows; base += 64u) {
-        const uint32_t own = base + lane < a.rows ? work_of(base + lane) : 0u;
+        const uint32_t own = !base ? first : base + lane < a.rows ? work_of(base + lane) : 0u;
         uint32_t sum = own;
 #pragma unroll
         for (int o = 1; o < 64; o <<= 1) { const uint32_t x = __shfl_up(sum, o); sum += lane >= (uint32_t)o ? x : 0u; }
