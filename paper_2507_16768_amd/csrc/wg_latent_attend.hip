@@ -286,8 +286,8 @@ constexpr float kEmpty = -1.f;                       // the sum of a share in wh
 // rest is that 256 workgroups, one on each compute unit, ask for 147 KB of queries for each of the two tiles or so that they have a part of, and store 256 KB for each part.  64 rows' 4 drafts, 16 heads, 8 bits: 88 us,
 // 6 of it joining (2.4 TB/s, 273 TFLOP/s): a block of 32 keys takes 3,900 cycles, of which the products are 1,100; the others are what comes one after the other in a block, the scores' exchange, the softmax, the keys to LDS.  One
 // row of 30,000, 16 heads, 8 bits: 22 us, 6 of it joining, a workgroup having one block of 128 keys: latencies, one behind the other, of lengths, page numbers, keys and stores.
-// Tried, and no faster: the keys' way to LDS beside the second product (124 us for 121; 172 with branches, whose waits are for everything), all queries asked for before one is used (123 for 123), values asked
-// for before the softmax; 32 query rows to a wavefront (its 256 accumulators leave no registers to scale them in).
+// Tried, and no faster: the keys' way to LDS beside the second product (124 us for 121; 172 with branches, whose waits are for everything), all queries asked for before one is used (123 for 123), two blocks of
+// keys asked for at first (122 for 122), slots found before the keys go to LDS (no difference), values asked for before the softmax; 32 query rows to a wavefront (its 256 accumulators leave no registers to scale them in).
 struct LatentAttendArgs {
     Requests of;
     const uint16_t *q_c, *q_r;
@@ -737,9 +737,9 @@ hipError_t launch_latent_attend(const void *q_c, const void *q_r, uint32_t token
 // operands out of LDS serve twice as many queries as those of 16 by 16: 138 us for 158); keys and values go through LDS 32 at a time, two workgroups on a compute unit (211 us with one).  Tiles of many tokens are
 // left to the chip, the last of a row first.
 //
-// What bounds it.  Four prompts of 800 to 2,000 tokens, 32 heads of 128: 136 to 145 us, 670 to 715 TFLOP/s (one of 16,000, 16 heads: 955; a large matrix product reaches 1,222).  Left out, the softmax's arithmetic would save
+// What bounds it.  Four prompts of 800 to 2,000 tokens, 32 heads of 128: 136 to 145 us, 670 to 715 TFLOP/s (one of 16,000, 16 heads: 981; a large matrix product reaches 1,222).  Left out, the softmax's arithmetic would save
 // 18 us of it, the second product 26, the keys' way from memory 12: no part bounds it alone.  131 queries behind 9,000 keys, 16 heads: 41 us, 1.9 TB/s; its 32 tiles are cut, and what the parts cost adds.
-// Tried, and no faster: one block's softmax under the next one's products with three blocks in LDS (143 us for 143), tiles in order of their keys over all rows (146 for 146), 16 rows to a wavefront and four of
+// Tried, and no faster: 256 tokens to a workgroup (143 us for 135; 131 queries behind 9,000 keys 37 for 41), one block's softmax under the next one's products with three blocks in LDS (143 us for 143), tiles in order of their keys over all rows (146 for 146), 16 rows to a wavefront and four of
 // them to a SIMD (158).
 struct LatentPromptArgs {
     Requests of;
