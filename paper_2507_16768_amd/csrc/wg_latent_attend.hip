@@ -648,15 +648,19 @@ latent_join_kernel(const JoinArgs a)
         for (uint32_t d = 0; d < kOwn; d += 2u) reinterpret_cast<Word *>(out)[d / 2u] = pk_bf16(acc[d], acc[(d + 1u) % kOwn]);
 }
 
-// Whether all work is dealt out, over how many workgroups, and the workspace's parts.  (tiles, blocks: the most there can be.)  Tiles of a request's many tokens see more keys the later they come, which the
-// chunks do not know: with twice as many as the chip holds at a time they are left to it; where requests have few tokens, as they decode, all work is dealt out however many there are (256 rows of 1,000 to
-// 4,000 tokens, 128 heads, a tile each: 541 us left to the chip, 307 dealt out).  Below three blocks of keys a tile is a workgroup's: joining it would cost more than it saves (one token of a row of 200, 16
-// heads: 17.3 us dealt out, 16.2 by one; a prompt of 200, 8 heads: 15.3 and 12.0; with three blocks 16.3 and 18.0).
+// Whether all work is dealt out, over how many workgroups, and the workspace's parts.  (tiles, blocks: the most there can be; of_row: blocks of keys of a row, as far as that is known.)  Tiles of a request's many tokens
+// see more keys the later they come, which the chunks do not know: with twice as many as the chip holds at a time they are left to it; where requests have few tokens, as they decode, all work is dealt out however
+// many there are (256 rows of 1,000 to 4,000 tokens, 128 heads, a tile each: 541 us left to the chip, 307 dealt out).
+//
+// A tile of few blocks is a workgroup's, since joining it would cost more than it saves: of one or two (one token of a row of 200, 16 heads: 17.3 us dealt out, 16.2 by one; with three blocks 16.3 and 18.0), and, where
+// requests have many tokens or keys of their own for each head, of up to four that would be cut into two or so (100 tokens of a row of 500, 128 heads 51 and 36, of 800 55 and 62; prompts of 400, 32 heads 26 and
+// 19, three of 170 24 and 11; 128 tokens behind 500 20 and 26).
 struct Plan { uint32_t chunks; uint64_t partial, ends, parts; };
-static Plan plan_of(uint64_t tiles, uint64_t blocks, uint32_t rows, bool few, uint32_t tile_rows, uint32_t dim, uint32_t slots, uint64_t outputs)
+static Plan plan_of(uint64_t tiles, uint64_t blocks, uint64_t of_row, uint32_t rows, bool few, bool cut_late, uint32_t tile_rows, uint32_t dim, uint32_t slots, uint64_t outputs)
 {
     Plan p{0u, 0u, 0u, 0u};
-    if (rows > 1024u || blocks < 3u || (tiles >= 2u * slots && !few) || tiles * (blocks + kTileCost) > 0x7FFFFFFFull) return p;
+    if (rows > 1024u || of_row < 3u || (tiles >= 2u * slots && !few) || tiles * (blocks + kTileCost) > 0x7FFFFFFFull) return p;
+    if (cut_late && of_row <= (tiles * (of_row + kTileCost) > slots ? 4u : 3u)) return p;
     const uint64_t most = (tiles * (blocks + kTileCost) + kAttendLeast - 1u) / kAttendLeast;
     p.chunks = (uint32_t)(most < slots ? most : slots);
     p.partial = (uint64_t)p.chunks * 2u * tile_rows * dim;
@@ -699,7 +703,8 @@ bool latent_attend_fits(uint32_t tokens, uint32_t rows, uint32_t heads) { return
 static Plan attend_plan(uint32_t tokens, uint32_t rows, uint32_t heads, uint32_t latent, uint32_t columns, uint32_t shift)
 {
     const uint64_t blocks = attend_blocks(columns, shift);
-    return plan_of(attend_tiles(tokens, rows, heads, blocks), blocks, rows, tokens <= 16u * rows, attend_rows(tokens, rows, heads, blocks), latent, kAttendSlots, (uint64_t)tokens * heads);
+    const bool few = tokens <= 16u * rows;
+    return plan_of(attend_tiles(tokens, rows, heads, blocks), blocks, blocks, rows, few, !few, attend_rows(tokens, rows, heads, blocks), latent, kAttendSlots, (uint64_t)tokens * heads);
 }
 uint64_t latent_attend_bytes(uint32_t tokens, uint32_t rows, uint32_t heads, uint32_t latent, uint32_t columns, uint32_t shift)
 {
@@ -959,7 +964,8 @@ static uint64_t prompt_tiles(uint32_t tokens, uint32_t rows, uint32_t heads) { r
 static Plan prompt_plan(uint32_t tokens, uint32_t rows, uint32_t heads, uint32_t dim, uint32_t keys)
 {
     const uint64_t tiles = prompt_tiles(tokens, rows, heads), blocks = ((uint64_t)keys + kAttendBlock - 1u) / kAttendBlock;
-    return plan_of(tiles, blocks, rows, tokens <= kPromptRows * rows, kPromptRows, dim, kPromptSlots, (uint64_t)tokens * heads);
+    // (keys of all rows: where there are not many, rows are taken to have as many each)
+    return plan_of(tiles, blocks, blocks <= 12u ? (blocks + rows - 1u) / rows : blocks, rows, tokens <= kPromptRows * rows, true, kPromptRows, dim, kPromptSlots, (uint64_t)tokens * heads);
 }
 uint64_t latent_prompt_bytes(uint32_t tokens, uint32_t rows, uint32_t heads, uint32_t dim, uint32_t keys) { return plan_bytes(prompt_plan(tokens, rows, heads, dim, keys)); }
 
