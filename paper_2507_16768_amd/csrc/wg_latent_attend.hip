@@ -742,7 +742,7 @@ hipError_t launch_latent_attend(const void *q_c, const void *q_r, uint32_t token
 // operands out of LDS serve twice as many queries as those of 16 by 16: 138 us for 158); keys and values go through LDS 32 at a time, two workgroups on a compute unit (211 us with one).  Tiles of many tokens are
 // left to the chip, the last of a row first.
 //
-// What bounds it.  Four prompts of 800 to 2,000 tokens, 32 heads of 128: 136 to 145 us, 670 to 715 TFLOP/s (one of 16,000, 16 heads: 981; a large matrix product reaches 1,222).  Left out, the softmax's arithmetic would save
+// What bounds it.  Four prompts of 800 to 2,000 tokens, 32 heads of 128: 134 to 145 us, 670 to 727 TFLOP/s (one of 16,000, 16 heads: 981; a large matrix product reaches 1,222).  Left out, the softmax's arithmetic would save
 // 18 us of it, the second product 26, the keys' way from memory 12: no part bounds it alone.  131 queries behind 9,000 keys, 16 heads: 41 us, 1.9 TB/s; its 32 tiles are cut, and what the parts cost adds.
 // Tried, and no faster: 256 tokens to a workgroup (143 us for 135; 131 queries behind 9,000 keys 37 for 41), one block's softmax under the next one's products with three blocks in LDS (143 us for 143), tiles in order of their keys over all rows (146 for 146), 16 rows to a wavefront and four of
 // them to a SIMD (158).
