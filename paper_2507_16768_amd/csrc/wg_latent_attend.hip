@@ -220,7 +220,7 @@ __device__ __forceinline__ Half8 signed_query(Half8 q, float factor)
     for (uint32_t w = 0; w < 4u; w++) v[w] = (v[w] ^ flip) & keep;
     return __builtin_bit_cast(Half8, v);
 }
-__device__ __forceinline__ float size_of(float factor) { return factor == 0.f ? 1.f : __builtin_fabsf(factor); }
+__host__ __device__ __forceinline__ float size_of(float factor) { return factor == 0.f ? 1.f : __builtin_fabsf(factor); }
 
 // The largest over lanes l, l ^ 16, l ^ 32 and l ^ 48.
 __device__ __forceinline__ float most_of_rows(float x)
@@ -230,6 +230,11 @@ __device__ __forceinline__ float most_of_rows(float x)
     const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
     return __builtin_fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
 }
+
+// A score relative to a base, in log2.  Bases are scores themselves, and the difference is taken before the factor: that of the base's own score is 0 whatever its size, where a product less another one that was
+// rounded would leave the rounding's error, which from scores of 2^31 on has the largest weight 0 or infinite.  (An operation more a score: 100 rows, 128 heads 123 us for 119, drafts 89.9 for 88, prompts 142.8 for 140.8;
+// one of 16,000 tokens 1,301 for 1,289.  Left to a branch that scores below 2^10 do not take, 123, 88.4, 140 and 1,299.)
+__device__ __forceinline__ float in_log2(float score, float base, float factor) { return (score - base) * factor; }
 
 // What a wavefront holds of its 16 queries: of query m, the base and its own part of the sum, and outputs, dims 4 g .. 4 g + 3 of each of kParts.
 template <uint32_t kParts>
@@ -248,10 +253,9 @@ struct Sums {
         float n = s[0];
 #pragma unroll
         for (uint32_t j = 0; j < 8u; j++) n = __builtin_fmaxf(n, s[j]);
-        n *= factor;
-        if (__ballot(n > base + kLift)) {
+        if (__ballot(in_log2(n, base, factor) > kLift)) {
             n = __builtin_fmaxf(base, most_of_rows(n));
-            const float by = __builtin_amdgcn_exp2f(base - (n > -__builtin_inff() ? n : 0.f));
+            const float by = __builtin_amdgcn_exp2f(in_log2(base, n > -__builtin_inff() ? n : 0.f, factor));
             base = n; sum *= by;
 #pragma unroll
             for (uint32_t d = 0; d < kParts; d++) acc[d] *= by;
@@ -260,7 +264,7 @@ struct Sums {
         Word4 w;
 #pragma unroll
         for (uint32_t j = 0; j < 4u; j++) {
-            const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(s[2u * j], factor, -from)), y = __builtin_amdgcn_exp2f(__builtin_fmaf(s[2u * j + 1u], factor, -from));
+            const float x = __builtin_amdgcn_exp2f(in_log2(s[2u * j], from, factor)), y = __builtin_amdgcn_exp2f(in_log2(s[2u * j + 1u], from, factor));
             w[j] = pk_bf16(x, y);
             sum += x; sum += y;
         }
@@ -541,7 +545,7 @@ latent_attend_kernel(const LatentAttendArgs a)
             Float4 v{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (uint32_t w = 0; w < kKeyGroups; w++) {
-                const float by = __builtin_amdgcn_exp2f(join_base[w][i] - rel);
+                const float by = __builtin_amdgcn_exp2f(in_log2(join_base[w][i], rel, size_of(a.factor)));
                 total += by * join_sum[w][i];
                 v += by * *reinterpret_cast<const Float4 *>(join + (w * kRows + i) * kJoinPitch + d);
             }
@@ -561,6 +565,7 @@ struct JoinArgs {
     const int32_t *starts;
     uint16_t *out;
     uint32_t requests, heads, chunks, rows;          // rows: of a tile
+    float factor;                                    // above 0: of the bases, to log2
 };
 // Few parts of a row are a wavefront's, all dims and all parts asked for together.  Many are dealt out to the four wavefronts of a workgroup, 64 at a time, and the dims, 64 at a time, to workgroups.  16 heads, a token
 // a row, attention and this: one row of 30,000, cut into 235 parts, 24 us dealt out and 58 not; four rows of 16,000, 64 parts each, 26 and 31; ten of 8,000, 25 parts, 27.6 and 27.2; 64 of 4,000, 68 and 43.
@@ -603,9 +608,9 @@ latent_join_kernel(const JoinArgs a)
         float top = __builtin_fmaxf(base, e[0]);
 #pragma unroll
         for (int o = 32; o > 0; o >>= 1) top = __builtin_fmaxf(top, __shfl_xor(top, o));
-        const float rel = top > -__builtin_inff() ? top : 0.f, by = __builtin_amdgcn_exp2f(base - rel);
+        const float rel = top > -__builtin_inff() ? top : 0.f, by = __builtin_amdgcn_exp2f(in_log2(base, rel, a.factor));
         any = any || e[1] == kEmpty;
-        const float w = e[1] == kEmpty || e[1] == 0.f ? 0.f : e[1] * __builtin_amdgcn_exp2f(e[0] - rel);
+        const float w = e[1] == kEmpty || e[1] == 0.f ? 0.f : e[1] * __builtin_amdgcn_exp2f(in_log2(e[0], rel, a.factor));
         total = total * by + w;
         base = top;
 #pragma unroll
@@ -633,7 +638,7 @@ latent_join_kernel(const JoinArgs a)
         acc[0] = 0.f; total = 0.f;
 #pragma unroll
         for (uint32_t w = 0; w < 4u; w++) {
-            const float by = __builtin_amdgcn_exp2f(tops[w] - rel);
+            const float by = __builtin_amdgcn_exp2f(in_log2(tops[w], rel, a.factor));
             acc[0] += by * part[w][lane]; total += by * sums[w];
             empty = empty || empties[w];
         }
@@ -720,7 +725,7 @@ static hipError_t launch_latent(const LatentAttendArgs &a, hipStream_t s)
     const hipError_t e = launch(rows == 16u ? latent_attend_kernel<kC, kBytes, 1, 4> : rows == 32u ? latent_attend_kernel<kC, kBytes, 2, 2> : rows == 64u ? latent_attend_kernel<kC, kBytes, 4, 2>
                                 : latent_attend_kernel<kC, kBytes, 8, 1>, grid, dim3(512), 0, s, nullptr, a);
     if (e != hipSuccess || !a.of.chunks) return e;
-    return launch_join<kC>(JoinArgs{a.partial, a.ends, a.parts, a.of.starts, a.out, a.of.rows, a.of.heads, a.of.chunks, rows}, a.of.tokens,
+    return launch_join<kC>(JoinArgs{a.partial, a.ends, a.parts, a.of.starts, a.out, a.of.rows, a.of.heads, a.of.chunks, rows, size_of(a.factor)}, a.of.tokens,
                            a.of.chunks > kManyParts * attend_tiles(a.of.tokens, a.of.rows, a.of.heads, blocks), s);
 }
 
@@ -890,11 +895,10 @@ latent_prompt_kernel(const LatentPromptArgs a)
                 float top = score[0];
 #pragma unroll
                 for (uint32_t e = 1; e < 16u; e++) top = __builtin_fmaxf(top, score[e]);
-                top *= factor;
-                if (__ballot(top > base + kLift)) {
+                if (__ballot(in_log2(top, base, factor) > kLift)) {
                     const auto both_halves = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top), false, false);
                     top = __builtin_fmaxf(base, __builtin_fmaxf(__uint_as_float(both_halves[0]), __uint_as_float(both_halves[1])));
-                    const float by = __builtin_amdgcn_exp2f(base - (top > -__builtin_inff() ? top : 0.f));
+                    const float by = __builtin_amdgcn_exp2f(in_log2(base, top > -__builtin_inff() ? top : 0.f, factor));
                     base = top; sum *= by;
 #pragma unroll
                     for (uint32_t d = 0; d < kParts; d++) acc[d] *= by;
@@ -905,7 +909,7 @@ latent_prompt_kernel(const LatentPromptArgs a)
                     Word4 w;
 #pragma unroll
                     for (uint32_t j = 0; j < 4u; j++) {
-                        const float u = __builtin_amdgcn_exp2f(__builtin_fmaf(score[8u * k + 2u * j], factor, -rel)), v = __builtin_amdgcn_exp2f(__builtin_fmaf(score[8u * k + 2u * j + 1u], factor, -rel));
+                        const float u = __builtin_amdgcn_exp2f(in_log2(score[8u * k + 2u * j], rel, factor)), v = __builtin_amdgcn_exp2f(in_log2(score[8u * k + 2u * j + 1u], rel, factor));
                         w[j] = pk_bf16(u, v);
                         sum += u; sum += v;
                     }
@@ -981,7 +985,7 @@ hipError_t launch_latent_prompt(const void *q_n, const void *q_r, const void *k_
     const dim3 grid(p.chunks ? p.chunks : (tokens / kPromptRows + rows) * heads);
     const hipError_t e = launch(dim == 128u ? latent_prompt_kernel<128> : latent_prompt_kernel<64>, grid, dim3(kThreads), 0, s, nullptr, a);
     if (e != hipSuccess || !p.chunks) return e;
-    const JoinArgs j{a.partial, a.ends, a.parts, starts, a.out, rows, heads, p.chunks, kPromptRows};
+    const JoinArgs j{a.partial, a.ends, a.parts, starts, a.out, rows, heads, p.chunks, kPromptRows, size_of(a.factor)};
     const bool many = p.chunks > kManyParts * prompt_tiles(tokens, rows, heads);
     return dim == 128u ? launch_join<128>(j, tokens, many, s) : launch_join<64>(j, tokens, many, s);
 }

@@ -721,3 +721,73 @@ def test_a_model_s_steps(bits):
             keys = slice(int(key_starts[row]), int(key_starts[row + 1]))
             want, off = attention(torch.cat((q_n[part], q2[part]), -1), torch.cat((k_n[keys], all_r[keys][:, None].expand(-1, H, -1)), -1), v[keys], seen, factor)
             assert ((out[part].double() - want).abs() <= off).all()
+
+
+# ---- values at the ends of the range ------------------------------------------------------------
+
+def one_takes_all(got, want, q, keys, winners, factor):
+    """Scores so far apart that all weight lies with one key, or with some whose scores are equal, bit for bit: then its weights are equal too, and 2^a / (n 2^a) leaves but the output's rounding and that of 1 / n.
+
+    q [n, H, A] and keys [m, A] as a kernel sees them, winners [m].  A score in fp32 is off by A * 2^-24 of the sum of its products' magnitudes; behind that 200 in log2 have to be left."""
+    s = torch.matmul(q.double(), keys.double().T.contiguous()) * (factor * math.log2(math.e))
+    size = torch.matmul(q.double().abs(), keys.double().abs().T.contiguous()).amax() * abs(factor) * math.log2(math.e)
+    best = s[..., winners]
+    assert (best == best[..., :1]).all()
+    assert (best[..., 0] - s[..., ~winners].amax(-1)).min() > 200 + 2 * q.shape[-1] * 2.0 ** -24 * size
+    assert ((got.double() - want).abs() <= 2 * HALF * want.abs()).all(), (got.double() - want).abs().max()
+
+
+@pytest.mark.parametrize("bits", [8, 16])
+@pytest.mark.parametrize("C", [256, 512])
+@pytest.mark.parametrize("H,n,columns", [(16, 100, 2), (32, 500, 8), (64, 300, 2000), (128, 200, 4), (128, 200, 2000), (16, 6000, 100), (128, 2500, 50)])
+@pytest.mark.parametrize("size,factor", [(14, 0.06), (14, -0.08), (19, 0.1), (12, 1.0)])
+def test_attend_scores_beyond_2_to_31(bits, C, H, n, columns, size, factor):
+    """Numbers of 2^12 to 2^20, and scores of up to 2^48: a key takes all the weight, or two whose scores are the same; the two lie in different parts where keys are cut."""
+    g = gen(n + size)
+    P = 64
+    sign = torch.where(torch.rand(C + E, generator=g, device="cuda") < 0.5, -1.0, 1.0)
+    heads = (1.0 + (torch.arange(H, device="cuda") * 37 % 128) / 128.0)[:, None]         # (sums of all these are whole multiples below 2^24: fp32 has them exactly)
+    q = (math.copysign(1.0, factor) * 2.0 ** size * heads * sign).to(torch.bfloat16)[None]
+    keys = torch.where(torch.rand((n, C + E), generator=g, device="cuda") < 0.5, -1.0, 1.0) * 2.0 ** size
+    a, b = n // 7, n - 3
+    by = torch.where(torch.arange(C + E, device="cuda") % 2 == 0, 3.0, 1.0)
+    keys[a], keys[b] = sign * by * 2.0 ** size, sign * by.roll(1) * 2.0 ** size
+    table, N = pages_of(g, [n], P, columns=columns)
+    i = torch.arange(n, device="cuda")
+    slots = table[0].long()[i // P] * P + i % P
+    c_cache, r_cache, scale = new_cache(g, N, P, C, bits)
+    wg.latent_append(keys[:, :C].to(torch.bfloat16), keys[:, C:].to(torch.bfloat16), slots.to(torch.int32), None, c_cache, r_cache, scale)
+    assert torch.equal(values(c_cache, scale)[slots], keys[:, :C].double())               # (1 and 3 times powers of two have a place in 8 bits)
+    work = torch.empty(max(16, wg.latent_attend_workspace(1, 1, H, C, table.shape[1], P)), dtype=torch.uint8, device="cuda")
+    out = torch.empty((1, H, C), dtype=torch.bfloat16, device="cuda")
+    for seen, winners in ((n, [a, b]), (b, [a])):
+        wg.latent_attend(q[..., :C], q[..., C:], c_cache, r_cache, scale, table, ints([seen]), ints([0, 1]), factor, out, work)
+        at = torch.zeros(seen, dtype=torch.bool, device="cuda")
+        at[winners] = True
+        one_takes_all(out, keys[:seen, :C][at].double().mean(0).expand(1, H, C), q, keys[:seen], at, factor)
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("H,n,m", [(2, 1, 100), (4, 150, 300), (8, 40, 4000), (1, 1, 9000)])
+@pytest.mark.parametrize("size,factor", [(14, 0.06), (14, -0.08), (19, 0.1), (12, 1.0)])
+def test_prompt_scores_beyond_2_to_31(D, H, n, m, size, factor):
+    g = gen(m + size)
+    sign = torch.where(torch.rand(D + E, generator=g, device="cuda") < 0.5, -1.0, 1.0)
+    tokens = (1.0 + (torch.arange(n * H, device="cuda") * 37 % 128) / 128.0).view(n, H, 1)
+    q = (math.copysign(1.0, factor) * 2.0 ** size * tokens * sign).to(torch.bfloat16)
+    keys = torch.where(torch.rand((m, D + E), generator=g, device="cuda") < 0.5, -1.0, 1.0) * 2.0 ** size
+    a, b = m // 7, m - n
+    by = torch.where(torch.arange(D + E, device="cuda") % 2 == 0, 3.0, 1.0)
+    keys[a], keys[b] = sign * by * 2.0 ** size, sign * by.roll(1) * 2.0 ** size
+    v = bf16(g, m, H, D)
+    k = keys.to(torch.bfloat16)
+    work = torch.empty(max(16, wg.latent_prompt_workspace(n, 1, H, D, m)), dtype=torch.uint8, device="cuda")
+    out = torch.empty((n, H, D), dtype=torch.bfloat16, device="cuda")
+    for winners in ([a, b], [a]):
+        if len(winners) == 1:
+            k[b] = 0
+            keys[b] = 0
+        wg.latent_prompt(q[..., :D], q[..., D:], k[:, None, :D].expand(-1, H, -1), k[:, D:], v, ints([0, n]), ints([0, m]), factor, out, work)
+        at = torch.zeros(m, dtype=torch.bool, device="cuda")
+        at[winners] = True
+        one_takes_all(out, v[at].double().mean(0).expand(n, H, D), q, keys, at, factor)       # (every token sees the winners: the second is the first token's own key)
