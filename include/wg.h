@@ -476,7 +476,7 @@ int wg_latent_read(const void *d_c_cache, const void *d_r_cache, const float *d_
  * [tokens][heads][64], both bfloat16 with strides in elements at multiples of 16 bytes; d_out bfloat16 [tokens][heads][latent] without gaps (what makes a head's values from vectors is applied to it
  * afterwards).  d_table, d_lens, d_starts, and which keys a token sees, as for wg_cache_attend: row r has d_lens[r] tokens in the cache, the tokens d_starts[r] .. d_starts[r + 1] of the
  * call being its last ones; token i of n sees the first d_lens[r] - n + i + 1 (none: its output is zeros); tokens from d_starts[rows] on belong to no row, and their outputs stay.  Products of
- * bfloat16 numbers (those in 8 bits times their scale exactly), sums and softmax in fp32 (scores of any size that this holds); weights are rounded to bfloat16, their sum is taken before.  An infinity or a NaN in a vector that a token sees makes
+ * bfloat16 numbers (those in 8 bits times their scale exactly), sums and softmax in fp32 (scores of any size that this holds); weights, 1 at the most, are rounded to bfloat16, their sum is taken before.  An infinity or a NaN in a vector that a token sees makes
  * its output NaN, in part or as a whole, and is nothing to a token that does not see it.  A page number of a row's tokens that is none reads as zeros; entries behind them may be anything.
  * d_out and d_workspace overlap no input.  d_workspace: wg_latent_attend_workspace(...) bytes (0: may be NULL), 16-byte aligned, overwritten; calls that share it must not overlap.  heads <= 4096, rows <= 65535, pages *
  * page_tokens and columns * page_tokens < 2^31, tokens * heads < 2^31, and no more than one launch holds: with n, the least of 16, 32, 64 and 128 that tokens * heads / min(rows, tokens) does not exceed, or 128,

@@ -6,9 +6,9 @@
 // m = l % 16 and g = l / 16, holds for query m the scores of keys 8 g .. 8 g + 7 of 32.  Keys lie in LDS as rows, and the second product's operand, eight keys of one dim, is read from there
 // by the transposing read: sixteen lanes that ask for four rows of sixteen numbers get a column of four each.
 //
-// The softmax is taken in one pass: weights e = 2^(score - base) relative to a base that moves only where a score is 8 above it, by their wavefront as a whole; so it
-// costs no exchange between lanes but where it moves.  Weights are rounded to bfloat16, as the values are that they multiply (values go as far as 2^127, which float16 would not hold): they
-// are off by 2^-8 at the most, as the output is by its own rounding.  Their sum, in fp32, is that of the weights before.
+// The softmax is taken in one pass: weights 2^(score - base - 8) relative to a base that moves only where a score is 8 above it, by their wavefront as a whole; so it
+// costs no exchange between lanes but where it moves, and the largest weight is 2^-8 to 1: a sum of values that 2^128 holds is not lost.  Weights are rounded to bfloat16, as the values are that they multiply (values go as far as 2^127,
+// which float16 would not hold): they are off by 2^-8 at the most, as the output is by its own rounding.  Their sum, in fp32, is that of the weights before.
 #include <hip/hip_runtime.h>
 
 #include "wg_buffer.h"
@@ -235,6 +235,8 @@ __device__ __forceinline__ float most_of_rows(float x)
 // rounded would leave the rounding's error, which from scores of 2^31 on has the largest weight 0 or infinite.  (An operation more a score: 100 rows, 128 heads 123 us for 119, drafts 89.9 for 88, prompts 142.8 for 140.8;
 // one of 16,000 tokens 1,301 for 1,289.  Left to a branch that scores below 2^10 do not take, 123, 88.4, 140 and 1,299.)
 __device__ __forceinline__ float in_log2(float score, float base, float factor) { return (score - base) * factor; }
+// (no score is more than kLift above its base: a weight is 1 at the most)
+__device__ __forceinline__ float weight_of(float score, float base, float factor) { return __builtin_amdgcn_exp2f(in_log2(score, base, factor) - kLift); }
 
 // What a wavefront holds of its 16 queries: of query m, the base and its own part of the sum, and outputs, dims 4 g .. 4 g + 3 of each of kParts.
 template <uint32_t kParts>
@@ -264,7 +266,7 @@ struct Sums {
         Word4 w;
 #pragma unroll
         for (uint32_t j = 0; j < 4u; j++) {
-            const float x = __builtin_amdgcn_exp2f(in_log2(s[2u * j], from, factor)), y = __builtin_amdgcn_exp2f(in_log2(s[2u * j + 1u], from, factor));
+            const float x = weight_of(s[2u * j], from, factor), y = weight_of(s[2u * j + 1u], from, factor);
             w[j] = pk_bf16(x, y);
             sum += x; sum += y;
         }
@@ -909,7 +911,7 @@ latent_prompt_kernel(const LatentPromptArgs a)
                     Word4 w;
 #pragma unroll
                     for (uint32_t j = 0; j < 4u; j++) {
-                        const float u = __builtin_amdgcn_exp2f(in_log2(score[8u * k + 2u * j], rel, factor)), v = __builtin_amdgcn_exp2f(in_log2(score[8u * k + 2u * j + 1u], rel, factor));
+                        const float u = weight_of(score[8u * k + 2u * j], rel, factor), v = weight_of(score[8u * k + 2u * j + 1u], rel, factor);
                         w[j] = pk_bf16(u, v);
                         sum += u; sum += v;
                     }

@@ -791,3 +791,52 @@ def test_prompt_scores_beyond_2_to_31(D, H, n, m, size, factor):
         at = torch.zeros(m, dtype=torch.bool, device="cuda")
         at[winners] = True
         one_takes_all(out, v[at].double().mean(0).expand(n, H, D), q, keys, at, factor)       # (every token sees the winners: the second is the first token's own key)
+
+
+def levels(n, first, last, size):
+    """Keys [n] whose scores are 0, and 7.75 in log2 for one behind the first 64 of every 128; values of about 2^size there, and none elsewhere.  (A softmax whose base is the first scores' may not weigh the later ones with 2^7.75.)"""
+    i = torch.arange(n, device="cuda")
+    late = i % 128 == 100
+    v = torch.where(late, 1.0 + (i * 37 % 128) / 128.0, 0.0) * 2.0 ** size
+    return torch.where(late, last, first), v
+
+
+@pytest.mark.parametrize("bits", [8, 16])
+@pytest.mark.parametrize("C", [256, 512])
+@pytest.mark.parametrize("H,n,columns", [(16, 120, 2), (32, 120, 2), (64, 120, 2), (128, 250, 4), (64, 250, 2000), (16, 3000, 50), (128, 2500, 50), (32, 4000, 2000)])
+@pytest.mark.parametrize("size", [120, -122])
+def test_attend_values_near_the_ends_of_the_range(bits, C, H, n, columns, size):
+    """2^120 to 2^121: the largest weight times it is beyond 2^128 if a weight may be 2^7.75; up to 32 of them with weights of 1 at the most are not."""
+    g = gen(n)
+    P = 64
+    level, v = levels(n, 0.0, 7.75, size)
+    table, N = pages_of(g, [n], P, columns=columns)
+    i = torch.arange(n, device="cuda")
+    slots = table[0].long()[i // P] * P + i % P
+    c_cache, r_cache, scale = new_cache(g, N, P, C, bits)
+    c, r = torch.zeros((n, C), device="cuda"), torch.zeros((n, E), device="cuda")
+    c[:, ::3], r[:, 5] = v[:, None], level
+    wg.latent_append(c.to(torch.bfloat16), r.to(torch.bfloat16), slots.to(torch.int32), None, c_cache, r_cache, scale)
+    q_c, q_r = torch.zeros((1, H, C), dtype=torch.bfloat16, device="cuda"), torch.zeros((1, H, E), dtype=torch.bfloat16, device="cuda")
+    q_r[..., 5] = 1.0
+    out, work = torch.empty_like(q_c), torch.empty(max(16, wg.latent_attend_workspace(1, 1, H, C, table.shape[1], P)), dtype=torch.uint8, device="cuda")
+    wg.latent_attend(q_c, q_r, c_cache, r_cache, scale, table, ints([n]), ints([0, 1]), math.log(2.0), out, work)
+    held_c, held_r = values(c_cache, scale)[slots], r_cache.view(-1, E)[slots].double()
+    want, off = attention(torch.cat((q_c, q_r), -1), torch.cat((held_c, held_r), -1)[:, None], held_c[:, None], torch.tensor([n], device="cuda"), math.log(2.0))
+    assert ((out.double() - want).abs() <= off).all(), (out.double() - want).abs().max()
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("H,n,m", [(2, 1, 120), (4, 150, 300), (8, 40, 4000), (1, 1, 4000)])
+@pytest.mark.parametrize("size", [120, -122])
+def test_prompt_values_near_the_ends_of_the_range(D, H, n, m, size):
+    level, of = levels(m, 0.0, 7.75, size)
+    q_n, q_r = torch.zeros((n, H, D), dtype=torch.bfloat16, device="cuda"), torch.zeros((n, H, E), dtype=torch.bfloat16, device="cuda")
+    k_n, k_r = bf16(gen(m), m, H, D), torch.zeros((m, E), dtype=torch.bfloat16, device="cuda")
+    q_r[..., 5], k_r[:, 5] = 1.0, level.to(torch.bfloat16)
+    v = of[:, None, None].expand(-1, H, D).to(torch.bfloat16)
+    out, work = torch.empty_like(q_n), torch.empty(max(16, wg.latent_prompt_workspace(n, 1, H, D, m)), dtype=torch.uint8, device="cuda")
+    wg.latent_prompt(q_n, q_r, k_n, k_r, v, ints([0, n]), ints([0, m]), math.log(2.0), out, work)
+    k = torch.cat((k_n, k_r[:, None].expand(-1, H, -1)), -1)
+    want, off = attention(torch.cat((q_n, q_r), -1), k, v, m - n + 1 + torch.arange(n, device="cuda"), math.log(2.0))
+    assert ((out.double() - want).abs() <= off).all(), (out.double() - want).abs().max()
