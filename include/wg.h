@@ -486,7 +486,7 @@ int wg_latent_read(const void *d_c_cache, const void *d_r_cache, const float *d_
  * many tokens see the same keys.  d_q_n [tokens][heads][dim] and d_q_r [tokens][heads][64] are the two parts of the queries, d_k_n and d_v [keys][heads][dim] the keys' own part and the values, d_k_r [keys][64] the shared part; bfloat16, strides in
  * elements at multiples of 16 bytes, keys and values less than 2^24 elements from one token to the next; dim is 64 or 128.  Row r has the queries d_starts[r] .. d_starts[r + 1] and the keys d_key_starts[r] .. d_key_starts[r + 1], its queries being the last of them: query i of n sees
  * the first m - n + i + 1 of its m keys (none: zeros); tokens from d_starts[rows] on belong to no row, and their outputs stay.  d_out bfloat16 [tokens][heads][dim] without gaps.  Rounding as above; an infinity or a NaN in a value that a
- * token sees makes that output infinite or NaN and is nothing to a token that does not see it.  Both starts do not descend.  d_workspace: wg_latent_prompt_workspace(...) bytes,
+ * token sees, whatever its weight, makes that output infinite or NaN and is nothing to a token that does not see it.  Both starts do not descend.  d_workspace: wg_latent_prompt_workspace(...) bytes,
  * as above.  heads <= 4096, rows <= 65535, tokens and keys < 2^31, tokens * heads < 2^31, (tokens / 128 + rows) * heads < 2^24.  One or two kernels. */
 uint64_t wg_latent_attend_workspace(uint32_t tokens, uint32_t rows, uint32_t heads, uint32_t latent, uint32_t columns, uint32_t page_tokens);
 int wg_latent_attend(const void *d_q_c, const void *d_q_r, uint32_t tokens, uint32_t heads, uint32_t latent, int64_t c_token_stride, int64_t c_head_stride, int64_t r_token_stride,

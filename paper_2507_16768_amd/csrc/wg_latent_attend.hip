@@ -622,7 +622,7 @@ latent_join_kernel(const JoinArgs a)
 #pragma unroll
             for (uint32_t k = 0; k < kRound; k++) {
                 const float wk = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(w), k0 + k < 64u ? k0 + k : 63u));
-                if (k0 + k >= more || wk == 0.f) continue;                 // (a part that weighs nothing may be anything)
+                if (k0 + k >= more) continue;                              // (one that weighs nothing counts: it is none where a value that is none has been weighed with 0)
 #pragma unroll
                 for (uint32_t d = 0; d < kOwn; d++) acc[d] += wk * v[k][d];
             }

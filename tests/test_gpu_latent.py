@@ -840,3 +840,52 @@ def test_prompt_values_near_the_ends_of_the_range(D, H, n, m, size):
     k = torch.cat((k_n, k_r[:, None].expand(-1, H, -1)), -1)
     want, off = attention(torch.cat((q_n, q_r), -1), k, v, m - n + 1 + torch.arange(n, device="cuda"), math.log(2.0))
     assert ((out.double() - want).abs() <= off).all(), (out.double() - want).abs().max()
+
+
+@pytest.mark.parametrize("bad", [NAN, INF, -INF])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("H,n,m", [(2, 100, 200), (8, 40, 4000), (1, 1, 9000), (16, 131, 2500)])
+def test_prompt_values_that_are_none_where_weights_vanish(bad, D, H, n, m):
+    """A value that is none times a weight of 0 is none, also where keys are cut and all of a part's weights vanish beside those of another."""
+    g = gen(m)
+    u = torch.where(torch.rand(D, generator=g, device="cuda") < 0.5, -1.0, 1.0)
+    q_n, q_r = u.to(torch.bfloat16).expand(n, H, D).contiguous(), bf16(g, n, H, E)
+    k_n, k_r, v = torch.zeros((m, H, D), dtype=torch.bfloat16, device="cuda"), torch.zeros((m, E), dtype=torch.bfloat16, device="cuda"), bf16(g, m, H, D)
+    k_n[m // 2:] = (u * 4.0).to(torch.bfloat16)                # scores of 4 D, which is 369 in log2 and more
+    fine = v.clone()
+    v[m // 50, :, 7], fine[m // 50, :, 7] = bad, 0.0
+    out, work = torch.empty_like(q_n), torch.empty(max(16, wg.latent_prompt_workspace(n, 1, H, D, m)), dtype=torch.uint8, device="cuda")
+    wg.latent_prompt(q_n, q_r, k_n, k_r, v, ints([0, n]), ints([0, m]), 1.0, out, work)
+    want, off = attention(torch.cat((q_n, q_r), -1), torch.cat((k_n, k_r[:, None].expand(-1, H, -1)), -1), fine, m - n + 1 + torch.arange(n, device="cuda"), 1.0)
+    close = (out.double() - want).abs() <= off
+    assert not out[..., 7].isfinite().any()
+    close[..., 7] = True
+    assert close.all()
+
+
+@pytest.mark.parametrize("bad", [NAN, INF, -INF])
+@pytest.mark.parametrize("C", [256, 512])
+@pytest.mark.parametrize("H,n,columns", [(16, 200, 4), (16, 3000, 50), (128, 2500, 50), (32, 30000, 500), (64, 250, 2000)])
+def test_attend_numbers_that_are_none_where_weights_vanish(bad, C, H, n, columns):
+    """An infinity that makes its key's score -inf, among keys whose scores are far below the others'."""
+    g = gen(n)
+    P = 64
+    table, N = pages_of(g, [n], P, columns=columns)
+    i = torch.arange(n, device="cuda")
+    slots = table[0].long()[i // P] * P + i % P
+    c_cache, r_cache, _ = new_cache(g, N, P, C, 16)
+    c, r = bf16(g, n, C), torch.zeros((n, E), dtype=torch.bfloat16, device="cuda")
+    c[:, 5], r[n // 2:] = 0.0, 8.0
+    c[n // 50, 5] = bad
+    wg.latent_append(c, r, slots.to(torch.int32), None, c_cache, r_cache, None)
+    q_c, q_r = torch.zeros((1, H, C), dtype=torch.bfloat16, device="cuda"), torch.ones((1, H, E), dtype=torch.bfloat16, device="cuda")
+    q_c[..., 5] = 1.0 if bad < 0 else -1.0
+    out, work = torch.empty_like(q_c), torch.empty(max(16, wg.latent_attend_workspace(1, 1, H, C, table.shape[1], P)), dtype=torch.uint8, device="cuda")
+    wg.latent_attend(q_c, q_r, c_cache, r_cache, None, table, ints([n]), ints([0, 1]), 1.0, out, work)
+    assert not out[..., 5].isfinite().any()
+    c[n // 50, 5] = 0.0
+    others = torch.arange(n, device="cuda") != n // 50
+    want, off = attention(torch.cat((q_c, q_r), -1), torch.cat((c, r), -1)[:, None][others], c[:, None][others], torch.tensor([n - 1], device="cuda"), 1.0)
+    close = (out.double() - want).abs() <= off
+    close[..., 5] = True
+    assert (close | out.isnan()).all()
