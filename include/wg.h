@@ -461,11 +461,11 @@ int wg_rotary_frequencies(double *host_out, uint32_t rotated, double base, doubl
  * wg_latent_append: token t's vector and shared key (bfloat16, strides of tokens in elements, at multiples of 16 bytes) go to slot d_slots[t]; a slot outside [0, pages * page_tokens)
  * takes none; no slot is given twice.  In 8 bits a token's scale is the least power of two, 2^-64 at least, times which 448 reaches the vector's largest finite magnitude; numbers are rounded to
  * nearest, ties to even, infinities become 448 times the scale, NaN stays.  (What reads the cache takes scales for powers of two.)  d_origins (may be NULL), as wg_page_step leaves them: where d_origins[t] is a page, the tokens in front of token t's
- * slot in its page come from the same places of that one; no token of the call goes to that page, or in front of token t in its own.  tokens <= 2^27, pages * page_tokens < 2^31.  One kernel.
+ * slot in its page come from the same places of that one; no token of the call goes to that page, or in front of token t in its own.  tokens <= 2^27, in 8 bits 2^26 - 4; pages * page_tokens < 2^31.  One kernel.
  *
  * wg_latent_read: the first d_starts[r + 1] - d_starts[r] cached tokens of row r of d_table, in bfloat16, into rows d_starts[r] .. of d_c_out and d_r_out (strides in elements, at multiples of
  * 16 bytes): what prompts behind a cached prefix expand into keys and values (numbers in 8 bits times their scale, which is exact; above what bfloat16 holds, an infinity).  d_starts does not descend; rows from d_starts[rows] on stay, and so do
- * those in front of d_starts[0].  A token whose page is no page or lies behind the table reads as zeros.  tokens: rows that d_c_out has, <= 2^29.  rows <= 65535.  One kernel. */
+ * those in front of d_starts[0].  A token whose page is no page or lies behind the table reads as zeros.  tokens: rows that d_c_out has, <= 2^28 - 16.  rows <= 65535.  One kernel. */
 int wg_latent_append(const void *d_c, const void *d_r, uint32_t tokens, uint32_t latent, int64_t c_token_stride, int64_t r_token_stride, const int32_t *d_slots,
                      const int32_t *d_origins, void *d_c_cache, void *d_r_cache, float *d_c_scale, uint32_t pages, uint32_t page_tokens, void *stream);
 int wg_latent_read(const void *d_c_cache, const void *d_r_cache, const float *d_c_scale, uint32_t latent, uint32_t pages, uint32_t page_tokens, const int32_t *d_table,

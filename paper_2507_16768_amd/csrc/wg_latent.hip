@@ -84,14 +84,20 @@ latent_append_kernel(const LatentAppendArgs a)
     }
 }
 
+constexpr uint32_t kMostGroups = 0xFFFFFFFFu / kLatentThreads;              // workgroups of a launch
+static uint32_t groups_of(uint32_t tokens, uint32_t per) { return (uint32_t)(((uint64_t)tokens + per - 1u) / per); }
+static bool many_tokens(uint32_t tokens, bool bytes) { return !bytes && tokens > 16384u; }
+static uint32_t tokens_of_workgroup(uint32_t tokens, bool bytes) { return tokens <= 1024u ? 1u : kLatentWaves * (many_tokens(tokens, bytes) ? 4u : 1u); }
+bool latent_append_fits(uint32_t tokens, bool bytes) { return groups_of(tokens, tokens_of_workgroup(tokens, bytes)) <= kMostGroups; }
+
 hipError_t launch_latent_append(const void *c, const void *r, uint32_t tokens, uint32_t latent, int64_t c_token, int64_t r_token, const int32_t *slots, const int32_t *origins,
                                 void *c_cache, void *r_cache, float *scale, uint32_t pages, uint32_t shift, hipStream_t s)
 {
-    const bool many = !scale && tokens > 16384u;
-    const uint32_t per = tokens <= 1024u ? 1u : kLatentWaves * (many ? 4u : 1u);
+    const bool many = many_tokens(tokens, scale != nullptr);
+    const uint32_t per = tokens_of_workgroup(tokens, scale != nullptr);
     const LatentAppendArgs a{static_cast<const uint16_t *>(c), static_cast<const uint16_t *>(r), c_token, r_token, slots, origins, static_cast<uint8_t *>(c_cache),
                              static_cast<uint16_t *>(r_cache), scale, tokens, pages, shift, per};
-    const dim3 grid((tokens + per - 1u) / per), block(kLatentThreads);
+    const dim3 grid(groups_of(tokens, per)), block(kLatentThreads);
     if (many) return launch(latent == 512u ? latent_append_kernel<512, false, 4> : latent_append_kernel<256, false, 4>, grid, block, 0, s, nullptr, a);
     return launch(latent == 512u ? (scale ? latent_append_kernel<512, true, 1> : latent_append_kernel<512, false, 1>) : scale ? latent_append_kernel<256, true, 1> : latent_append_kernel<256, false, 1>,
                   grid, block, 0, s, nullptr, a);
@@ -169,12 +175,14 @@ latent_read_kernel(const LatentReadArgs a)
     }
 }
 
+bool latent_read_fits(uint32_t tokens) { return groups_of(tokens, kLatentWaves * kReadTokens) <= kMostGroups; }
+
 hipError_t launch_latent_read(const void *c_cache, const void *r_cache, const float *scale, uint32_t latent, uint32_t pages, uint32_t shift, const int32_t *table, uint32_t rows,
                               uint32_t columns, const int32_t *starts, uint32_t tokens, void *c_out, int64_t c_token, void *r_out, int64_t r_token, hipStream_t s)
 {
     const LatentReadArgs a{static_cast<const uint8_t *>(c_cache), static_cast<const uint16_t *>(r_cache), scale, table, starts, static_cast<uint16_t *>(c_out),
                            static_cast<uint16_t *>(r_out), c_token, r_token, rows, columns, tokens, pages, shift};
-    const dim3 grid((tokens + kLatentWaves * kReadTokens - 1u) / (kLatentWaves * kReadTokens)), block(kLatentThreads);
+    const dim3 grid(groups_of(tokens, kLatentWaves * kReadTokens)), block(kLatentThreads);
     return launch(latent == 512u ? (scale ? latent_read_kernel<512, true> : latent_read_kernel<512, false>) : scale ? latent_read_kernel<256, true> : latent_read_kernel<256, false>,
                   grid, block, 0, s, nullptr, a);
 }

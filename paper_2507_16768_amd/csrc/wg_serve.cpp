@@ -208,7 +208,7 @@ int wg_latent_append(const void *d_c, const void *d_r, uint32_t tokens, uint32_t
     return entry("wg_latent_append", [&](const char **why) {
         WG_WANT(d_c && d_r && d_slots && d_c_cache && d_r_cache, "null argument");
         WG_WANT(tokens && pages, "no tokens or pages");
-        WG_WANT(tokens <= 1u << 27, "tokens above 2^27");
+        WG_WANT(tokens <= 1u << 27 && latent_append_fits(tokens, d_c_scale != nullptr), "tokens above 2^27, or, in 8 bits, 2^26 - 4");
         WG_WANT(latent_ok(latent), "latent must be 256 or 512");
         WG_WANT(shift_of(page_tokens), "page_tokens must be 16, 32 or 64");
         WG_WANT((uint64_t)pages * page_tokens <= 0x7FFFFFFFull, "slots above 2^31 - 1");
@@ -224,7 +224,7 @@ int wg_latent_read(const void *d_c_cache, const void *d_r_cache, const float *d_
     return entry("wg_latent_read", [&](const char **why) {
         WG_WANT(d_c_cache && d_r_cache && d_table && d_starts && d_c_out && d_r_out, "null argument");
         WG_WANT(tokens && rows && columns && pages, "no tokens, rows, columns or pages");
-        WG_WANT(tokens <= 1u << 29 && rows <= kMostRows, "tokens above 2^29 or rows above 65535");
+        WG_WANT(latent_read_fits(tokens) && rows <= kMostRows, "tokens above 2^28 - 16 or rows above 65535");
         WG_WANT(latent_ok(latent), "latent must be 256 or 512");
         WG_WANT(shift_of(page_tokens), "page_tokens must be 16, 32 or 64");
         WG_WANT((uint64_t)columns * page_tokens <= 0x7FFFFFFFull && (uint64_t)pages * page_tokens <= 0x7FFFFFFFull, "tokens above 2^31 - 1");

@@ -37,6 +37,9 @@ hipError_t launch_rotate(const void *q, const void *k, int dtype, uint32_t token
                          const int64_t (&strides)[8], const int32_t *positions, const double *frequencies, float magnitude, void *q_out, void *k_out, hipStream_t s);
 
 constexpr uint32_t kLatentKey = 64;          // numbers of a shared key
+// Whether a launch (fewer than 2^32 threads) holds so many tokens.
+bool latent_append_fits(uint32_t tokens, bool bytes);
+bool latent_read_fits(uint32_t tokens);
 hipError_t launch_latent_append(const void *c, const void *r, uint32_t tokens, uint32_t latent, int64_t c_token, int64_t r_token, const int32_t *slots, const int32_t *origins,
                                 void *c_cache, void *r_cache, float *scale, uint32_t pages, uint32_t shift, hipStream_t s);
 hipError_t launch_latent_read(const void *c_cache, const void *r_cache, const float *scale, uint32_t latent, uint32_t pages, uint32_t shift, const int32_t *table, uint32_t rows,

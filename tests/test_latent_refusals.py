@@ -89,3 +89,11 @@ def test_frequencies():
                 dict(factor=2.0, original=4096, low=-1), dict(factor=2.0, original=4096, low=0, log_ramp=True), dict(factor=2.0, original=math.inf)):
         with pytest.raises(wg.WgError):
             wg.rotary_frequencies(**dict(dict(rotated=64), **bad))
+
+
+def test_calls_that_no_launch_holds():
+    """A launch has fewer than 2^32 threads: 2^24 - 1 workgroups of 256, of four tokens each in 8 bits (sixteen in 16, which other limits end), or of sixteen that are read."""
+    append = dict(c=P, r=P, tokens=4, latent=512, c0=576, r0=576, slots=P, origins=P, c_cache=Q, r_cache=Q, scale=Q, pages=10, page_tokens=16, stream=None)
+    refused("wg_latent_append", append, [dict(tokens=n, latent=latent) for n in ((1 << 26) - 3, 1 << 26, (1 << 26) + 1, 1 << 27) for latent in (256, 512)] + [dict(scale=None, tokens=(1 << 27) + 1)])
+    read = dict(c_cache=P, r_cache=P, scale=P, latent=256, pages=10, page_tokens=32, table=P, rows=3, columns=5, starts=P, tokens=100, c_out=Q, c0=256, r_out=Q, r0=64, stream=None)
+    refused("wg_latent_read", read, [dict(tokens=n, scale=scale) for n in ((1 << 28) - 15, 1 << 28, (1 << 28) + 1, 1 << 29) for scale in (P, None)])
