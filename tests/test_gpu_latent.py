@@ -889,3 +889,42 @@ def test_attend_numbers_that_are_none_where_weights_vanish(bad, C, H, n, columns
     close = (out.double() - want).abs() <= off
     close[..., 5] = True
     assert (close | out.isnan()).all()
+
+
+@pytest.mark.parametrize("bits", [8, 16])
+@pytest.mark.parametrize("C", [256, 512])
+@pytest.mark.parametrize("T", [1023, 1024, 1025, 16384, 16385, 16391])
+def test_append_many(bits, C, T):
+    """On both sides of where workgroups take more tokens, wavefronts and workgroups that are not full; slots that are none inside a wavefront's tokens, and several tokens of a workgroup whose pages have begun in others."""
+    g = gen(T + C)
+    P, forks = 32, 60
+    N = 2 * (T // P + 1) + forks + 3
+    c_cache, r_cache, scale = new_cache(g, N, P, C, bits)
+    both = (torch.randn((T, C + E), generator=g, device="cuda") * torch.exp2(20 * torch.rand((T, 1), generator=g, device="cuda") - 10)).to(torch.bfloat16)
+    c, r = both[:, :C], both[:, C:]
+    pages = torch.randperm(N, generator=g, device="cuda")
+    origin_pages, fork_pages, other = pages[:2], pages[2:2 + forks], pages[2 + forks:]
+    slots = (other[:T // P + 1, None] * P + torch.arange(P, device="cuda")).view(-1)[torch.randperm(T // P * P + P, generator=g, device="cuda")[:T]]
+    origins = torch.full((T,), -1, device="cuda")
+    # tokens that take a begun page along: some behind one another, the call's last ones, and some with a slot or an origin that is none
+    at = torch.cat((torch.arange(5, 12), torch.arange(0, 40 * 13, 13) + 100, torch.arange(T - 13, T))).to("cuda")
+    assert at.numel() == forks and at.unique().numel() == forks
+    places = torch.arange(forks, device="cuda") * 7 % P
+    slots[at], origins[at] = fork_pages * P + places, origin_pages[torch.arange(forks, device="cuda") % 2]
+    origins[at[::9]] = N
+    none = torch.tensor([0, 2, 7, 17, 33, 34, 35, 37, 113, T - 2], device="cuda")
+    slots[none] = torch.tensor([-1, N * P, -2 ** 31, 2 ** 31 - 1, -1, -1, -1, N * P + 5, -3, N * P], device="cuda")
+    v, s = held(c)
+    caches = [c_cache.view(torch.uint8) if bits == 8 else c_cache, r_cache] + ([scale] if bits == 8 else [])
+    new = [v.float().to(torch.float8_e4m3fn).view(torch.uint8) if bits == 8 else c, r, s.float()]
+    want = [x.clone() for x in caches]
+    ok = (slots >= 0) & (slots < N * P)
+    for w, x in zip(want, new):
+        for t in at.tolist():
+            if ok[t] and 0 <= origins[t] < N:
+                page, o = divmod(int(slots[t]), P)
+                w[page, :o] = w[int(origins[t]), :o].clone()
+        w.view(-1, *w.shape[2:])[slots[ok]] = x[ok]
+    wg.latent_append(c, r, slots.to(torch.int32), origins.to(torch.int32), c_cache, r_cache, scale)
+    for w, x in zip(want, caches):
+        assert same(x, w)
