@@ -12,9 +12,9 @@ constexpr uint32_t kLatentThreads = 256, kLatentWaves = 4, kNoToken = 0xFFFFFFFF
 
 // ---------------------------------------------------------------------------------------------
 // append.  A wavefront for each token, or, of many in 16 bits, for four, all asked for at once (20,000 of 512 numbers 9.2 us for 10.6; in 8 bits 11.1 for 10.3).  A token has a scale of its own, so nothing that is in the
-// cache is rounded again; what comes along from another page is copied as it is, by all wavefronts of the workgroup (63 tokens of 644 bytes at the most).  Up to 1,024 tokens a workgroup has one, so that such
-// copies go side by side (256 rows, four beams each: 5.0 us, with four tokens to a workgroup 8.5; 2,048 rows 14.6 and 12.8).  Bound by memory: 16 prompts, 21,000 tokens in 8 bits, 9.8 us, 4.4 TB/s; a token for
-// each of 256 rows 4.8 us, of which 3 are a launch's.
+// cache is rounded again; what comes along from another page is copied as it is, by all wavefronts of the workgroup (63 tokens at the most, of 644 bytes in 8 bits and 1,152 in 16, with 512 numbers).  Up to 1,024 tokens a workgroup has
+// one, so that such copies go side by side (pages of 64, four beams to a request, 8 and 16 bits: 256 rows 4.8 us and 7.7, with four tokens to a workgroup 8.2 and 10.2; 1,024 rows 9.0 and 12.8, with four 11.2 and 15.0; 2,048 rows in 8 bits 14.6, with four 12.8).
+// Bound by memory: 16 prompts, 21,000 tokens in 8 bits, 9.8 us, 4.4 TB/s; a token for each of 256 rows 4.8 us, of which 3 are a launch's.
 struct LatentAppendArgs {
     const uint16_t *c, *r;
     int64_t c_token, r_token;                        // strides, elements

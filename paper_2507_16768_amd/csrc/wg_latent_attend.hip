@@ -288,10 +288,10 @@ constexpr float kEmpty = -1.f;                       // the sum of a share in wh
 // Attention over the cached vectors.  A workgroup's eight wavefronts are kGroups groups of 16 query rows (tokens times heads), times kCols groups of the vectors' columns (which make
 // the scores between them), times groups of 32 keys.  A block's keys go through LDS: from memory into registers, while the block before is worked on, and turned into bfloat16 (exactly) on the way.
 //
-// What bounds it.  100 rows of 1,000 to 4,000 tokens, 128 heads, bfloat16: 118 to 122 us, 590 to 614 TFLOP/s, an eighth of it joining.  Over its keys, 295 MB, it goes at 5.2 TB/s, what a copy reaches, 57 us; the
-// rest is that 256 workgroups, one on each compute unit, ask for 147 KB of queries for each of the two tiles or so that they have a part of, and store 256 KB for each part.  64 rows' 4 drafts, 16 heads, 8 bits: 88 us,
-// 6 of it joining (2.4 TB/s, 273 TFLOP/s): a block of 32 keys takes 3,900 cycles, of which the products are 1,100; the others are what comes one after the other in a block, the scores' exchange, the softmax, the keys to LDS.  One
-// row of 30,000, 16 heads, 8 bits: 22 us, 6 of it joining, a workgroup having one block of 128 keys: latencies, one behind the other, of lengths, page numbers, keys and stores.
+// What bounds it.  100 rows of 1,000 to 4,000 tokens, 128 heads, bfloat16: 119 to 124 us, 580 to 605 TFLOP/s, an eighth of it joining.  Over its keys, 295 MB, it goes at 5.2 TB/s, what a copy reaches, 57 us; the
+// rest is that 256 workgroups, one on each compute unit, ask for 147 KB of queries for each of the two tiles or so that they have a part of, and store 256 KB for each part.  64 rows' 4 drafts, 16 heads, 8 bits: 89 to 90 us,
+// 6 of it joining (2.4 TB/s, 270 TFLOP/s): a block of 32 keys takes 3,900 cycles, of which the products are 1,100; the others are what comes one after the other in a block, the scores' exchange, the softmax, the keys to LDS.  One
+// row of 30,000, 16 heads, 8 bits: 21.4 us, 6 of it joining, a workgroup having one block of 128 keys: latencies, one behind the other, of lengths, page numbers, keys and stores.
 // Tried, and no faster: the keys' way to LDS beside the second product (124 us for 121; 172 with branches, whose waits are for everything), all queries asked for before one is used (123 for 123), two blocks of
 // keys asked for at first (122 for 122), slots found before the keys go to LDS (no difference), values asked for before the softmax; 32 query rows to a wavefront (its 256 accumulators leave no registers to scale them in).
 struct LatentAttendArgs {
@@ -749,7 +749,8 @@ hipError_t launch_latent_attend(const void *q_c, const void *q_r, uint32_t token
 // operands out of LDS serve twice as many queries as those of 16 by 16: 138 us for 158); keys and values go through LDS 32 at a time, two workgroups on a compute unit (211 us with one).  Tiles of many tokens are
 // left to the chip, the last of a row first.
 //
-// What bounds it.  Four prompts of 800 to 2,000 tokens, 32 heads of 128: 134 to 145 us, 670 to 727 TFLOP/s (one of 16,000, 16 heads: 981; a large matrix product reaches 1,222).  Left out, the softmax's arithmetic would save
+// What bounds it.  Four prompts of 800 to 2,000 tokens, 32 heads of 128: 134 to 143 us, 680 to 723 TFLOP/s (one of 16,000, 16 heads: 1,010 to 1,050; a large matrix product reaches 1,222; with heads of 64 numbers 94 us, 620); two of 600 to 1,500 with
+// 128 heads 190 us, 679.  Left out, the softmax's arithmetic would save
 // 18 us of it, the second product 26, the keys' way from memory 12: no part bounds it alone.  131 queries behind 9,000 keys, 16 heads: 41 us, 1.9 TB/s; its 32 tiles are cut, and what the parts cost adds.
 // Tried, and no faster: 256 tokens to a workgroup (143 us for 135; 131 queries behind 9,000 keys 37 for 41), one block's softmax under the next one's products with three blocks in LDS (143 us for 143), tiles in order of their keys over all rows (146 for 146), 16 rows to a wavefront and four of
 // them to a SIMD (158).
@@ -970,7 +971,9 @@ static uint64_t prompt_tiles(uint32_t tokens, uint32_t rows, uint32_t heads) { r
 static Plan prompt_plan(uint32_t tokens, uint32_t rows, uint32_t heads, uint32_t dim, uint32_t keys)
 {
     const uint64_t tiles = prompt_tiles(tokens, rows, heads), blocks = ((uint64_t)keys + kAttendBlock - 1u) / kAttendBlock;
-    // (keys of all rows: where there are not many, rows are taken to have as many each)
+    // Keys are known for all rows together.  Up to 12 blocks of 128 rows are taken to have as many each, and are left whole where that is few; above, one of them may have them all, and what is left whole would be long.  16 heads, us
+    // left whole and cut: rows that are alike, 4 of 384 tokens 20 and 29, 5 of 384 23 and 31, 8 of 200 16 and 25; one row with nearly all keys, 128 tokens behind 1,500 51 and 20, behind 2,500 80 and 22, behind 4,000 124 and 26.  So
+    // prompts that are alike, and a few too many for the 12 blocks, pay for those that are not.
     return plan_of(tiles, blocks, blocks <= 12u ? (blocks + rows - 1u) / rows : blocks, rows, tokens <= kPromptRows * rows, true, kPromptRows, dim, kPromptSlots, (uint64_t)tokens * heads);
 }
 uint64_t latent_prompt_bytes(uint32_t tokens, uint32_t rows, uint32_t heads, uint32_t dim, uint32_t keys) { return plan_bytes(prompt_plan(tokens, rows, heads, dim, keys)); }

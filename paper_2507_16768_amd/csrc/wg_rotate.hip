@@ -78,7 +78,7 @@ template <> struct Numbers<float, 1> {
 
 // A workgroup makes the sines and cosines of a few tokens once, in LDS, and turns the numbers of all heads with them (heads are dealt out to more workgroups where there
 // are few tokens).  A unit is what a thread takes at once: two pieces of up to 16 bytes that are turned together (kBeside: one piece of neighbouring pairs), or, behind the pairs, one that is
-// copied.  Bound by memory: 7,001 tokens, 48 heads of 128 in bfloat16, half of each turned, 27.5 us, 6.2 TB/s (some of it does not leave the last cache); a token alone 3 to 4 us, a launch's time.
+// copied.  Bound by memory: 7,001 tokens, 48 heads of 128 in bfloat16, half of each turned, 27.5 us, 6.2 TB/s (some of it does not leave the last cache); in fp32 69 us, 5.0 TB/s; a token alone 3 to 4 us, a launch's time.
 template <typename T, uint32_t kN, bool kBeside>
 __global__ void __launch_bounds__(kRotateThreads)
 rotate_kernel(const RotateArgs a)
@@ -149,7 +149,8 @@ hipError_t launch_rotate(const void *q, const void *k, int dtype, uint32_t token
     RotateArgs a{{q, k}, {q_out, k_out}, {strides[0], strides[2]}, {strides[1], strides[3]}, {strides[4], strides[6]}, {strides[5], strides[7]},
                  positions, frequencies, magnitude, tokens, {q_heads, k_heads}, dim, rotated / 2u, 0, 0, 0};
     const bool f32 = dtype == WG_F32;
-    // by 16, 8 or 4 bytes, as all pieces lie at multiples of them (20,000 tokens of 20 heads of 80 numbers, 20 of them turned, by 4 bytes: 45 us; by single numbers 110)
+    // by 16, 8 or 4 bytes, as all pieces lie at multiples of them (20,000 tokens of 20 heads of 80 numbers, 20 of them turned, by 4 bytes: 45 us, 2.9 TB/s, a thread
+    // asking for 16 bytes at once where it asks for 64 by pieces of 16; by single numbers 110)
     auto lies = [&](uint32_t n) {
         bool fits = dim % n == 0 && (interleaved ? rotated % n == 0 : a.pairs % n == 0);
         for (const int64_t stride : strides) fits = fits && stride % n == 0;
